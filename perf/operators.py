@@ -335,30 +335,46 @@ def _plain_step(s):
         s["v"].copy_(v)
 
 
+def _kept(s):
+    """What a program keeps between its calls: the plan's and the adapters' descriptors (addresses and sizes, nothing computed), workspaces, outputs."""
+    import paper_2605_26660_amd as wq
+
+    if "kept" not in s:
+        c = s["case"]
+        if c["op"] == "adamw":
+            t = s["lists"]
+            s["kept"] = wq.AdamwItems(t["p"], t["g"], t["m"], t["v"], t.get("m_scale"), t.get("v_scale"), t.get("copy"))
+        else:
+            T, n, r = c["tokens"], c["adapters"], c["rank"]
+            packed = wq.Packed(s["W"], c["G"], c["unit_rows"], s["action"], s["code_off"], s["codes"], s["scale"], s["offset"])
+            adapters = wq.Adapters(s["a"], s["b"], s["alpha"], s["rank"]) if n else None
+            ws = wq.project_workspace(packed, s["X"], adapters, grad=c["op"] == "grad")
+            if c["op"] == "project":
+                outs = (torch.empty(T, c["rows"], dtype=s["X"].dtype, device=DEV), torch.empty(T, r, device=DEV) if n else None)
+            else:
+                outs = (torch.empty_like(s["X"]), torch.empty(n, r, c["cols"], device=DEV), torch.empty(n, c["rows"], r, device=DEV))
+            s["kept"] = packed, adapters, ws, outs
+    return wq, s["kept"]
+
+
 def run(s):
     c = s["case"]
     if c["op"] == "adamw":
         if own:
-            import paper_2605_26660_amd as wq
-
-            t = s["lists"]
-            wq.windq_adamw(t["p"], t["g"], t["m"], t["v"], s["step"], s["lr"], 0.9, 0.999, 1e-8, c["decay"],
-                           m_scales=t.get("m_scale"), v_scales=t.get("v_scale"), copies=t.get("copy"), grad_scale=s["clip"])
+            wq, items = _kept(s)
+            wq.windq_adamw(items, s["step"], s["lr"], 0.9, 0.999, 1e-8, c["decay"], grad_scale=s["clip"])
         else:
             _plain_step(s)
         return [s[k] for k in ("p", "m", "v", "m_scale", "v_scale", "copy") if k in s]
     if not own:
         return _plain_project(s) if c["op"] == "project" else _plain_grad(s)
-    import paper_2605_26660_amd as wq
-
-    packed = (s["W"], c["G"], c["unit_rows"], s["action"], s["code_off"], s["codes"], s["scale"], s["offset"])
-    adapters = wq.Adapters(s["a"], s["b"], s["alpha"], s["rank"]) if c["adapters"] else None
-    if c["op"] == "project":
-        if adapters is None:
-            return [wq.windq_project(*packed, s["X"])]
-        h = torch.empty(c["tokens"], c["rank"], device=DEV)
-        return [wq.windq_project(*packed, s["X"], adapters, s["adapter_of"], h=h), h]
-    return list(wq.windq_project_grad(*packed, s["dY"], s["X"], adapters, s["adapter_of"]))
+    wq, (packed, adapters, ws, outs) = _kept(s)
+    if c["op"] == "grad":
+        return list(wq.windq_project_grad(packed, s["dY"], s["X"], adapters, s["adapter_of"], ws=ws, outs=outs))
+    y, h = outs
+    if adapters is None:
+        return [wq.windq_project(packed, s["X"], ws=ws, out=y)]
+    return [wq.windq_project(packed, s["X"], adapters, s["adapter_of"], h=h, ws=ws, out=y), h]
 
 
 def work(case):
