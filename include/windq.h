@@ -616,6 +616,117 @@ typedef struct windq_refine_item {
 int windq_refine_plan_batch(const windq_refine_item* items /*HOST [n]*/, int32_t n, int32_t chunk_w, int64_t unit_rows,
                             const float* clip_grid /*HOST [K]*/, int32_t K, int32_t n_iter, void* stream);
 
+/*
+ * Adapting and serving a packed plan: low-rank adapters of many requests beside the packed projection, their way back,
+ * and the optimizer step that trains them.
+ *
+ * A packed matrix, as windq_apply_plan (or windq_refine_plan) left it.  W is read for skip units only; `mask` NULL or as
+ * in windq_apply_plan_prot (protected weights count as 0: their values live in the INT8 side stream).  Entries of the
+ * plan are checked as in windq_dequant_plan: a malformed one counts as skip.
+ */
+#define WINDQ_MAX_RANK 128           /* longest adapter */
+#define WINDQ_MAX_ADAPTERS (1 << 20) /* most adapters of one call */
+typedef struct windq_packed {
+    const windq_mat* W;       /* HOST descriptor */
+    const uint8_t* mask;      /* [rows][cols/8] or NULL */
+    const uint8_t* action;    /* [U] */
+    const int64_t* code_off;  /* [U+1] */
+    const uint8_t* codes;
+    size_t codes_bytes;
+    const float* scale;       /* [U*R_u] */
+    const float* offset;      /* [U*R_u] */
+    int32_t chunk_w;
+    int32_t reserved;         /* set to 0 */
+    int64_t unit_rows;
+} windq_packed;
+
+/* n adapters of up to max_rank ranks (a multiple of 8, at most WINDQ_MAX_RANK), one behind the other, 16-byte aligned. */
+typedef struct windq_adapters {
+    const void* a;            /* [n][max_rank][cols], rank[k] rows of adapter k are read */
+    const void* b;            /* [n][rows][max_rank], rank[k] values of a row are read */
+    const float* alpha;       /* [n] factor of the adapter's product, or NULL = 1 */
+    const int32_t* rank;      /* [n] in 0..max_rank (others are clamped), or NULL = max_rank */
+    int32_t n, max_rank;
+    int32_t dtype;            /* windq_dtype of a and b: the activations' */
+    int32_t reserved;         /* set to 0 */
+} windq_adapters;
+
+/*
+ * A batch of tokens through the packed matrix, each with the adapter of its own request beside it:
+ *   Y[t] = w_hat x_t + alpha_k B_k h_t,   h_t = A_k x_t,   k = adapter_of[t]
+ * A token whose adapter_of is outside 0..n-1 has none (h_t = 0); adapters NULL: no token has one, adapter_of and h unused.
+ * Tokens of one adapter may lie anywhere.
+ *   X  [tokens][cols], WINDQ_BF16 or WINDQ_F32 whatever W's type; Y [tokens][rows] of X's type, leading dimension
+ *      ld_y >= rows (any), written whole (nothing past a row's end)
+ *   h  [tokens][max_rank] f32 or NULL: h_t, zeros past the adapter's rank (what windq_project_grad can use again)
+ * Codes enter the matrix instructions as they are (small integers and signs are exact in bfloat16) and a group's sum over its
+ * chunk is scaled in fp32 afterwards: scale * sum code x + offset * sum x, so no weight is rounded.  fp32 activations and
+ * fp32 skip weights enter as three bfloat16 terms each, to fp32 accuracy.  Sums are fp32, in a fixed order:
+ * results are bit-reproducible and differ from the exact sum by a few 1e-7 of sum |w_hat x| before Y's own rounding.
+ * A result that is not finite is formed again weight by weight in fp64, so infinities and NaN of x, of scales and of skip
+ * weights come out as the formula has them, in their own token's and row's results only.
+ * At most 2^31 - 1 tokens x rows.  Workspace: windq_project_workspace_bytes.
+ */
+int windq_project(const windq_packed* P /*HOST*/, const windq_mat* X, const windq_adapters* adapters /*HOST or NULL*/,
+                  const int32_t* adapter_of /*[tokens] or NULL*/, void* Y, int64_t ld_y, float* h /*[tokens][max_rank] or NULL*/,
+                  void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The way back of windq_project, for the tokens and for the adapters (the packed weights stay as they are):
+ *   dh_t = alpha_k B_k^T dY_t
+ *   dX[t] = w_hat^T dY_t + A_k^T dh_t
+ *   dA[k] = sum_t dh_t x_t^T,   dB[k] = alpha_k sum_t dY_t h_t^T    over the tokens of adapter k
+ *   dY [tokens][rows] (leading dimension ld_dy >= rows, any); X [tokens][cols], of one type
+ *   dX [tokens][cols] of that type, ld_dx >= cols, or NULL: not wanted.  In WINDQ_BF16 the weights enter the product rounded
+ *      to bfloat16 once, as dY is.
+ *   dA [n][max_rank][cols], dB [n][rows][max_rank] f32, both or neither: written whole, zeros past an adapter's rank and for
+ *      adapters without a token
+ *   h  as windq_project left it, or NULL: formed again from X
+ * adapters NULL: dX alone; X, adapter_of, h, dA, dB unused.  X may be NULL where dA and dB are.  P may be NULL: the adapters' gradients
+ * alone, without the packed matrix's part of dX (rows and cols are those of dY's and X's descriptors).
+ * Sums over tokens run in a fixed order: results are bit-reproducible.
+ */
+int windq_project_grad(const windq_packed* P /*HOST*/, const windq_mat* dY, const windq_mat* X /*or NULL*/,
+                       const windq_adapters* adapters /*HOST or NULL*/, const int32_t* adapter_of /*[tokens] or NULL*/,
+                       const float* h /*[tokens][max_rank] or NULL*/, void* dX /*or NULL*/, int64_t ld_dx,
+                       float* dA /*or NULL*/, float* dB /*or NULL*/, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace of windq_project (grad = 0) or windq_project_grad (grad = 1); 0 if a size is out of range.  HOST only. */
+size_t windq_project_workspace_bytes(int32_t grad, int32_t dtype, int64_t tokens, int64_t rows, int64_t cols,
+                                     int32_t chunk_w, int32_t n_adapters, int32_t max_rank);
+
+/*
+ * One AdamW step over many tensors.  With g' = g * *grad_scale (grad_scale NULL: g) and t = step, in fp32, one rounded
+ * operation after the other:
+ *   m <- beta1 m + (1 - beta1) g',   v <- beta2 v + (1 - beta2) g'^2
+ *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) * (m / (sqrt(v) / sqrt(1 - beta2^t) + eps))
+ * p is rounded once to p_dtype; copy (or NULL) gets it in bfloat16 too, for the products.
+ *   state_bits 32: m, v f32 [n]; m_scale, v_scale unused
+ *   state_bits 8:  m, v hold 8-bit floats (e4m3: 1, 4 and 3 bits, largest 448, no infinities), one f32 scale for every
+ *      WINDQ_ADAMW_BLOCK values in a row.  v holds the ROOT of the second moment, so that its range is the gradients' and not their
+ *      squares'.  A block's scale is its largest magnitude / 448 (below the smallest normal fp32: scale 0, values 0); values
+ *      round to nearest, ties to even, but a root that is not zero never becomes zero (it takes the smallest magnitude,
+ *      2^-9 of the scale): a lost root would turn its next step into lr m / eps.  A block that holds a NaN loses its other
+ *      moments; one that holds an infinity becomes NaN.
+ * Tensors are contiguous and aligned to their element's size (16-byte aligned ones are faster); none may overlap another.
+ * n = 0 in an item or for the call is fine.  step >= 1; lr, weight_decay >= 0; beta1, beta2 in [0, 1); eps > 0 (finite, all).
+ * step and lr travel by value: a captured graph repeats its own.
+ */
+#define WINDQ_ADAMW_BLOCK 256
+typedef struct windq_adamw_item {
+    void* p;                  /* [n] p_dtype, updated */
+    const void* g;            /* [n] g_dtype */
+    void* m;                  /* [n] f32, or e4m3 bytes; updated */
+    void* v;                  /* [n] f32, or e4m3 bytes (of the root); updated */
+    float* m_scale;           /* [ceil(n / WINDQ_ADAMW_BLOCK)] */
+    float* v_scale;           /* [ceil(n / WINDQ_ADAMW_BLOCK)] */
+    void* copy;               /* [n] bf16 or NULL */
+    int64_t n;
+} windq_adamw_item;
+int windq_adamw(const windq_adamw_item* items /*HOST [n]*/, int64_t n, int32_t p_dtype, int32_t g_dtype, int32_t state_bits,
+                int64_t step, double lr, double beta1, double beta2, double eps, double weight_decay,
+                const float* grad_scale /*[1] or NULL*/, void* stream);
+
 /* Workspace bytes a call needs for these shapes (0 if the shape is invalid). HOST only. */
 size_t windq_workspace_bytes(int32_t which_call, int32_t dtype, int64_t rows, int64_t cols,
                              int32_t chunk_w, int64_t unit_rows, int32_t K);

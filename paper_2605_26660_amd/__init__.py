@@ -8,5 +8,6 @@ from .binding import (  # noqa: F401
     windq_fallback_promote, windq_heuristic_plan, windq_n_protected, windq_salient_encode, windq_unit_saliency, windq_salient_select, windq_unit_features, windq_unit_features_batch, workspace_bytes,
     windq_salient_select_batch, windq_salient_encode_batch, windq_refine_plan_batch, windq_dequant_plan_batch, windq_unit_features_exact_units,
     CALL_DEQUANT_GEMV, windq_dequant_gemv, windq_dequant_gemv_batch,
+    ADAMW_BLOCK, MAX_RANK, AdamwItems, Adapters, Packed, project_workspace, windq_adamw, windq_project, windq_project_grad,
 )
 from . import synth  # noqa: F401

@@ -20,6 +20,7 @@ WINDQ_F32, WINDQ_BF16 = 0, 1
 CALL_CALIB_STATS, CALL_UNIT_FEATURES, CALL_FIT_SCORE, CALL_APPLY_PLAN, CALL_SALIENT, CALL_UNIT_SALIENCY, CALL_DEQUANT, CALL_REFINE, CALL_FEATURES_FIT_SCORE, CALL_DEQUANT_GEMV = range(10)
 N_ACTIONS, N_ERR, N_FEAT, MAX_CLIP, MAX_CHUNK, MAX_BATCH = 7, 6, 8, 64, 512, 8
 STATIC_SCRATCH_BYTES = 8 << 20
+MAX_RANK, ADAMW_BLOCK = 128, 256
 
 EXPORTS = (
     "windq_calib_stats", "windq_unit_features", "windq_fit_score_all_bits", "windq_bytes_per_group",
@@ -31,7 +32,8 @@ EXPORTS = (
     "windq_fit_score_all_bits_static", "windq_features_fit_score", "windq_features_fit_score_batch",
     "windq_kernel_timer", "windq_kernel_timer_read", "windq_salient_select_batch", "windq_salient_encode_batch",
     "windq_refine_plan_batch", "windq_dequant_plan_batch", "windq_unit_features_exact_units",
-    "windq_dequant_gemv", "windq_dequant_gemv_batch",
+    "windq_dequant_gemv", "windq_dequant_gemv_batch", "windq_project", "windq_project_grad",
+    "windq_project_workspace_bytes", "windq_adamw",
 )
 
 
@@ -104,6 +106,23 @@ class windq_gemv_item(ctypes.Structure):
 class windq_calib_item(ctypes.Structure):
     _fields_ = [("X", ctypes.POINTER(windq_mat)), ("s_absmean", ctypes.c_void_p), ("s_rms", ctypes.c_void_p),
                 ("ws", ctypes.c_void_p), ("ws_bytes", ctypes.c_size_t)]
+
+
+class windq_packed(ctypes.Structure):
+    _fields_ = [("W", ctypes.POINTER(windq_mat)), ("mask", ctypes.c_void_p), ("action", ctypes.c_void_p),
+                ("code_off", ctypes.c_void_p), ("codes", ctypes.c_void_p), ("codes_bytes", ctypes.c_size_t),
+                ("scale", ctypes.c_void_p), ("offset", ctypes.c_void_p), ("chunk_w", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("unit_rows", ctypes.c_int64)]
+
+
+class windq_adapters(ctypes.Structure):
+    _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("alpha", ctypes.c_void_p), ("rank", ctypes.c_void_p),
+                ("n", ctypes.c_int32), ("max_rank", ctypes.c_int32), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class windq_adamw_item(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_int64)]
 
 
 _lib = None          # what lib() gives: descriptors and items are the structures above, checked by ctypes
@@ -181,6 +200,16 @@ def _declare(lib, by_address):
     lib.windq_dequant_gemv_batch.restype = c.c_int
     lib.windq_unit_features_exact_units.argtypes = [vp, i32, i64, i64, i32, i64, c.POINTER(i64)]
     lib.windq_unit_features_exact_units.restype = c.c_int
+    pp, pa = by_address(windq_packed), by_address(windq_adapters)
+    lib.windq_project.argtypes = [pp, pm, pa, vp, vp, i64, vp, vp, sz, vp]
+    lib.windq_project.restype = c.c_int
+    lib.windq_project_grad.argtypes = [pp, pm, pm, pa, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+    lib.windq_project_grad.restype = c.c_int
+    lib.windq_project_workspace_bytes.argtypes = [i32, i32, i64, i64, i64, i32, i32, i32]
+    lib.windq_project_workspace_bytes.restype = sz
+    f64 = c.c_double
+    lib.windq_adamw.argtypes = [by_address(windq_adamw_item), i64, i32, i32, i32, i64, f64, f64, f64, f64, f64, vp, vp]
+    lib.windq_adamw.restype = c.c_int
     lib.windq_status_str.argtypes = [c.c_int]
     lib.windq_status_str.restype = c.c_char_p
     for name in ("windq_calib_stats", "windq_unit_features", "windq_fit_score_all_bits", "windq_plan_layout",
@@ -839,3 +868,175 @@ def windq_dequant_gemv_batch(Ws, chunk_w: int, unit_rows: int, actions, code_off
                   ws.data_ptr(), ws.numel())
     _check(_packed().windq_dequant_gemv_batch(_addr(items := array("Q", items)), n, chunk_w, unit_rows, _stream()), "windq_dequant_gemv_batch")
     return ys
+
+
+# ------------------------------------------------- adapters beside a packed plan, and their optimizer
+class Packed:
+    """A packed matrix as windq_project and windq_project_grad take it: device tensors as windq_apply_plan wrote them, W [rows x cols]
+    (read for skip units only), mask as windq_salient_select wrote it or None.  Checked and described once; it keeps the tensors,
+    and sees what is written into them later."""
+
+    def __init__(self, W: torch.Tensor, chunk_w: int, unit_rows: int, action: torch.Tensor, code_off: torch.Tensor,
+                 codes: torch.Tensor, scale: torch.Tensor, offset: torch.Tensor, mask: torch.Tensor | None = None):
+        _require_cuda(W, action, code_off, codes, scale, offset, mask)
+        if chunk_w < 1 or unit_rows < 0 or W.dim() != 2 or W.shape[1] % chunk_w or (unit_rows and W.shape[0] % unit_rows):
+            raise WindqError(WINDQ_ESHAPE, "Packed")
+        U, R_u = n_units(W.shape[0], W.shape[1], chunk_w, unit_rows)
+        for t, dtype, least in ((action, torch.uint8, U), (code_off, torch.int64, U + 1), (codes, torch.uint8, 0),
+                                (scale, torch.float32, U * R_u), (offset, torch.float32, U * R_u),
+                                (mask, torch.uint8, W.shape[0] * (W.shape[1] // 8))):
+            if t is None:
+                continue
+            if t.dtype != dtype:
+                raise WindqError(WINDQ_EDTYPE, "Packed")
+            if t.numel() < least or not t.is_contiguous():
+                raise WindqError(WINDQ_ESHAPE, "Packed")
+        self.W, self.rows, self.cols, self.chunk_w = W, W.shape[0], W.shape[1], chunk_w
+        self.tensors = (action, code_off, codes, scale, offset, mask)
+        self._mat = _mats((W,))
+        self._words = array("Q", (_addr(self._mat), _ptr0(mask), action.data_ptr(), code_off.data_ptr(), codes.data_ptr(), codes.numel(),
+                                  scale.data_ptr(), offset.data_ptr(), chunk_w, unit_rows))
+        self.address = _addr(self._words)
+
+
+class Adapters:
+    """Low-rank adapters of one matrix: a [n x max_rank x cols], b [n x rows x max_rank] (float32 or bfloat16), alpha f32 [n] or None
+    (1), rank i32 [n] or None (max_rank).  Described once; it keeps the tensors, and sees what is written into them later."""
+
+    def __init__(self, a: torch.Tensor, b: torch.Tensor, alpha: torch.Tensor | None = None, rank: torch.Tensor | None = None):
+        _require_cuda(a, b, alpha, rank)
+        if a.dtype != b.dtype or (alpha is not None and alpha.dtype != torch.float32) or (rank is not None and rank.dtype != torch.int32):
+            raise WindqError(WINDQ_EDTYPE, "Adapters")
+        if a.dim() != 3 or b.dim() != 3 or a.shape[0] != b.shape[0] or a.shape[1] != b.shape[2] or \
+                not all(t is None or t.is_contiguous() for t in (a, b, alpha, rank)) or \
+                any(t is not None and t.numel() != a.shape[0] for t in (alpha, rank)):
+            raise WindqError(WINDQ_ESHAPE, "Adapters")
+        self.a, self.b, self.alpha, self.rank = a, b, alpha, rank
+        self.n, self.max_rank, self.cols, self.rows = a.shape[0], a.shape[1], a.shape[2], b.shape[1]
+        self._words = array("Q", (a.data_ptr(), b.data_ptr(), _ptr0(alpha), _ptr0(rank), self.n | self.max_rank << 32, _dtype_code(a)))
+        self.address = _addr(self._words)
+
+
+def project_workspace(packed: Packed | None, X: torch.Tensor, adapters: Adapters | None = None, grad: bool = False) -> torch.Tensor:
+    """Workspace of windq_project (or windq_project_grad) for tokens like X (any fewer of them fit too)."""
+    shape = adapters if packed is None else packed
+    need = load().windq_project_workspace_bytes(int(grad), _dtype_code(X), X.shape[0], shape.rows, shape.cols, 8 if packed is None else packed.chunk_w,
+                                                0 if adapters is None else adapters.n, 0 if adapters is None else adapters.max_rank)
+    return torch.empty(max(int(need), 256), dtype=torch.uint8, device=X.device)
+
+
+def _check_side(packed, adapters, adapter_of, h, tokens, where):
+    if adapters is None:
+        return
+    if adapter_of is None or (packed is not None and (adapters.rows, adapters.cols) != (packed.rows, packed.cols)) or adapter_of.numel() != tokens:
+        raise WindqError(WINDQ_ESHAPE, where)
+    if adapter_of.dtype != torch.int32 or (h is not None and h.dtype != torch.float32):
+        raise WindqError(WINDQ_EDTYPE, where)
+    if not adapter_of.is_contiguous() or (h is not None and (tuple(h.shape) != (tokens, adapters.max_rank) or not h.is_contiguous())):
+        raise WindqError(WINDQ_ESHAPE, where)
+    _require_cuda(adapter_of, h)
+
+
+def windq_project(packed: Packed, X: torch.Tensor, adapters: Adapters | None = None, adapter_of: torch.Tensor | None = None,
+                  h: torch.Tensor | None = None, ws: torch.Tensor | None = None, out: torch.Tensor | None = None):
+    """Y [tokens x rows] of X's type: X [tokens x cols] (float32 or bfloat16) through the packed matrix, and through the adapter
+    that adapter_of (i32 [tokens], outside 0..n-1: none) names for each token.  h: f32 [tokens x max_rank] to be filled, or None."""
+    _require_cuda(X, out, ws)
+    T = X.shape[0]
+    _check_side(packed, adapters, adapter_of, h, T, "windq_project")
+    y = out if out is not None else torch.empty(T, packed.rows, dtype=X.dtype, device=X.device)
+    if y.dtype != X.dtype or tuple(y.shape) != (T, packed.rows) or y.stride(1) != 1:
+        raise WindqError(WINDQ_EDTYPE if y.dtype != X.dtype else WINDQ_ESHAPE, "windq_project")
+    if ws is None:
+        ws = project_workspace(packed, X, adapters)
+    m = _mats((X,))
+    _check(_packed().windq_project(packed.address, _addr(m), None if adapters is None else adapters.address, _ptr(adapter_of), y.data_ptr(),
+                                   max(y.stride(0), packed.rows), _ptr(h), ws.data_ptr(), ws.numel(), _stream()), "windq_project")
+    return y
+
+
+def windq_project_grad(packed: Packed | None, dY: torch.Tensor, X: torch.Tensor | None = None, adapters: Adapters | None = None,
+                       adapter_of: torch.Tensor | None = None, h: torch.Tensor | None = None, ws: torch.Tensor | None = None,
+                       outs=None, want_dx: bool = True):
+    """The way back of windq_project: dY [tokens x rows], X as it was.  outs: (dX, dA, dB), any of them None to be allocated.  packed None:
+    the adapters alone, without the packed matrix's part of dX.
+    -> (dX [tokens x cols] of dY's type or None, dA f32 [n x max_rank x cols], dB f32 [n x rows x max_rank]; both None without adapters)."""
+    _require_cuda(dY, X, ws)
+    T = dY.shape[0]
+    if packed is None and adapters is None:
+        raise WindqError(WINDQ_EINVAL, "windq_project_grad")
+    shape = adapters if packed is None else packed
+    _check_side(packed, adapters, adapter_of, h, T, "windq_project_grad")
+    if (adapters is not None) != (X is not None) or (X is not None and (X.dtype != dY.dtype or tuple(X.shape) != (T, shape.cols))) or dY.shape[1] != shape.rows:
+        raise WindqError(WINDQ_ESHAPE, "windq_project_grad")
+    dx, da, db = (None, None, None) if outs is None else outs
+    _require_cuda(dx, da, db)
+    if want_dx and dx is None:
+        dx = torch.empty(T, shape.cols, dtype=dY.dtype, device=dY.device)
+    if not want_dx:
+        dx = None
+    if adapters is not None:
+        da = torch.empty(adapters.a.shape, dtype=torch.float32, device=dY.device) if da is None else da
+        db = torch.empty(adapters.b.shape, dtype=torch.float32, device=dY.device) if db is None else db
+        if da.shape != adapters.a.shape or db.shape != adapters.b.shape or not da.is_contiguous() or not db.is_contiguous():
+            raise WindqError(WINDQ_ESHAPE, "windq_project_grad")
+        if da.dtype != torch.float32 or db.dtype != torch.float32:
+            raise WindqError(WINDQ_EDTYPE, "windq_project_grad")
+    else:
+        da = db = None
+    if dx is not None and (dx.dtype != dY.dtype or tuple(dx.shape) != (T, shape.cols) or dx.stride(1) != 1):
+        raise WindqError(WINDQ_EDTYPE if dx.dtype != dY.dtype else WINDQ_ESHAPE, "windq_project_grad")
+    if ws is None:
+        ws = project_workspace(packed, dY, adapters, grad=True)
+    m = _mats((dY,) if X is None else (dY, X))
+    at = _addr(m)
+    _check(_packed().windq_project_grad(None if packed is None else packed.address, at, None if X is None else at + 8 * _MAT_WORDS,
+                                        None if adapters is None else adapters.address, _ptr(adapter_of), _ptr(h), _ptr(dx),
+                                        shape.cols if dx is None else max(dx.stride(0), shape.cols), _ptr(da), _ptr(db), ws.data_ptr(), ws.numel(),
+                                        _stream()), "windq_project_grad")
+    return dx, da, db
+
+
+class AdamwItems:
+    """The tensors of an AdamW step (lists of equal length): parameters (all float32 or all bfloat16), their gradients
+    (likewise), first moments and second moments, float32 or, in 8 bits, float8_e4m3fn (or its bytes, uint8) with the float32 scales
+    m_scales and v_scales, one for every ADAMW_BLOCK values; copies: bfloat16 copies of the parameters to be written, or None.
+    Checked and described once; it keeps the tensors."""
+
+    def __init__(self, params, grads, ms, vs, m_scales=None, v_scales=None, copies=None):
+        n = len(params)
+        lists = [grads, ms, vs] + [x for x in (m_scales, v_scales, copies) if x is not None]
+        if any(len(x) != n for x in lists) or (m_scales is None) != (v_scales is None):
+            raise WindqError(WINDQ_EINVAL, "AdamwItems")
+        _require_cuda(*params, *(t for x in lists for t in x))
+        self.state_bits = 32 if m_scales is None else 8
+        states = (torch.float32,) if self.state_bits == 32 else (torch.float8_e4m3fn, torch.uint8)
+        for ts, types in ((ms, states), (vs, states), (m_scales or [], (torch.float32,)), (v_scales or [], (torch.float32,)), (copies or [], (torch.bfloat16,))):
+            if any(t.dtype not in types for t in ts):
+                raise WindqError(WINDQ_EDTYPE, "AdamwItems")
+        if any(len({t.dtype for t in ts}) > 1 for ts in (params, grads)):
+            raise WindqError(WINDQ_EDTYPE, "AdamwItems")
+        self.p_dtype, self.g_dtype = (_dtype_code(ts[0]) if n else WINDQ_F32 for ts in (params, grads))
+        words = []
+        for i, p in enumerate(params):
+            k = p.numel()
+            same = [grads[i], ms[i], vs[i]] + ([copies[i]] if copies is not None else [])
+            scales = [m_scales[i], v_scales[i]] if m_scales is not None else []
+            if any(t.numel() != k or not t.is_contiguous() for t in [p, *same]) or \
+                    any(t.numel() != (k + ADAMW_BLOCK - 1) // ADAMW_BLOCK or not t.is_contiguous() for t in scales):
+                raise WindqError(WINDQ_ESHAPE, "AdamwItems")
+            words += (p.data_ptr(), grads[i].data_ptr(), ms[i].data_ptr(), vs[i].data_ptr(), *((t.data_ptr() for t in scales) if scales else (0, 0)),
+                      _ptr0(copies[i]) if copies is not None else 0, k)
+        self.n, self.tensors = n, (params, lists)
+        self._words = array("Q", words)
+        self.address = _addr(self._words) if n else None
+
+
+def windq_adamw(items: AdamwItems, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                weight_decay: float = 0.0, grad_scale: torch.Tensor | None = None):
+    """One AdamW step over all of the tensors, in place (step counts from 1).  grad_scale: f32 [1], what gradients are multiplied by, or None."""
+    _require_cuda(grad_scale)
+    if grad_scale is not None and (grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
+        raise WindqError(WINDQ_EDTYPE, "windq_adamw")
+    _check(_packed().windq_adamw(items.address, items.n, items.p_dtype, items.g_dtype, items.state_bits, step, lr, beta1, beta2, eps,
+                                 weight_decay, _ptr(grad_scale), _stream()), "windq_adamw")

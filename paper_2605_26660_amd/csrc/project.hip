@@ -1,0 +1,345 @@
+// windq_project: a batch of tokens through a packed matrix, each with the low-rank adapter of its own request beside it.
+//   Y[t] = w_hat x_t + alpha_k B_k h_t,   h_t = A_k x_t,   k = adapter_of[t]
+#include <math.h>
+
+#include "windq_adapters.hpp"
+
+namespace windq {
+
+// ------------------------------------------------------------------------------------------------ fp32 activations
+// X in fp32 enters the products as three planes of bfloat16 that add up to it.
+__global__ __launch_bounds__(256) void planes_kernel(const float* __restrict__ X, int64_t ldx, int64_t T, int32_t cols, uint16_t* __restrict__ planes) {
+    const int64_t octets = cols >> 3;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= T * octets) return;
+    const int64_t t = i / octets, c = (i - t * octets) * 8;
+    uint32_t v[3][8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) split3(X[t * ldx + c + j], v[0][j], v[1][j], v[2][j]);
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+        *reinterpret_cast<uint4*>(planes + (k * T + t) * cols + c) =
+            make_uint4(v[k][0] | v[k][1] << 16, v[k][2] | v[k][3] << 16, v[k][4] | v[k][5] << 16, v[k][6] | v[k][7] << 16);
+}
+
+// ------------------------------------------------------------------------------------------------ the product, any shape
+// A workgroup has 16 RF rows and 16 NT tokens; its eight wavefronts share the chunks among them and add up through LDS.  A
+// wavefront's rows are the M side of 16x16x32 matrix instructions: lane l has row l mod 16 and, of every chunk, the octets
+// of its quarter l / 16.  Which columns the four quarters pair up is free as long as X's operand does the same, so a lane's octets lie next to
+// each other and its codes are contiguous bytes.  sum_c x comes from the same instructions with ones for weights (under a mask: ones
+// where the weight is kept).
+constexpr int PJ_WAVES = 8;
+
+struct ProjectArgs {
+    PackArgs P;
+    const uint16_t* X;         // bfloat16, or the first of three planes
+    int64_t ldx, plane;        // elements between tokens, and between planes
+    const void* raw;           // the caller's X
+    int64_t ld_raw;
+    int64_t T;
+    void* Y;
+    int64_t ldy;
+    const float* h;            // or null: no adapters
+    AdapterArgs A;
+};
+
+// alpha_k B_k[row] . h_t
+template <typename YT>
+__device__ __forceinline__ float expand_one(const AdapterArgs& A, const float* __restrict__ h, int64_t t, int64_t row, int64_t rows) {
+    const int32_t k = A.of[t];
+    if (k < 0 || k >= A.n) return 0.0f;
+    const int32_t rank = adapter_rank(A, k);
+    const YT* __restrict__ const b = static_cast<const YT*>(A.b) + ((int64_t)k * rows + row) * A.max_rank;
+    const float* __restrict__ const ht = h + t * A.max_rank;
+    float sum = 0.0f;
+    for (int32_t r = 0; r < rank; r += 8) {
+        float bv[8], hv[8];
+        load8(b + r, bv);
+        load8(ht + r, hv);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (r + j < rank) sum = fmaf(bv[j], hv[j], sum);
+    }
+    return A.alpha != nullptr ? A.alpha[k] * sum : sum;
+}
+
+template <typename YT>
+__device__ __forceinline__ void store_y(YT* __restrict__ p, float v) {
+    if constexpr (sizeof(YT) == 4) *p = v;
+    else *p = (uint16_t)f32_to_bf16_bits(v);
+}
+
+template <typename YT, int RF, int NT, bool MASK>
+__global__ __launch_bounds__(PJ_WAVES * 64) void project_kernel(const ProjectArgs Q) {
+    constexpr int NP = sizeof(YT) == 4 ? 3 : 1;
+    __shared__ float red[PJ_WAVES][RF * NT * 4][64];
+    __shared__ uint16_t trits_of[256];
+    if (threadIdx.x < 256) trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
+    __syncthreads();
+    const PackArgs& P = Q.P;
+    const int32_t G = P.G, O = G >> 3, S = (O + 3) >> 2;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
+    const int64_t row_blocks = (P.rows + RF * 16 - 1) / (RF * 16);
+    const int64_t tb = blockIdx.x / row_blocks;
+    const int64_t row0 = (blockIdx.x - tb * row_blocks) * (RF * 16), t0 = tb * (NT * 16);
+
+    const uint16_t* xp[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int64_t t = t0 + n * 16 + sub;
+        xp[n] = Q.X + (t < Q.T ? t : Q.T - 1) * Q.ldx;
+    }
+    int64_t row[RF], rb[RF], lrow[RF];
+#pragma unroll
+    for (int f = 0; f < RF; ++f) {
+        row[f] = row0 + f * 16 + sub;
+        if (row[f] >= P.rows) row[f] = P.rows - 1;         // computed for nothing, stored by nobody
+        rb[f] = row[f] / P.R_u;
+        lrow[f] = row[f] - rb[f] * P.R_u;
+    }
+    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+    const uint32_t one = 0x3f803f80u;
+    const uint4 ones = make_uint4(one, one, one, one);
+
+    f32x4 tot[RF][NT] = {};
+    for (int32_t j = wave; j < P.n_chunks; j += PJ_WAVES) {
+        int act[RF];
+        const uint8_t* codes[RF];
+        float alpha[RF], beta[RF];
+        bool wide = false;                                  // fp32 skip weights among the rows
+#pragma unroll
+        for (int f = 0; f < RF; ++f) {
+            const int64_t u = rb[f] * P.n_chunks + j;
+            int64_t base;
+            act[f] = pk_action(P, u, base);
+            codes[f] = P.codes + base + lrow[f] * pk_bytes_per_group(act[f], G);
+            const int64_t g = u * P.R_u + lrow[f];
+            pk_affine(act[f], P.scale[g], P.offset[g], alpha[f], beta[f]);
+            wide |= act[f] == 0 && P.w_f32 != 0;
+        }
+        f32x4 acc[RF][NT] = {}, xs[MASK ? RF : 1][NT] = {};
+        for (int32_t s = 0; s < S; ++s) {
+            const int32_t o = q * S + s;
+            const bool valid = o < O;
+            const int64_t col = (int64_t)j * G + o * 8;
+            bf16x8 b[NP][NT];
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) b[p][n] = as_bf16x8(valid ? *reinterpret_cast<const uint4*>(xp[n] + p * Q.plane + col) : none);
+#pragma unroll
+            for (int f = 0; f < RF; ++f) {
+                uint4 w = none, k = ones;
+                if (valid) {
+                    w = act[f] == 0 ? skip_octet(P, row[f], col, 0) : octet_fields(act[f], codes[f], o, trits_of);
+                    if (MASK && act[f] != 0) {
+                        k = keep_words(P.mask[row[f] * P.mask_ld + (col >> 3)]);
+                        w = and4(w, k);
+                        k = and4(k, ones);
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int p = NP - 1; p >= 0; --p) {
+                        acc[f][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), b[p][n], acc[f][n], 0, 0, 0);
+                        if (MASK || f == 0) xs[MASK ? f : 0][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(k), b[p][n], xs[MASK ? f : 0][n], 0, 0, 0);
+                    }
+            }
+            if (__any(wide)) {
+#pragma unroll
+                for (int f = 0; f < RF; ++f)
+                    for (int term = 1; term < 3; ++term) {
+                        const uint4 w = valid && act[f] == 0 ? skip_octet(P, row[f], col, term) : none;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int p = 0; p < NP; ++p)
+                                if (p + term < 3) acc[f][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), b[p][n], acc[f][n], 0, 0, 0);
+                    }
+            }
+        }
+#pragma unroll
+        for (int f = 0; f < RF; ++f) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float al = __shfl(alpha[f], 4 * q + i, 64), be = __shfl(beta[f], 4 * q + i, 64);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) tot[f][n][i] = fmaf(al, acc[f][n][i], fmaf(be, xs[MASK ? f : 0][n][i], tot[f][n][i]));
+            }
+        }
+    }
+#pragma unroll
+    for (int f = 0; f < RF; ++f)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) red[wave][(f * NT + n) * 4 + i][lane] = tot[f][n][i];
+    __syncthreads();
+    YT* __restrict__ const Y = static_cast<YT*>(Q.Y);
+    for (int e = threadIdx.x; e < RF * NT * 256; e += PJ_WAVES * 64) {
+        // row by row within a token, so that neighbouring lanes write neighbouring rows
+        const int r = e & 15, n = (e >> 4) % (NT * 16), f = (e >> 4) / (NT * 16);
+        const int64_t y = row0 + f * 16 + r, t = t0 + n;
+        if (y >= P.rows || t >= Q.T) continue;
+        const int slot = (f * NT + (n >> 4)) * 4 + (r & 3), at = (r >> 2) * 16 + (n & 15);
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < PJ_WAVES; ++w) v += red[w][slot][at];
+        if (!isfinite(v)) v = (float)pk_slow_dot(P, y, static_cast<const YT*>(Q.raw) + t * Q.ld_raw);
+        if (Q.h != nullptr) v += expand_one<YT>(Q.A, Q.h, t, y, P.rows);
+        store_y(Y + t * Q.ldy + y, v);
+    }
+}
+
+template <typename YT, int RF, int NT, bool MASK>
+int launch_project(const ProjectArgs& Q, hipStream_t st) {
+    const int64_t wgs = ((Q.P.rows + RF * 16 - 1) / (RF * 16)) * ((Q.T + NT * 16 - 1) / (NT * 16));
+    if (!fits_launch(wgs, PJ_WAVES * 64)) return WINDQ_ESHAPE;
+    project_kernel<YT, RF, NT, MASK><<<dim3((uint32_t)wgs), dim3(PJ_WAVES * 64), 0, st>>>(Q);
+    return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
+}
+
+template <typename YT, bool MASK>
+int launch_project_any(const ProjectArgs& Q, hipStream_t st) {
+    if (Q.T <= 16) return launch_project<YT, 1, 1, MASK>(Q, st);
+    if (Q.T <= 32) return launch_project<YT, 1, 2, MASK>(Q, st);
+    return launch_project<YT, 1, 4, MASK>(Q, st);
+}
+
+int check_packed(const windq_packed* P, PackArgs* A) {
+    if (P == nullptr) return WINDQ_EINVAL;
+    Geometry g;
+    const int status = make_geometry(P->W, P->chunk_w, P->unit_rows, &g);
+    if (status != WINDQ_OK) return status;
+    if (P->action == nullptr || P->code_off == nullptr || P->codes == nullptr || P->scale == nullptr || P->offset == nullptr) return WINDQ_EINVAL;
+    if (!aligned(P->code_off, 8) || !aligned(P->codes, 16) || !aligned(P->scale, 4) || !aligned(P->offset, 4)) return WINDQ_EINVAL;
+    A->W = P->W->data;
+    A->ld = P->W->ld;
+    A->w_f32 = P->W->dtype == WINDQ_F32;
+    A->mask = P->mask;
+    A->mask_ld = g.cols / 8;
+    A->action = P->action;
+    A->code_off = P->code_off;
+    A->codes = P->codes;
+    A->codes_bytes = (int64_t)P->codes_bytes;
+    A->scale = P->scale;
+    A->offset = P->offset;
+    A->rows = g.rows;
+    A->cols = g.cols;
+    A->R_u = g.R_u;
+    A->G = g.chunk_w;
+    A->n_chunks = (int32_t)g.n_chunks;
+    return WINDQ_OK;
+}
+
+int check_adapters(const windq_adapters* ad, const int32_t* adapter_of, int32_t dtype, AdapterArgs* A) {
+    if (ad->a == nullptr || ad->b == nullptr || adapter_of == nullptr) return WINDQ_EINVAL;
+    if (ad->dtype != WINDQ_F32 && ad->dtype != WINDQ_BF16) return WINDQ_EDTYPE;
+    if (ad->dtype != dtype) return WINDQ_EDTYPE;
+    if (ad->n < 1 || ad->n > WINDQ_MAX_ADAPTERS || ad->max_rank < 8 || ad->max_rank > WINDQ_MAX_RANK || ad->max_rank % 8 != 0) return WINDQ_ESHAPE;
+    if (!aligned(ad->a, 16) || !aligned(ad->b, 16) || !aligned(ad->alpha, 4) || !aligned(ad->rank, 4) || !aligned(adapter_of, 4)) return WINDQ_EINVAL;
+    A->a = ad->a;
+    A->b = ad->b;
+    A->alpha = ad->alpha;
+    A->rank = ad->rank;
+    A->of = adapter_of;
+    A->n = ad->n;
+    A->max_rank = ad->max_rank;
+    return WINDQ_OK;
+}
+
+// Activations or their gradients: [tokens][width], no tokens is fine.  `vector`: read eight at a time.
+int check_tokens(const windq_mat* M, int64_t width, bool vector) {
+    if (M == nullptr) return WINDQ_EINVAL;
+    if (M->dtype != WINDQ_F32 && M->dtype != WINDQ_BF16) return WINDQ_EDTYPE;
+    if (M->rows < 0 || M->cols != width || M->ld < M->cols || M->rows > ((int64_t)1 << 31) - 1 || M->ld > (int64_t)1 << 31) return WINDQ_ESHAPE;
+    if (vector && M->ld % 8 != 0) return WINDQ_ESHAPE;
+    if (M->rows == 0) return WINDQ_OK;
+    if (M->data == nullptr || !aligned(M->data, vector ? 16 : (M->dtype == WINDQ_F32 ? 4 : 2))) return WINDQ_EINVAL;
+    return WINDQ_OK;
+}
+
+size_t grad_ws_bytes(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t n, int32_t max_rank);
+
+struct ProjectWs {
+    size_t planes, h, total;   // offsets
+};
+
+ProjectWs project_ws(int32_t dtype, int64_t T, int64_t cols, int32_t max_rank) {
+    ProjectWs w;
+    w.planes = 0;
+    w.h = dtype == WINDQ_F32 ? round_up((size_t)(3 * T * cols) * 2, 256) : 0;
+    w.total = w.h + round_up((size_t)(T * max_rank) * 4, 256);
+    if (w.total == 0) w.total = 256;
+    return w;
+}
+
+template <typename XT>
+int project_all(ProjectArgs& Q, const windq_mat* X, const windq_adapters* ad, float* h, char* ws, const ProjectWs& at, hipStream_t st) {
+    const int64_t T = Q.T;
+    if constexpr (sizeof(XT) == 4) {
+        uint16_t* planes = reinterpret_cast<uint16_t*>(ws + at.planes);
+        const int64_t pieces = T * (Q.P.cols / 8);
+        if (!fits_launch((pieces + 255) / 256, 256)) return WINDQ_ESHAPE;
+        planes_kernel<<<dim3((uint32_t)((pieces + 255) / 256)), dim3(256), 0, st>>>(static_cast<const float*>(X->data), X->ld, T, (int32_t)Q.P.cols, planes);
+        if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
+        Q.X = planes;
+        Q.ldx = Q.P.cols;
+        Q.plane = T * Q.P.cols;
+    }
+    if (ad != nullptr) {
+        float* const ht = h != nullptr ? h : reinterpret_cast<float*>(ws + at.h);
+        const int64_t wgs = T * ((Q.A.max_rank + 15) / 16);
+        if (!fits_launch(wgs, 256)) return WINDQ_ESHAPE;
+        shrink_token_kernel<XT><<<dim3((uint32_t)wgs), dim3(256), 0, st>>>(static_cast<const XT*>(X->data), X->ld, (int32_t)Q.P.cols, Q.A, false, ht);
+        if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
+        Q.h = ht;
+    }
+    return Q.P.mask != nullptr ? launch_project_any<XT, true>(Q, st) : launch_project_any<XT, false>(Q, st);
+}
+
+}  // namespace windq
+
+using namespace windq;
+
+extern "C" size_t windq_project_workspace_bytes(int32_t grad, int32_t dtype, int64_t tokens, int64_t rows, int64_t cols,
+                                                int32_t chunk_w, int32_t n_adapters, int32_t max_rank) {
+    if ((dtype != WINDQ_F32 && dtype != WINDQ_BF16) || tokens < 0 || rows <= 0 || cols <= 0 || chunk_w <= 0 || n_adapters < 0 || max_rank < 0) return 0;
+    if (tokens > ((int64_t)1 << 31) - 1 || rows > (int64_t)1 << 31 || cols > (int64_t)1 << 31 || max_rank > WINDQ_MAX_RANK) return 0;
+    if (n_adapters == 0) max_rank = 0;
+    return grad != 0 ? grad_ws_bytes(dtype, tokens, rows, cols, n_adapters, max_rank) : project_ws(dtype, tokens, cols, max_rank).total;
+}
+
+extern "C" int windq_project(const windq_packed* P, const windq_mat* X, const windq_adapters* adapters, const int32_t* adapter_of,
+                             void* Y, int64_t ld_y, float* h, void* ws, size_t ws_bytes, void* stream) {
+    ProjectArgs Q = {};
+    int status = check_packed(P, &Q.P);
+    if (status != WINDQ_OK) return status;
+    status = check_tokens(X, Q.P.cols, true);
+    if (status != WINDQ_OK) return status;
+    if (adapters != nullptr) {
+        static const int32_t nobody = -1;                  // no tokens: no list of theirs either
+        status = check_adapters(adapters, X->rows == 0 ? &nobody : adapter_of, X->dtype, &Q.A);
+        if (status != WINDQ_OK) return status;
+        if (!aligned(h, 16)) return WINDQ_EINVAL;
+    }
+    const size_t eb = X->dtype == WINDQ_F32 ? 4 : 2;
+    if (ld_y < Q.P.rows || ld_y > (int64_t)1 << 31) return WINDQ_ESHAPE;
+    if (X->rows == 0) return WINDQ_OK;
+    if (X->rows * Q.P.rows > (int64_t)0x7fffffff) return WINDQ_ESHAPE;
+    if (Y == nullptr || !aligned(Y, eb)) return WINDQ_EINVAL;
+    const ProjectWs at = project_ws(X->dtype, X->rows, Q.P.cols, adapters != nullptr ? Q.A.max_rank : 0);
+    if (ws == nullptr || ws_bytes < at.total) return WINDQ_EWORKSPACE;
+    if (!aligned(ws, 256)) return WINDQ_EINVAL;
+    Q.X = static_cast<const uint16_t*>(X->data);
+    Q.ldx = X->ld;
+    Q.raw = X->data;
+    Q.ld_raw = X->ld;
+    Q.T = X->rows;
+    Q.Y = Y;
+    Q.ldy = ld_y;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    char* w = static_cast<char*>(ws);
+    return X->dtype == WINDQ_F32 ? project_all<float>(Q, X, adapters, h, w, at, st) : project_all<uint16_t>(Q, X, adapters, h, w, at, st);
+}

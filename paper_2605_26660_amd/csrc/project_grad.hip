@@ -1,0 +1,489 @@
+// windq_project_grad: the way back of a packed product with adapters beside it.
+//   dh_t = alpha_k B_k^T dY_t     dX[t] = w_hat^T dY_t + A_k^T dh_t     dA[k] = sum_t dh_t x_t^T     dB[k] = alpha_k sum_t dY_t h_t^T
+#include <math.h>
+
+#include "windq_adapters.hpp"
+
+namespace windq {
+
+int check_tokens(const windq_mat* M, int64_t width, bool vector);
+
+// ------------------------------------------------------------------------------------------------ tokens by adapter
+// The tokens of adapter k in their own order, at places that start with a multiple of GROUP: place[] holds tokens, -1 where there is none.
+// Adapter k's first slot of GROUP places is (tokens of adapters below it) / GROUP + k: slots never overlap, and no adapter
+// has to wait for the counts of the others.
+constexpr int GROUP = 64;
+inline int64_t group_slots(int64_t T, int32_t n) { return T / GROUP + n + 1; }
+
+struct GroupArgs {
+    const int32_t* of;
+    int64_t T;
+    int32_t n;
+    int64_t slots;
+    int32_t* place;            // [slots * GROUP]
+    int32_t* first;            // [n] first place of an adapter
+    int32_t* count;            // [n] its tokens
+};
+
+__global__ __launch_bounds__(256) void group_kernel(const GroupArgs Q) {
+    __shared__ int32_t sums[2][4];
+    const int32_t k = blockIdx.x;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    int32_t below = 0, mine = 0;
+    for (int64_t t = threadIdx.x; t < Q.T; t += 256) {
+        const int32_t id = Q.of[t];
+        below += id >= 0 && id < k ? 1 : 0;
+        mine += id == k ? 1 : 0;
+    }
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) {
+        below += __shfl_xor(below, m, 64);
+        mine += __shfl_xor(mine, m, 64);
+    }
+    if (lane == 0) {
+        sums[0][wave] = below;
+        sums[1][wave] = mine;
+    }
+    __syncthreads();
+    below = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
+    mine = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
+    const int64_t first = ((int64_t)(below / GROUP) + k) * GROUP;
+    const int64_t end = k + 1 == Q.n ? Q.slots * GROUP : ((int64_t)((below + mine) / GROUP) + k + 1) * GROUP;
+    if (threadIdx.x == 0) {
+        Q.first[k] = (int32_t)first;
+        Q.count[k] = mine;
+    }
+    int64_t at = first;
+    __syncthreads();
+    for (int64_t t0 = 0; t0 < Q.T; t0 += 256) {             // a fixed order: tokens ascend
+        const int64_t t = t0 + threadIdx.x;
+        const bool hit = t < Q.T && Q.of[t] == k;
+        const uint64_t hits = __ballot(hit);
+        if (lane == 0) sums[0][wave] = __popcll(hits);
+        __syncthreads();
+        int32_t before = __popcll(hits & ((1ull << lane) - 1ull)), all = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            before += w < wave ? sums[0][w] : 0;
+            all += sums[0][w];
+        }
+        if (hit) Q.place[at + before] = (int32_t)t;
+        at += all;
+        __syncthreads();
+    }
+    for (int64_t p = at + threadIdx.x; p < end; p += 256) Q.place[p] = -1;
+}
+
+// ------------------------------------------------------------------------------------------------ layouts
+// out [n][C][ldo] = in [n][R][C] transposed, rows padded with zeros up to ldo.
+template <typename T>
+__global__ __launch_bounds__(256) void transpose_kernel(const T* __restrict__ in, int64_t R, int32_t C, int64_t ldo, T* __restrict__ out) {
+    __shared__ T tile[64][65];
+    const int64_t rt = (ldo + 63) / 64, ct = (C + 63) / 64;
+    const int64_t k = blockIdx.x / (rt * ct), rest = blockIdx.x - k * rt * ct;
+    const int64_t r0 = rest / ct * 64, c0 = (rest - rest / ct * ct) * 64;
+    for (int i = threadIdx.x; i < 4096; i += 256) {
+        const int64_t r = r0 + (i >> 6), c = c0 + (i & 63);
+        tile[i >> 6][i & 63] = r < R && c < C ? in[(k * R + r) * C + c] : (T)0;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 4096; i += 256) {
+        const int64_t c = c0 + (i >> 6), r = r0 + (i & 63);
+        if (c < C && r < ldo) out[(k * C + c) * ldo + r] = tile[i & 63][i >> 6];
+    }
+}
+
+// A copy of dY whose rows start on 16 bytes and end with zeros.
+template <typename T>
+__global__ __launch_bounds__(256) void align_kernel(const T* __restrict__ in, int64_t ld, int64_t T_, int64_t width, int64_t ldo, T* __restrict__ out) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= T_ * ldo) return;
+    const int64_t t = i / ldo, c = i - t * ldo;
+    out[i] = c < width ? in[t * ld + c] : (T)0;
+}
+
+// ------------------------------------------------------------------------------------------------ dA and dB
+// out = sum over an adapter's tokens of left_t right_t^T.  A lane owns a column of the right side and sixteen ranks.
+template <typename XT>
+__global__ __launch_bounds__(256) void outer_kernel(const XT* __restrict__ right, int64_t ld, int64_t width, const float* __restrict__ left,
+                                                    const AdapterArgs A, const int32_t* __restrict__ place, const int32_t* __restrict__ first,
+                                                    const int32_t* __restrict__ count, bool scaled, bool by_column, float* __restrict__ out) {
+    const int64_t wt = (width + 255) / 256;
+    const int32_t groups = (A.max_rank + 15) / 16;
+    const int32_t k = (int32_t)(blockIdx.x / (wt * groups));
+    const int64_t rest = blockIdx.x - k * wt * groups;
+    const int32_t r0 = (int32_t)(rest / wt) * 16;
+    const int64_t c = (rest - rest / wt * wt) * 256 + threadIdx.x;
+    if (c >= width) return;
+    const int32_t rank = adapter_rank(A, k), n = count[k], p0 = first[k];
+    float acc[16] = {};
+    if (r0 < rank) {
+        for (int32_t i = 0; i < n; ++i) {
+            const int64_t t = place[p0 + i];
+            const float x = elem(right, t * ld + c, sizeof(XT) == 4);
+            const float* __restrict__ const l = left + t * A.max_rank + r0;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (r0 + r < A.max_rank) acc[r] = fmaf(l[r], x, acc[r]);
+        }
+    }
+    const float factor = scaled && A.alpha != nullptr ? A.alpha[k] : 1.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        if (r0 + r >= A.max_rank) break;
+        const float v = r0 + r < rank && n > 0 ? factor * acc[r] : 0.0f;
+        if (by_column) out[((int64_t)k * width + c) * A.max_rank + r0 + r] = v;
+        else out[((int64_t)k * A.max_rank + r0 + r) * width + c] = v;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ dX
+struct DxArgs {
+    PackArgs P;                // rows, cols alone where packed is false
+    bool packed;
+    const void* dY;            // rows on 16 bytes, readable up to a multiple of 8
+    int64_t ldy;
+    int64_t T;
+    void* dX;
+    int64_t ldx;
+    const float* dh;           // [T][max_rank] or null
+    AdapterArgs A;
+};
+
+// Eight columns of A_k^T dh_t, added to v.
+template <typename XT>
+__device__ __forceinline__ void add_adapter8(const AdapterArgs& A, const float* __restrict__ dh, int64_t t, int64_t col, int64_t cols, float (&v)[8]) {
+    const int32_t k = A.of[t];
+    if (k < 0 || k >= A.n) return;
+    const int32_t rank = adapter_rank(A, k);
+    const XT* __restrict__ const a = static_cast<const XT*>(A.a) + (int64_t)k * A.max_rank * cols + col;
+    float sum[8] = {};
+    for (int32_t r = 0; r < rank; ++r) {
+        float av[8];
+        load8(a + (int64_t)r * cols, av);
+        const float d = dh[t * A.max_rank + r];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] = fmaf(av[j], d, sum[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += sum[j];
+}
+
+// An octet of one row as fp32 weights (rounded nowhere but by the multiply-add).
+__device__ __forceinline__ void weight_octet(const PackArgs& P, int64_t row, int64_t col, const uint16_t* __restrict__ trits_of, float (&w)[8]) {
+    const int64_t rb = row / P.R_u, lrow = row - rb * P.R_u;
+    const int32_t j = (int32_t)(col / P.G), o = (int32_t)(col - (int64_t)j * P.G) >> 3;
+    const int64_t u = rb * P.n_chunks + j;
+    int64_t base;
+    const int a = pk_action(P, u, base);
+    if (a == 0) {
+        if (P.w_f32 != 0) load8(static_cast<const float*>(P.W) + row * P.ld + col, w);
+        else load8(static_cast<const uint16_t*>(P.W) + row * P.ld + col, w);
+        return;
+    }
+    const int64_t g = u * P.R_u + lrow;
+    const float s = P.scale[g], of = a >= 5 ? 0.0f : P.offset[g];
+    const uint4 f = octet_fields(a, P.codes + base + lrow * pk_bytes_per_group(a, P.G), o, trits_of);
+    const float f0 = a == 2 ? 16.0f : (a == 3 ? 8.0f : (a == 4 ? 4.0f : (a == 5 ? 5.0f : 0.0f)));
+    const uint32_t m = P.mask != nullptr ? P.mask[row * P.mask_ld + (col >> 3)] : 0u;
+    const uint32_t v[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float q = ((i & 1) != 0 ? __uint_as_float(v[i >> 1] & 0xffff0000u) : bf16_bits_to_f32(v[i >> 1] & 0xffffu)) - f0;
+        w[i] = ((m >> i) & 1u) != 0u ? 0.0f : fmaf(q, s, of);
+    }
+}
+
+// bfloat16: a workgroup has 128 columns and 64 NT tokens and walks the rows 128 at a time.  The sum runs over rows, and a matrix
+// operand wants eight consecutive rows of one column in a lane, while codes lie along columns: a thread unpacks a block of eight rows by
+// eight columns and has, after rounding pairs of rows together, one operand for each of its eight columns.  Sixteen threads
+// side by side make the operands of eight instructions whose M side is every eighth column; which columns share an instruction is free, and a
+// lane ends up with eight consecutive columns of its token.
+constexpr int DX_COLS = 128, DX_ROWS = 128;
+
+template <int NT>
+__global__ __launch_bounds__(256) void dx_kernel(const DxArgs Q) {
+    __shared__ uint4 frag[DX_ROWS / 8][8][16];
+    __shared__ uint16_t trits_of[256];
+    trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
+    __syncthreads();
+    const PackArgs& P = Q.P;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
+    const int64_t col_blocks = (P.cols + DX_COLS - 1) / DX_COLS;
+    const int64_t tb = blockIdx.x / col_blocks;
+    const int64_t c0 = (blockIdx.x - tb * col_blocks) * DX_COLS, t0 = tb * (64 * NT) + wave * (16 * NT);
+    const int oc = threadIdx.x & 15, kg = threadIdx.x >> 4;
+    const int64_t col = c0 + oc * 8;
+    const uint16_t* dy[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int64_t t = t0 + n * 16 + sub;
+        dy[n] = static_cast<const uint16_t*>(Q.dY) + (t < Q.T ? t : Q.T - 1) * Q.ldy;
+    }
+    f32x4 acc[8][NT] = {};
+    if (Q.packed) {
+        for (int64_t r0 = 0; r0 < P.rows; r0 += DX_ROWS) {
+            uint32_t v[8][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float w0[8] = {}, w1[8] = {};
+                const int64_t row = r0 + kg * 8 + 2 * i;
+                if (col < P.cols && row < P.rows) weight_octet(P, row, col, trits_of, w0);
+                if (col < P.cols && row + 1 < P.rows) weight_octet(P, row + 1, col, trits_of, w1);
+#pragma unroll
+                for (int m = 0; m < 8; ++m) v[m][i] = f32_to_bf16_bits(w0[m]) | f32_to_bf16_bits(w1[m]) << 16;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int m = 0; m < 8; ++m) frag[kg][m][oc] = make_uint4(v[m][0], v[m][1], v[m][2], v[m][3]);
+            __syncthreads();
+#pragma unroll
+            for (int kk = 0; kk < DX_ROWS / 32; ++kk) {
+                const int64_t row = r0 + kk * 32 + q * 8;
+                bf16x8 b[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) b[n] = as_bf16x8(row < P.rows ? *reinterpret_cast<const uint4*>(dy[n] + row) : make_uint4(0u, 0u, 0u, 0u));
+#pragma unroll
+                for (int m = 0; m < 8; ++m) {
+                    const bf16x8 a = as_bf16x8(frag[kk * 4 + q][m][sub]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[n], acc[m][n], 0, 0, 0);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int64_t t = t0 + n * 16 + sub;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t c = c0 + (4 * q + i) * 8;
+            if (t >= Q.T || c >= P.cols) continue;
+            float v[8];
+#pragma unroll
+            for (int m = 0; m < 8; ++m) v[m] = acc[m][n][i];
+            if (Q.dh != nullptr) add_adapter8<uint16_t>(Q.A, Q.dh, t, c, P.cols, v);
+            uint16_t* __restrict__ const o = static_cast<uint16_t*>(Q.dX) + t * Q.ldx + c;
+#pragma unroll
+            for (int m = 0; m < 8; ++m) o[m] = (uint16_t)f32_to_bf16_bits(v[m]);
+        }
+    }
+}
+
+// fp32: 64 columns and 64 tokens a workgroup, 32 rows at a time through LDS, on the fp32 matrix instructions.
+__global__ __launch_bounds__(256) void dx_f32_kernel(const DxArgs Q) {
+    __shared__ float wt[32][68], yt[32][68];
+    __shared__ uint16_t trits_of[256];
+    trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
+    __syncthreads();
+    const PackArgs& P = Q.P;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
+    const int64_t col_blocks = (P.cols + 63) / 64;
+    const int64_t tb = blockIdx.x / col_blocks;
+    const int64_t c0 = (blockIdx.x - tb * col_blocks) * 64, t0 = tb * 64;
+    const float* __restrict__ const dY = static_cast<const float*>(Q.dY);
+    f32x4 acc[4] = {};
+    if (Q.packed) {
+        for (int64_t r0 = 0; r0 < P.rows; r0 += 32) {
+            __syncthreads();
+            {
+                const int r = threadIdx.x >> 3, o = threadIdx.x & 7;
+                float w[8] = {};
+                if (r0 + r < P.rows && c0 + o * 8 < P.cols) weight_octet(P, r0 + r, c0 + o * 8, trits_of, w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) wt[r][o * 8 + j] = w[j];
+            }
+            for (int i = threadIdx.x; i < 64 * 32; i += 256) {
+                const int r = i & 31, t = i >> 5;
+                yt[r][t] = r0 + r < P.rows && t0 + t < Q.T ? dY[(t0 + t) * Q.ldy + r0 + r] : 0.0f;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float a = wt[k * 4 + q][wave * 16 + sub];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) acc[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, yt[k * 4 + q][n * 16 + sub], acc[n], 0, 0, 0);
+            }
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        const int64_t t = t0 + n * 16 + sub;
+        const int64_t c = c0 + wave * 16 + 4 * q;
+        if (t >= Q.T || c >= P.cols) continue;              // columns come in eights: four of them are in or out together
+        float v[4] = {acc[n][0], acc[n][1], acc[n][2], acc[n][3]};
+        if (Q.dh != nullptr) {
+            const int32_t k = Q.A.of[t];
+            if (k >= 0 && k < Q.A.n) {
+                const int32_t rank = adapter_rank(Q.A, k);
+                const float* __restrict__ const a = static_cast<const float*>(Q.A.a) + (int64_t)k * Q.A.max_rank * P.cols + c;
+                float sum[4] = {};
+                for (int32_t r = 0; r < rank; ++r) {
+                    const float4 av = *reinterpret_cast<const float4*>(a + (int64_t)r * P.cols);
+                    const float d = Q.dh[t * Q.A.max_rank + r];
+                    sum[0] = fmaf(av.x, d, sum[0]);
+                    sum[1] = fmaf(av.y, d, sum[1]);
+                    sum[2] = fmaf(av.z, d, sum[2]);
+                    sum[3] = fmaf(av.w, d, sum[3]);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] += sum[i];
+            }
+        }
+        float* __restrict__ const o = static_cast<float*>(Q.dX) + t * Q.ldx + c;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = v[i];
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ the call
+struct GradWs {
+    size_t h, dh, bt, dy, place, first, count, total;
+    int64_t rows8;
+};
+
+GradWs grad_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t n, int32_t max_rank) {
+    const size_t eb = dtype == WINDQ_F32 ? 4 : 2;
+    GradWs w;
+    w.rows8 = (rows + 7) / 8 * 8;
+    size_t at = 0;
+    auto take = [&at](size_t bytes) {
+        const size_t here = at;
+        at += round_up(bytes, 256);
+        return here;
+    };
+    w.dy = take((size_t)(T * w.rows8) * eb);
+    w.h = take((size_t)(T * max_rank) * 4);
+    w.dh = take((size_t)(T * max_rank) * 4);
+    w.bt = take((size_t)n * (size_t)max_rank * (size_t)w.rows8 * eb);
+    w.place = take((size_t)group_slots(T, n) * GROUP * 4);
+    w.first = take((size_t)n * 4);
+    w.count = take((size_t)n * 4);
+    w.total = at == 0 ? 256 : at;
+    return w;
+}
+
+size_t grad_ws_bytes(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t n, int32_t max_rank) {
+    return grad_ws(dtype, T, rows, cols, n, max_rank).total;
+}
+
+#define WINDQ_LAUNCH(wgs, threads, kernel, ...)                                                   \
+    do {                                                                                          \
+        const int64_t wgs_ = (wgs);                                                               \
+        if (!fits_launch(wgs_, threads)) return WINDQ_ESHAPE;                                     \
+        if (wgs_ > 0) {                                                                           \
+            kernel<<<dim3((uint32_t)wgs_), dim3(threads), 0, st>>>(__VA_ARGS__);                  \
+            if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;                               \
+        }                                                                                         \
+    } while (0)
+
+template <typename XT>
+int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h, float* dA, float* dB, char* ws, const GradWs& at, hipStream_t st) {
+    const int64_t T = Q.T, rows = Q.P.rows, cols = Q.P.cols;
+    const bool side = Q.A.n > 0;
+    const AdapterArgs A = Q.A;
+    if (T > 0 && (dY->ld % 8 != 0 || rows % 8 != 0 || !aligned(dY->data, 16))) {
+        XT* to = reinterpret_cast<XT*>(ws + at.dy);
+        WINDQ_LAUNCH((T * at.rows8 + 255) / 256, 256, align_kernel<XT>, static_cast<const XT*>(dY->data), dY->ld, T, rows, at.rows8, to);
+        Q.dY = to;
+        Q.ldy = at.rows8;
+    } else {
+        Q.dY = dY->data;
+        Q.ldy = dY->ld;
+    }
+    if (side) {
+        float* const dh = reinterpret_cast<float*>(ws + at.dh);
+        XT* const bt = reinterpret_cast<XT*>(ws + at.bt);
+        WINDQ_LAUNCH((int64_t)A.n * ((at.rows8 + 63) / 64) * ((A.max_rank + 63) / 64), 256, transpose_kernel<XT>, static_cast<const XT*>(A.b), rows, A.max_rank, at.rows8, bt);
+        AdapterArgs B = A;
+        B.a = bt;
+        const int64_t wgs = T * ((A.max_rank + 15) / 16);
+        WINDQ_LAUNCH(wgs, 256, shrink_token_kernel<XT>, static_cast<const XT*>(Q.dY), Q.ldy, (int32_t)at.rows8, B, true, dh);
+        Q.dh = dh;
+        if (dA != nullptr) {
+            GroupArgs G;
+            G.of = A.of;
+            G.T = T;
+            G.n = A.n;
+            G.slots = group_slots(T, A.n);
+            G.place = reinterpret_cast<int32_t*>(ws + at.place);
+            G.first = reinterpret_cast<int32_t*>(ws + at.first);
+            G.count = reinterpret_cast<int32_t*>(ws + at.count);
+            WINDQ_LAUNCH(A.n, 256, group_kernel, G);
+            if (h == nullptr) {
+                float* const ht = reinterpret_cast<float*>(ws + at.h);
+                WINDQ_LAUNCH(wgs, 256, shrink_token_kernel<XT>, static_cast<const XT*>(X->data), X->ld, (int32_t)cols, A, false, ht);
+                h = ht;
+            }
+            const int64_t groups = (int64_t)A.n * ((A.max_rank + 15) / 16);
+            WINDQ_LAUNCH(groups * ((cols + 255) / 256), 256, outer_kernel<XT>, static_cast<const XT*>(X->data), X->ld, cols, dh, A, G.place, G.first, G.count, false, false, dA);
+            WINDQ_LAUNCH(groups * ((rows + 255) / 256), 256, outer_kernel<XT>, static_cast<const XT*>(Q.dY), Q.ldy, rows, h, A, G.place, G.first, G.count, true, true, dB);
+        }
+    }
+    if (Q.dX == nullptr) return WINDQ_OK;
+    if constexpr (sizeof(XT) == 4) {
+        WINDQ_LAUNCH(((cols + 63) / 64) * ((T + 63) / 64), 256, dx_f32_kernel, Q);
+    } else {
+        const int64_t blocks = (cols + DX_COLS - 1) / DX_COLS;
+        if (T <= 64) WINDQ_LAUNCH(blocks * ((T + 63) / 64), 256, dx_kernel<1>, Q);
+        else if (T <= 128) WINDQ_LAUNCH(blocks * ((T + 127) / 128), 256, dx_kernel<2>, Q);
+        else WINDQ_LAUNCH(blocks * ((T + 255) / 256), 256, dx_kernel<4>, Q);
+    }
+    return WINDQ_OK;
+}
+
+}  // namespace windq
+
+using namespace windq;
+
+extern "C" int windq_project_grad(const windq_packed* P, const windq_mat* dY, const windq_mat* X, const windq_adapters* adapters,
+                                  const int32_t* adapter_of, const float* h, void* dX, int64_t ld_dx, float* dA, float* dB, void* ws,
+                                  size_t ws_bytes, void* stream) {
+    DxArgs Q = {};
+    Q.packed = P != nullptr;
+    int status;
+    if (P != nullptr) {
+        status = check_packed(P, &Q.P);
+        if (status != WINDQ_OK) return status;
+    } else {
+        if (dY == nullptr || X == nullptr || adapters == nullptr) return WINDQ_EINVAL;
+        Q.P.rows = dY->cols;
+        Q.P.cols = X->cols;
+        if (Q.P.rows <= 0 || Q.P.cols <= 0 || Q.P.cols % 8 != 0 || Q.P.rows > (int64_t)1 << 31 || Q.P.cols > (int64_t)1 << 31) return WINDQ_ESHAPE;
+    }
+    status = check_tokens(dY, Q.P.rows, false);
+    if (status != WINDQ_OK) return status;
+    const int64_t T = dY->rows;
+    if (T * Q.P.rows > (int64_t)0x7fffffff || T * Q.P.cols > (int64_t)0x7fffffff) return WINDQ_ESHAPE;
+    if ((dA == nullptr) != (dB == nullptr)) return WINDQ_EINVAL;
+    if (adapters != nullptr) {
+        static const int32_t nobody = -1;
+        status = check_adapters(adapters, T == 0 ? &nobody : adapter_of, dY->dtype, &Q.A);
+        if (status != WINDQ_OK) return status;
+        if (dA != nullptr) {
+            status = check_tokens(X, Q.P.cols, true);
+            if (status != WINDQ_OK) return status;
+            if (X->dtype != dY->dtype) return WINDQ_EDTYPE;
+            if (X->rows != T) return WINDQ_ESHAPE;
+            if (!aligned(dA, 16) || !aligned(dB, 16) || !aligned(h, 16)) return WINDQ_EINVAL;
+        }
+    } else if (dA != nullptr) {
+        return WINDQ_EINVAL;
+    }
+    if (dX == nullptr && dA == nullptr && T > 0) return WINDQ_EINVAL;
+    const size_t eb = dY->dtype == WINDQ_F32 ? 4 : 2;
+    if (dX != nullptr) {
+        if (ld_dx < Q.P.cols || ld_dx > (int64_t)1 << 31) return WINDQ_ESHAPE;
+        if (!aligned(dX, eb)) return WINDQ_EINVAL;
+    }
+    const GradWs at = grad_ws(dY->dtype, T, Q.P.rows, Q.P.cols, Q.A.n, Q.A.max_rank);
+    if (ws == nullptr || ws_bytes < at.total) return WINDQ_EWORKSPACE;
+    if (!aligned(ws, 256)) return WINDQ_EINVAL;
+    Q.T = T;
+    Q.dX = dX;
+    Q.ldx = ld_dx;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    char* w = static_cast<char*>(ws);
+    return dY->dtype == WINDQ_F32 ? grad_all<float>(Q, dY, X, h, dA, dB, w, at, st) : grad_all<uint16_t>(Q, dY, X, h, dA, dB, w, at, st);
+}
+
