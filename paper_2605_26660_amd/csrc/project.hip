@@ -2,7 +2,7 @@
 //   Y[t] = w_hat x_t + alpha_k B_k h_t,   h_t = A_k x_t,   k = adapter_of[t]
 #include <math.h>
 
-#include "windq_adapters.hpp"
+#include "windq_project_tiles.hpp"
 
 namespace windq {
 
@@ -29,6 +29,7 @@ __global__ __launch_bounds__(256) void planes_kernel(const float* __restrict__ X
 // each other and its codes are contiguous bytes.  sum_c x comes from the same instructions with ones for weights (under a mask: ones
 // where the weight is kept).
 constexpr int PJ_WAVES = 8;
+constexpr int64_t PROJECT_FEW = 64;                       // tokens up to which this kernel is the faster one
 
 struct ProjectArgs {
     PackArgs P;
@@ -262,17 +263,57 @@ int check_tokens(const windq_mat* M, int64_t width, bool vector) {
 
 size_t grad_ws_bytes(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t n, int32_t max_rank);
 
+// Offsets of a workspace's parts.  They are those of the shape alone, so that fewer tokens, or rows in other units, never need more.
 struct ProjectWs {
-    size_t planes, h, total;   // offsets
+    size_t planes, h, fields, unit, xs, total;
 };
 
-ProjectWs project_ws(int32_t dtype, int64_t T, int64_t cols, int32_t max_rank) {
+ProjectWs project_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t G, int32_t max_rank) {
     ProjectWs w;
-    w.planes = 0;
-    w.h = dtype == WINDQ_F32 ? round_up((size_t)(3 * T * cols) * 2, 256) : 0;
-    w.total = w.h + round_up((size_t)(T * max_rank) * 4, 256);
-    if (w.total == 0) w.total = 256;
+    size_t at = 0;
+    auto take = [&at](size_t bytes) {
+        const size_t here = at;
+        at += round_up(bytes, 256);
+        return here;
+    };
+    w.planes = take(dtype == WINDQ_F32 ? (size_t)(3 * T * cols) * 2 : 0);
+    w.h = take((size_t)(T * max_rank) * 4);
+    const bool many = T > PROJECT_FEW;
+    w.fields = take(many ? (size_t)(rows * cols) / 2 : 0);
+    w.unit = take(many ? (size_t)((rows + PT_STRIP - 1) / PT_STRIP) * (size_t)(cols / G) * sizeof(UnitWord) : 0);
+    w.xs = take(many ? (size_t)(cols / 64) * (size_t)T * 16 : 0);
+    w.total = at == 0 ? 256 : at;
     return w;
+}
+
+// Tiles for many tokens (windq_project_tiles.hpp).
+template <typename XT, int S>
+int launch_tiles(const ProjectArgs& Q, char* ws, const ProjectWs& at, hipStream_t st) {
+    TileArgs A = {};
+    A.P = Q.P;
+    A.X = Q.X;
+    A.ldx = Q.ldx;
+    A.plane = Q.plane;
+    A.raw = Q.raw;
+    A.ld_raw = Q.ld_raw;
+    A.T = Q.T;
+    A.Y = Q.Y;
+    A.ldy = Q.ldy;
+    A.h = Q.h;
+    A.A = Q.A;
+    A.fields = reinterpret_cast<uint8_t*>(ws + at.fields);
+    A.unit = reinterpret_cast<UnitWord*>(ws + at.unit);
+    A.xs = reinterpret_cast<uint4*>(ws + at.xs);
+    A.n_kb = (int32_t)(Q.P.cols / (16 * S));
+    A.row_blocks = (uint32_t)((Q.P.rows + PT_ROWS - 1) / PT_ROWS);
+    const int64_t strips = (Q.P.rows / Q.P.R_u) * Q.P.n_chunks * ((Q.P.R_u + PT_STRIP - 1) / PT_STRIP);
+    const int64_t wgs = strips + (A.n_kb * Q.T + 255) / 256;
+    const int64_t tiles = (int64_t)A.row_blocks * ((Q.T + PT_TOKENS - 1) / PT_TOKENS);
+    if (!fits_launch(wgs, 256) || !fits_launch(tiles, PT_THREADS)) return WINDQ_ESHAPE;
+    tiles_prepare_kernel<XT, S><<<dim3((uint32_t)wgs), dim3(256), 0, st>>>(A, strips);
+    if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
+    project_tiles_kernel<XT, S><<<dim3((uint32_t)tiles), dim3(PT_THREADS), 0, st>>>(A);
+    return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
 }
 
 template <typename XT>
@@ -296,6 +337,10 @@ int project_all(ProjectArgs& Q, const windq_mat* X, const windq_adapters* ad, fl
         if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
         Q.h = ht;
     }
+    const int S = Q.P.mask == nullptr && T > PROJECT_FEW ? tile_steps(Q.P) : 0;
+    if (S == 8) return launch_tiles<XT, 8>(Q, ws, at, st);
+    if (S == 6) return launch_tiles<XT, 6>(Q, ws, at, st);
+    if (S == 4) return launch_tiles<XT, 4>(Q, ws, at, st);
     return Q.P.mask != nullptr ? launch_project_any<XT, true>(Q, st) : launch_project_any<XT, false>(Q, st);
 }
 
@@ -308,7 +353,7 @@ extern "C" size_t windq_project_workspace_bytes(int32_t grad, int32_t dtype, int
     if ((dtype != WINDQ_F32 && dtype != WINDQ_BF16) || tokens < 0 || rows <= 0 || cols <= 0 || chunk_w <= 0 || n_adapters < 0 || max_rank < 0) return 0;
     if (tokens > ((int64_t)1 << 31) - 1 || rows > (int64_t)1 << 31 || cols > (int64_t)1 << 31 || max_rank > WINDQ_MAX_RANK) return 0;
     if (n_adapters == 0) max_rank = 0;
-    return grad != 0 ? grad_ws_bytes(dtype, tokens, rows, cols, n_adapters, max_rank) : project_ws(dtype, tokens, cols, max_rank).total;
+    return grad != 0 ? grad_ws_bytes(dtype, tokens, rows, cols, n_adapters, max_rank) : project_ws(dtype, tokens, rows, cols, chunk_w, max_rank).total;
 }
 
 extern "C" int windq_project(const windq_packed* P, const windq_mat* X, const windq_adapters* adapters, const int32_t* adapter_of,
@@ -329,7 +374,7 @@ extern "C" int windq_project(const windq_packed* P, const windq_mat* X, const wi
     if (X->rows == 0) return WINDQ_OK;
     if (X->rows * Q.P.rows > (int64_t)0x7fffffff) return WINDQ_ESHAPE;
     if (Y == nullptr || !aligned(Y, eb)) return WINDQ_EINVAL;
-    const ProjectWs at = project_ws(X->dtype, X->rows, Q.P.cols, adapters != nullptr ? Q.A.max_rank : 0);
+    const ProjectWs at = project_ws(X->dtype, X->rows, Q.P.rows, Q.P.cols, Q.P.G, adapters != nullptr ? Q.A.max_rank : 0);
     if (ws == nullptr || ws_bytes < at.total) return WINDQ_EWORKSPACE;
     if (!aligned(ws, 256)) return WINDQ_EINVAL;
     Q.X = static_cast<const uint16_t*>(X->data);

@@ -1,0 +1,435 @@
+// windq_project for many tokens: tiles of 256 rows x 128 tokens.
+//
+// Bound by the matrix instructions once a tile's codes are unpacked often enough: 2 T rows cols operations against some 1.2 vector
+// instructions per weight and 64 tokens.  Eight wavefronts, four along the rows by two along the tokens, have 64 x 64 results
+// each as 2 x 2 fragments of 32x32x16 instructions, two wavefronts per SIMD so that one's unpacking runs under the other's matrix
+// instructions.  Weights never enter LDS: a lane holds one row of a fragment, and which columns its half of the wavefront takes is free as
+// long as X's operand does the same, so it takes half a k-block's columns in a row, whose codes are up to 64 contiguous bytes.
+//   X goes to LDS by direct loads, 128 tokens x one k-block, twice (the next one loads while this one is used).  A token's sixteen
+// 16-byte slots are exchanged by the token's low bits, so that 32 lanes reading 32 tokens' same slot meet all banks.
+//   A k-block's sum over f x is scaled by its group's scale and added to the total in registers: 64 multiply-adds beside
+// 32 instructions of 16 K operations.  beta sum x for all k-blocks is a product of its own at the end, with K = k-blocks: both factors as three
+// bfloat16 terms, six products in eight of an instruction's sixteen k, so one instruction does two k-blocks.
+//   Trits and 3-bit codes are laid out as 2- and 4-bit fields before (by the kernel that sums x): a row of them is visited by
+// T / 128 workgroups, and taking trits apart costs more than everything else in the loop.
+#pragma once
+
+#include "windq_adapters.hpp"
+
+namespace windq {
+
+constexpr int PT_ROWS = 256, PT_TOKENS = 128, PT_THREADS = 512;
+constexpr int PT_STRIP = 64;                               // rows of a unit that one workgroup lays out
+
+// Where a unit's fields begin in the code stream, or, with LAID set, in the workspace; and what they are (kind, top byte): 0 skip, 1: 8 bits,
+// 2: 4 bits, 4: 2 bits, 5: trits as 2 bits, 6: 1 bit.
+typedef unsigned long long UnitWord;
+constexpr UnitWord PT_LAID = 1ull << 55, PT_OFFSET = PT_LAID - 1;
+
+struct TileArgs {
+    PackArgs P;
+    const uint16_t* X;         // bfloat16, or the first of three planes
+    int64_t ldx, plane;
+    const void* raw;
+    int64_t ld_raw;
+    int64_t T;
+    void* Y;
+    int64_t ldy;
+    const float* h;            // or null: no adapters
+    AdapterArgs A;
+    uint8_t* fields;           // [U][R_u * G / 2] trits and 3-bit codes as fields
+    UnitWord* unit;            // [U]
+    uint4* xs;                 // [k-blocks][T] sum of x as terms
+    int32_t n_kb;              // k-blocks
+    uint32_t row_blocks;
+};
+
+// Columns of a k-block / 16, or 0 where the tiles do not fit the shape.
+inline int tile_steps(const PackArgs& P) {
+    if (P.rows % 8 != 0 || P.rows < PT_STRIP || (P.R_u != P.rows && P.R_u % PT_STRIP != 0)) return 0;
+    if (P.G % 128 == 0) return 8;
+    if (P.G % 96 == 0) return 6;
+    if (P.G % 64 == 0) return 4;
+    return 0;
+}
+
+#ifdef __HIPCC__
+
+// Workgroups [0, strips): fields of trits and 3-bit codes, and every unit's word.  The others: sums of x over k-blocks.
+template <typename XT, int S>
+__global__ __launch_bounds__(256) void tiles_prepare_kernel(const TileArgs Q, const int64_t strips) {
+    __shared__ uint16_t trits_of[256];
+    const PackArgs& P = Q.P;
+    if (blockIdx.x >= strips) {
+        const int64_t i = (blockIdx.x - strips) * 256 + threadIdx.x;
+        const int32_t kb = (int32_t)(i / Q.T);
+        const int64_t t = i - (int64_t)kb * Q.T;
+        if (kb >= Q.n_kb) return;
+        const XT* __restrict__ const x = static_cast<const XT*>(Q.raw) + t * Q.ld_raw + (int64_t)kb * (16 * S);
+        float sum = 0.0f;
+#pragma unroll
+        for (int o = 0; o < 2 * S; ++o) {
+            float v[8];
+            load8(x + o * 8, v);
+            sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        }
+        uint32_t hi, mid, lo;
+        split3(sum, hi, mid, lo);
+        Q.xs[i] = make_uint4(hi | mid << 16, hi | lo << 16, hi | mid << 16, 0u);
+        return;
+    }
+    const int64_t per_unit = (P.R_u + PT_STRIP - 1) / PT_STRIP;
+    const int64_t u = blockIdx.x / per_unit, strip = blockIdx.x - u * per_unit;
+    int64_t base;
+    const int a = pk_action(P, u, base);
+    const bool lay = a == 3 || a == 5;
+    uint8_t* __restrict__ const to = Q.fields + u * (P.R_u * P.G / 2);
+    if (strip == 0 && threadIdx.x == 0) {
+        const UnitWord at = lay ? (UnitWord)(to - Q.fields) | PT_LAID : (UnitWord)base;
+        Q.unit[u] = a == 0 ? 0ull : at | (UnitWord)(a == 3 ? 2 : a) << 56;
+    }
+    if (!lay) return;
+    if (a == 5) {
+        trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
+        __syncthreads();
+    }
+    const int32_t O = P.G >> 3;
+    const int64_t nb = pk_bytes_per_group(a, P.G);
+    const int64_t left = P.R_u - strip * PT_STRIP;
+    const int32_t total = (int32_t)(left < PT_STRIP ? left : PT_STRIP) * O;
+    for (int32_t i = threadIdx.x; i < total; i += 256) {
+        const int32_t r = i / O, o = i - r * O;
+        const int64_t lrow = strip * PT_STRIP + r;
+        const uint8_t* __restrict__ const row = P.codes + base + lrow * nb;
+        if (a == 5) {
+            reinterpret_cast<uint16_t*>(to)[lrow * O + o] = (uint16_t)octet_trits(row, o, trits_of);
+        } else {
+            const uint8_t* p = row + o * 3;
+            const uint32_t v = (uint32_t)p[0] | (uint32_t)p[1] << 8 | (uint32_t)p[2] << 16;
+            uint32_t w = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) w |= ((v >> (3 * k)) & 7u) << (4 * k);
+            reinterpret_cast<uint32_t*>(to)[lrow * O + o] = w;
+        }
+    }
+}
+
+// The fields of one lane's half row of a k-block, S octets, as loaded ahead (8 bits and skip are read where they are used).
+template <int S>
+__device__ __forceinline__ void tile_fetch(int kind, const uint8_t* __restrict__ p, uint32_t (&raw)[8]) {
+    if (kind == 6) __builtin_memcpy(raw, p, S);
+    else if (kind == 2) __builtin_memcpy(raw, p, 4 * S);
+    else if (kind == 4 || kind == 5) __builtin_memcpy(raw, p, 2 * S);
+}
+
+template <int KIND>
+__device__ __forceinline__ uint4 tile_octet(const uint32_t (&raw)[8], int s) {
+    if constexpr (KIND == 6) return fields1(raw[s >> 2] >> (8 * (s & 3)));
+    else if constexpr (KIND == 2) return fields4(raw[s]);
+    else return fields2((s & 1) != 0 ? raw[s >> 1] >> 16 : raw[s >> 1] & 0xffffu);
+}
+
+typedef const __attribute__((address_space(1))) void* global_ptr;
+typedef __attribute__((address_space(3))) void* lds_ptr;
+
+template <typename YT, int S>
+__global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArgs Q) {
+    constexpr int NP = sizeof(YT) == 4 ? 3 : 1;
+    __shared__ uint4 xt[2][PT_TOKENS * 16];
+    __shared__ float st[2][PT_ROWS];
+    const PackArgs& P = Q.P;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, sub = lane & 31, hh = lane >> 5;
+    const int wr = wave >> 1, wt = wave & 1;
+    // Consecutive workgroups land on the eight XCDs in turn; each XCD gets a run of tiles that share tokens.
+    const uint32_t n_tiles = gridDim.x, per = n_tiles >> 3;
+    const uint32_t tile = blockIdx.x < per * 8 ? (blockIdx.x & 7) * per + (blockIdx.x >> 3) : blockIdx.x;
+    const uint32_t tb = tile / Q.row_blocks;
+    const int64_t row0 = (int64_t)(tile - tb * Q.row_blocks) * PT_ROWS, t0 = (int64_t)tb * PT_TOKENS;
+
+    // X: four of a tile's slots a thread; slot p of token n holds the octet of slot p ^ (n & 15)
+    const uint16_t* xsrc[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int n = k * 32 + (tid >> 4), slot = (tid & 15) ^ (n & 15);
+        const int s = (slot & 7) < S ? (slot & 7) : 0;
+        const int64_t t = t0 + n;
+        xsrc[k] = Q.X + (t < Q.T ? t : Q.T - 1) * Q.ldx + ((slot >> 3) * S + s) * 8;
+    }
+    // rows: a lane's row of each fragment; the wavefront's unit row block
+    const int64_t wrow = row0 + wr * 64;
+    const int64_t rb = (wrow < P.rows ? wrow : P.rows - 1) / P.R_u;
+    int64_t lrow[2];
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+        const int64_t row = wrow + f * 32 + sub;
+        lrow[f] = (row < P.rows ? row : P.rows - 1) - rb * P.R_u;
+    }
+    // scales: one row a thread (the first 256)
+    const int64_t srow = row0 + (tid & 255) < P.rows ? row0 + (tid & 255) : P.rows - 1;
+    const int64_t srb = srow / P.R_u, slrow = srow - srb * P.R_u;
+    const int32_t per_chunk = P.G / (16 * S);
+
+    auto word_of = [&](int32_t j) {
+        const UnitWord* w = Q.unit + (rb * P.n_chunks + j);
+        return *w;
+    };
+    auto start_of = [&](UnitWord word) { return ((word & PT_LAID) != 0 ? Q.fields : P.codes) + (word & PT_OFFSET); };
+    auto fetch = [&](UnitWord word, int32_t kb, uint32_t (&raw)[2][8]) {
+        const int kind = (int)(word >> 56);
+        const uint8_t* const base = start_of(word);
+        const int32_t j = kb / per_chunk, c = (kb - j * per_chunk) * (16 * S) + hh * (8 * S);
+        const int shift = kind == 6 ? 3 : (kind == 2 ? 1 : 2);
+#pragma unroll
+        for (int f = 0; f < 2; ++f) tile_fetch<S>(kind, base + ((lrow[f] * P.G + c) >> shift), raw[f]);
+    };
+    auto load_tile = [&](int32_t it, int buf) {
+        const int32_t kb = it / NP, p = it - kb * NP;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            __builtin_amdgcn_global_load_lds((global_ptr)(xsrc[k] + p * Q.plane + (int64_t)kb * (16 * S)), (lds_ptr)&xt[buf][k * 512 + wave * 64], 16, 0, 0);
+    };
+    auto load_scale = [&](int32_t kb, int buf) {
+        if (tid < PT_ROWS) {
+            const int64_t u = srb * P.n_chunks + kb / per_chunk;
+            const float s = P.scale[u * P.R_u + slrow];
+            st[buf][tid] = (Q.unit[u] >> 56) == 0 ? 1.0f : s;
+        }
+    };
+
+    f32x16 tot[2][2] = {};
+    uint32_t raw[2][8] = {};
+    const int32_t n_it = Q.n_kb * NP;
+    UnitWord word = word_of(0);
+    load_tile(0, 0);
+    load_scale(0, 0);
+    fetch(word, 0, raw);
+    f32x16 acc[2][2];
+    for (int32_t it = 0; it < n_it; ++it) {
+        const int32_t kb = it / NP;
+        const int buf = it & 1;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        const int kind = __builtin_amdgcn_readfirstlane((int)(word >> 56));
+        UnitWord next_word = word;
+        uint32_t next[2][8];
+        const int32_t nkb = (it + 1) / NP;
+        if (it + 1 < n_it) {
+            load_tile(it + 1, buf ^ 1);
+            if (NP == 1 || nkb != kb) {
+                load_scale(nkb, nkb & 1);
+                next_word = word_of(nkb / per_chunk);
+                fetch(next_word, nkb, next);
+            }
+        }
+        if (NP == 1 || it == kb * NP) {
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) acc[f][n] = f32x16{};
+        }
+        const uint32_t xb = (uint32_t)buf * sizeof(xt[0]) + (wt * 64 + sub) * 256 + (((hh * 8) ^ (sub & 15)) << 4);
+        auto step = [&](int s, const uint4 (&a)[2]) {
+            const char* const at = reinterpret_cast<const char*>(xt) + (xb ^ (uint32_t)(s << 4));
+            const bf16x8 b0 = as_bf16x8(*reinterpret_cast<const uint4*>(at)), b1 = as_bf16x8(*reinterpret_cast<const uint4*>(at + 32 * 256));
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+                acc[f][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a[f]), b0, acc[f][0], 0, 0, 0);
+                acc[f][1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a[f]), b1, acc[f][1], 0, 0, 0);
+            }
+        };
+        if (kind == 6) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) step(s, {tile_octet<6>(raw[0], s), tile_octet<6>(raw[1], s)});
+        } else if (kind == 4 || kind == 5) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) step(s, {tile_octet<4>(raw[0], s), tile_octet<4>(raw[1], s)});
+        } else if (kind == 2) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) step(s, {tile_octet<2>(raw[0], s), tile_octet<2>(raw[1], s)});
+        } else if (kind == 1) {
+            const uint8_t* const base = start_of(word);
+            const int32_t c = (kb - kb / per_chunk * per_chunk) * (16 * S) + hh * (8 * S);
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                uint4 a[2];
+#pragma unroll
+                for (int f = 0; f < 2; ++f) {
+                    const uint2 v = *reinterpret_cast<const uint2*>(base + lrow[f] * P.G + c + s * 8);
+                    a[f] = fields8(v.x, v.y);
+                }
+                step(s, a);
+            }
+        } else {
+            const int64_t c = (int64_t)kb * (16 * S) + hh * (8 * S);
+            const int terms = P.w_f32 != 0 ? 3 - (NP == 1 ? 0 : it - kb * NP) : 1;       // of a weight's terms with this plane's: those that count
+            for (int term = 0; term < terms; ++term) {
+#pragma unroll 2
+                for (int s = 0; s < S; ++s)
+                    step(s, {skip_octet(P, rb * P.R_u + lrow[0], c + s * 8, term), skip_octet(P, rb * P.R_u + lrow[1], c + s * 8, term)});
+            }
+        }
+        if (NP == 1 || it == kb * NP + NP - 1) {
+            const float* const sc = st[kb & 1] + wr * 64 + 4 * hh;
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float4 a = *reinterpret_cast<const float4*>(sc + f * 32 + g * 8);
+                    const float av[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int n = 0; n < 2; ++n) tot[f][n][g * 4 + i] = fmaf(av[i], acc[f][n][g * 4 + i], tot[f][n][g * 4 + i]);
+                }
+        }
+        if (it + 1 < n_it && (NP == 1 || nkb != kb)) {
+            word = next_word;
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) raw[f][i] = next[f][i];
+        }
+    }
+
+    // beta sum x, two k-blocks an instruction
+    int64_t tok[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        tok[n] = t0 + wt * 64 + n * 32 + sub;
+        if (tok[n] >= Q.T) tok[n] = Q.T - 1;
+    }
+    for (int32_t k2 = 0; k2 < Q.n_kb; k2 += 2) {
+        const int32_t kb = k2 + hh;
+        uint4 b[2] = {}, a[2] = {};
+        if (kb < Q.n_kb) {
+            const int64_t u = rb * P.n_chunks + kb / per_chunk;
+            const int act = P.action[u];
+            const bool skip = (Q.unit[u] >> 56) == 0;
+#pragma unroll
+            for (int n = 0; n < 2; ++n) b[n] = Q.xs[(int64_t)kb * Q.T + tok[n]];
+#pragma unroll
+            for (int f = 0; f < 2; ++f) {
+                const int64_t g = u * P.R_u + lrow[f];
+                float alpha, beta;
+                pk_affine(skip ? 0 : (act == 3 ? 2 : act), P.scale[g], P.offset[g], alpha, beta);
+                uint32_t hi, mid, lo;
+                split3(beta, hi, mid, lo);
+                a[f] = make_uint4(hi | hi << 16, mid | hi << 16, lo | mid << 16, 0u);
+            }
+        }
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int n = 0; n < 2; ++n) tot[f][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a[f]), as_bf16x8(b[n]), tot[f][n], 0, 0, 0);
+    }
+
+    // what is not finite so far: weight by weight
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) bad |= !isfinite(tot[f][n][i]);
+            if (__any(bad)) {
+                for (int i = 0; i < 16; ++i) {
+                    const int64_t row = wrow + f * 32 + (i >> 2) * 8 + hh * 4 + (i & 3), t = t0 + wt * 64 + n * 32 + sub;
+                    float v = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) v = i == k ? tot[f][n][k] : v;
+                    if (!isfinite(v) && row < P.rows && t < Q.T) v = (float)pk_slow_dot(P, row, static_cast<const YT*>(Q.raw) + t * Q.ld_raw);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) tot[f][n][k] = i == k ? v : tot[f][n][k];
+                }
+            }
+        }
+
+    // adapters: for each one among the wavefront's tokens, its B against the others' zeros and its own tokens' h
+    if (Q.h != nullptr) {
+        constexpr int TA = sizeof(YT) == 4 ? 3 : 1, TH = sizeof(YT) == 4 ? 3 : 2;       // terms of B and of alpha h
+        const int64_t t = t0 + wt * 64 + lane;
+        const int32_t id = t < Q.T ? Q.A.of[t] : -1;
+        uint64_t left = __ballot(id >= 0 && id < Q.A.n);
+        while (left != 0) {
+            const int32_t k = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+            const uint64_t mine = __ballot(id == k);
+            left &= ~mine;
+            const int32_t rank = adapter_rank(Q.A, k);
+            const float factor = Q.A.alpha != nullptr ? Q.A.alpha[k] : 1.0f;
+            for (int32_t r0 = 0; r0 < rank; r0 += 16) {
+                const int32_t r = r0 + hh * 8;
+                uint4 bt[TH][2], at[TA][2];
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    const bool has = ((mine >> (n * 32 + sub)) & 1ull) != 0 && r < rank;
+                    float v[8] = {};
+                    if (has) load8(Q.h + (t0 + wt * 64 + n * 32 + sub) * Q.A.max_rank + r, v);
+                    uint32_t w[3][8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) split3(r + i < rank ? factor * v[i] : 0.0f, w[0][i], w[1][i], w[2][i]);
+#pragma unroll
+                    for (int m = 0; m < TH; ++m) bt[m][n] = make_uint4(w[m][0] | w[m][1] << 16, w[m][2] | w[m][3] << 16, w[m][4] | w[m][5] << 16, w[m][6] | w[m][7] << 16);
+                }
+#pragma unroll
+                for (int f = 0; f < 2; ++f) {
+                    const int64_t row = rb * P.R_u + lrow[f];
+                    float v[8] = {};
+                    if (r < rank) load8(static_cast<const YT*>(Q.A.b) + ((int64_t)k * P.rows + row) * Q.A.max_rank + r, v);
+                    uint32_t w[3][8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float x = r + i < rank ? v[i] : 0.0f;
+                        if (TA == 1) w[0][i] = __float_as_uint(x) >> 16;
+                        else split3(x, w[0][i], w[1][i], w[2][i]);
+                    }
+#pragma unroll
+                    for (int m = 0; m < TA; ++m) at[m][f] = make_uint4(w[m][0] | w[m][1] << 16, w[m][2] | w[m][3] << 16, w[m][4] | w[m][5] << 16, w[m][6] | w[m][7] << 16);
+                }
+#pragma unroll
+                for (int ma = 0; ma < TA; ++ma)
+#pragma unroll
+                    for (int mh = 0; mh < TH; ++mh)
+                        if (ma + mh < 3) {
+#pragma unroll
+                            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                                for (int n = 0; n < 2; ++n)
+                                    tot[f][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(at[ma][f]), as_bf16x8(bt[mh][n]), tot[f][n], 0, 0, 0);
+                        }
+            }
+        }
+    }
+
+    YT* __restrict__ const Y = static_cast<YT*>(Q.Y);
+    const bool whole = (Q.ldy & 3) == 0 && (reinterpret_cast<uintptr_t>(Y) & (4 * sizeof(YT) - 1)) == 0;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        const int64_t t = t0 + wt * 64 + n * 32 + sub;
+        if (t >= Q.T) continue;
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int64_t row = wrow + f * 32 + g * 8 + hh * 4;
+                if (row >= P.rows) continue;               // rows come in eights
+                YT* __restrict__ const o = Y + t * Q.ldy + row;
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = tot[f][n][g * 4 + i];
+                if (whole) {
+                    if constexpr (sizeof(YT) == 4) *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+                    else *reinterpret_cast<uint2*>(o) = make_uint2(f32_to_bf16_bits(v[0]) | f32_to_bf16_bits(v[1]) << 16, f32_to_bf16_bits(v[2]) | f32_to_bf16_bits(v[3]) << 16);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if constexpr (sizeof(YT) == 4) o[i] = v[i];
+                        else o[i] = (uint16_t)f32_to_bf16_bits(v[i]);
+                    }
+                }
+            }
+    }
+}
+
+#endif  // __HIPCC__
+
+}  // namespace windq
