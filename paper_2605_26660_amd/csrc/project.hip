@@ -279,7 +279,7 @@ ProjectWs project_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32
     w.planes = take(dtype == WINDQ_F32 ? (size_t)(3 * T * cols) * 2 : 0);
     w.h = take((size_t)(T * max_rank) * 4);
     const bool many = T > PROJECT_FEW;
-    w.fields = take(many ? (size_t)(rows * cols) / 2 : 0);
+    w.fields = take(many ? (size_t)(rows * cols) / (G % 128 == 0 || G == 96 || G == 64 ? 2 : 1) : 0);
     w.unit = take(many ? (size_t)((rows + PT_STRIP - 1) / PT_STRIP) * (size_t)(cols / G) * sizeof(UnitWord) : 0);
     w.xs = take(many ? (size_t)(cols / 64) * (size_t)T * 16 : 0);
     w.total = at == 0 ? 256 : at;
@@ -304,6 +304,7 @@ int launch_tiles(const ProjectArgs& Q, char* ws, const ProjectWs& at, hipStream_
     A.fields = reinterpret_cast<uint8_t*>(ws + at.fields);
     A.unit = reinterpret_cast<UnitWord*>(ws + at.unit);
     A.xs = reinterpret_cast<uint4*>(ws + at.xs);
+    A.unit_fields = Q.P.R_u * Q.P.G / (tile_natural(Q.P.G, S) ? 2 : 1);
     A.n_kb = (int32_t)(Q.P.cols / (16 * S));
     A.row_blocks = (uint32_t)((Q.P.rows + PT_ROWS - 1) / PT_ROWS);
     const int64_t strips = (Q.P.rows / Q.P.R_u) * Q.P.n_chunks * ((Q.P.R_u + PT_STRIP - 1) / PT_STRIP);

@@ -3,9 +3,10 @@
 // Bound by the matrix instructions once a tile's codes are unpacked often enough: 2 T rows cols operations against some 1.2 vector
 // instructions per weight and 64 tokens.  Eight wavefronts, four along the rows by two along the tokens, have 64 x 64 results
 // each as 2 x 2 fragments of 32x32x16 instructions, two wavefronts per SIMD so that one's unpacking runs under the other's matrix
-// instructions.  Weights never enter LDS: a lane holds one row of a fragment, and which columns its half of the wavefront takes is free as
+// instructions.  Weights enter LDS packed: a lane holds one row of a fragment, and which columns its half of the wavefront takes is free as
 // long as X's operand does the same, so it takes half a k-block's columns in a row, whose codes are up to 64 contiguous bytes.
-//   X goes to LDS by direct loads, 128 tokens x one k-block, twice (the next one loads while this one is used).  A token's sixteen
+//   X and the codes go to LDS by direct loads, one k-block ahead (the next one's load while this one's are used): 128 tokens' octets, and
+// for each pair of wavefronts their 64 rows' fields, up to 128 bytes a row.  No register waits for them.  A token's sixteen
 // 16-byte slots are exchanged by the token's low bits, so that 32 lanes reading 32 tokens' same slot meet all banks.
 //   A k-block's sum over f x is scaled by its group's scale and added to the total in registers: 64 multiply-adds beside
 // 32 instructions of 16 K operations.  beta sum x for all k-blocks is a product of its own at the end, with K = k-blocks: both factors as three
@@ -37,12 +38,16 @@ struct TileArgs {
     int64_t ldy;
     const float* h;            // or null: no adapters
     AdapterArgs A;
-    uint8_t* fields;           // [U][R_u * G / 2] trits and 3-bit codes as fields
+    uint8_t* fields;           // [U][k-blocks of a chunk][R_u] fields of the units that are laid out anew
+    int64_t unit_fields;       // bytes of a unit's
     UnitWord* unit;            // [U]
     uint4* xs;                 // [k-blocks][T] sum of x as terms
     int32_t n_kb;              // k-blocks
     uint32_t row_blocks;
 };
+
+// Whether a row's fields of a k-block can be loaded from the code stream as they lie: pieces of 16 bytes, or whole rows one behind the other.
+__host__ __device__ inline bool tile_natural(int32_t G, int S) { return S == 8 || G == 16 * S; }
 
 // Columns of a k-block / 16, or 0 where the tiles do not fit the shape.
 inline int tile_steps(const PackArgs& P) {
@@ -82,8 +87,8 @@ __global__ __launch_bounds__(256) void tiles_prepare_kernel(const TileArgs Q, co
     const int64_t u = blockIdx.x / per_unit, strip = blockIdx.x - u * per_unit;
     int64_t base;
     const int a = pk_action(P, u, base);
-    const bool lay = a == 3 || a == 5;
-    uint8_t* __restrict__ const to = Q.fields + u * (P.R_u * P.G / 2);
+    const bool lay = a == 3 || a == 5 || (a != 0 && !tile_natural(P.G, S));
+    uint8_t* __restrict__ const to = Q.fields + u * Q.unit_fields;
     if (strip == 0 && threadIdx.x == 0) {
         const UnitWord at = lay ? (UnitWord)(to - Q.fields) | PT_LAID : (UnitWord)base;
         Q.unit[u] = a == 0 ? 0ull : at | (UnitWord)(a == 3 ? 2 : a) << 56;
@@ -98,36 +103,68 @@ __global__ __launch_bounds__(256) void tiles_prepare_kernel(const TileArgs Q, co
     const int64_t left = P.R_u - strip * PT_STRIP;
     const int32_t total = (int32_t)(left < PT_STRIP ? left : PT_STRIP) * O;
     for (int32_t i = threadIdx.x; i < total; i += 256) {
-        const int32_t r = i / O, o = i - r * O;
+        const int32_t r = i / O, o = i - r * O, c = o / (2 * S);
         const int64_t lrow = strip * PT_STRIP + r;
+        const int64_t at = (c * P.R_u + lrow) * (2 * S) + (o - c * 2 * S);      // octets before this one
         const uint8_t* __restrict__ const row = P.codes + base + lrow * nb;
         if (a == 5) {
-            reinterpret_cast<uint16_t*>(to)[lrow * O + o] = (uint16_t)octet_trits(row, o, trits_of);
-        } else {
+            reinterpret_cast<uint16_t*>(to)[at] = (uint16_t)octet_trits(row, o, trits_of);
+        } else if (a == 3) {
             const uint8_t* p = row + o * 3;
             const uint32_t v = (uint32_t)p[0] | (uint32_t)p[1] << 8 | (uint32_t)p[2] << 16;
             uint32_t w = 0;
 #pragma unroll
             for (int k = 0; k < 8; ++k) w |= ((v >> (3 * k)) & 7u) << (4 * k);
-            reinterpret_cast<uint32_t*>(to)[lrow * O + o] = w;
+            reinterpret_cast<uint32_t*>(to)[at] = w;
+        } else {
+            const int b = a == 1 ? 8 : (a == 2 ? 4 : (a == 4 ? 2 : 1));
+            for (int k = 0; k < b; ++k) to[at * b + k] = row[o * b + k];
         }
     }
 }
 
-// The fields of one lane's half row of a k-block, S octets, as loaded ahead (8 bits and skip are read where they are used).
-template <int S>
-__device__ __forceinline__ void tile_fetch(int kind, const uint8_t* __restrict__ p, uint32_t (&raw)[8]) {
-    if (kind == 6) __builtin_memcpy(raw, p, S);
-    else if (kind == 2) __builtin_memcpy(raw, p, 4 * S);
-    else if (kind == 4 || kind == 5) __builtin_memcpy(raw, p, 2 * S);
-}
+// Masks and leading ones in registers: an and-or takes no constant of its own.
+struct TileBits {
+    uint32_t mask4 = 0x00780078u, one4 = 0x41804180u, mask2 = 0x00600060u, one2 = 0x40804080u, mask1 = 0x80008000u, one1 = 0x3f803f80u;
+    __device__ __forceinline__ TileBits() { asm volatile("" : "+s"(mask4), "+v"(one4), "+s"(mask2), "+v"(one2), "+s"(mask1), "+v"(one1)); }
+};
 
+// Octet s of a lane's half row of fields in LDS.
 template <int KIND>
-__device__ __forceinline__ uint4 tile_octet(const uint32_t (&raw)[8], int s) {
-    if constexpr (KIND == 6) return fields1(raw[s >> 2] >> (8 * (s & 3)));
-    else if constexpr (KIND == 2) return fields4(raw[s]);
-    else return fields2((s & 1) != 0 ? raw[s >> 1] >> 16 : raw[s >> 1] & 0xffffu);
-}
+struct TileFields {
+    uint32_t raw[KIND == 1 ? 16 : (KIND == 2 ? 8 : (KIND == 4 ? 4 : 2))];
+    template <int S>
+    __device__ __forceinline__ void read(const char* p) {
+        constexpr int bytes = S * (KIND == 1 ? 8 : (KIND == 2 ? 4 : (KIND == 4 ? 2 : 1)));
+        if constexpr (bytes % 16 == 0) {
+#pragma unroll
+            for (int i = 0; i < bytes / 16; ++i) {
+                const uint4 v = *reinterpret_cast<const uint4*>(p + 16 * i);
+                raw[4 * i] = v.x; raw[4 * i + 1] = v.y; raw[4 * i + 2] = v.z; raw[4 * i + 3] = v.w;
+            }
+        } else if constexpr (bytes % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < bytes / 4; ++i) raw[i] = *reinterpret_cast<const uint32_t*>(p + 4 * i);
+        } else {                                            // six octets of one bit: rows start on two bytes
+            const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+            raw[0] = (uint32_t)q[0] | (uint32_t)q[1] << 16;
+            raw[1] = q[2];
+        }
+    }
+    __device__ __forceinline__ uint4 octet(int s, const TileBits& C) const {
+        if constexpr (KIND == 1) return fields8(raw[2 * s], raw[2 * s + 1]);
+        else if constexpr (KIND == 2) {
+            const uint32_t v = raw[s], e = (v & 0xffffu) | v << 12, o = v >> 16 | (v >> 16) << 12;
+            return make_uint4(((e << 3) & C.mask4) | C.one4, ((e >> 5) & C.mask4) | C.one4, ((o << 3) & C.mask4) | C.one4, ((o >> 5) & C.mask4) | C.one4);
+        } else if constexpr (KIND == 4) {
+            const uint32_t v = (s & 1) != 0 ? raw[s >> 1] >> 16 : raw[s >> 1] & 0xffffu, t = v | v << 14;
+            return make_uint4(((t << 5) & C.mask2) | C.one2, ((t << 1) & C.mask2) | C.one2, ((t >> 3) & C.mask2) | C.one2, ((t >> 7) & C.mask2) | C.one2);
+        } else {                                            // minus the sign that fields1 gives: the scale has the other sign too
+            const uint32_t v = (raw[s >> 2] >> (8 * (s & 3))) & 0xffu, t = v | v << 15;
+            return make_uint4(((t << 15) & C.mask1) | C.one1, ((t << 13) & C.mask1) | C.one1, ((t << 11) & C.mask1) | C.one1, ((t << 9) & C.mask1) | C.one1);
+        }
+    }
+};
 
 typedef const __attribute__((address_space(1))) void* global_ptr;
 typedef __attribute__((address_space(3))) void* lds_ptr;
@@ -136,6 +173,7 @@ template <typename YT, int S>
 __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArgs Q) {
     constexpr int NP = sizeof(YT) == 4 ? 3 : 1;
     __shared__ uint4 xt[2][PT_TOKENS * 16];
+    __shared__ uint4 ct[2][4][512];                        // fields of 64 rows
     __shared__ float st[2][PT_ROWS];
     const PackArgs& P = Q.P;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, sub = lane & 31, hh = lane >> 5;
@@ -169,18 +207,31 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
     const int64_t srb = srow / P.R_u, slrow = srow - srb * P.R_u;
     const int32_t per_chunk = P.G / (16 * S);
 
-    auto word_of = [&](int32_t j) {
-        const UnitWord* w = Q.unit + (rb * P.n_chunks + j);
-        return *w;
+    auto word_of = [&](int32_t kb) {
+        const UnitWord w = Q.unit[rb * P.n_chunks + kb / per_chunk];
+        return (UnitWord)(uint32_t)__builtin_amdgcn_readfirstlane((int)(w >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)w);
     };
-    auto start_of = [&](UnitWord word) { return ((word & PT_LAID) != 0 ? Q.fields : P.codes) + (word & PT_OFFSET); };
-    auto fetch = [&](UnitWord word, int32_t kb, uint32_t (&raw)[2][8]) {
+    const int64_t lrow0 = ((wrow < P.rows ? wrow : P.rows - 1) - rb * P.R_u) & ~(int64_t)63;      // a wavefront past the last row loads the last ones
+    // The fields of the wavefront pair's rows: 16 S bits bytes / 8 a row, in pieces of 16 bytes, every other 64 of them by each of the two.
+    auto load_codes = [&](UnitWord word, int32_t kb, int buf) {
         const int kind = (int)(word >> 56);
-        const uint8_t* const base = start_of(word);
-        const int32_t j = kb / per_chunk, c = (kb - j * per_chunk) * (16 * S) + hh * (8 * S);
-        const int shift = kind == 6 ? 3 : (kind == 2 ? 1 : 2);
-#pragma unroll
-        for (int f = 0; f < 2; ++f) tile_fetch<S>(kind, base + ((lrow[f] * P.G + c) >> shift), raw[f]);
+        if (kind == 0) return;
+        const int bits = kind == 1 ? 8 : (kind == 2 ? 4 : (kind == 6 ? 1 : 2));
+        const int32_t seg = 2 * S * bits, c = kb - kb / per_chunk * per_chunk;         // bytes of a row
+        const bool laid = (word & PT_LAID) != 0;
+        const int64_t step = laid ? seg : (int64_t)seg * per_chunk;                    // from row to row
+        const int64_t first = laid ? (int64_t)c * P.R_u * seg : (int64_t)c * seg;
+        const uint8_t* const base = (laid ? Q.fields : P.codes) + (word & PT_OFFSET) + first;
+        const int64_t rows_left = P.R_u - lrow0;
+        const int32_t pieces = 4 * seg, have = rows_left < 64 ? (int32_t)rows_left * seg >> 4 : pieces;
+        for (int32_t i0 = wt * 64; i0 < pieces; i0 += 128) {
+            int32_t i = i0 + lane;
+            i = i < have ? i : have - 1;
+            int64_t at;
+            if (step == seg) at = lrow0 * seg + (int64_t)i * 16;
+            else at = (lrow0 + i / (seg >> 4)) * step + (i % (seg >> 4)) * 16;         // seg is 16 bits there
+            __builtin_amdgcn_global_load_lds((global_ptr)(base + at), (lds_ptr)&ct[buf][wr][i0], 16, 0, 0);
+        }
     };
     auto load_tile = [&](int32_t it, int buf) {
         const int32_t kb = it / NP, p = it - kb * NP;
@@ -192,33 +243,33 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
         if (tid < PT_ROWS) {
             const int64_t u = srb * P.n_chunks + kb / per_chunk;
             const float s = P.scale[u * P.R_u + slrow];
-            st[buf][tid] = (Q.unit[u] >> 56) == 0 ? 1.0f : s;
+            const int kind = (int)(Q.unit[u] >> 56);
+            st[buf][tid] = kind == 0 ? 1.0f : (kind == 6 ? -s : s);
         }
     };
 
     f32x16 tot[2][2] = {};
-    uint32_t raw[2][8] = {};
+    const TileBits bits;
     const int32_t n_it = Q.n_kb * NP;
     UnitWord word = word_of(0);
     load_tile(0, 0);
+    load_codes(word, 0, 0);
     load_scale(0, 0);
-    fetch(word, 0, raw);
     f32x16 acc[2][2];
     for (int32_t it = 0; it < n_it; ++it) {
         const int32_t kb = it / NP;
         const int buf = it & 1;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        const int kind = __builtin_amdgcn_readfirstlane((int)(word >> 56));
+        const int kind = (int)(word >> 56);
         UnitWord next_word = word;
-        uint32_t next[2][8];
         const int32_t nkb = (it + 1) / NP;
         if (it + 1 < n_it) {
             load_tile(it + 1, buf ^ 1);
             if (NP == 1 || nkb != kb) {
+                next_word = word_of(nkb);
+                load_codes(next_word, nkb, nkb & 1);
                 load_scale(nkb, nkb & 1);
-                next_word = word_of(nkb / per_chunk);
-                fetch(next_word, nkb, next);
             }
         }
         if (NP == 1 || it == kb * NP) {
@@ -228,6 +279,7 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
                 for (int n = 0; n < 2; ++n) acc[f][n] = f32x16{};
         }
         const uint32_t xb = (uint32_t)buf * sizeof(xt[0]) + (wt * 64 + sub) * 256 + (((hh * 8) ^ (sub & 15)) << 4);
+        const char* const cb = reinterpret_cast<const char*>(ct[kb & 1][wr]);
         auto step = [&](int s, const uint4 (&a)[2]) {
             const char* const at = reinterpret_cast<const char*>(xt) + (xb ^ (uint32_t)(s << 4));
             const bf16x8 b0 = as_bf16x8(*reinterpret_cast<const uint4*>(at)), b1 = as_bf16x8(*reinterpret_cast<const uint4*>(at + 32 * 256));
@@ -237,28 +289,21 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
                 acc[f][1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a[f]), b1, acc[f][1], 0, 0, 0);
             }
         };
+        auto steps = [&](auto fields, int row_bytes) {
+            decltype(fields) v[2];
+            v[0].template read<S>(cb + sub * row_bytes + hh * (row_bytes >> 1));
+            v[1].template read<S>(cb + (32 + sub) * row_bytes + hh * (row_bytes >> 1));
+#pragma unroll
+            for (int s = 0; s < S; ++s) step(s, {v[0].octet(s, bits), v[1].octet(s, bits)});
+        };
         if (kind == 6) {
-#pragma unroll
-            for (int s = 0; s < S; ++s) step(s, {tile_octet<6>(raw[0], s), tile_octet<6>(raw[1], s)});
+            steps(TileFields<6>(), 2 * S);
         } else if (kind == 4 || kind == 5) {
-#pragma unroll
-            for (int s = 0; s < S; ++s) step(s, {tile_octet<4>(raw[0], s), tile_octet<4>(raw[1], s)});
+            steps(TileFields<4>(), 4 * S);
         } else if (kind == 2) {
-#pragma unroll
-            for (int s = 0; s < S; ++s) step(s, {tile_octet<2>(raw[0], s), tile_octet<2>(raw[1], s)});
+            steps(TileFields<2>(), 8 * S);
         } else if (kind == 1) {
-            const uint8_t* const base = start_of(word);
-            const int32_t c = (kb - kb / per_chunk * per_chunk) * (16 * S) + hh * (8 * S);
-#pragma unroll
-            for (int s = 0; s < S; ++s) {
-                uint4 a[2];
-#pragma unroll
-                for (int f = 0; f < 2; ++f) {
-                    const uint2 v = *reinterpret_cast<const uint2*>(base + lrow[f] * P.G + c + s * 8);
-                    a[f] = fields8(v.x, v.y);
-                }
-                step(s, a);
-            }
+            steps(TileFields<1>(), 16 * S);
         } else {
             const int64_t c = (int64_t)kb * (16 * S) + hh * (8 * S);
             const int terms = P.w_f32 != 0 ? 3 - (NP == 1 ? 0 : it - kb * NP) : 1;       // of a weight's terms with this plane's: those that count
@@ -282,13 +327,7 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
                         for (int n = 0; n < 2; ++n) tot[f][n][g * 4 + i] = fmaf(av[i], acc[f][n][g * 4 + i], tot[f][n][g * 4 + i]);
                 }
         }
-        if (it + 1 < n_it && (NP == 1 || nkb != kb)) {
-            word = next_word;
-#pragma unroll
-            for (int f = 0; f < 2; ++f)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) raw[f][i] = next[f][i];
-        }
+        word = next_word;
     }
 
     // beta sum x, two k-blocks an instruction
