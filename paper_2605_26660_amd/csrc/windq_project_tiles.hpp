@@ -150,6 +150,10 @@ struct TileFields {
             raw[0] = (uint32_t)q[0] | (uint32_t)q[1] << 16;
             raw[1] = q[2];
         }
+        if constexpr (KIND == 6) {
+            raw[0] = ~raw[0];
+            raw[1] = ~raw[1];
+        }
     }
     __device__ __forceinline__ uint4 octet(int s, const TileBits& C) const {
         if constexpr (KIND == 1) return fields8(raw[2 * s], raw[2 * s + 1]);
@@ -159,7 +163,7 @@ struct TileFields {
         } else if constexpr (KIND == 4) {
             const uint32_t v = (s & 1) != 0 ? raw[s >> 1] >> 16 : raw[s >> 1] & 0xffffu, t = v | v << 14;
             return make_uint4(((t << 5) & C.mask2) | C.one2, ((t << 1) & C.mask2) | C.one2, ((t >> 3) & C.mask2) | C.one2, ((t >> 7) & C.mask2) | C.one2);
-        } else {                                            // minus the sign that fields1 gives: the scale has the other sign too
+        } else {                                            // of inverted bits: a set one is -1
             const uint32_t v = (raw[s >> 2] >> (8 * (s & 3))) & 0xffu, t = v | v << 15;
             return make_uint4(((t << 15) & C.mask1) | C.one1, ((t << 13) & C.mask1) | C.one1, ((t << 11) & C.mask1) | C.one1, ((t << 9) & C.mask1) | C.one1);
         }
@@ -202,77 +206,79 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
         const int64_t row = wrow + f * 32 + sub;
         lrow[f] = (row < P.rows ? row : P.rows - 1) - rb * P.R_u;
     }
-    // scales: one row a thread (the first 256)
-    const int64_t srow = row0 + (tid & 255) < P.rows ? row0 + (tid & 255) : P.rows - 1;
-    const int64_t srb = srow / P.R_u, slrow = srow - srb * P.R_u;
+    const int64_t lrow0 = ((wrow < P.rows ? wrow : P.rows - 1) - rb * P.R_u) & ~(int64_t)63;      // a wavefront past the last row loads the last ones
+    const int64_t rows_left = P.R_u - lrow0;
     const int32_t per_chunk = P.G / (16 * S);
+    const UnitWord* const words = Q.unit + rb * P.n_chunks;
 
-    auto word_of = [&](int32_t kb) {
-        const UnitWord w = Q.unit[rb * P.n_chunks + kb / per_chunk];
+    // Position of a k-block: its chunk, and its number in the chunk.
+    struct Place {
+        int32_t j, c;
+    };
+    auto after = [&](Place p) { return p.c + 1 < per_chunk ? Place{p.j, p.c + 1} : Place{p.j + 1, 0}; };
+    // A unit's word is asked for two k-blocks ahead, so that nothing waits for it.
+    auto uniform = [](UnitWord w) {
         return (UnitWord)(uint32_t)__builtin_amdgcn_readfirstlane((int)(w >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)w);
     };
-    const int64_t lrow0 = ((wrow < P.rows ? wrow : P.rows - 1) - rb * P.R_u) & ~(int64_t)63;      // a wavefront past the last row loads the last ones
-    // The fields of the wavefront pair's rows: 16 S bits bytes / 8 a row, in pieces of 16 bytes, every other 64 of them by each of the two.
-    auto load_codes = [&](UnitWord word, int32_t kb, int buf) {
+    // The fields of the wavefront pair's rows: 2 S bits bytes a row, in pieces of 16 bytes, every other 64 of them by each of the two; and
+    // the rows' scales.
+    auto load_codes = [&](UnitWord word, Place at, int buf) {
+        if (wt == 0) {
+            const int32_t r = lane < rows_left ? lane : (int32_t)rows_left - 1;
+            __builtin_amdgcn_global_load_lds((global_ptr)(P.scale + (rb * P.n_chunks + at.j) * P.R_u + lrow0 + r), (lds_ptr)&st[buf][wr * 64], 4, 0, 0);
+        }
         const int kind = (int)(word >> 56);
         if (kind == 0) return;
         const int bits = kind == 1 ? 8 : (kind == 2 ? 4 : (kind == 6 ? 1 : 2));
-        const int32_t seg = 2 * S * bits, c = kb - kb / per_chunk * per_chunk;         // bytes of a row
+        const int32_t seg = 2 * S * bits;                                              // bytes of a row
         const bool laid = (word & PT_LAID) != 0;
         const int64_t step = laid ? seg : (int64_t)seg * per_chunk;                    // from row to row
-        const int64_t first = laid ? (int64_t)c * P.R_u * seg : (int64_t)c * seg;
+        const int64_t first = laid ? (int64_t)at.c * P.R_u * seg : (int64_t)at.c * seg;
         const uint8_t* const base = (laid ? Q.fields : P.codes) + (word & PT_OFFSET) + first;
-        const int64_t rows_left = P.R_u - lrow0;
         const int32_t pieces = 4 * seg, have = rows_left < 64 ? (int32_t)rows_left * seg >> 4 : pieces;
         for (int32_t i0 = wt * 64; i0 < pieces; i0 += 128) {
             int32_t i = i0 + lane;
             i = i < have ? i : have - 1;
-            int64_t at;
-            if (step == seg) at = lrow0 * seg + (int64_t)i * 16;
-            else at = (lrow0 + i / (seg >> 4)) * step + (i % (seg >> 4)) * 16;         // seg is 16 bits there
-            __builtin_amdgcn_global_load_lds((global_ptr)(base + at), (lds_ptr)&ct[buf][wr][i0], 16, 0, 0);
+            int64_t from;
+            if (step == seg) from = lrow0 * seg + (int64_t)i * 16;
+            else from = (lrow0 + i / bits) * step + (i % bits) * 16;                   // a row is 16 bits bytes there
+            __builtin_amdgcn_global_load_lds((global_ptr)(base + from), (lds_ptr)&ct[buf][wr][i0], 16, 0, 0);
         }
     };
-    auto load_tile = [&](int32_t it, int buf) {
-        const int32_t kb = it / NP, p = it - kb * NP;
+    auto load_tile = [&](int32_t kb, int p, int buf) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             __builtin_amdgcn_global_load_lds((global_ptr)(xsrc[k] + p * Q.plane + (int64_t)kb * (16 * S)), (lds_ptr)&xt[buf][k * 512 + wave * 64], 16, 0, 0);
     };
-    auto load_scale = [&](int32_t kb, int buf) {
-        if (tid < PT_ROWS) {
-            const int64_t u = srb * P.n_chunks + kb / per_chunk;
-            const float s = P.scale[u * P.R_u + slrow];
-            const int kind = (int)(Q.unit[u] >> 56);
-            st[buf][tid] = kind == 0 ? 1.0f : (kind == 6 ? -s : s);
-        }
-    };
 
     f32x16 tot[2][2] = {};
     const TileBits bits;
-    const int32_t n_it = Q.n_kb * NP;
-    UnitWord word = word_of(0);
-    load_tile(0, 0);
-    load_codes(word, 0, 0);
-    load_scale(0, 0);
+    const int32_t n_it = Q.n_kb * NP;                       // k-block by k-block, plane by plane
+    Place next = after(Place{0, 0});
+    UnitWord word = uniform(words[0]);
+    UnitWord next_word = words[next.j < P.n_chunks ? next.j : 0];
+    load_tile(0, 0, 0);
+    load_codes(word, Place{0, 0}, 0);
     f32x16 acc[2][2];
+    int32_t kb = 0;
+    int plane = 0;
     for (int32_t it = 0; it < n_it; ++it) {
-        const int32_t kb = it / NP;
         const int buf = it & 1;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         const int kind = (int)(word >> 56);
-        UnitWord next_word = word;
-        const int32_t nkb = (it + 1) / NP;
+        const bool last = plane == NP - 1;                  // of the k-block's planes
+        const UnitWord coming = uniform(next_word);
         if (it + 1 < n_it) {
-            load_tile(it + 1, buf ^ 1);
-            if (NP == 1 || nkb != kb) {
-                next_word = word_of(nkb);
-                load_codes(next_word, nkb, nkb & 1);
-                load_scale(nkb, nkb & 1);
+            load_tile(last ? kb + 1 : kb, last ? 0 : plane + 1, buf ^ 1);
+            if (last) {
+                const Place then = after(next);
+                next_word = words[then.j < P.n_chunks ? then.j : 0];
+                load_codes(coming, next, (kb + 1) & 1);
+                next = then;
             }
         }
-        if (NP == 1 || it == kb * NP) {
+        if (plane == 0) {
 #pragma unroll
             for (int f = 0; f < 2; ++f)
 #pragma unroll
@@ -306,28 +312,33 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
             steps(TileFields<1>(), 16 * S);
         } else {
             const int64_t c = (int64_t)kb * (16 * S) + hh * (8 * S);
-            const int terms = P.w_f32 != 0 ? 3 - (NP == 1 ? 0 : it - kb * NP) : 1;       // of a weight's terms with this plane's: those that count
+            const int terms = P.w_f32 != 0 ? 3 - plane : 1;       // of a weight's terms with this plane's: those that count
             for (int term = 0; term < terms; ++term) {
 #pragma unroll 2
                 for (int s = 0; s < S; ++s)
                     step(s, {skip_octet(P, rb * P.R_u + lrow[0], c + s * 8, term), skip_octet(P, rb * P.R_u + lrow[1], c + s * 8, term)});
             }
         }
-        if (NP == 1 || it == kb * NP + NP - 1) {
+        if (last) {
             const float* const sc = st[kb & 1] + wr * 64 + 4 * hh;
 #pragma unroll
             for (int f = 0; f < 2; ++f)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const float4 a = *reinterpret_cast<const float4*>(sc + f * 32 + g * 8);
-                    const float av[4] = {a.x, a.y, a.z, a.w};
+                    float av[4] = {a.x, a.y, a.z, a.w};
+                    if (kind == 0) av[0] = av[1] = av[2] = av[3] = 1.0f;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
                         for (int n = 0; n < 2; ++n) tot[f][n][g * 4 + i] = fmaf(av[i], acc[f][n][g * 4 + i], tot[f][n][g * 4 + i]);
                 }
+            word = coming;
+            ++kb;
+            plane = 0;
+        } else {
+            ++plane;
         }
-        word = next_word;
     }
 
     // beta sum x, two k-blocks an instruction
