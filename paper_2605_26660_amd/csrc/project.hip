@@ -279,7 +279,7 @@ ProjectWs project_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32
     w.planes = take(dtype == WINDQ_F32 ? (size_t)(3 * T * cols) * 2 : 0);
     w.h = take((size_t)(T * max_rank) * 4);
     const bool many = T > PROJECT_FEW;
-    w.fields = take(many ? (size_t)(rows * cols) / (G % 128 == 0 || G == 96 || G == 64 ? 2 : 1) : 0);
+    w.fields = take(many ? (size_t)(rows * cols) / (G == 128 || G == 96 || G == 64 ? 2 : 1) : 0);
     w.unit = take(many ? (size_t)((rows + PT_STRIP - 1) / PT_STRIP) * (size_t)(cols / G) * sizeof(UnitWord) : 0);
     w.xs = take(many ? (size_t)(cols / 64) * (size_t)T * 16 : 0);
     w.total = at == 0 ? 256 : at;

@@ -22,10 +22,9 @@ namespace windq {
 constexpr int PT_ROWS = 256, PT_TOKENS = 128, PT_THREADS = 512;
 constexpr int PT_STRIP = 64;                               // rows of a unit that one workgroup lays out
 
-// Where a unit's fields begin in the code stream, or, with LAID set, in the workspace; and what they are (kind, top byte): 0 skip, 1: 8 bits,
+// Where a unit's fields begin (48 bits of address), how many bits they have (8) and what they are (kind, top byte): 0 skip, 1: 8 bits,
 // 2: 4 bits, 4: 2 bits, 5: trits as 2 bits, 6: 1 bit.
 typedef unsigned long long UnitWord;
-constexpr UnitWord PT_LAID = 1ull << 55, PT_OFFSET = PT_LAID - 1;
 
 struct TileArgs {
     PackArgs P;
@@ -46,8 +45,9 @@ struct TileArgs {
     uint32_t row_blocks;
 };
 
-// Whether a row's fields of a k-block can be loaded from the code stream as they lie: pieces of 16 bytes, or whole rows one behind the other.
-__host__ __device__ inline bool tile_natural(int32_t G, int S) { return S == 8 || G == 16 * S; }
+// Whether a chunk is one k-block: its rows lie one behind the other in the code stream.  Otherwise every unit is laid out anew, k-block by
+// k-block.
+__host__ __device__ inline bool tile_natural(int32_t G, int S) { return G == 16 * S; }
 
 // Columns of a k-block / 16, or 0 where the tiles do not fit the shape.
 inline int tile_steps(const PackArgs& P) {
@@ -90,8 +90,9 @@ __global__ __launch_bounds__(256) void tiles_prepare_kernel(const TileArgs Q, co
     const bool lay = a == 3 || a == 5 || (a != 0 && !tile_natural(P.G, S));
     uint8_t* __restrict__ const to = Q.fields + u * Q.unit_fields;
     if (strip == 0 && threadIdx.x == 0) {
-        const UnitWord at = lay ? (UnitWord)(to - Q.fields) | PT_LAID : (UnitWord)base;
-        Q.unit[u] = a == 0 ? 0ull : at | (UnitWord)(a == 3 ? 2 : a) << 56;
+        const UnitWord at = reinterpret_cast<UnitWord>(lay ? to : P.codes + base);
+        const UnitWord bits = a == 1 ? 8 : (a == 2 || a == 3 ? 4 : (a == 6 ? 1 : 2));
+        Q.unit[u] = a == 0 ? 0ull : (at & 0xffffffffffffull) | bits << 48 | (UnitWord)(a == 3 ? 2 : a) << 56;
     }
     if (!lay) return;
     if (a == 5) {
@@ -170,8 +171,17 @@ struct TileFields {
     }
 };
 
-typedef const __attribute__((address_space(1))) void* global_ptr;
-typedef __attribute__((address_space(3))) void* lds_ptr;
+// Direct loads to LDS: lane l's 16 (or 4) bytes go to `to` + 16 l (4 l); `to` is the same for the wavefront.  Written out because the compiler
+// would have every later read of LDS wait for them, whatever it reads; here whoever reads waits for vmcnt(0) and a barrier first.
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return (uint32_t)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p);
+}
+__device__ __forceinline__ void lds_load16(uint32_t to, const void* from) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory", "m0");
+}
+__device__ __forceinline__ void lds_load4(uint32_t to, const void* from) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory", "m0");
+}
 
 template <typename YT, int S>
 __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArgs Q) {
@@ -209,6 +219,7 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
     const int64_t lrow0 = ((wrow < P.rows ? wrow : P.rows - 1) - rb * P.R_u) & ~(int64_t)63;      // a wavefront past the last row loads the last ones
     const int64_t rows_left = P.R_u - lrow0;
     const int32_t per_chunk = P.G / (16 * S);
+    const uint32_t lds_xt = lds_address(xt), lds_ct = lds_address(ct), lds_st = lds_address(st);
     const UnitWord* const words = Q.unit + rb * P.n_chunks;
 
     // Position of a k-block: its chunk, and its number in the chunk.
@@ -225,30 +236,21 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
     auto load_codes = [&](UnitWord word, Place at, int buf) {
         if (wt == 0) {
             const int32_t r = lane < rows_left ? lane : (int32_t)rows_left - 1;
-            __builtin_amdgcn_global_load_lds((global_ptr)(P.scale + (rb * P.n_chunks + at.j) * P.R_u + lrow0 + r), (lds_ptr)&st[buf][wr * 64], 4, 0, 0);
+            lds_load4(lds_st + (buf * PT_ROWS + wr * 64) * 4, P.scale + (rb * P.n_chunks + at.j) * P.R_u + lrow0 + r);
         }
-        const int kind = (int)(word >> 56);
-        if (kind == 0) return;
-        const int bits = kind == 1 ? 8 : (kind == 2 ? 4 : (kind == 6 ? 1 : 2));
-        const int32_t seg = 2 * S * bits;                                              // bytes of a row
-        const bool laid = (word & PT_LAID) != 0;
-        const int64_t step = laid ? seg : (int64_t)seg * per_chunk;                    // from row to row
-        const int64_t first = laid ? (int64_t)at.c * P.R_u * seg : (int64_t)at.c * seg;
-        const uint8_t* const base = (laid ? Q.fields : P.codes) + (word & PT_OFFSET) + first;
-        const int32_t pieces = 4 * seg, have = rows_left < 64 ? (int32_t)rows_left * seg >> 4 : pieces;
+        if (word == 0) return;
+        const int32_t seg = 2 * S * (int32_t)((uint32_t)(word >> 48) & 0xffu);         // bytes of a row
+        const UnitWord base = (word & 0xffffffffffffull) + (UnitWord)((at.c * P.R_u + lrow0) * seg);
+        const int32_t pieces = 4 * seg, most = (rows_left < 64 ? (int32_t)rows_left * seg >> 4 : pieces) - 1;
         for (int32_t i0 = wt * 64; i0 < pieces; i0 += 128) {
-            int32_t i = i0 + lane;
-            i = i < have ? i : have - 1;
-            int64_t from;
-            if (step == seg) from = lrow0 * seg + (int64_t)i * 16;
-            else from = (lrow0 + i / bits) * step + (i % bits) * 16;                   // a row is 16 bits bytes there
-            __builtin_amdgcn_global_load_lds((global_ptr)(base + from), (lds_ptr)&ct[buf][wr][i0], 16, 0, 0);
+            const int32_t i = i0 + lane < most ? i0 + lane : most;
+            lds_load16(lds_ct + ((buf * 4 + wr) * 512 + i0) * 16, reinterpret_cast<const void*>(base + (uint32_t)(i * 16)));
         }
     };
     auto load_tile = [&](int32_t kb, int p, int buf) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-            __builtin_amdgcn_global_load_lds((global_ptr)(xsrc[k] + p * Q.plane + (int64_t)kb * (16 * S)), (lds_ptr)&xt[buf][k * 512 + wave * 64], 16, 0, 0);
+            lds_load16(lds_xt + (buf * (PT_TOKENS * 16) + k * 512 + wave * 64) * 16, xsrc[k] + p * Q.plane + (int64_t)kb * (16 * S));
     };
 
     f32x16 tot[2][2] = {};
