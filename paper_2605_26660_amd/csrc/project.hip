@@ -265,7 +265,7 @@ size_t grad_ws_bytes(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32
 
 // Offsets of a workspace's parts.  They are those of the shape alone, so that fewer tokens, or rows in other units, never need more.
 struct ProjectWs {
-    size_t planes, h, fields, unit, xs, total;
+    size_t planes, h, fields, unit, xs, beta, alpha, total;
 };
 
 ProjectWs project_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t G, int32_t max_rank) {
@@ -280,8 +280,10 @@ ProjectWs project_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32
     w.h = take((size_t)(T * max_rank) * 4);
     const bool many = T > PROJECT_FEW;
     w.fields = take(many ? (size_t)(rows * cols) / (G == 128 || G == 96 || G == 64 ? 2 : 1) : 0);
-    w.unit = take(many ? (size_t)((rows + PT_STRIP - 1) / PT_STRIP) * (size_t)(cols / G) * sizeof(UnitWord) : 0);
+    w.unit = take(many ? (size_t)((rows + PT_STRIP - 1) / PT_STRIP) * (size_t)(cols / 64) * sizeof(KbWord) : 0);
     w.xs = take(many ? (size_t)(cols / 64) * (size_t)T * 16 : 0);
+    w.beta = take(many ? (size_t)(cols / 64) * (size_t)rows * 16 : 0);
+    w.alpha = take(many ? (size_t)(cols / G) * (size_t)rows * 4 : 0);
     w.total = at == 0 ? 256 : at;
     return w;
 }
@@ -302,8 +304,10 @@ int launch_tiles(const ProjectArgs& Q, char* ws, const ProjectWs& at, hipStream_
     A.h = Q.h;
     A.A = Q.A;
     A.fields = reinterpret_cast<uint8_t*>(ws + at.fields);
-    A.unit = reinterpret_cast<UnitWord*>(ws + at.unit);
+    A.unit = reinterpret_cast<KbWord*>(ws + at.unit);
     A.xs = reinterpret_cast<uint4*>(ws + at.xs);
+    A.beta = reinterpret_cast<uint4*>(ws + at.beta);
+    A.alpha = reinterpret_cast<float*>(ws + at.alpha);
     A.unit_fields = Q.P.R_u * Q.P.G / (tile_natural(Q.P.G, S) ? 2 : 1);
     A.n_kb = (int32_t)(Q.P.cols / (16 * S));
     A.row_blocks = (uint32_t)((Q.P.rows + PT_ROWS - 1) / PT_ROWS);

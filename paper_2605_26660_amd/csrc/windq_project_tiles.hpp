@@ -5,6 +5,7 @@
 // each as 2 x 2 fragments of 32x32x16 instructions, two wavefronts per SIMD so that one's unpacking runs under the other's matrix
 // instructions.  Weights enter LDS packed: a lane holds one row of a fragment, and which columns its half of the wavefront takes is free as
 // long as X's operand does the same, so it takes half a k-block's columns in a row, whose codes are up to 64 contiguous bytes.
+//   The two wavefronts of a SIMD do not add up at the same time: one does behind its matrix instructions, the other ahead of its next ones.
 //   X and the codes go to LDS by direct loads, one k-block ahead (the next one's load while this one's are used): 128 tokens' octets, and
 // for each pair of wavefronts their 64 rows' fields, up to 128 bytes a row.  No register waits for them.  A token's sixteen
 // 16-byte slots are exchanged by the token's low bits, so that 32 lanes reading 32 tokens' same slot meet all banks.
@@ -25,6 +26,10 @@ constexpr int PT_STRIP = 64;                               // rows of a unit tha
 // Where a unit's fields begin (48 bits of address), how many bits they have (8) and what they are (kind, top byte): 0 skip, 1: 8 bits,
 // 2: 4 bits, 4: 2 bits, 5: trits as 2 bits, 6: 1 bit.
 typedef unsigned long long UnitWord;
+struct KbWord {
+    UnitWord fields;           // of the unit's first row in this k-block
+    const float* alpha;        // of the unit's first row
+};
 
 struct TileArgs {
     PackArgs P;
@@ -39,8 +44,10 @@ struct TileArgs {
     AdapterArgs A;
     uint8_t* fields;           // [U][k-blocks of a chunk][R_u] fields of the units that are laid out anew
     int64_t unit_fields;       // bytes of a unit's
-    UnitWord* unit;            // [U]
+    KbWord* unit;              // [row blocks of units][k-blocks]
     uint4* xs;                 // [k-blocks][T] sum of x as terms
+    uint4* beta;               // [k-blocks][rows] beta as terms
+    float* alpha;              // [chunks][rows] scales (1 where a unit is skipped)
     int32_t n_kb;              // k-blocks
     uint32_t row_blocks;
 };
@@ -60,11 +67,12 @@ inline int tile_steps(const PackArgs& P) {
 
 #ifdef __HIPCC__
 
-// Workgroups [0, strips): fields of trits and 3-bit codes, and every unit's word.  The others: sums of x over k-blocks.
+// Workgroups [0, strips): fields of trits and 3-bit codes, every unit's word, and beta of its rows.  The others: sums of x over k-blocks.
 template <typename XT, int S>
 __global__ __launch_bounds__(256) void tiles_prepare_kernel(const TileArgs Q, const int64_t strips) {
     __shared__ uint16_t trits_of[256];
     const PackArgs& P = Q.P;
+    const int32_t per_chunk = P.G / (16 * S);
     if (blockIdx.x >= strips) {
         const int64_t i = (blockIdx.x - strips) * 256 + threadIdx.x;
         const int32_t kb = (int32_t)(i / Q.T);
@@ -89,10 +97,26 @@ __global__ __launch_bounds__(256) void tiles_prepare_kernel(const TileArgs Q, co
     const int a = pk_action(P, u, base);
     const bool lay = a == 3 || a == 5 || (a != 0 && !tile_natural(P.G, S));
     uint8_t* __restrict__ const to = Q.fields + u * Q.unit_fields;
+    const int64_t rb = u / P.n_chunks, j = u - rb * P.n_chunks;
+    {
+        const int64_t lrow = strip * PT_STRIP + (threadIdx.x & 63);
+        if (lrow < P.R_u) {
+            float alpha, beta;
+            pk_affine(a == 3 ? 2 : a, P.scale[u * P.R_u + lrow], P.offset[u * P.R_u + lrow], alpha, beta);
+            uint32_t hi, mid, lo;
+            split3(beta, hi, mid, lo);
+            if (threadIdx.x < 64) Q.alpha[j * P.rows + rb * P.R_u + lrow] = alpha;
+            for (int32_t c = threadIdx.x >> 6; c < per_chunk; c += 4)
+                Q.beta[(j * per_chunk + c) * P.rows + rb * P.R_u + lrow] = make_uint4(hi | hi << 16, mid | hi << 16, lo | mid << 16, 0u);
+        }
+    }
     if (strip == 0 && threadIdx.x == 0) {
         const UnitWord at = reinterpret_cast<UnitWord>(lay ? to : P.codes + base);
         const UnitWord bits = a == 1 ? 8 : (a == 2 || a == 3 ? 4 : (a == 6 ? 1 : 2));
-        Q.unit[u] = a == 0 ? 0ull : (at & 0xffffffffffffull) | bits << 48 | (UnitWord)(a == 3 ? 2 : a) << 56;
+        for (int32_t c = 0; c < per_chunk; ++c) {
+            const UnitWord first = (at + (UnitWord)c * P.R_u * (2 * S * bits)) & 0xffffffffffffull;
+            Q.unit[rb * Q.n_kb + j * per_chunk + c] = {a == 0 ? 0ull : first | bits << 48 | (UnitWord)(a == 3 ? 2 : a) << 56, Q.alpha + j * P.rows + rb * P.R_u};
+        }
     }
     if (!lay) return;
     if (a == 5) {
@@ -159,13 +183,13 @@ struct TileFields {
     __device__ __forceinline__ uint4 octet(int s, const TileBits& C) const {
         if constexpr (KIND == 1) return fields8(raw[2 * s], raw[2 * s + 1]);
         else if constexpr (KIND == 2) {
-            const uint32_t v = raw[s], e = (v & 0xffffu) | v << 12, o = v >> 16 | (v >> 16) << 12;
+            const uint32_t v = raw[s], e = twice(v, 12, v & 0xffffu), o = twice(v >> 16, 12, v >> 16);
             return make_uint4(((e << 3) & C.mask4) | C.one4, ((e >> 5) & C.mask4) | C.one4, ((o << 3) & C.mask4) | C.one4, ((o >> 5) & C.mask4) | C.one4);
         } else if constexpr (KIND == 4) {
-            const uint32_t v = (s & 1) != 0 ? raw[s >> 1] >> 16 : raw[s >> 1] & 0xffffu, t = v | v << 14;
+            const uint32_t v = (s & 1) != 0 ? raw[s >> 1] >> 16 : raw[s >> 1] & 0xffffu, t = twice(v, 14, v);
             return make_uint4(((t << 5) & C.mask2) | C.one2, ((t << 1) & C.mask2) | C.one2, ((t >> 3) & C.mask2) | C.one2, ((t >> 7) & C.mask2) | C.one2);
         } else {                                            // of inverted bits: a set one is -1
-            const uint32_t v = (raw[s >> 2] >> (8 * (s & 3))) & 0xffu, t = v | v << 15;
+            const uint32_t v = (raw[s >> 2] >> (8 * (s & 3))) & 0xffu, t = twice(v, 15, v);
             return make_uint4(((t << 15) & C.mask1) | C.one1, ((t << 13) & C.mask1) | C.one1, ((t << 11) & C.mask1) | C.one1, ((t << 9) & C.mask1) | C.one1);
         }
     }
@@ -177,10 +201,10 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) {
     return (uint32_t)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p);
 }
 __device__ __forceinline__ void lds_load16(uint32_t to, const void* from) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
 }
 __device__ __forceinline__ void lds_load4(uint32_t to, const void* from) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
 }
 
 template <typename YT, int S>
@@ -189,20 +213,21 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
     __shared__ uint4 xt[2][PT_TOKENS * 16];
     __shared__ uint4 ct[2][4][512];                        // fields of 64 rows
     __shared__ float st[2][PT_ROWS];
+    __shared__ uint4 ring[4][8];                           // units' words, k-block by k-block
     const PackArgs& P = Q.P;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, sub = lane & 31, hh = lane >> 5;
-    const int wr = wave >> 1, wt = wave & 1;
+    const int wr = wave & 3, wt = wave >> 2;                // wavefronts w and w + 4 share a SIMD, and rows
     // Consecutive workgroups land on the eight XCDs in turn; each XCD gets a run of tiles that share tokens.
     const uint32_t n_tiles = gridDim.x, per = n_tiles >> 3;
     const uint32_t tile = blockIdx.x < per * 8 ? (blockIdx.x & 7) * per + (blockIdx.x >> 3) : blockIdx.x;
     const uint32_t tb = tile / Q.row_blocks;
     const int64_t row0 = (int64_t)(tile - tb * Q.row_blocks) * PT_ROWS, t0 = (int64_t)tb * PT_TOKENS;
 
-    // X: four of a tile's slots a thread; slot p of token n holds the octet of slot p ^ (n & 15)
+    // X: four of a tile's slots a lane; slot p of token n holds the octet of slot p ^ (n & 15)
     const uint16_t* xsrc[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const int n = k * 32 + (tid >> 4), slot = (tid & 15) ^ (n & 15);
+        const int n = k * 32 + wave * 4 + (lane >> 4), slot = (lane & 15) ^ (n & 15);
         const int s = (slot & 7) < S ? (slot & 7) : 0;
         const int64_t t = t0 + n;
         xsrc[k] = Q.X + (t < Q.T ? t : Q.T - 1) * Q.ldx + ((slot >> 3) * S + s) * 8;
@@ -218,67 +243,86 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
     }
     const int64_t lrow0 = ((wrow < P.rows ? wrow : P.rows - 1) - rb * P.R_u) & ~(int64_t)63;      // a wavefront past the last row loads the last ones
     const int64_t rows_left = P.R_u - lrow0;
-    const int32_t per_chunk = P.G / (16 * S);
-    const uint32_t lds_xt = lds_address(xt), lds_ct = lds_address(ct), lds_st = lds_address(st);
-    const UnitWord* const words = Q.unit + rb * P.n_chunks;
-
-    // Position of a k-block: its chunk, and its number in the chunk.
-    struct Place {
-        int32_t j, c;
+    const uint32_t lds_xt = lds_address(xt), lds_ct = lds_address(ct), lds_st = lds_address(st), lds_ring = lds_address(ring);
+    const int32_t n_kb = Q.n_kb;
+    const KbWord* const words = Q.unit + rb * n_kb;
+    auto uniform = [](uint32_t x, uint32_t y) {
+        return (UnitWord)(uint32_t)__builtin_amdgcn_readfirstlane((int)y) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
     };
-    auto after = [&](Place p) { return p.c + 1 < per_chunk ? Place{p.j, p.c + 1} : Place{p.j + 1, 0}; };
-    // A unit's word is asked for two k-blocks ahead, so that nothing waits for it.
-    auto uniform = [](UnitWord w) {
-        return (UnitWord)(uint32_t)__builtin_amdgcn_readfirstlane((int)(w >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)w);
+    struct Word {
+        UnitWord fields, alpha;
     };
-    // The fields of the wavefront pair's rows: 2 S bits bytes a row, in pieces of 16 bytes, every other 64 of them by each of the two; and
-    // the rows' scales.
-    auto load_codes = [&](UnitWord word, Place at, int buf) {
-        if (wt == 0) {
-            const int32_t r = lane < rows_left ? lane : (int32_t)rows_left - 1;
-            lds_load4(lds_st + (buf * PT_ROWS + wr * 64) * 4, P.scale + (rb * P.n_chunks + at.j) * P.R_u + lrow0 + r);
-        }
-        if (word == 0) return;
-        const int32_t seg = 2 * S * (int32_t)((uint32_t)(word >> 48) & 0xffu);         // bytes of a row
-        const UnitWord base = (word & 0xffffffffffffull) + (UnitWord)((at.c * P.R_u + lrow0) * seg);
-        const int32_t pieces = 4 * seg, most = (rows_left < 64 ? (int32_t)rows_left * seg >> 4 : pieces) - 1;
+    auto word_of = [&](uint4 w) { return Word{uniform(w.x, w.y), uniform(w.z, w.w)}; };
+    auto word_now = [&](int32_t kb) { return word_of(reinterpret_cast<const uint4*>(words)[kb < n_kb ? kb : n_kb - 1]); };
+    auto load_word = [&](int32_t kb) {
+        if (lane < 4) lds_load4(lds_ring + (wr * 8 + (kb & 7)) * 16, reinterpret_cast<const uint32_t*>(words + (kb < n_kb ? kb : n_kb - 1)) + lane);
+    };
+    // The fields of the wavefront's 64 rows, 2 S bits bytes a row: every other 64 pieces of 16 bytes by each of the two wavefronts that share them;
+    // and the rows' scales, by the one that has read the scales there before by then.
+    const uint32_t row_at = (uint32_t)(rows_left < 64 ? (lane < rows_left ? lane : (int32_t)rows_left - 1) : lane);
+    auto load_codes = [&](Word word, int32_t kb) {
+        const int buf = kb & 1;
+        if (wt == 1) lds_load4(lds_st + (buf * PT_ROWS + wr * 64) * 4, reinterpret_cast<const float*>(word.alpha) + lrow0 + row_at);
+        if (word.fields == 0) return;
+        const int32_t bytes = 2 * S * (int32_t)((uint32_t)(word.fields >> 48) & 0xffu), pieces = 4 * bytes;
+        const UnitWord base = (word.fields & 0xffffffffffffull) + (UnitWord)(lrow0 * bytes);
+        const int32_t most = (rows_left < 64 ? (int32_t)rows_left * bytes >> 4 : pieces) - 1;
         for (int32_t i0 = wt * 64; i0 < pieces; i0 += 128) {
             const int32_t i = i0 + lane < most ? i0 + lane : most;
             lds_load16(lds_ct + ((buf * 4 + wr) * 512 + i0) * 16, reinterpret_cast<const void*>(base + (uint32_t)(i * 16)));
         }
     };
-    auto load_tile = [&](int32_t kb, int p, int buf) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            lds_load16(lds_xt + (buf * (PT_TOKENS * 16) + k * 512 + wave * 64) * 16, xsrc[k] + p * Q.plane + (int64_t)kb * (16 * S));
+    auto load_piece = [&](int k, int32_t kb, int p, int buf) {
+        lds_load16(lds_xt + (buf * (PT_TOKENS * 16) + k * 512 + wave * 64) * 16, xsrc[k] + p * Q.plane + (int64_t)kb * (16 * S));
     };
 
     f32x16 tot[2][2] = {};
     const TileBits bits;
-    const int32_t n_it = Q.n_kb * NP;                       // k-block by k-block, plane by plane
-    Place next = after(Place{0, 0});
-    UnitWord word = uniform(words[0]);
-    UnitWord next_word = words[next.j < P.n_chunks ? next.j : 0];
-    load_tile(0, 0, 0);
-    load_codes(word, Place{0, 0}, 0);
+    const int32_t n_it = n_kb * NP;                         // k-block by k-block, plane by plane
+    Word word = word_now(0), next = word_now(1);
+    if (wt == 0) load_word(2);
+    load_codes(word, 0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) load_piece(k, 0, 0, 0);
     f32x16 acc[2][2];
+    // A k-block's sums times its groups' scales, added to the total.
+    auto fold = [&](int32_t kb) {
+        const float* const sc = st[kb & 1] + wr * 64 + 4 * hh;
+        float4 a[2][4];
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) a[f][g] = *reinterpret_cast<const float4*>(sc + f * 32 + g * 8);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float av[4] = {a[f][g].x, a[f][g].y, a[f][g].z, a[f][g].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) tot[f][n][g * 4 + i] = fmaf(av[i], acc[f][n][g * 4 + i], tot[f][n][g * 4 + i]);
+            }
+    };
     int32_t kb = 0;
     int plane = 0;
     for (int32_t it = 0; it < n_it; ++it) {
         const int buf = it & 1;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        const int kind = (int)(word >> 56);
+        const int kind = (int)(word.fields >> 56);
         const bool last = plane == NP - 1;                  // of the k-block's planes
-        const UnitWord coming = uniform(next_word);
-        if (it + 1 < n_it) {
-            load_tile(last ? kb + 1 : kb, last ? 0 : plane + 1, buf ^ 1);
-            if (last) {
-                const Place then = after(next);
-                next_word = words[then.j < P.n_chunks ? then.j : 0];
-                load_codes(coming, next, (kb + 1) & 1);
-                next = then;
-            }
+        if (wt == 1 && plane == 0 && it > 0) {
+            fold(kb - 1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // The next iteration's data.  The last one asks for its own again, into places that nobody reads any more: a branch would cost more.
+        const int32_t kb_then = last && kb + 1 < n_kb ? kb + 1 : kb;
+        const int plane_then = last ? 0 : plane + 1;
+        if (last) {
+            if (wt == 0) load_word(kb + 3);
+            load_codes(next, kb + 1);
         }
         if (plane == 0) {
 #pragma unroll
@@ -288,21 +332,51 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
         }
         const uint32_t xb = (uint32_t)buf * sizeof(xt[0]) + (wt * 64 + sub) * 256 + (((hh * 8) ^ (sub & 15)) << 4);
         const char* const cb = reinterpret_cast<const char*>(ct[kb & 1][wr]);
-        auto step = [&](int s, const uint4 (&a)[2]) {
+        auto tokens_of = [&](int s, bf16x8 (&b)[2]) {
             const char* const at = reinterpret_cast<const char*>(xt) + (xb ^ (uint32_t)(s << 4));
-            const bf16x8 b0 = as_bf16x8(*reinterpret_cast<const uint4*>(at)), b1 = as_bf16x8(*reinterpret_cast<const uint4*>(at + 32 * 256));
-#pragma unroll
-            for (int f = 0; f < 2; ++f) {
-                acc[f][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a[f]), b0, acc[f][0], 0, 0, 0);
-                acc[f][1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a[f]), b1, acc[f][1], 0, 0, 0);
-            }
+            b[0] = as_bf16x8(*reinterpret_cast<const uint4*>(at));
+            b[1] = as_bf16x8(*reinterpret_cast<const uint4*>(at + 32 * 256));
         };
+        auto multiply = [&](const uint4 (&a)[2], const bf16x8 (&b)[2]) {
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) acc[f][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a[f]), b[n], acc[f][n], 0, 0, 0);
+        };
+        // While one step's four matrix instructions run, the next one's codes are unpacked, six vector instructions behind each, and
+        // the tokens of the step DEPTH on are read: LDS takes longer than one step.  The next k-block's X is asked for in between, a
+        // piece a step: 64 lanes' 16 bytes keep the way to LDS busy for 16 clocks, and who asks for more at once waits for it.
         auto steps = [&](auto fields, int row_bytes) {
+            constexpr int DEPTH = 2;
             decltype(fields) v[2];
+            bf16x8 b[DEPTH + 1][2];
+            uint4 a[2][2];
             v[0].template read<S>(cb + sub * row_bytes + hh * (row_bytes >> 1));
             v[1].template read<S>(cb + (32 + sub) * row_bytes + hh * (row_bytes >> 1));
 #pragma unroll
-            for (int s = 0; s < S; ++s) step(s, {v[0].octet(s, bits), v[1].octet(s, bits)});
+            for (int s = 0; s < DEPTH; ++s) tokens_of(s, b[s]);
+            a[0][0] = v[0].octet(0, bits);
+            a[0][1] = v[1].octet(0, bits);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                if (s < 4) load_piece(s, kb_then, plane_then, buf ^ 1);
+                if (s + DEPTH < S) tokens_of(s + DEPTH, b[(s + DEPTH) % (DEPTH + 1)]);
+                if (s + 1 < S) {
+                    a[(s + 1) & 1][0] = v[0].octet(s + 1, bits);
+                    a[(s + 1) & 1][1] = v[1].octet(s + 1, bits);
+                }
+                multiply(a[s & 1], b[s % (DEPTH + 1)]);
+                if (s + DEPTH < S) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                if (s + 1 < S) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
         };
         if (kind == 6) {
             steps(TileFields<6>(), 2 * S);
@@ -314,34 +388,30 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
             steps(TileFields<1>(), 16 * S);
         } else {
             const int64_t c = (int64_t)kb * (16 * S) + hh * (8 * S);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) load_piece(k, kb_then, plane_then, buf ^ 1);
             const int terms = P.w_f32 != 0 ? 3 - plane : 1;       // of a weight's terms with this plane's: those that count
             for (int term = 0; term < terms; ++term) {
 #pragma unroll 2
-                for (int s = 0; s < S; ++s)
-                    step(s, {skip_octet(P, rb * P.R_u + lrow[0], c + s * 8, term), skip_octet(P, rb * P.R_u + lrow[1], c + s * 8, term)});
+                for (int s = 0; s < S; ++s) {
+                    bf16x8 b[2];
+                    tokens_of(s, b);
+                    multiply({skip_octet(P, rb * P.R_u + lrow[0], c + s * 8, term), skip_octet(P, rb * P.R_u + lrow[1], c + s * 8, term)}, b);
+                }
             }
         }
         if (last) {
-            const float* const sc = st[kb & 1] + wr * 64 + 4 * hh;
-#pragma unroll
-            for (int f = 0; f < 2; ++f)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const float4 a = *reinterpret_cast<const float4*>(sc + f * 32 + g * 8);
-                    float av[4] = {a.x, a.y, a.z, a.w};
-                    if (kind == 0) av[0] = av[1] = av[2] = av[3] = 1.0f;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int n = 0; n < 2; ++n) tot[f][n][g * 4 + i] = fmaf(av[i], acc[f][n][g * 4 + i], tot[f][n][g * 4 + i]);
-                }
-            word = coming;
+            if (wt == 0) fold(kb);
+            word = next;
             ++kb;
+            next = word_of(ring[wr][(kb + 1) & 7]);         // asked for a k-block ago
             plane = 0;
         } else {
             ++plane;
         }
     }
+    if (wt == 1) fold(n_kb - 1);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
     // beta sum x, two k-blocks an instruction
     int64_t tok[2];
@@ -350,29 +420,27 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
         tok[n] = t0 + wt * 64 + n * 32 + sub;
         if (tok[n] >= Q.T) tok[n] = Q.T - 1;
     }
-    for (int32_t k2 = 0; k2 < Q.n_kb; k2 += 2) {
-        const int32_t kb = k2 + hh;
-        uint4 b[2] = {}, a[2] = {};
-        if (kb < Q.n_kb) {
-            const int64_t u = rb * P.n_chunks + kb / per_chunk;
-            const int act = P.action[u];
-            const bool skip = (Q.unit[u] >> 56) == 0;
+    constexpr int ROUND = 6;                                // pairs of k-blocks whose operands are on their way together
+    const uint4 nothing = make_uint4(0u, 0u, 0u, 0u);
+    for (int32_t k0 = 0; k0 < n_kb; k0 += 2 * ROUND) {
+        uint4 a[ROUND][2], b[ROUND][2];
 #pragma unroll
-            for (int n = 0; n < 2; ++n) b[n] = Q.xs[(int64_t)kb * Q.T + tok[n]];
+        for (int k = 0; k < ROUND; ++k) {
+            const int32_t at = k0 + 2 * k + hh < n_kb ? k0 + 2 * k + hh : n_kb - 1;
 #pragma unroll
-            for (int f = 0; f < 2; ++f) {
-                const int64_t g = u * P.R_u + lrow[f];
-                float alpha, beta;
-                pk_affine(skip ? 0 : (act == 3 ? 2 : act), P.scale[g], P.offset[g], alpha, beta);
-                uint32_t hi, mid, lo;
-                split3(beta, hi, mid, lo);
-                a[f] = make_uint4(hi | hi << 16, mid | hi << 16, lo | mid << 16, 0u);
-            }
+            for (int f = 0; f < 2; ++f) a[k][f] = Q.beta[at * P.rows + rb * P.R_u + lrow[f]];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) b[k][n] = Q.xs[at * Q.T + tok[n]];
         }
 #pragma unroll
-        for (int f = 0; f < 2; ++f)
+        for (int k = 0; k < ROUND; ++k) {
+            const bool in = k0 + 2 * k + hh < n_kb;
 #pragma unroll
-            for (int n = 0; n < 2; ++n) tot[f][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(a[f]), as_bf16x8(b[n]), tot[f][n], 0, 0, 0);
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+                    tot[f][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(in ? a[k][f] : nothing), as_bf16x8(in ? b[k][n] : nothing), tot[f][n], 0, 0, 0);
+        }
     }
 
     // what is not finite so far: weight by weight
