@@ -1,0 +1,185 @@
+// Tokens grouped by adapter, and h = A x (or dh = alpha B^T dY) for many tokens of bfloat16.
+#include "windq_adapters.hpp"
+
+namespace windq {
+
+// A workgroup per adapter: counts its tokens and those of the adapters below it, then lists its own, in ascending order.
+__global__ __launch_bounds__(256) void group_kernel(const GroupArgs Q) {
+    __shared__ int32_t sums[2][4];
+    const int32_t k = blockIdx.x;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    int32_t below = 0, mine = 0;
+    for (int64_t t = threadIdx.x; t < Q.T; t += 256) {
+        const int32_t id = Q.of[t];
+        below += id >= 0 && id < k ? 1 : 0;
+        mine += id == k ? 1 : 0;
+    }
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) {
+        below += __shfl_xor(below, m, 64);
+        mine += __shfl_xor(mine, m, 64);
+    }
+    if (lane == 0) {
+        sums[0][wave] = below;
+        sums[1][wave] = mine;
+    }
+    __syncthreads();
+    below = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
+    mine = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
+    const int64_t slot = (int64_t)(below / GROUP) + k;
+    const int64_t end = k + 1 == Q.n ? Q.slots : (int64_t)((below + mine) / GROUP) + k + 1;
+    if (threadIdx.x == 0) {
+        Q.first[k] = (int32_t)(slot * GROUP);
+        Q.count[k] = mine;
+    }
+    const int64_t used = slot + (mine + GROUP - 1) / GROUP;
+    for (int64_t s = slot + threadIdx.x; s < end; s += 256) Q.owner[s] = s < used ? k : -1;
+    int64_t at = slot * GROUP;
+    __syncthreads();
+    for (int64_t t0 = 0; t0 < Q.T; t0 += 256) {
+        const int64_t t = t0 + threadIdx.x;
+        const bool hit = t < Q.T && Q.of[t] == k;
+        const uint64_t hits = __ballot(hit);
+        if (lane == 0) sums[0][wave] = __popcll(hits);
+        __syncthreads();
+        int32_t before = __popcll(hits & ((1ull << lane) - 1ull)), all = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            before += w < wave ? sums[0][w] : 0;
+            all += sums[0][w];
+        }
+        if (hit) Q.place[at + before] = (int32_t)t;
+        at += all;
+        __syncthreads();
+    }
+    for (int64_t p = at + threadIdx.x; p < end * GROUP; p += 256) Q.place[p] = -1;
+}
+
+int launch_group(const GroupArgs& G, hipStream_t st) {
+    if (!fits_launch(G.n, 256)) return WINDQ_ESHAPE;
+    group_kernel<<<dim3((uint32_t)G.n), dim3(256), 0, st>>>(G);
+    return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
+}
+
+// 64 tokens of one adapter by up to 16 RF ranks, over a piece of the columns that the four wavefronts share 32 at a time.  Both factors
+// are rows along the sum's axis, so operands come straight from memory; ranks are the M side.  Bound by reading X once.
+template <int RF>
+__global__ __launch_bounds__(256) void shrink_kernel(const ShrinkArgs Q) {
+    __shared__ float red[4][RF * 16][65];
+    const int64_t slot = blockIdx.x / Q.splits;
+    const int32_t split = (int32_t)(blockIdx.x - slot * Q.splits);
+    const int32_t k = Q.owner[slot];
+    if (k < 0) return;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
+    const int32_t rank = adapter_rank(Q.A, k);
+    const int32_t steps = (Q.width + 31) / 32, per = (steps + Q.splits - 1) / Q.splits;
+    const int32_t s0 = split * per, s1 = s0 + per < steps ? s0 + per : steps;
+    const uint16_t* xp[4];
+    const int32_t some = Q.place[slot * GROUP];            // a slot in use holds a token at its start
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+        const int32_t t = Q.place[slot * GROUP + n * 16 + sub];
+        xp[n] = static_cast<const uint16_t*>(Q.X) + (int64_t)(t < 0 ? some : t) * Q.ld + q * 8;
+    }
+    const uint16_t* ap[RF];
+#pragma unroll
+    for (int f = 0; f < RF; ++f) {
+        const int32_t r = f * 16 + sub;
+        ap[f] = static_cast<const uint16_t*>(Q.a) + ((int64_t)k * Q.A.max_rank + (r < rank ? r : 0)) * Q.lda + q * 8;
+    }
+    f32x4 acc[RF][4] = {};
+    if (rank > 0) {
+#pragma unroll 2
+        for (int32_t s = s0 + wave; s < s1; s += 4) {
+            const bool in = s * 32 + q * 8 < Q.width;
+            const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+            bf16x8 a[RF], b[4];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) b[n] = as_bf16x8(in ? *reinterpret_cast<const uint4*>(xp[n] + s * 32) : none);
+#pragma unroll
+            for (int f = 0; f < RF; ++f) a[f] = as_bf16x8(in ? *reinterpret_cast<const uint4*>(ap[f] + s * 32) : none);
+#pragma unroll
+            for (int f = 0; f < RF; ++f)
+#pragma unroll
+                for (int n = 0; n < 4; ++n) acc[f][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[f], b[n], acc[f][n], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int f = 0; f < RF; ++f)
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) red[wave][f * 16 + q * 4 + i][n * 16 + sub] = acc[f][n][i];
+    __syncthreads();
+    float* __restrict__ const out = Q.part + ((int64_t)split * Q.slots + slot) * GROUP * (RF * 16);
+    for (int e = threadIdx.x; e < GROUP * RF * 16; e += 256) {
+        const int r = e % (RF * 16), n = e / (RF * 16);
+        out[e] = r < rank ? ((red[0][r][n] + red[1][r][n]) + red[2][r][n]) + red[3][r][n] : 0.0f;
+    }
+}
+
+int launch_shrink(const ShrinkArgs& S, hipStream_t st) {
+    const int64_t wgs = S.slots * S.splits;
+    if (!fits_launch(wgs, 256)) return WINDQ_ESHAPE;
+    const dim3 g((uint32_t)wgs), b(256);
+    switch (shrink_ranks(S.A.max_rank) / 16) {
+        case 1: shrink_kernel<1><<<g, b, 0, st>>>(S); break;
+        case 2: shrink_kernel<2><<<g, b, 0, st>>>(S); break;
+        case 3: shrink_kernel<3><<<g, b, 0, st>>>(S); break;
+        case 4: shrink_kernel<4><<<g, b, 0, st>>>(S); break;
+        case 5: shrink_kernel<5><<<g, b, 0, st>>>(S); break;
+        case 6: shrink_kernel<6><<<g, b, 0, st>>>(S); break;
+        case 7: shrink_kernel<7><<<g, b, 0, st>>>(S); break;
+        default: shrink_kernel<8><<<g, b, 0, st>>>(S); break;
+    }
+    return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
+}
+
+// A workgroup per slot adds up its pieces; the workgroups behind them write the zeros of tokens without an adapter, 64 tokens each.
+__global__ __launch_bounds__(256) void join_kernel(const JoinArgs Q) {
+    const int32_t R = Q.A.max_rank, ranks = (R + 15) / 16 * 16;
+    if (blockIdx.x >= Q.slots) {
+        if (Q.h == nullptr) return;
+        const int64_t t0 = (blockIdx.x - Q.slots) * GROUP;
+        for (int e = threadIdx.x; e < GROUP * R; e += 256) {
+            const int64_t t = t0 + e / R;
+            if (t >= Q.T) break;
+            const int32_t id = Q.A.of[t];
+            if (id < 0 || id >= Q.A.n) Q.h[t * R + e % R] = 0.0f;
+        }
+        return;
+    }
+    const int64_t slot = blockIdx.x, places = Q.slots * GROUP;
+    const int32_t k = Q.owner[slot];
+    if (k < 0) return;
+    const float factor = Q.scaled && Q.A.alpha != nullptr ? Q.A.alpha[k] : 1.0f;
+    for (int e = threadIdx.x; e < GROUP * ranks; e += 256) {
+        const int r = e / GROUP, n = e % GROUP;            // places side by side
+        if (r >= R) break;
+        const int32_t t = Q.place[slot * GROUP + n];
+        float v = 0.0f;
+        if (t >= 0) {
+            const float* __restrict__ const p = Q.part + (slot * GROUP + n) * ranks + r;
+            for (int32_t s = 0; s < Q.splits; ++s) v += p[(int64_t)s * places * ranks];
+            v *= factor;
+            if (Q.h != nullptr) Q.h[(int64_t)t * R + r] = v;
+        }
+        if (Q.planes != nullptr) {
+            uint32_t hi, mid, lo;
+            split3(v, hi, mid, lo);
+            uint16_t* __restrict__ const o = Q.planes + r * places + slot * GROUP + n;
+            o[0] = (uint16_t)hi;
+            o[R * places] = (uint16_t)mid;
+            o[2 * R * places] = (uint16_t)lo;
+        }
+    }
+}
+
+int launch_join(const JoinArgs& J, hipStream_t st) {
+    const int64_t wgs = J.slots + (J.h != nullptr ? tokens_in(J.T, GROUP) : 0);
+    if (!fits_launch(wgs, 256)) return WINDQ_ESHAPE;
+    join_kernel<<<dim3((uint32_t)wgs), dim3(256), 0, st>>>(J);
+    return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
+}
+
+}  // namespace windq

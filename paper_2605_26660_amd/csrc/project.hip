@@ -265,10 +265,10 @@ size_t grad_ws_bytes(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32
 
 // Offsets of a workspace's parts.  They are those of the shape alone, so that fewer tokens, or rows in other units, never need more.
 struct ProjectWs {
-    size_t planes, h, fields, unit, xs, beta, alpha, total;
+    size_t planes, h, place, owner, first, count, part, fields, unit, xs, beta, alpha, total;
 };
 
-ProjectWs project_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t G, int32_t max_rank) {
+ProjectWs project_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t G, int32_t n, int32_t max_rank) {
     ProjectWs w;
     size_t at = 0;
     auto take = [&at](size_t bytes) {
@@ -278,6 +278,13 @@ ProjectWs project_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32
     };
     w.planes = take(dtype == WINDQ_F32 ? (size_t)(3 * T * cols) * 2 : 0);
     w.h = take((size_t)(T * max_rank) * 4);
+    const bool grouped = n > 0 && dtype == WINDQ_BF16 && T > SHRINK_FEW;
+    const int64_t slots = group_slots(T, n);
+    w.place = take(grouped ? (size_t)slots * GROUP * 4 : 0);
+    w.owner = take(grouped ? (size_t)slots * 4 : 0);
+    w.first = take(grouped ? (size_t)n * 4 : 0);
+    w.count = take(grouped ? (size_t)n * 4 : 0);
+    w.part = take(grouped ? (size_t)shrink_splits(slots, cols) * (size_t)slots * GROUP * (size_t)shrink_ranks(max_rank) * 4 : 0);
     const bool many = T > PROJECT_FEW;
     w.fields = take(many ? (size_t)(rows * cols) / (G == 128 || G == 96 || G == 64 ? 2 : 1) : 0);
     w.unit = take(many ? (size_t)((rows + PT_STRIP - 1) / PT_STRIP) * (size_t)(cols / 64) * sizeof(KbWord) : 0);
@@ -337,9 +344,26 @@ int project_all(ProjectArgs& Q, const windq_mat* X, const windq_adapters* ad, fl
     if (ad != nullptr) {
         float* const ht = h != nullptr ? h : reinterpret_cast<float*>(ws + at.h);
         const int64_t wgs = T * ((Q.A.max_rank + 15) / 16);
-        if (!fits_launch(wgs, 256)) return WINDQ_ESHAPE;
-        shrink_token_kernel<XT><<<dim3((uint32_t)wgs), dim3(256), 0, st>>>(static_cast<const XT*>(X->data), X->ld, (int32_t)Q.P.cols, Q.A, false, ht);
-        if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
+        bool grouped = false;
+        if constexpr (sizeof(XT) == 2) {
+            grouped = T > SHRINK_FEW;
+            if (grouped) {
+                GroupArgs G = {Q.A.of, T, Q.A.n, group_slots(T, Q.A.n), reinterpret_cast<int32_t*>(ws + at.place), reinterpret_cast<int32_t*>(ws + at.owner),
+                               reinterpret_cast<int32_t*>(ws + at.first), reinterpret_cast<int32_t*>(ws + at.count)};
+                ShrinkArgs S = {X->data, X->ld, Q.A.a, Q.P.cols, (int32_t)Q.P.cols, shrink_splits(G.slots, Q.P.cols), G.slots, G.place, G.owner, Q.A,
+                                reinterpret_cast<float*>(ws + at.part)};
+                JoinArgs J = {S.part, S.splits, G.slots, G.place, G.owner, T, Q.A, false, ht, nullptr};
+                int status = launch_group(G, st);
+                if (status == WINDQ_OK) status = launch_shrink(S, st);
+                if (status == WINDQ_OK) status = launch_join(J, st);
+                if (status != WINDQ_OK) return status;
+            }
+        }
+        if (!grouped) {
+            if (!fits_launch(wgs, 256)) return WINDQ_ESHAPE;
+            shrink_token_kernel<XT><<<dim3((uint32_t)wgs), dim3(256), 0, st>>>(static_cast<const XT*>(X->data), X->ld, (int32_t)Q.P.cols, Q.A, false, ht);
+            if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
+        }
         Q.h = ht;
     }
     const int S = Q.P.mask == nullptr && T > PROJECT_FEW ? tile_steps(Q.P) : 0;
@@ -358,7 +382,7 @@ extern "C" size_t windq_project_workspace_bytes(int32_t grad, int32_t dtype, int
     if ((dtype != WINDQ_F32 && dtype != WINDQ_BF16) || tokens < 0 || rows <= 0 || cols <= 0 || chunk_w <= 0 || n_adapters < 0 || max_rank < 0) return 0;
     if (tokens > ((int64_t)1 << 31) - 1 || rows > (int64_t)1 << 31 || cols > (int64_t)1 << 31 || max_rank > WINDQ_MAX_RANK) return 0;
     if (n_adapters == 0) max_rank = 0;
-    return grad != 0 ? grad_ws_bytes(dtype, tokens, rows, cols, n_adapters, max_rank) : project_ws(dtype, tokens, rows, cols, chunk_w, max_rank).total;
+    return grad != 0 ? grad_ws_bytes(dtype, tokens, rows, cols, n_adapters, max_rank) : project_ws(dtype, tokens, rows, cols, chunk_w, n_adapters, max_rank).total;
 }
 
 extern "C" int windq_project(const windq_packed* P, const windq_mat* X, const windq_adapters* adapters, const int32_t* adapter_of,
@@ -379,7 +403,7 @@ extern "C" int windq_project(const windq_packed* P, const windq_mat* X, const wi
     if (X->rows == 0) return WINDQ_OK;
     if (X->rows * Q.P.rows > (int64_t)0x7fffffff) return WINDQ_ESHAPE;
     if (Y == nullptr || !aligned(Y, eb)) return WINDQ_EINVAL;
-    const ProjectWs at = project_ws(X->dtype, X->rows, Q.P.rows, Q.P.cols, Q.P.G, adapters != nullptr ? Q.A.max_rank : 0);
+    const ProjectWs at = project_ws(X->dtype, X->rows, Q.P.rows, Q.P.cols, Q.P.G, Q.A.n, Q.A.max_rank);
     if (ws == nullptr || ws_bytes < at.total) return WINDQ_EWORKSPACE;
     if (!aligned(ws, 256)) return WINDQ_EINVAL;
     Q.X = static_cast<const uint16_t*>(X->data);

@@ -8,72 +8,6 @@ namespace windq {
 
 int check_tokens(const windq_mat* M, int64_t width, bool vector);
 
-// ------------------------------------------------------------------------------------------------ tokens by adapter
-// The tokens of adapter k in their own order, at places that start with a multiple of GROUP: place[] holds tokens, -1 where there is none.
-// Adapter k's first slot of GROUP places is (tokens of adapters below it) / GROUP + k: slots never overlap, and no adapter
-// has to wait for the counts of the others.
-constexpr int GROUP = 64;
-inline int64_t group_slots(int64_t T, int32_t n) { return T / GROUP + n + 1; }
-
-struct GroupArgs {
-    const int32_t* of;
-    int64_t T;
-    int32_t n;
-    int64_t slots;
-    int32_t* place;            // [slots * GROUP]
-    int32_t* first;            // [n] first place of an adapter
-    int32_t* count;            // [n] its tokens
-};
-
-__global__ __launch_bounds__(256) void group_kernel(const GroupArgs Q) {
-    __shared__ int32_t sums[2][4];
-    const int32_t k = blockIdx.x;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    int32_t below = 0, mine = 0;
-    for (int64_t t = threadIdx.x; t < Q.T; t += 256) {
-        const int32_t id = Q.of[t];
-        below += id >= 0 && id < k ? 1 : 0;
-        mine += id == k ? 1 : 0;
-    }
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) {
-        below += __shfl_xor(below, m, 64);
-        mine += __shfl_xor(mine, m, 64);
-    }
-    if (lane == 0) {
-        sums[0][wave] = below;
-        sums[1][wave] = mine;
-    }
-    __syncthreads();
-    below = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
-    mine = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
-    const int64_t first = ((int64_t)(below / GROUP) + k) * GROUP;
-    const int64_t end = k + 1 == Q.n ? Q.slots * GROUP : ((int64_t)((below + mine) / GROUP) + k + 1) * GROUP;
-    if (threadIdx.x == 0) {
-        Q.first[k] = (int32_t)first;
-        Q.count[k] = mine;
-    }
-    int64_t at = first;
-    __syncthreads();
-    for (int64_t t0 = 0; t0 < Q.T; t0 += 256) {             // a fixed order: tokens ascend
-        const int64_t t = t0 + threadIdx.x;
-        const bool hit = t < Q.T && Q.of[t] == k;
-        const uint64_t hits = __ballot(hit);
-        if (lane == 0) sums[0][wave] = __popcll(hits);
-        __syncthreads();
-        int32_t before = __popcll(hits & ((1ull << lane) - 1ull)), all = 0;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            before += w < wave ? sums[0][w] : 0;
-            all += sums[0][w];
-        }
-        if (hit) Q.place[at + before] = (int32_t)t;
-        at += all;
-        __syncthreads();
-    }
-    for (int64_t p = at + threadIdx.x; p < end; p += 256) Q.place[p] = -1;
-}
-
 // ------------------------------------------------------------------------------------------------ layouts
 // out [n][C][ldo] = in [n][R][C] transposed, rows padded with zeros up to ldo.
 template <typename T>
@@ -338,7 +272,7 @@ __global__ __launch_bounds__(256) void dx_f32_kernel(const DxArgs Q) {
 
 // ------------------------------------------------------------------------------------------------ the call
 struct GradWs {
-    size_t h, dh, bt, dy, place, first, count, total;
+    size_t h, dh, bt, dy, place, owner, first, count, total;
     int64_t rows8;
 };
 
@@ -357,6 +291,7 @@ GradWs grad_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t n, 
     w.dh = take((size_t)(T * max_rank) * 4);
     w.bt = take((size_t)n * (size_t)max_rank * (size_t)w.rows8 * eb);
     w.place = take((size_t)group_slots(T, n) * GROUP * 4);
+    w.owner = take((size_t)group_slots(T, n) * 4);
     w.first = take((size_t)n * 4);
     w.count = take((size_t)n * 4);
     w.total = at == 0 ? 256 : at;
@@ -409,7 +344,9 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
             G.place = reinterpret_cast<int32_t*>(ws + at.place);
             G.first = reinterpret_cast<int32_t*>(ws + at.first);
             G.count = reinterpret_cast<int32_t*>(ws + at.count);
-            WINDQ_LAUNCH(A.n, 256, group_kernel, G);
+            G.owner = reinterpret_cast<int32_t*>(ws + at.owner);
+            const int status = launch_group(G, st);
+            if (status != WINDQ_OK) return status;
             if (h == nullptr) {
                 float* const ht = reinterpret_cast<float*>(ws + at.h);
                 WINDQ_LAUNCH(wgs, 256, shrink_token_kernel<XT>, static_cast<const XT*>(X->data), X->ld, (int32_t)cols, A, false, ht);

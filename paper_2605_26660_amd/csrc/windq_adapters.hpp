@@ -5,6 +5,70 @@
 
 namespace windq {
 
+inline int64_t tokens_in(int64_t T, int64_t by) { return (T + by - 1) / by; }
+
+// The tokens of adapter k in their own order, at places that start with a multiple of GROUP: place[] holds tokens, -1 where there is none.
+// Adapter k's first slot of GROUP places is (tokens of adapters below it) / GROUP + k: slots never overlap, and no adapter
+// has to wait for the counts of the others.
+constexpr int GROUP = 64;
+inline int64_t group_slots(int64_t T, int32_t n) { return T / GROUP + n + 1; }
+
+struct GroupArgs {
+    const int32_t* of;
+    int64_t T;
+    int32_t n;
+    int64_t slots;
+    int32_t* place;            // [slots * GROUP]
+    int32_t* owner;            // [slots] adapter, or -1: an empty slot
+    int32_t* first;            // [n] first place of an adapter
+    int32_t* count;            // [n] its tokens
+};
+
+// Below so many tokens h is formed token by token: one launch instead of three.
+constexpr int64_t SHRINK_FEW = 64;
+
+// Sums of x_t a_r over pieces of the columns, tile by tile of one adapter's tokens.
+struct ShrinkArgs {
+    const void* X;             // [T][ld]
+    int64_t ld;
+    const void* a;             // [n][max_rank][lda]
+    int64_t lda;
+    int32_t width;             // columns, a multiple of 8
+    int32_t splits;
+    int64_t slots;
+    const int32_t* place;
+    const int32_t* owner;
+    AdapterArgs A;
+    float* part;               // [splits][slots * GROUP][ranks], ranks = max_rank rounded up to 16
+};
+
+// The pieces added up: h (times alpha where scaled) by token, and by place as three bfloat16 terms, transposed.
+struct JoinArgs {
+    const float* part;
+    int32_t splits;
+    int64_t slots;
+    const int32_t* place;
+    const int32_t* owner;
+    int64_t T;
+    AdapterArgs A;
+    bool scaled;
+    float* h;                  // [T][max_rank], or null
+    uint16_t* planes;          // [3][max_rank][slots * GROUP], or null
+};
+
+int launch_group(const GroupArgs& G, hipStream_t st);
+int launch_shrink(const ShrinkArgs& S, hipStream_t st);    // bfloat16
+int launch_join(const JoinArgs& J, hipStream_t st);
+inline int32_t shrink_ranks(int32_t max_rank) { return (max_rank + 15) / 16 * 16; }
+// Enough pieces that the launch has some workgroups for every CU, and a wavefront at least 64 columns.
+inline int32_t shrink_splits(int64_t slots, int64_t width) {
+    int64_t s = 1024 / slots;
+    if (s > width / 256) s = width / 256;
+    return (int32_t)(s < 1 ? 1 : (s > 32 ? 32 : s));
+}
+
+#ifdef __HIPCC__
+
 // ------------------------------------------------------------------------------------------------ h = A x, token by token
 // (On the way back: dh = alpha B^T dY, with B transposed in A's place.)  A workgroup takes 16 ranks of one token, a wavefront four of them; lanes walk the columns, eight at a time.
 template <typename XT>
@@ -57,5 +121,82 @@ __global__ __launch_bounds__(256) void shrink_token_kernel(const XT* __restrict_
         if (lane == i && r0 + i < A.max_rank) h[t * A.max_rank + r0 + i] = factor * acc[i];
     }
 }
+
+__device__ __forceinline__ uint4 pack8(const uint32_t (&w)[8]) {
+    return make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+}
+
+// What the adapters of a wavefront's 64 tokens add to a tile of 32 M rows x 64 tokens of 32x32x16 results (alpha_k B_k h_t, or A_k^T dh_t): for each
+// adapter among the tokens, its factors against its own tokens' h and the others' zeros.  row_of(f): where a lane's factors of
+// fragment f begin, k given; h [T][max_rank] times `scaled`'s alpha.  h enters as two bfloat16 terms (fp32: three, and the factors too).
+template <typename YT, int M, typename Rows>
+__device__ __forceinline__ void add_adapters(const AdapterArgs& A, const float* __restrict__ h, bool scaled, int64_t t0, int64_t T, int lane, Rows row_of,
+                                             f32x16 (&tot)[M][2]) {
+    constexpr int TA = sizeof(YT) == 4 ? 3 : 1, TH = sizeof(YT) == 4 ? 3 : 2;
+    const int sub = lane & 31, hh = lane >> 5;
+    const int32_t id = t0 + lane < T ? A.of[t0 + lane] : -1;
+    uint64_t left = __ballot(id >= 0 && id < A.n);
+    while (left != 0) {
+        const int32_t k = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+        const uint64_t mine = __ballot(id == k);
+        left &= ~mine;
+        const int32_t rank = adapter_rank(A, k);
+        const float factor = scaled && A.alpha != nullptr ? A.alpha[k] : 1.0f;
+        for (int32_t r0 = 0; r0 < rank; r0 += 16) {
+            const int32_t r = r0 + hh * 8;
+            uint4 bt[TH][2], at[TA][M];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                const bool has = ((mine >> (n * 32 + sub)) & 1ull) != 0 && r < rank;
+                float v[8] = {};
+                if (has) load8(h + (t0 + n * 32 + sub) * A.max_rank + r, v);
+                uint32_t w[3][8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) split3(r + i < rank ? factor * v[i] : 0.0f, w[0][i], w[1][i], w[2][i]);
+#pragma unroll
+                for (int m = 0; m < TH; ++m) bt[m][n] = pack8(w[m]);
+            }
+#pragma unroll
+            for (int f = 0; f < M; ++f) {
+                float v[8] = {};
+                if (r < rank) load8(row_of(k, f) + r, v);
+                uint32_t w[3][8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float x = r + i < rank ? v[i] : 0.0f;
+                    if (TA == 1) w[0][i] = __float_as_uint(x) >> 16;
+                    else split3(x, w[0][i], w[1][i], w[2][i]);
+                }
+#pragma unroll
+                for (int m = 0; m < TA; ++m) at[m][f] = pack8(w[m]);
+            }
+#pragma unroll
+            for (int ma = 0; ma < TA; ++ma)
+#pragma unroll
+                for (int mh = 0; mh < TH; ++mh)
+                    if (ma + mh < 3) {
+#pragma unroll
+                        for (int f = 0; f < M; ++f)
+#pragma unroll
+                            for (int n = 0; n < 2; ++n)
+                                tot[f][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(at[ma][f]), as_bf16x8(bt[mh][n]), tot[f][n], 0, 0, 0);
+                    }
+        }
+    }
+}
+
+// Direct loads to LDS: lane l's 16 (or 4) bytes go to `to` + 16 l (4 l); `to` is the same for the wavefront.  Written out because the compiler
+// would have every later read of LDS wait for them, whatever it reads; here whoever reads waits for vmcnt and a barrier first.
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return (uint32_t)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p);
+}
+__device__ __forceinline__ void lds_load16(uint32_t to, const void* from) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+}
+__device__ __forceinline__ void lds_load4(uint32_t to, const void* from) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+}
+
+#endif  // __HIPCC__
 
 }  // namespace windq

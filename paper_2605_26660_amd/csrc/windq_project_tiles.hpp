@@ -195,18 +195,6 @@ struct TileFields {
     }
 };
 
-// Direct loads to LDS: lane l's 16 (or 4) bytes go to `to` + 16 l (4 l); `to` is the same for the wavefront.  Written out because the compiler
-// would have every later read of LDS wait for them, whatever it reads; here whoever reads waits for vmcnt(0) and a barrier first.
-__device__ __forceinline__ uint32_t lds_address(const void* p) {
-    return (uint32_t)reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p);
-}
-__device__ __forceinline__ void lds_load16(uint32_t to, const void* from) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
-}
-__device__ __forceinline__ void lds_load4(uint32_t to, const void* from) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
-}
-
 template <typename YT, int S>
 __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArgs Q) {
     constexpr int NP = sizeof(YT) == 4 ? 3 : 1;
@@ -464,61 +452,9 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
             }
         }
 
-    // adapters: for each one among the wavefront's tokens, its B against the others' zeros and its own tokens' h
-    if (Q.h != nullptr) {
-        constexpr int TA = sizeof(YT) == 4 ? 3 : 1, TH = sizeof(YT) == 4 ? 3 : 2;       // terms of B and of alpha h
-        const int64_t t = t0 + wt * 64 + lane;
-        const int32_t id = t < Q.T ? Q.A.of[t] : -1;
-        uint64_t left = __ballot(id >= 0 && id < Q.A.n);
-        while (left != 0) {
-            const int32_t k = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
-            const uint64_t mine = __ballot(id == k);
-            left &= ~mine;
-            const int32_t rank = adapter_rank(Q.A, k);
-            const float factor = Q.A.alpha != nullptr ? Q.A.alpha[k] : 1.0f;
-            for (int32_t r0 = 0; r0 < rank; r0 += 16) {
-                const int32_t r = r0 + hh * 8;
-                uint4 bt[TH][2], at[TA][2];
-#pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    const bool has = ((mine >> (n * 32 + sub)) & 1ull) != 0 && r < rank;
-                    float v[8] = {};
-                    if (has) load8(Q.h + (t0 + wt * 64 + n * 32 + sub) * Q.A.max_rank + r, v);
-                    uint32_t w[3][8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) split3(r + i < rank ? factor * v[i] : 0.0f, w[0][i], w[1][i], w[2][i]);
-#pragma unroll
-                    for (int m = 0; m < TH; ++m) bt[m][n] = make_uint4(w[m][0] | w[m][1] << 16, w[m][2] | w[m][3] << 16, w[m][4] | w[m][5] << 16, w[m][6] | w[m][7] << 16);
-                }
-#pragma unroll
-                for (int f = 0; f < 2; ++f) {
-                    const int64_t row = rb * P.R_u + lrow[f];
-                    float v[8] = {};
-                    if (r < rank) load8(static_cast<const YT*>(Q.A.b) + ((int64_t)k * P.rows + row) * Q.A.max_rank + r, v);
-                    uint32_t w[3][8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float x = r + i < rank ? v[i] : 0.0f;
-                        if (TA == 1) w[0][i] = __float_as_uint(x) >> 16;
-                        else split3(x, w[0][i], w[1][i], w[2][i]);
-                    }
-#pragma unroll
-                    for (int m = 0; m < TA; ++m) at[m][f] = make_uint4(w[m][0] | w[m][1] << 16, w[m][2] | w[m][3] << 16, w[m][4] | w[m][5] << 16, w[m][6] | w[m][7] << 16);
-                }
-#pragma unroll
-                for (int ma = 0; ma < TA; ++ma)
-#pragma unroll
-                    for (int mh = 0; mh < TH; ++mh)
-                        if (ma + mh < 3) {
-#pragma unroll
-                            for (int f = 0; f < 2; ++f)
-#pragma unroll
-                                for (int n = 0; n < 2; ++n)
-                                    tot[f][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(at[ma][f]), as_bf16x8(bt[mh][n]), tot[f][n], 0, 0, 0);
-                        }
-            }
-        }
-    }
+    if (Q.h != nullptr)
+        add_adapters<YT, 2>(Q.A, Q.h, true, t0 + wt * 64, Q.T, lane,
+                            [&](int32_t k, int f) { return static_cast<const YT*>(Q.A.b) + ((int64_t)k * P.rows + rb * P.R_u + lrow[f]) * Q.A.max_rank; }, tot);
 
     YT* __restrict__ const Y = static_cast<YT*>(Q.Y);
     const bool whole = (Q.ldy & 3) == 0 && (reinterpret_cast<uintptr_t>(Y) & (4 * sizeof(YT) - 1)) == 0;
