@@ -89,19 +89,26 @@ __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkArgs Q) {
     }
     f32x4 acc[RF][4] = {};
     if (rank > 0) {
-#pragma unroll 2
-        for (int32_t s = s0 + wave; s < s1; s += 4) {
-            const bool in = s * 32 + q * 8 < Q.width;
-            const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-            bf16x8 a[RF], b[4];
+        constexpr int U = RF <= 4 ? 2 : 1;                  // steps whose loads are on their way together
+        const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+        for (int32_t s = s0 + wave; s < s1; s += 4 * U) {
+            uint4 a[U][RF], b[U][4];
 #pragma unroll
-            for (int n = 0; n < 4; ++n) b[n] = as_bf16x8(in ? *reinterpret_cast<const uint4*>(xp[n] + s * 32) : none);
+            for (int u = 0; u < U; ++u) {
+                const bool in = s + 4 * u < s1 && (s + 4 * u) * 32 + q * 8 < Q.width;
+                const int64_t c = in ? (s + 4 * u) * 32 : 0;
 #pragma unroll
-            for (int f = 0; f < RF; ++f) a[f] = as_bf16x8(in ? *reinterpret_cast<const uint4*>(ap[f] + s * 32) : none);
+                for (int n = 0; n < 4; ++n) b[u][n] = in ? *reinterpret_cast<const uint4*>(xp[n] + c) : none;
 #pragma unroll
-            for (int f = 0; f < RF; ++f)
+                for (int f = 0; f < RF; ++f) a[u][f] = in ? *reinterpret_cast<const uint4*>(ap[f] + c) : none;
+            }
 #pragma unroll
-                for (int n = 0; n < 4; ++n) acc[f][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[f], b[n], acc[f][n], 0, 0, 0);
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int f = 0; f < RF; ++f)
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+                        acc[f][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a[u][f]), as_bf16x8(b[u][n]), acc[f][n], 0, 0, 0);
         }
     }
 #pragma unroll
@@ -113,7 +120,7 @@ __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkArgs Q) {
     __syncthreads();
     float* __restrict__ const out = Q.part + ((int64_t)split * Q.slots + slot) * GROUP * (RF * 16);
     for (int e = threadIdx.x; e < GROUP * RF * 16; e += 256) {
-        const int r = e % (RF * 16), n = e / (RF * 16);
+        const int r = e / GROUP, n = e % GROUP;
         out[e] = r < rank ? ((red[0][r][n] + red[1][r][n]) + red[2][r][n]) + red[3][r][n] : 0.0f;
     }
 }
@@ -153,24 +160,35 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinArgs Q) {
     const int32_t k = Q.owner[slot];
     if (k < 0) return;
     const float factor = Q.scaled && Q.A.alpha != nullptr ? Q.A.alpha[k] : 1.0f;
-    for (int e = threadIdx.x; e < GROUP * ranks; e += 256) {
-        const int r = e / GROUP, n = e % GROUP;            // places side by side
-        if (r >= R) break;
-        const int32_t t = Q.place[slot * GROUP + n];
-        float v = 0.0f;
-        if (t >= 0) {
-            const float* __restrict__ const p = Q.part + (slot * GROUP + n) * ranks + r;
-            for (int32_t s = 0; s < Q.splits; ++s) v += p[(int64_t)s * places * ranks];
-            v *= factor;
-            if (Q.h != nullptr) Q.h[(int64_t)t * R + r] = v;
+    __shared__ float tile[GROUP][33];                      // 32 ranks at a time, places by ranks for h
+    for (int r0 = 0; r0 < R; r0 += 32) {
+        __syncthreads();
+        for (int e = threadIdx.x; e < GROUP * 32; e += 256) {
+            const int r = r0 + e / GROUP, n = e % GROUP;   // places side by side
+            if (r >= R) break;
+            float v = 0.0f;
+            if (Q.place[slot * GROUP + n] >= 0) {
+                const float* __restrict__ const p = Q.part + (slot * ranks + r) * GROUP + n;
+                for (int32_t s = 0; s < Q.splits; ++s) v += p[(int64_t)s * places * ranks];
+                v *= factor;
+            }
+            tile[n][r - r0] = v;
+            if (Q.planes != nullptr) {
+                uint32_t hi, mid, lo;
+                split3(v, hi, mid, lo);
+                uint16_t* __restrict__ const o = Q.planes + r * places + slot * GROUP + n;
+                o[0] = (uint16_t)hi;
+                o[R * places] = (uint16_t)mid;
+                o[2 * R * places] = (uint16_t)lo;
+            }
         }
-        if (Q.planes != nullptr) {
-            uint32_t hi, mid, lo;
-            split3(v, hi, mid, lo);
-            uint16_t* __restrict__ const o = Q.planes + r * places + slot * GROUP + n;
-            o[0] = (uint16_t)hi;
-            o[R * places] = (uint16_t)mid;
-            o[2 * R * places] = (uint16_t)lo;
+        __syncthreads();
+        if (Q.h != nullptr) {
+            for (int e = threadIdx.x; e < GROUP * 32; e += 256) {
+                const int n = e >> 5, r = r0 + (e & 31);
+                const int32_t t = Q.place[slot * GROUP + n];
+                if (t >= 0 && r < R) Q.h[(int64_t)t * R + r] = tile[n][e & 31];
+            }
         }
     }
 }

@@ -2,7 +2,7 @@
 //   dh_t = alpha_k B_k^T dY_t     dX[t] = w_hat^T dY_t + A_k^T dh_t     dA[k] = sum_t dh_t x_t^T     dB[k] = alpha_k sum_t dY_t h_t^T
 #include <math.h>
 
-#include "windq_adapters.hpp"
+#include "windq_gemm.hpp"
 
 namespace windq {
 
@@ -68,6 +68,118 @@ __global__ __launch_bounds__(256) void outer_kernel(const XT* __restrict__ right
         const float v = r0 + r < rank && n > 0 ? factor * acc[r] : 0.0f;
         if (by_column) out[((int64_t)k * width + c) * A.max_rank + r0 + r] = v;
         else out[((int64_t)k * A.max_rank + r0 + r) * width + c] = v;
+    }
+}
+
+// The same for bfloat16 on the matrix instructions: 128 columns of the right side by up to 64 ranks, the sum over an adapter's places 32 at a time,
+// shared by four wavefronts.  The sum runs over tokens, and an operand wants eight consecutive tokens of one column in a lane, while
+// a token's columns lie side by side: a lane reads eight tokens by eight columns and pairs tokens up in registers, which gives one
+// operand for each of its eight columns (every eighth column shares an instruction, as in the reconstruction).  The left side comes
+// transposed and as three bfloat16 terms, so products are exact to fp32.
+struct OuterArgs {
+    const uint16_t* right;     // [T][ld], readable up to a multiple of 8 columns
+    int64_t ld, width;
+    const uint16_t* planes;    // [3][max_rank][places]
+    int64_t places;
+    const int32_t* place;
+    const int32_t* first;
+    const int32_t* count;
+    AdapterArgs A;
+    bool scaled, by_column;
+    float* out;
+    int64_t tiles;             // of 128 columns
+};
+
+__device__ __forceinline__ uint32_t halves(uint32_t a, uint32_t b, bool high) {
+    return __builtin_amdgcn_perm(b, a, high ? 0x07060302u : 0x05040100u);
+}
+
+template <int RF>
+__global__ __launch_bounds__(256) void outer_tiles_kernel(const OuterArgs Q1, const OuterArgs Q2, const int64_t first2) {
+    __shared__ float red[2][RF * 16][132];
+    const OuterArgs& Q = blockIdx.x < first2 ? Q1 : Q2;
+    const int64_t block = blockIdx.x < first2 ? blockIdx.x : blockIdx.x - first2;
+    const int32_t groups = (Q.A.max_rank + 63) / 64;
+    const int32_t k = (int32_t)(block / (Q.tiles * groups));
+    const int64_t rest = block - k * Q.tiles * groups;
+    const int32_t r0 = (int32_t)(rest / Q.tiles) * 64;
+    const int64_t c0 = (rest - rest / Q.tiles * Q.tiles) * 128;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
+    const int32_t rank = adapter_rank(Q.A, k), n = Q.count[k], p0 = Q.first[k];
+    const int64_t col = c0 + sub * 8;
+    f32x4 acc[8][RF] = {};
+    if (r0 < rank) {
+        for (int32_t i0 = wave * 32; i0 < n; i0 += 128) {
+            uint4 x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int32_t i = i0 + q * 8 + j;
+                const int32_t t = i < n ? Q.place[p0 + i] : -1;
+                x[j] = t >= 0 && col < Q.width ? *reinterpret_cast<const uint4*>(Q.right + (int64_t)t * Q.ld + col) : make_uint4(0u, 0u, 0u, 0u);
+            }
+            bf16x8 b[3][RF];
+#pragma unroll
+            for (int m = 0; m < 3; ++m)
+#pragma unroll
+                for (int f = 0; f < RF; ++f) {
+                    const int32_t r = r0 + f * 16 + sub;
+                    b[m][f] = as_bf16x8(r < rank ? *reinterpret_cast<const uint4*>(Q.planes + ((int64_t)m * Q.A.max_rank + r) * Q.places + p0 + i0 + q * 8) : make_uint4(0u, 0u, 0u, 0u));
+                }
+#pragma unroll
+            for (int m = 0; m < 8; ++m) {
+                uint32_t w[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = (m >> 1) == 0 ? x[j].x : ((m >> 1) == 1 ? x[j].y : ((m >> 1) == 2 ? x[j].z : x[j].w));
+                const bool h = (m & 1) != 0;
+                const bf16x8 a = as_bf16x8(make_uint4(halves(w[0], w[1], h), halves(w[2], w[3], h), halves(w[4], w[5], h), halves(w[6], w[7], h)));
+#pragma unroll
+                for (int f = 0; f < RF; ++f)
+#pragma unroll
+                    for (int p = 2; p >= 0; --p) acc[m][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[p][f], acc[m][f], 0, 0, 0);
+            }
+        }
+    }
+    // wavefronts 2 and 3 hand theirs to 0 and 1, and 1 its own to 0: a fixed order
+#pragma unroll
+    for (int round = 2; round >= 1; round >>= 1) {
+        if (wave >= round && wave < 2 * round) {
+#pragma unroll
+            for (int m = 0; m < 8; ++m)
+#pragma unroll
+                for (int f = 0; f < RF; ++f)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) red[wave - round][f * 16 + sub][(4 * q + i) * 8 + m] = acc[m][f][i];
+        }
+        __syncthreads();
+        if (wave < round) {
+#pragma unroll
+            for (int m = 0; m < 8; ++m)
+#pragma unroll
+                for (int f = 0; f < RF; ++f)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[m][f][i] += red[wave][f * 16 + sub][(4 * q + i) * 8 + m];
+        }
+        __syncthreads();
+    }
+    if (wave == 0) {
+#pragma unroll
+        for (int m = 0; m < 8; ++m)
+#pragma unroll
+            for (int f = 0; f < RF; ++f)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) red[0][f * 16 + sub][(4 * q + i) * 8 + m] = acc[m][f][i];
+    }
+    __syncthreads();
+    const float factor = Q.scaled && Q.A.alpha != nullptr ? Q.A.alpha[k] : 1.0f;
+    const int32_t R = Q.A.max_rank, ranks = R - r0 < RF * 16 ? R - r0 : RF * 16;
+    const int64_t left = Q.width - c0;
+    const int32_t cols = left < 128 ? (int32_t)left : 128;
+    for (int e = threadIdx.x; e < ranks * 128; e += 256) {
+        const int r = Q.by_column ? e % ranks : e >> 7, c = Q.by_column ? e / ranks : e & 127;
+        if (c >= cols) continue;
+        const float v = r0 + r < rank ? factor * red[0][r][c] : 0.0f;
+        if (Q.by_column) Q.out[((int64_t)k * Q.width + c0 + c) * R + r0 + r] = v;
+        else Q.out[((int64_t)k * R + r0 + r) * Q.width + c0 + c] = v;
     }
 }
 
@@ -204,6 +316,28 @@ __global__ __launch_bounds__(256) void dx_kernel(const DxArgs Q) {
     }
 }
 
+// w_hat rounded to bfloat16 and turned: wt [cols][K], zeros from the last row to K.  A thread has eight rows by eight columns.
+__global__ __launch_bounds__(256) void turn_kernel(const PackArgs P, int32_t K, uint16_t* __restrict__ wt) {
+    __shared__ uint16_t trits_of[256];
+    trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
+    __syncthreads();
+    const int32_t row_blocks = (K + 255) / 256;
+    const int64_t cb = blockIdx.x / row_blocks;
+    const int64_t r0 = (blockIdx.x - cb * row_blocks) * 256 + (threadIdx.x & 31) * 8, col = cb * 64 + (threadIdx.x >> 5) * 8;
+    if (col >= P.cols || r0 >= K) return;
+    uint32_t v[8][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float w0[8] = {}, w1[8] = {};
+        if (r0 + 2 * i < P.rows) weight_octet(P, r0 + 2 * i, col, trits_of, w0);
+        if (r0 + 2 * i + 1 < P.rows) weight_octet(P, r0 + 2 * i + 1, col, trits_of, w1);
+#pragma unroll
+        for (int m = 0; m < 8; ++m) v[m][i] = f32_to_bf16_bits(w0[m]) | f32_to_bf16_bits(w1[m]) << 16;
+    }
+#pragma unroll
+    for (int m = 0; m < 8; ++m) *reinterpret_cast<uint4*>(wt + (col + m) * K + r0) = make_uint4(v[m][0], v[m][1], v[m][2], v[m][3]);
+}
+
 // fp32: 64 columns and 64 tokens a workgroup, 32 rows at a time through LDS, on the fp32 matrix instructions.
 __global__ __launch_bounds__(256) void dx_f32_kernel(const DxArgs Q) {
     __shared__ float wt[32][68], yt[32][68];
@@ -271,29 +405,40 @@ __global__ __launch_bounds__(256) void dx_f32_kernel(const DxArgs Q) {
 }
 
 // ------------------------------------------------------------------------------------------------ the call
+// Tokens from which on the packed matrix is reconstructed once for dX.
+constexpr int64_t TURN_FROM = 256;
+
 struct GradWs {
-    size_t h, dh, bt, dy, place, owner, first, count, total;
-    int64_t rows8;
+    size_t h, dh, bt, at, dy, place, owner, first, count, part, planes_h, planes_dh, wt, total;
+    int64_t ld;                // of dY's copy and of B transposed
 };
 
 GradWs grad_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t n, int32_t max_rank) {
     const size_t eb = dtype == WINDQ_F32 ? 4 : 2;
+    const bool bf = dtype == WINDQ_BF16;
     GradWs w;
-    w.rows8 = (rows + 7) / 8 * 8;
+    w.ld = bf ? gemm_k(rows) : (rows + 7) / 8 * 8;
     size_t at = 0;
     auto take = [&at](size_t bytes) {
         const size_t here = at;
         at += round_up(bytes, 256);
         return here;
     };
-    w.dy = take((size_t)(T * w.rows8) * eb);
+    const int64_t slots = group_slots(T, n);
+    const int64_t wide = rows > cols ? rows : cols;
+    w.dy = take((size_t)(T * w.ld) * eb);
     w.h = take((size_t)(T * max_rank) * 4);
     w.dh = take((size_t)(T * max_rank) * 4);
-    w.bt = take((size_t)n * (size_t)max_rank * (size_t)w.rows8 * eb);
-    w.place = take((size_t)group_slots(T, n) * GROUP * 4);
-    w.owner = take((size_t)group_slots(T, n) * 4);
+    w.bt = take((size_t)n * (size_t)max_rank * (size_t)w.ld * eb);
+    w.at = take(bf ? (size_t)n * (size_t)max_rank * (size_t)cols * eb : 0);
+    w.place = take((size_t)slots * GROUP * 4);
+    w.owner = take((size_t)slots * 4);
     w.first = take((size_t)n * 4);
     w.count = take((size_t)n * 4);
+    w.part = take(bf && n > 0 ? (size_t)shrink_splits(slots, wide) * (size_t)slots * GROUP * (size_t)shrink_ranks(max_rank) * 4 : 0);
+    w.planes_h = take(bf && n > 0 ? (size_t)slots * GROUP * (size_t)max_rank * 6 : 0);
+    w.planes_dh = take(bf && n > 0 ? (size_t)slots * GROUP * (size_t)max_rank * 6 : 0);
+    w.wt = take(bf && T >= TURN_FROM ? (size_t)gemm_cols(cols) * (size_t)gemm_k(rows) * 2 : 0);
     w.total = at == 0 ? 256 : at;
     return w;
 }
@@ -316,55 +461,95 @@ template <typename XT>
 int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h, float* dA, float* dB, char* ws, const GradWs& at, hipStream_t st) {
     const int64_t T = Q.T, rows = Q.P.rows, cols = Q.P.cols;
     const bool side = Q.A.n > 0;
+    constexpr bool bf = sizeof(XT) == 2;
+    const bool turn = bf && Q.packed && Q.dX != nullptr && T >= TURN_FROM;
     const AdapterArgs A = Q.A;
-    if (T > 0 && (dY->ld % 8 != 0 || rows % 8 != 0 || !aligned(dY->data, 16))) {
+    if (T > 0 && (dY->ld % 8 != 0 || rows % (turn ? GM_K : 8) != 0 || !aligned(dY->data, 16))) {
         XT* to = reinterpret_cast<XT*>(ws + at.dy);
-        WINDQ_LAUNCH((T * at.rows8 + 255) / 256, 256, align_kernel<XT>, static_cast<const XT*>(dY->data), dY->ld, T, rows, at.rows8, to);
+        WINDQ_LAUNCH((T * at.ld + 255) / 256, 256, align_kernel<XT>, static_cast<const XT*>(dY->data), dY->ld, T, rows, at.ld, to);
         Q.dY = to;
-        Q.ldy = at.rows8;
+        Q.ldy = at.ld;
     } else {
         Q.dY = dY->data;
         Q.ldy = dY->ld;
     }
+    const XT* const dYv = static_cast<const XT*>(Q.dY);
+    const int32_t rows8 = (int32_t)((rows + 7) / 8 * 8);
     if (side) {
         float* const dh = reinterpret_cast<float*>(ws + at.dh);
         XT* const bt = reinterpret_cast<XT*>(ws + at.bt);
-        WINDQ_LAUNCH((int64_t)A.n * ((at.rows8 + 63) / 64) * ((A.max_rank + 63) / 64), 256, transpose_kernel<XT>, static_cast<const XT*>(A.b), rows, A.max_rank, at.rows8, bt);
-        AdapterArgs B = A;
-        B.a = bt;
-        const int64_t wgs = T * ((A.max_rank + 15) / 16);
-        WINDQ_LAUNCH(wgs, 256, shrink_token_kernel<XT>, static_cast<const XT*>(Q.dY), Q.ldy, (int32_t)at.rows8, B, true, dh);
-        Q.dh = dh;
-        if (dA != nullptr) {
-            GroupArgs G;
-            G.of = A.of;
-            G.T = T;
-            G.n = A.n;
-            G.slots = group_slots(T, A.n);
-            G.place = reinterpret_cast<int32_t*>(ws + at.place);
-            G.first = reinterpret_cast<int32_t*>(ws + at.first);
-            G.count = reinterpret_cast<int32_t*>(ws + at.count);
-            G.owner = reinterpret_cast<int32_t*>(ws + at.owner);
+        WINDQ_LAUNCH((int64_t)A.n * ((at.ld + 63) / 64) * ((A.max_rank + 63) / 64), 256, transpose_kernel<XT>, static_cast<const XT*>(A.b), rows, A.max_rank, at.ld, bt);
+        GroupArgs G = {A.of, T, A.n, group_slots(T, A.n), reinterpret_cast<int32_t*>(ws + at.place), reinterpret_cast<int32_t*>(ws + at.owner),
+                       reinterpret_cast<int32_t*>(ws + at.first), reinterpret_cast<int32_t*>(ws + at.count)};
+        const bool outer = dA != nullptr;
+        const int64_t tokens = T * ((A.max_rank + 15) / 16);
+        if (bf || outer) {
             const int status = launch_group(G, st);
             if (status != WINDQ_OK) return status;
-            if (h == nullptr) {
-                float* const ht = reinterpret_cast<float*>(ws + at.h);
-                WINDQ_LAUNCH(wgs, 256, shrink_token_kernel<XT>, static_cast<const XT*>(X->data), X->ld, (int32_t)cols, A, false, ht);
-                h = ht;
-            }
-            const int64_t groups = (int64_t)A.n * ((A.max_rank + 15) / 16);
-            WINDQ_LAUNCH(groups * ((cols + 255) / 256), 256, outer_kernel<XT>, static_cast<const XT*>(X->data), X->ld, cols, dh, A, G.place, G.first, G.count, false, false, dA);
-            WINDQ_LAUNCH(groups * ((rows + 255) / 256), 256, outer_kernel<XT>, static_cast<const XT*>(Q.dY), Q.ldy, rows, h, A, G.place, G.first, G.count, true, true, dB);
         }
+        if constexpr (bf) {
+            float* const part = reinterpret_cast<float*>(ws + at.part);
+            uint16_t* const planes_h = reinterpret_cast<uint16_t*>(ws + at.planes_h);
+            uint16_t* const planes_dh = reinterpret_cast<uint16_t*>(ws + at.planes_dh);
+            auto shrink = [&](const void* x, int64_t ld, const void* a, int64_t lda, int64_t width, bool scaled, float* to, uint16_t* planes) {
+                ShrinkArgs S = {x, ld, a, lda, (int32_t)width, shrink_splits(G.slots, width), G.slots, G.place, G.owner, A, part};
+                JoinArgs J = {part, S.splits, G.slots, G.place, G.owner, T, A, scaled, to, planes};
+                const int status = launch_shrink(S, st);
+                return status == WINDQ_OK ? launch_join(J, st) : status;
+            };
+            int status = shrink(Q.dY, Q.ldy, bt, at.ld, rows8, true, dh, outer ? planes_dh : nullptr);
+            if (status == WINDQ_OK && outer) status = shrink(X->data, X->ld, A.a, cols, cols, false, nullptr, planes_h);
+            if (status != WINDQ_OK) return status;
+            if (outer) {
+                const int32_t groups = (A.max_rank + 63) / 64;
+                OuterArgs O1 = {static_cast<const uint16_t*>(X->data), X->ld, cols, planes_dh, G.slots * GROUP, G.place, G.first, G.count, A, false, false, dA, (cols + 127) / 128};
+                OuterArgs O2 = {dYv, Q.ldy, rows, planes_h, G.slots * GROUP, G.place, G.first, G.count, A, true, true, dB, (rows + 127) / 128};
+                const int64_t n1 = (int64_t)A.n * groups * O1.tiles, n2 = (int64_t)A.n * groups * O2.tiles;
+                const int32_t RF = A.max_rank >= 64 ? 4 : shrink_ranks(A.max_rank) / 16;
+                if (RF == 1) WINDQ_LAUNCH(n1 + n2, 256, outer_tiles_kernel<1>, O1, O2, n1);
+                else if (RF == 2) WINDQ_LAUNCH(n1 + n2, 256, outer_tiles_kernel<2>, O1, O2, n1);
+                else if (RF == 3) WINDQ_LAUNCH(n1 + n2, 256, outer_tiles_kernel<3>, O1, O2, n1);
+                else WINDQ_LAUNCH(n1 + n2, 256, outer_tiles_kernel<4>, O1, O2, n1);
+            }
+        } else {
+            AdapterArgs B = A;
+            B.a = bt;
+            WINDQ_LAUNCH(tokens, 256, shrink_token_kernel<XT>, dYv, Q.ldy, rows8, B, true, dh);
+            if (outer) {
+                if (h == nullptr) {
+                    float* const ht = reinterpret_cast<float*>(ws + at.h);
+                    WINDQ_LAUNCH(tokens, 256, shrink_token_kernel<XT>, static_cast<const XT*>(X->data), X->ld, (int32_t)cols, A, false, ht);
+                    h = ht;
+                }
+                const int64_t groups = (int64_t)A.n * ((A.max_rank + 15) / 16);
+                WINDQ_LAUNCH(groups * ((cols + 255) / 256), 256, outer_kernel<XT>, static_cast<const XT*>(X->data), X->ld, cols, dh, A, G.place, G.first, G.count, false, false, dA);
+                WINDQ_LAUNCH(groups * ((rows + 255) / 256), 256, outer_kernel<XT>, dYv, Q.ldy, rows, h, A, G.place, G.first, G.count, true, true, dB);
+            }
+        }
+        Q.dh = dh;
     }
-    if (Q.dX == nullptr) return WINDQ_OK;
-    if constexpr (sizeof(XT) == 4) {
-        WINDQ_LAUNCH(((cols + 63) / 64) * ((T + 63) / 64), 256, dx_f32_kernel, Q);
-    } else {
+    if (Q.dX == nullptr || T == 0) return WINDQ_OK;
+    if constexpr (bf) {
+        if (turn) {
+            uint16_t* const wt = reinterpret_cast<uint16_t*>(ws + at.wt);
+            const int32_t K = (int32_t)gemm_k(rows);
+            WINDQ_LAUNCH(((cols + 63) / 64) * ((K + 255) / 256), 256, turn_kernel, Q.P, K, wt);
+            GemmArgs M = {wt, dYv, Q.ldy, K, T, cols, static_cast<uint16_t*>(Q.dX), Q.ldx, Q.dh, nullptr, A, (uint32_t)((cols + GM_M - 1) / GM_M)};
+            if (side) {
+                uint16_t* const to = reinterpret_cast<uint16_t*>(ws + at.at);
+                WINDQ_LAUNCH((int64_t)A.n * ((A.max_rank + 63) / 64) * ((cols + 63) / 64), 256, transpose_kernel<uint16_t>, static_cast<const uint16_t*>(A.a), (int64_t)A.max_rank,
+                             (int32_t)cols, (int64_t)A.max_rank, to);
+                M.at = to;
+            }
+            WINDQ_LAUNCH((int64_t)M.col_blocks * tokens_in(T, GM_N), GM_THREADS, dx_gemm_kernel, M);
+            return WINDQ_OK;
+        }
         const int64_t blocks = (cols + DX_COLS - 1) / DX_COLS;
         if (T <= 64) WINDQ_LAUNCH(blocks * ((T + 63) / 64), 256, dx_kernel<1>, Q);
         else if (T <= 128) WINDQ_LAUNCH(blocks * ((T + 127) / 128), 256, dx_kernel<2>, Q);
         else WINDQ_LAUNCH(blocks * ((T + 255) / 256), 256, dx_kernel<4>, Q);
+    } else {
+        WINDQ_LAUNCH(((cols + 63) / 64) * ((T + 63) / 64), 256, dx_f32_kernel, Q);
     }
     return WINDQ_OK;
 }

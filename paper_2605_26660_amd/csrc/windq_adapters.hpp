@@ -39,7 +39,7 @@ struct ShrinkArgs {
     const int32_t* place;
     const int32_t* owner;
     AdapterArgs A;
-    float* part;               // [splits][slots * GROUP][ranks], ranks = max_rank rounded up to 16
+    float* part;               // [splits][slots][ranks][GROUP], ranks = max_rank rounded up to 16
 };
 
 // The pieces added up: h (times alpha where scaled) by token, and by place as three bfloat16 terms, transposed.
@@ -62,7 +62,7 @@ int launch_join(const JoinArgs& J, hipStream_t st);
 inline int32_t shrink_ranks(int32_t max_rank) { return (max_rank + 15) / 16 * 16; }
 // Enough pieces that the launch has some workgroups for every CU, and a wavefront at least 64 columns.
 inline int32_t shrink_splits(int64_t slots, int64_t width) {
-    int64_t s = 1024 / slots;
+    int64_t s = 512 / slots;
     if (s > width / 256) s = width / 256;
     return (int32_t)(s < 1 ? 1 : (s > 32 ? 32 : s));
 }

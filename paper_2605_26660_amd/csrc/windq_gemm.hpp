@@ -1,0 +1,152 @@
+// dX = w_hat^T dY for many tokens of bfloat16: a plain product of two matrices whose rows lie along the sum's axis.
+//
+// Codes lie along columns and the sum runs along rows, so a tile of weights would have to be turned for every 128 tokens.  The packed
+// matrix is reconstructed once instead, rounded to bfloat16 and turned (wt [cols][rows], 2 bytes a weight: less than a tenth of the
+// product's time), and the product then spends nothing but matrix instructions and their operands' way: 256 columns x 128
+// tokens a workgroup, four wavefronts with 128 x 64 results each as 4 x 2 fragments of 32x32x16 instructions, one per SIMD.
+//   64 of the sum at a time go to LDS by direct loads, three buffers: while one is multiplied the next has landed and the one
+// after is on its way.  There is one barrier per buffer, ahead of its last step: by then all of it has been read into registers, and the next
+// one's first operands are read across it.  A row's eight 16-byte slots are exchanged by the row's low bits, so that 32 lanes reading 32
+// rows' same slot meet all banks.
+#pragma once
+
+#include "windq_adapters.hpp"
+
+namespace windq {
+
+constexpr int GM_M = 256, GM_N = 128, GM_K = 64, GM_THREADS = 256, GM_BUFFERS = 3;
+
+struct GemmArgs {
+    const uint16_t* wt;        // [cols rounded up to GM_M][K]
+    const uint16_t* dY;        // [T][ldy], zeros from rows to K
+    int64_t ldy;
+    int32_t K;                 // rows rounded up to GM_K
+    int64_t T, cols;
+    uint16_t* dX;
+    int64_t ldx;
+    const float* dh;           // or null: no adapters
+    const uint16_t* at;        // [n][cols][max_rank]
+    AdapterArgs A;
+    uint32_t col_blocks;
+};
+
+inline int64_t gemm_k(int64_t rows) { return (rows + GM_K - 1) / GM_K * GM_K; }
+inline int64_t gemm_cols(int64_t cols) { return (cols + GM_M - 1) / GM_M * GM_M; }
+
+#ifdef __HIPCC__
+
+__global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
+    __shared__ uint4 tile[GM_BUFFERS][(GM_M + GM_N) * 8];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, sub = lane & 31, hh = lane >> 5;
+    const int wm = wave & 1, wn = wave >> 1;
+    // Consecutive workgroups land on the eight XCDs in turn; each XCD gets a run of tiles that share tokens.
+    const uint32_t n_tiles = gridDim.x, per = n_tiles >> 3;
+    const uint32_t id = blockIdx.x < per * 8 ? (blockIdx.x & 7) * per + (blockIdx.x >> 3) : blockIdx.x;
+    const uint32_t tb = id / Q.col_blocks;
+    const int64_t c0 = (int64_t)(id - tb * Q.col_blocks) * GM_M, t0 = (int64_t)tb * GM_N;
+
+    // A lane's share of a tile: slot (lane & 7) of rows 8 wave + lane / 8, 32 rows further on each time; slot p of row r holds the
+    // sixteen bytes of slot p ^ (r & 7).
+    const int lr = wave * 8 + (lane >> 3), slot = (lane & 7) ^ (lr & 7);
+    const uint16_t* const am = Q.wt + (c0 + lr) * Q.K + slot * 8;
+    const uint16_t* bn[GM_N / 32];
+#pragma unroll
+    for (int i = 0; i < GM_N / 32; ++i) {
+        const int64_t t = t0 + i * 32 + lr;
+        bn[i] = Q.dY + (t < Q.T ? t : Q.T - 1) * Q.ldy + slot * 8;
+    }
+    const uint32_t lds = lds_address(tile);
+    auto load_a = [&](int i, int32_t k, int buf) { lds_load16(lds + (buf * (GM_M + GM_N) * 8 + i * 256 + wave * 64) * 16, am + (int64_t)i * 32 * Q.K + k * GM_K); };
+    auto load_b = [&](int i, int32_t k, int buf) { lds_load16(lds + (buf * (GM_M + GM_N) * 8 + GM_M * 8 + i * 256 + wave * 64) * 16, bn[i] + k * GM_K); };
+    // Operands of step s (16 of the sum): octet 2 s + hh of a row.
+    const uint32_t arow = (wm * 128 + sub) * 128, brow = GM_M * 128 + (wn * 64 + sub) * 128;
+    auto read = [&](int buf, int s, bf16x8 (&a)[4], bf16x8 (&b)[2]) {
+        const char* const at = reinterpret_cast<const char*>(tile[buf]);
+        const uint32_t o = (uint32_t)((2 * s + hh) ^ (sub & 7)) * 16;
+#pragma unroll
+        for (int f = 0; f < 4; ++f) a[f] = as_bf16x8(*reinterpret_cast<const uint4*>(at + arow + f * 32 * 128 + o));
+#pragma unroll
+        for (int n = 0; n < 2; ++n) b[n] = as_bf16x8(*reinterpret_cast<const uint4*>(at + brow + n * 32 * 128 + o));
+    };
+
+    const int32_t n_k = Q.K / GM_K;
+    f32x16 acc[4][2] = {};
+    if (n_k > 0) {
+#pragma unroll
+        for (int i = 0; i < GM_M / 32; ++i) load_a(i, 0, 0);
+#pragma unroll
+        for (int i = 0; i < GM_N / 32; ++i) load_b(i, 0, 0);
+        const int32_t k1 = n_k > 1 ? 1 : 0;
+#pragma unroll
+        for (int i = 0; i < GM_M / 32; ++i) load_a(i, k1, 1);
+#pragma unroll
+        for (int i = 0; i < GM_N / 32; ++i) load_b(i, k1, 1);
+        asm volatile("s_waitcnt vmcnt(12)" ::: "memory");
+        __syncthreads();
+        bf16x8 a[2][4], b[2][2];
+        read(0, 0, a[0], b[0]);
+        int buf = 0;
+        for (int32_t k = 0; k < n_k; ++k) {
+            const int next = buf == 2 ? 0 : buf + 1, then = next == 2 ? 0 : next + 1;
+            const int32_t k2 = k + 2 < n_k ? k + 2 : n_k - 1;       // past the end: again the last, into a buffer that nobody reads
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                // twelve loads in the first three steps
+                if (s < 3) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int j = s * 4 + i;
+                        if (j < GM_M / 32) load_a(j, k2, then);
+                        else load_b(j - GM_M / 32, k2, then);
+                    }
+                    read(buf, s + 1, a[(s + 1) & 1], b[(s + 1) & 1]);
+                } else {
+                    asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)" ::: "memory");       // the next buffer's loads are done, this one's reads too
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    read(next, 0, a[0], b[0]);
+                }
+#pragma unroll
+                for (int f = 0; f < 4; ++f)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) acc[f][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s & 1][f], b[s & 1][n], acc[f][n], 0, 0, 0);
+            }
+            buf = next;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+
+    if (Q.dh != nullptr)
+        add_adapters<uint16_t, 4>(Q.A, Q.dh, false, t0 + wn * 64, Q.T, lane, [&](int32_t k, int f) {
+            const int64_t c = c0 + wm * 128 + f * 32 + sub;
+            return Q.at + ((int64_t)k * Q.cols + (c < Q.cols ? c : Q.cols - 1)) * Q.A.max_rank;
+        }, acc);
+
+    const bool whole = (Q.ldx & 3) == 0 && (reinterpret_cast<uintptr_t>(Q.dX) & 7) == 0;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        const int64_t t = t0 + wn * 64 + n * 32 + sub;
+        if (t >= Q.T) continue;
+#pragma unroll
+        for (int f = 0; f < 4; ++f)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int64_t c = c0 + wm * 128 + f * 32 + g * 8 + hh * 4;
+                if (c >= Q.cols) continue;                 // columns come in eights
+                uint16_t* __restrict__ const o = Q.dX + t * Q.ldx + c;
+                uint32_t v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = f32_to_bf16_bits(acc[f][n][g * 4 + i]);
+                if (whole) {
+                    *reinterpret_cast<uint2*>(o) = make_uint2(v[0] | v[1] << 16, v[2] | v[3] << 16);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] = (uint16_t)v[i];
+                }
+            }
+    }
+}
+
+#endif  // __HIPCC__
+
+}  // namespace windq
