@@ -61,7 +61,7 @@ int launch_group(const GroupArgs& G, hipStream_t st) {
     return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
 }
 
-// 64 tokens of one adapter by up to 16 RF ranks, over a piece of the columns that the four wavefronts share 32 at a time.  Both factors
+// 64 tokens of one adapter by up to 16 RF ranks, over a piece of the columns that the four wavefronts share 64 at a time.  Both factors
 // are rows along the sum's axis, so operands come straight from memory; ranks are the M side.  Bound by reading X once.
 template <int RF>
 __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkArgs Q) {
@@ -72,38 +72,38 @@ __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkArgs Q) {
     if (k < 0) return;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
     const int32_t rank = adapter_rank(Q.A, k);
-    const int32_t steps = (Q.width + 31) / 32, per = (steps + Q.splits - 1) / Q.splits;
+    const int32_t steps = (Q.width + 63) / 64, per = (steps + Q.splits - 1) / Q.splits;
     const int32_t s0 = split * per, s1 = s0 + per < steps ? s0 + per : steps;
     const uint16_t* xp[4];
     const int32_t some = Q.place[slot * GROUP];            // a slot in use holds a token at its start
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
         const int32_t t = Q.place[slot * GROUP + n * 16 + sub];
-        xp[n] = static_cast<const uint16_t*>(Q.X) + (int64_t)(t < 0 ? some : t) * Q.ld + q * 8;
+        xp[n] = static_cast<const uint16_t*>(Q.X) + (int64_t)(t < 0 ? some : t) * Q.ld + q * 16;
     }
     const uint16_t* ap[RF];
 #pragma unroll
     for (int f = 0; f < RF; ++f) {
         const int32_t r = f * 16 + sub;
-        ap[f] = static_cast<const uint16_t*>(Q.a) + ((int64_t)k * Q.A.max_rank + (r < rank ? r : 0)) * Q.lda + q * 8;
+        ap[f] = static_cast<const uint16_t*>(Q.a) + ((int64_t)k * Q.A.max_rank + (r < rank ? r : 0)) * Q.lda + q * 16;
     }
     f32x4 acc[RF][4] = {};
     if (rank > 0) {
-        constexpr int U = RF <= 4 ? 2 : 1;                  // steps whose loads are on their way together
+        // 64 columns a step, in two instructions each: a quarter's sixteen lie side by side, so that a row's cache line is read at once
         const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-        for (int32_t s = s0 + wave; s < s1; s += 4 * U) {
-            uint4 a[U][RF], b[U][4];
+        for (int32_t s = s0 + wave; s < s1; s += 4) {
+            uint4 a[2][RF], b[2][4];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const bool in = s + 4 * u < s1 && (s + 4 * u) * 32 + q * 8 < Q.width;
-                const int64_t c = in ? (s + 4 * u) * 32 : 0;
+            for (int u = 0; u < 2; ++u) {
+                const bool in = s * 64 + q * 16 + u * 8 < Q.width;
+                const int64_t c = in ? s * 64 + u * 8 : 0;
 #pragma unroll
                 for (int n = 0; n < 4; ++n) b[u][n] = in ? *reinterpret_cast<const uint4*>(xp[n] + c) : none;
 #pragma unroll
                 for (int f = 0; f < RF; ++f) a[u][f] = in ? *reinterpret_cast<const uint4*>(ap[f] + c) : none;
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u)
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int f = 0; f < RF; ++f)
 #pragma unroll
@@ -142,12 +142,13 @@ int launch_shrink(const ShrinkArgs& S, hipStream_t st) {
     return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
 }
 
-// A workgroup per slot adds up its pieces; the workgroups behind them write the zeros of tokens without an adapter, 64 tokens each.
+// A workgroup adds up eight ranks of a slot's pieces; the workgroups behind them write the zeros of tokens without an adapter, 64 tokens each.
+constexpr int JOIN_RANKS = 8;
 __global__ __launch_bounds__(256) void join_kernel(const JoinArgs Q) {
-    const int32_t R = Q.A.max_rank, ranks = (R + 15) / 16 * 16;
-    if (blockIdx.x >= Q.slots) {
-        if (Q.h == nullptr) return;
-        const int64_t t0 = (blockIdx.x - Q.slots) * GROUP;
+    const int32_t R = Q.A.max_rank, ranks = (R + 15) / 16 * 16, groups = R / JOIN_RANKS;
+    const int64_t slot = blockIdx.x / groups;
+    if (slot >= Q.slots) {
+        const int64_t t0 = (blockIdx.x - Q.slots * groups) * GROUP;
         for (int e = threadIdx.x; e < GROUP * R; e += 256) {
             const int64_t t = t0 + e / R;
             if (t >= Q.T) break;
@@ -156,45 +157,42 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinArgs Q) {
         }
         return;
     }
-    const int64_t slot = blockIdx.x, places = Q.slots * GROUP;
+    __shared__ float tile[GROUP][JOIN_RANKS + 1];          // places by ranks, for h
     const int32_t k = Q.owner[slot];
     if (k < 0) return;
+    const int64_t places = Q.slots * GROUP;
+    const int32_t r0 = (int32_t)(blockIdx.x - slot * groups) * JOIN_RANKS;
+    const int n = threadIdx.x & 63;                        // places side by side
+    const int32_t t = Q.place[slot * GROUP + n];
     const float factor = Q.scaled && Q.A.alpha != nullptr ? Q.A.alpha[k] : 1.0f;
-    __shared__ float tile[GROUP][33];                      // 32 ranks at a time, places by ranks for h
-    for (int r0 = 0; r0 < R; r0 += 32) {
-        __syncthreads();
-        for (int e = threadIdx.x; e < GROUP * 32; e += 256) {
-            const int r = r0 + e / GROUP, n = e % GROUP;   // places side by side
-            if (r >= R) break;
-            float v = 0.0f;
-            if (Q.place[slot * GROUP + n] >= 0) {
-                const float* __restrict__ const p = Q.part + (slot * ranks + r) * GROUP + n;
-                for (int32_t s = 0; s < Q.splits; ++s) v += p[(int64_t)s * places * ranks];
-                v *= factor;
-            }
-            tile[n][r - r0] = v;
-            if (Q.planes != nullptr) {
-                uint32_t hi, mid, lo;
-                split3(v, hi, mid, lo);
-                uint16_t* __restrict__ const o = Q.planes + r * places + slot * GROUP + n;
-                o[0] = (uint16_t)hi;
-                o[R * places] = (uint16_t)mid;
-                o[2 * R * places] = (uint16_t)lo;
-            }
+#pragma unroll
+    for (int i = 0; i < JOIN_RANKS / 4; ++i) {
+        const int r = r0 + i * 4 + (threadIdx.x >> 6);
+        const float* __restrict__ const p = Q.part + (slot * ranks + r) * GROUP + n;
+        float v = 0.0f;
+#pragma unroll 8
+        for (int32_t s = 0; s < Q.splits; ++s) v += p[(int64_t)s * places * ranks];
+        v = t >= 0 ? factor * v : 0.0f;
+        tile[n][r - r0] = v;
+        if (Q.planes != nullptr) {
+            uint32_t hi, mid, lo;
+            split3(v, hi, mid, lo);
+            uint16_t* __restrict__ const o = Q.planes + r * places + slot * GROUP + n;
+            o[0] = (uint16_t)hi;
+            o[R * places] = (uint16_t)mid;
+            o[2 * R * places] = (uint16_t)lo;
         }
-        __syncthreads();
-        if (Q.h != nullptr) {
-            for (int e = threadIdx.x; e < GROUP * 32; e += 256) {
-                const int n = e >> 5, r = r0 + (e & 31);
-                const int32_t t = Q.place[slot * GROUP + n];
-                if (t >= 0 && r < R) Q.h[(int64_t)t * R + r] = tile[n][e & 31];
-            }
-        }
+    }
+    if (Q.h == nullptr) return;
+    __syncthreads();
+    for (int e = threadIdx.x; e < GROUP * JOIN_RANKS; e += 256) {
+        const int32_t to = Q.place[slot * GROUP + e / JOIN_RANKS];
+        if (to >= 0) Q.h[(int64_t)to * R + r0 + e % JOIN_RANKS] = tile[e / JOIN_RANKS][e % JOIN_RANKS];
     }
 }
 
 int launch_join(const JoinArgs& J, hipStream_t st) {
-    const int64_t wgs = J.slots + (J.h != nullptr ? tokens_in(J.T, GROUP) : 0);
+    const int64_t wgs = J.slots * (J.A.max_rank / JOIN_RANKS) + (J.h != nullptr ? tokens_in(J.T, GROUP) : 0);
     if (!fits_launch(wgs, 256)) return WINDQ_ESHAPE;
     join_kernel<<<dim3((uint32_t)wgs), dim3(256), 0, st>>>(J);
     return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;

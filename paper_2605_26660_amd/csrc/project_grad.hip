@@ -71,13 +71,14 @@ __global__ __launch_bounds__(256) void outer_kernel(const XT* __restrict__ right
     }
 }
 
-// The same for bfloat16 on the matrix instructions: 128 columns of the right side by up to 64 ranks, the sum over an adapter's places 32 at a time,
-// shared by four wavefronts.  The sum runs over tokens, and an operand wants eight consecutive tokens of one column in a lane, while
-// a token's columns lie side by side: a lane reads eight tokens by eight columns and pairs tokens up in registers, which gives one
-// operand for each of its eight columns (every eighth column shares an instruction, as in the reconstruction).  The left side comes
-// transposed and as three bfloat16 terms, so products are exact to fp32.
+// The same for bfloat16 on the matrix instructions: 64 columns of the right side by up to 64 ranks, the sum over an adapter's places 32 at a time,
+// shared by eight wavefronts.  The sum runs over tokens, and an operand wants eight consecutive tokens of one column in a lane, while
+// a token's columns lie side by side: a lane reads eight tokens by four columns and pairs tokens up in registers, which gives one
+// operand for each of its four columns (every fourth column shares an instruction, as in the reconstruction).  The left side comes
+// transposed and as three bfloat16 terms, so products are exact to fp32.  Bound by reading X and dY once.
+constexpr int OUTER_COLS = 64, OUTER_THREADS = 512;
 struct OuterArgs {
-    const uint16_t* right;     // [T][ld], readable up to a multiple of 8 columns
+    const uint16_t* right;     // [T][ld], on 16 bytes, columns in eights readable
     int64_t ld, width;
     const uint16_t* planes;    // [3][max_rank][places]
     int64_t places;
@@ -87,95 +88,101 @@ struct OuterArgs {
     AdapterArgs A;
     bool scaled, by_column;
     float* out;
-    int64_t tiles;             // of 128 columns
+    int64_t tiles;             // of OUTER_COLS columns
 };
 
-__device__ __forceinline__ uint32_t halves(uint32_t a, uint32_t b, bool high) {
-    return __builtin_amdgcn_perm(b, a, high ? 0x07060302u : 0x05040100u);
-}
-
 template <int RF>
-__global__ __launch_bounds__(256) void outer_tiles_kernel(const OuterArgs Q1, const OuterArgs Q2, const int64_t first2) {
-    __shared__ float red[2][RF * 16][132];
+__global__ __launch_bounds__(OUTER_THREADS) void outer_tiles_kernel(const OuterArgs Q1, const OuterArgs Q2, const int64_t first2) {
+    __shared__ float red[4][RF * 16][OUTER_COLS + 4];
     const OuterArgs& Q = blockIdx.x < first2 ? Q1 : Q2;
     const int64_t block = blockIdx.x < first2 ? blockIdx.x : blockIdx.x - first2;
     const int32_t groups = (Q.A.max_rank + 63) / 64;
     const int32_t k = (int32_t)(block / (Q.tiles * groups));
     const int64_t rest = block - k * Q.tiles * groups;
     const int32_t r0 = (int32_t)(rest / Q.tiles) * 64;
-    const int64_t c0 = (rest - rest / Q.tiles * Q.tiles) * 128;
+    const int64_t c0 = (rest - rest / Q.tiles * Q.tiles) * OUTER_COLS;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
     const int32_t rank = adapter_rank(Q.A, k), n = Q.count[k], p0 = Q.first[k];
-    const int64_t col = c0 + sub * 8;
-    f32x4 acc[8][RF] = {};
+    const int64_t col = c0 + sub * 4;
+    f32x4 acc[4][RF] = {};
     if (r0 < rank) {
-        for (int32_t i0 = wave * 32; i0 < n; i0 += 128) {
-            uint4 x[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int32_t i = i0 + q * 8 + j;
-                const int32_t t = i < n ? Q.place[p0 + i] : -1;
-                x[j] = t >= 0 && col < Q.width ? *reinterpret_cast<const uint4*>(Q.right + (int64_t)t * Q.ld + col) : make_uint4(0u, 0u, 0u, 0u);
+        auto tokens_of = [&](int32_t i0, uint2 (&x)[8]) {
+            const int32_t at = i0 + q * 8;
+            int32_t t[8] = {-1, -1, -1, -1, -1, -1, -1, -1};
+            if (at < n) {                                   // a slot's places are all written
+                const int4 a = *reinterpret_cast<const int4*>(Q.place + p0 + at), b = *reinterpret_cast<const int4*>(Q.place + p0 + at + 4);
+                t[0] = a.x; t[1] = a.y; t[2] = a.z; t[3] = a.w; t[4] = b.x; t[5] = b.y; t[6] = b.z; t[7] = b.w;
             }
-            bf16x8 b[3][RF];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                x[j] = t[j] >= 0 && col < Q.width ? *reinterpret_cast<const uint2*>(Q.right + (int64_t)t[j] * Q.ld + col) : make_uint2(0u, 0u);
+        };
+        uint2 x[8], next[8];
+        tokens_of(wave * 32, x);
+        for (int32_t i0 = wave * 32; i0 < n; i0 += 256) {
+            uint4 b[3][RF];
 #pragma unroll
             for (int m = 0; m < 3; ++m)
 #pragma unroll
                 for (int f = 0; f < RF; ++f) {
                     const int32_t r = r0 + f * 16 + sub;
-                    b[m][f] = as_bf16x8(r < rank ? *reinterpret_cast<const uint4*>(Q.planes + ((int64_t)m * Q.A.max_rank + r) * Q.places + p0 + i0 + q * 8) : make_uint4(0u, 0u, 0u, 0u));
+                    b[m][f] = r < rank ? *reinterpret_cast<const uint4*>(Q.planes + ((int64_t)m * Q.A.max_rank + r) * Q.places + p0 + i0 + q * 8) : make_uint4(0u, 0u, 0u, 0u);
                 }
+            tokens_of(i0 + 256, next);
 #pragma unroll
-            for (int m = 0; m < 8; ++m) {
+            for (int m = 0; m < 4; ++m) {
                 uint32_t w[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] = (m >> 1) == 0 ? x[j].x : ((m >> 1) == 1 ? x[j].y : ((m >> 1) == 2 ? x[j].z : x[j].w));
-                const bool h = (m & 1) != 0;
-                const bf16x8 a = as_bf16x8(make_uint4(halves(w[0], w[1], h), halves(w[2], w[3], h), halves(w[4], w[5], h), halves(w[6], w[7], h)));
+                for (int j = 0; j < 8; ++j) w[j] = m < 2 ? x[j].x : x[j].y;
+                const uint32_t pick = (m & 1) != 0 ? 0x07060302u : 0x05040100u;         // halves of two tokens side by side
+                const bf16x8 a = as_bf16x8(make_uint4(__builtin_amdgcn_perm(w[1], w[0], pick), __builtin_amdgcn_perm(w[3], w[2], pick),
+                                                      __builtin_amdgcn_perm(w[5], w[4], pick), __builtin_amdgcn_perm(w[7], w[6], pick)));
 #pragma unroll
                 for (int f = 0; f < RF; ++f)
 #pragma unroll
-                    for (int p = 2; p >= 0; --p) acc[m][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[p][f], acc[m][f], 0, 0, 0);
+                    for (int p = 2; p >= 0; --p) acc[m][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, as_bf16x8(b[p][f]), acc[m][f], 0, 0, 0);
             }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = next[j];
         }
     }
-    // wavefronts 2 and 3 hand theirs to 0 and 1, and 1 its own to 0: a fixed order
+    // the upper half of the wavefronts hand theirs to the lower half, until one has all: a fixed order
 #pragma unroll
-    for (int round = 2; round >= 1; round >>= 1) {
+    for (int round = 4; round >= 1; round >>= 1) {
         if (wave >= round && wave < 2 * round) {
 #pragma unroll
-            for (int m = 0; m < 8; ++m)
+            for (int m = 0; m < 4; ++m)
 #pragma unroll
                 for (int f = 0; f < RF; ++f)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) red[wave - round][f * 16 + sub][(4 * q + i) * 8 + m] = acc[m][f][i];
+                    for (int i = 0; i < 4; ++i) red[wave - round][f * 16 + sub][(4 * q + i) * 4 + m] = acc[m][f][i];
         }
         __syncthreads();
         if (wave < round) {
 #pragma unroll
-            for (int m = 0; m < 8; ++m)
+            for (int m = 0; m < 4; ++m)
 #pragma unroll
                 for (int f = 0; f < RF; ++f)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[m][f][i] += red[wave][f * 16 + sub][(4 * q + i) * 8 + m];
+                    for (int i = 0; i < 4; ++i) acc[m][f][i] += red[wave][f * 16 + sub][(4 * q + i) * 4 + m];
         }
         __syncthreads();
     }
     if (wave == 0) {
 #pragma unroll
-        for (int m = 0; m < 8; ++m)
+        for (int m = 0; m < 4; ++m)
 #pragma unroll
             for (int f = 0; f < RF; ++f)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) red[0][f * 16 + sub][(4 * q + i) * 8 + m] = acc[m][f][i];
+                for (int i = 0; i < 4; ++i) red[0][f * 16 + sub][(4 * q + i) * 4 + m] = acc[m][f][i];
     }
     __syncthreads();
     const float factor = Q.scaled && Q.A.alpha != nullptr ? Q.A.alpha[k] : 1.0f;
     const int32_t R = Q.A.max_rank, ranks = R - r0 < RF * 16 ? R - r0 : RF * 16;
     const int64_t left = Q.width - c0;
-    const int32_t cols = left < 128 ? (int32_t)left : 128;
-    for (int e = threadIdx.x; e < ranks * 128; e += 256) {
-        const int r = Q.by_column ? e % ranks : e >> 7, c = Q.by_column ? e / ranks : e & 127;
+    const int32_t cols = left < OUTER_COLS ? (int32_t)left : OUTER_COLS;
+    for (int e = threadIdx.x; e < ranks * OUTER_COLS; e += OUTER_THREADS) {
+        const int r = Q.by_column ? e % ranks : e / OUTER_COLS, c = Q.by_column ? e / ranks : e % OUTER_COLS;
         if (c >= cols) continue;
         const float v = r0 + r < rank ? factor * red[0][r][c] : 0.0f;
         if (Q.by_column) Q.out[((int64_t)k * Q.width + c0 + c) * R + r0 + r] = v;
@@ -502,14 +509,14 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
             if (status != WINDQ_OK) return status;
             if (outer) {
                 const int32_t groups = (A.max_rank + 63) / 64;
-                OuterArgs O1 = {static_cast<const uint16_t*>(X->data), X->ld, cols, planes_dh, G.slots * GROUP, G.place, G.first, G.count, A, false, false, dA, (cols + 127) / 128};
-                OuterArgs O2 = {dYv, Q.ldy, rows, planes_h, G.slots * GROUP, G.place, G.first, G.count, A, true, true, dB, (rows + 127) / 128};
+                OuterArgs O1 = {static_cast<const uint16_t*>(X->data), X->ld, cols, planes_dh, G.slots * GROUP, G.place, G.first, G.count, A, false, false, dA, (cols + OUTER_COLS - 1) / OUTER_COLS};
+                OuterArgs O2 = {dYv, Q.ldy, rows, planes_h, G.slots * GROUP, G.place, G.first, G.count, A, true, true, dB, (rows + OUTER_COLS - 1) / OUTER_COLS};
                 const int64_t n1 = (int64_t)A.n * groups * O1.tiles, n2 = (int64_t)A.n * groups * O2.tiles;
                 const int32_t RF = A.max_rank >= 64 ? 4 : shrink_ranks(A.max_rank) / 16;
-                if (RF == 1) WINDQ_LAUNCH(n1 + n2, 256, outer_tiles_kernel<1>, O1, O2, n1);
-                else if (RF == 2) WINDQ_LAUNCH(n1 + n2, 256, outer_tiles_kernel<2>, O1, O2, n1);
-                else if (RF == 3) WINDQ_LAUNCH(n1 + n2, 256, outer_tiles_kernel<3>, O1, O2, n1);
-                else WINDQ_LAUNCH(n1 + n2, 256, outer_tiles_kernel<4>, O1, O2, n1);
+                if (RF == 1) WINDQ_LAUNCH(n1 + n2, OUTER_THREADS, outer_tiles_kernel<1>, O1, O2, n1);
+                else if (RF == 2) WINDQ_LAUNCH(n1 + n2, OUTER_THREADS, outer_tiles_kernel<2>, O1, O2, n1);
+                else if (RF == 3) WINDQ_LAUNCH(n1 + n2, OUTER_THREADS, outer_tiles_kernel<3>, O1, O2, n1);
+                else WINDQ_LAUNCH(n1 + n2, OUTER_THREADS, outer_tiles_kernel<4>, O1, O2, n1);
             }
         } else {
             AdapterArgs B = A;
