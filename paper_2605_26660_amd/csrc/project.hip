@@ -2,7 +2,7 @@
 //   Y[t] = w_hat x_t + alpha_k B_k h_t,   h_t = A_k x_t,   k = adapter_of[t]
 #include <math.h>
 
-#include "windq_project_tiles.hpp"
+#include "windq_project_few.hpp"
 
 namespace windq {
 
@@ -43,26 +43,6 @@ struct ProjectArgs {
     const float* h;            // or null: no adapters
     AdapterArgs A;
 };
-
-// alpha_k B_k[row] . h_t
-template <typename YT>
-__device__ __forceinline__ float expand_one(const AdapterArgs& A, const float* __restrict__ h, int64_t t, int64_t row, int64_t rows) {
-    const int32_t k = A.of[t];
-    if (k < 0 || k >= A.n) return 0.0f;
-    const int32_t rank = adapter_rank(A, k);
-    const YT* __restrict__ const b = static_cast<const YT*>(A.b) + ((int64_t)k * rows + row) * A.max_rank;
-    const float* __restrict__ const ht = h + t * A.max_rank;
-    float sum = 0.0f;
-    for (int32_t r = 0; r < rank; r += 8) {
-        float bv[8], hv[8];
-        load8(b + r, bv);
-        load8(ht + r, hv);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (r + j < rank) sum = fmaf(bv[j], hv[j], sum);
-    }
-    return A.alpha != nullptr ? A.alpha[k] * sum : sum;
-}
 
 template <typename YT>
 __device__ __forceinline__ void store_y(YT* __restrict__ p, float v) {
@@ -265,7 +245,7 @@ size_t grad_ws_bytes(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32
 
 // Offsets of a workspace's parts.  They are those of the shape alone, so that fewer tokens, or rows in other units, never need more.
 struct ProjectWs {
-    size_t planes, h, place, owner, first, count, part, fields, unit, xs, beta, alpha, total;
+    size_t planes, h, frag, few_xs, place, owner, first, count, part, fields, unit, xs, beta, alpha, total;
 };
 
 ProjectWs project_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t G, int32_t n, int32_t max_rank) {
@@ -278,6 +258,9 @@ ProjectWs project_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32
     };
     w.planes = take(dtype == WINDQ_F32 ? (size_t)(3 * T * cols) * 2 : 0);
     w.h = take((size_t)(T * max_rank) * 4);
+    const bool few = dtype == WINDQ_BF16;                   // fewer tokens than asked for fit too
+    w.frag = take(few ? (size_t)cols * 64 * 2 : 0);
+    w.few_xs = take(few ? (size_t)(cols / 64 + 1) * 64 * 4 : 0);
     const bool grouped = n > 0 && dtype == WINDQ_BF16 && T > SHRINK_FEW;
     const int64_t slots = group_slots(T, n);
     w.place = take(grouped ? (size_t)slots * GROUP * 4 : 0);
@@ -340,6 +323,15 @@ int project_all(ProjectArgs& Q, const windq_mat* X, const windq_adapters* ad, fl
         Q.X = planes;
         Q.ldx = Q.P.cols;
         Q.plane = T * Q.P.cols;
+    }
+    if constexpr (sizeof(XT) == 2) {
+        if (T <= PROJECT_FEW && few_fits(Q.P)) {
+            float* const ht = ad == nullptr ? nullptr : (h != nullptr ? h : reinterpret_cast<float*>(ws + at.h));
+            FewArgs F = {Q.P, Q.X, Q.ldx, T, static_cast<uint16_t*>(Q.Y), Q.ldy, ht, Q.A, 0, reinterpret_cast<uint4*>(ws + at.frag), reinterpret_cast<float*>(ws + at.few_xs)};
+            const int steps = Q.P.G % 128 == 0 ? 8 : Q.P.G / 16;
+            F.n_kb = (int32_t)(Q.P.cols / (16 * steps));
+            return steps == 8 ? launch_few<8>(F, ht, st) : (steps == 6 ? launch_few<6>(F, ht, st) : launch_few<4>(F, ht, st));
+        }
     }
     if (ad != nullptr) {
         float* const ht = h != nullptr ? h : reinterpret_cast<float*>(ws + at.h);

@@ -86,11 +86,10 @@ __device__ __forceinline__ void load8(const XT* __restrict__ p, float (&v)[8]) {
 }
 
 template <typename XT>
-__global__ __launch_bounds__(256) void shrink_token_kernel(const XT* __restrict__ X, int64_t ldx, int32_t cols, const AdapterArgs A,
-                                                            bool scaled, float* __restrict__ h) {
+__device__ __forceinline__ void shrink_token(const XT* __restrict__ X, int64_t ldx, int32_t cols, const AdapterArgs& A, bool scaled, float* __restrict__ h, uint32_t block) {
     const int32_t groups = (A.max_rank + 15) >> 4;
-    const int64_t t = blockIdx.x / groups;
-    const int32_t r0 = (int32_t)(blockIdx.x - t * groups) * 16 + (threadIdx.x >> 6) * 4;
+    const int64_t t = block / groups;
+    const int32_t r0 = (int32_t)(block - t * groups) * 16 + (threadIdx.x >> 6) * 4;
     if (r0 >= A.max_rank) return;                          // the same for a wavefront
     const int lane = threadIdx.x & 63;
     const int32_t k = A.of[t];
@@ -100,7 +99,7 @@ __global__ __launch_bounds__(256) void shrink_token_kernel(const XT* __restrict_
     if (r0 < rank) {
         const XT* __restrict__ const a = static_cast<const XT*>(A.a) + ((int64_t)k * A.max_rank + r0) * cols;
         const XT* __restrict__ const x = X + t * ldx;
-#pragma unroll 2
+#pragma unroll 4
         for (int32_t c = lane * 8; c < cols; c += 512) {
             float xv[8], av[8];
             load8(x + c, xv);
@@ -120,6 +119,11 @@ __global__ __launch_bounds__(256) void shrink_token_kernel(const XT* __restrict_
         for (int m = 32; m >= 1; m >>= 1) acc[i] += __shfl_xor(acc[i], m, 64);
         if (lane == i && r0 + i < A.max_rank) h[t * A.max_rank + r0 + i] = factor * acc[i];
     }
+}
+
+template <typename XT>
+__global__ __launch_bounds__(256) void shrink_token_kernel(const XT* __restrict__ X, int64_t ldx, int32_t cols, const AdapterArgs A, bool scaled, float* __restrict__ h) {
+    shrink_token(X, ldx, cols, A, scaled, h, blockIdx.x);
 }
 
 __device__ __forceinline__ uint4 pack8(const uint32_t (&w)[8]) {
