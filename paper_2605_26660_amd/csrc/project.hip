@@ -335,7 +335,7 @@ int project_all(ProjectArgs& Q, const windq_mat* X, const windq_adapters* ad, fl
     }
     if (ad != nullptr) {
         float* const ht = h != nullptr ? h : reinterpret_cast<float*>(ws + at.h);
-        const int64_t wgs = T * ((Q.A.max_rank + 15) / 16);
+        const int64_t wgs = shrink_token_workgroups(T, Q.A.max_rank);
         bool grouped = false;
         if constexpr (sizeof(XT) == 2) {
             grouped = T > SHRINK_FEW;

@@ -489,7 +489,7 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
         GroupArgs G = {A.of, T, A.n, group_slots(T, A.n), reinterpret_cast<int32_t*>(ws + at.place), reinterpret_cast<int32_t*>(ws + at.owner),
                        reinterpret_cast<int32_t*>(ws + at.first), reinterpret_cast<int32_t*>(ws + at.count)};
         const bool outer = dA != nullptr;
-        const int64_t tokens = T * ((A.max_rank + 15) / 16);
+        const int64_t tokens = shrink_token_workgroups(T, A.max_rank);
         if (bf || outer) {
             const int status = launch_group(G, st);
             if (status != WINDQ_OK) return status;

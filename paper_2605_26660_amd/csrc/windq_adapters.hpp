@@ -70,7 +70,8 @@ inline int32_t shrink_splits(int64_t slots, int64_t width) {
 #ifdef __HIPCC__
 
 // ------------------------------------------------------------------------------------------------ h = A x, token by token
-// (On the way back: dh = alpha B^T dY, with B transposed in A's place.)  A workgroup takes 16 ranks of one token, a wavefront four of them; lanes walk the columns, eight at a time.
+// (On the way back: dh = alpha B^T dY, with B transposed in A's place.)  A wavefront per token and rank, eight columns a lane at a time: bound by latency,
+// so as many wavefronts as there are, and eight loads on their way.
 template <typename XT>
 __device__ __forceinline__ void load8(const XT* __restrict__ p, float (&v)[8]) {
     if constexpr (sizeof(XT) == 4) {
@@ -85,41 +86,37 @@ __device__ __forceinline__ void load8(const XT* __restrict__ p, float (&v)[8]) {
     }
 }
 
+constexpr int SHRINK_RANKS = 4;                           // of a workgroup
 template <typename XT>
 __device__ __forceinline__ void shrink_token(const XT* __restrict__ X, int64_t ldx, int32_t cols, const AdapterArgs& A, bool scaled, float* __restrict__ h, uint32_t block) {
-    const int32_t groups = (A.max_rank + 15) >> 4;
+    const uint32_t groups = (uint32_t)A.max_rank / SHRINK_RANKS;
     const int64_t t = block / groups;
-    const int32_t r0 = (int32_t)(block - t * groups) * 16 + (threadIdx.x >> 6) * 4;
-    if (r0 >= A.max_rank) return;                          // the same for a wavefront
+    const int32_t r = (int32_t)(block - (uint32_t)t * groups) * SHRINK_RANKS + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     const int32_t k = A.of[t];
     const int32_t rank = k < 0 || k >= A.n ? 0 : adapter_rank(A, k);
-    float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    const float factor = scaled && rank > 0 && A.alpha != nullptr ? A.alpha[k] : 1.0f;
-    if (r0 < rank) {
-        const XT* __restrict__ const a = static_cast<const XT*>(A.a) + ((int64_t)k * A.max_rank + r0) * cols;
+    float sum = 0.0f;
+    if (r < rank) {
+        const XT* __restrict__ const a = static_cast<const XT*>(A.a) + ((int64_t)k * A.max_rank + r) * cols;
         const XT* __restrict__ const x = X + t * ldx;
+        float acc[2] = {0.0f, 0.0f};
 #pragma unroll 4
         for (int32_t c = lane * 8; c < cols; c += 512) {
             float xv[8], av[8];
             load8(x + c, xv);
+            load8(a + c, av);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (r0 + i < rank) {
-                    load8(a + (int64_t)i * cols + c, av);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[i] = fmaf(av[j], xv[j], acc[i]);
-                }
-            }
+            for (int j = 0; j < 8; ++j) acc[j & 1] = fmaf(av[j], xv[j], acc[j & 1]);
         }
+        sum = acc[0] + acc[1];
+        if (scaled && A.alpha != nullptr) sum *= A.alpha[k];
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-#pragma unroll
-        for (int m = 32; m >= 1; m >>= 1) acc[i] += __shfl_xor(acc[i], m, 64);
-        if (lane == i && r0 + i < A.max_rank) h[t * A.max_rank + r0 + i] = factor * acc[i];
-    }
+    for (int m = 32; m >= 1; m >>= 1) sum += __shfl_xor(sum, m, 64);
+    if (lane == 0) h[t * A.max_rank + r] = sum;
 }
+
+inline int64_t shrink_token_workgroups(int64_t T, int32_t max_rank) { return T * (max_rank / SHRINK_RANKS); }
 
 template <typename XT>
 __global__ __launch_bounds__(256) void shrink_token_kernel(const XT* __restrict__ X, int64_t ldx, int32_t cols, const AdapterArgs A, bool scaled, float* __restrict__ h) {

@@ -43,6 +43,7 @@ __device__ __forceinline__ float expand_one(const AdapterArgs& A, const float* _
     const YT* __restrict__ const b = static_cast<const YT*>(A.b) + ((int64_t)k * rows + row) * A.max_rank;
     const float* __restrict__ const ht = h + t * A.max_rank;
     float sum = 0.0f;
+#pragma unroll 2
     for (int32_t r = 0; r < rank; r += 8) {
         float bv[8], hv[8];
         load8(b + r, bv);
@@ -105,7 +106,13 @@ __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q
     const uint32_t one = 0x3f803f80u;
     const bf16x8 ones = as_bf16x8(make_uint4(one, one, one, one));
 
+    auto x_at = [&](int n, int32_t kb) {
+        const int64_t t = n * 32 + sub;
+        return LAID ? Q.frag + ((int64_t)(kb * NTF + n) * S * 64 + lane)
+                    : reinterpret_cast<const uint4*>(Q.X + (t < Q.T ? t : Q.T - 1) * Q.ldx + (int64_t)kb * (16 * S) + hh * (8 * S));
+    };
     f32x16 tot[NTF] = {};
+    float more = 0.0f;                                      // the adapters' part of a thread's first result
     // a k-block's treatment, known a k-block ahead
     int64_t base = 0;
     int a = 0;
@@ -139,14 +146,17 @@ __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q
         uint4 x[S][NTF];
 #pragma unroll
         for (int n = 0; n < NTF; ++n) {
-            const int64_t t = n * 32 + sub;
-            const uint4* const from = LAID ? Q.frag + ((int64_t)(kb * NTF + n) * S * 64 + lane)
-                                           : reinterpret_cast<const uint4*>(Q.X + (t < Q.T ? t : Q.T - 1) * Q.ldx + (int64_t)kb * (16 * S) + hh * (8 * S));
+            const uint4* const from = x_at(n, kb);
 #pragma unroll
             for (int s = 0; s < S; ++s) x[s][n] = from[LAID ? s * 64 : s];
-            if (LAID) xsum[n] = Q.xs[kb * 64 + t];
+            if (LAID) xsum[n] = Q.xs[kb * 64 + n * 32 + sub];
         }
         if (kb + WAVES < Q.n_kb) a = __builtin_amdgcn_readfirstlane(pk_action(P, rb * P.n_chunks + (kb + WAVES) / per_chunk, base));
+        if (kb == wave && Q.h != nullptr) {                 // while all of this is on its way
+            const int r = threadIdx.x & 31;
+            const int64_t t = threadIdx.x >> 5;
+            if (r < rows_left && t < Q.T) more = expand_one<uint16_t>(Q.A, Q.h, t, row0 + r, P.rows);
+        }
         if (hh == 0) {
             ab[wave][0][sub] = alpha;
             ab[wave][1][sub] = beta;
@@ -202,11 +212,11 @@ __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q
             if (P.w_f32 != 0) {
 #pragma unroll 1
                 for (int term = 1; term < 3; ++term)
-#pragma unroll
-                    for (int s = 0; s < S; ++s) {
+#pragma unroll 1
+                    for (int s = 0; s < S; ++s) {           // rare: X once more from where it lies
                         const bf16x8 w = as_bf16x8(skip_octet(P, rb * P.R_u + lrow0 + lr, wcol + s * 8, term));
 #pragma unroll
-                        for (int n = 0; n < NTF; ++n) acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, as_bf16x8(x[s][n]), acc[n], 0, 0, 0);
+                        for (int n = 0; n < NTF; ++n) acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, as_bf16x8(x_at(n, kb)[LAID ? s * 64 : s]), acc[n], 0, 0, 0);
                     }
             }
         }
@@ -228,12 +238,12 @@ __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q
 #pragma unroll
         for (int i = 0; i < 16; ++i) red[((wave * NTF + n) * 16 + i) * 64 + lane] = tot[n][i];
     __syncthreads();
-#pragma unroll
-    for (int e0 = 0; e0 < NTF * 1024; e0 += WAVES * 64) {
-        const int e = e0 + threadIdx.x, r = e & 31, n = e >> 5;        // neighbouring lanes: neighbouring rows of a token
+#pragma unroll 1
+    for (int e = threadIdx.x; e < NTF * 1024; e += WAVES * 64) {
+        const int r = e & 31, n = e >> 5;                  // neighbouring lanes: neighbouring rows of a token
         const int64_t y = row0 + r, t = n;
         if (r >= rows_left || t >= Q.T) continue;
-        const float more = Q.h != nullptr ? expand_one<uint16_t>(Q.A, Q.h, t, y, P.rows) : 0.0f;
+        if (Q.h != nullptr && (e != (int)threadIdx.x || wave >= Q.n_kb)) more = expand_one<uint16_t>(Q.A, Q.h, t, y, P.rows);
         const int at = ((n >> 5) * 16 + (r >> 3) * 4 + (r & 3)) * 64 + ((r >> 2) & 1) * 32 + (n & 31);
         float v = 0.0f;
 #pragma unroll
@@ -249,7 +259,7 @@ int launch_few(const FewArgs& Q, float* h, hipStream_t st) {
     const int64_t blocks = (Q.P.rows + PF_ROWS - 1) / PF_ROWS;
     const int fragments = Q.T <= 32 ? 1 : 2;
     const bool laid = Q.T > FEW_DIRECT;
-    const int64_t shrinks = h != nullptr ? Q.T * ((Q.A.max_rank + 15) / 16) : 0;
+    const int64_t shrinks = h != nullptr ? shrink_token_workgroups(Q.T, Q.A.max_rank) : 0;
     const int64_t wgs = shrinks + (laid ? tokens_in((int64_t)Q.n_kb * fragments, 4) : 0);
     if (!fits_launch(blocks, 1024) || !fits_launch(wgs, 256)) return WINDQ_ESHAPE;
     if (wgs > 0) {
