@@ -18,7 +18,7 @@ namespace windq {
 constexpr int AW_THREADS = 256;
 constexpr int AW_STEPS = 4;                               // blocks of 256 values a wavefront takes
 constexpr int64_t AW_TILE = (int64_t)AW_THREADS * 4 * AW_STEPS;
-constexpr int AW_FEW = 16, AW_MANY = 56;                  // tensors of a launch: 4 KB of kernel arguments hold 56
+constexpr int AW_FEW = 16, AW_MANY = 224;                 // tensors of a launch
 
 struct AdamwRates {
     float b1, c1, b2, c2, eps, decay, size, inverse;
