@@ -95,7 +95,7 @@ __global__ __launch_bounds__(PJ_WAVES * 64) void project_kernel(const ProjectArg
             act[f] = pk_action(P, u, base);
             codes[f] = P.codes + base + lrow[f] * pk_bytes_per_group(act[f], G);
             const int64_t g = u * P.R_u + lrow[f];
-            pk_affine(act[f], P.scale[g], P.offset[g], alpha[f], beta[f]);
+            pk_affine(act[f], P.scale[g], P.offset[g], NP == 3, alpha[f], beta[f]);
             wide |= act[f] == 0 && P.w_f32 != 0;
         }
         f32x4 acc[RF][NT] = {}, xs[MASK ? RF : 1][NT] = {};
@@ -113,6 +113,7 @@ __global__ __launch_bounds__(PJ_WAVES * 64) void project_kernel(const ProjectArg
                 uint4 w = none, k = ones;
                 if (valid) {
                     w = act[f] == 0 ? skip_octet(P, row[f], col, 0) : octet_fields(act[f], codes[f], o, trits_of);
+                    if (NP == 3 && act[f] != 0) w = centred(w, pk_centre(act[f]));
                     if (MASK && act[f] != 0) {
                         k = keep_words(P.mask[row[f] * P.mask_ld + (col >> 3)]);
                         w = and4(w, k);
@@ -259,8 +260,9 @@ ProjectWs project_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32
     w.planes = take(dtype == WINDQ_F32 ? (size_t)(3 * T * cols) * 2 : 0);
     w.h = take((size_t)(T * max_rank) * 4);
     const bool few = dtype == WINDQ_BF16;                   // fewer tokens than asked for fit too
-    w.frag = take(few ? (size_t)cols * 64 * 2 : 0);
-    w.few_xs = take(few ? (size_t)(cols / 64 + 1) * 64 * 4 : 0);
+    const int64_t few_tokens = T < FEW_MOST ? tokens_in(T, 32) * 32 : FEW_MOST;
+    w.frag = take(few ? (size_t)cols * (size_t)few_tokens * 2 : 0);
+    w.few_xs = take(few ? (size_t)(cols / 64 + 1) * FEW_MOST * 4 : 0);
     const bool grouped = n > 0 && dtype == WINDQ_BF16 && T > SHRINK_FEW;
     const int64_t slots = group_slots(T, n);
     w.place = take(grouped ? (size_t)slots * GROUP * 4 : 0);
@@ -325,9 +327,9 @@ int project_all(ProjectArgs& Q, const windq_mat* X, const windq_adapters* ad, fl
         Q.plane = T * Q.P.cols;
     }
     if constexpr (sizeof(XT) == 2) {
-        if (T <= PROJECT_FEW && few_fits(Q.P)) {
+        if (few_fits(Q.P, T)) {
             float* const ht = ad == nullptr ? nullptr : (h != nullptr ? h : reinterpret_cast<float*>(ws + at.h));
-            FewArgs F = {Q.P, Q.X, Q.ldx, T, static_cast<uint16_t*>(Q.Y), Q.ldy, ht, Q.A, 0, reinterpret_cast<uint4*>(ws + at.frag), reinterpret_cast<float*>(ws + at.few_xs)};
+            FewArgs F = {Q.P, Q.X, Q.ldx, T, static_cast<uint16_t*>(Q.Y), Q.ldy, ht, Q.A, 0, reinterpret_cast<uint4*>(ws + at.frag), reinterpret_cast<float*>(ws + at.few_xs), 0, 0};
             const int steps = Q.P.G % 128 == 0 ? 8 : Q.P.G / 16;
             F.n_kb = (int32_t)(Q.P.cols / (16 * steps));
             return steps == 8 ? launch_few<8>(F, ht, st) : (steps == 6 ? launch_few<6>(F, ht, st) : launch_few<4>(F, ht, st));
@@ -358,7 +360,10 @@ int project_all(ProjectArgs& Q, const windq_mat* X, const windq_adapters* ad, fl
         }
         Q.h = ht;
     }
-    const int S = Q.P.mask == nullptr && T > PROJECT_FEW ? tile_steps(Q.P) : 0;
+    // The general kernel where its workgroups run about at once.  bfloat16, 1024 x 1024: 160 tokens (192 of them) 21 us, tiles 31; 320 tokens (320) 39
+    // and 31.  fp32, 4096 x 4096: 80 tokens (512) 237 us, tiles 303; 160 tokens (768) 450 and 312.
+    const int64_t general = (Q.P.rows + 15) / 16 * tokens_in(T, 64);
+    const int S = Q.P.mask == nullptr && T > PROJECT_FEW && general > (sizeof(XT) == 2 ? 256 : 512) ? tile_steps(Q.P) : 0;
     if (S == 8) return launch_tiles<XT, 8>(Q, ws, at, st);
     if (S == 6) return launch_tiles<XT, 6>(Q, ws, at, st);
     if (S == 4) return launch_tiles<XT, 4>(Q, ws, at, st);

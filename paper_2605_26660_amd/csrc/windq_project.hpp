@@ -8,7 +8,8 @@
 // 2^b + code has the bit pattern of 2^b with the code or-ed in.
 //     8 bits  code         (0 .. 255, converted)    4 bits  16 + code     3 bits  8 + code     2 bits  4 + code
 //     1.58    4 + trit, beta = -5 scale             1 bit   +-1, beta = 0                       skip    the weight, scale 1
-// f is off centre by less than its own range, which costs two to three bits of the fp32 sum over one chunk.
+// f is off centre by up to five times its spread, which costs two to three bits of the fp32 sum over one chunk: nothing to an output of
+// bfloat16.  For fp32 activations f is brought to its centre first (q - 7.5 and the like: still exact in bfloat16).
 #pragma once
 
 #include "windq_common.hpp"
@@ -92,13 +93,20 @@ __device__ __forceinline__ int pk_action(const PackArgs& P, int64_t u, int64_t& 
     return a;
 }
 
-// f0 of the treatment: beta = offset - f0 * scale (1.58 and 1 bit have no offset of their own).
-__device__ __forceinline__ void pk_affine(int a, float scale, float offset, float& alpha, float& beta) {
+// beta = offset - f0 * scale (1.58 and 1 bit have no offset of their own).
+__device__ __forceinline__ void pk_affine(int a, float scale, float offset, bool centred, float& alpha, float& beta) {
     alpha = a == 0 ? 1.0f : scale;
     const float o = a >= 5 || a == 0 ? 0.0f : offset;
-    const float f0 = a == 2 ? 16.0f : (a == 3 ? 8.0f : (a == 4 ? 4.0f : (a == 5 ? 5.0f : 0.0f)));
+    const float f0 = centred ? (a == 1 ? -127.5f : (a == 2 ? -7.5f : (a == 3 ? -3.5f : (a == 4 ? -1.5f : 0.0f))))
+                             : (a == 2 ? 16.0f : (a == 3 ? 8.0f : (a == 4 ? 4.0f : (a == 5 ? 5.0f : 0.0f))));
     beta = a == 0 ? 0.0f : o - f0 * scale;
 }
+// What f comes down by when it is centred.
+__device__ __forceinline__ float pk_centre(int a) { return a == 1 ? 127.5f : (a == 2 ? 23.5f : (a == 3 ? 11.5f : (a == 4 ? 5.5f : (a == 5 ? 5.0f : 0.0f)))); }
+__device__ __forceinline__ uint32_t centred_pair(uint32_t v, float c) {
+    return __builtin_amdgcn_perm(__float_as_uint(__uint_as_float(v & 0xffff0000u) - c), __float_as_uint(__uint_as_float(v << 16) - c), 0x07060302u);
+}
+__device__ __forceinline__ uint4 centred(uint4 f, float c) { return make_uint4(centred_pair(f.x, c), centred_pair(f.y, c), centred_pair(f.z, c), centred_pair(f.w, c)); }
 
 // Two copies of v side by side, kept from the compiler: it would make one multiplication (16 clocks) of this and the shift that follows.
 __device__ __forceinline__ uint32_t twice(uint32_t v, int by, uint32_t with) {

@@ -1,4 +1,4 @@
-// windq_project for few tokens of bfloat16: 32 rows and up to 64 tokens a workgroup, the k-blocks shared by its wavefronts.
+// windq_project for few tokens of bfloat16 (up to 64, or 256 where rows are few): 32 rows and up to 64 tokens a workgroup, the k-blocks shared by its wavefronts.
 //
 // Bound by latency, not by the codes: 7 MB at 2 bits for 11008 x 4096.  So the sum is cut into as many pieces as there are k-blocks per
 // wavefront, every wavefront works by itself until the end, and what it needs of a k-block is asked for at once: codes by direct
@@ -24,13 +24,20 @@ struct FewArgs {
     const float* h;            // or null: no adapters
     AdapterArgs A;
     int32_t n_kb;
-    uint4* frag;               // [k-blocks][fragments of 32 tokens][S][64 lanes], or unused
-    float* xs;                 // [k-blocks][64]
+    uint4* frag;               // [k-blocks][fragments][S][64 lanes], or unused
+    float* xs;                 // [k-blocks][FEW_MOST]
+    int32_t fragments;         // of 32 tokens
+    uint32_t row_blocks;
 };
 
-constexpr int64_t FEW_DIRECT = 8;
+constexpr int64_t FEW_DIRECT = 8, FEW_ALWAYS = 64, FEW_MOST = 256;
 
-inline bool few_fits(const PackArgs& P) { return P.mask == nullptr && P.rows % 8 == 0 && (P.R_u == P.rows || P.R_u % PF_ROWS == 0) && (P.G % 128 == 0 || P.G == 96 || P.G == 64); }
+// Past 64 tokens as long as the workgroups take no more than three rounds (one a CU): 4096 x 4096 at 128 tokens (256 of them) 27 us, tiles 80;
+// 11008 x 4096 at 256 tokens would be 1376, tiles 94 us, and 64 tokens' 344 take 45.
+inline bool few_fits(const PackArgs& P, int64_t T) {
+    if (T > FEW_MOST || (T > FEW_ALWAYS && (P.rows + PF_ROWS - 1) / PF_ROWS * ((T + 63) / 64) > 768)) return false;
+    return P.mask == nullptr && P.rows % 8 == 0 && (P.R_u == P.rows || P.R_u % PF_ROWS == 0) && (P.G % 128 == 0 || P.G == 96 || P.G == 64);
+}
 
 #ifdef __HIPCC__
 
@@ -57,14 +64,14 @@ __device__ __forceinline__ float expand_one(const AdapterArgs& A, const float* _
 
 // Workgroups [0, shrinks): h, token by token; the others: X in the lanes' order, and its sums, one k-block and fragment a wavefront.
 template <int S>
-__global__ __launch_bounds__(256) void few_prepare_kernel(const FewArgs Q, const int32_t fragments, const int64_t shrinks, float* __restrict__ h) {
+__global__ __launch_bounds__(256) void few_prepare_kernel(const FewArgs Q, const int64_t shrinks, float* __restrict__ h) {
     if (blockIdx.x < shrinks) {
         shrink_token(Q.X, Q.ldx, (int32_t)Q.P.cols, Q.A, false, h, blockIdx.x);
         return;
     }
     const int64_t at = (blockIdx.x - shrinks) * 4 + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63, sub = lane & 31, hh = lane >> 5;
-    const int32_t kb = (int32_t)(at / fragments), n = (int32_t)(at - (int64_t)kb * fragments);
+    const int32_t kb = (int32_t)(at / Q.fragments), n = (int32_t)(at - (int64_t)kb * Q.fragments);
     if (kb >= Q.n_kb) return;
     const int64_t t = n * 32 + sub;
     const bool in = t < Q.T;
@@ -81,7 +88,7 @@ __global__ __launch_bounds__(256) void few_prepare_kernel(const FewArgs Q, const
         sum += (p[0] + p[1]) + (p[2] + p[3]);
     }
     sum += __shfl_xor(sum, 32, 64);
-    if (hh == 0) Q.xs[kb * 64 + t] = sum;
+    if (hh == 0) Q.xs[kb * FEW_MOST + t] = sum;
 }
 
 template <int S, int NTF, int WAVES, bool LAID>
@@ -96,7 +103,8 @@ __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q
     __syncthreads();
     const PackArgs& P = Q.P;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, sub = lane & 31, hh = lane >> 5;
-    const int64_t row0 = (int64_t)blockIdx.x * PF_ROWS;
+    const uint32_t tb = blockIdx.x / Q.row_blocks;
+    const int64_t row0 = (int64_t)(blockIdx.x - tb * Q.row_blocks) * PF_ROWS, t0 = (int64_t)tb * (NTF * 32);
     const int64_t rb = row0 / P.R_u, lrow0 = row0 - rb * P.R_u;
     const int32_t rows_left = P.R_u - lrow0 < PF_ROWS ? (int32_t)(P.R_u - lrow0) : PF_ROWS;
     const int32_t lr = sub < rows_left ? sub : rows_left - 1;
@@ -107,8 +115,9 @@ __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q
     const bf16x8 ones = as_bf16x8(make_uint4(one, one, one, one));
 
     auto x_at = [&](int n, int32_t kb) {
-        const int64_t t = n * 32 + sub;
-        return LAID ? Q.frag + ((int64_t)(kb * NTF + n) * S * 64 + lane)
+        const int64_t t = t0 + n * 32 + sub;
+        const int32_t f = (int32_t)tb * NTF + n;            // the last workgroup's second fragment may not exist
+        return LAID ? Q.frag + (((int64_t)kb * Q.fragments + (f < Q.fragments ? f : Q.fragments - 1)) * S * 64 + lane)
                     : reinterpret_cast<const uint4*>(Q.X + (t < Q.T ? t : Q.T - 1) * Q.ldx + (int64_t)kb * (16 * S) + hh * (8 * S));
     };
     f32x16 tot[NTF] = {};
@@ -142,19 +151,19 @@ __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q
         }
         const int64_t g = u * P.R_u + lrow0 + lr;
         float alpha, beta, xsum[NTF];
-        pk_affine(a, P.scale[g], P.offset[g], alpha, beta);
+        pk_affine(a, P.scale[g], P.offset[g], false, alpha, beta);
         uint4 x[S][NTF];
 #pragma unroll
         for (int n = 0; n < NTF; ++n) {
             const uint4* const from = x_at(n, kb);
 #pragma unroll
             for (int s = 0; s < S; ++s) x[s][n] = from[LAID ? s * 64 : s];
-            if (LAID) xsum[n] = Q.xs[kb * 64 + n * 32 + sub];
+            if (LAID) xsum[n] = Q.xs[kb * FEW_MOST + t0 + n * 32 + sub];
         }
         if (kb + WAVES < Q.n_kb) a = __builtin_amdgcn_readfirstlane(pk_action(P, rb * P.n_chunks + (kb + WAVES) / per_chunk, base));
         if (kb == wave && Q.h != nullptr) {                 // while all of this is on its way
             const int r = threadIdx.x & 31;
-            const int64_t t = threadIdx.x >> 5;
+            const int64_t t = t0 + (threadIdx.x >> 5);
             if (r < rows_left && t < Q.T) more = expand_one<uint16_t>(Q.A, Q.h, t, row0 + r, P.rows);
         }
         if (hh == 0) {
@@ -241,7 +250,7 @@ __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q
 #pragma unroll 1
     for (int e = threadIdx.x; e < NTF * 1024; e += WAVES * 64) {
         const int r = e & 31, n = e >> 5;                  // neighbouring lanes: neighbouring rows of a token
-        const int64_t y = row0 + r, t = n;
+        const int64_t y = row0 + r, t = t0 + n;
         if (r >= rows_left || t >= Q.T) continue;
         if (Q.h != nullptr && (e != (int)threadIdx.x || wave >= Q.n_kb)) more = expand_one<uint16_t>(Q.A, Q.h, t, y, P.rows);
         const int at = ((n >> 5) * 16 + (r >> 3) * 4 + (r & 3)) * 64 + ((r >> 2) & 1) * 32 + (n & 31);
@@ -253,22 +262,23 @@ __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q
     }
 }
 
-// h is formed ahead where tokens are read directly, here otherwise.
+// h, or null: formed here.
 template <int S>
-int launch_few(const FewArgs& Q, float* h, hipStream_t st) {
-    const int64_t blocks = (Q.P.rows + PF_ROWS - 1) / PF_ROWS;
-    const int fragments = Q.T <= 32 ? 1 : 2;
+int launch_few(FewArgs Q, float* h, hipStream_t st) {
+    Q.fragments = (int32_t)tokens_in(Q.T, 32);
+    Q.row_blocks = (uint32_t)((Q.P.rows + PF_ROWS - 1) / PF_ROWS);
     const bool laid = Q.T > FEW_DIRECT;
+    const int64_t wgs = (int64_t)Q.row_blocks * tokens_in(Q.T, Q.fragments == 1 ? 32 : 64);
     const int64_t shrinks = h != nullptr ? shrink_token_workgroups(Q.T, Q.A.max_rank) : 0;
-    const int64_t wgs = shrinks + (laid ? tokens_in((int64_t)Q.n_kb * fragments, 4) : 0);
-    if (!fits_launch(blocks, 1024) || !fits_launch(wgs, 256)) return WINDQ_ESHAPE;
-    if (wgs > 0) {
-        few_prepare_kernel<S><<<dim3((uint32_t)wgs), dim3(256), 0, st>>>(Q, fragments, shrinks, h);
+    const int64_t ahead = shrinks + (laid ? tokens_in((int64_t)Q.n_kb * Q.fragments, 4) : 0);
+    if (!fits_launch(wgs, 1024) || !fits_launch(ahead, 256)) return WINDQ_ESHAPE;
+    if (ahead > 0) {
+        few_prepare_kernel<S><<<dim3((uint32_t)ahead), dim3(256), 0, st>>>(Q, shrinks, h);
         if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
     }
-    const dim3 g((uint32_t)blocks);
+    const dim3 g((uint32_t)wgs);
     if (!laid) project_few_kernel<S, 1, 16, false><<<g, dim3(1024), 0, st>>>(Q);
-    else if (fragments == 1) project_few_kernel<S, 1, 8, true><<<g, dim3(512), 0, st>>>(Q);
+    else if (Q.fragments == 1) project_few_kernel<S, 1, 8, true><<<g, dim3(512), 0, st>>>(Q);
     else project_few_kernel<S, 2, 8, true><<<g, dim3(512), 0, st>>>(Q);
     return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
 }

@@ -102,7 +102,7 @@ __global__ __launch_bounds__(256) void tiles_prepare_kernel(const TileArgs Q, co
         const int64_t lrow = strip * PT_STRIP + (threadIdx.x & 63);
         if (lrow < P.R_u) {
             float alpha, beta;
-            pk_affine(a == 3 ? 2 : a, P.scale[u * P.R_u + lrow], P.offset[u * P.R_u + lrow], alpha, beta);
+            pk_affine(a == 3 ? 2 : a, P.scale[u * P.R_u + lrow], P.offset[u * P.R_u + lrow], sizeof(XT) == 4, alpha, beta);
             uint32_t hi, mid, lo;
             split3(beta, hi, mid, lo);
             if (threadIdx.x < 64) Q.alpha[j * P.rows + rb * P.R_u + lrow] = alpha;
@@ -335,24 +335,25 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
         // the tokens of the step DEPTH on are read: LDS takes longer than one step.  The next k-block's X is asked for in between, a
         // piece a step: 64 lanes' 16 bytes keep the way to LDS busy for 16 clocks, and who asks for more at once waits for it.
         auto steps = [&](auto fields, int row_bytes) {
-            constexpr int DEPTH = 2;
             decltype(fields) v[2];
+            auto octet = [&](int f, int s) { return NP == 3 ? centred(v[f].octet(s, bits), pk_centre(kind)) : v[f].octet(s, bits); };
+            constexpr int DEPTH = 2;
             bf16x8 b[DEPTH + 1][2];
             uint4 a[2][2];
             v[0].template read<S>(cb + sub * row_bytes + hh * (row_bytes >> 1));
             v[1].template read<S>(cb + (32 + sub) * row_bytes + hh * (row_bytes >> 1));
 #pragma unroll
             for (int s = 0; s < DEPTH; ++s) tokens_of(s, b[s]);
-            a[0][0] = v[0].octet(0, bits);
-            a[0][1] = v[1].octet(0, bits);
+            a[0][0] = octet(0, 0);
+            a[0][1] = octet(1, 0);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int s = 0; s < S; ++s) {
                 if (s < 4) load_piece(s, kb_then, plane_then, buf ^ 1);
                 if (s + DEPTH < S) tokens_of(s + DEPTH, b[(s + DEPTH) % (DEPTH + 1)]);
                 if (s + 1 < S) {
-                    a[(s + 1) & 1][0] = v[0].octet(s + 1, bits);
-                    a[(s + 1) & 1][1] = v[1].octet(s + 1, bits);
+                    a[(s + 1) & 1][0] = octet(0, s + 1);
+                    a[(s + 1) & 1][1] = octet(1, s + 1);
                 }
                 multiply(a[s & 1], b[s % (DEPTH + 1)]);
                 if (s + DEPTH < S) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
