@@ -3,57 +3,7 @@
 
 namespace windq {
 
-// A workgroup per adapter: counts its tokens and those of the adapters below it, then lists its own, in ascending order.
-__global__ __launch_bounds__(256) void group_kernel(const GroupArgs Q) {
-    __shared__ int32_t sums[2][4];
-    const int32_t k = blockIdx.x;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    int32_t below = 0, mine = 0;
-    for (int64_t t = threadIdx.x; t < Q.T; t += 256) {
-        const int32_t id = Q.of[t];
-        below += id >= 0 && id < k ? 1 : 0;
-        mine += id == k ? 1 : 0;
-    }
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) {
-        below += __shfl_xor(below, m, 64);
-        mine += __shfl_xor(mine, m, 64);
-    }
-    if (lane == 0) {
-        sums[0][wave] = below;
-        sums[1][wave] = mine;
-    }
-    __syncthreads();
-    below = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
-    mine = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
-    const int64_t slot = (int64_t)(below / GROUP) + k;
-    const int64_t end = k + 1 == Q.n ? Q.slots : (int64_t)((below + mine) / GROUP) + k + 1;
-    if (threadIdx.x == 0) {
-        Q.first[k] = (int32_t)(slot * GROUP);
-        Q.count[k] = mine;
-    }
-    const int64_t used = slot + (mine + GROUP - 1) / GROUP;
-    for (int64_t s = slot + threadIdx.x; s < end; s += 256) Q.owner[s] = s < used ? k : -1;
-    int64_t at = slot * GROUP;
-    __syncthreads();
-    for (int64_t t0 = 0; t0 < Q.T; t0 += 256) {
-        const int64_t t = t0 + threadIdx.x;
-        const bool hit = t < Q.T && Q.of[t] == k;
-        const uint64_t hits = __ballot(hit);
-        if (lane == 0) sums[0][wave] = __popcll(hits);
-        __syncthreads();
-        int32_t before = __popcll(hits & ((1ull << lane) - 1ull)), all = 0;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            before += w < wave ? sums[0][w] : 0;
-            all += sums[0][w];
-        }
-        if (hit) Q.place[at + before] = (int32_t)t;
-        at += all;
-        __syncthreads();
-    }
-    for (int64_t p = at + threadIdx.x; p < end * GROUP; p += 256) Q.place[p] = -1;
-}
+__global__ __launch_bounds__(256) void group_kernel(const GroupArgs Q) { group_adapter(Q, blockIdx.x); }
 
 int launch_group(const GroupArgs& G, hipStream_t st) {
     if (!fits_launch(G.n, 256)) return WINDQ_ESHAPE;
@@ -64,10 +14,12 @@ int launch_group(const GroupArgs& G, hipStream_t st) {
 // 64 tokens of one adapter by up to 16 RF ranks, over a piece of the columns that the four wavefronts share 64 at a time.  Both factors
 // are rows along the sum's axis, so operands come straight from memory; ranks are the M side.  Bound by reading X once.
 template <int RF>
-__global__ __launch_bounds__(256) void shrink_kernel(const ShrinkArgs Q) {
+__global__ __launch_bounds__(256) void shrink_kernel(const ShrinkArgs Q1, const ShrinkArgs Q2, const int64_t first2) {
     __shared__ float red[4][RF * 16][65];
-    const int64_t slot = blockIdx.x / Q.splits;
-    const int32_t split = (int32_t)(blockIdx.x - slot * Q.splits);
+    const ShrinkArgs& Q = blockIdx.x < first2 ? Q1 : Q2;
+    const int64_t block = blockIdx.x < first2 ? blockIdx.x : blockIdx.x - first2;
+    const int64_t slot = block / Q.splits;
+    const int32_t split = (int32_t)(block - slot * Q.splits);
     const int32_t k = Q.owner[slot];
     if (k < 0) return;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
@@ -125,30 +77,33 @@ __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkArgs Q) {
     }
 }
 
-int launch_shrink(const ShrinkArgs& S, hipStream_t st) {
-    const int64_t wgs = S.slots * S.splits;
+int launch_shrink(const ShrinkArgs& S, const ShrinkArgs* more, hipStream_t st) {
+    const ShrinkArgs& S2 = more != nullptr ? *more : S;
+    const int64_t first2 = S.slots * S.splits, wgs = first2 + (more != nullptr ? S2.slots * S2.splits : 0);
     if (!fits_launch(wgs, 256)) return WINDQ_ESHAPE;
     const dim3 g((uint32_t)wgs), b(256);
     switch (shrink_ranks(S.A.max_rank) / 16) {
-        case 1: shrink_kernel<1><<<g, b, 0, st>>>(S); break;
-        case 2: shrink_kernel<2><<<g, b, 0, st>>>(S); break;
-        case 3: shrink_kernel<3><<<g, b, 0, st>>>(S); break;
-        case 4: shrink_kernel<4><<<g, b, 0, st>>>(S); break;
-        case 5: shrink_kernel<5><<<g, b, 0, st>>>(S); break;
-        case 6: shrink_kernel<6><<<g, b, 0, st>>>(S); break;
-        case 7: shrink_kernel<7><<<g, b, 0, st>>>(S); break;
-        default: shrink_kernel<8><<<g, b, 0, st>>>(S); break;
+        case 1: shrink_kernel<1><<<g, b, 0, st>>>(S, S2, first2); break;
+        case 2: shrink_kernel<2><<<g, b, 0, st>>>(S, S2, first2); break;
+        case 3: shrink_kernel<3><<<g, b, 0, st>>>(S, S2, first2); break;
+        case 4: shrink_kernel<4><<<g, b, 0, st>>>(S, S2, first2); break;
+        case 5: shrink_kernel<5><<<g, b, 0, st>>>(S, S2, first2); break;
+        case 6: shrink_kernel<6><<<g, b, 0, st>>>(S, S2, first2); break;
+        case 7: shrink_kernel<7><<<g, b, 0, st>>>(S, S2, first2); break;
+        default: shrink_kernel<8><<<g, b, 0, st>>>(S, S2, first2); break;
     }
     return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
 }
 
 // A workgroup adds up eight ranks of a slot's pieces; the workgroups behind them write the zeros of tokens without an adapter, 64 tokens each.
 constexpr int JOIN_RANKS = 8;
-__global__ __launch_bounds__(256) void join_kernel(const JoinArgs Q) {
+__global__ __launch_bounds__(256) void join_kernel(const JoinArgs Q1, const JoinArgs Q2, const int64_t first2) {
+    const JoinArgs& Q = blockIdx.x < first2 ? Q1 : Q2;
+    const int64_t block = blockIdx.x < first2 ? blockIdx.x : blockIdx.x - first2;
     const int32_t R = Q.A.max_rank, ranks = (R + 15) / 16 * 16, groups = R / JOIN_RANKS;
-    const int64_t slot = blockIdx.x / groups;
+    const int64_t slot = block / groups;
     if (slot >= Q.slots) {
-        const int64_t t0 = (blockIdx.x - Q.slots * groups) * GROUP;
+        const int64_t t0 = (block - Q.slots * groups) * GROUP;
         for (int e = threadIdx.x; e < GROUP * R; e += 256) {
             const int64_t t = t0 + e / R;
             if (t >= Q.T) break;
@@ -161,7 +116,7 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinArgs Q) {
     const int32_t k = Q.owner[slot];
     if (k < 0) return;
     const int64_t places = Q.slots * GROUP;
-    const int32_t r0 = (int32_t)(blockIdx.x - slot * groups) * JOIN_RANKS;
+    const int32_t r0 = (int32_t)(block - slot * groups) * JOIN_RANKS;
     const int n = threadIdx.x & 63;                        // places side by side
     const int32_t t = Q.place[slot * GROUP + n];
     const float factor = Q.scaled && Q.A.alpha != nullptr ? Q.A.alpha[k] : 1.0f;
@@ -170,8 +125,12 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinArgs Q) {
         const int r = r0 + i * 4 + (threadIdx.x >> 6);
         const float* __restrict__ const p = Q.part + (slot * ranks + r) * GROUP + n;
         float v = 0.0f;
+        if (Q.given != nullptr) {
+            if (t >= 0) v = Q.given[(int64_t)t * R + r];
+        } else {
 #pragma unroll 8
-        for (int32_t s = 0; s < Q.splits; ++s) v += p[(int64_t)s * places * ranks];
+            for (int32_t s = 0; s < Q.splits; ++s) v += p[(int64_t)s * places * ranks];
+        }
         v = t >= 0 ? factor * v : 0.0f;
         tile[n][r - r0] = v;
         if (Q.planes != nullptr) {
@@ -191,10 +150,11 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinArgs Q) {
     }
 }
 
-int launch_join(const JoinArgs& J, hipStream_t st) {
-    const int64_t wgs = J.slots * (J.A.max_rank / JOIN_RANKS) + (J.h != nullptr ? tokens_in(J.T, GROUP) : 0);
+int launch_join(const JoinArgs& J, const JoinArgs* more, hipStream_t st) {
+    auto count = [](const JoinArgs& j) { return j.slots * (j.A.max_rank / JOIN_RANKS) + (j.h != nullptr ? tokens_in(j.T, GROUP) : 0); };
+    const int64_t first2 = count(J), wgs = first2 + (more != nullptr ? count(*more) : 0);
     if (!fits_launch(wgs, 256)) return WINDQ_ESHAPE;
-    join_kernel<<<dim3((uint32_t)wgs), dim3(256), 0, st>>>(J);
+    join_kernel<<<dim3((uint32_t)wgs), dim3(256), 0, st>>>(J, more != nullptr ? *more : J, first2);
     return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
 }
 

@@ -346,10 +346,10 @@ int project_all(ProjectArgs& Q, const windq_mat* X, const windq_adapters* ad, fl
                                reinterpret_cast<int32_t*>(ws + at.first), reinterpret_cast<int32_t*>(ws + at.count)};
                 ShrinkArgs S = {X->data, X->ld, Q.A.a, Q.P.cols, (int32_t)Q.P.cols, shrink_splits(G.slots, Q.P.cols), G.slots, G.place, G.owner, Q.A,
                                 reinterpret_cast<float*>(ws + at.part)};
-                JoinArgs J = {S.part, S.splits, G.slots, G.place, G.owner, T, Q.A, false, ht, nullptr};
+                JoinArgs J = {S.part, S.splits, G.slots, G.place, G.owner, T, Q.A, false, ht, nullptr, nullptr};
                 int status = launch_group(G, st);
-                if (status == WINDQ_OK) status = launch_shrink(S, st);
-                if (status == WINDQ_OK) status = launch_join(J, st);
+                if (status == WINDQ_OK) status = launch_shrink(S, nullptr, st);
+                if (status == WINDQ_OK) status = launch_join(J, nullptr, st);
                 if (status != WINDQ_OK) return status;
             }
         }

@@ -11,10 +11,10 @@ int check_tokens(const windq_mat* M, int64_t width, bool vector);
 // ------------------------------------------------------------------------------------------------ layouts
 // out [n][C][ldo] = in [n][R][C] transposed, rows padded with zeros up to ldo.
 template <typename T>
-__global__ __launch_bounds__(256) void transpose_kernel(const T* __restrict__ in, int64_t R, int32_t C, int64_t ldo, T* __restrict__ out) {
+__device__ __forceinline__ void transpose(const T* __restrict__ in, int64_t R, int32_t C, int64_t ldo, T* __restrict__ out, int64_t block) {
     __shared__ T tile[64][65];
     const int64_t rt = (ldo + 63) / 64, ct = (C + 63) / 64;
-    const int64_t k = blockIdx.x / (rt * ct), rest = blockIdx.x - k * rt * ct;
+    const int64_t k = block / (rt * ct), rest = block - k * rt * ct;
     const int64_t r0 = rest / ct * 64, c0 = (rest - rest / ct * ct) * 64;
     for (int i = threadIdx.x; i < 4096; i += 256) {
         const int64_t r = r0 + (i >> 6), c = c0 + (i & 63);
@@ -26,6 +26,8 @@ __global__ __launch_bounds__(256) void transpose_kernel(const T* __restrict__ in
         if (c < C && r < ldo) out[(k * C + c) * ldo + r] = tile[i & 63][i >> 6];
     }
 }
+
+inline int64_t transpose_workgroups(int64_t n, int64_t C, int64_t ldo) { return n * ((ldo + 63) / 64) * ((C + 63) / 64); }
 
 // A copy of dY whose rows start on 16 bytes and end with zeros.
 template <typename T>
@@ -324,13 +326,13 @@ __global__ __launch_bounds__(256) void dx_kernel(const DxArgs Q) {
 }
 
 // w_hat rounded to bfloat16 and turned: wt [cols][K], zeros from the last row to K.  A thread has eight rows by eight columns.
-__global__ __launch_bounds__(256) void turn_kernel(const PackArgs P, int32_t K, uint16_t* __restrict__ wt) {
+__device__ __forceinline__ void turn(const PackArgs& P, int32_t K, uint16_t* __restrict__ wt, int64_t block) {
     __shared__ uint16_t trits_of[256];
     trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
     __syncthreads();
     const int32_t row_blocks = (K + 255) / 256;
-    const int64_t cb = blockIdx.x / row_blocks;
-    const int64_t r0 = (blockIdx.x - cb * row_blocks) * 256 + (threadIdx.x & 31) * 8, col = cb * 64 + (threadIdx.x >> 5) * 8;
+    const int64_t cb = block / row_blocks;
+    const int64_t r0 = (block - cb * row_blocks) * 256 + (threadIdx.x & 31) * 8, col = cb * 64 + (threadIdx.x >> 5) * 8;
     if (col >= P.cols || r0 >= K) return;
     uint32_t v[8][4];
 #pragma unroll
@@ -345,34 +347,76 @@ __global__ __launch_bounds__(256) void turn_kernel(const PackArgs P, int32_t K, 
     for (int m = 0; m < 8; ++m) *reinterpret_cast<uint4*>(wt + (col + m) * K + r0) = make_uint4(v[m][0], v[m][1], v[m][2], v[m][3]);
 }
 
-// fp32: 64 columns and 64 tokens a workgroup, 32 rows at a time through LDS, on the fp32 matrix instructions.
-__global__ __launch_bounds__(256) void dx_f32_kernel(const DxArgs Q) {
-    __shared__ float wt[32][68], yt[32][68];
+// What the later kernels read, in one launch: the reconstruction turned, B and A transposed, tokens by adapter.  Workgroups in that order.
+template <typename XT>
+struct PrepareArgs {
+    PackArgs P;
+    int32_t K;
+    uint16_t* wt;
+    const XT* b;
+    XT* bt;
+    const XT* a;
+    XT* at;
+    int64_t ld;                // of B transposed
+    AdapterArgs A;
+    GroupArgs G;
+    int64_t turns, bs, as, groups;
+};
+
+template <typename XT>
+__global__ __launch_bounds__(256) void grad_prepare_kernel(const PrepareArgs<XT> Q) {
+    int64_t block = blockIdx.x;
+    if (block < Q.turns) return turn(Q.P, Q.K, Q.wt, block);
+    block -= Q.turns;
+    if (block < Q.bs) return transpose(Q.b, Q.P.rows, Q.A.max_rank, Q.ld, Q.bt, block);
+    block -= Q.bs;
+    if (block < Q.as) return transpose(Q.a, (int64_t)Q.A.max_rank, (int32_t)Q.P.cols, (int64_t)Q.A.max_rank, Q.at, block);
+    group_adapter(Q.G, (int32_t)(block - Q.as));
+}
+
+// fp32: 64 columns and 64 tokens a workgroup on the fp32 matrix instructions.  Sixteen wavefronts, four to a quarter of the rows, which go
+// through LDS 32 at a time, the next ones on their way meanwhile: small layers leave few workgroups, and a wavefront's time is latency.
+constexpr int DXF_THREADS = 1024, DXF_PARTS = DXF_THREADS / 256;
+__global__ __launch_bounds__(DXF_THREADS) void dx_f32_kernel(const DxArgs Q) {
+    __shared__ float wts[DXF_PARTS][32][68], yts[DXF_PARTS][32][68];
     __shared__ uint16_t trits_of[256];
-    trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
+    if (threadIdx.x < 256) trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
     __syncthreads();
     const PackArgs& P = Q.P;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
+    const int part = threadIdx.x >> 8, tid = threadIdx.x & 255, wave = tid >> 6, lane = tid & 63, sub = lane & 15, q = lane >> 4;
+    float(&wt)[32][68] = wts[part];
+    float(&yt)[32][68] = yts[part];
     const int64_t col_blocks = (P.cols + 63) / 64;
     const int64_t tb = blockIdx.x / col_blocks;
     const int64_t c0 = (blockIdx.x - tb * col_blocks) * 64, t0 = tb * 64;
     const float* __restrict__ const dY = static_cast<const float*>(Q.dY);
     f32x4 acc[4] = {};
     if (Q.packed) {
-        for (int64_t r0 = 0; r0 < P.rows; r0 += 32) {
-            __syncthreads();
-            {
-                const int r = threadIdx.x >> 3, o = threadIdx.x & 7;
-                float w[8] = {};
-                if (r0 + r < P.rows && c0 + o * 8 < P.cols) weight_octet(P, r0 + r, c0 + o * 8, trits_of, w);
+        const int64_t blocks = (P.rows + 31) / 32, each = (blocks + DXF_PARTS - 1) / DXF_PARTS;       // the same for all parts: barriers are shared
+        const int r = tid >> 3, o = tid & 7, yr = tid & 31;
+        float w[8], y[8];
+        auto fetch = [&](int64_t block) {
+            const int64_t r0 = block * 32;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) wt[r][o * 8 + j] = w[j];
+            for (int j = 0; j < 8; ++j) w[j] = 0.0f;
+            if (r0 + r < P.rows && c0 + o * 8 < P.cols) weight_octet(P, r0 + r, c0 + o * 8, trits_of, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int64_t t = t0 + (tid >> 5) + 8 * j;
+                y[j] = r0 + yr < P.rows && t < Q.T ? dY[t * Q.ldy + r0 + yr] : 0.0f;
             }
-            for (int i = threadIdx.x; i < 64 * 32; i += 256) {
-                const int r = i & 31, t = i >> 5;
-                yt[r][t] = r0 + r < P.rows && t0 + t < Q.T ? dY[(t0 + t) * Q.ldy + r0 + r] : 0.0f;
+        };
+        fetch(part * each);
+        for (int64_t i = 0; i < each; ++i) {
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                wt[r][o * 8 + j] = w[j];
+                yt[yr][(tid >> 5) + 8 * j] = y[j];
             }
             __syncthreads();
+            // past its quarter a part multiplies zeros
+            fetch(i + 1 < each ? part * each + i + 1 : blocks);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const float a = wt[k * 4 + q][wave * 16 + sub];
@@ -380,7 +424,32 @@ __global__ __launch_bounds__(256) void dx_f32_kernel(const DxArgs Q) {
                 for (int n = 0; n < 4; ++n) acc[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, yt[k * 4 + q][n * 16 + sub], acc[n], 0, 0, 0);
             }
         }
+        __syncthreads();
+        // the parts' sums, in order
+        float(*const red)[DXF_PARTS][4][64][4] = reinterpret_cast<float(*)[DXF_PARTS][4][64][4]>(&wts[0][0][0]);    // [n pair][part][wave][lane][i], two at a time
+        static_assert(sizeof(float) * 2 * DXF_PARTS * 4 * 64 * 4 <= sizeof(wts), "the sums fit");
+#pragma unroll
+        for (int n2 = 0; n2 < 4; n2 += 2) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) red[n][part][wave][lane][i] = acc[n2 + n][i];
+            __syncthreads();
+            if (part == 0) {
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float v = red[n][0][wave][lane][i];
+#pragma unroll
+                        for (int p = 1; p < DXF_PARTS; ++p) v += red[n][p][wave][lane][i];
+                        acc[n2 + n][i] = v;
+                    }
+            }
+            __syncthreads();
+        }
     }
+    if (part != 0) return;
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
         const int64_t t = t0 + n * 16 + sub;
@@ -416,7 +485,7 @@ __global__ __launch_bounds__(256) void dx_f32_kernel(const DxArgs Q) {
 constexpr int64_t TURN_FROM = 256;
 
 struct GradWs {
-    size_t h, dh, bt, at, dy, place, owner, first, count, part, planes_h, planes_dh, wt, total;
+    size_t h, dh, bt, at, dy, place, owner, first, count, part, part2, planes_h, planes_dh, wt, total;
     int64_t ld;                // of dY's copy and of B transposed
 };
 
@@ -443,6 +512,7 @@ GradWs grad_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t n, 
     w.first = take((size_t)n * 4);
     w.count = take((size_t)n * 4);
     w.part = take(bf && n > 0 ? (size_t)shrink_splits(slots, wide) * (size_t)slots * GROUP * (size_t)shrink_ranks(max_rank) * 4 : 0);
+    w.part2 = take(bf && n > 0 ? (size_t)shrink_splits(slots, wide) * (size_t)slots * GROUP * (size_t)shrink_ranks(max_rank) * 4 : 0);
     w.planes_h = take(bf && n > 0 ? (size_t)slots * GROUP * (size_t)max_rank * 6 : 0);
     w.planes_dh = take(bf && n > 0 ? (size_t)slots * GROUP * (size_t)max_rank * 6 : 0);
     w.wt = take(bf && T >= TURN_FROM ? (size_t)gemm_cols(cols) * (size_t)gemm_k(rows) * 2 : 0);
@@ -482,30 +552,57 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
     }
     const XT* const dYv = static_cast<const XT*>(Q.dY);
     const int32_t rows8 = (int32_t)((rows + 7) / 8 * 8);
+    PrepareArgs<XT> R = {};
+    R.P = Q.P;
+    R.A = A;
+    const GroupArgs G = {A.of, T, A.n, group_slots(T, A.n), reinterpret_cast<int32_t*>(ws + at.place), reinterpret_cast<int32_t*>(ws + at.owner),
+                         reinterpret_cast<int32_t*>(ws + at.first), reinterpret_cast<int32_t*>(ws + at.count)};
+    XT* const bt = reinterpret_cast<XT*>(ws + at.bt);
+    const bool outer = dA != nullptr;
+    if (turn) {
+        R.K = (int32_t)gemm_k(rows);
+        R.wt = reinterpret_cast<uint16_t*>(ws + at.wt);
+        R.turns = ((cols + 63) / 64) * ((R.K + 255) / 256);
+    }
+    if (side) {
+        R.b = static_cast<const XT*>(A.b);
+        R.bt = bt;
+        R.ld = at.ld;
+        R.bs = transpose_workgroups(A.n, A.max_rank, at.ld);
+        if (bf && Q.dX != nullptr && T >= TURN_FROM) {
+            R.a = static_cast<const XT*>(A.a);
+            R.at = reinterpret_cast<XT*>(ws + at.at);
+            R.as = transpose_workgroups(A.n, cols, A.max_rank);
+        }
+        if (bf || outer) {
+            R.G = G;
+            R.groups = A.n;
+        }
+    }
+    WINDQ_LAUNCH(R.turns + R.bs + R.as + R.groups, 256, grad_prepare_kernel<XT>, R);
     if (side) {
         float* const dh = reinterpret_cast<float*>(ws + at.dh);
-        XT* const bt = reinterpret_cast<XT*>(ws + at.bt);
-        WINDQ_LAUNCH((int64_t)A.n * ((at.ld + 63) / 64) * ((A.max_rank + 63) / 64), 256, transpose_kernel<XT>, static_cast<const XT*>(A.b), rows, A.max_rank, at.ld, bt);
-        GroupArgs G = {A.of, T, A.n, group_slots(T, A.n), reinterpret_cast<int32_t*>(ws + at.place), reinterpret_cast<int32_t*>(ws + at.owner),
-                       reinterpret_cast<int32_t*>(ws + at.first), reinterpret_cast<int32_t*>(ws + at.count)};
-        const bool outer = dA != nullptr;
         const int64_t tokens = shrink_token_workgroups(T, A.max_rank);
-        if (bf || outer) {
-            const int status = launch_group(G, st);
-            if (status != WINDQ_OK) return status;
-        }
         if constexpr (bf) {
             float* const part = reinterpret_cast<float*>(ws + at.part);
             uint16_t* const planes_h = reinterpret_cast<uint16_t*>(ws + at.planes_h);
             uint16_t* const planes_dh = reinterpret_cast<uint16_t*>(ws + at.planes_dh);
-            auto shrink = [&](const void* x, int64_t ld, const void* a, int64_t lda, int64_t width, bool scaled, float* to, uint16_t* planes) {
-                ShrinkArgs S = {x, ld, a, lda, (int32_t)width, shrink_splits(G.slots, width), G.slots, G.place, G.owner, A, part};
-                JoinArgs J = {part, S.splits, G.slots, G.place, G.owner, T, A, scaled, to, planes};
-                const int status = launch_shrink(S, st);
-                return status == WINDQ_OK ? launch_join(J, st) : status;
+            float* const part2 = reinterpret_cast<float*>(ws + at.part2);
+            auto pieces = [&](const void* x, int64_t ld, const void* a, int64_t lda, int64_t width, float* to) {
+                return ShrinkArgs{x, ld, a, lda, (int32_t)width, shrink_splits(G.slots, width), G.slots, G.place, G.owner, A, to};
             };
-            int status = shrink(Q.dY, Q.ldy, bt, at.ld, rows8, true, dh, outer ? planes_dh : nullptr);
-            if (status == WINDQ_OK && outer) status = shrink(X->data, X->ld, A.a, cols, cols, false, nullptr, planes_h);
+            const ShrinkArgs S1 = pieces(Q.dY, Q.ldy, bt, at.ld, rows8, part);
+            const JoinArgs J1 = {part, S1.splits, G.slots, G.place, G.owner, T, A, true, dh, outer ? planes_dh : nullptr, nullptr};
+            JoinArgs J2 = {part2, 0, G.slots, G.place, G.owner, T, A, false, nullptr, planes_h, h};
+            int status;
+            if (outer && h == nullptr) {
+                const ShrinkArgs S2 = pieces(X->data, X->ld, A.a, cols, cols, part2);
+                J2.splits = S2.splits;
+                status = launch_shrink(S1, &S2, st);
+            } else {
+                status = launch_shrink(S1, nullptr, st);
+            }
+            if (status == WINDQ_OK) status = launch_join(J1, outer ? &J2 : nullptr, st);
             if (status != WINDQ_OK) return status;
             if (outer) {
                 const int32_t groups = (A.max_rank + 63) / 64;
@@ -538,17 +635,12 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
     if (Q.dX == nullptr || T == 0) return WINDQ_OK;
     if constexpr (bf) {
         if (turn) {
-            uint16_t* const wt = reinterpret_cast<uint16_t*>(ws + at.wt);
-            const int32_t K = (int32_t)gemm_k(rows);
-            WINDQ_LAUNCH(((cols + 63) / 64) * ((K + 255) / 256), 256, turn_kernel, Q.P, K, wt);
-            GemmArgs M = {wt, dYv, Q.ldy, K, T, cols, static_cast<uint16_t*>(Q.dX), Q.ldx, Q.dh, nullptr, A, (uint32_t)((cols + GM_M - 1) / GM_M)};
-            if (side) {
-                uint16_t* const to = reinterpret_cast<uint16_t*>(ws + at.at);
-                WINDQ_LAUNCH((int64_t)A.n * ((A.max_rank + 63) / 64) * ((cols + 63) / 64), 256, transpose_kernel<uint16_t>, static_cast<const uint16_t*>(A.a), (int64_t)A.max_rank,
-                             (int32_t)cols, (int64_t)A.max_rank, to);
-                M.at = to;
-            }
-            WINDQ_LAUNCH((int64_t)M.col_blocks * tokens_in(T, GM_N), GM_THREADS, dx_gemm_kernel, M);
+            const int64_t wide = tokens_in(cols, 256) * tokens_in(T, GM_N);
+            const int64_t by = wide >= 256 ? 256 : 128;
+            const GemmArgs M = {R.wt, dYv, Q.ldy, R.K, T, cols, static_cast<uint16_t*>(Q.dX), Q.ldx, Q.dh, R.at, A, (uint32_t)tokens_in(cols, by)};
+            const int64_t wgs = (int64_t)M.col_blocks * tokens_in(T, GM_N);
+            if (by == 256) WINDQ_LAUNCH(wgs, GM_THREADS, dx_gemm_kernel<4>, M);
+            else WINDQ_LAUNCH(wgs, GM_THREADS, dx_gemm_kernel<2>, M);
             return WINDQ_OK;
         }
         const int64_t blocks = (cols + DX_COLS - 1) / DX_COLS;
@@ -556,7 +648,7 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
         else if (T <= 128) WINDQ_LAUNCH(blocks * ((T + 127) / 128), 256, dx_kernel<2>, Q);
         else WINDQ_LAUNCH(blocks * ((T + 255) / 256), 256, dx_kernel<4>, Q);
     } else {
-        WINDQ_LAUNCH(((cols + 63) / 64) * ((T + 63) / 64), 256, dx_f32_kernel, Q);
+        WINDQ_LAUNCH(((cols + 63) / 64) * ((T + 63) / 64), DXF_THREADS, dx_f32_kernel, Q);
     }
     return WINDQ_OK;
 }

@@ -54,11 +54,12 @@ struct JoinArgs {
     bool scaled;
     float* h;                  // [T][max_rank], or null
     uint16_t* planes;          // [3][max_rank][slots * GROUP], or null
+    const float* given;        // [T][max_rank] h in the pieces' place, or null
 };
 
 int launch_group(const GroupArgs& G, hipStream_t st);
-int launch_shrink(const ShrinkArgs& S, hipStream_t st);    // bfloat16
-int launch_join(const JoinArgs& J, hipStream_t st);
+int launch_shrink(const ShrinkArgs& S, const ShrinkArgs* more /* or null */, hipStream_t st);    // bfloat16; both of one max_rank
+int launch_join(const JoinArgs& J, const JoinArgs* more /* or null */, hipStream_t st);
 inline int32_t shrink_ranks(int32_t max_rank) { return (max_rank + 15) / 16 * 16; }
 // Enough pieces that the launch has some workgroups for every CU, and a wavefront at least 64 columns.
 inline int32_t shrink_splits(int64_t slots, int64_t width) {
@@ -68,6 +69,57 @@ inline int32_t shrink_splits(int64_t slots, int64_t width) {
 }
 
 #ifdef __HIPCC__
+
+// A workgroup per adapter: counts its tokens and those of the adapters below it, then lists its own, in ascending order.
+__device__ __forceinline__ void group_adapter(const GroupArgs& Q, const int32_t k) {
+    __shared__ int32_t sums[2][4];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    int32_t below = 0, mine = 0;
+    for (int64_t t = threadIdx.x; t < Q.T; t += 256) {
+        const int32_t id = Q.of[t];
+        below += id >= 0 && id < k ? 1 : 0;
+        mine += id == k ? 1 : 0;
+    }
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) {
+        below += __shfl_xor(below, m, 64);
+        mine += __shfl_xor(mine, m, 64);
+    }
+    if (lane == 0) {
+        sums[0][wave] = below;
+        sums[1][wave] = mine;
+    }
+    __syncthreads();
+    below = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
+    mine = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
+    const int64_t slot = (int64_t)(below / GROUP) + k;
+    const int64_t end = k + 1 == Q.n ? Q.slots : (int64_t)((below + mine) / GROUP) + k + 1;
+    if (threadIdx.x == 0) {
+        Q.first[k] = (int32_t)(slot * GROUP);
+        Q.count[k] = mine;
+    }
+    const int64_t used = slot + (mine + GROUP - 1) / GROUP;
+    for (int64_t s = slot + threadIdx.x; s < end; s += 256) Q.owner[s] = s < used ? k : -1;
+    int64_t at = slot * GROUP;
+    __syncthreads();
+    for (int64_t t0 = 0; t0 < Q.T; t0 += 256) {
+        const int64_t t = t0 + threadIdx.x;
+        const bool hit = t < Q.T && Q.of[t] == k;
+        const uint64_t hits = __ballot(hit);
+        if (lane == 0) sums[0][wave] = __popcll(hits);
+        __syncthreads();
+        int32_t before = __popcll(hits & ((1ull << lane) - 1ull)), all = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            before += w < wave ? sums[0][w] : 0;
+            all += sums[0][w];
+        }
+        if (hit) Q.place[at + before] = (int32_t)t;
+        at += all;
+        __syncthreads();
+    }
+    for (int64_t p = at + threadIdx.x; p < end * GROUP; p += 256) Q.place[p] = -1;
+}
 
 // ------------------------------------------------------------------------------------------------ h = A x, token by token
 // (On the way back: dh = alpha B^T dY, with B transposed in A's place.)  A wavefront per token and rank, eight columns a lane at a time: bound by latency,

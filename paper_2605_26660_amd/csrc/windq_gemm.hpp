@@ -3,7 +3,8 @@
 // Codes lie along columns and the sum runs along rows, so a tile of weights would have to be turned for every 128 tokens.  The packed
 // matrix is reconstructed once instead, rounded to bfloat16 and turned (wt [cols][rows], 2 bytes a weight: less than a tenth of the
 // product's time), and the product then spends nothing but matrix instructions and their operands' way: 256 columns x 128
-// tokens a workgroup, four wavefronts with 128 x 64 results each as 4 x 2 fragments of 32x32x16 instructions, one per SIMD.
+// tokens a workgroup, four wavefronts with 128 x 64 results each as 4 x 2 fragments of 32x32x16 instructions, one per SIMD; 128 columns where
+// that would leave CUs without a workgroup.
 //   64 of the sum at a time go to LDS by direct loads, three buffers: while one is multiplied the next has landed and the one
 // after is on its way.  There is one barrier per buffer, ahead of its last step: by then all of it has been read into registers, and the next
 // one's first operands are read across it.  A row's eight 16-byte slots are exchanged by the row's low bits, so that 32 lanes reading 32
@@ -14,10 +15,10 @@
 
 namespace windq {
 
-constexpr int GM_M = 256, GM_N = 128, GM_K = 64, GM_THREADS = 256, GM_BUFFERS = 3;
+constexpr int GM_MOST = 256, GM_N = 128, GM_K = 64, GM_THREADS = 256, GM_BUFFERS = 3;
 
 struct GemmArgs {
-    const uint16_t* wt;        // [cols rounded up to GM_M][K]
+    const uint16_t* wt;        // [cols rounded up to GM_MOST][K]
     const uint16_t* dY;        // [T][ldy], zeros from rows to K
     int64_t ldy;
     int32_t K;                 // rows rounded up to GM_K
@@ -31,11 +32,13 @@ struct GemmArgs {
 };
 
 inline int64_t gemm_k(int64_t rows) { return (rows + GM_K - 1) / GM_K * GM_K; }
-inline int64_t gemm_cols(int64_t cols) { return (cols + GM_M - 1) / GM_M * GM_M; }
+inline int64_t gemm_cols(int64_t cols) { return (cols + GM_MOST - 1) / GM_MOST * GM_MOST; }
 
 #ifdef __HIPCC__
 
+template <int MF>                                          // fragments of a wavefront along the columns
 __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
+    constexpr int GM_M = MF * 64, WM = MF * 32, LOADS = (GM_M + GM_N) / 32;
     __shared__ uint4 tile[GM_BUFFERS][(GM_M + GM_N) * 8];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, sub = lane & 31, hh = lane >> 5;
     const int wm = wave & 1, wn = wave >> 1;
@@ -59,18 +62,18 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
     auto load_a = [&](int i, int32_t k, int buf) { lds_load16(lds + (buf * (GM_M + GM_N) * 8 + i * 256 + wave * 64) * 16, am + (int64_t)i * 32 * Q.K + k * GM_K); };
     auto load_b = [&](int i, int32_t k, int buf) { lds_load16(lds + (buf * (GM_M + GM_N) * 8 + GM_M * 8 + i * 256 + wave * 64) * 16, bn[i] + k * GM_K); };
     // Operands of step s (16 of the sum): octet 2 s + hh of a row.
-    const uint32_t arow = (wm * 128 + sub) * 128, brow = GM_M * 128 + (wn * 64 + sub) * 128;
-    auto read = [&](int buf, int s, bf16x8 (&a)[4], bf16x8 (&b)[2]) {
+    const uint32_t arow = (wm * WM + sub) * 128, brow = GM_M * 128 + (wn * 64 + sub) * 128;
+    auto read = [&](int buf, int s, bf16x8 (&a)[MF], bf16x8 (&b)[2]) {
         const char* const at = reinterpret_cast<const char*>(tile[buf]);
         const uint32_t o = (uint32_t)((2 * s + hh) ^ (sub & 7)) * 16;
 #pragma unroll
-        for (int f = 0; f < 4; ++f) a[f] = as_bf16x8(*reinterpret_cast<const uint4*>(at + arow + f * 32 * 128 + o));
+        for (int f = 0; f < MF; ++f) a[f] = as_bf16x8(*reinterpret_cast<const uint4*>(at + arow + f * 32 * 128 + o));
 #pragma unroll
         for (int n = 0; n < 2; ++n) b[n] = as_bf16x8(*reinterpret_cast<const uint4*>(at + brow + n * 32 * 128 + o));
     };
 
     const int32_t n_k = Q.K / GM_K;
-    f32x16 acc[4][2] = {};
+    f32x16 acc[MF][2] = {};
     if (n_k > 0) {
 #pragma unroll
         for (int i = 0; i < GM_M / 32; ++i) load_a(i, 0, 0);
@@ -81,9 +84,9 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
         for (int i = 0; i < GM_M / 32; ++i) load_a(i, k1, 1);
 #pragma unroll
         for (int i = 0; i < GM_N / 32; ++i) load_b(i, k1, 1);
-        asm volatile("s_waitcnt vmcnt(12)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
         __syncthreads();
-        bf16x8 a[2][4], b[2][2];
+        bf16x8 a[2][MF], b[2][2];
         read(0, 0, a[0], b[0]);
         int buf = 0;
         for (int32_t k = 0; k < n_k; ++k) {
@@ -91,23 +94,25 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
             const int32_t k2 = k + 2 < n_k ? k + 2 : n_k - 1;       // past the end: again the last, into a buffer that nobody reads
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                // twelve loads in the first three steps
+                // all loads in the first three steps
                 if (s < 3) {
+                    constexpr int EACH = (LOADS + 2) / 3;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int j = s * 4 + i;
+                    for (int i = 0; i < EACH; ++i) {
+                        const int j = s * EACH + i;
+                        if (j >= LOADS) break;
                         if (j < GM_M / 32) load_a(j, k2, then);
                         else load_b(j - GM_M / 32, k2, then);
                     }
                     read(buf, s + 1, a[(s + 1) & 1], b[(s + 1) & 1]);
                 } else {
-                    asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)" ::: "memory");       // the next buffer's loads are done, this one's reads too
+                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LOADS) : "memory");       // the next buffer's loads are done, this one's reads too
                     __builtin_amdgcn_s_barrier();
                     asm volatile("" ::: "memory");
                     read(next, 0, a[0], b[0]);
                 }
 #pragma unroll
-                for (int f = 0; f < 4; ++f)
+                for (int f = 0; f < MF; ++f)
 #pragma unroll
                     for (int n = 0; n < 2; ++n) acc[f][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s & 1][f], b[s & 1][n], acc[f][n], 0, 0, 0);
             }
@@ -117,8 +122,8 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
     }
 
     if (Q.dh != nullptr)
-        add_adapters<uint16_t, 4>(Q.A, Q.dh, false, t0 + wn * 64, Q.T, lane, [&](int32_t k, int f) {
-            const int64_t c = c0 + wm * 128 + f * 32 + sub;
+        add_adapters<uint16_t, MF>(Q.A, Q.dh, false, t0 + wn * 64, Q.T, lane, [&](int32_t k, int f) {
+            const int64_t c = c0 + wm * WM + f * 32 + sub;
             return Q.at + ((int64_t)k * Q.cols + (c < Q.cols ? c : Q.cols - 1)) * Q.A.max_rank;
         }, acc);
 
@@ -128,10 +133,10 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
         const int64_t t = t0 + wn * 64 + n * 32 + sub;
         if (t >= Q.T) continue;
 #pragma unroll
-        for (int f = 0; f < 4; ++f)
+        for (int f = 0; f < MF; ++f)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const int64_t c = c0 + wm * 128 + f * 32 + g * 8 + hh * 4;
+                const int64_t c = c0 + wm * WM + f * 32 + g * 8 + hh * 4;
                 if (c >= Q.cols) continue;                 // columns come in eights
                 uint16_t* __restrict__ const o = Q.dX + t * Q.ldx + c;
                 uint32_t v[4];
