@@ -31,28 +31,34 @@ __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkArgs Q1, const 
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
         const int32_t t = Q.place[slot * GROUP + n * 16 + sub];
-        xp[n] = static_cast<const uint16_t*>(Q.X) + (int64_t)(t < 0 ? some : t) * Q.ld + q * 16;
+        xp[n] = static_cast<const uint16_t*>(Q.X) + (int64_t)(t < 0 ? some : t) * Q.ld + q * 8;
     }
     const uint16_t* ap[RF];
 #pragma unroll
     for (int f = 0; f < RF; ++f) {
         const int32_t r = f * 16 + sub;
-        ap[f] = static_cast<const uint16_t*>(Q.a) + ((int64_t)k * Q.A.max_rank + (r < rank ? r : 0)) * Q.lda + q * 16;
+        ap[f] = static_cast<const uint16_t*>(Q.a) + ((int64_t)k * Q.A.max_rank + (r < rank ? r : 0)) * Q.lda + q * 8;
     }
     f32x4 acc[RF][4] = {};
     if (rank > 0) {
-        // 64 columns a step, in two instructions each: a quarter's sixteen lie side by side, so that a row's cache line is read at once
+        // 64 columns, a row's cache line, in two instructions each
         const uint4 none = make_uint4(0u, 0u, 0u, 0u);
         for (int32_t s = s0 + wave; s < s1; s += 4) {
             uint4 a[2][RF], b[2][4];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const bool in = s * 64 + q * 16 + u * 8 < Q.width;
-                const int64_t c = in ? s * 64 + u * 8 : 0;
+                const bool in = s * 64 + u * 32 + q * 8 < Q.width;
+                const int64_t c = in ? s * 64 + u * 32 : -q * 8;          // past the end the row's start, counted as zeros
 #pragma unroll
-                for (int n = 0; n < 4; ++n) b[u][n] = in ? *reinterpret_cast<const uint4*>(xp[n] + c) : none;
+                for (int n = 0; n < 4; ++n) b[u][n] = *reinterpret_cast<const uint4*>(xp[n] + c);
 #pragma unroll
-                for (int f = 0; f < RF; ++f) a[u][f] = in ? *reinterpret_cast<const uint4*>(ap[f] + c) : none;
+                for (int f = 0; f < RF; ++f) {
+                    a[u][f] = *reinterpret_cast<const uint4*>(ap[f] + c);
+                    if (!in) a[u][f] = none;
+                }
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+                    if (!in) b[u][n] = none;
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u)

@@ -107,17 +107,18 @@ __global__ __launch_bounds__(OUTER_THREADS) void outer_tiles_kernel(const OuterA
     const int32_t rank = adapter_rank(Q.A, k), n = Q.count[k], p0 = Q.first[k];
     const int64_t col = c0 + sub * 4;
     f32x4 acc[4][RF] = {};
-    if (r0 < rank) {
+    if (r0 < rank && n > 0) {
+        // past the last token, and past the last column, what lies there is read again and counted as zeros
+        const int64_t at_col = col < Q.width ? col : 0;
         auto tokens_of = [&](int32_t i0, uint2 (&x)[8]) {
-            const int32_t at = i0 + q * 8;
-            int32_t t[8] = {-1, -1, -1, -1, -1, -1, -1, -1};
-            if (at < n) {                                   // a slot's places are all written
-                const int4 a = *reinterpret_cast<const int4*>(Q.place + p0 + at), b = *reinterpret_cast<const int4*>(Q.place + p0 + at + 4);
-                t[0] = a.x; t[1] = a.y; t[2] = a.z; t[3] = a.w; t[4] = b.x; t[5] = b.y; t[6] = b.z; t[7] = b.w;
-            }
+            const int32_t at = i0 + q * 8 < n ? i0 + q * 8 : 0;           // a slot's places are all written
+            const int4 a = *reinterpret_cast<const int4*>(Q.place + p0 + at), b = *reinterpret_cast<const int4*>(Q.place + p0 + at + 4);
+            const int32_t t[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const uint2*>(Q.right + (int64_t)(t[j] < 0 ? t[0] : t[j]) * Q.ld + at_col);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                x[j] = t[j] >= 0 && col < Q.width ? *reinterpret_cast<const uint2*>(Q.right + (int64_t)t[j] * Q.ld + col) : make_uint2(0u, 0u);
+                if (i0 + q * 8 + j >= n || col >= Q.width) x[j] = make_uint2(0u, 0u);
         };
         uint2 x[8], next[8];
         tokens_of(wave * 32, x);
@@ -128,7 +129,7 @@ __global__ __launch_bounds__(OUTER_THREADS) void outer_tiles_kernel(const OuterA
 #pragma unroll
                 for (int f = 0; f < RF; ++f) {
                     const int32_t r = r0 + f * 16 + sub;
-                    b[m][f] = r < rank ? *reinterpret_cast<const uint4*>(Q.planes + ((int64_t)m * Q.A.max_rank + r) * Q.places + p0 + i0 + q * 8) : make_uint4(0u, 0u, 0u, 0u);
+                    b[m][f] = *reinterpret_cast<const uint4*>(Q.planes + ((int64_t)m * Q.A.max_rank + (r < rank ? r : 0)) * Q.places + p0 + i0 + q * 8);
                 }
             tokens_of(i0 + 256, next);
 #pragma unroll
@@ -224,6 +225,11 @@ __device__ __forceinline__ void add_adapter8(const AdapterArgs& A, const float* 
     for (int j = 0; j < 8; ++j) v[j] += sum[j];
 }
 
+__device__ __forceinline__ void skip_row(const PackArgs& P, int64_t row, int64_t col, float (&w)[8]) {
+    if (P.w_f32 != 0) load8(static_cast<const float*>(P.W) + row * P.ld + col, w);
+    else load8(static_cast<const uint16_t*>(P.W) + row * P.ld + col, w);
+}
+
 // An octet of one row as fp32 weights (rounded nowhere but by the multiply-add).
 __device__ __forceinline__ void weight_octet(const PackArgs& P, int64_t row, int64_t col, const uint16_t* __restrict__ trits_of, float (&w)[8]) {
     const int64_t rb = row / P.R_u, lrow = row - rb * P.R_u;
@@ -231,11 +237,7 @@ __device__ __forceinline__ void weight_octet(const PackArgs& P, int64_t row, int
     const int64_t u = rb * P.n_chunks + j;
     int64_t base;
     const int a = pk_action(P, u, base);
-    if (a == 0) {
-        if (P.w_f32 != 0) load8(static_cast<const float*>(P.W) + row * P.ld + col, w);
-        else load8(static_cast<const uint16_t*>(P.W) + row * P.ld + col, w);
-        return;
-    }
+    if (a == 0) return skip_row(P, row, col, w);
     const int64_t g = u * P.R_u + lrow;
     const float s = P.scale[g], of = a >= 5 ? 0.0f : P.offset[g];
     const uint4 f = octet_fields(a, P.codes + base + lrow * pk_bytes_per_group(a, P.G), o, trits_of);
@@ -335,13 +337,72 @@ __device__ __forceinline__ void turn(const PackArgs& P, int32_t K, uint16_t* __r
     const int64_t r0 = (block - cb * row_blocks) * 256 + (threadIdx.x & 31) * 8, col = cb * 64 + (threadIdx.x >> 5) * 8;
     if (col >= P.cols || r0 >= K) return;
     uint32_t v[8][4];
+    const uint32_t R_u = (uint32_t)P.R_u, rb = (uint32_t)r0 / R_u, lrow = (uint32_t)r0 - rb * R_u;
+    if (r0 + 8 <= P.rows && lrow + 8 <= R_u) {              // one unit's rows
+        const uint32_t j = (uint32_t)col / (uint32_t)P.G;
+        const int o = ((int)col - (int)j * P.G) >> 3;
+        const int64_t u = (int64_t)rb * P.n_chunks + j;
+        int64_t base;
+        const int a = pk_action(P, u, base);
+        if (a == 0) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float w0[8] = {}, w1[8] = {};
-        if (r0 + 2 * i < P.rows) weight_octet(P, r0 + 2 * i, col, trits_of, w0);
-        if (r0 + 2 * i + 1 < P.rows) weight_octet(P, r0 + 2 * i + 1, col, trits_of, w1);
+            for (int i = 0; i < 4; ++i) {
+                float w0[8], w1[8];
+                skip_row(P, r0 + 2 * i, col, w0);
+                skip_row(P, r0 + 2 * i + 1, col, w1);
 #pragma unroll
-        for (int m = 0; m < 8; ++m) v[m][i] = f32_to_bf16_bits(w0[m]) | f32_to_bf16_bits(w1[m]) << 16;
+                for (int m = 0; m < 8; ++m) v[m][i] = f32_to_bf16_bits(w0[m]) | f32_to_bf16_bits(w1[m]) << 16;
+            }
+        } else {
+            const int32_t nb = (int32_t)pk_bytes_per_group(a, P.G);
+            const uint8_t* const first = P.codes + base + (int64_t)lrow * nb;
+            float sc[8], of[8];
+            __builtin_memcpy(sc, P.scale + u * P.R_u + lrow, 32);
+            __builtin_memcpy(of, P.offset + u * P.R_u + lrow, 32);
+            uint4 f[8];
+            auto rows = [&](auto octet) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] = octet(first + i * nb);
+            };
+            switch (a) {
+                case 1: rows([&](const uint8_t* p) { uint2 q; __builtin_memcpy(&q, p + o * 8, 8); return fields8(q.x, q.y); }); break;
+                case 2: rows([&](const uint8_t* p) { uint32_t q; __builtin_memcpy(&q, p + o * 4, 4); return fields4(q); }); break;
+                case 3: rows([&](const uint8_t* p) { return octet_fields(3, p, o, trits_of); }); break;
+                case 4: rows([&](const uint8_t* p) { uint16_t q; __builtin_memcpy(&q, p + o * 2, 2); return fields2(q); }); break;
+                case 5: rows([&](const uint8_t* p) { return fields2(octet_trits(p, o, trits_of) & 0xffffu); }); break;
+                default: rows([&](const uint8_t* p) { return fields1(p[o]); }); break;
+            }
+            const float f0 = a == 2 ? 16.0f : (a == 3 ? 8.0f : (a == 4 ? 4.0f : (a == 5 ? 5.0f : 0.0f)));
+            uint32_t m8[8] = {};
+            if (P.mask != nullptr) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) m8[i] = P.mask[(r0 + i) * P.mask_ld + (col >> 3)];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int m = 0; m < 8; ++m) {
+                    uint32_t w[2];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const uint4& g = f[2 * i + k];
+                        const uint32_t pair = (m >> 1) == 0 ? g.x : ((m >> 1) == 1 ? g.y : ((m >> 1) == 2 ? g.z : g.w));
+                        const float q = ((m & 1) != 0 ? __uint_as_float(pair & 0xffff0000u) : __uint_as_float(pair << 16)) - f0;
+                        const float x = fmaf(q, sc[2 * i + k], a >= 5 ? 0.0f : of[2 * i + k]);
+                        w[k] = f32_to_bf16_bits(((m8[2 * i + k] >> m) & 1u) != 0u ? 0.0f : x);
+                    }
+                    v[m][i] = w[0] | w[1] << 16;
+                }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float w0[8] = {}, w1[8] = {};
+            if (r0 + 2 * i < P.rows) weight_octet(P, r0 + 2 * i, col, trits_of, w0);
+            if (r0 + 2 * i + 1 < P.rows) weight_octet(P, r0 + 2 * i + 1, col, trits_of, w1);
+#pragma unroll
+            for (int m = 0; m < 8; ++m) v[m][i] = f32_to_bf16_bits(w0[m]) | f32_to_bf16_bits(w1[m]) << 16;
+        }
     }
 #pragma unroll
     for (int m = 0; m < 8; ++m) *reinterpret_cast<uint4*>(wt + (col + m) * K + r0) = make_uint4(v[m][0], v[m][1], v[m][2], v[m][3]);
