@@ -63,13 +63,11 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
     auto load_b = [&](int i, int32_t k, int buf) { lds_load16(lds + (buf * (GM_M + GM_N) * 8 + GM_M * 8 + i * 256 + wave * 64) * 16, bn[i] + k * GM_K); };
     // Operands of step s (16 of the sum): octet 2 s + hh of a row.
     const uint32_t arow = (wm * WM + sub) * 128, brow = GM_M * 128 + (wn * 64 + sub) * 128;
-    auto read = [&](int buf, int s, bf16x8 (&a)[MF], bf16x8 (&b)[2]) {
+    auto read_one = [&](int buf, int s, int i, bf16x8 (&a)[MF], bf16x8 (&b)[2]) {
         const char* const at = reinterpret_cast<const char*>(tile[buf]);
         const uint32_t o = (uint32_t)((2 * s + hh) ^ (sub & 7)) * 16;
-#pragma unroll
-        for (int f = 0; f < MF; ++f) a[f] = as_bf16x8(*reinterpret_cast<const uint4*>(at + arow + f * 32 * 128 + o));
-#pragma unroll
-        for (int n = 0; n < 2; ++n) b[n] = as_bf16x8(*reinterpret_cast<const uint4*>(at + brow + n * 32 * 128 + o));
+        if (i < 2) b[i] = as_bf16x8(*reinterpret_cast<const uint4*>(at + brow + i * 32 * 128 + o));
+        else a[i - 2] = as_bf16x8(*reinterpret_cast<const uint4*>(at + arow + (i - 2) * 32 * 128 + o));
     };
 
     const int32_t n_k = Q.K / GM_K;
@@ -87,34 +85,35 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
         __syncthreads();
         bf16x8 a[2][MF], b[2][2];
-        read(0, 0, a[0], b[0]);
+#pragma unroll
+        for (int i = 0; i < MF + 2; ++i) read_one(0, 0, i, a[0], b[0]);
         int buf = 0;
         for (int32_t k = 0; k < n_k; ++k) {
             const int next = buf == 2 ? 0 : buf + 1, then = next == 2 ? 0 : next + 1;
             const int32_t k2 = k + 2 < n_k ? k + 2 : n_k - 1;       // past the end: again the last, into a buffer that nobody reads
+            // Behind every matrix instruction one or two operands of the next step are read, and in the first three steps a load is
+            // asked for: put ahead of the instructions they would leave the matrix unit idle for half of the time.
+            constexpr int EACH = (LOADS + 2) / 3, MM = MF * 2, READS = (MF + 2 + MM - 2) / (MM - 1);
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                // all loads in the first three steps
-                if (s < 3) {
-                    constexpr int EACH = (LOADS + 2) / 3;
 #pragma unroll
-                    for (int i = 0; i < EACH; ++i) {
-                        const int j = s * EACH + i;
-                        if (j >= LOADS) break;
+                for (int i = 0; i < MM; ++i) {
+                    acc[i >> 1][i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s & 1][i >> 1], b[s & 1][i & 1], acc[i >> 1][i & 1], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (s == 3 && i == 0) {
+                        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LOADS) : "memory");       // the next buffer's loads are done, this one's reads too
+                        __builtin_amdgcn_s_barrier();
+                        asm volatile("" ::: "memory");
+                    }
+#pragma unroll
+                    for (int r = i * READS; r < (i + 1) * READS && r < MF + 2; ++r) read_one(s < 3 ? buf : next, s < 3 ? s + 1 : 0, r, a[(s + 1) & 1], b[(s + 1) & 1]);
+                    const int j = s * EACH + i;
+                    if (s < 3 && i < EACH && j < LOADS) {
                         if (j < GM_M / 32) load_a(j, k2, then);
                         else load_b(j - GM_M / 32, k2, then);
                     }
-                    read(buf, s + 1, a[(s + 1) & 1], b[(s + 1) & 1]);
-                } else {
-                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LOADS) : "memory");       // the next buffer's loads are done, this one's reads too
-                    __builtin_amdgcn_s_barrier();
-                    asm volatile("" ::: "memory");
-                    read(next, 0, a[0], b[0]);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-#pragma unroll
-                for (int f = 0; f < MF; ++f)
-#pragma unroll
-                    for (int n = 0; n < 2; ++n) acc[f][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s & 1][f], b[s & 1][n], acc[f][n], 0, 0, 0);
             }
             buf = next;
         }
