@@ -73,12 +73,14 @@ __global__ __launch_bounds__(256) void outer_kernel(const XT* __restrict__ right
     }
 }
 
-// The same for bfloat16 on the matrix instructions: 64 columns of the right side by up to 64 ranks, the sum over an adapter's places 32 at a time,
-// shared by eight wavefronts.  The sum runs over tokens, and an operand wants eight consecutive tokens of one column in a lane, while
+// The same for bfloat16 on the matrix instructions: up to 64 ranks by 64 columns of the right side a wavefront, the sum over an adapter's places 32 at a
+// time.  Eight wavefronts share the places (PARTS = 8, many tokens an adapter) or four pairs do, a pair's two with 64 columns each.  The sum runs over tokens, and an operand wants eight consecutive tokens of one column in a lane, while
 // a token's columns lie side by side: a lane reads eight tokens by four columns and pairs tokens up in registers, which gives one
 // operand for each of its four columns (every fourth column shares an instruction, as in the reconstruction).  The left side comes
-// transposed and as three bfloat16 terms, so products are exact to fp32.  Bound by reading X and dY once.
-constexpr int OUTER_COLS = 64, OUTER_THREADS = 512;
+// transposed and as three bfloat16 terms, so products are exact to fp32.  Bound by latency: a wavefront has a
+// step's operands on their way while it multiplies the step before, and the tokens of the step after.
+constexpr int OUTER_THREADS = 512;
+inline int outer_parts(int64_t T, int32_t n) { return T >= (int64_t)512 * n ? 8 : 4; }        // 2048 tokens of one adapter: 43 us by eight, 81 by pairs; 700 of sixteen: 20 and 13
 struct OuterArgs {
     const uint16_t* right;     // [T][ld], on 16 bytes, columns in eights readable
     int64_t ld, width;
@@ -93,9 +95,10 @@ struct OuterArgs {
     int64_t tiles;             // of OUTER_COLS columns
 };
 
-template <int RF>
+template <int RF, int OUTER_PARTS>
 __global__ __launch_bounds__(OUTER_THREADS) void outer_tiles_kernel(const OuterArgs Q1, const OuterArgs Q2, const int64_t first2) {
-    __shared__ float red[4][RF * 16][OUTER_COLS + 4];
+    constexpr int OUTER_COLS = 512 / OUTER_PARTS;
+    __shared__ float red[OUTER_PARTS / 2][RF * 16][OUTER_COLS + 4];
     const OuterArgs& Q = blockIdx.x < first2 ? Q1 : Q2;
     const int64_t block = blockIdx.x < first2 ? blockIdx.x : blockIdx.x - first2;
     const int32_t groups = (Q.A.max_rank + 63) / 64;
@@ -103,35 +106,43 @@ __global__ __launch_bounds__(OUTER_THREADS) void outer_tiles_kernel(const OuterA
     const int64_t rest = block - k * Q.tiles * groups;
     const int32_t r0 = (int32_t)(rest / Q.tiles) * 64;
     const int64_t c0 = (rest - rest / Q.tiles * Q.tiles) * OUTER_COLS;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
+    const int part = (threadIdx.x >> 6) * OUTER_PARTS / 8, side = OUTER_PARTS == 8 ? 0 : ((threadIdx.x >> 6) & 1) * 64, lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
     const int32_t rank = adapter_rank(Q.A, k), n = Q.count[k], p0 = Q.first[k];
-    const int64_t col = c0 + sub * 4;
+    const int64_t col = c0 + side + sub * 4;
     f32x4 acc[4][RF] = {};
     if (r0 < rank && n > 0) {
         // past the last token, and past the last column, what lies there is read again and counted as zeros
         const int64_t at_col = col < Q.width ? col : 0;
-        auto tokens_of = [&](int32_t i0, uint2 (&x)[8]) {
+        auto places_of = [&](int32_t i0, int4 (&t)[2]) {
             const int32_t at = i0 + q * 8 < n ? i0 + q * 8 : 0;           // a slot's places are all written
-            const int4 a = *reinterpret_cast<const int4*>(Q.place + p0 + at), b = *reinterpret_cast<const int4*>(Q.place + p0 + at + 4);
-            const int32_t t[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            t[0] = *reinterpret_cast<const int4*>(Q.place + p0 + at);
+            t[1] = *reinterpret_cast<const int4*>(Q.place + p0 + at + 4);
+        };
+        auto operands_of = [&](int32_t i0, const int4 (&p)[2], uint2 (&x)[8], uint4 (&b)[3][RF]) {
+            const int32_t t[8] = {p[0].x, p[0].y, p[0].z, p[0].w, p[1].x, p[1].y, p[1].z, p[1].w};
+            const int32_t at = i0 < n ? i0 : 0;
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const uint2*>(Q.right + (int64_t)(t[j] < 0 ? t[0] : t[j]) * Q.ld + at_col);
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (i0 + q * 8 + j >= n || col >= Q.width) x[j] = make_uint2(0u, 0u);
-        };
-        uint2 x[8], next[8];
-        tokens_of(wave * 32, x);
-        for (int32_t i0 = wave * 32; i0 < n; i0 += 256) {
-            uint4 b[3][RF];
 #pragma unroll
             for (int m = 0; m < 3; ++m)
 #pragma unroll
                 for (int f = 0; f < RF; ++f) {
                     const int32_t r = r0 + f * 16 + sub;
-                    b[m][f] = *reinterpret_cast<const uint4*>(Q.planes + ((int64_t)m * Q.A.max_rank + (r < rank ? r : 0)) * Q.places + p0 + i0 + q * 8);
+                    b[m][f] = *reinterpret_cast<const uint4*>(Q.planes + ((int64_t)m * Q.A.max_rank + (r < rank ? r : 0)) * Q.places + p0 + at + q * 8);
                 }
-            tokens_of(i0 + 256, next);
+        };
+        uint2 x[8], next_x[8];
+        uint4 b[3][RF], next_b[3][RF];
+        int4 t[2];
+        places_of(part * 32, t);
+        operands_of(part * 32, t, x, b);
+        places_of((part + OUTER_PARTS) * 32, t);
+        for (int32_t i0 = part * 32; i0 < n; i0 += OUTER_PARTS * 32) {
+            operands_of(i0 + OUTER_PARTS * 32, t, next_x, next_b);
+            places_of(i0 + 2 * OUTER_PARTS * 32, t);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (i0 + q * 8 + j >= n || col >= Q.width) x[j] = make_uint2(0u, 0u);
 #pragma unroll
             for (int m = 0; m < 4; ++m) {
                 uint32_t w[8];
@@ -146,38 +157,42 @@ __global__ __launch_bounds__(OUTER_THREADS) void outer_tiles_kernel(const OuterA
                     for (int p = 2; p >= 0; --p) acc[m][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, as_bf16x8(b[p][f]), acc[m][f], 0, 0, 0);
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = next[j];
+            for (int j = 0; j < 8; ++j) x[j] = next_x[j];
+#pragma unroll
+            for (int m = 0; m < 3; ++m)
+#pragma unroll
+                for (int f = 0; f < RF; ++f) b[m][f] = next_b[m][f];
         }
     }
-    // the upper half of the wavefronts hand theirs to the lower half, until one has all: a fixed order
+    // the upper half of the parts hand theirs to the lower half, until one has all: a fixed order
 #pragma unroll
-    for (int round = 4; round >= 1; round >>= 1) {
-        if (wave >= round && wave < 2 * round) {
+    for (int round = OUTER_PARTS / 2; round >= 1; round >>= 1) {
+        if (part >= round && part < 2 * round) {
 #pragma unroll
             for (int m = 0; m < 4; ++m)
 #pragma unroll
                 for (int f = 0; f < RF; ++f)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) red[wave - round][f * 16 + sub][(4 * q + i) * 4 + m] = acc[m][f][i];
+                    for (int i = 0; i < 4; ++i) red[part - round][f * 16 + sub][side + (4 * q + i) * 4 + m] = acc[m][f][i];
         }
         __syncthreads();
-        if (wave < round) {
+        if (part < round) {
 #pragma unroll
             for (int m = 0; m < 4; ++m)
 #pragma unroll
                 for (int f = 0; f < RF; ++f)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[m][f][i] += red[wave][f * 16 + sub][(4 * q + i) * 4 + m];
+                    for (int i = 0; i < 4; ++i) acc[m][f][i] += red[part][f * 16 + sub][side + (4 * q + i) * 4 + m];
         }
         __syncthreads();
     }
-    if (wave == 0) {
+    if (part == 0) {
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
             for (int f = 0; f < RF; ++f)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) red[0][f * 16 + sub][(4 * q + i) * 4 + m] = acc[m][f][i];
+                for (int i = 0; i < 4; ++i) red[0][f * 16 + sub][side + (4 * q + i) * 4 + m] = acc[m][f][i];
     }
     __syncthreads();
     const float factor = Q.scaled && Q.A.alpha != nullptr ? Q.A.alpha[k] : 1.0f;
@@ -667,14 +682,22 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
             if (status != WINDQ_OK) return status;
             if (outer) {
                 const int32_t groups = (A.max_rank + 63) / 64;
-                OuterArgs O1 = {static_cast<const uint16_t*>(X->data), X->ld, cols, planes_dh, G.slots * GROUP, G.place, G.first, G.count, A, false, false, dA, (cols + OUTER_COLS - 1) / OUTER_COLS};
-                OuterArgs O2 = {dYv, Q.ldy, rows, planes_h, G.slots * GROUP, G.place, G.first, G.count, A, true, true, dB, (rows + OUTER_COLS - 1) / OUTER_COLS};
+                const int parts = outer_parts(T, A.n);
+                const int64_t by = 512 / parts;
+                OuterArgs O1 = {static_cast<const uint16_t*>(X->data), X->ld, cols, planes_dh, G.slots * GROUP, G.place, G.first, G.count, A, false, false, dA, tokens_in(cols, by)};
+                OuterArgs O2 = {dYv, Q.ldy, rows, planes_h, G.slots * GROUP, G.place, G.first, G.count, A, true, true, dB, tokens_in(rows, by)};
                 const int64_t n1 = (int64_t)A.n * groups * O1.tiles, n2 = (int64_t)A.n * groups * O2.tiles;
                 const int32_t RF = A.max_rank >= 64 ? 4 : shrink_ranks(A.max_rank) / 16;
-                if (RF == 1) WINDQ_LAUNCH(n1 + n2, OUTER_THREADS, outer_tiles_kernel<1>, O1, O2, n1);
-                else if (RF == 2) WINDQ_LAUNCH(n1 + n2, OUTER_THREADS, outer_tiles_kernel<2>, O1, O2, n1);
-                else if (RF == 3) WINDQ_LAUNCH(n1 + n2, OUTER_THREADS, outer_tiles_kernel<3>, O1, O2, n1);
-                else WINDQ_LAUNCH(n1 + n2, OUTER_THREADS, outer_tiles_kernel<4>, O1, O2, n1);
+#define WINDQ_OUTER(F)                                                                                    \
+    do {                                                                                                  \
+        if (parts == 8) WINDQ_LAUNCH(n1 + n2, OUTER_THREADS, (outer_tiles_kernel<F, 8>), O1, O2, n1);     \
+        else WINDQ_LAUNCH(n1 + n2, OUTER_THREADS, (outer_tiles_kernel<F, 4>), O1, O2, n1);                \
+    } while (0)
+                if (RF == 1) WINDQ_OUTER(1);
+                else if (RF == 2) WINDQ_OUTER(2);
+                else if (RF == 3) WINDQ_OUTER(3);
+                else WINDQ_OUTER(4);
+#undef WINDQ_OUTER
             }
         } else {
             AdapterArgs B = A;
