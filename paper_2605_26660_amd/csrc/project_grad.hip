@@ -587,8 +587,8 @@ GradWs grad_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t n, 
     w.owner = take((size_t)slots * 4);
     w.first = take((size_t)n * 4);
     w.count = take((size_t)n * 4);
-    w.part = take(bf && n > 0 ? (size_t)shrink_splits(slots, wide) * (size_t)slots * GROUP * (size_t)shrink_ranks(max_rank) * 4 : 0);
-    w.part2 = take(bf && n > 0 ? (size_t)shrink_splits(slots, wide) * (size_t)slots * GROUP * (size_t)shrink_ranks(max_rank) * 4 : 0);
+    w.part = take(bf && n > 0 ? (size_t)shrink_pieces(slots, wide) * GROUP * (size_t)shrink_ranks(max_rank) * 4 : 0);
+    w.part2 = take(bf && n > 0 ? (size_t)shrink_pieces(slots, wide) * GROUP * (size_t)shrink_ranks(max_rank) * 4 : 0);
     w.planes_h = take(bf && n > 0 ? (size_t)slots * GROUP * (size_t)max_rank * 6 : 0);
     w.planes_dh = take(bf && n > 0 ? (size_t)slots * GROUP * (size_t)max_rank * 6 : 0);
     w.wt = take(bf && T >= TURN_FROM ? (size_t)gemm_cols(cols) * (size_t)gemm_k(rows) * 2 : 0);

@@ -67,6 +67,12 @@ inline int32_t shrink_splits(int64_t slots, int64_t width) {
     if (s > width / 256) s = width / 256;
     return (int32_t)(s < 1 ? 1 : (s > 32 ? 32 : s));
 }
+// Most slots x splits of as many slots or fewer: a workspace sized for more tokens does for fewer.
+inline int64_t shrink_pieces(int64_t slots, int64_t width) {
+    const int64_t splits = width / 256 < 32 ? width / 256 : 32;
+    const int64_t most = slots * splits < 512 ? slots * splits : 512;
+    return most > slots ? most : slots;
+}
 
 #ifdef __HIPCC__
 
