@@ -967,8 +967,10 @@ def windq_project_grad(packed: Packed | None, dY: torch.Tensor, X: torch.Tensor 
         raise WindqError(WINDQ_EINVAL, "windq_project_grad")
     shape = adapters if packed is None else packed
     _check_side(packed, adapters, adapter_of, h, T, "windq_project_grad")
-    if (adapters is not None) != (X is not None) or (X is not None and (X.dtype != dY.dtype or tuple(X.shape) != (T, shape.cols))) or dY.shape[1] != shape.rows:
+    if (adapters is not None) != (X is not None) or (X is not None and tuple(X.shape) != (T, shape.cols)) or dY.shape[1] != shape.rows:
         raise WindqError(WINDQ_ESHAPE, "windq_project_grad")
+    if X is not None and X.dtype != dY.dtype:
+        raise WindqError(WINDQ_EDTYPE, "windq_project_grad")
     dx, da, db = (None, None, None) if outs is None else outs
     _require_cuda(dx, da, db)
     if want_dx and dx is None:

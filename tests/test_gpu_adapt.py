@@ -1,0 +1,102 @@
+"""The three calls together, as the example runs them; adapters beyond 2^31 values; refusals of the binding."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_26660_amd import adapt
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def test_adapters_trained_through_a_packed_matrix_repair_it_and_serve():
+    first, last, differs = adapt.run(rows=512, cols=768, chunk_w=64, steps=120, tokens=600, rank=16)
+    assert np.all(np.isfinite(first + last))
+    # a kind's activations lie in rank / 2 directions up to a hundredth of their energy; an adapter of that rank can repair all the others
+    assert all(y < 0.25 * x for x, y in zip(first, last)), (first, last)
+    assert differs < 3 * 2.0 ** -8                       # three bfloat16 roundings of values at most the largest one
+
+
+def test_the_example_gives_the_same_numbers_again():
+    assert adapt.run(rows=256, cols=256, chunk_w=64, steps=3, tokens=300) == adapt.run(rows=256, cols=256, chunk_w=64, steps=3, tokens=300)
+
+
+def test_adapters_of_more_than_two_to_the_31_values(windq):
+    """The last of 1100 adapters of up to 128 ranks by 16384 columns: its offsets pass 32 bits in every table."""
+    n, r, rows, cols, T = 1100, 128, 64, 16384, 130
+    g = torch.Generator().manual_seed(3)
+    a = torch.empty(n, r, cols, dtype=torch.bfloat16, device=DEV)
+    b = torch.empty(n, rows, r, dtype=torch.bfloat16, device=DEV)
+    a[n - 1] = (torch.randn(r, cols, generator=g) / 128).to(DEV)
+    b[n - 1] = (0.05 * torch.randn(rows, r, generator=g)).to(DEV)
+    ranks = torch.zeros(n, dtype=torch.int32, device=DEV)
+    ranks[n - 1] = r
+    ad = windq.Adapters(a, b, None, ranks)
+    W = torch.zeros(rows, cols, dtype=torch.bfloat16, device=DEV)
+    U, R_u = windq.n_units(rows, cols, 128, 0)
+    action = torch.zeros(U, dtype=torch.uint8)
+    off = windq.windq_plan_layout(action, R_u, 128).to(DEV)
+    z = torch.zeros(U * R_u, device=DEV)
+    packed = windq.Packed(W, 128, 0, action.to(DEV), off, torch.zeros(16, dtype=torch.uint8, device=DEV), z, z)
+    X = torch.randn(T, cols, generator=g).to(torch.bfloat16).to(DEV)
+    dY = torch.randn(T, rows, generator=g).to(torch.bfloat16).to(DEV)
+    x, dy = X.double().cpu(), dY.double().cpu()
+    av, bv = a[n - 1].double().cpu(), b[n - 1].double().cpu()
+
+    def near(got, want, mag, rounded):                   # the bounds of the products' own tests
+        tol = 16 * 2.0 ** -24 * mag + (2.0 ** -16 * mag + 2.0 ** -8 * 1.001 * want.abs() if rounded else 0.0)
+        assert torch.all((got.double().cpu() - want).abs() <= tol + 1e-300)
+
+    for t in (3, T):                                     # a token at a time, and by tiles of an adapter's tokens
+        of = torch.full((t,), n - 1, dtype=torch.int32, device=DEV)
+        y = windq.windq_project(packed, X[:t], ad, of)
+        h, hm = x[:t] @ av.T, x[:t].abs() @ av.abs().T
+        near(y, h @ bv.T, hm @ bv.abs().T, True)
+        dx, da, db = windq.windq_project_grad(packed, dY[:t], X[:t], ad, of)
+        d, dm = dy[:t] @ bv, dy[:t].abs() @ bv.abs()
+        near(dx, d @ av, dm @ av.abs(), True)
+        near(da[n - 1], d.T @ x[:t], dm.T @ x[:t].abs(), False)
+        near(db[n - 1], dy[:t].T @ h, dy[:t].abs().T @ hm, False)
+        assert not da[:n - 1].any() and not db[:n - 1].any()
+        del dx, da, db
+
+
+def test_the_binding_refuses(windq):
+    bf, f32 = torch.bfloat16, torch.float32
+    rows, cols, G, T = 64, 128, 64, 5
+    W = torch.randn(rows, cols, dtype=f32, device=DEV).to(bf)
+    packed = adapt.pack(W, torch.ones(cols, device=DEV), G)
+    x, dy = torch.zeros(T, cols, dtype=bf, device=DEV), torch.zeros(T, rows, dtype=bf, device=DEV)
+    a, b = torch.zeros(2, 8, cols, dtype=bf, device=DEV), torch.zeros(2, rows, 8, dtype=bf, device=DEV)
+    ad, of = windq.Adapters(a, b), torch.zeros(T, dtype=torch.int32, device=DEV)
+
+    def refused(status, f, *p, **q):
+        with pytest.raises(windq.WindqError) as e:
+            f(*p, **q)
+        assert e.value.status == status
+
+    shape, dtype, space = windq.WINDQ_ESHAPE, windq.WINDQ_EDTYPE, windq.WINDQ_EWORKSPACE
+    act, off, codes, scale, offset, _ = packed.tensors
+    refused(shape, windq.Packed, W, 48, 0, act, off, codes, scale, offset)
+    refused(shape, windq.Packed, W, G, 0, act[:1], off, codes, scale, offset)
+    refused(dtype, windq.Packed, W, G, 0, act.int(), off, codes, scale, offset)
+    refused(shape, windq.Packed, W, G, 0, act, off, codes, scale[:-1], offset)
+    refused(dtype, windq.Adapters, a, b.float())
+    refused(shape, windq.Adapters, a, b[:1])
+    refused(shape, windq.Adapters, a, b, torch.ones(3, device=DEV))
+    refused(dtype, windq.Adapters, a, b, None, torch.ones(2, device=DEV))
+    refused(shape, windq.windq_project, packed, x, ad)                                       # whose tokens they are is not said
+    refused(shape, windq.windq_project, packed, x, ad, of[:-1])
+    refused(dtype, windq.windq_project, packed, x, ad, of.long())
+    refused(dtype, windq.windq_project, packed, x.float(), ad, of)
+    refused(shape, windq.windq_project, packed, x, ad, of, torch.zeros(T, 16, device=DEV))
+    refused(shape, windq.windq_project, packed, x[:, :64])
+    refused(shape, windq.windq_project, packed, x, out=torch.zeros(T, rows + 8, dtype=bf, device=DEV))
+    refused(dtype, windq.windq_project, packed, x, out=torch.zeros(T, rows, device=DEV))
+    refused(space, windq.windq_project, packed, x, ad, of, ws=torch.empty(256, dtype=torch.uint8, device=DEV))
+    refused(space, windq.windq_project_grad, packed, dy, x, ad, of, ws=torch.empty(256, dtype=torch.uint8, device=DEV))
+    refused(shape, windq.windq_project_grad, packed, dy[:, :32], x, ad, of)
+    refused(dtype, windq.windq_project_grad, packed, dy, x.float(), ad, of)
+    refused(shape, windq.windq_project_grad, packed, dy, None, ad, of)
+    refused(windq.WINDQ_EINVAL, windq.windq_project_grad, None, dy)
+    refused(dtype, windq.windq_project_grad, packed, dy, x, ad, of, outs=(None, torch.zeros_like(a), None))
