@@ -23,13 +23,13 @@ __global__ __launch_bounds__(256) void planes_kernel(const float* __restrict__ X
 }
 
 // ------------------------------------------------------------------------------------------------ the product, any shape
-// A workgroup has 16 RF rows and 16 NT tokens; its eight wavefronts share the chunks among them and add up through LDS.  A
+// A workgroup has 16 rows and 16 NT tokens; its eight wavefronts share the chunks among them and add up through LDS.  A
 // wavefront's rows are the M side of 16x16x32 matrix instructions: lane l has row l mod 16 and, of every chunk, the octets
 // of its quarter l / 16.  Which columns the four quarters pair up is free as long as X's operand does the same, so a lane's octets lie next to
 // each other and its codes are contiguous bytes.  sum_c x comes from the same instructions with ones for weights (under a mask: ones
 // where the weight is kept).
 constexpr int PJ_WAVES = 8;
-constexpr int64_t PROJECT_FEW = 64;                       // tokens up to which this kernel is the faster one
+constexpr int64_t PROJECT_FEW = 64;                       // tokens up to which this kernel, or that for few tokens, is the faster one
 
 struct ProjectArgs {
     PackArgs P;
@@ -50,19 +50,19 @@ __device__ __forceinline__ void store_y(YT* __restrict__ p, float v) {
     else *p = (uint16_t)f32_to_bf16_bits(v);
 }
 
-template <typename YT, int RF, int NT, bool MASK>
+template <typename YT, int NT, bool MASK>
 __global__ __launch_bounds__(PJ_WAVES * 64) void project_kernel(const ProjectArgs Q) {
     constexpr int NP = sizeof(YT) == 4 ? 3 : 1;
-    __shared__ float red[PJ_WAVES][RF * NT * 4][64];
+    __shared__ float red[PJ_WAVES][NT * 4][64];
     __shared__ uint16_t trits_of[256];
     if (threadIdx.x < 256) trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
     __syncthreads();
     const PackArgs& P = Q.P;
     const int32_t G = P.G, O = G >> 3, S = (O + 3) >> 2;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
-    const int64_t row_blocks = (P.rows + RF * 16 - 1) / (RF * 16);
+    const int64_t row_blocks = (P.rows + 15) / 16;
     const int64_t tb = blockIdx.x / row_blocks;
-    const int64_t row0 = (blockIdx.x - tb * row_blocks) * (RF * 16), t0 = tb * (NT * 16);
+    const int64_t row0 = (blockIdx.x - tb * row_blocks) * 16, t0 = tb * (NT * 16);
 
     const uint16_t* xp[NT];
 #pragma unroll
@@ -70,35 +70,22 @@ __global__ __launch_bounds__(PJ_WAVES * 64) void project_kernel(const ProjectArg
         const int64_t t = t0 + n * 16 + sub;
         xp[n] = Q.X + (t < Q.T ? t : Q.T - 1) * Q.ldx;
     }
-    int64_t row[RF], rb[RF], lrow[RF];
-#pragma unroll
-    for (int f = 0; f < RF; ++f) {
-        row[f] = row0 + f * 16 + sub;
-        if (row[f] >= P.rows) row[f] = P.rows - 1;         // computed for nothing, stored by nobody
-        rb[f] = row[f] / P.R_u;
-        lrow[f] = row[f] - rb[f] * P.R_u;
-    }
+    const int64_t row = row0 + sub < P.rows ? row0 + sub : P.rows - 1;        // past the last one: computed for nothing, stored by nobody
+    const int64_t rb = row / P.R_u, lrow = row - rb * P.R_u;
     const uint4 none = make_uint4(0u, 0u, 0u, 0u);
     const uint32_t one = 0x3f803f80u;
     const uint4 ones = make_uint4(one, one, one, one);
 
-    f32x4 tot[RF][NT] = {};
+    f32x4 tot[NT] = {};
     for (int32_t j = wave; j < P.n_chunks; j += PJ_WAVES) {
-        int act[RF];
-        const uint8_t* codes[RF];
-        float alpha[RF], beta[RF];
-        bool wide = false;                                  // fp32 skip weights among the rows
-#pragma unroll
-        for (int f = 0; f < RF; ++f) {
-            const int64_t u = rb[f] * P.n_chunks + j;
-            int64_t base;
-            act[f] = pk_action(P, u, base);
-            codes[f] = P.codes + base + lrow[f] * pk_bytes_per_group(act[f], G);
-            const int64_t g = u * P.R_u + lrow[f];
-            pk_affine(act[f], P.scale[g], P.offset[g], NP == 3, alpha[f], beta[f]);
-            wide |= act[f] == 0 && P.w_f32 != 0;
-        }
-        f32x4 acc[RF][NT] = {}, xs[MASK ? RF : 1][NT] = {};
+        const int64_t u = rb * P.n_chunks + j, g = u * P.R_u + lrow;
+        int64_t base;
+        const int act = pk_action(P, u, base);
+        const uint8_t* const codes = P.codes + base + lrow * pk_bytes_per_group(act, G);
+        float alpha, beta;
+        pk_affine(act, P.scale[g], P.offset[g], NP == 3, alpha, beta);
+        const bool wide = act == 0 && P.w_f32 != 0;         // fp32 skip weights
+        f32x4 acc[NT] = {}, xs[NT] = {};
         for (int32_t s = 0; s < S; ++s) {
             const int32_t o = q * S + s;
             const bool valid = o < O;
@@ -108,63 +95,53 @@ __global__ __launch_bounds__(PJ_WAVES * 64) void project_kernel(const ProjectArg
             for (int p = 0; p < NP; ++p)
 #pragma unroll
                 for (int n = 0; n < NT; ++n) b[p][n] = as_bf16x8(valid ? *reinterpret_cast<const uint4*>(xp[n] + p * Q.plane + col) : none);
-#pragma unroll
-            for (int f = 0; f < RF; ++f) {
-                uint4 w = none, k = ones;
-                if (valid) {
-                    w = act[f] == 0 ? skip_octet(P, row[f], col, 0) : octet_fields(act[f], codes[f], o, trits_of);
-                    if (NP == 3 && act[f] != 0) w = centred(w, pk_centre(act[f]));
-                    if (MASK && act[f] != 0) {
-                        k = keep_words(P.mask[row[f] * P.mask_ld + (col >> 3)]);
-                        w = and4(w, k);
-                        k = and4(k, ones);
-                    }
+            uint4 w = none, k = ones;
+            if (valid) {
+                w = act == 0 ? skip_octet(P, row, col, 0) : octet_fields(act, codes, o, trits_of);
+                if (NP == 3 && act != 0) w = centred(w, pk_centre(act));
+                if (MASK && act != 0) {
+                    k = keep_words(P.mask[row * P.mask_ld + (col >> 3)]);
+                    w = and4(w, k);
+                    k = and4(k, ones);
                 }
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int p = NP - 1; p >= 0; --p) {
-                        acc[f][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), b[p][n], acc[f][n], 0, 0, 0);
-                        if (MASK || f == 0) xs[MASK ? f : 0][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(k), b[p][n], xs[MASK ? f : 0][n], 0, 0, 0);
-                    }
             }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p) {
+                    acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), b[p][n], acc[n], 0, 0, 0);
+                    xs[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(k), b[p][n], xs[n], 0, 0, 0);
+                }
             if (__any(wide)) {
+                for (int term = 1; term < 3; ++term) {
+                    const uint4 more = valid && act == 0 ? skip_octet(P, row, col, term) : none;
 #pragma unroll
-                for (int f = 0; f < RF; ++f)
-                    for (int term = 1; term < 3; ++term) {
-                        const uint4 w = valid && act[f] == 0 ? skip_octet(P, row[f], col, term) : none;
+                    for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
-#pragma unroll
-                            for (int p = 0; p < NP; ++p)
-                                if (p + term < 3) acc[f][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), b[p][n], acc[f][n], 0, 0, 0);
-                    }
+                        for (int p = 0; p < NP; ++p)
+                            if (p + term < 3) acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(more), b[p][n], acc[n], 0, 0, 0);
+                }
             }
         }
 #pragma unroll
-        for (int f = 0; f < RF; ++f) {
+        for (int i = 0; i < 4; ++i) {
+            const float al = __shfl(alpha, 4 * q + i, 64), be = __shfl(beta, 4 * q + i, 64);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float al = __shfl(alpha[f], 4 * q + i, 64), be = __shfl(beta[f], 4 * q + i, 64);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) tot[f][n][i] = fmaf(al, acc[f][n][i], fmaf(be, xs[MASK ? f : 0][n][i], tot[f][n][i]));
-            }
+            for (int n = 0; n < NT; ++n) tot[n][i] = fmaf(al, acc[n][i], fmaf(be, xs[n][i], tot[n][i]));
         }
     }
 #pragma unroll
-    for (int f = 0; f < RF; ++f)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) red[wave][(f * NT + n) * 4 + i][lane] = tot[f][n][i];
+        for (int i = 0; i < 4; ++i) red[wave][n * 4 + i][lane] = tot[n][i];
     __syncthreads();
     YT* __restrict__ const Y = static_cast<YT*>(Q.Y);
-    for (int e = threadIdx.x; e < RF * NT * 256; e += PJ_WAVES * 64) {
+    for (int e = threadIdx.x; e < NT * 256; e += PJ_WAVES * 64) {
         // row by row within a token, so that neighbouring lanes write neighbouring rows
-        const int r = e & 15, n = (e >> 4) % (NT * 16), f = (e >> 4) / (NT * 16);
-        const int64_t y = row0 + f * 16 + r, t = t0 + n;
+        const int r = e & 15, n = e >> 4;
+        const int64_t y = row0 + r, t = t0 + n;
         if (y >= P.rows || t >= Q.T) continue;
-        const int slot = (f * NT + (n >> 4)) * 4 + (r & 3), at = (r >> 2) * 16 + (n & 15);
+        const int slot = (n >> 4) * 4 + (r & 3), at = (r >> 2) * 16 + (n & 15);
         float v = 0.0f;
 #pragma unroll
         for (int w = 0; w < PJ_WAVES; ++w) v += red[w][slot][at];
@@ -174,19 +151,21 @@ __global__ __launch_bounds__(PJ_WAVES * 64) void project_kernel(const ProjectArg
     }
 }
 
-template <typename YT, int RF, int NT, bool MASK>
+template <typename YT, int NT, bool MASK>
 int launch_project(const ProjectArgs& Q, hipStream_t st) {
-    const int64_t wgs = ((Q.P.rows + RF * 16 - 1) / (RF * 16)) * ((Q.T + NT * 16 - 1) / (NT * 16));
+    const int64_t wgs = tokens_in(Q.P.rows, 16) * tokens_in(Q.T, NT * 16);
     if (!fits_launch(wgs, PJ_WAVES * 64)) return WINDQ_ESHAPE;
-    project_kernel<YT, RF, NT, MASK><<<dim3((uint32_t)wgs), dim3(PJ_WAVES * 64), 0, st>>>(Q);
+    project_kernel<YT, NT, MASK><<<dim3((uint32_t)wgs), dim3(PJ_WAVES * 64), 0, st>>>(Q);
     return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
 }
 
+// Sixteen tokens a workgroup while that leaves two workgroups a CU at most: their time is latency.  fp32, 1000 x 1056: 77 tokens (315 of them) 35 us,
+// 58 with 64 tokens each; 512 x 512, 64 tokens (128) 12 and 29; bfloat16, 1024 x 1120, 64 tokens (256) 9 and 21.  Else 32, so that a weight
+// is unpacked half as often: bfloat16, 4096 x 4000, 2000 tokens 1863 us, 2041 with 16 each and 1895 with 64.
 template <typename YT, bool MASK>
 int launch_project_any(const ProjectArgs& Q, hipStream_t st) {
-    if (Q.T <= 16) return launch_project<YT, 1, 1, MASK>(Q, st);
-    if (Q.T <= 32) return launch_project<YT, 1, 2, MASK>(Q, st);
-    return launch_project<YT, 1, 4, MASK>(Q, st);
+    if (tokens_in(Q.P.rows, 16) * tokens_in(Q.T, 16) <= 512) return launch_project<YT, 1, MASK>(Q, st);
+    return launch_project<YT, 2, MASK>(Q, st);
 }
 
 int check_packed(const windq_packed* P, PackArgs* A) {
