@@ -39,37 +39,55 @@ __global__ __launch_bounds__(256) void align_kernel(const T* __restrict__ in, in
 }
 
 // ------------------------------------------------------------------------------------------------ dA and dB
-// out = sum over an adapter's tokens of left_t right_t^T.  A lane owns a column of the right side and sixteen ranks.
-template <typename XT>
-__global__ __launch_bounds__(256) void outer_kernel(const XT* __restrict__ right, int64_t ld, int64_t width, const float* __restrict__ left,
-                                                    const AdapterArgs A, const int32_t* __restrict__ place, const int32_t* __restrict__ first,
-                                                    const int32_t* __restrict__ count, bool scaled, bool by_column, float* __restrict__ out) {
-    const int64_t wt = (width + 255) / 256;
+// out = sum over an adapter's tokens of left_t right_t^T.  fp32: a lane owns a column of the right side and sixteen ranks, and has four tokens on
+// their way at a time (bound by their latency: an adapter's tokens are few where calls are small).  Both sums in one launch.
+struct OuterRows {
+    const float* right;        // [T][ld]
+    int64_t ld, width;
+    const float* left;         // [T][max_rank]
+    bool scaled, by_column;
+    float* out;
+};
+
+__global__ __launch_bounds__(256) void outer_kernel(const OuterRows Q1, const OuterRows Q2, const int64_t first2, const AdapterArgs A, const GroupArgs G) {
+    const OuterRows& Q = blockIdx.x < first2 ? Q1 : Q2;
+    const int64_t block = blockIdx.x < first2 ? blockIdx.x : blockIdx.x - first2;
+    const int64_t wt = (Q.width + 255) / 256;
     const int32_t groups = (A.max_rank + 15) / 16;
-    const int32_t k = (int32_t)(blockIdx.x / (wt * groups));
-    const int64_t rest = blockIdx.x - k * wt * groups;
+    const int32_t k = (int32_t)(block / (wt * groups));
+    const int64_t rest = block - k * wt * groups;
     const int32_t r0 = (int32_t)(rest / wt) * 16;
     const int64_t c = (rest - rest / wt * wt) * 256 + threadIdx.x;
-    if (c >= width) return;
-    const int32_t rank = adapter_rank(A, k), n = count[k], p0 = first[k];
+    if (c >= Q.width) return;
+    const int32_t rank = adapter_rank(A, k), n = G.count[k], p0 = G.first[k];
+    const int32_t ranks = A.max_rank - r0 < 16 ? A.max_rank - r0 : 16;
     float acc[16] = {};
     if (r0 < rank) {
-        for (int32_t i = 0; i < n; ++i) {
-            const int64_t t = place[p0 + i];
-            const float x = elem(right, t * ld + c, sizeof(XT) == 4);
-            const float* __restrict__ const l = left + t * A.max_rank + r0;
+        constexpr int AHEAD = 4;
+        for (int32_t i0 = 0; i0 < n; i0 += AHEAD) {
+            float x[AHEAD], l[AHEAD][16];
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (r0 + r < A.max_rank) acc[r] = fmaf(l[r], x, acc[r]);
+            for (int i = 0; i < AHEAD; ++i) {
+                const int64_t t = G.place[p0 + (i0 + i < n ? i0 + i : n - 1)];          // past the last token: read again, not counted
+                x[i] = Q.right[t * Q.ld + c];
+#pragma unroll
+                for (int r = 0; r < 16; ++r) l[i][r] = Q.left[t * A.max_rank + r0 + (r < ranks ? r : 0)];
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (i0 + i < n) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[r] = fmaf(l[i][r], x[i], acc[r]);
+                }
         }
     }
-    const float factor = scaled && A.alpha != nullptr ? A.alpha[k] : 1.0f;
+    const float factor = Q.scaled && A.alpha != nullptr ? A.alpha[k] : 1.0f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-        if (r0 + r >= A.max_rank) break;
+        if (r >= ranks) break;
         const float v = r0 + r < rank && n > 0 ? factor * acc[r] : 0.0f;
-        if (by_column) out[((int64_t)k * width + c) * A.max_rank + r0 + r] = v;
-        else out[((int64_t)k * A.max_rank + r0 + r) * width + c] = v;
+        if (Q.by_column) Q.out[((int64_t)k * Q.width + c) * A.max_rank + r0 + r] = v;
+        else Q.out[((int64_t)k * A.max_rank + r0 + r) * Q.width + c] = v;
     }
 }
 
@@ -219,6 +237,8 @@ struct DxArgs {
     int64_t ldx;
     const float* dh;           // [T][max_rank] or null
     AdapterArgs A;
+    float* part;               // fp32: [splits][tiles][4][1024][4], sums of a part of the rows
+    int32_t splits;
 };
 
 // Eight columns of A_k^T dh_t, added to v.
@@ -452,7 +472,58 @@ __global__ __launch_bounds__(256) void grad_prepare_kernel(const PrepareArgs<XT>
 
 // fp32: 64 columns and 64 tokens a workgroup on the fp32 matrix instructions.  Sixteen wavefronts, four to a quarter of the rows, which go
 // through LDS 32 at a time, the next ones on their way meanwhile: small layers leave few workgroups, and a wavefront's time is latency.
-constexpr int DXF_THREADS = 1024, DXF_PARTS = DXF_THREADS / 256;
+// Where tiles are fewer than the CUs the rows are split further, over workgroups, whose sums another kernel joins in order: 1000 x 1056 at 77
+// tokens (34 tiles of 8 steps) takes 60 us without the split and 17 + 5 with it (four parts of 2 steps).
+constexpr int DXF_THREADS = 1024, DXF_PARTS = DXF_THREADS / 256, DXF_TILES = 256;
+inline int64_t dxf_tiles(int64_t T, int64_t cols) { return tokens_in(cols, 64) * tokens_in(T, 64); }
+inline int32_t dxf_splits(int64_t tiles, int64_t rows) {
+    const int64_t steps = tokens_in(rows, 32 * DXF_PARTS), most = DXF_TILES / tiles < 1 ? 1 : DXF_TILES / tiles;
+    const int64_t each = tokens_in(steps, most < steps ? most : steps);
+    return (int32_t)tokens_in(steps, each);
+}
+
+// Four columns of a token: the adapter's part, and out.
+__device__ __forceinline__ void dx_f32_store(const DxArgs& Q, int64_t t, int64_t c, float (&v)[4]) {
+    const PackArgs& P = Q.P;
+    if (t >= Q.T || c >= P.cols) return;                    // columns come in eights: four of them are in or out together
+    if (Q.dh != nullptr) {
+        const int32_t k = Q.A.of[t];
+        if (k >= 0 && k < Q.A.n) {
+            const int32_t rank = adapter_rank(Q.A, k);
+            const float* __restrict__ const a = static_cast<const float*>(Q.A.a) + (int64_t)k * Q.A.max_rank * P.cols + c;
+            float sum[4] = {};
+#pragma unroll 4
+            for (int32_t r = 0; r < rank; ++r) {
+                const float4 av = *reinterpret_cast<const float4*>(a + (int64_t)r * P.cols);
+                const float d = Q.dh[t * Q.A.max_rank + r];
+                sum[0] = fmaf(av.x, d, sum[0]);
+                sum[1] = fmaf(av.y, d, sum[1]);
+                sum[2] = fmaf(av.z, d, sum[2]);
+                sum[3] = fmaf(av.w, d, sum[3]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += sum[i];
+        }
+    }
+    float* __restrict__ const o = static_cast<float*>(Q.dX) + t * Q.ldx + c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = v[i];
+}
+
+__global__ __launch_bounds__(256) void dx_f32_join_kernel(const DxArgs Q, const int64_t tiles) {
+    const int64_t tile = blockIdx.x >> 2, col_blocks = (Q.P.cols + 63) / 64, tb = tile / col_blocks;
+    const int n = blockIdx.x & 3, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    float v[4] = {};
+    for (int32_t s = 0; s < Q.splits; ++s) {
+        const float4 p = reinterpret_cast<const float4*>(Q.part)[(s * tiles + tile) * 1024 + n * 256 + threadIdx.x];
+        v[0] += p.x;
+        v[1] += p.y;
+        v[2] += p.z;
+        v[3] += p.w;
+    }
+    dx_f32_store(Q, tb * 64 + n * 16 + (lane & 15), (tile - tb * col_blocks) * 64 + wave * 16 + 4 * (lane >> 4), v);
+}
+
 __global__ __launch_bounds__(DXF_THREADS) void dx_f32_kernel(const DxArgs Q) {
     __shared__ float wts[DXF_PARTS][32][68], yts[DXF_PARTS][32][68];
     __shared__ uint16_t trits_of[256];
@@ -462,13 +533,14 @@ __global__ __launch_bounds__(DXF_THREADS) void dx_f32_kernel(const DxArgs Q) {
     const int part = threadIdx.x >> 8, tid = threadIdx.x & 255, wave = tid >> 6, lane = tid & 63, sub = lane & 15, q = lane >> 4;
     float(&wt)[32][68] = wts[part];
     float(&yt)[32][68] = yts[part];
-    const int64_t col_blocks = (P.cols + 63) / 64;
-    const int64_t tb = blockIdx.x / col_blocks;
-    const int64_t c0 = (blockIdx.x - tb * col_blocks) * 64, t0 = tb * 64;
+    const int64_t col_blocks = (P.cols + 63) / 64, tiles = col_blocks * ((Q.T + 63) / 64);
+    const int64_t split = blockIdx.x / tiles, tile = blockIdx.x - split * tiles, tb = tile / col_blocks;
+    const int64_t c0 = (tile - tb * col_blocks) * 64, t0 = tb * 64;
     const float* __restrict__ const dY = static_cast<const float*>(Q.dY);
     f32x4 acc[4] = {};
     if (Q.packed) {
-        const int64_t blocks = (P.rows + 31) / 32, each = (blocks + DXF_PARTS - 1) / DXF_PARTS;       // the same for all parts: barriers are shared
+        // steps of a quarter, the same for all of them: barriers are shared
+        const int64_t blocks = (P.rows + 31) / 32, each = (blocks + DXF_PARTS * Q.splits - 1) / (DXF_PARTS * Q.splits), from = (split * DXF_PARTS + part) * each;
         const int r = tid >> 3, o = tid & 7, yr = tid & 31;
         float w[8], y[8];
         auto fetch = [&](int64_t block) {
@@ -482,7 +554,7 @@ __global__ __launch_bounds__(DXF_THREADS) void dx_f32_kernel(const DxArgs Q) {
                 y[j] = r0 + yr < P.rows && t < Q.T ? dY[t * Q.ldy + r0 + yr] : 0.0f;
             }
         };
-        fetch(part * each);
+        fetch(from);
         for (int64_t i = 0; i < each; ++i) {
             __syncthreads();
 #pragma unroll
@@ -492,7 +564,7 @@ __global__ __launch_bounds__(DXF_THREADS) void dx_f32_kernel(const DxArgs Q) {
             }
             __syncthreads();
             // past its quarter a part multiplies zeros
-            fetch(i + 1 < each ? part * each + i + 1 : blocks);
+            fetch(i + 1 < each ? from + i + 1 : blocks);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const float a = wt[k * 4 + q][wave * 16 + sub];
@@ -528,31 +600,9 @@ __global__ __launch_bounds__(DXF_THREADS) void dx_f32_kernel(const DxArgs Q) {
     if (part != 0) return;
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-        const int64_t t = t0 + n * 16 + sub;
-        const int64_t c = c0 + wave * 16 + 4 * q;
-        if (t >= Q.T || c >= P.cols) continue;              // columns come in eights: four of them are in or out together
         float v[4] = {acc[n][0], acc[n][1], acc[n][2], acc[n][3]};
-        if (Q.dh != nullptr) {
-            const int32_t k = Q.A.of[t];
-            if (k >= 0 && k < Q.A.n) {
-                const int32_t rank = adapter_rank(Q.A, k);
-                const float* __restrict__ const a = static_cast<const float*>(Q.A.a) + (int64_t)k * Q.A.max_rank * P.cols + c;
-                float sum[4] = {};
-                for (int32_t r = 0; r < rank; ++r) {
-                    const float4 av = *reinterpret_cast<const float4*>(a + (int64_t)r * P.cols);
-                    const float d = Q.dh[t * Q.A.max_rank + r];
-                    sum[0] = fmaf(av.x, d, sum[0]);
-                    sum[1] = fmaf(av.y, d, sum[1]);
-                    sum[2] = fmaf(av.z, d, sum[2]);
-                    sum[3] = fmaf(av.w, d, sum[3]);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] += sum[i];
-            }
-        }
-        float* __restrict__ const o = static_cast<float*>(Q.dX) + t * Q.ldx + c;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = v[i];
+        if (Q.splits > 1) reinterpret_cast<float4*>(Q.part)[blockIdx.x * 1024 + n * 256 + tid] = make_float4(v[0], v[1], v[2], v[3]);
+        else dx_f32_store(Q, t0 + n * 16 + sub, c0 + wave * 16 + 4 * q, v);
     }
 }
 
@@ -561,7 +611,7 @@ __global__ __launch_bounds__(DXF_THREADS) void dx_f32_kernel(const DxArgs Q) {
 constexpr int64_t TURN_FROM = 256;
 
 struct GradWs {
-    size_t h, dh, bt, at, dy, place, owner, first, count, part, part2, planes_h, planes_dh, wt, total;
+    size_t h, dh, bt, at, dy, place, owner, first, count, part, part2, planes_h, planes_dh, wt, dxf, total;
     int64_t ld;                // of dY's copy and of B transposed
 };
 
@@ -592,6 +642,7 @@ GradWs grad_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t n, 
     w.planes_h = take(bf && n > 0 ? (size_t)slots * GROUP * (size_t)max_rank * 6 : 0);
     w.planes_dh = take(bf && n > 0 ? (size_t)slots * GROUP * (size_t)max_rank * 6 : 0);
     w.wt = take(bf && T >= TURN_FROM ? (size_t)gemm_cols(cols) * (size_t)gemm_k(rows) * 2 : 0);
+    w.dxf = take(bf ? 0 : (size_t)DXF_TILES * 64 * 64 * 4);       // tiles x splits are no more
     w.total = at == 0 ? 256 : at;
     return w;
 }
@@ -710,8 +761,10 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
                     h = ht;
                 }
                 const int64_t groups = (int64_t)A.n * ((A.max_rank + 15) / 16);
-                WINDQ_LAUNCH(groups * ((cols + 255) / 256), 256, outer_kernel<XT>, static_cast<const XT*>(X->data), X->ld, cols, dh, A, G.place, G.first, G.count, false, false, dA);
-                WINDQ_LAUNCH(groups * ((rows + 255) / 256), 256, outer_kernel<XT>, dYv, Q.ldy, rows, h, A, G.place, G.first, G.count, true, true, dB);
+                const OuterRows O1 = {static_cast<const float*>(X->data), X->ld, cols, dh, false, false, dA};
+                const OuterRows O2 = {dYv, Q.ldy, rows, h, true, true, dB};
+                const int64_t n1 = groups * tokens_in(cols, 256), n2 = groups * tokens_in(rows, 256);
+                WINDQ_LAUNCH(n1 + n2, 256, outer_kernel, O1, O2, n1, A, G);
             }
         }
         Q.dh = dh;
@@ -732,7 +785,11 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
         else if (T <= 128) WINDQ_LAUNCH(blocks * ((T + 127) / 128), 256, dx_kernel<2>, Q);
         else WINDQ_LAUNCH(blocks * ((T + 255) / 256), 256, dx_kernel<4>, Q);
     } else {
-        WINDQ_LAUNCH(((cols + 63) / 64) * ((T + 63) / 64), DXF_THREADS, dx_f32_kernel, Q);
+        const int64_t tiles = dxf_tiles(T, cols);
+        Q.splits = Q.packed ? dxf_splits(tiles, rows) : 1;
+        Q.part = reinterpret_cast<float*>(ws + at.dxf);
+        WINDQ_LAUNCH(tiles * Q.splits, DXF_THREADS, dx_f32_kernel, Q);
+        if (Q.splits > 1) WINDQ_LAUNCH(tiles * 4, 256, dx_f32_join_kernel, Q, tiles);
     }
     return WINDQ_OK;
 }
