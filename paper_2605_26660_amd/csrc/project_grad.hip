@@ -242,13 +242,13 @@ struct DxArgs {
 };
 
 // Eight columns of A_k^T dh_t, added to v.
-template <typename XT>
 __device__ __forceinline__ void add_adapter8(const AdapterArgs& A, const float* __restrict__ dh, int64_t t, int64_t col, int64_t cols, float (&v)[8]) {
     const int32_t k = A.of[t];
     if (k < 0 || k >= A.n) return;
     const int32_t rank = adapter_rank(A, k);
-    const XT* __restrict__ const a = static_cast<const XT*>(A.a) + (int64_t)k * A.max_rank * cols + col;
+    const uint16_t* __restrict__ const a = static_cast<const uint16_t*>(A.a) + (int64_t)k * A.max_rank * cols + col;
     float sum[8] = {};
+#pragma unroll 4
     for (int32_t r = 0; r < rank; ++r) {
         float av[8];
         load8(a + (int64_t)r * cols, av);
@@ -286,80 +286,16 @@ __device__ __forceinline__ void weight_octet(const PackArgs& P, int64_t row, int
     }
 }
 
-// bfloat16: a workgroup has 128 columns and 64 NT tokens and walks the rows 128 at a time.  The sum runs over rows, and a matrix
-// operand wants eight consecutive rows of one column in a lane, while codes lie along columns: a thread unpacks a block of eight rows by
-// eight columns and has, after rounding pairs of rows together, one operand for each of its eight columns.  Sixteen threads
-// side by side make the operands of eight instructions whose M side is every eighth column; which columns share an instruction is free, and a
-// lane ends up with eight consecutive columns of its token.
-constexpr int DX_COLS = 128, DX_ROWS = 128;
-
-template <int NT>
-__global__ __launch_bounds__(256) void dx_kernel(const DxArgs Q) {
-    __shared__ uint4 frag[DX_ROWS / 8][8][16];
-    __shared__ uint16_t trits_of[256];
-    trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
-    __syncthreads();
-    const PackArgs& P = Q.P;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
-    const int64_t col_blocks = (P.cols + DX_COLS - 1) / DX_COLS;
-    const int64_t tb = blockIdx.x / col_blocks;
-    const int64_t c0 = (blockIdx.x - tb * col_blocks) * DX_COLS, t0 = tb * (64 * NT) + wave * (16 * NT);
-    const int oc = threadIdx.x & 15, kg = threadIdx.x >> 4;
-    const int64_t col = c0 + oc * 8;
-    const uint16_t* dy[NT];
+// The adapters' part alone, in bfloat16: a thread per token and octet of columns.
+__global__ __launch_bounds__(256) void dx_side_kernel(const DxArgs Q) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, octets = Q.P.cols >> 3;
+    const int64_t t = i / octets, c = (i - t * octets) * 8;
+    if (t >= Q.T) return;
+    float v[8] = {};
+    add_adapter8(Q.A, Q.dh, t, c, Q.P.cols, v);
+    uint16_t* __restrict__ const o = static_cast<uint16_t*>(Q.dX) + t * Q.ldx + c;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int64_t t = t0 + n * 16 + sub;
-        dy[n] = static_cast<const uint16_t*>(Q.dY) + (t < Q.T ? t : Q.T - 1) * Q.ldy;
-    }
-    f32x4 acc[8][NT] = {};
-    if (Q.packed) {
-        for (int64_t r0 = 0; r0 < P.rows; r0 += DX_ROWS) {
-            uint32_t v[8][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float w0[8] = {}, w1[8] = {};
-                const int64_t row = r0 + kg * 8 + 2 * i;
-                if (col < P.cols && row < P.rows) weight_octet(P, row, col, trits_of, w0);
-                if (col < P.cols && row + 1 < P.rows) weight_octet(P, row + 1, col, trits_of, w1);
-#pragma unroll
-                for (int m = 0; m < 8; ++m) v[m][i] = f32_to_bf16_bits(w0[m]) | f32_to_bf16_bits(w1[m]) << 16;
-            }
-            __syncthreads();
-#pragma unroll
-            for (int m = 0; m < 8; ++m) frag[kg][m][oc] = make_uint4(v[m][0], v[m][1], v[m][2], v[m][3]);
-            __syncthreads();
-#pragma unroll
-            for (int kk = 0; kk < DX_ROWS / 32; ++kk) {
-                const int64_t row = r0 + kk * 32 + q * 8;
-                bf16x8 b[NT];
-#pragma unroll
-                for (int n = 0; n < NT; ++n) b[n] = as_bf16x8(row < P.rows ? *reinterpret_cast<const uint4*>(dy[n] + row) : make_uint4(0u, 0u, 0u, 0u));
-#pragma unroll
-                for (int m = 0; m < 8; ++m) {
-                    const bf16x8 a = as_bf16x8(frag[kk * 4 + q][m][sub]);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[n], acc[m][n], 0, 0, 0);
-                }
-            }
-        }
-    }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int64_t t = t0 + n * 16 + sub;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t c = c0 + (4 * q + i) * 8;
-            if (t >= Q.T || c >= P.cols) continue;
-            float v[8];
-#pragma unroll
-            for (int m = 0; m < 8; ++m) v[m] = acc[m][n][i];
-            if (Q.dh != nullptr) add_adapter8<uint16_t>(Q.A, Q.dh, t, c, P.cols, v);
-            uint16_t* __restrict__ const o = static_cast<uint16_t*>(Q.dX) + t * Q.ldx + c;
-#pragma unroll
-            for (int m = 0; m < 8; ++m) o[m] = (uint16_t)f32_to_bf16_bits(v[m]);
-        }
-    }
+    for (int m = 0; m < 8; ++m) o[m] = (uint16_t)f32_to_bf16_bits(v[m]);
 }
 
 // w_hat rounded to bfloat16 and turned: wt [cols][K], zeros from the last row to K.  A thread has eight rows by eight columns.
@@ -607,9 +543,6 @@ __global__ __launch_bounds__(DXF_THREADS) void dx_f32_kernel(const DxArgs Q) {
 }
 
 // ------------------------------------------------------------------------------------------------ the call
-// Tokens from which on the packed matrix is reconstructed once for dX.
-constexpr int64_t TURN_FROM = 256;
-
 struct GradWs {
     size_t h, dh, bt, at, dy, place, owner, first, count, part, part2, planes_h, planes_dh, wt, dxf, total;
     int64_t ld;                // of dY's copy and of B transposed
@@ -641,7 +574,7 @@ GradWs grad_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t n, 
     w.part2 = take(bf && n > 0 ? (size_t)shrink_pieces(slots, wide) * GROUP * (size_t)shrink_ranks(max_rank) * 4 : 0);
     w.planes_h = take(bf && n > 0 ? (size_t)slots * GROUP * (size_t)max_rank * 6 : 0);
     w.planes_dh = take(bf && n > 0 ? (size_t)slots * GROUP * (size_t)max_rank * 6 : 0);
-    w.wt = take(bf && T >= TURN_FROM ? (size_t)gemm_cols(cols) * (size_t)gemm_k(rows) * 2 : 0);
+    w.wt = take(bf && T > 0 ? (size_t)gemm_cols(cols) * (size_t)gemm_k(rows) * 2 : 0);
     w.dxf = take(bf ? 0 : (size_t)DXF_TILES * 64 * 64 * 4);       // tiles x splits are no more
     w.total = at == 0 ? 256 : at;
     return w;
@@ -666,7 +599,7 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
     const int64_t T = Q.T, rows = Q.P.rows, cols = Q.P.cols;
     const bool side = Q.A.n > 0;
     constexpr bool bf = sizeof(XT) == 2;
-    const bool turn = bf && Q.packed && Q.dX != nullptr && T >= TURN_FROM;
+    const bool turn = bf && Q.packed && Q.dX != nullptr && T > 0;
     const AdapterArgs A = Q.A;
     if (T > 0 && (dY->ld % 8 != 0 || rows % (turn ? GM_K : 8) != 0 || !aligned(dY->data, 16))) {
         XT* to = reinterpret_cast<XT*>(ws + at.dy);
@@ -696,7 +629,7 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
         R.bt = bt;
         R.ld = at.ld;
         R.bs = transpose_workgroups(A.n, A.max_rank, at.ld);
-        if (bf && Q.dX != nullptr && T >= TURN_FROM) {
+        if (turn) {
             R.a = static_cast<const XT*>(A.a);
             R.at = reinterpret_cast<XT*>(ws + at.at);
             R.as = transpose_workgroups(A.n, cols, A.max_rank);
@@ -780,10 +713,7 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
             else WINDQ_LAUNCH(wgs, GM_THREADS, dx_gemm_kernel<2>, M);
             return WINDQ_OK;
         }
-        const int64_t blocks = (cols + DX_COLS - 1) / DX_COLS;
-        if (T <= 64) WINDQ_LAUNCH(blocks * ((T + 63) / 64), 256, dx_kernel<1>, Q);
-        else if (T <= 128) WINDQ_LAUNCH(blocks * ((T + 127) / 128), 256, dx_kernel<2>, Q);
-        else WINDQ_LAUNCH(blocks * ((T + 255) / 256), 256, dx_kernel<4>, Q);
+        WINDQ_LAUNCH(tokens_in(T * (cols / 8), 256), 256, dx_side_kernel, Q);
     } else {
         const int64_t tiles = dxf_tiles(T, cols);
         Q.splits = Q.packed ? dxf_splits(tiles, rows) : 1;
