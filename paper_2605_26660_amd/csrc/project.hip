@@ -239,9 +239,9 @@ ProjectWs project_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32
     w.planes = take(dtype == WINDQ_F32 ? (size_t)(3 * T * cols) * 2 : 0);
     w.h = take((size_t)(T * max_rank) * 4);
     const bool few = dtype == WINDQ_BF16;                   // fewer tokens than asked for fit too
-    const int64_t few_tokens = T < FEW_MOST ? tokens_in(T, 32) * 32 : FEW_MOST;
+    const int64_t few_tokens = T < few_most(rows, cols, G) ? tokens_in(T, 64) * 64 : few_most(rows, cols, G);
     w.frag = take(few ? (size_t)cols * (size_t)few_tokens * 2 : 0);
-    w.few_xs = take(few ? (size_t)(cols / 64 + 1) * FEW_MOST * 4 : 0);
+    w.few_xs = take(few ? (size_t)(cols / 64 + 1) * (size_t)few_tokens * 4 : 0);
     const bool grouped = n > 0 && dtype == WINDQ_BF16 && T > SHRINK_FEW;
     const int64_t slots = group_slots(T, n);
     w.place = take(grouped ? (size_t)slots * GROUP * 4 : 0);
@@ -305,17 +305,10 @@ int project_all(ProjectArgs& Q, const windq_mat* X, const windq_adapters* ad, fl
         Q.ldx = Q.P.cols;
         Q.plane = T * Q.P.cols;
     }
-    if constexpr (sizeof(XT) == 2) {
-        if (few_fits(Q.P, T)) {
-            float* const ht = ad == nullptr ? nullptr : (h != nullptr ? h : reinterpret_cast<float*>(ws + at.h));
-            FewArgs F = {Q.P, Q.X, Q.ldx, T, static_cast<uint16_t*>(Q.Y), Q.ldy, ht, Q.A, 0, reinterpret_cast<uint4*>(ws + at.frag), reinterpret_cast<float*>(ws + at.few_xs), 0, 0};
-            const int steps = Q.P.G % 128 == 0 ? 8 : Q.P.G / 16;
-            F.n_kb = (int32_t)(Q.P.cols / (16 * steps));
-            return steps == 8 ? launch_few<8>(F, ht, st) : (steps == 6 ? launch_few<6>(F, ht, st) : launch_few<4>(F, ht, st));
-        }
-    }
-    if (ad != nullptr) {
-        float* const ht = h != nullptr ? h : reinterpret_cast<float*>(ws + at.h);
+    // Few tokens' h is formed by the kernel that lays X out, a wavefront a rank.
+    const bool few = sizeof(XT) == 2 && few_fits(Q.P, T), own_h = few && T <= FEW_OWN_H;
+    float* const ht = ad == nullptr ? nullptr : (h != nullptr ? h : reinterpret_cast<float*>(ws + at.h));
+    if (ad != nullptr && !own_h) {
         const int64_t wgs = shrink_token_workgroups(T, Q.A.max_rank);
         bool grouped = false;
         if constexpr (sizeof(XT) == 2) {
@@ -337,7 +330,16 @@ int project_all(ProjectArgs& Q, const windq_mat* X, const windq_adapters* ad, fl
             shrink_token_kernel<XT><<<dim3((uint32_t)wgs), dim3(256), 0, st>>>(static_cast<const XT*>(X->data), X->ld, (int32_t)Q.P.cols, Q.A, false, ht);
             if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
         }
-        Q.h = ht;
+    }
+    Q.h = ht;
+    if constexpr (sizeof(XT) == 2) {
+        if (few) {
+            FewArgs F = {Q.P, Q.X, Q.ldx, T, static_cast<uint16_t*>(Q.Y), Q.ldy, ht, Q.A, 0, reinterpret_cast<uint4*>(ws + at.frag), reinterpret_cast<float*>(ws + at.few_xs), 0, 0, 0};
+            const int steps = Q.P.G % 128 == 0 ? 8 : Q.P.G / 16;
+            F.n_kb = (int32_t)(Q.P.cols / (16 * steps));
+            float* const form = own_h ? ht : nullptr;
+            return steps == 8 ? launch_few<8>(F, form, st) : (steps == 6 ? launch_few<6>(F, form, st) : launch_few<4>(F, form, st));
+        }
     }
     // The general kernel where its workgroups run about at once.  bfloat16, 1024 x 1024: 160 tokens (192 of them) 21 us, tiles 31; 320 tokens (320) 39
     // and 31.  fp32, 4096 x 4096: 80 tokens (512) 237 us, tiles 303; 160 tokens (768) 450 and 312.

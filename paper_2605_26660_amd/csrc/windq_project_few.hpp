@@ -1,4 +1,4 @@
-// windq_project for few tokens of bfloat16 (up to 64, or 256 where rows are few): 32 rows and up to 64 tokens a workgroup, the k-blocks shared by its wavefronts.
+// windq_project for few tokens of bfloat16 (up to 64, or more where rows are few): 32 rows and up to 64 tokens a workgroup, the k-blocks shared by its wavefronts.
 //
 // Bound by latency, not by the codes: 7 MB at 2 bits for 11008 x 4096.  So the sum is cut into as many pieces as there are k-blocks per
 // wavefront, every wavefront works by itself until the end, and what it needs of a k-block is asked for at once: codes by direct
@@ -25,17 +25,24 @@ struct FewArgs {
     AdapterArgs A;
     int32_t n_kb;
     uint4* frag;               // [k-blocks][fragments][S][64 lanes], or unused
-    float* xs;                 // [k-blocks][FEW_MOST]
+    float* xs;                 // [k-blocks][xs_ld]
+    int64_t xs_ld;             // tokens in 64s
     int32_t fragments;         // of 32 tokens
     uint32_t row_blocks;
 };
 
-constexpr int64_t FEW_DIRECT = 8, FEW_ALWAYS = 64, FEW_MOST = 256;
+constexpr int64_t FEW_DIRECT = 8, FEW_ALWAYS = 64, FEW_OWN_H = 256;
 
-// Past 64 tokens as long as the workgroups take no more than three rounds (one a CU): 4096 x 4096 at 128 tokens (256 of them) 27 us, tiles 80;
-// 11008 x 4096 at 256 tokens would be 1376, tiles 94 us, and 64 tokens' 344 take 45.
+// Most tokens of a matrix: 64, or as many as make one round of workgroups (one a CU), two from 8 k-blocks on, three from 32 on.  A round takes
+// some 10 us + 0.55 a k-block, tiles of 128 tokens 14 + 2.0 as long as they are no more than the CUs: 280 x 4864, 725 tokens (one round) 35 us, tiles 94;
+// 384 x 1344, 1371 tokens (two, 14 k-blocks) 33 and 39; 3968 x 768, 300 tokens (three, 6) 38 and 28; 4096 x 4096, 300 tokens (three, 32) 66 and 83.
+inline int64_t few_most(int64_t rows, int64_t cols, int32_t G) {
+    const int64_t k_blocks = cols / (G % 128 == 0 ? 128 : G), rounds = k_blocks >= 32 ? 3 : (k_blocks >= 8 ? 2 : 1);
+    const int64_t most = 256 * rounds / tokens_in(rows, PF_ROWS) * 64;
+    return most > FEW_ALWAYS ? most : FEW_ALWAYS;
+}
 inline bool few_fits(const PackArgs& P, int64_t T) {
-    if (T > FEW_MOST || (T > FEW_ALWAYS && (P.rows + PF_ROWS - 1) / PF_ROWS * ((T + 63) / 64) > 768)) return false;
+    if (T > few_most(P.rows, P.cols, P.G)) return false;
     return P.mask == nullptr && P.rows % 8 == 0 && (P.R_u == P.rows || P.R_u % PF_ROWS == 0) && (P.G % 128 == 0 || P.G == 96 || P.G == 64);
 }
 
@@ -88,7 +95,7 @@ __global__ __launch_bounds__(256) void few_prepare_kernel(const FewArgs Q, const
         sum += (p[0] + p[1]) + (p[2] + p[3]);
     }
     sum += __shfl_xor(sum, 32, 64);
-    if (hh == 0) Q.xs[kb * FEW_MOST + t] = sum;
+    if (hh == 0) Q.xs[kb * Q.xs_ld + t] = sum;
 }
 
 template <int S, int NTF, int WAVES, bool LAID>
@@ -158,7 +165,7 @@ __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q
             const uint4* const from = x_at(n, kb);
 #pragma unroll
             for (int s = 0; s < S; ++s) x[s][n] = from[LAID ? s * 64 : s];
-            if (LAID) xsum[n] = Q.xs[kb * FEW_MOST + t0 + n * 32 + sub];
+            if (LAID) xsum[n] = Q.xs[kb * Q.xs_ld + t0 + n * 32 + sub];
         }
         if (kb + WAVES < Q.n_kb) a = __builtin_amdgcn_readfirstlane(pk_action(P, rb * P.n_chunks + (kb + WAVES) / per_chunk, base));
         if (kb == wave && Q.h != nullptr) {                 // while all of this is on its way
@@ -262,10 +269,11 @@ __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q
     }
 }
 
-// h, or null: formed here.
+// h, or null: formed here (Q.h without it: there already).
 template <int S>
 int launch_few(FewArgs Q, float* h, hipStream_t st) {
     Q.fragments = (int32_t)tokens_in(Q.T, 32);
+    Q.xs_ld = tokens_in(Q.T, 64) * 64;
     Q.row_blocks = (uint32_t)((Q.P.rows + PF_ROWS - 1) / PF_ROWS);
     const bool laid = Q.T > FEW_DIRECT;
     const int64_t wgs = (int64_t)Q.row_blocks * tokens_in(Q.T, Q.fragments == 1 ? 32 : 64);
