@@ -237,7 +237,7 @@ struct DxArgs {
     int64_t ldx;
     const float* dh;           // [T][max_rank] or null
     AdapterArgs A;
-    float* part;               // fp32: [splits][tiles][4][1024][4], sums of a part of the rows
+    float* part;               // sums of parts of the rows; fp32: [splits][tiles][4][256][4], bfloat16: [splits][T][cols]
     int32_t splits;
 };
 
@@ -286,16 +286,30 @@ __device__ __forceinline__ void weight_octet(const PackArgs& P, int64_t row, int
     }
 }
 
-// The adapters' part alone, in bfloat16: a thread per token and octet of columns.
-__global__ __launch_bounds__(256) void dx_side_kernel(const DxArgs Q) {
+// bfloat16: the sums of the product's parts (none: the packed matrix is not wanted) and the adapters', a thread per token and octet of columns.
+__global__ __launch_bounds__(256) void dx_join_kernel(const DxArgs Q) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, octets = Q.P.cols >> 3;
     const int64_t t = i / octets, c = (i - t * octets) * 8;
     if (t >= Q.T) return;
     float v[8] = {};
-    add_adapter8(Q.A, Q.dh, t, c, Q.P.cols, v);
-    uint16_t* __restrict__ const o = static_cast<uint16_t*>(Q.dX) + t * Q.ldx + c;
+#pragma unroll 4
+    for (int32_t s = 0; s < Q.splits; ++s) {
+        float p[8];
+        load8(Q.part + (s * Q.T + t) * Q.P.cols + c, p);
 #pragma unroll
-    for (int m = 0; m < 8; ++m) o[m] = (uint16_t)f32_to_bf16_bits(v[m]);
+        for (int m = 0; m < 8; ++m) v[m] += p[m];
+    }
+    if (Q.dh != nullptr) add_adapter8(Q.A, Q.dh, t, c, Q.P.cols, v);
+    uint16_t* __restrict__ const o = static_cast<uint16_t*>(Q.dX) + t * Q.ldx + c;
+    uint32_t w[8];
+#pragma unroll
+    for (int m = 0; m < 8; ++m) w[m] = f32_to_bf16_bits(v[m]);
+    if ((Q.ldx & 7) == 0 && (reinterpret_cast<uintptr_t>(Q.dX) & 15) == 0) {
+        *reinterpret_cast<uint4*>(o) = pack8(w);
+    } else {
+#pragma unroll
+        for (int m = 0; m < 8; ++m) o[m] = (uint16_t)w[m];
+    }
 }
 
 // w_hat rounded to bfloat16 and turned: wt [cols][K], zeros from the last row to K.  A thread has eight rows by eight columns.
@@ -544,7 +558,7 @@ __global__ __launch_bounds__(DXF_THREADS) void dx_f32_kernel(const DxArgs Q) {
 
 // ------------------------------------------------------------------------------------------------ the call
 struct GradWs {
-    size_t h, dh, bt, at, dy, place, owner, first, count, part, part2, planes_h, planes_dh, wt, dxf, total;
+    size_t h, dh, bt, at, dy, place, owner, first, count, part, part2, planes_h, planes_dh, wt, gm, dxf, total;
     int64_t ld;                // of dY's copy and of B transposed
 };
 
@@ -575,6 +589,7 @@ GradWs grad_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t n, 
     w.planes_h = take(bf && n > 0 ? (size_t)slots * GROUP * (size_t)max_rank * 6 : 0);
     w.planes_dh = take(bf && n > 0 ? (size_t)slots * GROUP * (size_t)max_rank * 6 : 0);
     w.wt = take(bf && T > 0 ? (size_t)gemm_cols(cols) * (size_t)gemm_k(rows) * 2 : 0);
+    w.gm = take(bf ? (size_t)gemm_parts(T, gemm_k(rows), cols) * 4 : 0);
     w.dxf = take(bf ? 0 : (size_t)DXF_TILES * 64 * 64 * 4);       // tiles x splits are no more
     w.total = at == 0 ? 256 : at;
     return w;
@@ -705,15 +720,22 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
     if (Q.dX == nullptr || T == 0) return WINDQ_OK;
     if constexpr (bf) {
         if (turn) {
-            const int64_t wide = tokens_in(cols, 256) * tokens_in(T, GM_N);
-            const int64_t by = wide >= 256 ? 256 : 128;
-            const GemmArgs M = {R.wt, dYv, Q.ldy, R.K, T, cols, static_cast<uint16_t*>(Q.dX), Q.ldx, Q.dh, R.at, A, (uint32_t)tokens_in(cols, by)};
-            const int64_t wgs = (int64_t)M.col_blocks * tokens_in(T, GM_N);
-            if (by == 256) WINDQ_LAUNCH(wgs, GM_THREADS, dx_gemm_kernel<4>, M);
-            else WINDQ_LAUNCH(wgs, GM_THREADS, dx_gemm_kernel<2>, M);
-            return WINDQ_OK;
+            const int64_t tall = tokens_in(T, GM_N), by = tokens_in(cols, 256) * tall >= GM_TILES ? 256 : 128, tiles = tokens_in(cols, by) * tall;
+            GemmArgs M = {R.wt, dYv, Q.ldy, R.K, T, cols, static_cast<uint16_t*>(Q.dX), Q.ldx, Q.dh, R.at, A, (uint32_t)tokens_in(cols, by), nullptr, (int32_t)tiles, R.K / GM_K};
+            if (by == 256) {
+                WINDQ_LAUNCH(tiles, GM_THREADS, dx_gemm_kernel<4>, M);
+                return WINDQ_OK;
+            }
+            const int32_t each = gemm_each(R.K, tiles), splits = (int32_t)tokens_in(R.K / GM_K, each);
+            if (splits > 1) {
+                M.each = each;
+                M.part = Q.part = reinterpret_cast<float*>(ws + at.gm);
+                Q.splits = splits;
+            }
+            WINDQ_LAUNCH(tiles * splits, GM_THREADS, dx_gemm_kernel<2>, M);
+            if (splits == 1) return WINDQ_OK;
         }
-        WINDQ_LAUNCH(tokens_in(T * (cols / 8), 256), 256, dx_side_kernel, Q);
+        WINDQ_LAUNCH(tokens_in(T * (cols / 8), 256), 256, dx_join_kernel, Q);
     } else {
         const int64_t tiles = dxf_tiles(T, cols);
         Q.splits = Q.packed ? dxf_splits(tiles, rows) : 1;

@@ -2,7 +2,7 @@
 //
 // Codes lie along columns and the sum runs along rows, so a tile of weights would have to be turned for every 128 tokens.  The packed
 // matrix is reconstructed once instead, rounded to bfloat16 and turned (wt [cols][rows], 2 bytes a weight; 35 of 294 us at 2048 tokens through
-// 11008 x 4096; for one token too: 4096 x 4096 60 us, 373 with tiles turned on the way), and the product then spends nothing but matrix instructions and their operands' way: 256 columns x 128
+// 11008 x 4096; for one token too: 4096 x 4096 45 us, 373 with tiles turned on the way), and the product then spends nothing but matrix instructions and their operands' way: 256 columns x 128
 // tokens a workgroup, four wavefronts with 128 x 64 results each as 4 x 2 fragments of 32x32x16 instructions, one per SIMD; 128 columns where
 // that would leave CUs without a workgroup.
 //   64 of the sum at a time go to LDS by direct loads, three buffers: while one is multiplied the next has landed and the one
@@ -29,9 +29,23 @@ struct GemmArgs {
     const uint16_t* at;        // [n][cols][max_rank]
     AdapterArgs A;
     uint32_t col_blocks;
+    float* part;               // [splits][T][cols] sums over a part of the rows, or null: one workgroup has them all
+    int32_t tiles, each;       // workgroups of a split, its steps of GM_K
 };
 
 inline int64_t gemm_k(int64_t rows) { return (rows + GM_K - 1) / GM_K * GM_K; }
+// Where 128-column tiles are fewer than the CUs the sum is split over workgroups, four steps or more each, and another kernel joins the
+// parts in order and adds the adapters': 11008 x 4096, 64 tokens (32 tiles) 109 -> 70 us, 4096 x 4096, 1 token 59 -> 45.
+constexpr int GM_TILES = 256, GM_LEAST = 4;
+inline int32_t gemm_each(int64_t K, int64_t tiles) {
+    const int64_t steps = K / GM_K, most = tiles < GM_TILES ? GM_TILES / tiles : 1, each = (steps + most - 1) / most;
+    return (int32_t)(each > GM_LEAST ? each : GM_LEAST);
+}
+// Most floats of the parts, for so many tokens or fewer.
+inline int64_t gemm_parts(int64_t T, int64_t K, int64_t cols) {
+    const int64_t all = (int64_t)GM_TILES * 128 * GM_N, splits = (K / GM_K + GM_LEAST - 1) / GM_LEAST;
+    return T * cols * splits < all ? T * cols * splits : all;
+}
 inline int64_t gemm_cols(int64_t cols) { return (cols + GM_MOST - 1) / GM_MOST * GM_MOST; }
 
 #ifdef __HIPCC__
@@ -45,18 +59,19 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
     // Consecutive workgroups land on the eight XCDs in turn; each XCD gets a run of tiles that share tokens.
     const uint32_t n_tiles = gridDim.x, per = n_tiles >> 3;
     const uint32_t id = blockIdx.x < per * 8 ? (blockIdx.x & 7) * per + (blockIdx.x >> 3) : blockIdx.x;
-    const uint32_t tb = id / Q.col_blocks;
-    const int64_t c0 = (int64_t)(id - tb * Q.col_blocks) * GM_M, t0 = (int64_t)tb * GM_N;
+    const uint32_t split = id / (uint32_t)Q.tiles, in = id - split * (uint32_t)Q.tiles, tb = in / Q.col_blocks;
+    const int64_t c0 = (int64_t)(in - tb * Q.col_blocks) * GM_M, t0 = (int64_t)tb * GM_N;
+    const int32_t first = (int32_t)split * Q.each, steps = Q.K / GM_K - first;
 
     // A lane's share of a tile: slot (lane & 7) of rows 8 wave + lane / 8, 32 rows further on each time; slot p of row r holds the
     // sixteen bytes of slot p ^ (r & 7).
     const int lr = wave * 8 + (lane >> 3), slot = (lane & 7) ^ (lr & 7);
-    const uint16_t* const am = Q.wt + (c0 + lr) * Q.K + slot * 8;
+    const uint16_t* const am = Q.wt + (c0 + lr) * Q.K + first * GM_K + slot * 8;
     const uint16_t* bn[GM_N / 32];
 #pragma unroll
     for (int i = 0; i < GM_N / 32; ++i) {
         const int64_t t = t0 + i * 32 + lr;
-        bn[i] = Q.dY + (t < Q.T ? t : Q.T - 1) * Q.ldy + slot * 8;
+        bn[i] = Q.dY + (t < Q.T ? t : Q.T - 1) * Q.ldy + first * GM_K + slot * 8;
     }
     const uint32_t lds = lds_address(tile);
     auto load_a = [&](int i, int32_t k, int buf) { lds_load16(lds + (buf * (GM_M + GM_N) * 8 + i * 256 + wave * 64) * 16, am + (int64_t)i * 32 * Q.K + k * GM_K); };
@@ -70,7 +85,7 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
         else a[i - 2] = as_bf16x8(*reinterpret_cast<const uint4*>(at + arow + (i - 2) * 32 * 128 + o));
     };
 
-    const int32_t n_k = Q.K / GM_K;
+    const int32_t n_k = steps < Q.each ? steps : Q.each;
     f32x16 acc[MF][2] = {};
     if (n_k > 0) {
 #pragma unroll
@@ -120,6 +135,22 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
 
+    if (Q.part != nullptr) {
+        float* const to = Q.part + (int64_t)split * Q.T * Q.cols;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int64_t t = t0 + wn * 64 + n * 32 + sub;
+            if (t >= Q.T) continue;
+#pragma unroll
+            for (int f = 0; f < MF; ++f)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int64_t c = c0 + wm * WM + f * 32 + g * 8 + hh * 4;
+                    if (c < Q.cols) *reinterpret_cast<float4*>(to + t * Q.cols + c) = make_float4(acc[f][n][g * 4], acc[f][n][g * 4 + 1], acc[f][n][g * 4 + 2], acc[f][n][g * 4 + 3]);
+                }
+        }
+        return;
+    }
     if (Q.dh != nullptr)
         add_adapters<uint16_t, MF>(Q.A, Q.dh, false, t0 + wn * 64, Q.T, lane, [&](int32_t k, int f) {
             const int64_t c = c0 + wm * WM + f * 32 + sub;
