@@ -665,7 +665,8 @@ typedef struct windq_adapters {
  * results are bit-reproducible and differ from the exact sum by a few 1e-7 of sum |w_hat x| before Y's own rounding.
  * A result that is not finite is formed again weight by weight in fp64, so infinities and NaN of x, of scales and of skip
  * weights come out as the formula has them, in their own token's and row's results only.
- * At most 2^31 - 1 tokens x rows.  Workspace: windq_project_workspace_bytes.
+ * X is 16-byte aligned with a leading dimension that is a multiple of 8; Y and ld_y are free.  At most 2^31 - 1 tokens x rows.
+ * Workspace: windq_project_workspace_bytes (256-byte aligned), written anew by every call.
  */
 int windq_project(const windq_packed* P /*HOST*/, const windq_mat* X, const windq_adapters* adapters /*HOST or NULL*/,
                   const int32_t* adapter_of /*[tokens] or NULL*/, void* Y, int64_t ld_y, float* h /*[tokens][max_rank] or NULL*/,
@@ -681,17 +682,21 @@ int windq_project(const windq_packed* P /*HOST*/, const windq_mat* X, const wind
  *      to bfloat16 once, as dY is.
  *   dA [n][max_rank][cols], dB [n][rows][max_rank] f32, both or neither: written whole, zeros past an adapter's rank and for
  *      adapters without a token
- *   h  as windq_project left it, or NULL: formed again from X
+ *   h  as windq_project left it (for the same X and adapters), or NULL: formed again from X
  * adapters NULL: dX alone; X, adapter_of, h, dA, dB unused.  X may be NULL where dA and dB are.  P may be NULL: the adapters' gradients
  * alone, without the packed matrix's part of dX (rows and cols are those of dY's and X's descriptors).
- * Sums over tokens run in a fixed order: results are bit-reproducible.
+ * Sums are fp32 in a fixed order: results are bit-reproducible.  A dY, X or weight that is not finite makes what the formula multiplies
+ * it with not finite (infinities may come out as NaN); other tokens' dX and other adapters' gradients keep their values.
+ * X as for windq_project; dY, dX and their leading dimensions are free.  At most 2^31 - 1 tokens x rows and tokens x cols.
+ * Workspace: windq_project_workspace_bytes; in WINDQ_BF16 it has 2 bytes a weight for the reconstruction that dX goes through.
  */
 int windq_project_grad(const windq_packed* P /*HOST*/, const windq_mat* dY, const windq_mat* X /*or NULL*/,
                        const windq_adapters* adapters /*HOST or NULL*/, const int32_t* adapter_of /*[tokens] or NULL*/,
                        const float* h /*[tokens][max_rank] or NULL*/, void* dX /*or NULL*/, int64_t ld_dx,
                        float* dA /*or NULL*/, float* dB /*or NULL*/, void* ws, size_t ws_bytes, void* stream);
 
-/* Workspace of windq_project (grad = 0) or windq_project_grad (grad = 1); 0 if a size is out of range.  HOST only. */
+/* Workspace of windq_project (grad = 0) or windq_project_grad (grad = 1); 0 if a size is out of range.  It never shrinks with more
+ * tokens, so one for the largest batch does for all.  HOST only. */
 size_t windq_project_workspace_bytes(int32_t grad, int32_t dtype, int64_t tokens, int64_t rows, int64_t cols,
                                      int32_t chunk_w, int32_t n_adapters, int32_t max_rank);
 
