@@ -215,6 +215,7 @@ __device__ __forceinline__ void add_adapters(const AdapterArgs& A, const float* 
 #pragma unroll
                 for (int m = 0; m < TH; ++m) bt[m][n] = pack8(w[m]);
             }
+            bool broken = false;
 #pragma unroll
             for (int f = 0; f < M; ++f) {
                 float v[8] = {};
@@ -223,11 +224,29 @@ __device__ __forceinline__ void add_adapters(const AdapterArgs& A, const float* 
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float x = r + i < rank ? v[i] : 0.0f;
+                    broken |= !isfinite(x);
                     if (TA == 1) w[0][i] = __float_as_uint(x) >> 16;
                     else split3(x, w[0][i], w[1][i], w[2][i]);
                 }
 #pragma unroll
                 for (int m = 0; m < TA; ++m) at[m][f] = pack8(w[m]);
+            }
+            if (__any(broken)) {                            // times the other tokens' zeros they would be NaN: kept apart
+#pragma unroll
+                for (int f = 0; f < M; ++f)
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        f32x16 own = {};
+#pragma unroll
+                        for (int ma = 0; ma < TA; ++ma)
+#pragma unroll
+                            for (int mh = 0; mh < TH; ++mh)
+                                if (ma + mh < 3) own = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(at[ma][f]), as_bf16x8(bt[mh][n]), own, 0, 0, 0);
+                        const bool in = ((mine >> (n * 32 + sub)) & 1ull) != 0;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) tot[f][n][i] += in ? own[i] : 0.0f;
+                    }
+                continue;
             }
 #pragma unroll
             for (int ma = 0; ma < TA; ++ma)

@@ -61,6 +61,30 @@ def test_adapters_of_more_than_two_to_the_31_values(windq):
         del dx, da, db
 
 
+@pytest.mark.parametrize("rows,cols,T", [(1024, 512, 700), (256, 512, 300), (1024, 512, 40), (100, 160, 90)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_one_adapter_that_is_not_finite_leaves_the_other_requests_alone(windq, rows, cols, T, dtype):
+    g = torch.Generator().manual_seed(rows + T)
+    W = (0.02 * torch.randn(rows, cols, generator=g)).to(dtype).to(DEV)
+    packed = adapt.pack(W, torch.ones(cols, device=DEV), 32 if cols == 160 else 64)
+    a, b = (torch.randn(3, 16, cols, generator=g) / cols ** 0.5).to(dtype).to(DEV), (0.05 * torch.randn(3, rows, 16, generator=g)).to(dtype).to(DEV)
+    of = torch.randint(-1, 3, (T,), generator=g).to(torch.int32).to(DEV)
+    x, dy = torch.randn(T, cols, generator=g).to(dtype).to(DEV), torch.randn(T, rows, generator=g).to(dtype).to(DEV)
+
+    def both(a, b):
+        ad = windq.Adapters(a, b)
+        return windq.windq_project(packed, x, ad, of), *windq.windq_project_grad(packed, dy, x, ad, of)
+
+    clean, others = both(a, b), of != 1
+    for bad in (float("nan"), float("inf")):
+        a2, b2 = a.clone(), b.clone()
+        a2[1, 3, 5], b2[1, 7, 2] = bad, bad
+        y, dx, da, db = both(a2, b2)
+        assert torch.equal(y[others], clean[0][others]) and torch.equal(dx[others], clean[1][others])
+        assert torch.equal(da[[0, 2]], clean[2][[0, 2]]) and torch.equal(db[[0, 2]], clean[3][[0, 2]])
+        assert not torch.isfinite(y[~others][:, 7]).any() and not torch.isfinite(dx[~others][:, 5]).any()
+
+
 def test_the_binding_refuses(windq):
     bf, f32 = torch.bfloat16, torch.float32
     rows, cols, G, T = 64, 128, 64, 5
