@@ -7,8 +7,8 @@
 // that would leave CUs without a workgroup.
 //   64 of the sum at a time go to LDS by direct loads, three buffers: while one is multiplied the next has landed and the one
 // after is on its way.  There is one barrier per buffer, ahead of its last step: by then all of it has been read into registers, and the next
-// one's first operands are read across it.  A row's eight 16-byte slots are exchanged by the row's low bits, so that 32 lanes reading 32
-// rows' same slot meet all banks.
+// one's first operands are read across it.  A row's eight 16-byte slots are exchanged by the bits above the row's lowest, so that sixteen
+// lanes reading sixteen rows' same slot meet all 64 banks (two rows have a turn of them).
 #pragma once
 
 #include "windq_adapters.hpp"
@@ -56,16 +56,19 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
     __shared__ uint4 tile[GM_BUFFERS][(GM_M + GM_N) * 8];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, sub = lane & 31, hh = lane >> 5;
     const int wm = wave & 1, wn = wave >> 1;
-    // Consecutive workgroups land on the eight XCDs in turn; each XCD gets a run of tiles that share tokens.
+    // Consecutive workgroups land on the eight XCDs in turn; each XCD gets a run of tiles, four columns of tiles wide, so that it shares
+    // both factors: a run of whole rows of tiles would read all of wt into every XCD's L2.
     const uint32_t n_tiles = gridDim.x, per = n_tiles >> 3;
     const uint32_t id = blockIdx.x < per * 8 ? (blockIdx.x & 7) * per + (blockIdx.x >> 3) : blockIdx.x;
-    const uint32_t split = id / (uint32_t)Q.tiles, in = id - split * (uint32_t)Q.tiles, tb = in / Q.col_blocks;
-    const int64_t c0 = (int64_t)(in - tb * Q.col_blocks) * GM_M, t0 = (int64_t)tb * GM_N;
+    const uint32_t split = id / (uint32_t)Q.tiles, in = id - split * (uint32_t)Q.tiles, tall = (uint32_t)Q.tiles / Q.col_blocks;
+    const uint32_t band = in / (4 * tall), inside = in - band * (4 * tall), width = Q.col_blocks - band * 4 < 4 ? Q.col_blocks - band * 4 : 4;
+    const uint32_t tb = inside / width;
+    const int64_t c0 = (int64_t)(band * 4 + inside - tb * width) * GM_M, t0 = (int64_t)tb * GM_N;
     const int32_t first = (int32_t)split * Q.each, steps = Q.K / GM_K - first;
 
     // A lane's share of a tile: slot (lane & 7) of rows 8 wave + lane / 8, 32 rows further on each time; slot p of row r holds the
-    // sixteen bytes of slot p ^ (r & 7).
-    const int lr = wave * 8 + (lane >> 3), slot = (lane & 7) ^ (lr & 7);
+    // sixteen bytes of slot p ^ (r / 2 & 7).
+    const int lr = wave * 8 + (lane >> 3), slot = (lane & 7) ^ ((lr >> 1) & 7);
     const uint16_t* const am = Q.wt + (c0 + lr) * Q.K + first * GM_K + slot * 8;
     const uint16_t* bn[GM_N / 32];
 #pragma unroll
@@ -80,7 +83,7 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
     const uint32_t arow = (wm * WM + sub) * 128, brow = GM_M * 128 + (wn * 64 + sub) * 128;
     auto read_one = [&](int buf, int s, int i, bf16x8 (&a)[MF], bf16x8 (&b)[2]) {
         const char* const at = reinterpret_cast<const char*>(tile[buf]);
-        const uint32_t o = (uint32_t)((2 * s + hh) ^ (sub & 7)) * 16;
+        const uint32_t o = (uint32_t)((2 * s + hh) ^ ((sub >> 1) & 7)) * 16;
         if (i < 2) b[i] = as_bf16x8(*reinterpret_cast<const uint4*>(at + brow + i * 32 * 128 + o));
         else a[i - 2] = as_bf16x8(*reinterpret_cast<const uint4*>(at + arow + (i - 2) * 32 * 128 + o));
     };
