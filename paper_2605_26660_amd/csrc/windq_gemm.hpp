@@ -1,7 +1,7 @@
 // dX = w_hat^T dY in bfloat16: a plain product of two matrices whose rows lie along the sum's axis.
 //
 // Codes lie along columns and the sum runs along rows, so a tile of weights would have to be turned for every 128 tokens.  The packed
-// matrix is reconstructed once instead, rounded to bfloat16 and turned (wt [cols][rows], 2 bytes a weight; 35 of 294 us at 2048 tokens through
+// matrix is reconstructed once instead, rounded to bfloat16 and turned (wt [cols][rows], 2 bytes a weight; 33 of 286 us at 2048 tokens through
 // 11008 x 4096; for one token too: 4096 x 4096 45 us, 373 with tiles turned on the way), and the product then spends nothing but matrix instructions and their operands' way: 256 columns x 128
 // tokens a workgroup, four wavefronts with 128 x 64 results each as 4 x 2 fragments of 32x32x16 instructions, one per SIMD; 128 columns where
 // that would leave CUs without a workgroup.

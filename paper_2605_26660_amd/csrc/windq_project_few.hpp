@@ -7,6 +7,8 @@
 //   X is read by every workgroup, so a kernel ahead (with the adapters' first half, if there is one) lays it out in the order in which the
 // lanes want it, 1 KB a load, and sums it up.  Up to FEW_DIRECT tokens it is read as it lies, and summed up by instructions with ones for weights.
 //   Totals meet in LDS, in the order of the wavefronts.
+//   1 token through 4096 x 4096 at 2 bits 12 us (+ 3 for h), 48 tokens of 32 adapters through 11008 x 4096 46 us (+ 5): two rounds of workgroups, waits are 58 % of
+// the wavefronts' time.
 #pragma once
 
 #include "windq_project_tiles.hpp"
