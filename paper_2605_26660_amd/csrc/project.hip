@@ -283,7 +283,7 @@ int launch_tiles(const ProjectArgs& Q, char* ws, const ProjectWs& at, hipStream_
     A.n_kb = (int32_t)(Q.P.cols / (16 * S));
     A.row_blocks = (uint32_t)((Q.P.rows + PT_ROWS - 1) / PT_ROWS);
     const int64_t strips = (Q.P.rows / Q.P.R_u) * Q.P.n_chunks * ((Q.P.R_u + PT_STRIP - 1) / PT_STRIP);
-    const int64_t wgs = strips + (A.n_kb * Q.T + 255) / 256;
+    const int64_t wgs = strips + tokens_in(A.n_kb * Q.T, PT_SUMS);
     const int64_t tiles = (int64_t)A.row_blocks * ((Q.T + PT_TOKENS - 1) / PT_TOKENS);
     if (!fits_launch(wgs, 256) || !fits_launch(tiles, PT_THREADS)) return WINDQ_ESHAPE;
     tiles_prepare_kernel<XT, S><<<dim3((uint32_t)wgs), dim3(256), 0, st>>>(A, strips);

@@ -14,7 +14,7 @@
 // bfloat16 terms, six products in eight of an instruction's sixteen k, so one instruction does two k-blocks.
 //   Trits and 3-bit codes are laid out as 2- and 4-bit fields before (by the kernel that sums x): a row of them is visited by
 // T / 128 workgroups, and taking trits apart costs more than everything else in the loop.
-//   2000 tokens through 4096 x 11008 at 2 bits: 195 to 225 us (800 to 920 TFLOP/s) + 26 for laying out; 4096 through 13824 x 5120 with 4 adapters of 64
+//   2000 tokens through 4096 x 11008 at 2 bits: 195 to 225 us (800 to 920 TFLOP/s) + 22 for laying out; 4096 through 13824 x 5120 with 4 adapters of 64
 // ranks 780 in all.  27560 vector instructions against 2944 matrix instructions a wavefront: neither unit is full, waits are 46 % of the wavefronts' time.
 #pragma once
 
@@ -24,6 +24,7 @@ namespace windq {
 
 constexpr int PT_ROWS = 256, PT_TOKENS = 128, PT_THREADS = 512;
 constexpr int PT_STRIP = 64;                               // rows of a unit that one workgroup lays out
+constexpr int PT_SUMS = 16;                                // tokens whose sums over a k-block one workgroup forms
 
 // Where a unit's fields begin (48 bits of address), how many bits they have (8) and what they are (kind, top byte): 0 skip, 1: 8 bits,
 // 2: 4 bits, 4: 2 bits, 5: trits as 2 bits, 6: 1 bit.
@@ -76,21 +77,28 @@ __global__ __launch_bounds__(256) void tiles_prepare_kernel(const TileArgs Q, co
     const PackArgs& P = Q.P;
     const int32_t per_chunk = P.G / (16 * S);
     if (blockIdx.x >= strips) {
-        const int64_t i = (blockIdx.x - strips) * 256 + threadIdx.x;
-        const int32_t kb = (int32_t)(i / Q.T);
-        const int64_t t = i - (int64_t)kb * Q.T;
-        if (kb >= Q.n_kb) return;
-        const XT* __restrict__ const x = static_cast<const XT*>(Q.raw) + t * Q.ld_raw + (int64_t)kb * (16 * S);
-        float sum = 0.0f;
-#pragma unroll
-        for (int o = 0; o < 2 * S; ++o) {
-            float v[8];
-            load8(x + o * 8, v);
-            sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        // sixteen lanes a token, an octet each
+        const int64_t first = (blockIdx.x - strips) * PT_SUMS;
+        int32_t kb = (int32_t)(first / Q.T);
+        int64_t t = first - (int64_t)kb * Q.T + (threadIdx.x >> 4);
+        if (t >= Q.T) {                                     // there are more tokens than a workgroup sums up
+            t -= Q.T;
+            ++kb;
         }
+        if (kb >= Q.n_kb) return;
+        const int o = threadIdx.x & 15;
+        float sum = 0.0f;
+        if (o < 2 * S) {
+            float v[8];
+            load8(static_cast<const XT*>(Q.raw) + t * Q.ld_raw + (int64_t)kb * (16 * S) + o * 8, v);
+            sum = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        }
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 16);
+        if (o != 0) return;
         uint32_t hi, mid, lo;
         split3(sum, hi, mid, lo);
-        Q.xs[i] = make_uint4(hi | mid << 16, hi | lo << 16, hi | mid << 16, 0u);
+        Q.xs[(int64_t)kb * Q.T + t] = make_uint4(hi | mid << 16, hi | lo << 16, hi | mid << 16, 0u);
         return;
     }
     const int64_t per_unit = (P.R_u + PT_STRIP - 1) / PT_STRIP;
