@@ -248,7 +248,7 @@ ProjectWs project_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32
     w.owner = take(grouped ? (size_t)slots * 4 : 0);
     w.first = take(grouped ? (size_t)n * 4 : 0);
     w.count = take(grouped ? (size_t)n * 4 : 0);
-    w.part = take(grouped ? (size_t)shrink_pieces(slots, cols) * GROUP * (size_t)shrink_ranks(max_rank) * 4 : 0);
+    w.part = take(grouped ? shrink_floats(slots, cols, max_rank) * 4 : 0);
     const bool many = T > PROJECT_FEW;
     w.fields = take(many ? (size_t)(rows * cols) / (G == 128 || G == 96 || G == 64 ? 2 : 1) : 0);
     w.unit = take(many ? (size_t)((rows + PT_STRIP - 1) / PT_STRIP) * (size_t)(cols / 64) * sizeof(KbWord) : 0);

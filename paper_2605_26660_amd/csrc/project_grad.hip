@@ -567,7 +567,7 @@ GradWs grad_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t n, 
     const size_t eb = dtype == WINDQ_F32 ? 4 : 2;
     const bool bf = dtype == WINDQ_BF16;
     GradWs w;
-    w.ld = bf ? gemm_k(rows) : (rows + 7) / 8 * 8;
+    w.ld = bf ? gemm_k(rows) : in_eights(rows);
     size_t at = 0;
     auto take = [&at](size_t bytes) {
         const size_t here = at;
@@ -575,7 +575,6 @@ GradWs grad_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t n, 
         return here;
     };
     const int64_t slots = group_slots(T, n);
-    const int64_t wide = rows > cols ? rows : cols;
     w.dy = take((size_t)(T * w.ld) * eb);
     w.h = take((size_t)(T * max_rank) * 4);
     w.dh = take((size_t)(T * max_rank) * 4);
@@ -585,8 +584,8 @@ GradWs grad_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t n, 
     w.owner = take((size_t)slots * 4);
     w.first = take((size_t)n * 4);
     w.count = take((size_t)n * 4);
-    w.part = take(bf && n > 0 ? (size_t)shrink_pieces(slots, wide) * GROUP * (size_t)shrink_ranks(max_rank) * 4 : 0);
-    w.part2 = take(bf && n > 0 ? (size_t)shrink_pieces(slots, wide) * GROUP * (size_t)shrink_ranks(max_rank) * 4 : 0);
+    w.part = take(bf && n > 0 ? shrink_floats(slots, in_eights(rows), max_rank) * 4 : 0);        // dh's pieces
+    w.part2 = take(bf && n > 0 ? shrink_floats(slots, cols, max_rank) * 4 : 0);                  // h's
     w.planes_h = take(bf && n > 0 ? (size_t)slots * GROUP * (size_t)max_rank * 6 : 0);
     w.planes_dh = take(bf && n > 0 ? (size_t)slots * GROUP * (size_t)max_rank * 6 : 0);
     w.wt = take(bf && T > 0 ? (size_t)gemm_cols(cols) * (size_t)gemm_k(rows) * 2 : 0);
@@ -627,7 +626,7 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
         Q.ldy = dY->ld;
     }
     const XT* const dYv = static_cast<const XT*>(Q.dY);
-    const int32_t rows8 = (int32_t)((rows + 7) / 8 * 8);
+    const int32_t rows8 = (int32_t)in_eights(rows);
     PrepareArgs<XT> R = {};
     R.P = Q.P;
     R.A = A;

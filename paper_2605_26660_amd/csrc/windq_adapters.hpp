@@ -73,6 +73,9 @@ inline int64_t shrink_pieces(int64_t slots, int64_t width) {
     const int64_t most = slots * splits < 512 ? slots * splits : 512;
     return most > slots ? most : slots;
 }
+// Floats of ShrinkArgs::part for sums over so many columns: the width that is launched, B transposed and dY have their rows in eights.
+inline size_t shrink_floats(int64_t slots, int64_t width, int32_t max_rank) { return (size_t)shrink_pieces(slots, width) * GROUP * (size_t)shrink_ranks(max_rank); }
+inline int64_t in_eights(int64_t rows) { return (rows + 7) / 8 * 8; }
 
 #ifdef __HIPCC__
 

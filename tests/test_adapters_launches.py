@@ -1,0 +1,26 @@
+"""What windq_project, windq_project_grad and windq_adamw launch, and what of the workspace they hand to it: the host code alone, without a GPU."""
+import random
+
+from host_launches import recorder  # noqa: F401
+
+
+def apart(regions, at, need):
+    """The regions lie in the workspace and none reaches into another."""
+    ends = sorted(regions)
+    return all(at <= a <= b <= at + need for a, b in ends) and all(x[1] <= y[0] for x, y in zip(ends, ends[1:]))
+
+
+def test_pieces_of_the_adapters_sums_stay_in_their_own_part_of_the_workspace(recorder):
+    """Pieces are as many as the width allows, and dY's width is that of its rows in eights."""
+    rng = random.Random(1)
+    shapes = [(511, 256, 100, 2), (1023, 512, 700, 3), (4095, 4088, 64, 1)]
+    for k in range(2, 33):
+        shapes += [(256 * k - rng.randint(0, 9), 8 * rng.randint(1, 32 * k), rng.choice([1, 65, 100, 700, 3000]), rng.choice([1, 2, 5, 40])) for _ in range(6)]
+    for rows, cols, T, n in shapes:
+        for h in (False, True):
+            status, at, need = recorder.product(True, T, rows, cols, 8, n=n, rank=16, h=h)
+            assert status == 0
+            regions = recorder.regions()
+            assert len(regions) == (3 if h else 4) and apart(regions, at, need), (rows, cols, T, n, h)
+            status, at, need = recorder.product(False, T, rows, cols, 8, n=n, rank=16, h=h)
+            assert status == 0 and apart(recorder.regions(), at, need)
