@@ -1003,9 +1003,11 @@ class AdamwItems:
     """The tensors of an AdamW step (lists of equal length): parameters (all float32 or all bfloat16), their gradients
     (likewise), first moments and second moments, float32 or, in 8 bits, float8_e4m3fn (or its bytes, uint8) with the float32 scales
     m_scales and v_scales, one for every ADAMW_BLOCK values; copies: bfloat16 copies of the parameters to be written, or None.
-    Checked and described once; it keeps the tensors."""
+    Checked and described once; it keeps the tensors, not the lists: what becomes of those later changes nothing."""
 
     def __init__(self, params, grads, ms, vs, m_scales=None, v_scales=None, copies=None):
+        # the caller's lists may change later; the addresses below are these tensors'
+        params, grads, ms, vs, m_scales, v_scales, copies = (None if x is None else tuple(x) for x in (params, grads, ms, vs, m_scales, v_scales, copies))
         n = len(params)
         lists = [grads, ms, vs] + [x for x in (m_scales, v_scales, copies) if x is not None]
         if any(len(x) != n for x in lists) or (m_scales is None) != (v_scales is None):
