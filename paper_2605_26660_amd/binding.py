@@ -937,6 +937,14 @@ def _check_side(packed, adapters, adapter_of, h, tokens, where):
     _require_cuda(adapter_of, h)
 
 
+def _rows_apart(t, where):
+    """The leading dimension of an output: its rows do not overlap (of a single row, or none, any stride will do)."""
+    T, width = t.shape
+    if T > 1 and t.stride(0) < width:
+        raise WindqError(WINDQ_ESHAPE, where)
+    return max(t.stride(0), width)
+
+
 def windq_project(packed: Packed, X: torch.Tensor, adapters: Adapters | None = None, adapter_of: torch.Tensor | None = None,
                   h: torch.Tensor | None = None, ws: torch.Tensor | None = None, out: torch.Tensor | None = None):
     """Y [tokens x rows] of X's type: X [tokens x cols] (float32 or bfloat16) through the packed matrix, and through the adapter
@@ -947,11 +955,12 @@ def windq_project(packed: Packed, X: torch.Tensor, adapters: Adapters | None = N
     y = out if out is not None else torch.empty(T, packed.rows, dtype=X.dtype, device=X.device)
     if y.dtype != X.dtype or tuple(y.shape) != (T, packed.rows) or y.stride(1) != 1:
         raise WindqError(WINDQ_EDTYPE if y.dtype != X.dtype else WINDQ_ESHAPE, "windq_project")
+    ld_y = _rows_apart(y, "windq_project")
     if ws is None:
         ws = project_workspace(packed, X, adapters)
     m = _mats((X,))
     _check(_packed().windq_project(packed.address, _addr(m), None if adapters is None else adapters.address, _ptr(adapter_of), y.data_ptr(),
-                                   max(y.stride(0), packed.rows), _ptr(h), ws.data_ptr(), ws.numel(), _stream()), "windq_project")
+                                   ld_y, _ptr(h), ws.data_ptr(), ws.numel(), _stream()), "windq_project")
     return y
 
 
@@ -988,13 +997,14 @@ def windq_project_grad(packed: Packed | None, dY: torch.Tensor, X: torch.Tensor 
         da = db = None
     if dx is not None and (dx.dtype != dY.dtype or tuple(dx.shape) != (T, shape.cols) or dx.stride(1) != 1):
         raise WindqError(WINDQ_EDTYPE if dx.dtype != dY.dtype else WINDQ_ESHAPE, "windq_project_grad")
+    ld_dx = shape.cols if dx is None else _rows_apart(dx, "windq_project_grad")
     if ws is None:
         ws = project_workspace(packed, dY, adapters, grad=True)
     m = _mats((dY,) if X is None else (dY, X))
     at = _addr(m)
     _check(_packed().windq_project_grad(None if packed is None else packed.address, at, None if X is None else at + 8 * _MAT_WORDS,
                                         None if adapters is None else adapters.address, _ptr(adapter_of), _ptr(h), _ptr(dx),
-                                        shape.cols if dx is None else max(dx.stride(0), shape.cols), _ptr(da), _ptr(db), ws.data_ptr(), ws.numel(),
+                                        ld_dx, _ptr(da), _ptr(db), ws.data_ptr(), ws.numel(),
                                         _stream()), "windq_project_grad")
     return dx, da, db
 
