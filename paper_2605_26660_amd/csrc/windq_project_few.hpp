@@ -43,8 +43,10 @@ inline int64_t few_most(int64_t rows, int64_t cols, int32_t G) {
     const int64_t most = 256 * rounds / tokens_in(rows, PF_ROWS) * 64;
     return most > FEW_ALWAYS ? most : FEW_ALWAYS;
 }
+// Codes are read in whole pieces of 16 bytes, and units start on 16: a stream that ends between two (the last unit then may, too; the plan's layout
+// leaves none such) is left to the kernels that read codes as they are.
 inline bool few_fits(const PackArgs& P, int64_t T) {
-    if (T > few_most(P.rows, P.cols, P.G)) return false;
+    if (T > few_most(P.rows, P.cols, P.G) || (P.codes_bytes & 15) != 0) return false;
     return P.mask == nullptr && P.rows % 8 == 0 && (P.R_u == P.rows || P.R_u % PF_ROWS == 0) && (P.G % 128 == 0 || P.G == 96 || P.G == 64);
 }
 
@@ -146,7 +148,7 @@ __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q
             const uint8_t* const from = P.codes + base + lrow0 * bpg;
             if (kind == 5 || per_chunk == 1) {              // whole rows, one behind the other
                 stride = (int32_t)bpg;
-                const int32_t most = (rows_left * stride + 15) / 16 - 1;       // a unit ends on 16 bytes
+                const int32_t most = (rows_left * stride + 15) / 16 - 1;       // up to 8 bytes past the unit: the stream has them
                 for (int32_t i0 = 0; i0 * 16 < PF_ROWS * stride; i0 += 64)
                     lds_load16(lds_codes + i0 * 16, from + (i0 + lane < most ? i0 + lane : most) * 16);
             } else {                                        // 128 columns of wider rows: pieces of 16 bytes, as many as a code has bits

@@ -24,3 +24,18 @@ def test_pieces_of_the_adapters_sums_stay_in_their_own_part_of_the_workspace(rec
             assert len(regions) == (3 if h else 4) and apart(regions, at, need), (rows, cols, T, n, h)
             status, at, need = recorder.product(False, T, rows, cols, 8, n=n, rank=16, h=h)
             assert status == 0 and apart(recorder.regions(), at, need)
+
+
+def names(recorder):
+    return " ".join(x.name for x in recorder.launches())
+
+
+def test_codes_are_read_in_whole_pieces_only_where_the_stream_has_them_whole(recorder):
+    """The kernel for few tokens reads a unit's codes 16 bytes at a time, and units start on 16: a stream of whole pieces holds the last one whole."""
+    for rows, G in ((8, 64), (40, 128), (24, 384)):
+        for T in (1, 40):
+            status, _, _ = recorder.product(False, T, rows, 4 * G, G, codes_bytes=4096)
+            assert status == 0 and "project_few_kernel" in names(recorder)
+            for left in (1, 8, 15):                          # 8 rows of 1.58 bits at G = 64 are 104 bytes
+                status, _, _ = recorder.product(False, T, rows, 4 * G, G, codes_bytes=4096 + left)
+                assert status == 0 and "project_few_kernel" not in names(recorder) and "project_kernel" in names(recorder)
