@@ -214,7 +214,7 @@ __device__ __forceinline__ void add_adapters(const AdapterArgs& A, const float* 
                 if (has) load8(h + (t0 + n * 32 + sub) * A.max_rank + r, v);
                 uint32_t w[3][8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) split3(r + i < rank ? factor * v[i] : 0.0f, w[0][i], w[1][i], w[2][i]);
+                for (int i = 0; i < 8; ++i) split3(has && r + i < rank ? factor * v[i] : 0.0f, w[0][i], w[1][i], w[2][i]);      // a factor that is not finite: its own tokens' alone
 #pragma unroll
                 for (int m = 0; m < TH; ++m) bt[m][n] = pack8(w[m]);
             }

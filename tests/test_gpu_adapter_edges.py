@@ -22,3 +22,33 @@ def test_a_code_stream_that_ends_with_its_last_code(windq, rows, G):
         x = X.double().cpu().numpy()
         want = x @ c.w.T
         near(windq.windq_project(packed, X), want, y_tol(c, x, torch.bfloat16, want))
+
+
+def three(windq, rows, cols, T, dtype, seed):
+    """Three adapters beside a packed matrix: (packed, a, b, adapter_of, x, dy)."""
+    g = torch.Generator().manual_seed(seed)
+    c = Case(windq, rows, cols, 128, 0, dtype, seed=seed)
+    a, b = (torch.randn(3, 16, cols, generator=g) / cols ** 0.5).to(dtype).to(DEV), (0.05 * torch.randn(3, rows, 16, generator=g)).to(dtype).to(DEV)
+    of = torch.randint(-1, 3, (T,), generator=g).to(torch.int32).to(DEV)
+    return c, a, b, of, tokens(T, cols, dtype, seed + 1), tokens(T, rows, dtype, seed + 2)
+
+
+# for few tokens, for any shape, and tiles (1024 rows, 4 k-blocks: more than 512 tokens)
+ROUTES = [(256, 512, 40), (256, 512, 300), (1024, 512, 700), (100, 256, 90)]
+
+
+@pytest.mark.parametrize("rows,cols,T", ROUTES)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_factor_that_is_not_finite_leaves_the_other_requests_alone(windq, rows, cols, T, dtype):
+    c, a, b, of, x, dy = three(windq, rows, cols, T, dtype, 1)
+
+    def both(alpha):
+        ad = windq.Adapters(a, b, torch.tensor(alpha, device=DEV))
+        return windq.windq_project(c.packed, x, ad, of), *windq.windq_project_grad(c.packed, dy, x, ad, of)
+
+    clean, others = both([0.5, 2.0, 1.5]), of != 1
+    for bad in (float("nan"), float("inf"), float("-inf")):
+        y, dx, da, db = both([0.5, bad, 1.5])
+        assert torch.equal(y[others], clean[0][others]) and torch.equal(dx[others], clean[1][others])
+        assert torch.equal(da[[0, 2]], clean[2][[0, 2]]) and torch.equal(db[[0, 2]], clean[3][[0, 2]])
+        assert not torch.isfinite(y[~others]).any() and not torch.isfinite(dx[~others]).any()
