@@ -220,7 +220,7 @@ __global__ __launch_bounds__(OUTER_THREADS) void outer_tiles_kernel(const OuterA
     for (int e = threadIdx.x; e < ranks * OUTER_COLS; e += OUTER_THREADS) {
         const int r = Q.by_column ? e % ranks : e / OUTER_COLS, c = Q.by_column ? e / ranks : e % OUTER_COLS;
         if (c >= cols) continue;
-        const float v = r0 + r < rank ? factor * red[0][r][c] : 0.0f;
+        const float v = r0 + r < rank && n > 0 ? factor * red[0][r][c] : 0.0f;
         if (Q.by_column) Q.out[((int64_t)k * Q.width + c0 + c) * R + r0 + r] = v;
         else Q.out[((int64_t)k * R + r0 + r) * Q.width + c0 + c] = v;
     }

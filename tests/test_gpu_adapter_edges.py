@@ -52,3 +52,14 @@ def test_a_factor_that_is_not_finite_leaves_the_other_requests_alone(windq, rows
         assert torch.equal(y[others], clean[0][others]) and torch.equal(dx[others], clean[1][others])
         assert torch.equal(da[[0, 2]], clean[2][[0, 2]]) and torch.equal(db[[0, 2]], clean[3][[0, 2]])
         assert not torch.isfinite(y[~others]).any() and not torch.isfinite(dx[~others]).any()
+
+
+@pytest.mark.parametrize("T", [0, 3, 90, 700])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_an_adapter_without_tokens_has_no_gradient_whatever_its_factor(windq, T, dtype):
+    c, a, b, of, x, dy = three(windq, 256, 256, T, dtype, 2)
+    of[of == 1] = 0
+    for bad in (float("nan"), float("inf")):
+        ad = windq.Adapters(a, b, torch.tensor([0.5, bad, 1.5], device=DEV))
+        _, da, db = windq.windq_project_grad(c.packed, dy, x, ad, of)
+        assert torch.all(da[1] == 0) and torch.all(db[1] == 0) and torch.all(torch.isfinite(da)) and torch.all(torch.isfinite(db))
