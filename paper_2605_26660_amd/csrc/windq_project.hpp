@@ -57,11 +57,12 @@ __device__ __forceinline__ uint32_t f32_to_bf16_bits(float x) {
     return (uint32_t)__builtin_bit_cast(uint16_t, b);
 }
 
-// x as three bfloat16 terms that add up to it (24 bits of mantissa).  What is not finite is its first term alone.
+// x as three bfloat16 terms that add up to it (24 bits of mantissa).  What is not finite is its first term alone.  Finite values that would round
+// to infinity, from 2^128 - 2^119 on, have bfloat16's largest one for their first term.
 __device__ __forceinline__ void split3(float x, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
-    hi = f32_to_bf16_bits(x);
+    hi = f32_to_bf16_bits(x) - ((__float_as_uint(x) & 0x7fff8000u) == 0x7f7f8000u ? 1u : 0u);
     float r = x - bf16_bits_to_f32(hi);
-    const bool fine = (__float_as_uint(r) & 0x7f800000u) != 0x7f800000u;      // x, and x rounded, are finite
+    const bool fine = (__float_as_uint(r) & 0x7f800000u) != 0x7f800000u;      // x is finite
     r = fine ? r : 0.0f;
     mid = f32_to_bf16_bits(r);
     lo = f32_to_bf16_bits(r - bf16_bits_to_f32(mid));

@@ -63,3 +63,37 @@ def test_an_adapter_without_tokens_has_no_gradient_whatever_its_factor(windq, T,
         ad = windq.Adapters(a, b, torch.tensor([0.5, bad, 1.5], device=DEV))
         _, da, db = windq.windq_project_grad(c.packed, dy, x, ad, of)
         assert torch.all(da[1] == 0) and torch.all(db[1] == 0) and torch.all(torch.isfinite(da)) and torch.all(torch.isfinite(db))
+
+
+@pytest.mark.parametrize("rows,cols,T", ROUTES)
+@pytest.mark.parametrize("top", [3.4e38, -3.4e38])
+def test_the_largest_fp32_values_are_values(windq, rows, cols, T, top):
+    """fp32 above bfloat16's largest value is finite: in an adapter (the other requests keep their bits, its own follow the formula) and in h."""
+    c, a, b, of, x, dy = three(windq, rows, cols, T, torch.float32, 3)
+
+    def y_of(a, b):
+        return windq.windq_project(c.packed, x, windq.Adapters(a, b), of)
+
+    clean, others = y_of(a, b), of != 1
+    a2, b2 = a.clone(), b.clone()
+    a2[1, 2] *= 1e-30
+    b2[1, 7, 2] = top
+    b2[1, rows - 1, 2] = top / 1.0000001
+    y = y_of(a2, b2)
+    assert torch.equal(y[others], clean[others])
+    x64, mine = x.double().cpu().numpy(), (~others).cpu().numpy()
+    A, B = a2[1].double().cpu().numpy(), b2[1].double().cpu().numpy()
+    want, mag = x64[mine] @ c.w.T + x64[mine] @ A.T @ B.T, np.abs(x64[mine]) @ c.mag.T + np.abs(x64[mine]) @ np.abs(A).T @ np.abs(B).T
+    near(y[~others], want, EPS * mag)
+    # the same for h: an A whose sums come close to the largest value, a B that brings them back
+    a3, b3 = torch.zeros_like(a), b.clone()
+    a3[:, :, 0] = top
+    x1 = x.clone()
+    x1[:, 0] = 1.0
+    b3 *= 1e-20
+    y = windq.windq_project(c.packed, x1, windq.Adapters(a3, b3), of)
+    x64, on = x1.double().cpu().numpy(), (of >= 0).cpu().numpy()
+    B = b3.double().cpu().numpy()[np.maximum(of.cpu().numpy(), 0)]
+    h = float(np.float32(top)) * np.ones(16)
+    side = (B @ h) * on[:, None]
+    near(y, x64 @ c.w.T + side, EPS * (np.abs(x64) @ c.mag.T + np.abs(B) @ np.abs(h) * on[:, None]))
