@@ -665,7 +665,8 @@ typedef struct windq_adapters {
  * results are bit-reproducible and differ from the exact sum by a few 1e-7 of sum |w_hat x| before Y's own rounding.
  * A result that is not finite is formed again weight by weight in fp64, so infinities and NaN of x, of scales and of skip
  * weights come out as the formula has them, in their own token's and row's results only.
- * X is 16-byte aligned with a leading dimension that is a multiple of 8; Y and ld_y are free.  At most 2^31 - 1 tokens x rows.
+ * X is 16-byte aligned with a leading dimension that is a multiple of 8; Y and ld_y are free.  At most 2^31 - 1 tokens x rows, 2^31 - 512 rows
+ * and as many columns; no tensor of more than 2^40 values (WINDQ_ESHAPE beyond, as for windq_project_grad).
  * Workspace: windq_project_workspace_bytes (256-byte aligned), written anew by every call.
  */
 int windq_project(const windq_packed* P /*HOST*/, const windq_mat* X, const windq_adapters* adapters /*HOST or NULL*/,

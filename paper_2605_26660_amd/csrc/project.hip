@@ -358,8 +358,8 @@ using namespace windq;
 extern "C" size_t windq_project_workspace_bytes(int32_t grad, int32_t dtype, int64_t tokens, int64_t rows, int64_t cols,
                                                 int32_t chunk_w, int32_t n_adapters, int32_t max_rank) {
     if ((dtype != WINDQ_F32 && dtype != WINDQ_BF16) || tokens < 0 || rows <= 0 || cols <= 0 || chunk_w <= 0 || n_adapters < 0 || max_rank < 0) return 0;
-    if (tokens > ((int64_t)1 << 31) - 1 || rows > (int64_t)1 << 31 || cols > (int64_t)1 << 31 || max_rank > WINDQ_MAX_RANK) return 0;
-    if (n_adapters == 0) max_rank = 0;
+    if (n_adapters == 0 && max_rank <= WINDQ_MAX_RANK) max_rank = 0;
+    if (!sizes_fit(tokens, rows, cols, n_adapters, max_rank) || (grad != 0 && !grad_sizes_fit(tokens, rows, cols))) return 0;
     return grad != 0 ? grad_ws_bytes(dtype, tokens, rows, cols, n_adapters, max_rank) : project_ws(dtype, tokens, rows, cols, chunk_w, n_adapters, max_rank).total;
 }
 
@@ -377,6 +377,7 @@ extern "C" int windq_project(const windq_packed* P, const windq_mat* X, const wi
         if (!aligned(h, 16)) return WINDQ_EINVAL;
     }
     const size_t eb = X->dtype == WINDQ_F32 ? 4 : 2;
+    if (!sizes_fit(X->rows, Q.P.rows, Q.P.cols, Q.A.n, Q.A.max_rank)) return WINDQ_ESHAPE;
     if (ld_y < Q.P.rows || ld_y > (int64_t)1 << 31) return WINDQ_ESHAPE;
     if (X->rows == 0) return WINDQ_OK;
     if (X->rows * Q.P.rows > (int64_t)0x7fffffff) return WINDQ_ESHAPE;

@@ -768,7 +768,7 @@ extern "C" int windq_project_grad(const windq_packed* P, const windq_mat* dY, co
     status = check_tokens(dY, Q.P.rows, false);
     if (status != WINDQ_OK) return status;
     const int64_t T = dY->rows;
-    if (T * Q.P.rows > (int64_t)0x7fffffff || T * Q.P.cols > (int64_t)0x7fffffff) return WINDQ_ESHAPE;
+    if (!grad_sizes_fit(T, Q.P.rows, Q.P.cols)) return WINDQ_ESHAPE;
     if ((dA == nullptr) != (dB == nullptr)) return WINDQ_EINVAL;
     if (adapters != nullptr) {
         static const int32_t nobody = -1;
@@ -786,6 +786,7 @@ extern "C" int windq_project_grad(const windq_packed* P, const windq_mat* dY, co
     }
     if (dX == nullptr && dA == nullptr && T > 0) return WINDQ_EINVAL;
     const size_t eb = dY->dtype == WINDQ_F32 ? 4 : 2;
+    if (!sizes_fit(T, Q.P.rows, Q.P.cols, Q.A.n, Q.A.max_rank)) return WINDQ_ESHAPE;
     if (dX != nullptr) {
         if (ld_dx < Q.P.cols || ld_dx > (int64_t)1 << 31) return WINDQ_ESHAPE;
         if (!aligned(dX, eb)) return WINDQ_EINVAL;

@@ -7,6 +7,16 @@ namespace windq {
 
 inline int64_t tokens_in(int64_t T, int64_t by) { return (T + by - 1) / by; }
 
+// Kernels count a side's values in 32 bits, some of them up to a step past its end; and no tensor of more than 2^40 values fits a card, so that
+// bytes counted from what is left never pass 64 bits.
+constexpr int64_t MOST_SIDE = ((int64_t)1 << 31) - 512, MOST_VALUES = (int64_t)1 << 40;
+inline bool sizes_fit(int64_t T, int64_t rows, int64_t cols, int32_t n, int32_t max_rank) {
+    if (T > ((int64_t)1 << 31) - 1 || rows > MOST_SIDE || cols > MOST_SIDE || n > WINDQ_MAX_ADAPTERS || max_rank > WINDQ_MAX_RANK) return false;
+    const int64_t wide = rows > cols ? rows : cols;
+    return rows * cols <= MOST_VALUES && T * wide <= MOST_VALUES && (int64_t)n * max_rank * wide <= MOST_VALUES;
+}
+inline bool grad_sizes_fit(int64_t T, int64_t rows, int64_t cols) { return T * rows <= (int64_t)0x7fffffff && T * cols <= (int64_t)0x7fffffff; }
+
 // The tokens of adapter k in their own order, at places that start with a multiple of GROUP: place[] holds tokens, -1 where there is none.
 // Adapter k's first slot of GROUP places is (tokens of adapters below it) / GROUP + k: slots never overlap, and no adapter
 // has to wait for the counts of the others.

@@ -39,3 +39,21 @@ def test_codes_are_read_in_whole_pieces_only_where_the_stream_has_them_whole(rec
             for left in (1, 8, 15):                          # 8 rows of 1.58 bits at G = 64 are 104 bytes
                 status, _, _ = recorder.product(False, T, rows, 4 * G, G, codes_bytes=4096 + left)
                 assert status == 0 and "project_few_kernel" not in names(recorder) and "project_kernel" in names(recorder)
+
+
+def test_sizes_that_no_card_holds_are_refused_instead_of_wrapping_round(recorder):
+    """Bytes of a workspace are counted in 64 bits: what would pass them, or a side that a kernel's 32-bit index would, is out of range."""
+    L, F, B = recorder.lib, 0, 1
+    side = (1 << 31) - 512
+    for grad, dtype, T, rows, cols, G, n, rank in ((0, F, (1 << 31) - 1, 1, 1 << 31, 8, 0, 0), (0, F, 1 << 30, 1, side, 8, 0, 0), (1, F, 8, 8, side + 8, 8, 0, 0),
+                                                   (1, B, 1, side + 8, 8, 8, 0, 0), (0, F, 1, 1, 1 << 31, 512, 0, 0), (1, B, 10, side, side, 8, (1 << 20), 128),
+                                                   (1, B, 1000, side, 8, 8, 0, 0), (1, B, 1000, 8, side, 8, 0, 0), (0, B, 10, 64, 64, 64, (1 << 20) + 1, 8),
+                                                   (0, B, 10, 1 << 24, 1 << 24, 64, 0, 0), (0, B, 10, 64, 1 << 24, 64, 1 << 20, 128)):
+        assert L.windq_project_workspace_bytes(grad, dtype, T, rows, cols, G, n, rank) == 0
+        status, _, _ = recorder.product(grad, T, rows, cols, G, dtype=dtype, n=n, rank=rank)
+        assert status == 2 and not recorder.launches()            # WINDQ_ESHAPE
+    for grad in (0, 1):                                       # whatever comes out is what the parts add up to
+        for dtype in (F, B):
+            for T, rows, cols in ((1, 1 << 24, 1 << 12), (1 << 17, 1 << 13, 1 << 13), (100, 1 << 14, 1 << 20)):
+                planes = 6 * T * cols if dtype == F and not grad else 2 * rows * cols if dtype == B and grad else 0
+                assert planes <= L.windq_project_workspace_bytes(grad, dtype, T, rows, cols, 128, 0, 0) < 1 << 44
