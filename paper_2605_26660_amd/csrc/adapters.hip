@@ -15,10 +15,11 @@ int launch_group(const GroupArgs& G, hipStream_t st) {
 // are rows along the sum's axis, so operands come straight from memory; ranks are the M side.  Bound by reading X once:
 // 2048 tokens of 4096 and of 11008 columns by 64 ranks, both in one launch, 32 us (3.2 TB/s).
 template <int RF>
-__global__ __launch_bounds__(256) void shrink_kernel(const ShrinkArgs Q1, const ShrinkArgs Q2, const int64_t first2) {
+__global__ __launch_bounds__(256) void shrink_kernel(const ShrinkArgs Q1, const ShrinkArgs Q2, const int64_t first2, const int64_t first) {
     __shared__ float red[4][RF * 16][65];
-    const ShrinkArgs& Q = blockIdx.x < first2 ? Q1 : Q2;
-    const int64_t block = blockIdx.x < first2 ? blockIdx.x : blockIdx.x - first2;
+    const int64_t id = first + blockIdx.x;
+    const ShrinkArgs& Q = id < first2 ? Q1 : Q2;
+    const int64_t block = id < first2 ? id : id - first2;
     const int64_t slot = block / Q.splits;
     const int32_t split = (int32_t)(block - slot * Q.splits);
     const int32_t k = Q.owner[slot];
@@ -87,26 +88,27 @@ __global__ __launch_bounds__(256) void shrink_kernel(const ShrinkArgs Q1, const 
 int launch_shrink(const ShrinkArgs& S, const ShrinkArgs* more, hipStream_t st) {
     const ShrinkArgs& S2 = more != nullptr ? *more : S;
     const int64_t first2 = S.slots * S.splits, wgs = first2 + (more != nullptr ? S2.slots * S2.splits : 0);
-    if (!fits_launch(wgs, 256)) return WINDQ_ESHAPE;
-    const dim3 g((uint32_t)wgs), b(256);
-    switch (shrink_ranks(S.A.max_rank) / 16) {
-        case 1: shrink_kernel<1><<<g, b, 0, st>>>(S, S2, first2); break;
-        case 2: shrink_kernel<2><<<g, b, 0, st>>>(S, S2, first2); break;
-        case 3: shrink_kernel<3><<<g, b, 0, st>>>(S, S2, first2); break;
-        case 4: shrink_kernel<4><<<g, b, 0, st>>>(S, S2, first2); break;
-        case 5: shrink_kernel<5><<<g, b, 0, st>>>(S, S2, first2); break;
-        case 6: shrink_kernel<6><<<g, b, 0, st>>>(S, S2, first2); break;
-        case 7: shrink_kernel<7><<<g, b, 0, st>>>(S, S2, first2); break;
-        default: shrink_kernel<8><<<g, b, 0, st>>>(S, S2, first2); break;
-    }
-    return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
+    const dim3 b(256);
+    return launch_pieces(wgs, 256, [&](int64_t first, dim3 g) {
+        switch (shrink_ranks(S.A.max_rank) / 16) {
+            case 1: shrink_kernel<1><<<g, b, 0, st>>>(S, S2, first2, first); break;
+            case 2: shrink_kernel<2><<<g, b, 0, st>>>(S, S2, first2, first); break;
+            case 3: shrink_kernel<3><<<g, b, 0, st>>>(S, S2, first2, first); break;
+            case 4: shrink_kernel<4><<<g, b, 0, st>>>(S, S2, first2, first); break;
+            case 5: shrink_kernel<5><<<g, b, 0, st>>>(S, S2, first2, first); break;
+            case 6: shrink_kernel<6><<<g, b, 0, st>>>(S, S2, first2, first); break;
+            case 7: shrink_kernel<7><<<g, b, 0, st>>>(S, S2, first2, first); break;
+            default: shrink_kernel<8><<<g, b, 0, st>>>(S, S2, first2, first); break;
+        }
+    });
 }
 
 // A workgroup adds up eight ranks of a slot's pieces; the workgroups behind them write the zeros of tokens without an adapter, 64 tokens each.
 constexpr int JOIN_RANKS = 8;
-__global__ __launch_bounds__(256) void join_kernel(const JoinArgs Q1, const JoinArgs Q2, const int64_t first2) {
-    const JoinArgs& Q = blockIdx.x < first2 ? Q1 : Q2;
-    const int64_t block = blockIdx.x < first2 ? blockIdx.x : blockIdx.x - first2;
+__global__ __launch_bounds__(256) void join_kernel(const JoinArgs Q1, const JoinArgs Q2, const int64_t first2, const int64_t first) {
+    const int64_t id = first + blockIdx.x;
+    const JoinArgs& Q = id < first2 ? Q1 : Q2;
+    const int64_t block = id < first2 ? id : id - first2;
     const int32_t R = Q.A.max_rank, ranks = (R + 15) / 16 * 16, groups = R / JOIN_RANKS;
     const int64_t slot = block / groups;
     if (slot >= Q.slots) {
@@ -160,9 +162,7 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinArgs Q1, const Join
 int launch_join(const JoinArgs& J, const JoinArgs* more, hipStream_t st) {
     auto count = [](const JoinArgs& j) { return j.slots * (j.A.max_rank / JOIN_RANKS) + (j.h != nullptr ? tokens_in(j.T, GROUP) : 0); };
     const int64_t first2 = count(J), wgs = first2 + (more != nullptr ? count(*more) : 0);
-    if (!fits_launch(wgs, 256)) return WINDQ_ESHAPE;
-    join_kernel<<<dim3((uint32_t)wgs), dim3(256), 0, st>>>(J, more != nullptr ? *more : J, first2);
-    return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
+    return launch_pieces(wgs, 256, [&](int64_t first, dim3 g) { join_kernel<<<g, dim3(256), 0, st>>>(J, more != nullptr ? *more : J, first2, first); });
 }
 
 }  // namespace windq

@@ -42,6 +42,7 @@ struct ProjectArgs {
     int64_t ldy;
     const float* h;            // or null: no adapters
     AdapterArgs A;
+    int64_t first;             // of the workgroups of this launch
 };
 
 template <typename YT>
@@ -61,8 +62,8 @@ __global__ __launch_bounds__(PJ_WAVES * 64) void project_kernel(const ProjectArg
     const int32_t G = P.G, O = G >> 3, S = (O + 3) >> 2;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
     const int64_t row_blocks = (P.rows + 15) / 16;
-    const int64_t tb = blockIdx.x / row_blocks;
-    const int64_t row0 = (blockIdx.x - tb * row_blocks) * 16, t0 = tb * (NT * 16);
+    const int64_t block = Q.first + blockIdx.x, tb = block / row_blocks;
+    const int64_t row0 = (block - tb * row_blocks) * 16, t0 = tb * (NT * 16);
 
     const uint16_t* xp[NT];
 #pragma unroll
@@ -152,11 +153,11 @@ __global__ __launch_bounds__(PJ_WAVES * 64) void project_kernel(const ProjectArg
 }
 
 template <typename YT, int NT, bool MASK>
-int launch_project(const ProjectArgs& Q, hipStream_t st) {
-    const int64_t wgs = tokens_in(Q.P.rows, 16) * tokens_in(Q.T, NT * 16);
-    if (!fits_launch(wgs, PJ_WAVES * 64)) return WINDQ_ESHAPE;
-    project_kernel<YT, NT, MASK><<<dim3((uint32_t)wgs), dim3(PJ_WAVES * 64), 0, st>>>(Q);
-    return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
+int launch_project(ProjectArgs Q, hipStream_t st) {
+    return launch_pieces(tokens_in(Q.P.rows, 16) * tokens_in(Q.T, NT * 16), PJ_WAVES * 64, [&](int64_t first, dim3 g) {
+        Q.first = first;
+        project_kernel<YT, NT, MASK><<<g, dim3(PJ_WAVES * 64), 0, st>>>(Q);
+    });
 }
 
 // Sixteen tokens a workgroup while that leaves two workgroups a CU at most: their time is latency.  fp32, 1000 x 1056: 77 tokens (315 of them) 35 us,
@@ -285,9 +286,9 @@ int launch_tiles(const ProjectArgs& Q, char* ws, const ProjectWs& at, hipStream_
     const int64_t strips = (Q.P.rows / Q.P.R_u) * Q.P.n_chunks * ((Q.P.R_u + PT_STRIP - 1) / PT_STRIP);
     const int64_t wgs = strips + tokens_in(A.n_kb * Q.T, PT_SUMS);
     const int64_t tiles = (int64_t)A.row_blocks * ((Q.T + PT_TOKENS - 1) / PT_TOKENS);
-    if (!fits_launch(wgs, 256) || !fits_launch(tiles, PT_THREADS)) return WINDQ_ESHAPE;
-    tiles_prepare_kernel<XT, S><<<dim3((uint32_t)wgs), dim3(256), 0, st>>>(A, strips);
-    if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
+    // tiles are no more than 2^31 / (64 x 128) and two sides' edges: one launch holds them
+    const int status = launch_pieces(wgs, 256, [&](int64_t first, dim3 g) { tiles_prepare_kernel<XT, S><<<g, dim3(256), 0, st>>>(A, strips, first); });
+    if (status != WINDQ_OK) return status;
     project_tiles_kernel<XT, S><<<dim3((uint32_t)tiles), dim3(PT_THREADS), 0, st>>>(A);
     return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
 }
@@ -309,7 +310,6 @@ int project_all(ProjectArgs& Q, const windq_mat* X, const windq_adapters* ad, fl
     const bool few = sizeof(XT) == 2 && few_fits(Q.P, T), own_h = few && T <= FEW_OWN_H;
     float* const ht = ad == nullptr ? nullptr : (h != nullptr ? h : reinterpret_cast<float*>(ws + at.h));
     if (ad != nullptr && !own_h) {
-        const int64_t wgs = shrink_token_workgroups(T, Q.A.max_rank);
         bool grouped = false;
         if constexpr (sizeof(XT) == 2) {
             grouped = T > SHRINK_FEW;
@@ -326,9 +326,8 @@ int project_all(ProjectArgs& Q, const windq_mat* X, const windq_adapters* ad, fl
             }
         }
         if (!grouped) {
-            if (!fits_launch(wgs, 256)) return WINDQ_ESHAPE;
-            shrink_token_kernel<XT><<<dim3((uint32_t)wgs), dim3(256), 0, st>>>(static_cast<const XT*>(X->data), X->ld, (int32_t)Q.P.cols, Q.A, false, ht);
-            if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
+            const int status = launch_shrink_token(static_cast<const XT*>(X->data), X->ld, T, (int32_t)Q.P.cols, Q.A, false, ht, st);
+            if (status != WINDQ_OK) return status;
         }
     }
     Q.h = ht;

@@ -31,8 +31,8 @@ inline int64_t transpose_workgroups(int64_t n, int64_t C, int64_t ldo) { return 
 
 // A copy of dY whose rows start on 16 bytes and end with zeros.
 template <typename T>
-__global__ __launch_bounds__(256) void align_kernel(const T* __restrict__ in, int64_t ld, int64_t T_, int64_t width, int64_t ldo, T* __restrict__ out) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(256) void align_kernel(const T* __restrict__ in, int64_t ld, int64_t T_, int64_t width, int64_t ldo, T* __restrict__ out, int64_t first) {
+    const int64_t i = (first + blockIdx.x) * 256 + threadIdx.x;
     if (i >= T_ * ldo) return;
     const int64_t t = i / ldo, c = i - t * ldo;
     out[i] = c < width ? in[t * ld + c] : (T)0;
@@ -49,9 +49,10 @@ struct OuterRows {
     float* out;
 };
 
-__global__ __launch_bounds__(256) void outer_kernel(const OuterRows Q1, const OuterRows Q2, const int64_t first2, const AdapterArgs A, const GroupArgs G) {
-    const OuterRows& Q = blockIdx.x < first2 ? Q1 : Q2;
-    const int64_t block = blockIdx.x < first2 ? blockIdx.x : blockIdx.x - first2;
+__global__ __launch_bounds__(256) void outer_kernel(const OuterRows Q1, const OuterRows Q2, const int64_t first2, const AdapterArgs A, const GroupArgs G, const int64_t first) {
+    const int64_t id = first + blockIdx.x;
+    const OuterRows& Q = id < first2 ? Q1 : Q2;
+    const int64_t block = id < first2 ? id : id - first2;
     const int64_t wt = (Q.width + 255) / 256;
     const int32_t groups = (A.max_rank + 15) / 16;
     const int32_t k = (int32_t)(block / (wt * groups));
@@ -114,11 +115,12 @@ struct OuterArgs {
 };
 
 template <int RF, int OUTER_PARTS>
-__global__ __launch_bounds__(OUTER_THREADS) void outer_tiles_kernel(const OuterArgs Q1, const OuterArgs Q2, const int64_t first2) {
+__global__ __launch_bounds__(OUTER_THREADS) void outer_tiles_kernel(const OuterArgs Q1, const OuterArgs Q2, const int64_t first2, const int64_t first) {
     constexpr int OUTER_COLS = 512 / OUTER_PARTS;
     __shared__ float red[OUTER_PARTS / 2][RF * 16][OUTER_COLS + 4];
-    const OuterArgs& Q = blockIdx.x < first2 ? Q1 : Q2;
-    const int64_t block = blockIdx.x < first2 ? blockIdx.x : blockIdx.x - first2;
+    const int64_t id = first + blockIdx.x;
+    const OuterArgs& Q = id < first2 ? Q1 : Q2;
+    const int64_t block = id < first2 ? id : id - first2;
     const int32_t groups = (Q.A.max_rank + 63) / 64;
     const int32_t k = (int32_t)(block / (Q.tiles * groups));
     const int64_t rest = block - k * Q.tiles * groups;
@@ -287,8 +289,8 @@ __device__ __forceinline__ void weight_octet(const PackArgs& P, int64_t row, int
 }
 
 // bfloat16: the sums of the product's parts (none: the packed matrix is not wanted) and the adapters', a thread per token and octet of columns.
-__global__ __launch_bounds__(256) void dx_join_kernel(const DxArgs Q) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, octets = Q.P.cols >> 3;
+__global__ __launch_bounds__(256) void dx_join_kernel(const DxArgs Q, const int64_t first) {
+    const int64_t i = (first + blockIdx.x) * 256 + threadIdx.x, octets = Q.P.cols >> 3;
     const int64_t t = i / octets, c = (i - t * octets) * 8;
     if (t >= Q.T) return;
     float v[8] = {};
@@ -411,8 +413,8 @@ struct PrepareArgs {
 };
 
 template <typename XT>
-__global__ __launch_bounds__(256) void grad_prepare_kernel(const PrepareArgs<XT> Q) {
-    int64_t block = blockIdx.x;
+__global__ __launch_bounds__(256) void grad_prepare_kernel(const PrepareArgs<XT> Q, const int64_t first) {
+    int64_t block = first + blockIdx.x;
     if (block < Q.turns) return turn(Q.P, Q.K, Q.wt, block);
     block -= Q.turns;
     if (block < Q.bs) return transpose(Q.b, Q.P.rows, Q.A.max_rank, Q.ld, Q.bt, block);
@@ -461,9 +463,9 @@ __device__ __forceinline__ void dx_f32_store(const DxArgs& Q, int64_t t, int64_t
     for (int i = 0; i < 4; ++i) o[i] = v[i];
 }
 
-__global__ __launch_bounds__(256) void dx_f32_join_kernel(const DxArgs Q, const int64_t tiles) {
-    const int64_t tile = blockIdx.x >> 2, col_blocks = (Q.P.cols + 63) / 64, tb = tile / col_blocks;
-    const int n = blockIdx.x & 3, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+__global__ __launch_bounds__(256) void dx_f32_join_kernel(const DxArgs Q, const int64_t tiles, const int64_t first) {
+    const int64_t tile = (first + blockIdx.x) >> 2, col_blocks = (Q.P.cols + 63) / 64, tb = tile / col_blocks;
+    const int n = (int)(first + blockIdx.x) & 3, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     float v[4] = {};
     for (int32_t s = 0; s < Q.splits; ++s) {
         const float4 p = reinterpret_cast<const float4*>(Q.part)[(s * tiles + tile) * 1024 + n * 256 + threadIdx.x];
@@ -475,7 +477,7 @@ __global__ __launch_bounds__(256) void dx_f32_join_kernel(const DxArgs Q, const 
     dx_f32_store(Q, tb * 64 + n * 16 + (lane & 15), (tile - tb * col_blocks) * 64 + wave * 16 + 4 * (lane >> 4), v);
 }
 
-__global__ __launch_bounds__(DXF_THREADS) void dx_f32_kernel(const DxArgs Q) {
+__global__ __launch_bounds__(DXF_THREADS) void dx_f32_kernel(const DxArgs Q, const int64_t first) {
     __shared__ float wts[DXF_PARTS][32][68], yts[DXF_PARTS][32][68];
     __shared__ uint16_t trits_of[256];
     if (threadIdx.x < 256) trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
@@ -485,7 +487,7 @@ __global__ __launch_bounds__(DXF_THREADS) void dx_f32_kernel(const DxArgs Q) {
     float(&wt)[32][68] = wts[part];
     float(&yt)[32][68] = yts[part];
     const int64_t col_blocks = (P.cols + 63) / 64, tiles = col_blocks * ((Q.T + 63) / 64);
-    const int64_t split = blockIdx.x / tiles, tile = blockIdx.x - split * tiles, tb = tile / col_blocks;
+    const int64_t block = first + blockIdx.x, split = block / tiles, tile = block - split * tiles, tb = tile / col_blocks;
     const int64_t c0 = (tile - tb * col_blocks) * 64, t0 = tb * 64;
     const float* __restrict__ const dY = static_cast<const float*>(Q.dY);
     f32x4 acc[4] = {};
@@ -552,7 +554,7 @@ __global__ __launch_bounds__(DXF_THREADS) void dx_f32_kernel(const DxArgs Q) {
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
         float v[4] = {acc[n][0], acc[n][1], acc[n][2], acc[n][3]};
-        if (Q.splits > 1) reinterpret_cast<float4*>(Q.part)[blockIdx.x * 1024 + n * 256 + tid] = make_float4(v[0], v[1], v[2], v[3]);
+        if (Q.splits > 1) reinterpret_cast<float4*>(Q.part)[block * 1024 + n * 256 + tid] = make_float4(v[0], v[1], v[2], v[3]);
         else dx_f32_store(Q, t0 + n * 16 + sub, c0 + wave * 16 + 4 * q, v);
     }
 }
@@ -599,14 +601,11 @@ size_t grad_ws_bytes(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32
     return grad_ws(dtype, T, rows, cols, n, max_rank).total;
 }
 
-#define WINDQ_LAUNCH(wgs, threads, kernel, ...)                                                   \
-    do {                                                                                          \
-        const int64_t wgs_ = (wgs);                                                               \
-        if (!fits_launch(wgs_, threads)) return WINDQ_ESHAPE;                                     \
-        if (wgs_ > 0) {                                                                           \
-            kernel<<<dim3((uint32_t)wgs_), dim3(threads), 0, st>>>(__VA_ARGS__);                  \
-            if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;                               \
-        }                                                                                         \
+// Behind its arguments a kernel takes the first of a piece's workgroups.
+#define WINDQ_LAUNCH(wgs, threads, kernel, ...)                                                                                                  \
+    do {                                                                                                                                         \
+        const int launched_ = launch_pieces(wgs, threads, [&](int64_t first_, dim3 g_) { kernel<<<g_, dim3(threads), 0, st>>>(__VA_ARGS__, first_); }); \
+        if (launched_ != WINDQ_OK) return launched_;                                                                                             \
     } while (0)
 
 template <typename XT>
@@ -657,7 +656,6 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
     WINDQ_LAUNCH(R.turns + R.bs + R.as + R.groups, 256, grad_prepare_kernel<XT>, R);
     if (side) {
         float* const dh = reinterpret_cast<float*>(ws + at.dh);
-        const int64_t tokens = shrink_token_workgroups(T, A.max_rank);
         if constexpr (bf) {
             float* const part = reinterpret_cast<float*>(ws + at.part);
             uint16_t* const planes_h = reinterpret_cast<uint16_t*>(ws + at.planes_h);
@@ -701,11 +699,13 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
         } else {
             AdapterArgs B = A;
             B.a = bt;
-            WINDQ_LAUNCH(tokens, 256, shrink_token_kernel<XT>, dYv, Q.ldy, rows8, B, true, dh);
+            int status = launch_shrink_token(dYv, Q.ldy, T, rows8, B, true, dh, st);
+            if (status != WINDQ_OK) return status;
             if (outer) {
                 if (h == nullptr) {
                     float* const ht = reinterpret_cast<float*>(ws + at.h);
-                    WINDQ_LAUNCH(tokens, 256, shrink_token_kernel<XT>, static_cast<const XT*>(X->data), X->ld, (int32_t)cols, A, false, ht);
+                    status = launch_shrink_token(static_cast<const XT*>(X->data), X->ld, T, (int32_t)cols, A, false, ht, st);
+                    if (status != WINDQ_OK) return status;
                     h = ht;
                 }
                 const int64_t groups = (int64_t)A.n * ((A.max_rank + 15) / 16);
@@ -720,11 +720,12 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
     if (Q.dX == nullptr || T == 0) return WINDQ_OK;
     if constexpr (bf) {
         if (turn) {
+            // tiles are no more than 2^31 / 128^2 and two sides' edges: one launch holds them
             const int64_t tall = tokens_in(T, GM_N), by = tokens_in(cols, 256) * tall >= GM_TILES ? 256 : 128, tiles = tokens_in(cols, by) * tall;
             GemmArgs M = {R.wt, dYv, Q.ldy, R.K, T, cols, static_cast<uint16_t*>(Q.dX), Q.ldx, Q.dh, R.at, A, (uint32_t)tokens_in(cols, by), nullptr, (int32_t)tiles, R.K / GM_K};
             if (by == 256) {
-                WINDQ_LAUNCH(tiles, GM_THREADS, dx_gemm_kernel<4>, M);
-                return WINDQ_OK;
+                dx_gemm_kernel<4><<<dim3((uint32_t)tiles), dim3(GM_THREADS), 0, st>>>(M);
+                return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
             }
             const int32_t each = gemm_each(R.K, tiles), splits = (int32_t)tokens_in(R.K / GM_K, each);
             if (splits > 1) {
@@ -732,7 +733,8 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
                 M.part = Q.part = reinterpret_cast<float*>(ws + at.gm);
                 Q.splits = splits;
             }
-            WINDQ_LAUNCH(tiles * splits, GM_THREADS, dx_gemm_kernel<2>, M);
+            dx_gemm_kernel<2><<<dim3((uint32_t)(tiles * splits)), dim3(GM_THREADS), 0, st>>>(M);
+            if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
             if (splits == 1) return WINDQ_OK;
         }
         WINDQ_LAUNCH(tokens_in(T * (cols / 8), 256), 256, dx_join_kernel, Q);

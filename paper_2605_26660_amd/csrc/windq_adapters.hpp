@@ -17,6 +17,17 @@ inline bool sizes_fit(int64_t T, int64_t rows, int64_t cols, int32_t n, int32_t 
 }
 inline bool grad_sizes_fit(int64_t T, int64_t rows, int64_t cols) { return T * rows <= (int64_t)0x7fffffff && T * cols <= (int64_t)0x7fffffff; }
 
+// A launch of any number of workgroups, in pieces where one would hold 2^32 threads: launch(first, count).
+template <typename Launch>
+inline int launch_pieces(int64_t workgroups, int64_t threads, Launch launch) {
+    const int64_t most = (int64_t)0xffffffff / threads;
+    for (int64_t first = 0; first < workgroups; first += most) {
+        launch(first, dim3((uint32_t)(workgroups - first < most ? workgroups - first : most)));
+        if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
+    }
+    return WINDQ_OK;
+}
+
 // The tokens of adapter k in their own order, at places that start with a multiple of GROUP: place[] holds tokens, -1 where there is none.
 // Adapter k's first slot of GROUP places is (tokens of adapters below it) / GROUP + k: slots never overlap, and no adapter
 // has to wait for the counts of the others.
@@ -192,6 +203,19 @@ inline int64_t shrink_token_workgroups(int64_t T, int32_t max_rank) { return T *
 template <typename XT>
 __global__ __launch_bounds__(256) void shrink_token_kernel(const XT* __restrict__ X, int64_t ldx, int32_t cols, const AdapterArgs A, bool scaled, float* __restrict__ h) {
     shrink_token(X, ldx, cols, A, scaled, h, blockIdx.x);
+}
+
+template <typename XT>
+int launch_shrink_token(const XT* X, int64_t ldx, int64_t T, int32_t cols, const AdapterArgs& A, bool scaled, float* h, hipStream_t st) {
+    const int64_t most = (int64_t)0xffffff / (A.max_rank / SHRINK_RANKS);      // tokens of a launch: less than 2^32 threads
+    for (int64_t t = 0; t < T; t += most) {
+        AdapterArgs here = A;
+        here.of = A.of + t;
+        const int64_t wgs = shrink_token_workgroups(T - t < most ? T - t : most, A.max_rank);
+        shrink_token_kernel<XT><<<dim3((uint32_t)wgs), dim3(256), 0, st>>>(X + t * ldx, ldx, cols, here, scaled, h + t * A.max_rank);
+        if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
+    }
+    return WINDQ_OK;
 }
 
 __device__ __forceinline__ uint4 pack8(const uint32_t (&w)[8]) {

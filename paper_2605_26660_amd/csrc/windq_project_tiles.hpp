@@ -72,13 +72,14 @@ inline int tile_steps(const PackArgs& P) {
 
 // Workgroups [0, strips): fields of trits and 3-bit codes, every unit's word, and beta of its rows.  The others: sums of x over k-blocks.
 template <typename XT, int S>
-__global__ __launch_bounds__(256) void tiles_prepare_kernel(const TileArgs Q, const int64_t strips) {
+__global__ __launch_bounds__(256) void tiles_prepare_kernel(const TileArgs Q, const int64_t strips, const int64_t first_block) {
     __shared__ uint16_t trits_of[256];
     const PackArgs& P = Q.P;
     const int32_t per_chunk = P.G / (16 * S);
-    if (blockIdx.x >= strips) {
+    const int64_t block = first_block + blockIdx.x;
+    if (block >= strips) {
         // sixteen lanes a token, an octet each
-        const int64_t first = (blockIdx.x - strips) * PT_SUMS;
+        const int64_t first = (block - strips) * PT_SUMS;
         int32_t kb = (int32_t)(first / Q.T);
         int64_t t = first - (int64_t)kb * Q.T + (threadIdx.x >> 4);
         if (t >= Q.T) {                                     // there are more tokens than a workgroup sums up
@@ -102,7 +103,7 @@ __global__ __launch_bounds__(256) void tiles_prepare_kernel(const TileArgs Q, co
         return;
     }
     const int64_t per_unit = (P.R_u + PT_STRIP - 1) / PT_STRIP;
-    const int64_t u = blockIdx.x / per_unit, strip = blockIdx.x - u * per_unit;
+    const int64_t u = block / per_unit, strip = block - u * per_unit;
     int64_t base;
     const int a = pk_action(P, u, base);
     const bool lay = a == 3 || a == 5 || (a != 0 && !tile_natural(P.G, S));

@@ -57,3 +57,21 @@ def test_sizes_that_no_card_holds_are_refused_instead_of_wrapping_round(recorder
             for T, rows, cols in ((1, 1 << 24, 1 << 12), (1 << 17, 1 << 13, 1 << 13), (100, 1 << 14, 1 << 20)):
                 planes = 6 * T * cols if dtype == F and not grad else 2 * rows * cols if dtype == B and grad else 0
                 assert planes <= L.windq_project_workspace_bytes(grad, dtype, T, rows, cols, 128, 0, 0) < 1 << 44
+
+
+def test_no_launch_holds_as_many_threads_as_the_runtime_cuts_short(recorder):
+    """A launch of 2^32 threads or more loses the rest without an error: work of that size goes in several, and no size is refused between them."""
+    F, B = 0, 1
+    for grad, dtype, T, rows, cols, G, n, rank, kernel, workgroups in (
+            (0, F, 1 << 20, 8, 64, 64, 4, 128, "shrink_token_kernel", 1 << 25), (1, F, 1 << 20, 8, 64, 64, 4, 128, "shrink_token_kernel", 1 << 26),
+            (0, F, (1 << 19) + 77, 16, 64, 64, 4, 128, "shrink_token_kernel", 32 * ((1 << 19) + 77)),
+            (1, B, 500, 4096, 4096, 128, 200000, 8, "outer_tiles_kernel", 200000 * 64), (1, B, 500, 4096, 4096, 128, 200000, 8, "grad_prepare_kernel", 200000 * 129 + 64 * 16),
+            (1, F, 500, 4096, 4096, 128, 1000000, 8, "outer_kernel", 1000000 * 32), (1, B, 500, 64, 64, 64, 1 << 20, 128, "join_kernel", None),
+            (0, B, (1 << 28) - 1, 8, 64, 64, 0, 0, "project_kernel", 1 << 23), (0, B, (1 << 25) - 1, 64, 640, 64, 0, 0, "tiles_prepare_kernel", 10 + 10 * (1 << 21)),
+            (1, F, (1 << 28) - 1, 8, 8, 8, 0, 0, "dx_f32_kernel", 1 << 22), (1, B, (1 << 28) - 1, 1, 8, 8, 0, 0, "align_kernel", 1 << 26),
+            (0, B, (1 << 28) - 1, 8, 64, 64, 1, 128, "join_kernel", None), (0, B, (1 << 28) - 1, 8, 64, 64, 4, 8, "shrink_kernel", None)):
+        status, _, _ = recorder.product(grad, T, rows, cols, G, dtype=dtype, n=n, rank=rank)
+        all_ = recorder.launches()
+        assert status == 0 and all(x.grid * x.block < 1 << 32 for x in all_), (kernel, status)
+        mine = [x.grid for x in all_ if kernel + "I" in x.name or kernel + "E" in x.name]
+        assert mine and (workgroups is None or sum(mine) == workgroups), (kernel, mine)

@@ -8,6 +8,13 @@ from test_gpu_project import DEV, EPS, Case, Side, near, tokens, y_tol
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture
+def much_memory():
+    """What the test took goes back, for the tests behind it."""
+    yield
+    torch.cuda.empty_cache()
+
+
 @pytest.mark.parametrize("rows,G", [(8, 64), (24, 128), (40, 384)])
 def test_a_code_stream_that_ends_with_its_last_code(windq, rows, G):
     """The padding behind the last unit is not there: trits of an odd number of bytes a row."""
@@ -97,3 +104,58 @@ def test_the_largest_fp32_values_are_values(windq, rows, cols, T, top):
     h = float(np.float32(top)) * np.ones(16)
     side = (B @ h) * on[:, None]
     near(y, x64 @ c.w.T + side, EPS * (np.abs(x64) @ c.mag.T + np.abs(B) @ np.abs(h) * on[:, None]))
+
+
+def test_more_tokens_times_ranks_than_one_launch_takes(windq):
+    """fp32, 2^26 and some: h of the first and last tokens, and of those on both sides of a launch's end."""
+    rows, cols, T, r = 8, 64, (1 << 19) + 77, 128
+    c = Case(windq, rows, cols, 64, 0, torch.float32, seed=3)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    X, dY = torch.randn(T, cols, generator=g, device=DEV), torch.randn(T, rows, generator=g, device=DEV)
+    a, b = torch.randn(2, r, cols, generator=g, device=DEV) / 8, 0.05 * torch.randn(2, rows, r, generator=g, device=DEV)
+    of = torch.randint(0, 2, (T,), generator=g, device=DEV, dtype=torch.int32)
+    h = torch.full((T, r), float("nan"), device=DEV)
+    ad = windq.Adapters(a, b)
+    y = windq.windq_project(c.packed, X, ad, of, h=h)
+    dx = windq.windq_project_grad(c.packed, dY, X, ad, of, h=h)[0]
+    end = ((1 << 24) - 1) // 32                          # tokens of a launch
+    some = [*range(40), *range(end - 40, end + 40), *range(T - 90, T)]
+    x, dy, k = X[some].double().cpu().numpy(), dY[some].double().cpu().numpy(), of[some].long().cpu().numpy()
+    A, B = a.double().cpu().numpy()[k], b.double().cpu().numpy()[k]
+    hw, hm = np.matmul(A, x[:, :, None])[:, :, 0], np.matmul(np.abs(A), np.abs(x)[:, :, None])[:, :, 0]
+    near(h[some], hw, EPS * hm)
+    near(y[some], x @ c.w.T + np.matmul(B, hw[:, :, None])[:, :, 0], EPS * (np.abs(x) @ c.mag.T + np.matmul(np.abs(B), hm[:, :, None])[:, :, 0]))
+    d, dm = np.matmul(dy[:, None, :], B), np.matmul(np.abs(dy)[:, None, :], np.abs(B))
+    near(dx[some], dy @ c.w + np.matmul(d, A)[:, 0], EPS * (np.abs(dy) @ c.mag + np.matmul(dm, np.abs(A))[:, 0]))
+
+
+def test_more_adapters_than_one_launch_takes(windq, much_memory):
+    """2^20 adapters, three of them in use: the first, one in the middle and the last; every other one's gradient is zero."""
+    n, r, rows, cols, T = 1 << 20, 8, 64, 1024, 100
+    c = Case(windq, rows, cols, 128, 0, seed=3)
+    g = torch.Generator().manual_seed(2)
+    a, b = torch.zeros(n, r, cols, dtype=torch.bfloat16, device=DEV), torch.zeros(n, rows, r, dtype=torch.bfloat16, device=DEV)
+    used = [0, n // 2 + 5, n - 1]
+    for k in used:
+        a[k], b[k] = (torch.randn(r, cols, generator=g) / 32).to(DEV), (0.05 * torch.randn(rows, r, generator=g)).to(DEV)
+    of = torch.tensor(used)[torch.randint(0, 3, (T,), generator=g)].to(torch.int32)
+    X, dY = tokens(T, cols, torch.bfloat16, 3), tokens(T, rows, torch.bfloat16, 4)
+    ad = windq.Adapters(a, b)
+    y = windq.windq_project(c.packed, X, ad, of.to(DEV))
+    da, db = (torch.full(t.shape, float("nan"), device=DEV) for t in (a, b))
+    windq.windq_project_grad(c.packed, dY, X, ad, of.to(DEV), outs=(None, da, db))
+    x, dy = X.double().cpu().numpy(), dY.double().cpu().numpy()
+    want, tol = x @ c.w.T, np.abs(x) @ c.mag.T
+    for k in used:
+        at = np.flatnonzero(of.numpy() == k)
+        A, B = a[k].double().cpu().numpy(), b[k].double().cpu().numpy()
+        h, hm = x[at] @ A.T, np.abs(x[at]) @ np.abs(A).T
+        want[at] += h @ B.T
+        tol[at] += hm @ np.abs(B).T
+        near(da[k], (dy[at] @ B).T @ x[at], EPS * ((np.abs(dy[at]) @ np.abs(B)).T @ np.abs(x[at])))
+        near(db[k], dy[at].T @ h, EPS * (np.abs(dy[at]).T @ hm))
+    near(y, want, EPS * tol + 2.0 ** -8 * 1.001 * np.abs(want) + 2.0 ** -16 * tol)
+    for t in (da, db):
+        t[used] = 0
+        for part in t.split(1 << 16):
+            assert not part.any()
