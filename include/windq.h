@@ -631,7 +631,7 @@ typedef struct windq_packed {
     const uint8_t* mask;      /* [rows][cols/8] or NULL */
     const uint8_t* action;    /* [U] */
     const int64_t* code_off;  /* [U+1] */
-    const uint8_t* codes;
+    const uint8_t* codes;     /* 16-byte aligned; may be NULL with codes_bytes 0 (skip units alone) */
     size_t codes_bytes;
     const float* scale;       /* [U*R_u] */
     const float* offset;      /* [U*R_u] */

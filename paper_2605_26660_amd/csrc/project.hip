@@ -174,7 +174,8 @@ int check_packed(const windq_packed* P, PackArgs* A) {
     Geometry g;
     const int status = make_geometry(P->W, P->chunk_w, P->unit_rows, &g);
     if (status != WINDQ_OK) return status;
-    if (P->action == nullptr || P->code_off == nullptr || P->codes == nullptr || P->scale == nullptr || P->offset == nullptr) return WINDQ_EINVAL;
+    if (P->action == nullptr || P->code_off == nullptr || P->scale == nullptr || P->offset == nullptr) return WINDQ_EINVAL;
+    if (P->codes == nullptr && P->codes_bytes != 0) return WINDQ_EINVAL;     // no codes: skip units alone
     if (!aligned(P->code_off, 8) || !aligned(P->codes, 16) || !aligned(P->scale, 4) || !aligned(P->offset, 4)) return WINDQ_EINVAL;
     A->W = P->W->data;
     A->ld = P->W->ld;

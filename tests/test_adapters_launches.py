@@ -1,7 +1,9 @@
 """What windq_project, windq_project_grad and windq_adamw launch, and what of the workspace they hand to it: the host code alone, without a GPU."""
+import ctypes
 import random
 
-from host_launches import recorder  # noqa: F401
+from host_launches import AT, recorder  # noqa: F401
+from paper_2605_26660_amd import binding
 
 
 def apart(regions, at, need):
@@ -75,3 +77,12 @@ def test_no_launch_holds_as_many_threads_as_the_runtime_cuts_short(recorder):
         assert status == 0 and all(x.grid * x.block < 1 << 32 for x in all_), (kernel, status)
         mine = [x.grid for x in all_ if kernel + "I" in x.name or kernel + "E" in x.name]
         assert mine and (workgroups is None or sum(mine) == workgroups), (kernel, mine)
+
+
+def test_a_plan_of_skip_units_alone_needs_no_codes(recorder):
+    """As for the other calls on a packed plan: no codes are given where there are none."""
+    L, B = recorder.lib, binding
+    W, X = B.windq_mat(AT, 1, 0, 64, 128, 128), B.windq_mat(AT, 1, 0, 9, 128, 128)
+    for codes, codes_bytes, want in ((None, 0, 0), (None, 16, 1), (AT, 0, 0)):
+        P = B.windq_packed(ctypes.pointer(W), None, AT, AT, codes, codes_bytes, AT, AT, 64, 0, 0)
+        assert L.windq_project(ctypes.byref(P), ctypes.byref(X), None, None, AT, 64, None, AT, 1 << 30, None) == want

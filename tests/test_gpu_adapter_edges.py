@@ -159,3 +159,15 @@ def test_more_adapters_than_one_launch_takes(windq, much_memory):
         t[used] = 0
         for part in t.split(1 << 16):
             assert not part.any()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_plan_of_skip_units_alone(windq, dtype):
+    """No codes at all, and none given."""
+    c = Case(windq, 96, 256, 64, 0, seed=2, only=0)
+    packed = c.describe(windq, codes=torch.empty(0, dtype=torch.uint8, device=DEV))
+    for T in (1, 40, 200):
+        X, dY = tokens(T, 256, dtype, T), tokens(T, 96, dtype, T + 1)
+        x, dy = X.double().cpu().numpy(), dY.double().cpu().numpy()
+        near(windq.windq_project(packed, X), x @ c.w.T, y_tol(c, x, dtype, x @ c.w.T))
+        near(windq.windq_project_grad(packed, dY)[0], dy @ c.w, EPS * (np.abs(dy) @ c.mag) + (2.0 ** -8 * 1.001 * np.abs(dy @ c.w) if dtype == torch.bfloat16 else 0.0))
