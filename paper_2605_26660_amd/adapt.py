@@ -16,6 +16,7 @@ from . import synth
 from .binding import (ADAMW_BLOCK, Adapters, AdamwItems, Packed, n_units, project_workspace, windq_adamw, windq_apply_plan,
                       windq_fit_score_all_bits, windq_plan_layout, windq_project, windq_project_grad)
 
+SERVED = 24                                       # requests of the decoding step
 MIX = (2, 4, 5, 5, 6, 6, 4, 5, 6, 5)              # treatments of the units in turn: 2.0 bits a weight with the scales left out
 
 
@@ -46,7 +47,8 @@ class Trainer:
         self.items = AdamwItems(self.params, self.grads, bytes_of(), bytes_of(), scales(), scales(), self.copies)
         self.packed, self.adapters = packed, Adapters(*self.copies, alpha=torch.ones(n, device=dev))
         like = torch.empty(tokens, packed.cols, dtype=torch.bfloat16, device=dev)
-        self.ws = project_workspace(packed, like, self.adapters)
+        serving = torch.empty(max(tokens, SERVED), packed.cols, dtype=torch.bfloat16, device=dev)
+        self.ws = project_workspace(packed, serving, self.adapters)
         self.ws_grad = project_workspace(packed, like, self.adapters, grad=True)
         self.h = torch.empty(tokens, rank, device=dev)
         self.step_no = 0
@@ -88,8 +90,8 @@ def run(rows: int = 4096, cols: int = 4096, chunk_w: int = 128, steps: int = 60,
         err = trainer.step(X, of, X.float() @ full, lr * (1.0 - k / (steps + 1)))
         last = torch.stack([err[of == i].mean() for i in range(kinds)])
         first = last if first is None else first
-    # a decoding step of 24 requests, every fourth one without an adapter
-    X, of = draw(24)
+    # a decoding step, every fourth request without an adapter
+    X, of = draw(SERVED)
     of[::4] = -1
     served = windq_project(packed, X, trainer.adapters, of, ws=trainer.ws).float()
     plain = windq_project(packed, X, ws=trainer.ws).float()
@@ -107,7 +109,7 @@ def main():
     first, last, differs = run(p.rows, p.cols, p.chunk, p.steps, p.tokens, p.rank)
     for k, (x, y) in enumerate(zip(first, last)):
         print(f"kind {k}: mean squared error {x:.3e} packed, {y:.3e} with its adapter after {p.steps} steps")
-    print(f"served batch of 24 requests: {differs:.1e} off the sum of its parts")
+    print(f"served batch of {SERVED} requests: {differs:.1e} off the sum of its parts")
 
 
 if __name__ == "__main__":

@@ -171,3 +171,10 @@ def test_a_plan_of_skip_units_alone(windq, dtype):
         x, dy = X.double().cpu().numpy(), dY.double().cpu().numpy()
         near(windq.windq_project(packed, X), x @ c.w.T, y_tol(c, x, dtype, x @ c.w.T))
         near(windq.windq_project_grad(packed, dY)[0], dy @ c.w, EPS * (np.abs(dy) @ c.mag) + (2.0 ** -8 * 1.001 * np.abs(dy @ c.w) if dtype == torch.bfloat16 else 0.0))
+
+
+def test_the_example_with_fewer_tokens_than_it_serves(windq):
+    from paper_2605_26660_amd import adapt
+
+    first, last, differs = adapt.run(rows=64, cols=128, chunk_w=64, steps=2, tokens=16, rank=8)
+    assert len(first) == len(last) == 3 and differs < 3 * 2.0 ** -8
