@@ -86,3 +86,19 @@ def test_a_plan_of_skip_units_alone_needs_no_codes(recorder):
     for codes, codes_bytes, want in ((None, 0, 0), (None, 16, 1), (AT, 0, 0)):
         P = B.windq_packed(ctypes.pointer(W), None, AT, AT, codes, codes_bytes, AT, AT, 64, 0, 0)
         assert L.windq_project(ctypes.byref(P), ctypes.byref(X), None, None, AT, 64, None, AT, 1 << 30, None) == want
+
+
+def test_the_routes_tests_take_the_routes_they_name(recorder):
+    """The shapes that are compared with 64 bits on the GPU, kernel by kernel: a rule that moves one of them to another kernel shows here."""
+    import torch
+
+    import test_gpu_project_routes as R
+
+    code = {torch.bfloat16: 1, torch.float32: 0}
+    for kernel, x_type, w_type, T, rows, cols, G, unit_rows, n, rank, masked in R.FORWARD:
+        for adapters in {0, n}:
+            status, _, _ = recorder.product(False, T, rows, cols, G, unit_rows, code[x_type], adapters, rank if adapters else 0, masked, code[w_type], codes_bytes=1 << 20)
+            assert status == 0 and kernel in names(recorder), (kernel, names(recorder))
+    for kernels, x_type, w_type, T, rows, cols, G, unit_rows, n, rank, masked in R.BACK:
+        status, _, _ = recorder.product(True, T, rows, cols, G, unit_rows, code[x_type], n, rank, masked, code[w_type], codes_bytes=1 << 20)
+        assert status == 0 and all(k in names(recorder) for k in kernels), (kernels, names(recorder))
