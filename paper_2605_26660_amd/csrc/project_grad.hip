@@ -278,7 +278,7 @@ __device__ __forceinline__ void weight_octet(const PackArgs& P, int64_t row, int
     const int64_t g = u * P.R_u + lrow;
     const float s = P.scale[g], of = a >= 5 ? 0.0f : P.offset[g];
     const uint4 f = octet_fields(a, P.codes + base + lrow * pk_bytes_per_group(a, P.G), o, trits_of);
-    const float f0 = a == 2 ? 16.0f : (a == 3 ? 8.0f : (a == 4 ? 4.0f : (a == 5 ? 5.0f : 0.0f)));
+    const float f0 = pk_f0(a);
     const uint32_t m = P.mask != nullptr ? P.mask[row * P.mask_ld + (col >> 3)] : 0u;
     const uint32_t v[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
@@ -359,7 +359,7 @@ __device__ __forceinline__ void turn(const PackArgs& P, int32_t K, uint16_t* __r
                 case 5: rows([&](const uint8_t* p) { return fields2(octet_trits(p, o, trits_of) & 0xffffu); }); break;
                 default: rows([&](const uint8_t* p) { return fields1(p[o]); }); break;
             }
-            const float f0 = a == 2 ? 16.0f : (a == 3 ? 8.0f : (a == 4 ? 4.0f : (a == 5 ? 5.0f : 0.0f)));
+            const float f0 = pk_f0(a);
             uint32_t m8[8] = {};
             if (P.mask != nullptr) {
 #pragma unroll

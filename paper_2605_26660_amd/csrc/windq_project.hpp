@@ -94,16 +94,17 @@ __device__ __forceinline__ int pk_action(const PackArgs& P, int64_t u, int64_t& 
     return a;
 }
 
+// f0, and what f comes down by when it is centred.
+__device__ __forceinline__ float pk_f0(int a) { return a == 2 ? 16.0f : (a == 3 ? 8.0f : (a == 4 ? 4.0f : (a == 5 ? 5.0f : 0.0f))); }
+__device__ __forceinline__ float pk_centre(int a) { return a == 1 ? 127.5f : (a == 2 ? 23.5f : (a == 3 ? 11.5f : (a == 4 ? 5.5f : (a == 5 ? 5.0f : 0.0f)))); }
+
 // beta = offset - f0 * scale (1.58 and 1 bit have no offset of their own).
 __device__ __forceinline__ void pk_affine(int a, float scale, float offset, bool centred, float& alpha, float& beta) {
     alpha = a == 0 ? 1.0f : scale;
     const float o = a >= 5 || a == 0 ? 0.0f : offset;
-    const float f0 = centred ? (a == 1 ? -127.5f : (a == 2 ? -7.5f : (a == 3 ? -3.5f : (a == 4 ? -1.5f : 0.0f))))
-                             : (a == 2 ? 16.0f : (a == 3 ? 8.0f : (a == 4 ? 4.0f : (a == 5 ? 5.0f : 0.0f))));
+    const float f0 = centred ? pk_f0(a) - pk_centre(a) : pk_f0(a);
     beta = a == 0 ? 0.0f : o - f0 * scale;
 }
-// What f comes down by when it is centred.
-__device__ __forceinline__ float pk_centre(int a) { return a == 1 ? 127.5f : (a == 2 ? 23.5f : (a == 3 ? 11.5f : (a == 4 ? 5.5f : (a == 5 ? 5.0f : 0.0f)))); }
 __device__ __forceinline__ uint32_t centred_pair(uint32_t v, float c) {
     return __builtin_amdgcn_perm(__float_as_uint(__uint_as_float(v & 0xffff0000u) - c), __float_as_uint(__uint_as_float(v << 16) - c), 0x07060302u);
 }
