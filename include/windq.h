@@ -621,11 +621,12 @@ int windq_refine_plan_batch(const windq_refine_item* items /*HOST [n]*/, int32_t
  * and the optimizer step that trains them.
  *
  * A packed matrix, as windq_apply_plan (or windq_refine_plan) left it.  W is read for skip units only; `mask` NULL or as
- * in windq_apply_plan_prot (protected weights count as 0: their values live in the INT8 side stream).  Entries of the
- * plan are checked as in windq_dequant_plan: a malformed one counts as skip.
+ * in windq_apply_plan_prot.  Protected weights count as 0: their values live in the INT8 side stream, which no call here multiplies, so
+ * that Y and dX of a protected plan are without their part.  Entries of the plan are checked as in windq_dequant_plan: a malformed
+ * one counts as skip.
  */
 #define WINDQ_MAX_RANK 128           /* longest adapter */
-#define WINDQ_MAX_ADAPTERS (1 << 20) /* most adapters of one call */
+#define WINDQ_MAX_ADAPTERS (1 << 20) /* most adapters of one call; beyond some tokens its time and workspace grow with them, used or not */
 typedef struct windq_packed {
     const windq_mat* W;       /* HOST descriptor */
     const uint8_t* mask;      /* [rows][cols/8] or NULL */
@@ -660,9 +661,13 @@ typedef struct windq_adapters {
  *      ld_y >= rows (any), written whole (nothing past a row's end)
  *   h  [tokens][max_rank] f32 or NULL: h_t, zeros past the adapter's rank (what windq_project_grad can use again)
  * Codes enter the matrix instructions as they are (small integers and signs are exact in bfloat16) and a group's sum over its
- * chunk is scaled in fp32 afterwards: scale * sum code x + offset * sum x, so no weight is rounded.  fp32 activations and
- * fp32 skip weights enter as three bfloat16 terms each, to fp32 accuracy.  Sums are fp32, in a fixed order:
- * results are bit-reproducible and differ from the exact sum by a few 1e-7 of sum |w_hat x| before Y's own rounding.
+ * chunk is scaled in fp32 afterwards: scale * sum f x + beta * sum x with f = code + f0 and beta = offset - f0 * scale, so no weight is rounded.
+ * fp32 activations, fp32 skip weights and fp32 adapters enter as three bfloat16 terms each, to fp32 accuracy (magnitudes below 2^-100 may lose
+ * low bits: no term is below 2^-133).  Sums are fp32, in a fixed order: results are bit-reproducible and before Y's own rounding differ from the
+ * exact sum by a few 1e-7 of sum |scale f x| + |beta x|, the magnitudes that are added.  For WINDQ_F32 f is the code less its range's middle, so
+ * that those are about |w_hat x|; for WINDQ_BF16 f0 is 16 (4 bits), 8 (3 bits), 4 (2 bits), 5 (1.58 bits, code -1..1) or 0, and f up to six times as
+ * far from 0 as the codes are from their middle: two to three bits, far below Y's rounding unless a sum all but cancels.  In WINDQ_BF16 h_t enters
+ * alpha_k B_k h_t in 16 bits or more (two bfloat16 terms).
  * A result that is not finite is formed again weight by weight in fp64, so infinities and NaN of x, of scales and of skip
  * weights come out as the formula has them, in their own token's and row's results only.
  * X is 16-byte aligned with a leading dimension that is a multiple of 8; Y and ld_y are free.  At most 2^31 - 1 tokens x rows, 2^31 - 512 rows
@@ -680,7 +685,7 @@ int windq_project(const windq_packed* P /*HOST*/, const windq_mat* X, const wind
  *   dA[k] = sum_t dh_t x_t^T,   dB[k] = alpha_k sum_t dY_t h_t^T    over the tokens of adapter k
  *   dY [tokens][rows] (leading dimension ld_dy >= rows, any); X [tokens][cols], of one type
  *   dX [tokens][cols] of that type, ld_dx >= cols, or NULL: not wanted.  In WINDQ_BF16 the weights enter the product rounded
- *      to bfloat16 once, as dY is.
+ *      to bfloat16 once, as dY is, and dh_t enters A_k^T dh_t as two bfloat16 terms; in WINDQ_F32 neither is rounded.
  *   dA [n][max_rank][cols], dB [n][rows][max_rank] f32, both or neither: written whole, zeros past an adapter's rank and for
  *      adapters without a token
  *   h  as windq_project left it (for the same X and adapters), or NULL: formed again from X

@@ -873,7 +873,7 @@ def windq_dequant_gemv_batch(Ws, chunk_w: int, unit_rows: int, actions, code_off
 # ------------------------------------------------- adapters beside a packed plan, and their optimizer
 class Packed:
     """A packed matrix as windq_project and windq_project_grad take it: device tensors as windq_apply_plan wrote them, W [rows x cols]
-    (read for skip units only), mask as windq_salient_select wrote it or None.  Checked and described once; it keeps the tensors,
+    (read for skip units only), mask as windq_salient_select wrote it or None (protected weights count as 0).  Checked and described once; it keeps the tensors,
     and sees what is written into them later."""
 
     def __init__(self, W: torch.Tensor, chunk_w: int, unit_rows: int, action: torch.Tensor, code_off: torch.Tensor,

@@ -1,14 +1,16 @@
 // windq_adamw: one AdamW step over many tensors at once, moments in 32 bits or in 8.
 //   m <- b1 m + (1 - b1) g     v <- b2 v + (1 - b2) g^2     p <- p decay - size m / (sqrt(v) inverse + eps)
 // Every value is read once and written once and nothing else moves: 28 bytes a parameter with fp32 moments, 16 with 8-bit
-// ones, against some 60 vector instructions, so HBM is what bounds it.
+// ones, against some 75 vector instructions in 8 bits, so HBM is what bounds it but for bfloat16 parameters.
 //   A launch takes up to AW_MANY tensors: their descriptors travel in the kernel arguments and a workgroup finds its tensor by
 // bisection over first-tile numbers.  A workgroup has AW_TILE consecutive values; a wavefront reads 256 of them at a time,
 // four a lane, so that the block that shares an 8-bit scale is exactly a wavefront's step: its largest magnitude is a butterfly
 // over 64 lanes and no value is visited twice.
 //   Magnitudes are compared as integers (a float's bits without its sign): NaN and infinities order above all else and cannot
 // get lost in a maximum.
-//   45 M parameters, fp32 moments, bfloat16 gradients and copy 249 us (5.1 TB/s); 448 tensors of 65536 in 8 bits 110 us in two launches (4.9 TB/s in each).
+//   45 M parameters, fp32 moments, bfloat16 gradients and copy 249 us (5.1 TB/s); 448 tensors of 65536 in 8 bits 110 us in two launches of 46 to 49 us (4.9 TB/s
+// in each).  In 8 bits with bfloat16 parameters (8 bytes a parameter) the instructions take as long as the bytes: 6.5 M in 37 ragged tensors 22.5 us, 21.3 in
+// one tensor (12.7 us of instruction issue, 12.5 us of bytes, in one generation of workgroups that load, compute and store about in step).
 #include <math.h>
 #include <string.h>
 
@@ -19,7 +21,9 @@ namespace windq {
 constexpr int AW_THREADS = 256;
 constexpr int AW_STEPS = 4;                               // blocks of 256 values a wavefront takes
 constexpr int64_t AW_TILE = (int64_t)AW_THREADS * 4 * AW_STEPS;
-constexpr int AW_FEW = 16, AW_MANY = 224;                 // tensors of a launch
+// Tensors of a launch.  AW_MANY is what keeps the arguments below 16 KB; 448 tensors of 65536 in 8 bits, one after the other on the same data: 224 a launch 95 us,
+// 112 a launch 115, 64 a launch 137.  Up to AW_FEW they take 1 KB of arguments: two tensors of 8192 5.7 us and 6.3, sixteen 5.9 and 6.4.
+constexpr int AW_FEW = 16, AW_MANY = 224;
 
 struct AdamwRates {
     float b1, c1, b2, c2, eps, decay, size, inverse;

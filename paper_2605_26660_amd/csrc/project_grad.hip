@@ -99,7 +99,7 @@ __global__ __launch_bounds__(256) void outer_kernel(const OuterRows Q1, const Ou
 // transposed and as three bfloat16 terms, so products are exact to fp32.  Bound by latency: a wavefront has a
 // step's operands on their way while it multiplies the step before, and the tokens of the step after.
 constexpr int OUTER_THREADS = 512;
-inline int outer_parts(int64_t T, int32_t n) { return T >= (int64_t)512 * n ? 8 : 4; }        // 2048 tokens of one adapter: 42 us by eight, 81 by pairs; 700 of sixteen: 20 and 13
+inline int outer_parts(int64_t T, int32_t n) { return T >= (int64_t)512 * n ? 8 : 4; }        // 2048 tokens of one adapter: 35 to 42 us by eight, 81 by pairs; 700 of sixteen: 20 and 13
 struct OuterArgs {
     const uint16_t* right;     // [T][ld], on 16 bytes, columns in eights readable
     int64_t ld, width;
@@ -396,7 +396,7 @@ __device__ __forceinline__ void turn(const PackArgs& P, int32_t K, uint16_t* __r
 }
 
 // What the later kernels read, in one launch: the reconstruction turned, B and A transposed, tokens by adapter.  Workgroups in that order.
-// 11008 x 4096: 33 us, 88 MB written (3.7 TB/s).
+// 11008 x 4096: 29 to 33 us, 92 MB written (3.2 to 2.8 TB/s).
 template <typename XT>
 struct PrepareArgs {
     PackArgs P;

@@ -1,9 +1,11 @@
 // dX = w_hat^T dY in bfloat16: a plain product of two matrices whose rows lie along the sum's axis.
 //
 // Codes lie along columns and the sum runs along rows, so a tile of weights would have to be turned for every 128 tokens.  The packed
-// matrix is reconstructed once instead, rounded to bfloat16 and turned (wt [cols][rows], 2 bytes a weight; 33 of 286 us at 2048 tokens through
-// 11008 x 4096; for one token too: 4096 x 4096 45 us, 373 with tiles turned on the way), and the product then spends nothing but matrix instructions and their operands' way: 256 columns x 128
-// tokens a workgroup, four wavefronts with 128 x 64 results each as 4 x 2 fragments of 32x32x16 instructions, one per SIMD; 128 columns where
+// matrix is reconstructed once instead, rounded to bfloat16 and turned (wt [cols][rows], 2 bytes a weight; 29 to 33 of 289 us at 2048 tokens through
+// 11008 x 4096; for one token too: 4096 x 4096 45 us, 373 with tiles turned on the way), and the product then spends nothing but matrix instructions and their operands' way (160 us, 1160 TFLOP/s).
+// That rounding is of the weights alone and once: dX is 2.4e-3 off the formula in 64 bits (norm by norm) where its own rounding to bfloat16 alone would make it 1.7e-3.  Two terms of a
+// weight would undo it for twice the matrix instructions; a caller who needs it passes fp32, where nothing is rounded.
+//   256 columns x 128 tokens a workgroup, four wavefronts with 128 x 64 results each as 4 x 2 fragments of 32x32x16 instructions, one per SIMD; 128 columns where
 // that would leave CUs without a workgroup.
 //   64 of the sum at a time go to LDS by direct loads, three buffers: while one is multiplied the next has landed and the one
 // after is on its way.  There is one barrier per buffer, ahead of its last step: by then all of it has been read into registers, and the next

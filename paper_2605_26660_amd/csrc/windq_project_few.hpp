@@ -7,8 +7,8 @@
 //   X is read by every workgroup, so a kernel ahead (with the adapters' first half, if there is one) lays it out in the order in which the
 // lanes want it, 1 KB a load, and sums it up.  Up to FEW_DIRECT tokens it is read as it lies, and summed up by instructions with ones for weights.
 //   Totals meet in LDS, in the order of the wavefronts.
-//   1 token through 4096 x 4096 at 2 bits 12 us (+ 3 for h), 48 tokens of 32 adapters through 11008 x 4096 46 us (+ 5): two rounds of workgroups, waits are 58 % of
-// the wavefronts' time.
+//   1 token through 4096 x 4096 at 2 bits 12 us (+ 3 for h), 48 tokens of 32 adapters through 11008 x 4096 44 to 46 us (+ 5): two rounds of workgroups, waits
+// are 59 % of the wavefronts' time.
 #pragma once
 
 #include "windq_project_tiles.hpp"
@@ -33,6 +33,10 @@ struct FewArgs {
     uint32_t row_blocks;
 };
 
+// Up to FEW_DIRECT tokens X is read as it lies, a launch less: at 8 tokens 4096 x 4096 takes 13.7 us and 18.5 laid out, 11008 x 4096 25.7 and 31.4 (at 16
+// 4096 x 4096 would still take 16.2 instead of 19.4, at 32 11008 x 4096 40.1 instead of 36.6).  Up to FEW_OWN_H tokens h is formed token by token beside
+// the laying out, no launch of its own: 1024 x 2048, 8 adapters of 32 ranks, 256 tokens 26.8 us, by tiles of an adapter's tokens 36.2 (512 tokens 31.6 and
+// 38.7, 1000 tokens 58.6 and 60.6: the margin shrinks with tokens x ranks).
 constexpr int64_t FEW_DIRECT = 8, FEW_ALWAYS = 64, FEW_OWN_H = 256;
 
 // Most tokens of a matrix: 64, or as many as make one round of workgroups (one a CU), two from 8 k-blocks on, three from 32 on.  A round takes

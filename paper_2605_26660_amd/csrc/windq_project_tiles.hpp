@@ -14,8 +14,9 @@
 // bfloat16 terms, six products in eight of an instruction's sixteen k, so one instruction does two k-blocks.
 //   Trits and 3-bit codes are laid out as 2- and 4-bit fields before (by the kernel that sums x): a row of them is visited by
 // T / 128 workgroups, and taking trits apart costs more than everything else in the loop.
-//   2000 tokens through 4096 x 11008 at 2 bits: 195 to 225 us (800 to 920 TFLOP/s) + 22 for laying out; 4096 through 13824 x 5120 with 4 adapters of 64
-// ranks 780 in all.  27560 vector instructions against 2944 matrix instructions a wavefront: neither unit is full, waits are 46 % of the wavefronts' time.
+//   2000 tokens through 4096 x 11008 at 2 bits: 231 us (780 TFLOP/s) + 20 for laying out, 4096 through 13824 x 5120 with 4 adapters of 64 ranks 705 us
+// (820 TFLOP/s) + 62; both traced once the card's clock has settled, 251 to 280 and 730 to 920 in the first 10 ms under load.  27560 vector instructions a
+// wavefront, 2944 matrix instructions among them: neither unit is full, waits are 46 % of the wavefronts' time.
 #pragma once
 
 #include "windq_adapters.hpp"
