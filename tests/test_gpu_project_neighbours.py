@@ -119,3 +119,39 @@ def test_gradients_that_are_not_finite_stay_with_their_token_and_adapter(windq, 
         assert torch.equal(first[0][others], then[0][others])
         assert all(torch.equal(x[[0, 1, 3]], y[[0, 1, 3]]) for x, y in zip(first[1:], then[1:]))
         assert not torch.isfinite(then[1][2]).all() and not torch.isfinite(then[2][2]).all() and not torch.isfinite(then[0][[1, 3]]).all(1).any()
+
+
+@pytest.mark.parametrize("T,rows,cols,G,unit_rows,masked", SHAPES)
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_graph_of_both_ways_replays_what_eager_calls_give(windq, T, rows, cols, G, unit_rows, masked, dtype):
+    """Inputs change between replays, and the workspaces hold other calls' values by then."""
+    c = Case(windq, rows, cols, G, unit_rows, masked=masked, seed=1)
+    s = Side(windq, 4, 16, rows, cols, dtype, T, seed=2)
+    X, dY = tokens(T, cols, dtype, 1), tokens(T, rows, dtype, 2)
+    of = s.of_dev.clone()
+    ws = [windq.project_workspace(c.packed, X, s.adapters, grad=k) for k in (False, True)]
+    y, h = torch.empty(T, rows, dtype=dtype, device=DEV), torch.empty(T, 16, device=DEV)
+    outs = torch.empty_like(X), torch.empty(s.a.shape, device=DEV), torch.empty(s.b.shape, device=DEV)
+
+    def step():
+        windq.windq_project(c.packed, X, s.adapters, of, h=h, ws=ws[0], out=y)
+        windq.windq_project_grad(c.packed, dY, X, s.adapters, of, ws=ws[1], outs=outs)
+
+    step()
+    torch.cuda.synchronize()
+    G_ = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(G_):
+        step()
+    for k in range(3):
+        X.copy_(tokens(T, cols, dtype, 10 + k))
+        dY.copy_(tokens(T, rows, dtype, 20 + k))
+        of.copy_(of.roll(7))
+        for w in ws:
+            w.fill_(255)
+        G_.replay()
+        got = [t.clone() for t in (y, h, *outs)]
+        want = [windq.windq_project(c.packed, X, s.adapters, of), got[1], *windq.windq_project_grad(c.packed, dY, X, s.adapters, of)]
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+        windq.windq_project(c.packed, X, s.adapters, of, h=h)
+        assert torch.equal(got[1], h)
+        torch.cuda.synchronize()
