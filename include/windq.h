@@ -633,7 +633,7 @@ typedef struct windq_packed {
     const uint8_t* action;    /* [U] */
     const int64_t* code_off;  /* [U+1] */
     const uint8_t* codes;     /* 16-byte aligned; may be NULL with codes_bytes 0 (skip units alone) */
-    size_t codes_bytes;
+    size_t codes_bytes;       /* a multiple of 16 in windq_plan_layout's plans; with another windq_project serves few tokens more slowly */
     const float* scale;       /* [U*R_u] */
     const float* offset;      /* [U*R_u] */
     int32_t chunk_w;
