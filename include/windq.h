@@ -738,6 +738,84 @@ int windq_adamw(const windq_adamw_item* items /*HOST [n]*/, int64_t n, int32_t p
                 int64_t step, double lr, double beta1, double beta2, double eps, double weight_decay,
                 const float* grad_scale /*[1] or NULL*/, void* stream);
 
+/*
+ * Feed-forward blocks: a pair of packed matrices of one input, gate and up, whose products G and U are used as H = act(G) * U alone.
+ */
+enum windq_act {
+    WINDQ_SILU = 0,      /* x / (1 + e^-x)                                          */
+    WINDQ_GELU = 1,      /* x (1 + erf(x / sqrt 2)) / 2                             */
+    WINDQ_GELU_TANH = 2  /* x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2       */
+};
+
+/*
+ * Tokens in 8 bits, as windq_project8 and windq_gated8 take them: integers -127 .. 127 with one scale a token.
+ *   codes  [tokens][windq_tokens8_width(cols, chunk_w)], 16-byte aligned.  A chunk's columns lie together, zeros behind them up to
+ *          a multiple of 32 k: with chunk_w a multiple of 32 up to 128, or of 128, there are none and a token's row is its cols integers.
+ *   scale  [tokens]: x_c is scale * code_c
+ *   sums   [tokens][windq_tokens8_sums(cols, chunk_w)], 16-byte aligned: of the codes of each k-block (32 k columns, k <= 4), zeros up to a multiple of four
+ * A k-block is ceil(chunk_w / 32) steps of 32 columns, cut into as few parts of four steps at most as will do, all alike.
+ */
+typedef struct windq_tokens {
+    const int8_t* codes;
+    const float* scale;
+    const int32_t* sums;
+    int64_t tokens, cols;
+    int32_t chunk_w;
+    int32_t reserved;         /* set to 0 */
+} windq_tokens;
+
+/* Bytes of a token's codes, and how many sums it has; 0 if cols or chunk_w is out of range.  HOST only. */
+int64_t windq_tokens8_width(int64_t cols, int32_t chunk_w);
+int64_t windq_tokens8_sums(int64_t cols, int32_t chunk_w);
+
+/*
+ * Tokens to 8 bits, in fp32, one rounded operation after the other:
+ *   scale[t] = sigma = max_c |x_tc| / 127 (0 below the smallest normal fp32), code = clamp(rne(x * (1 / sigma)), -127, 127), 0 where sigma = 0
+ * A token that holds an infinity or a NaN gets the scale NaN and codes 0: its own products are NaN, no other's.
+ *   X  [tokens][cols], WINDQ_BF16 or WINDQ_F32, 16-byte aligned, leading dimension a multiple of 8
+ * codes, scale and sums as in windq_tokens, written whole.  Results are bit-reproducible.
+ */
+int windq_tokens8(const windq_mat* X, int32_t chunk_w, int8_t* codes, float* scale, int32_t* sums, void* stream);
+
+/*
+ * A packed plan in the order in which 8-bit products read it: laid out once, read by every call after that.
+ * windq_serving_layout (HOST only): where every unit's fields go, from the plan's treatments on the host.  image_off[U] is the image's size.  Codes
+ * of 3 and of 1.58 bits take 4 and 2; weights of skip units are copied (fp32 ones: 6 bytes); rows of a unit are filled up to a multiple of 32, chunks
+ * as windq_tokens says; 8 bytes a group and a unit beside them.
+ * windq_serving_lay: writes the image (256-byte aligned) of a packed matrix on the stream.  image_off is the layout's, on the DEVICE.  A unit whose
+ * entry of the plan is malformed counts as skip, as elsewhere; one whose fields do not fit in [image_off[u], image_off[u+1]) or in image_bytes, so that an
+ * image of another plan's layout is no harm to memory, counts as zeros.  P->mask is not supported (WINDQ_EINVAL): protected weights are windq_project's.
+ * WINDQ_EWORKSPACE: the image does not hold what stands ahead of the fields.
+ */
+typedef struct windq_serving {
+    const void* image;        /* as windq_serving_lay left it */
+    size_t image_bytes;
+    int64_t rows, cols, unit_rows;
+    int32_t chunk_w;
+    int32_t dtype;            /* W's */
+} windq_serving;
+int windq_serving_layout(const uint8_t* action /*HOST [U]*/, int64_t rows, int64_t cols, int32_t chunk_w, int64_t unit_rows, int32_t dtype,
+                         int64_t* image_off /*HOST [U+1]*/);
+int windq_serving_lay(const windq_packed* P, const int64_t* image_off /*[U+1]*/, void* image, size_t image_bytes, void* stream);
+
+/*
+ * 8-bit tokens through a plan laid out for them:
+ *   Y[t] = scale_t * sum_c w_hat[.][c] code_tc
+ * A group's sums over its chunk are exact integers; they are scaled and added up over chunks in fp32, in a fixed order:
+ * scale * sum f code + beta * sum code with f the weight's code (of 8 bits: less 128), so that before Y's own rounding a result differs from the exact one by a few 1e-7 of
+ * the sum of |scale f code| + |beta code|.  Weights of skip units are multiplied as they are.  Results are bit-reproducible.
+ * A group whose scale or offset is not finite, and a skip weight that is not, make their row's results not finite (infinities may come out as NaN); other rows keep theirs.
+ *   X has the plan's cols and chunk_w.  Y [tokens][rows] of y_dtype, ld_y >= rows (any), written whole (nothing past a row's end).
+ */
+int windq_project8(const windq_serving* P, const windq_tokens* X, void* Y, int32_t y_dtype, int64_t ld_y, void* stream);
+
+/*
+ * 8-bit tokens through gate and up, H[t] = act(G_t) * U_t, without G and U ever leaving the chip: each of them as windq_project8 has it, in fp32, and
+ * H rounded once.  Both plans of one shape, chunk_w, unit_rows and weight type, their treatments their own.
+ */
+int windq_gated8(const windq_serving* gate, const windq_serving* up, const windq_tokens* X, int32_t act, void* H, int32_t h_dtype, int64_t ld_h,
+                 void* stream);
+
 /* Workspace bytes a call needs for these shapes (0 if the shape is invalid). HOST only. */
 size_t windq_workspace_bytes(int32_t which_call, int32_t dtype, int64_t rows, int64_t cols,
                              int32_t chunk_w, int64_t unit_rows, int32_t K);

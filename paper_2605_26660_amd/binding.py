@@ -33,7 +33,8 @@ EXPORTS = (
     "windq_kernel_timer", "windq_kernel_timer_read", "windq_salient_select_batch", "windq_salient_encode_batch",
     "windq_refine_plan_batch", "windq_dequant_plan_batch", "windq_unit_features_exact_units",
     "windq_dequant_gemv", "windq_dequant_gemv_batch", "windq_project", "windq_project_grad",
-    "windq_project_workspace_bytes", "windq_adamw",
+    "windq_project_workspace_bytes", "windq_adamw", "windq_tokens8_width", "windq_tokens8_sums", "windq_tokens8",
+    "windq_serving_layout", "windq_serving_lay", "windq_project8", "windq_gated8",
 )
 
 
@@ -125,6 +126,16 @@ class windq_adamw_item(ctypes.Structure):
                 ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_int64)]
 
 
+class windq_tokens(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("sums", ctypes.c_void_p), ("tokens", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("chunk_w", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class windq_serving(ctypes.Structure):
+    _fields_ = [("image", ctypes.c_void_p), ("image_bytes", ctypes.c_size_t), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("unit_rows", ctypes.c_int64), ("chunk_w", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
 _lib = None          # what lib() gives: descriptors and items are the structures above, checked by ctypes
 _packed_lib = None   # the same entry points for this module's own calls, which pass the same words packed (_mats)
 
@@ -210,6 +221,16 @@ def _declare(lib, by_address):
     f64 = c.c_double
     lib.windq_adamw.argtypes = [by_address(windq_adamw_item), i64, i32, i32, i32, i64, f64, f64, f64, f64, f64, vp, vp]
     lib.windq_adamw.restype = c.c_int
+    ps, pt = by_address(windq_serving), by_address(windq_tokens)
+    for name in ("windq_tokens8_width", "windq_tokens8_sums"):
+        getattr(lib, name).argtypes, getattr(lib, name).restype = [i64, i32], i64
+    lib.windq_tokens8.argtypes = [pm, i32, vp, vp, vp, vp]
+    lib.windq_serving_layout.argtypes = [vp, i64, i64, i32, i64, i32, vp]
+    lib.windq_serving_lay.argtypes = [pp, vp, vp, sz, vp]
+    lib.windq_project8.argtypes = [ps, pt, vp, i32, i64, vp]
+    lib.windq_gated8.argtypes = [ps, ps, pt, i32, vp, i32, i64, vp]
+    for name in ("windq_tokens8", "windq_serving_layout", "windq_serving_lay", "windq_project8", "windq_gated8"):
+        getattr(lib, name).restype = c.c_int
     lib.windq_status_str.argtypes = [c.c_int]
     lib.windq_status_str.restype = c.c_char_p
     for name in ("windq_calib_stats", "windq_unit_features", "windq_fit_score_all_bits", "windq_plan_layout",
@@ -237,6 +258,7 @@ def _check(status: int, where: str):
 
 
 _DTYPE_CODES = {torch.float32: WINDQ_F32, torch.bfloat16: WINDQ_BF16}
+ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}    # enum windq_act
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -891,7 +913,7 @@ class Packed:
                 raise WindqError(WINDQ_EDTYPE, "Packed")
             if t.numel() < least or not t.is_contiguous():
                 raise WindqError(WINDQ_ESHAPE, "Packed")
-        self.W, self.rows, self.cols, self.chunk_w = W, W.shape[0], W.shape[1], chunk_w
+        self.W, self.rows, self.cols, self.chunk_w, self.unit_rows = W, W.shape[0], W.shape[1], chunk_w, unit_rows
         self.tensors = (action, code_off, codes, scale, offset, mask)
         self._mat = _mats((W,))
         self._words = array("Q", (_addr(self._mat), _ptr0(mask), action.data_ptr(), code_off.data_ptr(), codes.data_ptr(), codes.numel(),
@@ -1054,3 +1076,97 @@ def windq_adamw(items: AdamwItems, step: int, lr: float, beta1: float = 0.9, bet
         raise WindqError(WINDQ_EDTYPE, "windq_adamw")
     _check(_packed().windq_adamw(items.address, items.n, items.p_dtype, items.g_dtype, items.state_bits, step, lr, beta1, beta2, eps,
                                  weight_decay, _ptr(grad_scale), _stream()), "windq_adamw")
+
+
+# ------------------------------------------------- feed-forward blocks, and products with 8-bit tokens
+def _act_code(act: str) -> int:
+    code = ACTS.get(act)
+    if code is None:
+        raise WindqError(WINDQ_EINVAL, "act")
+    return code
+
+
+class Tokens8:
+    """Tokens in 8 bits: codes int8 [tokens x width], scale f32 [tokens], sums i32 [tokens x sums], as windq_tokens8 writes them for chunks of
+    chunk_w columns.  Described once; it keeps the tensors, and sees what is written into them later."""
+
+    def __init__(self, codes: torch.Tensor, scale: torch.Tensor, sums: torch.Tensor, cols: int, chunk_w: int):
+        _require_cuda(codes, scale, sums)
+        if codes.dtype != torch.int8 or scale.dtype != torch.float32 or sums.dtype != torch.int32:
+            raise WindqError(WINDQ_EDTYPE, "Tokens8")
+        width, n_sums = load().windq_tokens8_width(cols, chunk_w), load().windq_tokens8_sums(cols, chunk_w)
+        T = scale.numel()
+        if width == 0 or tuple(codes.shape) != (T, width) or tuple(sums.shape) != (T, n_sums) or scale.dim() != 1 or \
+                not all(t.is_contiguous() for t in (codes, scale, sums)):
+            raise WindqError(WINDQ_ESHAPE, "Tokens8")
+        self.codes, self.scale, self.sums, self.tokens, self.cols, self.chunk_w = codes, scale, sums, T, cols, chunk_w
+        self._words = array("Q", (codes.data_ptr(), scale.data_ptr(), sums.data_ptr(), T, cols, chunk_w))
+        self.address = _addr(self._words)
+
+    @classmethod
+    def empty(cls, tokens: int, cols: int, chunk_w: int, device) -> "Tokens8":
+        width, n_sums = load().windq_tokens8_width(cols, chunk_w), load().windq_tokens8_sums(cols, chunk_w)
+        if width == 0 or tokens < 0:
+            raise WindqError(WINDQ_ESHAPE, "Tokens8")
+        return cls(torch.empty(tokens, width, dtype=torch.int8, device=device), torch.empty(tokens, dtype=torch.float32, device=device),
+                   torch.empty(tokens, n_sums, dtype=torch.int32, device=device), cols, chunk_w)
+
+
+def windq_tokens8(X: torch.Tensor, chunk_w: int, out: Tokens8 | None = None) -> Tokens8:
+    """X [tokens x cols] (float32 or bfloat16) in 8 bits, one scale a token, for plans of chunks of chunk_w columns."""
+    _require_cuda(X)
+    if out is None:
+        out = Tokens8.empty(X.shape[0], X.shape[1], chunk_w, X.device)
+    if (out.tokens, out.cols, out.chunk_w) != (X.shape[0], X.shape[1], chunk_w):
+        raise WindqError(WINDQ_ESHAPE, "windq_tokens8")
+    m = _mats((X,))
+    _check(_packed().windq_tokens8(_addr(m), chunk_w, out.codes.data_ptr(), out.scale.data_ptr(), out.sums.data_ptr(), _stream()), "windq_tokens8")
+    return out
+
+
+class Serving:
+    """A packed matrix laid out for products with 8-bit tokens, on the current stream; the packed one is not needed afterwards.  action: the plan's
+    treatments on the host (uint8 [U]), or None: copied from the packed matrix (that waits for the device)."""
+
+    def __init__(self, packed: Packed, action: torch.Tensor | None = None):
+        on_device = packed.tensors[0]
+        U = (packed.rows // (packed.unit_rows or packed.rows)) * (packed.cols // packed.chunk_w)
+        host = on_device.cpu() if action is None else action
+        if host.is_cuda or host.dtype != torch.uint8:
+            raise WindqError(WINDQ_EDTYPE, "Serving")
+        if host.numel() < U or not host.is_contiguous():
+            raise WindqError(WINDQ_ESHAPE, "Serving")
+        off = torch.empty(U + 1, dtype=torch.int64)
+        dtype = _dtype_code(packed.W)
+        _check(load().windq_serving_layout(host.data_ptr(), packed.rows, packed.cols, packed.chunk_w, packed.unit_rows, dtype, off.data_ptr()), "Serving")
+        dev = packed.W.device
+        self.rows, self.cols, self.chunk_w, self.unit_rows = packed.rows, packed.cols, packed.chunk_w, packed.unit_rows
+        self.image_off = off.to(dev)
+        self.image = torch.empty(int(off[-1]), dtype=torch.uint8, device=dev)
+        _check(_packed().windq_serving_lay(packed.address, self.image_off.data_ptr(), self.image.data_ptr(), self.image.numel(), _stream()), "Serving")
+        self._words = array("Q", (self.image.data_ptr(), self.image.numel(), self.rows, self.cols, self.unit_rows, self.chunk_w | dtype << 32))
+        self.address = _addr(self._words)
+
+
+def _product8(where, serving, tokens, dtype, out):
+    """The output of a product of 8-bit tokens, and its leading dimension."""
+    _require_cuda(out)
+    y = out if out is not None else torch.empty(tokens.tokens, serving.rows, dtype=dtype, device=tokens.codes.device)
+    if tuple(y.shape) != (tokens.tokens, serving.rows) or y.stride(1) != 1:
+        raise WindqError(WINDQ_ESHAPE, where)
+    return y, _rows_apart(y, where)
+
+
+def windq_project8(serving: Serving, tokens: Tokens8, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Y [tokens x rows]: 8-bit tokens through a plan laid out for them.  out (float32 or bfloat16) or dtype says what comes out."""
+    y, ld = _product8("windq_project8", serving, tokens, dtype, out)
+    _check(_packed().windq_project8(serving.address, tokens.address, y.data_ptr(), _dtype_code(y), ld, _stream()), "windq_project8")
+    return y
+
+
+def windq_gated8(gate: Serving, up: Serving, tokens: Tokens8, act: str = "silu", dtype: torch.dtype = torch.bfloat16,
+                 out: torch.Tensor | None = None) -> torch.Tensor:
+    """H [tokens x rows] = act(gate's product) * up's product, act "silu", "gelu" or "gelu_tanh": 8-bit tokens through both."""
+    y, ld = _product8("windq_gated8", gate, tokens, dtype, out)
+    _check(_packed().windq_gated8(gate.address, up.address, tokens.address, _act_code(act), y.data_ptr(), _dtype_code(y), ld, _stream()), "windq_gated8")
+    return y

@@ -1,0 +1,467 @@
+// 8-bit tokens (windq_tokens8), a plan's form for serving them (windq_serving_lay), and their products (windq_project8, windq_gated8).
+#include <math.h>
+
+#include "windq_eight.hpp"
+
+namespace windq {
+
+int check_tokens(const windq_mat* M, int64_t width, bool vector);
+
+// ------------------------------------------------------------------------------------------------ tokens
+// A workgroup a token.  Its largest magnitude first, as bits: a NaN's are above an infinity's, and those above every number's.  Octets of the padded
+// width go to neighbouring threads; a k-block's sum is collected in LDS by integer additions, whose order does not matter.
+constexpr int TOKENS_SUMS = 4096;                          // k-blocks whose sums fit
+
+struct TokensArgs {
+    const void* X;
+    int64_t ld, T;
+    int8_t* codes;
+    float* scale;
+    int32_t* sums;
+    int32_t G, octets_chunk;   // octets of a chunk with its padding
+    int32_t octets_kb;
+    int64_t octets, sums_ld;   // of the padded width
+    int32_t n_kb;
+};
+
+template <typename XT>
+__device__ __forceinline__ bool tokens_octet(const TokensArgs& Q, const XT* __restrict__ x, int64_t o, float (&v)[8]) {
+    const int64_t j = (int64_t)((uint64_t)o / (uint32_t)Q.octets_chunk);
+    const int32_t in = (int32_t)(o - j * Q.octets_chunk);
+    if (in * 8 >= Q.G) return false;
+    load8(x + j * Q.G + in * 8, v);
+    return true;
+}
+
+template <typename XT>
+__global__ __launch_bounds__(256) void tokens8_kernel(const TokensArgs Q, const int64_t first) {
+    __shared__ uint32_t most[4];
+    __shared__ int32_t sums[TOKENS_SUMS];
+    const int64_t t = first + blockIdx.x;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const XT* __restrict__ const x = static_cast<const XT*>(Q.X) + t * Q.ld;
+    const bool own_sums = Q.n_kb <= TOKENS_SUMS;
+    if (own_sums)
+        for (int32_t k = threadIdx.x; k < Q.n_kb; k += 256) sums[k] = 0;
+    uint32_t m = 0;
+    for (int64_t o = threadIdx.x; o < Q.octets; o += 256) {
+        float v[8];
+        if (!tokens_octet(Q, x, o, v)) continue;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
+            m = b > m ? b : m;
+        }
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) {
+        const uint32_t b = (uint32_t)__shfl_xor((int)m, d, 64);
+        m = b > m ? b : m;
+    }
+    if (lane == 0) most[wave] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m = most[w] > m ? most[w] : m;
+    const bool finite = m < 0x7f800000u;
+    float sigma = __uint_as_float(m) / 127.0f;
+    if (sigma < 1.17549435e-38f) sigma = 0.0f;
+    const float inverse = finite && sigma > 0.0f ? 1.0f / sigma : 0.0f;
+    if (threadIdx.x == 0) Q.scale[t] = finite ? sigma : __uint_as_float(0x7fc00000u);
+    uint2* __restrict__ const to = reinterpret_cast<uint2*>(Q.codes + t * Q.octets * 8);
+    for (int64_t o = threadIdx.x; o < Q.octets; o += 256) {
+        float v[8];
+        uint32_t w[2] = {0u, 0u};
+        if (tokens_octet(Q, x, o, v)) {
+            int32_t sum = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float r = fminf(fmaxf(rintf(v[i] * inverse), -127.0f), 127.0f);
+                const int32_t q = finite ? (int32_t)r : 0;
+                sum += q;
+                w[i >> 2] |= ((uint32_t)q & 0xffu) << (8 * (i & 3));
+            }
+            if (own_sums && sum != 0) atomicAdd(&sums[(uint32_t)o / (uint32_t)Q.octets_kb], sum);
+        }
+        to[o] = make_uint2(w[0], w[1]);
+    }
+    if (!own_sums) return;
+    __syncthreads();
+    for (int64_t k = threadIdx.x; k < Q.sums_ld; k += 256) Q.sums[t * Q.sums_ld + k] = k < Q.n_kb ? sums[k] : 0;
+}
+
+// Sums of tokens of more k-blocks than fit LDS, a thread a sum, from the codes.
+__global__ __launch_bounds__(256) void tokens8_sums_kernel(const TokensArgs Q, const int64_t first) {
+    const int64_t i = (first + blockIdx.x) * 256 + threadIdx.x;
+    if (i >= Q.T * Q.sums_ld) return;
+    const int64_t t = i / Q.sums_ld, k = i - t * Q.sums_ld;
+    int32_t sum = 0;
+    if (k < Q.n_kb)
+        for (int32_t c = 0; c < Q.octets_kb * 8; ++c) sum += Q.codes[t * Q.octets * 8 + k * Q.octets_kb * 8 + c];
+    Q.sums[i] = sum;
+}
+
+// ------------------------------------------------------------------------------------------------ the plan's form for serving
+// A wavefront a row block of a unit and k-block; a lane gathers its 16 columns of every step.  Laid once, bound by nothing in particular.
+__device__ __forceinline__ int eight_code(int a, const uint8_t* __restrict__ row, int c) {
+    switch (a) {
+        case 1: return (int)row[c] - 128;
+        case 2: return (row[c >> 1] >> (4 * (c & 1))) & 15;
+        case 3: {
+            const int bit = 3 * c;
+            const uint32_t v = (uint32_t)row[bit >> 3] | ((bit & 7) > 5 ? (uint32_t)row[(bit >> 3) + 1] << 8 : 0u);
+            return (int)((v >> (bit & 7)) & 7u);
+        }
+        case 4: return (row[c >> 2] >> (2 * (c & 3))) & 3;
+        case 5: {
+            uint32_t v = row[c / 5];
+            for (int i = c % 5; i > 0; --i) v /= 3u;
+            return (int)(v % 3u);
+        }
+        default: return (row[c >> 3] >> (c & 7)) & 1;
+    }
+}
+
+__global__ __launch_bounds__(256) void serving_lay_kernel(const PackArgs P, const EightShape E, const int64_t* __restrict__ image_off, char* __restrict__ image,
+                                                          const int64_t bytes, const int64_t first) {
+    const int64_t id = (first + blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, sub = lane & 31, hh = lane >> 5;
+    const int64_t per_unit = E.RB * E.per_chunk;
+    const int64_t u = id / per_unit;
+    if (u >= E.U) return;
+    const int64_t i = (id - u * per_unit) / E.per_chunk;
+    const int32_t c = (int32_t)(id - u * per_unit - i * E.per_chunk);
+    const int64_t rb = u / E.n_chunks, j = u - rb * E.n_chunks;
+    int64_t base;
+    const int a = pk_action(P, u, base);
+    int kind = eight_kind(a);
+    const int64_t block = eight_bytes(kind, E.S, P.w_f32 != 0), need = block * per_unit, at = image_off[u], end = image_off[u + 1];
+    if (at < E.header || (at & 255) != 0 || end > bytes || end - at < need) kind = 7;
+    if (i == 0 && c == 0 && lane == 0)
+        reinterpret_cast<uint64_t*>(image)[u] = (kind == 7 ? 0ull : (uint64_t)at) | (uint64_t)kind << 56;
+    const int64_t lrow = i * EIGHT_ROWS + sub;
+    const bool in = lrow < P.R_u;
+    const int64_t row = rb * P.R_u + (in ? lrow : 0);
+    if (c == 0) {
+        const float scale = in ? P.scale[u * P.R_u + lrow] : 0.0f, offset = in ? P.offset[u * P.R_u + lrow] : 0.0f;
+        float alpha = scale, beta = offset;
+        if (a == 1) beta = fmaf(128.0f, scale, offset);
+        if (a == 5) beta = -scale;
+        if (a == 6) {
+            alpha = 2.0f * scale;
+            beta = -scale;
+        }
+        if (kind == 0 || kind == 7) {
+            alpha = in && kind == 0 ? 1.0f : 0.0f;
+            beta = 0.0f;
+        }
+        float* const to = reinterpret_cast<float*>(image + (E.U * 8 + 255) / 256 * 256) + ((rb * E.RB + i) * E.n_chunks + j) * 64;
+        to[hh * 32 + sub] = hh == 0 ? alpha : beta;
+    }
+    if (kind == 7) return;
+    char* const to = image + at + (i * E.per_chunk + c) * block;
+    const uint8_t* const codes = P.codes + base + (in ? lrow : 0) * pk_bytes_per_group(a, P.G);
+    uint32_t bits = 0;
+    for (int s = 0; s < E.S; ++s) {
+        const int32_t c0 = (c * E.S + s) * 32 + hh * 16;    // of the chunk's columns
+        if (kind == 0) {
+            for (int half = 0; half < 2; ++half) {
+                const int32_t col = c0 + half * 8;
+                const int terms = P.w_f32 != 0 ? 3 : 1;
+                for (int term = 0; term < terms; ++term) {
+                    const uint4 w = in && col < P.G ? skip_octet(P, row, j * P.G + col, term) : make_uint4(0u, 0u, 0u, 0u);
+                    reinterpret_cast<uint4*>(to)[((s * terms + term) * 2 + half) * 64 + lane] = w;
+                }
+            }
+            continue;
+        }
+        uint32_t v[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] = in && c0 + k < P.G ? (uint32_t)eight_code(a, codes, c0 + k) : 0u;
+        if (kind == 1) {
+            uint32_t w[4] = {};
+#pragma unroll
+            for (int k = 0; k < 16; ++k) w[k >> 2] |= (v[k] & 0xffu) << (8 * (k & 3));
+            reinterpret_cast<uint4*>(to)[s * 64 + lane] = make_uint4(w[0], w[1], w[2], w[3]);
+        } else if (kind == 2) {
+            uint32_t w[2] = {};
+#pragma unroll
+            for (int k = 0; k < 16; ++k) w[k >> 3] |= v[k] << (8 * (k & 3) + 4 * ((k >> 2) & 1));
+            reinterpret_cast<uint2*>(to)[s * 64 + lane] = make_uint2(w[0], w[1]);
+        } else if (kind == 4) {
+            uint32_t w = 0;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) w |= v[k] << (8 * (k & 3) + 2 * (k >> 2));
+            reinterpret_cast<uint32_t*>(to)[lane * E.S + s] = w;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) bits |= v[k] << (8 * (k & 3) + (k >> 2) + 4 * (s & 1));
+            if ((s & 1) != 0 || s + 1 == E.S) {
+                reinterpret_cast<uint32_t*>(to)[lane * ((E.S + 1) / 2) + (s >> 1)] = bits;
+                bits = 0;
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ the product
+// A row block and 32 N tokens a workgroup; its wavefronts share the k-blocks (of a pair: half of them the gate's, the others the up's) and
+// add up through LDS.  Fields and tokens go straight to the registers that the matrix instructions read.
+template <typename YT, int S, int N, int WAVES, bool PAIR>
+__global__ __launch_bounds__(WAVES * 64) void eight_kernel(const EightArgs Q, const int64_t first) {
+    constexpr int EACH = PAIR ? WAVES / 2 : WAVES;
+    __shared__ float red[WAVES][N * 16][64];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, sub = lane & 31, hh = lane >> 5;
+    const EightPlan& P = Q.P[PAIR ? wave / EACH : 0];
+    const int64_t id = first + blockIdx.x, tb = id / Q.NB, b = id - tb * Q.NB, t0 = tb * (N * 32);
+    const int64_t rb = b / Q.RB, i = b - rb * Q.RB;
+    const bool w_f32 = Q.w_f32 != 0;
+
+    const int8_t* x[N];
+    const int32_t* xs[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const int64_t t = t0 + n * 32 + sub < Q.T ? t0 + n * 32 + sub : Q.T - 1;
+        x[n] = Q.codes + t * Q.width + hh * 16;
+        xs[n] = Q.sums + t * Q.sums_ld;
+    }
+    const float* const affine = reinterpret_cast<const float*>(P.image + Q.affine) + b * Q.n_chunks * 64 + hh * 4;
+    f32x16 tot[N] = {};
+    for (int32_t kb = wave % EACH; kb < Q.n_kb; kb += EACH) {
+        const int32_t j = kb / Q.per_chunk, c = kb - j * Q.per_chunk;
+        const EightUnit u = eight_unit(P, rb * Q.n_chunks + j, Q.RB * Q.per_chunk, S, w_f32);
+        const int kind = __builtin_amdgcn_readfirstlane(u.kind);
+        if (kind == 7) continue;
+        const char* const fields = u.fields + (i * Q.per_chunk + c) * eight_bytes(kind, S, w_f32);
+        uint4 xv[S][N];
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int n = 0; n < N; ++n) xv[s][n] = *reinterpret_cast<const uint4*>(x[n] + (int64_t)kb * (32 * S) + s * 32);
+        if (kind == 0) {
+            const int terms = w_f32 ? 3 : 1;
+            const uint4* const w = reinterpret_cast<const uint4*>(fields) + lane;
+#pragma unroll
+            for (int s = 0; s < S; ++s)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    bf16x8 xb[N];
+#pragma unroll
+                    for (int n = 0; n < N; ++n) xb[n] = half == 0 ? eight_as_bf16(xv[s][n].x, xv[s][n].y) : eight_as_bf16(xv[s][n].z, xv[s][n].w);
+                    for (int term = 0; term < terms; ++term) {
+                        const bf16x8 wv = as_bf16x8(w[((s * terms + term) * 2 + half) * 64]);
+#pragma unroll
+                        for (int n = 0; n < N; ++n) tot[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv, xb[n], tot[n], 0, 0, 0);
+                    }
+                }
+            continue;
+        }
+        float4 al[4], be[4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            al[g] = *reinterpret_cast<const float4*>(affine + j * 64 + g * 8);
+            be[g] = *reinterpret_cast<const float4*>(affine + j * 64 + 32 + g * 8);
+        }
+        float sum[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) sum[n] = (float)xs[n][kb];
+        i32x16 acc[N] = {};
+        auto steps = [&](auto operand) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                const i32x4 f = operand(s);
+#pragma unroll
+                for (int n = 0; n < N; ++n) acc[n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f, as_i32x4(xv[s][n]), acc[n], 0, 0, 0);
+            }
+        };
+        if (kind == 6) {
+            uint32_t v[(S + 1) / 2];
+            __builtin_memcpy(v, fields + lane * (int)sizeof(v), sizeof(v));
+            steps([&](int s) { return eight_fields1(v[s >> 1], s & 1); });
+        } else if (kind == 4) {
+            uint32_t v[S];
+            __builtin_memcpy(v, fields + lane * (int)sizeof(v), sizeof(v));
+            steps([&](int s) { return eight_fields2(v[s]); });
+        } else if (kind == 2) {
+            uint2 v[S];
+#pragma unroll
+            for (int s = 0; s < S; ++s) v[s] = reinterpret_cast<const uint2*>(fields)[s * 64 + lane];
+            steps([&](int s) { return eight_fields4(v[s]); });
+        } else {
+            uint4 v[S];
+#pragma unroll
+            for (int s = 0; s < S; ++s) v[s] = reinterpret_cast<const uint4*>(fields)[s * 64 + lane];
+            steps([&](int s) { return as_i32x4(v[s]); });
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const float av[4] = {al[g].x, al[g].y, al[g].z, al[g].w}, bv[4] = {be[g].x, be[g].y, be[g].z, be[g].w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+                    tot[n][g * 4 + k] = fmaf(av[k], (float)acc[n][g * 4 + k], fmaf(bv[k], sum[n], tot[n][g * 4 + k]));
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) red[wave][n * 16 + k][lane] = tot[n][k];
+    __syncthreads();
+    const int32_t rows_left = Q.R_u - i * EIGHT_ROWS < EIGHT_ROWS ? (int32_t)(Q.R_u - i * EIGHT_ROWS) : EIGHT_ROWS;
+    for (int e = threadIdx.x; e < N * 1024; e += WAVES * 64) {
+        const int r = e & 31, n = e >> 5;                  // neighbouring lanes: neighbouring rows of a token
+        const int64_t t = t0 + n;
+        if (r >= rows_left || t >= Q.T) continue;
+        const int slot = (n >> 5) * 16 + (r >> 3) * 4 + (r & 3), at = ((r >> 2) & 1) * 32 + (n & 31);
+        float v = 0.0f, up = 0.0f;
+#pragma unroll
+        for (int w = 0; w < EACH; ++w) v += red[w][slot][at];
+        const float scale = Q.scale[t];
+        v *= scale;
+        if constexpr (PAIR) {
+#pragma unroll
+            for (int w = EACH; w < WAVES; ++w) up += red[w][slot][at];
+            float none;
+            v = activation<false>(Q.act, v, none) * (up * scale);
+        }
+        eight_store(static_cast<YT*>(Q.Y) + t * Q.ldy + rb * Q.R_u + i * EIGHT_ROWS + r, v);
+    }
+}
+
+template <typename YT, int S, bool PAIR>
+int launch_eight(const EightArgs& Q, hipStream_t st) {
+    constexpr int WAVES = 8;
+    if (Q.T <= 32) return launch_pieces(Q.NB, WAVES * 64, [&](int64_t first, dim3 g) { eight_kernel<YT, S, 1, WAVES, PAIR><<<g, dim3(WAVES * 64), 0, st>>>(Q, first); });
+    return launch_pieces(Q.NB * tokens_in(Q.T, 64), WAVES * 64, [&](int64_t first, dim3 g) { eight_kernel<YT, S, 2, WAVES, PAIR><<<g, dim3(WAVES * 64), 0, st>>>(Q, first); });
+}
+
+template <typename YT, bool PAIR>
+int launch_eight_steps(const EightArgs& Q, int S, hipStream_t st) {
+    switch (S) {
+        case 1: return launch_eight<YT, 1, PAIR>(Q, st);
+        case 2: return launch_eight<YT, 2, PAIR>(Q, st);
+        case 3: return launch_eight<YT, 3, PAIR>(Q, st);
+        default: return launch_eight<YT, 4, PAIR>(Q, st);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ checks
+static bool chunk_ok(int64_t cols, int32_t chunk_w) { return cols > 0 && chunk_w >= 8 && chunk_w <= WINDQ_MAX_CHUNK && chunk_w % 8 == 0 && cols % chunk_w == 0 && cols <= MOST_SIDE; }
+
+static int check_serving(const windq_serving* S, EightShape* E, EightPlan* P) {
+    if (S == nullptr || S->image == nullptr || !aligned(S->image, 256)) return WINDQ_EINVAL;
+    if (S->dtype != WINDQ_F32 && S->dtype != WINDQ_BF16) return WINDQ_EDTYPE;
+    if (!chunk_ok(S->cols, S->chunk_w) || S->rows <= 0 || S->rows > MOST_SIDE || S->unit_rows < 0 || (S->unit_rows != 0 && S->rows % S->unit_rows != 0)) return WINDQ_ESHAPE;
+    if (!sizes_fit(0, S->rows, S->cols, 0, 0)) return WINDQ_ESHAPE;
+    *E = eight_shape(S->rows, S->cols, S->unit_rows == 0 ? S->rows : S->unit_rows, S->chunk_w);
+    if ((int64_t)S->image_bytes < E->header) return WINDQ_EINVAL;
+    *P = {static_cast<const char*>(S->image), (int64_t)S->image_bytes, E->header};
+    return WINDQ_OK;
+}
+
+static int product(const windq_serving* first, const windq_serving* second, const windq_tokens* X, int32_t act, void* Y, int32_t y_dtype, int64_t ld_y, void* stream) {
+    EightArgs Q = {};
+    EightShape E, other;
+    int status = check_serving(first, &E, &Q.P[0]);
+    if (status != WINDQ_OK) return status;
+    if (second != nullptr) {
+        status = check_serving(second, &other, &Q.P[1]);
+        if (status != WINDQ_OK) return status;
+        if (other.rows != E.rows || other.cols != E.cols || other.G != E.G || other.R_u != E.R_u) return WINDQ_ESHAPE;
+        if (first->dtype != second->dtype) return WINDQ_EDTYPE;
+    }
+    if (X == nullptr) return WINDQ_EINVAL;
+    if (y_dtype != WINDQ_F32 && y_dtype != WINDQ_BF16) return WINDQ_EDTYPE;
+    if (X->cols != E.cols || X->chunk_w != E.G || X->tokens < 0) return WINDQ_ESHAPE;
+    if (!sizes_fit(X->tokens, E.rows, E.cols, 0, 0) || !sizes_fit(X->tokens, E.rows, E.width, 0, 0)) return WINDQ_ESHAPE;
+    if (ld_y < E.rows || ld_y > (int64_t)1 << 31) return WINDQ_ESHAPE;
+    if (X->tokens == 0) return WINDQ_OK;
+    if (X->codes == nullptr || X->scale == nullptr || X->sums == nullptr || Y == nullptr) return WINDQ_EINVAL;
+    if (!aligned(X->codes, 16) || !aligned(X->scale, 4) || !aligned(X->sums, 16) || !aligned(Y, y_dtype == WINDQ_F32 ? 4 : 2)) return WINDQ_EINVAL;
+    Q.codes = X->codes;
+    Q.scale = X->scale;
+    Q.sums = X->sums;
+    Q.T = X->tokens;
+    Q.Y = Y;
+    Q.ldy = ld_y;
+    Q.rows = E.rows;
+    Q.R_u = E.R_u;
+    Q.RB = E.RB;
+    Q.NB = E.NB;
+    Q.width = E.width;
+    Q.sums_ld = E.sums_ld;
+    Q.affine = (int64_t)round_up((size_t)E.U * 8, 256);
+    Q.n_chunks = E.n_chunks;
+    Q.per_chunk = E.per_chunk;
+    Q.n_kb = E.n_kb;
+    Q.act = act;
+    Q.w_f32 = first->dtype == WINDQ_F32;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (second != nullptr) return y_dtype == WINDQ_F32 ? launch_eight_steps<float, true>(Q, E.S, st) : launch_eight_steps<uint16_t, true>(Q, E.S, st);
+    return y_dtype == WINDQ_F32 ? launch_eight_steps<float, false>(Q, E.S, st) : launch_eight_steps<uint16_t, false>(Q, E.S, st);
+}
+
+}  // namespace windq
+
+using namespace windq;
+
+extern "C" int64_t windq_tokens8_width(int64_t cols, int32_t chunk_w) { return chunk_ok(cols, chunk_w) ? eight_shape(1, cols, 1, chunk_w).width : 0; }
+extern "C" int64_t windq_tokens8_sums(int64_t cols, int32_t chunk_w) { return chunk_ok(cols, chunk_w) ? eight_shape(1, cols, 1, chunk_w).sums_ld : 0; }
+
+extern "C" int windq_tokens8(const windq_mat* X, int32_t chunk_w, int8_t* codes, float* scale, int32_t* sums, void* stream) {
+    if (X == nullptr) return WINDQ_EINVAL;
+    const int status = check_tokens(X, X->cols, true);
+    if (status != WINDQ_OK) return status;
+    if (!chunk_ok(X->cols, chunk_w)) return WINDQ_ESHAPE;
+    const EightShape E = eight_shape(1, X->cols, 1, chunk_w);
+    if (!sizes_fit(X->rows, 1, E.width, 0, 0)) return WINDQ_ESHAPE;
+    if (X->rows == 0) return WINDQ_OK;
+    if (codes == nullptr || scale == nullptr || sums == nullptr) return WINDQ_EINVAL;
+    if (!aligned(codes, 16) || !aligned(scale, 4) || !aligned(sums, 16)) return WINDQ_EINVAL;
+    const TokensArgs Q = {X->data, X->ld, X->rows, codes, scale, sums, chunk_w, E.per_chunk * E.S * 4, E.S * 4, E.width / 8, E.sums_ld, E.n_kb};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int launched = launch_pieces(X->rows, 256, [&](int64_t first, dim3 g) {
+        if (X->dtype == WINDQ_F32) tokens8_kernel<float><<<g, dim3(256), 0, st>>>(Q, first);
+        else tokens8_kernel<uint16_t><<<g, dim3(256), 0, st>>>(Q, first);
+    });
+    if (launched != WINDQ_OK || E.n_kb <= TOKENS_SUMS) return launched;
+    return launch_pieces(tokens_in(X->rows * E.sums_ld, 256), 256, [&](int64_t first, dim3 g) { tokens8_sums_kernel<<<g, dim3(256), 0, st>>>(Q, first); });
+}
+
+extern "C" int windq_serving_layout(const uint8_t* action, int64_t rows, int64_t cols, int32_t chunk_w, int64_t unit_rows, int32_t dtype, int64_t* image_off) {
+    if (action == nullptr || image_off == nullptr) return WINDQ_EINVAL;
+    if (dtype != WINDQ_F32 && dtype != WINDQ_BF16) return WINDQ_EDTYPE;
+    if (!chunk_ok(cols, chunk_w) || rows <= 0 || rows > MOST_SIDE || unit_rows < 0 || (unit_rows != 0 && rows % unit_rows != 0) || !sizes_fit(0, rows, cols, 0, 0)) return WINDQ_ESHAPE;
+    const EightShape E = eight_shape(rows, cols, unit_rows == 0 ? rows : unit_rows, chunk_w);
+    int64_t at = E.header;
+    for (int64_t u = 0; u < E.U; ++u) {
+        if (action[u] >= WINDQ_N_ACTIONS) return WINDQ_EINVAL;
+        image_off[u] = at;
+        at += eight_bytes(eight_kind(action[u]), E.S, dtype == WINDQ_F32) * E.RB * E.per_chunk;
+    }
+    image_off[E.U] = at;
+    return WINDQ_OK;
+}
+
+extern "C" int windq_serving_lay(const windq_packed* P, const int64_t* image_off, void* image, size_t image_bytes, void* stream) {
+    PackArgs A = {};
+    const int status = check_packed(P, &A);
+    if (status != WINDQ_OK) return status;
+    if (A.mask != nullptr || image_off == nullptr || image == nullptr || !aligned(image_off, 8) || !aligned(image, 256)) return WINDQ_EINVAL;
+    if (!sizes_fit(0, A.rows, A.cols, 0, 0)) return WINDQ_ESHAPE;
+    const EightShape E = eight_shape(A.rows, A.cols, A.R_u, A.G);
+    if (image_bytes > (size_t)1 << 47) return WINDQ_ESHAPE;
+    if ((int64_t)image_bytes < E.header) return WINDQ_EWORKSPACE;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return launch_pieces(tokens_in(E.U * E.RB * E.per_chunk, 4), 256,
+                         [&](int64_t first, dim3 g) { serving_lay_kernel<<<g, dim3(256), 0, st>>>(A, E, image_off, static_cast<char*>(image), (int64_t)image_bytes, first); });
+}
+
+extern "C" int windq_project8(const windq_serving* P, const windq_tokens* X, void* Y, int32_t y_dtype, int64_t ld_y, void* stream) {
+    return product(P, nullptr, X, WINDQ_SILU, Y, y_dtype, ld_y, stream);
+}
+
+extern "C" int windq_gated8(const windq_serving* gate, const windq_serving* up, const windq_tokens* X, int32_t act, void* H, int32_t h_dtype, int64_t ld_h, void* stream) {
+    if (up == nullptr || act < WINDQ_SILU || act > WINDQ_GELU_TANH) return WINDQ_EINVAL;
+    return product(gate, up, X, act, H, h_dtype, ld_h, stream);
+}

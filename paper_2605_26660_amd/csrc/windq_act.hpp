@@ -1,0 +1,40 @@
+// The activations of a gated feed-forward block and their slopes, in fp32.
+//   silu      x s(x), s(x) = 1 / (1 + e^-x)                    slope  s (1 + x (1 - s))
+//   gelu      x Phi(x), Phi(x) = (1 + erf(x / sqrt 2)) / 2     slope  Phi + x e^(-x^2 / 2) / sqrt(2 pi)
+//   gelu_tanh x t(x), t(x) = s(2 k (x + 0.044715 x^3)), k = sqrt(2 / pi), since (1 + tanh z) / 2 = s(2 z)
+//                                                              slope  t + x t (1 - t) 2 k (1 + 3 0.044715 x^2)
+#pragma once
+
+#include "windq_common.hpp"
+
+namespace windq {
+
+#ifdef __HIPCC__
+
+__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
+
+// act(x), and its slope where SLOPE.
+template <bool SLOPE>
+__device__ __forceinline__ float activation(int act, float x, float& slope) {
+    float y;
+    if (act == WINDQ_SILU) {
+        const float s = sigmoid(x);
+        y = x * s;
+        if (SLOPE) slope = s * (1.0f + x * (1.0f - s));
+    } else if (act == WINDQ_GELU) {
+        // erfc in the place of 1 + erf: Phi keeps its digits far to the left
+        const float phi = 0.5f * erfcf(x * -0.70710678118654752f);
+        y = x * phi;
+        if (SLOPE) slope = phi + x * (expf(-0.5f * x * x) * 0.39894228040143268f);
+    } else {
+        constexpr float K2 = 1.5957691216057308f;          // 2 sqrt(2 / pi)
+        const float x2 = x * x, t = sigmoid(K2 * (x + 0.044715f * x2 * x));
+        y = x * t;
+        if (SLOPE) slope = t + x * (t * (1.0f - t)) * (K2 * (1.0f + 0.134145f * x2));
+    }
+    return y;
+}
+
+#endif  // __HIPCC__
+
+}  // namespace windq

@@ -1,0 +1,158 @@
+// Products of 8-bit tokens with a packed plan: the tokens' and the plan's forms, and what their kernels share.
+//
+// A token is x_c = sigma q_c with integers q_c of eight bits; a group's weights are w_c = alpha f_c + beta with f_c its code, or the code less 128
+// where it has eight bits.  So
+//     sum_c w_c x_c = sigma * sum over chunks of (alpha * sum_c f_c q_c + beta * sum_c q_c)
+// and both sums over a chunk are exact in 32-bit integers (512 columns x 128 x 127 at most): the matrix instructions multiply codes as they are, at
+// twice the rate of bfloat16, and a code needs no more unpacking than a shift and a mask of four at a time.
+//     8 bits  code - 128, beta = offset + 128 scale     4, 3 and 2 bits  code, beta = offset
+//     1.58    trit 0 .. 2, beta = -scale                1 bit            bit 0 or 1, alpha = 2 scale, beta = -scale
+//
+// A chunk's columns are cut into k-blocks of 32 S columns, S <= 4 alike; where they do not come out even the last one is filled with zeros, in
+// the tokens and in the plan.  In a step of 32 columns the lower half of a wavefront's lanes takes the first 16 of them, the upper half the others.
+#pragma once
+
+#include "windq_act.hpp"
+#include "windq_adapters.hpp"
+
+namespace windq {
+
+constexpr int EIGHT_ROWS = 32;                             // rows of a row block: the M side of 32x32x32 instructions
+
+struct EightShape {
+    int64_t rows, cols, R_u;
+    int32_t G, n_chunks;
+    int32_t S, per_chunk;      // steps of a k-block, k-blocks of a chunk
+    int32_t n_kb;
+    int64_t width, sums_ld;    // bytes of a token, sums of a token (in fours)
+    int64_t RB;                // row blocks of a unit
+    int64_t n_rb, NB;          // unit row blocks; row blocks of the matrix
+    int64_t U, header;         // units; bytes ahead of the fields
+};
+
+// How a chunk is cut: as few k-blocks as have four steps at most, alike.
+inline void eight_cut(int32_t G, int32_t* S, int32_t* per_chunk) {
+    const int32_t steps = (G + 31) / 32;
+    *per_chunk = (steps + 3) / 4;
+    *S = (steps + *per_chunk - 1) / *per_chunk;
+}
+
+// The serving form's first part: a word a unit (offset of its fields, 48 bits, and its kind, top byte), then for every unit and row block
+// of it the 32 rows' alpha and beta.
+inline EightShape eight_shape(int64_t rows, int64_t cols, int64_t R_u, int32_t G) {
+    EightShape E;
+    E.rows = rows;
+    E.cols = cols;
+    E.R_u = R_u;
+    E.G = G;
+    E.n_chunks = (int32_t)(cols / G);
+    eight_cut(G, &E.S, &E.per_chunk);
+    E.n_kb = E.n_chunks * E.per_chunk;
+    E.width = (int64_t)E.n_kb * E.S * 32;
+    E.sums_ld = ((int64_t)E.n_kb + 3) / 4 * 4;
+    E.RB = (R_u + EIGHT_ROWS - 1) / EIGHT_ROWS;
+    E.n_rb = rows / R_u;
+    E.NB = E.n_rb * E.RB;
+    E.U = E.n_rb * E.n_chunks;
+    E.header = (int64_t)round_up((size_t)E.U * 8, 256) + E.U * E.RB * 256;
+    return E;
+}
+
+// Kinds of fields: 0 weights that stay as they are, 1: 8 bits, 2: 4 bits (3 as well), 4: 2 bits (trits as well), 6: 1 bit, 7: nothing (zeros).
+__host__ __device__ inline int eight_kind(int action) { return action == 3 ? 2 : (action == 5 ? 4 : action); }
+
+// Bytes of a row block's fields of one k-block.
+//   8 bits   [step][lane][16 bytes]      4 bits [step][lane][8 bytes]     2 bits [lane][step][4 bytes]     1 bit [lane][pair of steps][4 bytes]
+//   weights  [step][term][half of its 16 columns][lane][8 bfloat16], one term, or three where the weights are fp32
+// A word's four bytes hold columns 4 i + (0 .. 3) at bits b i of each byte, b bits a field: w >> b i, masked, are four operands of the matrix instruction.
+__host__ __device__ inline int64_t eight_bytes(int kind, int S, bool w_f32) {
+    switch (kind) {
+        case 0: return (w_f32 ? 6144 : 2048) * (int64_t)S;
+        case 1: return 1024 * (int64_t)S;
+        case 2: return 512 * (int64_t)S;
+        case 4: return 256 * (int64_t)S;
+        case 6: return 256 * (int64_t)((S + 1) / 2);
+        default: return 0;
+    }
+}
+
+struct EightPlan {
+    const char* image;
+    int64_t bytes;
+    int64_t header;
+};
+
+struct EightArgs {
+    EightPlan P[2];            // gate and up, or one
+    const int8_t* codes;
+    const float* scale;
+    const int32_t* sums;
+    int64_t T;
+    void* Y;
+    int64_t ldy;
+    int64_t rows, R_u, RB, NB, width, sums_ld, affine;      // affine: where alpha and beta begin
+    int32_t n_chunks, per_chunk, n_kb, act, w_f32;
+};
+
+#ifdef __HIPCC__
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ i32x4 as_i32x4(uint4 v) { return __builtin_bit_cast(i32x4, v); }
+
+// Where a unit's fields lie and what they are; what does not fit the image counts as nothing.
+struct EightUnit {
+    const char* fields;
+    int kind;
+};
+__device__ __forceinline__ EightUnit eight_unit(const EightPlan& P, int64_t u, int64_t blocks, int S, bool w_f32) {
+    const uint64_t word = reinterpret_cast<const uint64_t*>(P.image)[u];
+    const int64_t at = (int64_t)(word & 0xffffffffffffull);
+    const int kind = (int)(word >> 56);
+    const int64_t need = eight_bytes(kind, S, w_f32) * blocks;
+    const bool fits = kind < 7 && kind != 3 && kind != 5 && at >= P.header && (at & 255) == 0 && at <= P.bytes - need;
+    return {P.image + at, fits ? kind : 7};
+}
+
+// Operands of step s out of a lane's fields.
+__device__ __forceinline__ i32x4 eight_fields4(uint2 v) {
+    i32x4 f;
+    f[0] = (int)(v.x & 0x0f0f0f0fu);
+    f[1] = (int)((v.x >> 4) & 0x0f0f0f0fu);
+    f[2] = (int)(v.y & 0x0f0f0f0fu);
+    f[3] = (int)((v.y >> 4) & 0x0f0f0f0fu);
+    return f;
+}
+__device__ __forceinline__ i32x4 eight_fields2(uint32_t v) {
+    i32x4 f;
+    f[0] = (int)(v & 0x03030303u);
+    f[1] = (int)((v >> 2) & 0x03030303u);
+    f[2] = (int)((v >> 4) & 0x03030303u);
+    f[3] = (int)((v >> 6) & 0x03030303u);
+    return f;
+}
+__device__ __forceinline__ i32x4 eight_fields1(uint32_t v, int odd) {
+    i32x4 f;
+    f[0] = (int)((v >> (4 * odd)) & 0x01010101u);
+    f[1] = (int)((v >> (4 * odd + 1)) & 0x01010101u);
+    f[2] = (int)((v >> (4 * odd + 2)) & 0x01010101u);
+    f[3] = (int)((v >> (4 * odd + 3)) & 0x01010101u);
+    return f;
+}
+
+// Eight of a token's integers as bfloat16: exact.
+__device__ __forceinline__ bf16x8 eight_as_bf16(uint32_t a, uint32_t b) {
+    auto pair = [](uint32_t v, int lo) {
+        const float x = (float)(int)(int8_t)(v >> (8 * lo)), y = (float)(int)(int8_t)(v >> (8 * lo + 8));
+        return __float_as_uint(x) >> 16 | (__float_as_uint(y) & 0xffff0000u);
+    };
+    return as_bf16x8(make_uint4(pair(a, 0), pair(a, 2), pair(b, 0), pair(b, 2)));
+}
+
+__device__ __forceinline__ void eight_store(float* p, float v) { *p = v; }
+__device__ __forceinline__ void eight_store(uint16_t* p, float v) { *p = (uint16_t)f32_to_bf16_bits(v); }
+
+#endif  // __HIPCC__
+
+}  // namespace windq
