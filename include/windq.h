@@ -816,6 +816,38 @@ int windq_project8(const windq_serving* P, const windq_tokens* X, void* Y, int32
 int windq_gated8(const windq_serving* gate, const windq_serving* up, const windq_tokens* X, int32_t act, void* H, int32_t h_dtype, int64_t ld_h,
                  void* stream);
 
+/*
+ * Tokens as they are through gate and up in one call, for training and for serving without rounding them:
+ *   G[t] = w_gate x_t,   U[t] = w_up x_t,   H[t] = act(G[t]) * U[t]
+ * G and U as windq_project has its product (the same sums, masks and treatment of what is not finite), in fp32; the activation in fp32; H rounded once.
+ * An infinite G makes silu and the gelus what fp32 makes of their formulas (-infinity: NaN).
+ *   X  [tokens][cols] as for windq_project; H [tokens][rows] of X's type, ld_h >= rows (any), written whole
+ *   G, U  [tokens][rows] of X's type, ld_save >= rows: the products, rounded once, that windq_gated_grad starts from; both or neither
+ * gate and up: of one shape, chunk_w, unit_rows and weight type; treatments and masks are their own.  At most 2^31 - 1 tokens x rows.
+ * Workspace: windq_gated_workspace_bytes (256-byte aligned), written anew by every call.
+ * Low-rank adapters of gate or up are windq_project's; dG and dU below are what their gradients (windq_project_grad with P NULL) start from.
+ */
+int windq_gated(const windq_packed* gate /*HOST*/, const windq_packed* up /*HOST*/, const windq_mat* X, int32_t act, void* H, int64_t ld_h,
+                void* G /*or NULL*/, void* U /*or NULL*/, int64_t ld_save, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The way back of windq_gated:
+ *   dG = dH * U * act'(G),   dU = dH * act(G),   dX[t] = w_gate^T dG[t] + w_up^T dU[t]
+ *   dH  [tokens][rows] (leading dimension >= rows, any); G, U of its type as windq_gated left them
+ *   dX  [tokens][cols] of that type, ld_dx >= cols, or NULL: not wanted (then no workspace is either)
+ *   dG, dU [tokens][rows] of that type, ld_d >= rows; both or neither, not NULL where dX is
+ * dG and dU are formed in fp32 and rounded once on their way out.  In WINDQ_BF16 they and the weights enter dX's product in half precision (11 bits), each token and
+ * each chunk times a power of two of its own, so that dX's own rounding outweighs theirs by far; in WINDQ_F32 neither is rounded.  Sums are fp32 in a fixed
+ * order: results are bit-reproducible.  A token that holds something not finite, or a weight that is not, makes what the formula multiplies it with not finite (infinities may come
+ * out as NaN); other tokens and columns keep their values.  No output may overlap an input.  At most 2^31 - 1 tokens x rows and tokens x cols, 2^30 - 512 rows.
+ */
+int windq_gated_grad(const windq_packed* gate /*HOST*/, const windq_packed* up /*HOST*/, const windq_mat* dH, const void* G, const void* U, int64_t ld_save,
+                     int32_t act, void* dX /*or NULL*/, int64_t ld_dx, void* dG /*or NULL*/, void* dU /*or NULL*/, int64_t ld_d, void* ws,
+                     size_t ws_bytes, void* stream);
+
+/* Workspace of windq_gated (grad = 0) or windq_gated_grad (grad = 1); 0 if a size is out of range.  It never shrinks with more tokens.  HOST only. */
+size_t windq_gated_workspace_bytes(int32_t grad, int32_t dtype, int64_t tokens, int64_t rows, int64_t cols, int32_t chunk_w);
+
 /* Workspace bytes a call needs for these shapes (0 if the shape is invalid). HOST only. */
 size_t windq_workspace_bytes(int32_t which_call, int32_t dtype, int64_t rows, int64_t cols,
                              int32_t chunk_w, int64_t unit_rows, int32_t K);

@@ -9,6 +9,6 @@ from .binding import (  # noqa: F401
     windq_salient_select_batch, windq_salient_encode_batch, windq_refine_plan_batch, windq_dequant_plan_batch, windq_unit_features_exact_units,
     CALL_DEQUANT_GEMV, windq_dequant_gemv, windq_dequant_gemv_batch,
     ADAMW_BLOCK, MAX_RANK, AdamwItems, Adapters, Packed, project_workspace, windq_adamw, windq_project, windq_project_grad,
-    Serving, Tokens8, windq_gated8, windq_project8, windq_tokens8,
+    Serving, Tokens8, gated_workspace, windq_gated, windq_gated8, windq_gated_grad, windq_project8, windq_tokens8,
 )
 from . import synth  # noqa: F401

@@ -35,6 +35,7 @@ EXPORTS = (
     "windq_dequant_gemv", "windq_dequant_gemv_batch", "windq_project", "windq_project_grad",
     "windq_project_workspace_bytes", "windq_adamw", "windq_tokens8_width", "windq_tokens8_sums", "windq_tokens8",
     "windq_serving_layout", "windq_serving_lay", "windq_project8", "windq_gated8",
+    "windq_gated", "windq_gated_grad", "windq_gated_workspace_bytes",
 )
 
 
@@ -229,7 +230,11 @@ def _declare(lib, by_address):
     lib.windq_serving_lay.argtypes = [pp, vp, vp, sz, vp]
     lib.windq_project8.argtypes = [ps, pt, vp, i32, i64, vp]
     lib.windq_gated8.argtypes = [ps, ps, pt, i32, vp, i32, i64, vp]
-    for name in ("windq_tokens8", "windq_serving_layout", "windq_serving_lay", "windq_project8", "windq_gated8"):
+    lib.windq_gated.argtypes = [pp, pp, pm, i32, vp, i64, vp, vp, i64, vp, sz, vp]
+    lib.windq_gated_grad.argtypes = [pp, pp, pm, vp, vp, i64, i32, vp, i64, vp, vp, i64, vp, sz, vp]
+    lib.windq_gated_workspace_bytes.argtypes = [i32, i32, i64, i64, i64, i32]
+    lib.windq_gated_workspace_bytes.restype = sz
+    for name in ("windq_tokens8", "windq_serving_layout", "windq_serving_lay", "windq_project8", "windq_gated8", "windq_gated", "windq_gated_grad"):
         getattr(lib, name).restype = c.c_int
     lib.windq_status_str.argtypes = [c.c_int]
     lib.windq_status_str.restype = c.c_char_p
@@ -1170,3 +1175,69 @@ def windq_gated8(gate: Serving, up: Serving, tokens: Tokens8, act: str = "silu",
     y, ld = _product8("windq_gated8", gate, tokens, dtype, out)
     _check(_packed().windq_gated8(gate.address, up.address, tokens.address, _act_code(act), y.data_ptr(), _dtype_code(y), ld, _stream()), "windq_gated8")
     return y
+
+
+def gated_workspace(gate: Packed, up: Packed, X: torch.Tensor, grad: bool = False) -> torch.Tensor:
+    """Workspace of windq_gated (or windq_gated_grad) for tokens like X, or their gradients (any fewer of them fit too)."""
+    need = load().windq_gated_workspace_bytes(int(grad), _dtype_code(X), X.shape[0], gate.rows, gate.cols, gate.chunk_w)
+    return torch.empty(max(int(need), 256), dtype=torch.uint8, device=X.device)
+
+
+def _both_alike(a, b, shape, dtype, where):
+    """Two tensors [tokens x rows] of one stride: that stride."""
+    for t in (a, b):
+        if t.dtype != dtype:
+            raise WindqError(WINDQ_EDTYPE, where)
+        if tuple(t.shape) != shape or t.stride(1) != 1:
+            raise WindqError(WINDQ_ESHAPE, where)
+    _require_cuda(a, b)
+    if a.stride(0) != b.stride(0) and shape[0] > 1:
+        raise WindqError(WINDQ_ESHAPE, where)
+    return _rows_apart(a, where)
+
+
+def windq_gated(gate: Packed, up: Packed, X: torch.Tensor, act: str = "silu", save=None, ws: torch.Tensor | None = None,
+                out: torch.Tensor | None = None) -> torch.Tensor:
+    """H [tokens x rows] of X's type = act(gate's product) * up's product, act "silu", "gelu" or "gelu_tanh".  save: (G, U) to be filled with the
+    products, of H's shape and type and of one stride (windq_gated_grad starts from them), or None."""
+    _require_cuda(X, out, ws)
+    T = X.shape[0]
+    h = out if out is not None else torch.empty(T, gate.rows, dtype=X.dtype, device=X.device)
+    if h.dtype != X.dtype or tuple(h.shape) != (T, gate.rows) or h.stride(1) != 1:
+        raise WindqError(WINDQ_EDTYPE if h.dtype != X.dtype else WINDQ_ESHAPE, "windq_gated")
+    ld_h, ld_save = _rows_apart(h, "windq_gated"), gate.rows
+    g, u = (None, None) if save is None else save
+    if save is not None:
+        ld_save = _both_alike(g, u, (T, gate.rows), X.dtype, "windq_gated")
+    if ws is None:
+        ws = gated_workspace(gate, up, X)
+    m = _mats((X,))
+    _check(_packed().windq_gated(gate.address, up.address, _addr(m), _act_code(act), h.data_ptr(), ld_h, _ptr(g), _ptr(u), ld_save, ws.data_ptr(),
+                                 ws.numel(), _stream()), "windq_gated")
+    return h
+
+
+def windq_gated_grad(gate: Packed, up: Packed, dH: torch.Tensor, G: torch.Tensor, U: torch.Tensor, act: str = "silu", ws: torch.Tensor | None = None,
+                     outs=None, want_dx: bool = True, want_dgu: bool = True):
+    """The way back of windq_gated: dH [tokens x rows], G and U as it saved them (of one stride).  outs: (dX, dG, dU), any of them None to be allocated (dG and dU
+    of one stride). -> (dX [tokens x cols] or None, dG, dU [tokens x rows] or None, None), of dH's type."""
+    _require_cuda(dH, ws)
+    T = dH.shape[0]
+    if dH.shape[1] != gate.rows:
+        raise WindqError(WINDQ_ESHAPE, "windq_gated_grad")
+    ld_save = _both_alike(G, U, (T, gate.rows), dH.dtype, "windq_gated_grad")
+    dx, dg, du = (None, None, None) if outs is None else outs
+    _require_cuda(dx, dg, du)
+    new = lambda width: torch.empty(T, width, dtype=dH.dtype, device=dH.device)  # noqa: E731
+    dx = (new(gate.cols) if dx is None else dx) if want_dx else None
+    dg, du = ((new(gate.rows) if t is None else t) if want_dgu else None for t in (dg, du))
+    if dx is not None and (dx.dtype != dH.dtype or tuple(dx.shape) != (T, gate.cols) or dx.stride(1) != 1):
+        raise WindqError(WINDQ_EDTYPE if dx.dtype != dH.dtype else WINDQ_ESHAPE, "windq_gated_grad")
+    ld_dx = gate.cols if dx is None else _rows_apart(dx, "windq_gated_grad")
+    ld_d = gate.rows if dg is None else _both_alike(dg, du, (T, gate.rows), dH.dtype, "windq_gated_grad")
+    if ws is None and dx is not None:
+        ws = gated_workspace(gate, up, dH, grad=True)
+    m = _mats((dH,))
+    _check(_packed().windq_gated_grad(gate.address, up.address, _addr(m), G.data_ptr(), U.data_ptr(), ld_save, _act_code(act), _ptr(dx), ld_dx, _ptr(dg),
+                                      _ptr(du), ld_d, _ptr(ws), 0 if ws is None else ws.numel(), _stream()), "windq_gated_grad")
+    return dx, dg, du

@@ -1,0 +1,478 @@
+// windq_gated: a batch of tokens through a pair of packed matrices, gate and up, of which act(gate) * up is kept; and its way back.
+//   G[t] = w_gate x_t,   U[t] = w_up x_t,   H[t] = act(G[t]) * U[t]
+//   dG = dH U act'(G),   dU = dH act(G),    dX[t] = w_gate^T dG[t] + w_up^T dU[t]
+#include <math.h>
+
+#include "windq_dx.hpp"
+#include "windq_project_any.hpp"
+
+namespace windq {
+
+struct GatedWs {
+    size_t planes, frag, few_xs, fields[2], unit[2], xs, beta[2], alpha[2], total;
+};
+
+GatedWs gated_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t G) {
+    GatedWs w;
+    size_t at = 0;
+    auto take = [&at](size_t bytes) {
+        const size_t here = at;
+        at += round_up(bytes, 256);
+        return here;
+    };
+    w.planes = take(dtype == WINDQ_F32 ? (size_t)(3 * T * cols) * 2 : 0);
+    const bool few = dtype == WINDQ_BF16;                   // fewer tokens than asked for fit too
+    const int64_t few_tokens = T < few_most(rows, cols, G) ? tokens_in(T, 64) * 64 : few_most(rows, cols, G);
+    w.frag = take(few ? (size_t)cols * (size_t)few_tokens * 2 : 0);
+    w.few_xs = take(few ? (size_t)(cols / 64 + 1) * (size_t)few_tokens * 4 : 0);
+    const bool many = T > PROJECT_FEW;
+    w.xs = take(many ? (size_t)(cols / 64) * (size_t)T * 16 : 0);
+    for (int m = 0; m < 2; ++m) {
+        w.fields[m] = take(many ? (size_t)(rows * cols) / (G == 128 || G == 96 || G == 64 ? 2 : 1) : 0);
+        w.unit[m] = take(many ? (size_t)((rows + PT_STRIP - 1) / PT_STRIP) * (size_t)(cols / 64) * sizeof(KbWord) : 0);
+        w.beta[m] = take(many ? (size_t)(cols / 64) * (size_t)rows * 16 : 0);
+        w.alpha[m] = take(many ? (size_t)(cols / G) * (size_t)rows * 4 : 0);
+    }
+    w.total = at == 0 ? 256 : at;
+    return w;
+}
+
+template <typename XT, int S>
+int launch_gated_tiles(const ProjectArgs& Q, char* ws, const GatedWs& at, hipStream_t st) {
+    TileArgs A = {};
+    A.P = Q.P;
+    A.X = Q.X;
+    A.ldx = Q.ldx;
+    A.plane = Q.plane;
+    A.raw = Q.raw;
+    A.ld_raw = Q.ld_raw;
+    A.T = Q.T;
+    A.Y = Q.Y;
+    A.ldy = Q.ldy;
+    A.xs = reinterpret_cast<uint4*>(ws + at.xs);
+    A.unit_fields = Q.P.R_u * Q.P.G / (tile_natural(Q.P.G, S) ? 2 : 1);
+    A.n_kb = (int32_t)(Q.P.cols / (16 * S));
+    A.row_blocks = (uint32_t)((Q.P.rows + PT_ROWS / 2 - 1) / (PT_ROWS / 2));
+    A.pair = Q.pair;
+    auto matrix = [&](int m) {
+        A.fields = reinterpret_cast<uint8_t*>(ws + at.fields[m]);
+        A.unit = reinterpret_cast<KbWord*>(ws + at.unit[m]);
+        A.beta = reinterpret_cast<uint4*>(ws + at.beta[m]);
+        A.alpha = reinterpret_cast<float*>(ws + at.alpha[m]);
+    };
+    const int64_t strips = (Q.P.rows / Q.P.R_u) * Q.P.n_chunks * ((Q.P.R_u + PT_STRIP - 1) / PT_STRIP);
+    for (int m = 1; m >= 0; --m) {                          // the sums of X with the gate's
+        matrix(m);
+        A.P = m == 1 ? Q.pair.up : Q.P;
+        const int64_t wgs = strips + (m == 0 ? tokens_in(A.n_kb * Q.T, PT_SUMS) : 0);
+        const int status = launch_pieces(wgs, 256, [&](int64_t first, dim3 g) { tiles_prepare_kernel<XT, S><<<g, dim3(256), 0, st>>>(A, strips, first); });
+        if (status != WINDQ_OK) return status;
+    }
+    A.unit_up = reinterpret_cast<KbWord*>(ws + at.unit[1]);
+    A.beta_up = reinterpret_cast<uint4*>(ws + at.beta[1]);
+    // tiles are no more than 2^31 / (64 x 128) and two sides' edges: one launch holds them
+    const int64_t tiles = (int64_t)A.row_blocks * ((Q.T + PT_TOKENS - 1) / PT_TOKENS);
+    project_tiles_kernel<XT, S, true><<<dim3((uint32_t)tiles), dim3(PT_THREADS), 0, st>>>(A);
+    return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
+}
+
+template <typename XT>
+int gated_all(ProjectArgs& Q, const windq_mat* X, char* ws, const GatedWs& at, hipStream_t st) {
+    const int64_t T = Q.T;
+    if constexpr (sizeof(XT) == 4) {
+        uint16_t* planes = reinterpret_cast<uint16_t*>(ws + at.planes);
+        const int status = launch_planes(static_cast<const float*>(X->data), X->ld, T, (int32_t)Q.P.cols, planes, st);
+        if (status != WINDQ_OK) return status;
+        Q.X = planes;
+        Q.ldx = Q.P.cols;
+        Q.plane = T * Q.P.cols;
+    } else {
+        if (few_fits(Q.P, T) && few_fits(Q.pair.up, T)) {
+            FewArgs F = {Q.P, Q.X, Q.ldx, T, static_cast<uint16_t*>(Q.Y), Q.ldy, nullptr, Q.A, 0, reinterpret_cast<uint4*>(ws + at.frag), reinterpret_cast<float*>(ws + at.few_xs), 0, 0, 0, Q.pair};
+            const int steps = Q.P.G % 128 == 0 ? 8 : Q.P.G / 16;
+            F.n_kb = (int32_t)(Q.P.cols / (16 * steps));
+            return steps == 8 ? launch_few<8, true>(F, nullptr, st) : (steps == 6 ? launch_few<6, true>(F, nullptr, st) : launch_few<4, true>(F, nullptr, st));
+        }
+    }
+    const bool mask = Q.P.mask != nullptr || Q.pair.up.mask != nullptr;
+    const int64_t general = (Q.P.rows + 15) / 16 * tokens_in(T, 64);
+    const int S = !mask && T > PROJECT_FEW && general > (sizeof(XT) == 2 ? 256 : 512) ? tile_steps(Q.P) : 0;
+    if (S == 8) return launch_gated_tiles<XT, 8>(Q, ws, at, st);
+    if (S == 6) return launch_gated_tiles<XT, 6>(Q, ws, at, st);
+    if (S == 4) return launch_gated_tiles<XT, 4>(Q, ws, at, st);
+    return mask ? launch_project_any<XT, true, true>(Q, st) : launch_project_any<XT, false, true>(Q, st);
+}
+
+// Two packed matrices of one shape, chunk width, units and weight type.
+int check_pair(const windq_packed* gate, const windq_packed* up, PackArgs* A, PackArgs* B) {
+    int status = check_packed(gate, A);
+    if (status == WINDQ_OK) status = check_packed(up, B);
+    if (status != WINDQ_OK) return status;
+    if (A->rows != B->rows || A->cols != B->cols || A->G != B->G || A->R_u != B->R_u) return WINDQ_ESHAPE;
+    return A->w_f32 != B->w_f32 ? WINDQ_EDTYPE : WINDQ_OK;
+}
+
+// ------------------------------------------------------------------------------------------------ the way back
+// dX is one product whose sum runs along the gate's rows and then the up's.  In bfloat16 calls both factors are half precision numbers: 11 bits of
+// significand, where bfloat16's 8 would be as coarse as dX's own rounding three times over (dX 1.7 times as far off as its rounding alone).  Their
+// range is what powers of two make of it: a token's dG and dU, and a chunk's weights in both matrices, are brought below 2^15, and what lies 2^28 below the
+// largest of them still has all of its digits.  The powers come off dX in fp32.
+//   The launch ahead: a workgroup a token (dG, dU and the token's power from a bound on them, |dH U| 1.13 and |dH G|: no activation is steeper than 1.13), and
+// workgroups of 512 rows by one chunk (the largest magnitude their groups can take).  Then the reconstruction, turned, then the product.
+constexpr int RANGE_ROWS = 512;
+
+struct SlopeArgs {
+    const void* dH;
+    const void* G;
+    const void* U;
+    int64_t ld_dh, ld_save, T, rows;
+    int32_t act;
+    void* dG;                  // the caller's, or null
+    void* dU;
+    int64_t ld_d;
+    void* to;                  // bfloat16 calls: [T][2 K] in half precision; fp32: [2][T][K]; or null: dX is not wanted
+    int64_t K;
+    float* by_token;
+    bool wide;                 // all rows of all tensors on 16 bytes
+    PackArgs P[2];
+    float* range;              // [chunks][2][strips]
+    int32_t strips;
+};
+
+template <typename XT>
+__device__ __forceinline__ void load_octet(const XT* __restrict__ p, int64_t left, bool wide, float (&v)[8]) {
+    if (wide && left >= 8) return load8(p, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        v[i] = 0.0f;
+        if (i < left) {
+            if constexpr (sizeof(XT) == 4) v[i] = p[i];
+            else v[i] = bf16_bits_to_f32(p[i]);
+        }
+    }
+}
+
+template <typename XT>
+__device__ __forceinline__ void store_octet(XT* __restrict__ p, int64_t left, bool wide, const float (&v)[8]) {
+    if (wide && left >= 8) {
+        if constexpr (sizeof(XT) == 4) {
+            reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+            reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        } else {
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = f32_to_bf16_bits(v[i]);
+            *reinterpret_cast<uint4*>(p) = pack8(w);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < left) store_y(p + i, v[i]);
+}
+
+// The power of two that brings magnitudes up to `most` below 2^15 (1 where there are none), itself within fp32's normal numbers.
+__device__ __forceinline__ float power_below(float most) {
+    const int e = (int)(__float_as_uint(most) >> 23);       // biased; most < 2^(e - 126)
+    const int by = most > 0.0f ? 127 + 14 - (e - 127) : 127;
+    return __uint_as_float((uint32_t)(by > 253 ? 253 : by) << 23);
+}
+__device__ __forceinline__ float finite_max(float m, float x) { return isfinite(x) && fabsf(x) > m ? fabsf(x) : m; }
+
+template <typename XT>
+__device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
+    __shared__ float most[4];
+    const XT* __restrict__ const dh = static_cast<const XT*>(Q.dH) + t * Q.ld_dh;
+    const XT* __restrict__ const g = static_cast<const XT*>(Q.G) + t * Q.ld_save;
+    const XT* __restrict__ const u = static_cast<const XT*>(Q.U) + t * Q.ld_save;
+    float by = 1.0f;
+    if (sizeof(XT) == 2 && Q.to != nullptr) {
+        float m = 0.0f;
+        for (int64_t r = threadIdx.x * 8; r < Q.rows; r += 2048) {
+            float a[8], b[8], c[8];
+            load_octet(dh + r, Q.rows - r, Q.wide, a);
+            load_octet(g + r, Q.rows - r, Q.wide, b);
+            load_octet(u + r, Q.rows - r, Q.wide, c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = finite_max(finite_max(m, 1.13f * a[i] * c[i]), a[i] * b[i]);
+        }
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+        if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = m;
+        __syncthreads();
+        by = power_below(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
+        if (threadIdx.x == 0) Q.by_token[t] = 1.0f / by;
+    }
+    for (int64_t r = threadIdx.x * 8; r < (Q.to != nullptr ? Q.K : Q.rows); r += 2048) {
+        float a[8] = {}, b[8] = {}, c[8] = {}, dg[8], du[8];
+        const int64_t left = Q.rows - r;
+        if (left > 0) {
+            load_octet(dh + r, left, Q.wide, a);
+            load_octet(g + r, left, Q.wide, b);
+            load_octet(u + r, left, Q.wide, c);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float slope;
+            const float y = activation<true>(Q.act, b[i], slope);
+            dg[i] = a[i] * c[i] * slope;
+            du[i] = a[i] * y;
+        }
+        if (Q.dG != nullptr && left > 0) {
+            store_octet(static_cast<XT*>(Q.dG) + t * Q.ld_d + r, left, Q.wide, dg);
+            store_octet(static_cast<XT*>(Q.dU) + t * Q.ld_d + r, left, Q.wide, du);
+        }
+        if (Q.to == nullptr) continue;
+        if constexpr (sizeof(XT) == 2) {
+            uint16_t* const to = static_cast<uint16_t*>(Q.to) + t * 2 * Q.K + r;
+            uint32_t w[2][8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                w[0][i] = half_bits<_Float16>(dg[i] * by);
+                w[1][i] = half_bits<_Float16>(du[i] * by);
+            }
+            *reinterpret_cast<uint4*>(to) = pack8(w[0]);
+            *reinterpret_cast<uint4*>(to + Q.K) = pack8(w[1]);
+        } else {
+            store_octet(static_cast<float*>(Q.to) + t * Q.K + r, 8, true, dg);
+            store_octet(static_cast<float*>(Q.to) + (Q.T + t) * Q.K + r, 8, true, du);
+        }
+    }
+}
+
+// The largest finite magnitude that a weight of RANGE_ROWS rows of a chunk can have.
+__device__ __forceinline__ void range_of(const SlopeArgs& Q, int64_t block) {
+    __shared__ float most[4];
+    const int m = (int)(block / ((int64_t)Q.strips * Q.P[0].n_chunks));
+    const PackArgs& P = Q.P[m];
+    const int64_t rest = block - (int64_t)m * Q.strips * P.n_chunks, j = rest / Q.strips, strip = rest - j * Q.strips;
+    float most_here = 0.0f;
+    for (int k = threadIdx.x; k < RANGE_ROWS; k += 256) {
+        const int64_t row = strip * RANGE_ROWS + k;
+        if (row >= P.rows) break;
+        const int64_t rb = row / P.R_u, u = rb * P.n_chunks + j, g = u * P.R_u + row - rb * P.R_u;
+        int64_t base;
+        const int a = pk_action(P, u, base);
+        if (a == 0) {
+            for (int32_t c = 0; c < P.G; c += 8) {
+                float w[8];
+                skip_row(P, row, j * P.G + c, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) most_here = finite_max(most_here, w[i]);
+            }
+        } else {
+            const float s = P.scale[g], o = a >= 5 ? 0.0f : P.offset[g];
+            const float L = a == 1 ? 255.0f : (a == 2 ? 15.0f : (a == 3 ? 7.0f : (a == 4 ? 3.0f : 1.0f)));
+            most_here = finite_max(finite_max(most_here, o), fmaf(s, L, o));
+        }
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) most_here = fmaxf(most_here, __shfl_xor(most_here, d, 64));
+    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = most_here;
+    __syncthreads();
+    if (threadIdx.x == 0) Q.range[(j * 2 + m) * Q.strips + strip] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+}
+
+template <typename XT>
+__global__ __launch_bounds__(256) void gated_slopes_kernel(const SlopeArgs Q, const int64_t first) {
+    const int64_t block = first + blockIdx.x;
+    if (block < Q.T) slopes<XT>(Q, block);
+    else range_of(Q, block - Q.T);
+}
+
+struct GatedTurnArgs {
+    PackArgs P[2];
+    int32_t K;
+    uint16_t* wt;              // [cols][2 K]
+    int64_t turns;             // workgroups of a matrix
+    const float* range;
+    int32_t strips;
+    float* by_octet;
+};
+
+__global__ __launch_bounds__(256) void gated_turn_kernel(const GatedTurnArgs Q, const int64_t first) {
+    const int64_t id = first + blockIdx.x;
+    const int m = id >= Q.turns ? 1 : 0;
+    const int64_t block = id - m * Q.turns;
+    const int32_t row_blocks = (Q.K + 255) / 256;
+    const int64_t cb = block / row_blocks, col = cb * 64 + (threadIdx.x >> 5) * 8;
+    const PackArgs& P = Q.P[m];
+    float most = 0.0f;
+    if (col < P.cols) {
+        const float* const range = Q.range + col / P.G * 2 * Q.strips;
+        for (int32_t k = threadIdx.x & 31; k < 2 * Q.strips; k += 32) most = fmaxf(most, range[k]);
+    }
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 32));
+    const float by = power_below(most);
+    if (id - cb * row_blocks == 0 && (threadIdx.x & 31) == 0 && col < P.cols) Q.by_octet[col >> 3] = 1.0f / by;
+    turn<_Float16>(P, Q.K, 2 * (int64_t)Q.K, by, Q.wt + (int64_t)m * Q.K, block);
+}
+
+struct GatedGradWs {
+    size_t to, wt, gm, by_token, by_octet, range, dxf, total;
+    int64_t K;
+};
+
+GatedGradWs gated_grad_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t G) {
+    GatedGradWs w;
+    const bool bf = dtype == WINDQ_BF16;
+    w.K = bf ? gemm_k(rows) : in_eights(rows);
+    size_t at = 0;
+    auto take = [&at](size_t bytes) {
+        const size_t here = at;
+        at += round_up(bytes, 256);
+        return here;
+    };
+    w.to = take((size_t)(2 * T * w.K) * (bf ? 2 : 4));
+    w.wt = take(bf && T > 0 ? (size_t)gemm_cols(cols) * (size_t)(2 * w.K) * 2 : 0);
+    w.gm = take(bf ? (size_t)gemm_parts(T, 2 * w.K, cols) * 4 : 0);
+    w.by_token = take(bf ? (size_t)T * 4 : 0);
+    w.by_octet = take(bf ? (size_t)(cols / 8 + 1) * 4 : 0);
+    w.range = take(bf ? (size_t)(cols / G + 1) * 2 * (size_t)tokens_in(rows, RANGE_ROWS) * 4 : 0);
+    w.dxf = take(bf ? 0 : DXF_BYTES);
+    w.total = at == 0 ? 256 : at;
+    return w;
+}
+
+size_t gated_grad_ws_bytes(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t G) { return gated_grad_ws(dtype, T, rows, cols, G).total; }
+
+template <typename XT>
+int gated_grad_all(SlopeArgs& S, void* dX, int64_t ld_dx, char* ws, const GatedGradWs& at, hipStream_t st) {
+    constexpr bool bf = sizeof(XT) == 2;
+    const PackArgs& P = S.P[0];
+    const int64_t T = S.T, cols = P.cols;
+    int64_t ahead = T;
+    if (dX != nullptr) {
+        S.to = ws + at.to;
+        S.K = at.K;
+        if (bf) {
+            S.by_token = reinterpret_cast<float*>(ws + at.by_token);
+            S.range = reinterpret_cast<float*>(ws + at.range);
+            S.strips = (int32_t)tokens_in(P.rows, RANGE_ROWS);
+            ahead += 2 * (int64_t)S.strips * P.n_chunks;
+        }
+    }
+    int status = launch_pieces(ahead, 256, [&](int64_t first, dim3 g) { gated_slopes_kernel<XT><<<g, dim3(256), 0, st>>>(S, first); });
+    if (status != WINDQ_OK || dX == nullptr) return status;
+    DxArgs Q = {};
+    Q.P = P;
+    Q.packed = true;
+    Q.T = T;
+    Q.dX = dX;
+    Q.ldx = ld_dx;
+    if constexpr (bf) {
+        const int32_t K2 = (int32_t)(2 * at.K);
+        const GatedTurnArgs R = {{S.P[0], S.P[1]}, (int32_t)at.K, reinterpret_cast<uint16_t*>(ws + at.wt), ((cols + 63) / 64) * ((at.K + 255) / 256), S.range, S.strips,
+                                 reinterpret_cast<float*>(ws + at.by_octet)};
+        status = launch_pieces(2 * R.turns, 256, [&](int64_t first, dim3 g) { gated_turn_kernel<<<g, dim3(256), 0, st>>>(R, first); });
+        if (status != WINDQ_OK) return status;
+        // tiles are no more than 2^31 / 128^2 and two sides' edges: one launch holds them
+        const int64_t tall = tokens_in(T, GM_N), by = tokens_in(cols, 256) * tall >= GM_TILES ? 256 : 128, tiles = tokens_in(cols, by) * tall;
+        GemmArgs M = {R.wt, static_cast<const uint16_t*>(S.to), K2, K2, T, cols, static_cast<uint16_t*>(dX), ld_dx, nullptr, nullptr, {}, (uint32_t)tokens_in(cols, by), nullptr,
+                      (int32_t)tiles, K2 / GM_K, S.by_token, R.by_octet};
+        if (by == 256) {
+            dx_gemm_kernel<4, true><<<dim3((uint32_t)tiles), dim3(GM_THREADS), 0, st>>>(M);
+            return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
+        }
+        const int32_t each = gemm_each(K2, tiles), splits = (int32_t)tokens_in(K2 / GM_K, each);
+        if (splits > 1) {
+            M.each = each;
+            M.part = Q.part = reinterpret_cast<float*>(ws + at.gm);
+            Q.splits = splits;
+        }
+        dx_gemm_kernel<2, true><<<dim3((uint32_t)(tiles * splits)), dim3(GM_THREADS), 0, st>>>(M);
+        if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
+        return splits == 1 ? WINDQ_OK : launch_dx_join(Q, st);
+    } else {
+        Q.dY = S.to;
+        Q.ldy = at.K;
+        Q.up = S.P[1];
+        Q.dY_up = static_cast<float*>(S.to) + T * at.K;
+        Q.part = reinterpret_cast<float*>(ws + at.dxf);
+        return launch_dx_f32(Q, st);
+    }
+}
+
+}  // namespace windq
+
+using namespace windq;
+
+extern "C" size_t windq_gated_workspace_bytes(int32_t grad, int32_t dtype, int64_t tokens, int64_t rows, int64_t cols, int32_t chunk_w) {
+    if ((dtype != WINDQ_F32 && dtype != WINDQ_BF16) || tokens < 0 || rows <= 0 || cols <= 0 || chunk_w <= 0) return 0;
+    if (!sizes_fit(tokens, rows, cols, 0, 0) || (grad != 0 && !grad_sizes_fit(tokens, rows, cols))) return 0;
+    return grad != 0 ? gated_grad_ws_bytes(dtype, tokens, rows, cols, chunk_w) : gated_ws(dtype, tokens, rows, cols, chunk_w).total;
+}
+
+extern "C" int windq_gated(const windq_packed* gate, const windq_packed* up, const windq_mat* X, int32_t act, void* H, int64_t ld_h, void* G, void* U,
+                           int64_t ld_save, void* ws, size_t ws_bytes, void* stream) {
+    ProjectArgs Q = {};
+    int status = check_pair(gate, up, &Q.P, &Q.pair.up);
+    if (status != WINDQ_OK) return status;
+    status = check_tokens(X, Q.P.cols, true);
+    if (status != WINDQ_OK) return status;
+    if (act < WINDQ_SILU || act > WINDQ_GELU_TANH || (G == nullptr) != (U == nullptr)) return WINDQ_EINVAL;
+    const size_t eb = X->dtype == WINDQ_F32 ? 4 : 2;
+    if (!sizes_fit(X->rows, Q.P.rows, Q.P.cols, 0, 0)) return WINDQ_ESHAPE;
+    if (ld_h < Q.P.rows || ld_h > (int64_t)1 << 31) return WINDQ_ESHAPE;
+    if (G != nullptr && (ld_save < Q.P.rows || ld_save > (int64_t)1 << 31)) return WINDQ_ESHAPE;
+    if (X->rows == 0) return WINDQ_OK;
+    if (X->rows * Q.P.rows > (int64_t)0x7fffffff) return WINDQ_ESHAPE;
+    if (H == nullptr || !aligned(H, eb) || !aligned(G, eb) || !aligned(U, eb)) return WINDQ_EINVAL;
+    const GatedWs at = gated_ws(X->dtype, X->rows, Q.P.rows, Q.P.cols, Q.P.G);
+    if (ws == nullptr || ws_bytes < at.total) return WINDQ_EWORKSPACE;
+    if (!aligned(ws, 256)) return WINDQ_EINVAL;
+    Q.X = static_cast<const uint16_t*>(X->data);
+    Q.ldx = X->ld;
+    Q.raw = X->data;
+    Q.ld_raw = X->ld;
+    Q.T = X->rows;
+    Q.Y = H;
+    Q.ldy = ld_h;
+    Q.pair.act = act;
+    Q.pair.G = G;
+    Q.pair.U = U;
+    Q.pair.ld_save = ld_save;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    char* w = static_cast<char*>(ws);
+    return X->dtype == WINDQ_F32 ? gated_all<float>(Q, X, w, at, st) : gated_all<uint16_t>(Q, X, w, at, st);
+}
+
+extern "C" int windq_gated_grad(const windq_packed* gate, const windq_packed* up, const windq_mat* dH, const void* G, const void* U, int64_t ld_save, int32_t act,
+                                void* dX, int64_t ld_dx, void* dG, void* dU, int64_t ld_d, void* ws, size_t ws_bytes, void* stream) {
+    SlopeArgs S = {};
+    int status = check_pair(gate, up, &S.P[0], &S.P[1]);
+    if (status != WINDQ_OK) return status;
+    const int64_t rows = S.P[0].rows, cols = S.P[0].cols;
+    status = check_tokens(dH, rows, false);
+    if (status != WINDQ_OK) return status;
+    const int64_t T = dH->rows;
+    if (act < WINDQ_SILU || act > WINDQ_GELU_TANH || (dG == nullptr) != (dU == nullptr) || (dX == nullptr && dG == nullptr && T > 0)) return WINDQ_EINVAL;
+    if (!sizes_fit(T, rows, cols, 0, 0) || !grad_sizes_fit(T, rows, cols) || rows > ((int64_t)1 << 30) - 512) return WINDQ_ESHAPE;
+    if (ld_save < rows || ld_save > (int64_t)1 << 31) return WINDQ_ESHAPE;
+    if (dX != nullptr && (ld_dx < cols || ld_dx > (int64_t)1 << 31)) return WINDQ_ESHAPE;
+    if (dG != nullptr && (ld_d < rows || ld_d > (int64_t)1 << 31)) return WINDQ_ESHAPE;
+    if (T == 0) return WINDQ_OK;
+    const size_t eb = dH->dtype == WINDQ_F32 ? 4 : 2;
+    if (G == nullptr || U == nullptr || !aligned(G, eb) || !aligned(U, eb) || !aligned(dX, eb) || !aligned(dG, eb) || !aligned(dU, eb)) return WINDQ_EINVAL;
+    const GatedGradWs at = gated_grad_ws(dH->dtype, T, rows, cols, S.P[0].G);
+    if (dX != nullptr) {
+        if (ws == nullptr || ws_bytes < at.total) return WINDQ_EWORKSPACE;
+        if (!aligned(ws, 256)) return WINDQ_EINVAL;
+    }
+    S.dH = dH->data;
+    S.G = G;
+    S.U = U;
+    S.ld_dh = dH->ld;
+    S.ld_save = ld_save;
+    S.T = T;
+    S.rows = rows;
+    S.act = act;
+    S.dG = dG;
+    S.dU = dU;
+    S.ld_d = ld_d;
+    S.wide = dH->ld % 8 == 0 && ld_save % 8 == 0 && (dG == nullptr || ld_d % 8 == 0) && aligned(dH->data, 16) && aligned(G, 16) && aligned(U, 16) && aligned(dG, 16) && aligned(dU, 16);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    char* w = static_cast<char*>(ws);
+    return dH->dtype == WINDQ_F32 ? gated_grad_all<float>(S, dX, ld_dx, w, at, st) : gated_grad_all<uint16_t>(S, dX, ld_dx, w, at, st);
+}

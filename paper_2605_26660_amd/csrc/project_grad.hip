@@ -2,7 +2,7 @@
 //   dh_t = alpha_k B_k^T dY_t     dX[t] = w_hat^T dY_t + A_k^T dh_t     dA[k] = sum_t dh_t x_t^T     dB[k] = alpha_k sum_t dY_t h_t^T
 #include <math.h>
 
-#include "windq_gemm.hpp"
+#include "windq_dx.hpp"
 
 namespace windq {
 
@@ -229,20 +229,6 @@ __global__ __launch_bounds__(OUTER_THREADS) void outer_tiles_kernel(const OuterA
 }
 
 // ------------------------------------------------------------------------------------------------ dX
-struct DxArgs {
-    PackArgs P;                // rows, cols alone where packed is false
-    bool packed;
-    const void* dY;            // rows on 16 bytes, readable up to a multiple of 8
-    int64_t ldy;
-    int64_t T;
-    void* dX;
-    int64_t ldx;
-    const float* dh;           // [T][max_rank] or null
-    AdapterArgs A;
-    float* part;               // sums of parts of the rows; fp32: [splits][tiles][4][256][4], bfloat16: [splits][T][cols]
-    int32_t splits;
-};
-
 // Eight columns of A_k^T dh_t, added to v.
 __device__ __forceinline__ void add_adapter8(const AdapterArgs& A, const float* __restrict__ dh, int64_t t, int64_t col, int64_t cols, float (&v)[8]) {
     const int32_t k = A.of[t];
@@ -260,32 +246,6 @@ __device__ __forceinline__ void add_adapter8(const AdapterArgs& A, const float* 
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] += sum[j];
-}
-
-__device__ __forceinline__ void skip_row(const PackArgs& P, int64_t row, int64_t col, float (&w)[8]) {
-    if (P.w_f32 != 0) load8(static_cast<const float*>(P.W) + row * P.ld + col, w);
-    else load8(static_cast<const uint16_t*>(P.W) + row * P.ld + col, w);
-}
-
-// An octet of one row as fp32 weights (rounded nowhere but by the multiply-add).
-__device__ __forceinline__ void weight_octet(const PackArgs& P, int64_t row, int64_t col, const uint16_t* __restrict__ trits_of, float (&w)[8]) {
-    const int64_t rb = row / P.R_u, lrow = row - rb * P.R_u;
-    const int32_t j = (int32_t)(col / P.G), o = (int32_t)(col - (int64_t)j * P.G) >> 3;
-    const int64_t u = rb * P.n_chunks + j;
-    int64_t base;
-    const int a = pk_action(P, u, base);
-    if (a == 0) return skip_row(P, row, col, w);
-    const int64_t g = u * P.R_u + lrow;
-    const float s = P.scale[g], of = a >= 5 ? 0.0f : P.offset[g];
-    const uint4 f = octet_fields(a, P.codes + base + lrow * pk_bytes_per_group(a, P.G), o, trits_of);
-    const float f0 = pk_f0(a);
-    const uint32_t m = P.mask != nullptr ? P.mask[row * P.mask_ld + (col >> 3)] : 0u;
-    const uint32_t v[4] = {f.x, f.y, f.z, f.w};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float q = ((i & 1) != 0 ? __uint_as_float(v[i >> 1] & 0xffff0000u) : bf16_bits_to_f32(v[i >> 1] & 0xffffu)) - f0;
-        w[i] = ((m >> i) & 1u) != 0u ? 0.0f : fmaf(q, s, of);
-    }
 }
 
 // bfloat16: the sums of the product's parts (none: the packed matrix is not wanted) and the adapters', a thread per token and octet of columns.
@@ -314,87 +274,6 @@ __global__ __launch_bounds__(256) void dx_join_kernel(const DxArgs Q, const int6
     }
 }
 
-// w_hat rounded to bfloat16 and turned: wt [cols][K], zeros from the last row to K.  A thread has eight rows by eight columns.
-__device__ __forceinline__ void turn(const PackArgs& P, int32_t K, uint16_t* __restrict__ wt, int64_t block) {
-    __shared__ uint16_t trits_of[256];
-    trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
-    __syncthreads();
-    const int32_t row_blocks = (K + 255) / 256;
-    const int64_t cb = block / row_blocks;
-    const int64_t r0 = (block - cb * row_blocks) * 256 + (threadIdx.x & 31) * 8, col = cb * 64 + (threadIdx.x >> 5) * 8;
-    if (col >= P.cols || r0 >= K) return;
-    uint32_t v[8][4];
-    const uint32_t R_u = (uint32_t)P.R_u, rb = (uint32_t)r0 / R_u, lrow = (uint32_t)r0 - rb * R_u;
-    if (r0 + 8 <= P.rows && lrow + 8 <= R_u) {              // one unit's rows
-        const uint32_t j = (uint32_t)col / (uint32_t)P.G;
-        const int o = ((int)col - (int)j * P.G) >> 3;
-        const int64_t u = (int64_t)rb * P.n_chunks + j;
-        int64_t base;
-        const int a = pk_action(P, u, base);
-        if (a == 0) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float w0[8], w1[8];
-                skip_row(P, r0 + 2 * i, col, w0);
-                skip_row(P, r0 + 2 * i + 1, col, w1);
-#pragma unroll
-                for (int m = 0; m < 8; ++m) v[m][i] = f32_to_bf16_bits(w0[m]) | f32_to_bf16_bits(w1[m]) << 16;
-            }
-        } else {
-            const int32_t nb = (int32_t)pk_bytes_per_group(a, P.G);
-            const uint8_t* const first = P.codes + base + (int64_t)lrow * nb;
-            float sc[8], of[8];
-            __builtin_memcpy(sc, P.scale + u * P.R_u + lrow, 32);
-            __builtin_memcpy(of, P.offset + u * P.R_u + lrow, 32);
-            uint4 f[8];
-            auto rows = [&](auto octet) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] = octet(first + i * nb);
-            };
-            switch (a) {
-                case 1: rows([&](const uint8_t* p) { uint2 q; __builtin_memcpy(&q, p + o * 8, 8); return fields8(q.x, q.y); }); break;
-                case 2: rows([&](const uint8_t* p) { uint32_t q; __builtin_memcpy(&q, p + o * 4, 4); return fields4(q); }); break;
-                case 3: rows([&](const uint8_t* p) { return octet_fields(3, p, o, trits_of); }); break;
-                case 4: rows([&](const uint8_t* p) { uint16_t q; __builtin_memcpy(&q, p + o * 2, 2); return fields2(q); }); break;
-                case 5: rows([&](const uint8_t* p) { return fields2(octet_trits(p, o, trits_of) & 0xffffu); }); break;
-                default: rows([&](const uint8_t* p) { return fields1(p[o]); }); break;
-            }
-            const float f0 = pk_f0(a);
-            uint32_t m8[8] = {};
-            if (P.mask != nullptr) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) m8[i] = P.mask[(r0 + i) * P.mask_ld + (col >> 3)];
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int m = 0; m < 8; ++m) {
-                    uint32_t w[2];
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const uint4& g = f[2 * i + k];
-                        const uint32_t pair = (m >> 1) == 0 ? g.x : ((m >> 1) == 1 ? g.y : ((m >> 1) == 2 ? g.z : g.w));
-                        const float q = ((m & 1) != 0 ? __uint_as_float(pair & 0xffff0000u) : __uint_as_float(pair << 16)) - f0;
-                        const float x = fmaf(q, sc[2 * i + k], a >= 5 ? 0.0f : of[2 * i + k]);
-                        w[k] = f32_to_bf16_bits(((m8[2 * i + k] >> m) & 1u) != 0u ? 0.0f : x);
-                    }
-                    v[m][i] = w[0] | w[1] << 16;
-                }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float w0[8] = {}, w1[8] = {};
-            if (r0 + 2 * i < P.rows) weight_octet(P, r0 + 2 * i, col, trits_of, w0);
-            if (r0 + 2 * i + 1 < P.rows) weight_octet(P, r0 + 2 * i + 1, col, trits_of, w1);
-#pragma unroll
-            for (int m = 0; m < 8; ++m) v[m][i] = f32_to_bf16_bits(w0[m]) | f32_to_bf16_bits(w1[m]) << 16;
-        }
-    }
-#pragma unroll
-    for (int m = 0; m < 8; ++m) *reinterpret_cast<uint4*>(wt + (col + m) * K + r0) = make_uint4(v[m][0], v[m][1], v[m][2], v[m][3]);
-}
-
 // What the later kernels read, in one launch: the reconstruction turned, B and A transposed, tokens by adapter.  Workgroups in that order.
 // 11008 x 4096: 29 to 33 us, 92 MB written (3.2 to 2.8 TB/s).
 template <typename XT>
@@ -415,7 +294,7 @@ struct PrepareArgs {
 template <typename XT>
 __global__ __launch_bounds__(256) void grad_prepare_kernel(const PrepareArgs<XT> Q, const int64_t first) {
     int64_t block = first + blockIdx.x;
-    if (block < Q.turns) return turn(Q.P, Q.K, Q.wt, block);
+    if (block < Q.turns) return turn<uint16_t>(Q.P, Q.K, Q.K, 1.0f, Q.wt, block);
     block -= Q.turns;
     if (block < Q.bs) return transpose(Q.b, Q.P.rows, Q.A.max_rank, Q.ld, Q.bt, block);
     block -= Q.bs;
@@ -427,7 +306,7 @@ __global__ __launch_bounds__(256) void grad_prepare_kernel(const PrepareArgs<XT>
 // through LDS 32 at a time, the next ones on their way meanwhile: small layers leave few workgroups, and a wavefront's time is latency.
 // Where tiles are fewer than the CUs the rows are split further, over workgroups, whose sums another kernel joins in order: 1000 x 1056 at 77
 // tokens (34 tiles of 8 steps) takes 60 us without the split and 17 + 5 with it (four parts of 2 steps).
-constexpr int DXF_THREADS = 1024, DXF_PARTS = DXF_THREADS / 256, DXF_TILES = 256;
+constexpr int DXF_THREADS = 1024, DXF_PARTS = DXF_THREADS / 256;
 inline int64_t dxf_tiles(int64_t T, int64_t cols) { return tokens_in(cols, 64) * tokens_in(T, 64); }
 inline int32_t dxf_splits(int64_t tiles, int64_t rows) {
     const int64_t steps = tokens_in(rows, 32 * DXF_PARTS), most = DXF_TILES / tiles < 1 ? 1 : DXF_TILES / tiles;
@@ -477,6 +356,8 @@ __global__ __launch_bounds__(256) void dx_f32_join_kernel(const DxArgs Q, const 
     dx_f32_store(Q, tb * 64 + n * 16 + (lane & 15), (tile - tb * col_blocks) * 64 + wave * 16 + 4 * (lane >> 4), v);
 }
 
+// Of a pair (windq_gated_grad) the up's rows follow the gate's, both rounded up to a step.
+template <bool PAIR>
 __global__ __launch_bounds__(DXF_THREADS) void dx_f32_kernel(const DxArgs Q, const int64_t first) {
     __shared__ float wts[DXF_PARTS][32][68], yts[DXF_PARTS][32][68];
     __shared__ uint16_t trits_of[256];
@@ -493,18 +374,20 @@ __global__ __launch_bounds__(DXF_THREADS) void dx_f32_kernel(const DxArgs Q, con
     f32x4 acc[4] = {};
     if (Q.packed) {
         // steps of a quarter, the same for all of them: barriers are shared
-        const int64_t blocks = (P.rows + 31) / 32, each = (blocks + DXF_PARTS * Q.splits - 1) / (DXF_PARTS * Q.splits), from = (split * DXF_PARTS + part) * each;
+        const int64_t own = (P.rows + 31) / 32, blocks = PAIR ? 2 * own : own, each = (blocks + DXF_PARTS * Q.splits - 1) / (DXF_PARTS * Q.splits), from = (split * DXF_PARTS + part) * each;
         const int r = tid >> 3, o = tid & 7, yr = tid & 31;
         float w[8], y[8];
         auto fetch = [&](int64_t block) {
-            const int64_t r0 = block * 32;
+            const bool up = PAIR && block >= own;
+            const int64_t r0 = (up ? (block < blocks ? block - own : own) : block) * 32;       // past the last step: past the last row
+            const float* __restrict__ const dy = up ? static_cast<const float*>(Q.dY_up) : dY;
 #pragma unroll
             for (int j = 0; j < 8; ++j) w[j] = 0.0f;
-            if (r0 + r < P.rows && c0 + o * 8 < P.cols) weight_octet(P, r0 + r, c0 + o * 8, trits_of, w);
+            if (r0 + r < P.rows && c0 + o * 8 < P.cols) weight_octet(up ? Q.up : P, r0 + r, c0 + o * 8, trits_of, w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int64_t t = t0 + (tid >> 5) + 8 * j;
-                y[j] = r0 + yr < P.rows && t < Q.T ? dY[t * Q.ldy + r0 + yr] : 0.0f;
+                y[j] = r0 + yr < P.rows && t < Q.T ? dy[t * Q.ldy + r0 + yr] : 0.0f;
             }
         };
         fetch(from);
@@ -592,7 +475,7 @@ GradWs grad_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t n, 
     w.planes_dh = take(bf && n > 0 ? (size_t)slots * GROUP * (size_t)max_rank * 6 : 0);
     w.wt = take(bf && T > 0 ? (size_t)gemm_cols(cols) * (size_t)gemm_k(rows) * 2 : 0);
     w.gm = take(bf ? (size_t)gemm_parts(T, gemm_k(rows), cols) * 4 : 0);
-    w.dxf = take(bf ? 0 : (size_t)DXF_TILES * 64 * 64 * 4);       // tiles x splits are no more
+    w.dxf = take(bf ? 0 : DXF_BYTES);
     w.total = at == 0 ? 256 : at;
     return w;
 }
@@ -607,6 +490,21 @@ size_t grad_ws_bytes(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32
         const int launched_ = launch_pieces(wgs, threads, [&](int64_t first_, dim3 g_) { kernel<<<g_, dim3(threads), 0, st>>>(__VA_ARGS__, first_); }); \
         if (launched_ != WINDQ_OK) return launched_;                                                                                             \
     } while (0)
+
+int launch_dx_join(const DxArgs& Q, hipStream_t st) {
+    WINDQ_LAUNCH(tokens_in(Q.T * (Q.P.cols / 8), 256), 256, dx_join_kernel, Q);
+    return WINDQ_OK;
+}
+
+int launch_dx_f32(DxArgs Q, hipStream_t st) {
+    const bool pair = Q.dY_up != nullptr;
+    const int64_t tiles = dxf_tiles(Q.T, Q.P.cols);
+    Q.splits = Q.packed ? dxf_splits(tiles, pair ? 2 * tokens_in(Q.P.rows, 32) * 32 : Q.P.rows) : 1;
+    if (pair) WINDQ_LAUNCH(tiles * Q.splits, DXF_THREADS, dx_f32_kernel<true>, Q);
+    else WINDQ_LAUNCH(tiles * Q.splits, DXF_THREADS, dx_f32_kernel<false>, Q);
+    if (Q.splits > 1) WINDQ_LAUNCH(tiles * 4, 256, dx_f32_join_kernel, Q, tiles);
+    return WINDQ_OK;
+}
 
 template <typename XT>
 int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h, float* dA, float* dB, char* ws, const GradWs& at, hipStream_t st) {
@@ -737,13 +635,10 @@ int grad_all(DxArgs& Q, const windq_mat* dY, const windq_mat* X, const float* h,
             if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
             if (splits == 1) return WINDQ_OK;
         }
-        WINDQ_LAUNCH(tokens_in(T * (cols / 8), 256), 256, dx_join_kernel, Q);
+        return launch_dx_join(Q, st);
     } else {
-        const int64_t tiles = dxf_tiles(T, cols);
-        Q.splits = Q.packed ? dxf_splits(tiles, rows) : 1;
         Q.part = reinterpret_cast<float*>(ws + at.dxf);
-        WINDQ_LAUNCH(tiles * Q.splits, DXF_THREADS, dx_f32_kernel, Q);
-        if (Q.splits > 1) WINDQ_LAUNCH(tiles * 4, 256, dx_f32_join_kernel, Q, tiles);
+        return launch_dx_f32(Q, st);
     }
     return WINDQ_OK;
 }

@@ -1,0 +1,150 @@
+// dX of packed products on their way back: what windq_project_grad and windq_gated_grad share.
+#pragma once
+
+#include "windq_gemm.hpp"
+
+namespace windq {
+
+constexpr int DXF_TILES = 256;
+constexpr size_t DXF_BYTES = (size_t)DXF_TILES * 64 * 64 * 4;      // of fp32's parts: tiles x splits are no more
+
+struct DxArgs {
+    PackArgs P;                // rows, cols alone where packed is false
+    bool packed;
+    const void* dY;            // rows on 16 bytes, readable up to a multiple of 8
+    int64_t ldy;
+    int64_t T;
+    void* dX;
+    int64_t ldx;
+    const float* dh;           // [T][max_rank] or null
+    AdapterArgs A;
+    float* part;               // sums of parts of the rows; fp32: [splits][tiles][4][256][4], bfloat16: [splits][T][cols]
+    int32_t splits;
+    PackArgs up;               // of a pair: the second matrix and its side of the sum
+    const void* dY_up;         // or null
+};
+
+int launch_dx_join(const DxArgs& Q, hipStream_t st);           // bfloat16: the parts added up, and the adapters'
+int launch_dx_f32(DxArgs Q, hipStream_t st);
+
+#ifdef __HIPCC__
+
+__device__ __forceinline__ void skip_row(const PackArgs& P, int64_t row, int64_t col, float (&w)[8]) {
+    if (P.w_f32 != 0) load8(static_cast<const float*>(P.W) + row * P.ld + col, w);
+    else load8(static_cast<const uint16_t*>(P.W) + row * P.ld + col, w);
+}
+
+// An octet of one row as fp32 weights (rounded nowhere but by the multiply-add).
+__device__ __forceinline__ void weight_octet(const PackArgs& P, int64_t row, int64_t col, const uint16_t* __restrict__ trits_of, float (&w)[8]) {
+    const int64_t rb = row / P.R_u, lrow = row - rb * P.R_u;
+    const int32_t j = (int32_t)(col / P.G), o = (int32_t)(col - (int64_t)j * P.G) >> 3;
+    const int64_t u = rb * P.n_chunks + j;
+    int64_t base;
+    const int a = pk_action(P, u, base);
+    if (a == 0) return skip_row(P, row, col, w);
+    const int64_t g = u * P.R_u + lrow;
+    const float s = P.scale[g], of = a >= 5 ? 0.0f : P.offset[g];
+    const uint4 f = octet_fields(a, P.codes + base + lrow * pk_bytes_per_group(a, P.G), o, trits_of);
+    const float f0 = pk_f0(a);
+    const uint32_t m = P.mask != nullptr ? P.mask[row * P.mask_ld + (col >> 3)] : 0u;
+    const uint32_t v[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float q = ((i & 1) != 0 ? __uint_as_float(v[i >> 1] & 0xffff0000u) : bf16_bits_to_f32(v[i >> 1] & 0xffffu)) - f0;
+        w[i] = ((m >> i) & 1u) != 0u ? 0.0f : fmaf(q, s, of);
+    }
+}
+
+// w_hat rounded to bfloat16 and turned: wt [cols][ld], zeros from the last row to K.  A thread has eight rows by eight columns.  In half precision (_Float16)
+// weights are multiplied by a power of two first, the same for an octet of columns.
+template <typename HT>
+__device__ __forceinline__ uint32_t half_bits(float x) {
+    if constexpr (__is_same(HT, _Float16)) return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x);
+    else return f32_to_bf16_bits(x);
+}
+
+template <typename HT>
+__device__ __forceinline__ void turn(const PackArgs& P, int32_t K, int64_t ld, float by, uint16_t* __restrict__ wt, int64_t block) {
+    __shared__ uint16_t trits_of[256];
+    trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
+    __syncthreads();
+    const int32_t row_blocks = (K + 255) / 256;
+    const int64_t cb = block / row_blocks;
+    const int64_t r0 = (block - cb * row_blocks) * 256 + (threadIdx.x & 31) * 8, col = cb * 64 + (threadIdx.x >> 5) * 8;
+    if (col >= P.cols || r0 >= K) return;
+    auto bits_of = [&](float x) { return half_bits<HT>(__is_same(HT, _Float16) ? x * by : x); };
+    uint32_t v[8][4];
+    const uint32_t R_u = (uint32_t)P.R_u, rb = (uint32_t)r0 / R_u, lrow = (uint32_t)r0 - rb * R_u;
+    if (r0 + 8 <= P.rows && lrow + 8 <= R_u) {              // one unit's rows
+        const uint32_t j = (uint32_t)col / (uint32_t)P.G;
+        const int o = ((int)col - (int)j * P.G) >> 3;
+        const int64_t u = (int64_t)rb * P.n_chunks + j;
+        int64_t base;
+        const int a = pk_action(P, u, base);
+        if (a == 0) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float w0[8], w1[8];
+                skip_row(P, r0 + 2 * i, col, w0);
+                skip_row(P, r0 + 2 * i + 1, col, w1);
+#pragma unroll
+                for (int m = 0; m < 8; ++m) v[m][i] = bits_of(w0[m]) | bits_of(w1[m]) << 16;
+            }
+        } else {
+            const int32_t nb = (int32_t)pk_bytes_per_group(a, P.G);
+            const uint8_t* const first = P.codes + base + (int64_t)lrow * nb;
+            float sc[8], of[8];
+            __builtin_memcpy(sc, P.scale + u * P.R_u + lrow, 32);
+            __builtin_memcpy(of, P.offset + u * P.R_u + lrow, 32);
+            uint4 f[8];
+            auto rows = [&](auto octet) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) f[i] = octet(first + i * nb);
+            };
+            switch (a) {
+                case 1: rows([&](const uint8_t* p) { uint2 q; __builtin_memcpy(&q, p + o * 8, 8); return fields8(q.x, q.y); }); break;
+                case 2: rows([&](const uint8_t* p) { uint32_t q; __builtin_memcpy(&q, p + o * 4, 4); return fields4(q); }); break;
+                case 3: rows([&](const uint8_t* p) { return octet_fields(3, p, o, trits_of); }); break;
+                case 4: rows([&](const uint8_t* p) { uint16_t q; __builtin_memcpy(&q, p + o * 2, 2); return fields2(q); }); break;
+                case 5: rows([&](const uint8_t* p) { return fields2(octet_trits(p, o, trits_of) & 0xffffu); }); break;
+                default: rows([&](const uint8_t* p) { return fields1(p[o]); }); break;
+            }
+            const float f0 = pk_f0(a);
+            uint32_t m8[8] = {};
+            if (P.mask != nullptr) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) m8[i] = P.mask[(r0 + i) * P.mask_ld + (col >> 3)];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int m = 0; m < 8; ++m) {
+                    uint32_t w[2];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const uint4& g = f[2 * i + k];
+                        const uint32_t pair = (m >> 1) == 0 ? g.x : ((m >> 1) == 1 ? g.y : ((m >> 1) == 2 ? g.z : g.w));
+                        const float q = ((m & 1) != 0 ? __uint_as_float(pair & 0xffff0000u) : __uint_as_float(pair << 16)) - f0;
+                        const float x = fmaf(q, sc[2 * i + k], a >= 5 ? 0.0f : of[2 * i + k]);
+                        w[k] = bits_of(((m8[2 * i + k] >> m) & 1u) != 0u ? 0.0f : x);
+                    }
+                    v[m][i] = w[0] | w[1] << 16;
+                }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float w0[8] = {}, w1[8] = {};
+            if (r0 + 2 * i < P.rows) weight_octet(P, r0 + 2 * i, col, trits_of, w0);
+            if (r0 + 2 * i + 1 < P.rows) weight_octet(P, r0 + 2 * i + 1, col, trits_of, w1);
+#pragma unroll
+            for (int m = 0; m < 8; ++m) v[m][i] = bits_of(w0[m]) | bits_of(w1[m]) << 16;
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < 8; ++m) *reinterpret_cast<uint4*>(wt + (col + m) * ld + r0) = make_uint4(v[m][0], v[m][1], v[m][2], v[m][3]);
+}
+
+#endif  // __HIPCC__
+
+}  // namespace windq

@@ -33,6 +33,8 @@ struct GemmArgs {
     uint32_t col_blocks;
     float* part;               // [splits][T][cols] sums over a part of the rows, or null: one workgroup has them all
     int32_t tiles, each;       // workgroups of a split, its steps of GM_K
+    const float* by_token;     // halves: what a token's results are multiplied by, and an octet of columns'
+    const float* by_octet;
 };
 
 inline int64_t gemm_k(int64_t rows) { return (rows + GM_K - 1) / GM_K * GM_K; }
@@ -52,7 +54,9 @@ inline int64_t gemm_cols(int64_t cols) { return (cols + GM_MOST - 1) / GM_MOST *
 
 #ifdef __HIPCC__
 
-template <int MF>                                          // fragments of a wavefront along the columns
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+template <int MF, bool HALF = false>                       // fragments of a wavefront along the columns; factors in half precision
 __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
     constexpr int GM_M = MF * 64, WM = MF * 32, LOADS = (GM_M + GM_N) / 32;
     __shared__ uint4 tile[GM_BUFFERS][(GM_M + GM_N) * 8];
@@ -118,7 +122,10 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
             for (int s = 0; s < 4; ++s) {
 #pragma unroll
                 for (int i = 0; i < MM; ++i) {
-                    acc[i >> 1][i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s & 1][i >> 1], b[s & 1][i & 1], acc[i >> 1][i & 1], 0, 0, 0);
+                    if constexpr (HALF)
+                        acc[i >> 1][i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a[s & 1][i >> 1]), __builtin_bit_cast(f16x8, b[s & 1][i & 1]), acc[i >> 1][i & 1], 0, 0, 0);
+                    else
+                        acc[i >> 1][i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[s & 1][i >> 1], b[s & 1][i & 1], acc[i >> 1][i & 1], 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
                     if (s == 3 && i == 0) {
                         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LOADS) : "memory");       // the next buffer's loads are done, this one's reads too
@@ -140,6 +147,22 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
 
+    if constexpr (HALF) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int64_t t = t0 + wn * 64 + n * 32 + sub;
+            const float token = Q.by_token[t < Q.T ? t : Q.T - 1];
+#pragma unroll
+            for (int f = 0; f < MF; ++f)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int64_t c = c0 + wm * WM + f * 32 + g * 8;
+                    const float octet = Q.by_octet[(c < Q.cols ? c : 0) >> 3];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[f][n][g * 4 + i] = acc[f][n][g * 4 + i] * token * octet;
+                }
+        }
+    }
     if (Q.part != nullptr) {
         float* const to = Q.part + (int64_t)split * Q.T * Q.cols;
 #pragma unroll

@@ -31,6 +31,7 @@ struct FewArgs {
     int64_t xs_ld;             // tokens in 64s
     int32_t fragments;         // of 32 tokens
     uint32_t row_blocks;
+    PairArgs pair;
 };
 
 // Up to FEW_DIRECT tokens X is read as it lies, a launch less: at 8 tokens 4096 x 4096 takes 13.7 us and 18.5 laid out, 11008 x 4096 25.7 and 31.4 (at 16
@@ -106,7 +107,8 @@ __global__ __launch_bounds__(256) void few_prepare_kernel(const FewArgs Q, const
     if (hh == 0) Q.xs[kb * Q.xs_ld + t] = sum;
 }
 
-template <int S, int NTF, int WAVES, bool LAID>
+// Of a pair (windq_gated) half of the wavefronts has the gate's k-blocks, the others the up's.
+template <int S, int NTF, int WAVES, bool LAID, bool PAIR = false>
 __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q) {
     constexpr int CODES = 32 * 128 + 32;                   // bytes: 32 rows of a k-block's fields (or of a chunk's trits), and what a last octet reads past them
     constexpr int RED_BYTES = WAVES * NTF * 16 * 64 * 4;
@@ -116,8 +118,10 @@ __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q
     __shared__ uint16_t trits_of[256];
     for (int i = threadIdx.x; i < 256; i += WAVES * 64) trits_of[i] = (uint16_t)trit_fields(i);
     __syncthreads();
-    const PackArgs& P = Q.P;
+    constexpr int EACH = PAIR ? WAVES / 2 : WAVES;          // wavefronts of a matrix
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, sub = lane & 31, hh = lane >> 5;
+    const int matrix = PAIR ? wave / EACH : 0, turn = wave - matrix * EACH;
+    const PackArgs& P = PAIR && matrix == 1 ? Q.pair.up : Q.P;
     const uint32_t tb = blockIdx.x / Q.row_blocks;
     const int64_t row0 = (int64_t)(blockIdx.x - tb * Q.row_blocks) * PF_ROWS, t0 = (int64_t)tb * (NTF * 32);
     const int64_t rb = row0 / P.R_u, lrow0 = row0 - rb * P.R_u;
@@ -140,8 +144,8 @@ __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q
     // a k-block's treatment, known a k-block ahead
     int64_t base = 0;
     int a = 0;
-    if (wave < Q.n_kb) a = __builtin_amdgcn_readfirstlane(pk_action(P, rb * P.n_chunks + wave / per_chunk, base));
-    for (int32_t kb = wave; kb < Q.n_kb; kb += WAVES) {
+    if (turn < Q.n_kb) a = __builtin_amdgcn_readfirstlane(pk_action(P, rb * P.n_chunks + turn / per_chunk, base));
+    for (int32_t kb = turn; kb < Q.n_kb; kb += EACH) {
         const int32_t j = kb / per_chunk, c = kb - j * per_chunk;
         const int64_t u = rb * P.n_chunks + j;
         const int64_t bpg = pk_bytes_per_group(a, P.G);
@@ -175,8 +179,8 @@ __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q
             for (int s = 0; s < S; ++s) x[s][n] = from[LAID ? s * 64 : s];
             if (LAID) xsum[n] = Q.xs[kb * Q.xs_ld + t0 + n * 32 + sub];
         }
-        if (kb + WAVES < Q.n_kb) a = __builtin_amdgcn_readfirstlane(pk_action(P, rb * P.n_chunks + (kb + WAVES) / per_chunk, base));
-        if (kb == wave && Q.h != nullptr) {                 // while all of this is on its way
+        if (kb + EACH < Q.n_kb) a = __builtin_amdgcn_readfirstlane(pk_action(P, rb * P.n_chunks + (kb + EACH) / per_chunk, base));
+        if (!PAIR && kb == wave && Q.h != nullptr) {                 // while all of this is on its way
             const int r = threadIdx.x & 31;
             const int64_t t = t0 + (threadIdx.x >> 5);
             if (r < rows_left && t < Q.T) more = expand_one<uint16_t>(Q.A, Q.h, t, row0 + r, P.rows);
@@ -267,18 +271,25 @@ __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q
         const int r = e & 31, n = e >> 5;                  // neighbouring lanes: neighbouring rows of a token
         const int64_t y = row0 + r, t = t0 + n;
         if (r >= rows_left || t >= Q.T) continue;
-        if (Q.h != nullptr && (e != (int)threadIdx.x || wave >= Q.n_kb)) more = expand_one<uint16_t>(Q.A, Q.h, t, y, P.rows);
+        if (!PAIR && Q.h != nullptr && (e != (int)threadIdx.x || wave >= Q.n_kb)) more = expand_one<uint16_t>(Q.A, Q.h, t, y, P.rows);
         const int at = ((n >> 5) * 16 + (r >> 3) * 4 + (r & 3)) * 64 + ((r >> 2) & 1) * 32 + (n & 31);
         float v = 0.0f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) v += red[w * NTF * 1024 + at];
-        if (!isfinite(v)) v = (float)pk_slow_dot(P, y, Q.X + t * Q.ldx);
+        for (int w = 0; w < EACH; ++w) v += red[w * NTF * 1024 + at];
+        if (!isfinite(v)) v = (float)pk_slow_dot(Q.P, y, Q.X + t * Q.ldx);
+        if constexpr (PAIR) {
+            float up = 0.0f;
+#pragma unroll
+            for (int w = EACH; w < WAVES; ++w) up += red[w * NTF * 1024 + at];
+            if (!isfinite(up)) up = (float)pk_slow_dot(Q.pair.up, y, Q.X + t * Q.ldx);
+            v = pair_result<uint16_t>(Q.pair, t, y, v, up);
+        }
         Q.Y[t * Q.ldy + y] = (uint16_t)f32_to_bf16_bits(v + more);
     }
 }
 
 // h, or null: formed here (Q.h without it: there already).
-template <int S>
+template <int S, bool PAIR = false>
 int launch_few(FewArgs Q, float* h, hipStream_t st) {
     Q.fragments = (int32_t)tokens_in(Q.T, 32);
     Q.xs_ld = tokens_in(Q.T, 64) * 64;
@@ -293,9 +304,9 @@ int launch_few(FewArgs Q, float* h, hipStream_t st) {
         if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
     }
     const dim3 g((uint32_t)wgs);
-    if (!laid) project_few_kernel<S, 1, 16, false><<<g, dim3(1024), 0, st>>>(Q);
-    else if (Q.fragments == 1) project_few_kernel<S, 1, 8, true><<<g, dim3(512), 0, st>>>(Q);
-    else project_few_kernel<S, 2, 8, true><<<g, dim3(512), 0, st>>>(Q);
+    if (!laid) project_few_kernel<S, 1, 16, false, PAIR><<<g, dim3(1024), 0, st>>>(Q);
+    else if (Q.fragments == 1) project_few_kernel<S, 1, PAIR ? 16 : 8, true, PAIR><<<g, dim3(PAIR ? 1024 : 512), 0, st>>>(Q);
+    else project_few_kernel<S, 2, PAIR ? 16 : 8, true, PAIR><<<g, dim3(PAIR ? 1024 : 512), 0, st>>>(Q);
     return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
 }
 

@@ -19,7 +19,7 @@
 // wavefront, 2944 matrix instructions among them: neither unit is full, waits are 46 % of the wavefronts' time.
 #pragma once
 
-#include "windq_adapters.hpp"
+#include "windq_pair.hpp"
 
 namespace windq {
 
@@ -54,6 +54,9 @@ struct TileArgs {
     float* alpha;              // [chunks][rows] scales (1 where a unit is skipped)
     int32_t n_kb;              // k-blocks
     uint32_t row_blocks;
+    PairArgs pair;             // and what the up matrix has of its own
+    KbWord* unit_up;
+    uint4* beta_up;
 };
 
 // Whether a chunk is one k-block: its rows lie one behind the other in the code stream.  Otherwise every unit is laid out anew, k-block by
@@ -207,21 +210,24 @@ struct TileFields {
     }
 };
 
-template <typename YT, int S>
+// Of a pair (windq_gated) a tile is 128 rows of both: the wavefronts of the lower two strips have the gate's, the others the up's, and those hand their
+// results over through LDS at the end.
+template <typename YT, int S, bool PAIR = false>
 __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArgs Q) {
     constexpr int NP = sizeof(YT) == 4 ? 3 : 1;
     __shared__ uint4 xt[2][PT_TOKENS * 16];
     __shared__ uint4 ct[2][4][512];                        // fields of 64 rows
     __shared__ float st[2][PT_ROWS];
     __shared__ uint4 ring[4][8];                           // units' words, k-block by k-block
-    const PackArgs& P = Q.P;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, sub = lane & 31, hh = lane >> 5;
+    const int matrix = PAIR ? (wave >> 1) & 1 : 0;
+    const PackArgs& P = PAIR && matrix == 1 ? Q.pair.up : Q.P;
     const int wr = wave & 3, wt = wave >> 2;                // wavefronts w and w + 4 share a SIMD, and rows
     // Consecutive workgroups land on the eight XCDs in turn; each XCD gets a run of tiles that share tokens.
     const uint32_t n_tiles = gridDim.x, per = n_tiles >> 3;
     const uint32_t tile = blockIdx.x < per * 8 ? (blockIdx.x & 7) * per + (blockIdx.x >> 3) : blockIdx.x;
     const uint32_t tb = tile / Q.row_blocks;
-    const int64_t row0 = (int64_t)(tile - tb * Q.row_blocks) * PT_ROWS, t0 = (int64_t)tb * PT_TOKENS;
+    const int64_t row0 = (int64_t)(tile - tb * Q.row_blocks) * (PAIR ? PT_ROWS / 2 : PT_ROWS), t0 = (int64_t)tb * PT_TOKENS;
 
     // X: four of a tile's slots a lane; slot p of token n holds the octet of slot p ^ (n & 15)
     const uint16_t* xsrc[4];
@@ -233,7 +239,7 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
         xsrc[k] = Q.X + (t < Q.T ? t : Q.T - 1) * Q.ldx + ((slot >> 3) * S + s) * 8;
     }
     // rows: a lane's row of each fragment; the wavefront's unit row block
-    const int64_t wrow = row0 + wr * 64;
+    const int64_t wrow = row0 + (PAIR ? wr & 1 : wr) * 64;
     const int64_t rb = (wrow < P.rows ? wrow : P.rows - 1) / P.R_u;
     int64_t lrow[2];
 #pragma unroll
@@ -245,7 +251,8 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
     const int64_t rows_left = P.R_u - lrow0;
     const uint32_t lds_xt = lds_address(xt), lds_ct = lds_address(ct), lds_st = lds_address(st), lds_ring = lds_address(ring);
     const int32_t n_kb = Q.n_kb;
-    const KbWord* const words = Q.unit + rb * n_kb;
+    const KbWord* const words = (PAIR && matrix == 1 ? Q.unit_up : Q.unit) + rb * n_kb;
+    const uint4* const betas = PAIR && matrix == 1 ? Q.beta_up : Q.beta;
     auto uniform = [](uint32_t x, uint32_t y) {
         return (UnitWord)(uint32_t)__builtin_amdgcn_readfirstlane((int)y) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
     };
@@ -429,7 +436,7 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
         for (int k = 0; k < ROUND; ++k) {
             const int32_t at = k0 + 2 * k + hh < n_kb ? k0 + 2 * k + hh : n_kb - 1;
 #pragma unroll
-            for (int f = 0; f < 2; ++f) a[k][f] = Q.beta[at * P.rows + rb * P.R_u + lrow[f]];
+            for (int f = 0; f < 2; ++f) a[k][f] = betas[at * P.rows + rb * P.R_u + lrow[f]];
 #pragma unroll
             for (int n = 0; n < 2; ++n) b[k][n] = Q.xs[at * Q.T + tok[n]];
         }
@@ -465,38 +472,66 @@ __global__ __launch_bounds__(PT_THREADS) void project_tiles_kernel(const TileArg
             }
         }
 
-    if (Q.h != nullptr)
+    if (!PAIR && Q.h != nullptr)
         add_adapters<YT, 2>(Q.A, Q.h, true, t0 + wt * 64, Q.T, lane,
                             [&](int32_t k, int f) { return static_cast<const YT*>(Q.A.b) + ((int64_t)k * P.rows + rb * P.R_u + lrow[f]) * Q.A.max_rank; }, tot);
 
-    YT* __restrict__ const Y = static_cast<YT*>(Q.Y);
-    const bool whole = (Q.ldy & 3) == 0 && (reinterpret_cast<uintptr_t>(Y) & (4 * sizeof(YT) - 1)) == 0;
+    auto store = [&](void* to, int64_t ld) {
+        YT* __restrict__ const Y = static_cast<YT*>(to);
+        const bool whole = (ld & 3) == 0 && (reinterpret_cast<uintptr_t>(Y) & (4 * sizeof(YT) - 1)) == 0;
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-        const int64_t t = t0 + wt * 64 + n * 32 + sub;
-        if (t >= Q.T) continue;
+        for (int n = 0; n < 2; ++n) {
+            const int64_t t = t0 + wt * 64 + n * 32 + sub;
+            if (t >= Q.T) continue;
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int64_t row = wrow + f * 32 + g * 8 + hh * 4;
+                    if (row >= P.rows) continue;           // rows come in eights
+                    YT* __restrict__ const o = Y + t * ld + row;
+                    float v[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = tot[f][n][g * 4 + i];
+                    if (whole) {
+                        if constexpr (sizeof(YT) == 4) *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+                        else *reinterpret_cast<uint2*>(o) = make_uint2(f32_to_bf16_bits(v[0]) | f32_to_bf16_bits(v[1]) << 16, f32_to_bf16_bits(v[2]) | f32_to_bf16_bits(v[3]) << 16);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if constexpr (sizeof(YT) == 4) o[i] = v[i];
+                            else o[i] = (uint16_t)f32_to_bf16_bits(v[i]);
+                        }
+                    }
+                }
+        }
+    };
+    if constexpr (PAIR) {
+        if (Q.pair.G != nullptr) store(matrix == 1 ? Q.pair.U : Q.pair.G, Q.pair.ld_save);
+        float* const over = reinterpret_cast<float*>(xt) + ((wr & 1) * 2 + wt) * 4096 + lane;    // 64 results a lane
+        static_assert(sizeof(xt) >= 4 * 4096 * sizeof(float), "the up's results fit");
+        __syncthreads();                                    // everybody is done with X
+        if (matrix == 1) {
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) over[((f * 2 + n) * 16 + i) * 64] = tot[f][n][i];
+        }
+        __syncthreads();
+        if (matrix == 1) return;
 #pragma unroll
         for (int f = 0; f < 2; ++f)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int64_t row = wrow + f * 32 + g * 8 + hh * 4;
-                if (row >= P.rows) continue;               // rows come in eights
-                YT* __restrict__ const o = Y + t * Q.ldy + row;
-                float v[4];
+            for (int n = 0; n < 2; ++n)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = tot[f][n][g * 4 + i];
-                if (whole) {
-                    if constexpr (sizeof(YT) == 4) *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
-                    else *reinterpret_cast<uint2*>(o) = make_uint2(f32_to_bf16_bits(v[0]) | f32_to_bf16_bits(v[1]) << 16, f32_to_bf16_bits(v[2]) | f32_to_bf16_bits(v[3]) << 16);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if constexpr (sizeof(YT) == 4) o[i] = v[i];
-                        else o[i] = (uint16_t)f32_to_bf16_bits(v[i]);
-                    }
+                for (int i = 0; i < 16; ++i) {
+                    float none;
+                    tot[f][n][i] = activation<false>(Q.pair.act, tot[f][n][i], none) * over[((f * 2 + n) * 16 + i) * 64];
                 }
-            }
     }
+    store(Q.Y, Q.ldy);
 }
 
 #endif  // __HIPCC__
