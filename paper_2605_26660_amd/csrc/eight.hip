@@ -1,7 +1,7 @@
 // 8-bit tokens (windq_tokens8), a plan's form for serving them (windq_serving_lay), and their products (windq_project8, windq_gated8).
 #include <math.h>
 
-#include "windq_eight.hpp"
+#include "windq_eight_tiles.hpp"
 
 namespace windq {
 
@@ -332,6 +332,14 @@ template <typename YT, int S, bool PAIR>
 int launch_eight(const EightArgs& Q, hipStream_t st) {
     constexpr int WAVES = 8;
     if (Q.T <= 32) return launch_pieces(Q.NB, WAVES * 64, [&](int64_t first, dim3 g) { eight_kernel<YT, S, 1, WAVES, PAIR><<<g, dim3(WAVES * 64), 0, st>>>(Q, first); });
+    if (Q.T > 128) {
+        constexpr int WR = 4, WT = 2;
+        const int64_t row_tiles = tokens_in(Q.NB, PAIR ? WR : 2 * WR), tiles = row_tiles * tokens_in(Q.T, WT * 64);
+        if (fits_launch(tiles, WR * WT * 64)) {
+            eight_tiles_kernel<YT, S, WR, WT, PAIR><<<dim3((uint32_t)tiles), dim3(WR * WT * 64), 0, st>>>(Q, (uint32_t)row_tiles);
+            return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
+        }
+    }
     return launch_pieces(Q.NB * tokens_in(Q.T, 64), WAVES * 64, [&](int64_t first, dim3 g) { eight_kernel<YT, S, 2, WAVES, PAIR><<<g, dim3(WAVES * 64), 0, st>>>(Q, first); });
 }
 
