@@ -135,9 +135,9 @@ __global__ __launch_bounds__(256) void serving_lay_kernel(const PackArgs P, cons
     const int a = pk_action(P, u, base);
     int kind = eight_kind(a);
     const int64_t block = eight_bytes(kind, E.S, P.w_f32 != 0), need = block * per_unit, at = image_off[u], end = image_off[u + 1];
-    if (at < E.header || (at & 255) != 0 || end > bytes || end - at < need) kind = 7;
+    if (at < E.header || (at & 255) != 0 || end > bytes || end - at < need || at > bytes - EIGHT_PAST - need) kind = 7;
     if (i == 0 && c == 0 && lane == 0)
-        reinterpret_cast<uint64_t*>(image)[u] = (kind == 7 ? 0ull : (uint64_t)at) | (uint64_t)kind << 56;
+        reinterpret_cast<uint2*>(image)[u] = kind == 7 ? make_uint2(0u, 7u) : make_uint2((uint32_t)(at >> 8), (uint32_t)kind | (uint32_t)(block >> 8) << 8);
     const int64_t lrow = i * EIGHT_ROWS + sub;
     const bool in = lrow < P.R_u;
     const int64_t row = rb * P.R_u + (in ? lrow : 0);
@@ -177,26 +177,31 @@ __global__ __launch_bounds__(256) void serving_lay_kernel(const PackArgs P, cons
         uint32_t v[16];
 #pragma unroll
         for (int k = 0; k < 16; ++k) v[k] = in && c0 + k < P.G ? (uint32_t)eight_code(a, codes, c0 + k) : 0u;
+        // words of a lane's string, each to its piece
+        auto put = [&](int k, uint32_t w) {
+            const int length = eight_string(kind, E.S), full = length >> 4;
+            char* const p = (k >> 2) < full ? to + (k >> 2) * 1024 + lane * 16 : to + full * 1024 + lane * (length & 15);
+            reinterpret_cast<uint32_t*>(p)[k & 3] = w;
+        };
+        uint32_t w[4] = {};
         if (kind == 1) {
-            uint32_t w[4] = {};
 #pragma unroll
             for (int k = 0; k < 16; ++k) w[k >> 2] |= (v[k] & 0xffu) << (8 * (k & 3));
-            reinterpret_cast<uint4*>(to)[s * 64 + lane] = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int k = 0; k < 4; ++k) put(4 * s + k, w[k]);
         } else if (kind == 2) {
-            uint32_t w[2] = {};
 #pragma unroll
             for (int k = 0; k < 16; ++k) w[k >> 3] |= v[k] << (8 * (k & 3) + 4 * ((k >> 2) & 1));
-            reinterpret_cast<uint2*>(to)[s * 64 + lane] = make_uint2(w[0], w[1]);
+            put(2 * s, w[0]);
+            put(2 * s + 1, w[1]);
         } else if (kind == 4) {
-            uint32_t w = 0;
 #pragma unroll
-            for (int k = 0; k < 16; ++k) w |= v[k] << (8 * (k & 3) + 2 * (k >> 2));
-            reinterpret_cast<uint32_t*>(to)[lane * E.S + s] = w;
+            for (int k = 0; k < 16; ++k) w[0] |= v[k] << (8 * (k & 3) + 2 * (k >> 2));
+            put(s, w[0]);
         } else {
 #pragma unroll
             for (int k = 0; k < 16; ++k) bits |= v[k] << (8 * (k & 3) + (k >> 2) + 4 * (s & 1));
             if ((s & 1) != 0 || s + 1 == E.S) {
-                reinterpret_cast<uint32_t*>(to)[lane * ((E.S + 1) / 2) + (s >> 1)] = bits;
+                put(s >> 1, bits);
                 bits = 0;
             }
         }
@@ -228,10 +233,11 @@ __global__ __launch_bounds__(WAVES * 64) void eight_kernel(const EightArgs Q, co
     f32x16 tot[N] = {};
     for (int32_t kb = wave % EACH; kb < Q.n_kb; kb += EACH) {
         const int32_t j = kb / Q.per_chunk, c = kb - j * Q.per_chunk;
-        const EightUnit u = eight_unit(P, rb * Q.n_chunks + j, Q.RB * Q.per_chunk, S, w_f32);
-        const int kind = __builtin_amdgcn_readfirstlane(u.kind);
+        const uint2 word = reinterpret_cast<const uint2*>(P.image)[rb * Q.n_chunks + j];
+        const EightBlock u = eight_block(P, __builtin_amdgcn_readfirstlane((int)word.x), __builtin_amdgcn_readfirstlane((int)word.y), (uint32_t)(i * Q.per_chunk + c));
+        const int kind = u.kind;
         if (kind == 7) continue;
-        const char* const fields = u.fields + (i * Q.per_chunk + c) * eight_bytes(kind, S, w_f32);
+        const char* const fields = u.fields;
         uint4 xv[S][N];
 #pragma unroll
         for (int s = 0; s < S; ++s)
@@ -265,33 +271,14 @@ __global__ __launch_bounds__(WAVES * 64) void eight_kernel(const EightArgs Q, co
 #pragma unroll
         for (int n = 0; n < N; ++n) sum[n] = (float)xs[n][kb];
         i32x16 acc[N] = {};
-        auto steps = [&](auto operand) {
+        EightFields<S> raw;
+        raw.load(kind, fields, lane);
+        i32x4 w[S];
+        raw.operands(kind, w);
 #pragma unroll
-            for (int s = 0; s < S; ++s) {
-                const i32x4 f = operand(s);
+        for (int s = 0; s < S; ++s)
 #pragma unroll
-                for (int n = 0; n < N; ++n) acc[n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(f, as_i32x4(xv[s][n]), acc[n], 0, 0, 0);
-            }
-        };
-        if (kind == 6) {
-            uint32_t v[(S + 1) / 2];
-            __builtin_memcpy(v, fields + lane * (int)sizeof(v), sizeof(v));
-            steps([&](int s) { return eight_fields1(v[s >> 1], s & 1); });
-        } else if (kind == 4) {
-            uint32_t v[S];
-            __builtin_memcpy(v, fields + lane * (int)sizeof(v), sizeof(v));
-            steps([&](int s) { return eight_fields2(v[s]); });
-        } else if (kind == 2) {
-            uint2 v[S];
-#pragma unroll
-            for (int s = 0; s < S; ++s) v[s] = reinterpret_cast<const uint2*>(fields)[s * 64 + lane];
-            steps([&](int s) { return eight_fields4(v[s]); });
-        } else {
-            uint4 v[S];
-#pragma unroll
-            for (int s = 0; s < S; ++s) v[s] = reinterpret_cast<const uint4*>(fields)[s * 64 + lane];
-            steps([&](int s) { return as_i32x4(v[s]); });
-        }
+            for (int n = 0; n < N; ++n) acc[n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[s], as_i32x4(xv[s][n]), acc[n], 0, 0, 0);
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const float av[4] = {al[g].x, al[g].y, al[g].z, al[g].w}, bv[4] = {be[g].x, be[g].y, be[g].z, be[g].w};
@@ -362,6 +349,7 @@ static int check_serving(const windq_serving* S, EightShape* E, EightPlan* P) {
     if (!chunk_ok(S->cols, S->chunk_w) || S->rows <= 0 || S->rows > MOST_SIDE || S->unit_rows < 0 || (S->unit_rows != 0 && S->rows % S->unit_rows != 0)) return WINDQ_ESHAPE;
     if (!sizes_fit(0, S->rows, S->cols, 0, 0)) return WINDQ_ESHAPE;
     *E = eight_shape(S->rows, S->cols, S->unit_rows == 0 ? S->rows : S->unit_rows, S->chunk_w);
+    if (S->image_bytes > (size_t)1 << 39) return WINDQ_ESHAPE;
     if ((int64_t)S->image_bytes < E->header) return WINDQ_EINVAL;
     *P = {static_cast<const char*>(S->image), (int64_t)S->image_bytes, E->header};
     return WINDQ_OK;
@@ -447,7 +435,7 @@ extern "C" int windq_serving_layout(const uint8_t* action, int64_t rows, int64_t
         image_off[u] = at;
         at += eight_bytes(eight_kind(action[u]), E.S, dtype == WINDQ_F32) * E.RB * E.per_chunk;
     }
-    image_off[E.U] = at;
+    image_off[E.U] = at + EIGHT_PAST;
     return WINDQ_OK;
 }
 
@@ -458,7 +446,7 @@ extern "C" int windq_serving_lay(const windq_packed* P, const int64_t* image_off
     if (A.mask != nullptr || image_off == nullptr || image == nullptr || !aligned(image_off, 8) || !aligned(image, 256)) return WINDQ_EINVAL;
     if (!sizes_fit(0, A.rows, A.cols, 0, 0)) return WINDQ_ESHAPE;
     const EightShape E = eight_shape(A.rows, A.cols, A.R_u, A.G);
-    if (image_bytes > (size_t)1 << 47) return WINDQ_ESHAPE;
+    if (image_bytes > (size_t)1 << 39 || E.RB * E.per_chunk > (int64_t)1 << 31) return WINDQ_ESHAPE;
     if ((int64_t)image_bytes < E.header) return WINDQ_EWORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     return launch_pieces(tokens_in(E.U * E.RB * E.per_chunk, 4), 256,

@@ -37,8 +37,8 @@ inline void eight_cut(int32_t G, int32_t* S, int32_t* per_chunk) {
     *S = (steps + *per_chunk - 1) / *per_chunk;
 }
 
-// The serving form's first part: a word a unit (offset of its fields, 48 bits, and its kind, top byte), then for every unit and row block
-// of it the 32 rows' alpha and beta.
+// The serving form's first part: two words a unit (where its fields begin, in 256s of bytes; its kind, and the 256s of bytes of a block of them), then for every
+// unit and row block of it the 32 rows' alpha and beta.
 inline EightShape eight_shape(int64_t rows, int64_t cols, int64_t R_u, int32_t G) {
     EightShape E;
     E.rows = rows;
@@ -61,10 +61,10 @@ inline EightShape eight_shape(int64_t rows, int64_t cols, int64_t R_u, int32_t G
 // Kinds of fields: 0 weights that stay as they are, 1: 8 bits, 2: 4 bits (3 as well), 4: 2 bits (trits as well), 6: 1 bit, 7: nothing (zeros).
 __host__ __device__ inline int eight_kind(int action) { return action == 3 ? 2 : (action == 5 ? 4 : action); }
 
-// Bytes of a row block's fields of one k-block.
-//   8 bits   [step][lane][16 bytes]      4 bits [step][lane][8 bytes]     2 bits [lane][step][4 bytes]     1 bit [lane][pair of steps][4 bytes]
-//   weights  [step][term][half of its 16 columns][lane][8 bfloat16], one term, or three where the weights are fp32
-// A word's four bytes hold columns 4 i + (0 .. 3) at bits b i of each byte, b bits a field: w >> b i, masked, are four operands of the matrix instruction.
+// Bytes of a row block's fields of one k-block: a string of words a lane, step by step, in pieces of 16 bytes, [piece][lane][16], and what is left over,
+// [lane][the rest].  8 bits: four words a step, 4 bits: two, 2 bits: one, 1 bit: one for two steps.  A word's four bytes hold columns 4 i + (0 .. 3)
+// at bits b i of each byte, b bits a field: w >> b i, masked, are four operands of the matrix instruction.
+//   Weights that stay as they are: [step][term][half of its 16 columns][lane][8 bfloat16], one term, or three where they are fp32.
 __host__ __device__ inline int64_t eight_bytes(int kind, int S, bool w_f32) {
     switch (kind) {
         case 0: return (w_f32 ? 6144 : 2048) * (int64_t)S;
@@ -75,6 +75,10 @@ __host__ __device__ inline int64_t eight_bytes(int kind, int S, bool w_f32) {
         default: return 0;
     }
 }
+
+// Bytes of a lane's string.
+__host__ __device__ inline int eight_string(int kind, int S) { return kind == 1 ? 16 * S : (kind == 2 ? 8 * S : (kind == 4 ? 4 * S : 4 * ((S + 1) / 2))); }
+constexpr int EIGHT_PAST = 256;                            // bytes past its last fields that an image has: a lane reads whole pieces
 
 struct EightPlan {
     const char* image;
@@ -101,21 +105,19 @@ typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ i32x4 as_i32x4(uint4 v) { return __builtin_bit_cast(i32x4, v); }
 
-// Where a unit's fields lie and what they are; what does not fit the image counts as nothing.
-struct EightUnit {
+// Where a row block's fields of a k-block lie and what they are: block `index` of its unit's, whose words are `unit`.  What does not lie
+// between the header and the image's end counts as nothing.
+struct EightBlock {
     const char* fields;
     int kind;
 };
-__device__ __forceinline__ EightUnit eight_unit(const EightPlan& P, int64_t u, int64_t blocks, int S, bool w_f32) {
-    const uint64_t word = reinterpret_cast<const uint64_t*>(P.image)[u];
-    const int64_t at = (int64_t)(word & 0xffffffffffffull);
-    const int kind = (int)(word >> 56);
-    const int64_t need = eight_bytes(kind, S, w_f32) * blocks;
-    const bool fits = kind < 7 && kind != 3 && kind != 5 && at >= P.header && (at & 255) == 0 && at <= P.bytes - need;
-    return {P.image + at, fits ? kind : 7};
+__device__ __forceinline__ EightBlock eight_block(const EightPlan& P, uint32_t unit, uint32_t what, uint32_t index) {
+    const uint32_t size = what >> 8, at = unit + index * size;
+    const bool fits = at >= (uint32_t)(P.header >> 8) && at < (uint32_t)(P.bytes >> 8) && size < (uint32_t)(P.bytes >> 8) - at;
+    return {fits ? P.image + ((uint64_t)at << 8) : P.image, fits ? (int)(what & 7u) : 7};
 }
 
-// Operands of step s out of a lane's fields.
+// Operands of a step out of a lane's words.
 __device__ __forceinline__ i32x4 eight_fields4(uint2 v) {
     i32x4 f;
     f[0] = (int)(v.x & 0x0f0f0f0fu);
@@ -140,6 +142,48 @@ __device__ __forceinline__ i32x4 eight_fields1(uint32_t v, int odd) {
     f[3] = (int)((v >> (4 * odd + 3)) & 0x01010101u);
     return f;
 }
+
+// A lane's string of one row block and k-block.
+template <int S>
+struct EightFields {
+    uint32_t v[S][4];
+    __device__ __forceinline__ void load(int kind, const char* __restrict__ fields, int lane) {
+        auto piece = [&](int k, int stride) { __builtin_memcpy(v[k], fields + k * 1024 + lane * stride, 16); };
+        // the first piece whatever the kind (what holds no string reads its first bytes), so that no register waits for what comes in by another way
+        piece(0, kind == 0 || kind == 7 ? 0 : (kind == 6 ? 4 * ((S + 1) / 2) : (kind == 4 ? 4 * S : (kind == 2 && S == 1 ? 8 : 16))));
+        if constexpr (S >= 3) {
+            if (kind == 2 || kind == 1) piece(1, kind == 2 && S == 3 ? 8 : 16);
+        } else if constexpr (S == 2) {
+            if (kind == 1) piece(1, 16);
+        }
+        if constexpr (S >= 3) {
+            if (kind == 1) {
+                piece(2, 16);
+                if constexpr (S == 4) piece(3, 16);
+            }
+        }
+    }
+    __device__ __forceinline__ uint32_t word(int k) const { return v[k >> 2][k & 3]; }
+    // The operands of all steps; zeros for what holds no string.
+    __device__ __forceinline__ void operands(int kind, i32x4 (&w)[S]) const {
+        if (kind == 6) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) w[s] = eight_fields1(word(s >> 1), s & 1);
+        } else if (kind == 4) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) w[s] = eight_fields2(word(s));
+        } else if (kind == 2) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) w[s] = eight_fields4(make_uint2(word(2 * s), word(2 * s + 1)));
+        } else if (kind == 1) {
+#pragma unroll
+            for (int s = 0; s < S; ++s) w[s] = as_i32x4(make_uint4(v[s][0], v[s][1], v[s][2], v[s][3]));
+        } else {
+#pragma unroll
+            for (int s = 0; s < S; ++s) w[s] = i32x4{};
+        }
+    }
+};
 
 // Eight of a token's integers as bfloat16: exact.
 __device__ __forceinline__ bf16x8 eight_as_bf16(uint32_t a, uint32_t b) {

@@ -7,47 +7,6 @@ namespace windq {
 
 #ifdef __HIPCC__
 
-// A lane's fields of one row block and k-block.
-template <int S>
-struct EightRaw {
-    uint32_t v[4 * S];
-    __device__ __forceinline__ void load(int kind, const char* __restrict__ fields, int lane) {
-        if (kind == 6) {
-            __builtin_memcpy(v, fields + lane * (4 * ((S + 1) / 2)), 4 * ((S + 1) / 2));
-        } else if (kind == 4) {
-            __builtin_memcpy(v, fields + lane * (4 * S), 4 * S);
-        } else if (kind == 2) {
-#pragma unroll
-            for (int s = 0; s < S; ++s) {
-                const uint2 w = reinterpret_cast<const uint2*>(fields)[s * 64 + lane];
-                v[2 * s] = w.x;
-                v[2 * s + 1] = w.y;
-            }
-        } else if (kind == 1) {
-#pragma unroll
-            for (int s = 0; s < S; ++s) {
-                const uint4 w = reinterpret_cast<const uint4*>(fields)[s * 64 + lane];
-                v[4 * s] = w.x;
-                v[4 * s + 1] = w.y;
-                v[4 * s + 2] = w.z;
-                v[4 * s + 3] = w.w;
-            }
-        }
-    }
-    template <int KIND>
-    __device__ __forceinline__ void operands(i32x4 (&w)[S]) const {
-#pragma unroll
-        for (int s = 0; s < S; ++s) w[s] = operand<KIND>(s);
-    }
-    template <int KIND>
-    __device__ __forceinline__ i32x4 operand(int s) const {
-        if constexpr (KIND == 6) return eight_fields1(v[s >> 1], s & 1);
-        else if constexpr (KIND == 4) return eight_fields2(v[s]);
-        else if constexpr (KIND == 2) return eight_fields4(make_uint2(v[2 * s], v[2 * s + 1]));
-        else return as_i32x4(make_uint4(v[4 * s], v[4 * s + 1], v[4 * s + 2], v[4 * s + 3]));
-    }
-};
-
 template <int V>
 struct Const {
     static constexpr int value = V;
@@ -69,16 +28,19 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
 
     // a wavefront's two row blocks: neighbours, or the same of the gate and of the up; past the last one: computed for nothing, stored by nobody
     int64_t b[2], rb[2], in[2];
-    const char* image[2];
+    const uint2* words[2];
     const float* affine[2];
+    uint32_t first[2];
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
         b[f] = PAIR ? b0 : 2 * b0 + f;
         const int64_t at = b[f] < Q.NB ? b[f] : Q.NB - 1;
         rb[f] = at / Q.RB;
         in[f] = at - rb[f] * Q.RB;
-        image[f] = Q.P[PAIR ? f : 0].image;
-        affine[f] = reinterpret_cast<const float*>(image[f] + Q.affine) + at * Q.n_chunks * 64 + sub;
+        const char* const image = Q.P[PAIR ? f : 0].image;
+        words[f] = reinterpret_cast<const uint2*>(image) + rb[f] * Q.n_chunks;
+        affine[f] = reinterpret_cast<const float*>(image + Q.affine) + at * Q.n_chunks * 64;
+        first[f] = (uint32_t)(in[f] * Q.per_chunk);
     }
 
     // X: a row of 128 bytes a token, eight slots; slot p of token n holds slot p ^ (n / 2 & 7)
@@ -101,54 +63,68 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
         sums[n] = Q.sums + (t < Q.T ? t : Q.T - 1) * Q.sums_ld;
     }
 
-    struct Unit {
-        const char* fields;
-        int kind;
+    // Where a k-block's fields lie: its unit's words are asked for two k-blocks ahead, its fields one.
+    struct Place {
+        int32_t j, c;
     };
-    auto unit_of = [&](int f, int32_t kb) {
-        const int32_t j = kb / Q.per_chunk, c = kb - j * Q.per_chunk;
-        const EightUnit u = eight_unit(Q.P[PAIR ? f : 0], rb[f] * Q.n_chunks + j, Q.RB * Q.per_chunk, S, w_f32);
-        const int kind = __builtin_amdgcn_readfirstlane(u.kind);
-        return Unit{u.fields + (in[f] * Q.per_chunk + c) * eight_bytes(kind, S, w_f32), kind};
+    auto after = [&](Place p) {                             // of the last k-block: itself
+        const bool wrap = p.c + 1 == Q.per_chunk;
+        if (wrap && p.j + 1 == Q.n_chunks) return p;
+        return Place{p.j + (wrap ? 1 : 0), wrap ? 0 : p.c + 1};
+    };
+    auto block_of = [&](int f, uint2 v, int32_t c) {
+        return eight_block(Q.P[PAIR ? f : 0], (uint32_t)__builtin_amdgcn_readfirstlane((int)v.x), (uint32_t)__builtin_amdgcn_readfirstlane((int)v.y), first[f] + (uint32_t)c);
     };
 
     f32x16 tot[2][2] = {};
     i32x16 acc[2][2] = {};
-    EightRaw<S> raw[2];
-    Unit now[2];
-    float alpha[2], behind = 0.0f;                         // of the k-block; of the second row block's sums that are still to be added up
+    EightFields<S> raw[2];
+    EightBlock now[2], next[2];
+    uint2 word[2];
+    Place ahead = {0, 0};
+    float alpha[2], alpha_next[2], behind = 0.0f;           // of the k-block; of the second row block's sums that are still to be added up
+    // beta times the tokens' sums, two k-blocks an instruction, a lane's half one of them: asked for a k-block ahead
+    float beta[2] = {};
+    int32_t sum[2] = {};
+    auto last_of_pair = [&](int32_t kb) { return (kb & 1) != 0 || kb + 1 == n_kb; };
+    auto load_pair = [&](int32_t kb) {
+        const int32_t at = (kb & ~1) + hh < n_kb ? (kb & ~1) + hh : kb, j = (int32_t)((uint32_t)at / (uint32_t)Q.per_chunk);
+#pragma unroll
+        for (int f = 0; f < 2; ++f) beta[f] = affine[f][j * 64 + 32 + sub];
+#pragma unroll
+        for (int n = 0; n < 2; ++n) sum[n] = sums[n][at];
+    };
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
-        now[f] = unit_of(f, 0);
+        now[f] = block_of(f, words[f][0], 0);
         raw[f].load(now[f].kind, now[f].fields, lane);
-        alpha[f] = now[f].kind == 0 || now[f].kind == 7 ? 0.0f : affine[f][0];
+        alpha[f] = now[f].kind == 0 || now[f].kind == 7 ? 0.0f : affine[f][sub];
     }
+    ahead = after(ahead);
+#pragma unroll
+    for (int f = 0; f < 2; ++f) word[f] = words[f][ahead.j];
     load_x(0, 0);
-    float pair_beta[2] = {}, pair_sum[2] = {};
+    if (n_kb == 1) load_pair(0);
 
     for (int32_t kb = 0; kb < n_kb; ++kb) {
         const int buf = kb & 1;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        const int32_t then = kb + 1 < n_kb ? kb + 1 : kb;
-        load_x(then, buf ^ 1);
-        // beta times the tokens' sums, two k-blocks an instruction: a lane's half has one of them
-        const bool both = (kb & 1) != 0 || kb + 1 == n_kb;
-        if (both) {
-            const int32_t at = (kb & ~1) + hh;
-            const bool valid = at < n_kb;
-            const int32_t j = (valid ? at : kb) / Q.per_chunk;
+        const Place then = ahead;
+        ahead = after(ahead);
 #pragma unroll
-            for (int f = 0; f < 2; ++f) {
-                const float v = affine[f][j * 64 + 32];
-                pair_beta[f] = valid ? v : 0.0f;
-            }
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                const int32_t v = sums[n][valid ? at : kb];
-                pair_sum[n] = valid ? (float)v : 0.0f;
-            }
+        for (int f = 0; f < 2; ++f) {
+            next[f] = block_of(f, word[f], then.c);
+            word[f] = words[f][ahead.j];
         }
+        load_x(kb + 1 < n_kb ? kb + 1 : kb, buf ^ 1);
+        const bool both = last_of_pair(kb);
+        float pair_beta[2], pair_sum[2];
+#pragma unroll
+        for (int f = 0; f < 2; ++f) pair_beta[f] = (kb & ~1) + hh < n_kb ? beta[f] : 0.0f;
+#pragma unroll
+        for (int n = 0; n < 2; ++n) pair_sum[n] = (kb & ~1) + hh < n_kb ? (float)sum[n] : 0.0f;
+        if (kb + 1 < n_kb && last_of_pair(kb + 1)) load_pair(kb + 1);
         uint4 x[S][2];
         const char* const xb = reinterpret_cast<const char*>(xt[buf]) + (wt * 64 + sub) * 128;
 #pragma unroll
@@ -169,30 +145,10 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
             // Only the operands differ by kind; where there are no codes they are zeros.
             const int kind = now[f].kind;
             i32x4 w[S];
-            if (kind == 6) raw[f].template operands<6>(w);
-            else if (kind == 4) raw[f].template operands<4>(w);
-            else if (kind == 2) raw[f].template operands<2>(w);
-            else if (kind == 1) raw[f].template operands<1>(w);
-            else {
-#pragma unroll
-                for (int s = 0; s < S; ++s) w[s] = i32x4{};
-                if (kind == 0) {
-                    const int terms = w_f32 ? 3 : 1;
-                    const uint4* const wv = reinterpret_cast<const uint4*>(now[f].fields) + lane;
-#pragma unroll 1
-                    for (int term = 0; term < terms; ++term)
-#pragma unroll
-                        for (int s = 0; s < S; ++s)
-#pragma unroll
-                            for (int half = 0; half < 2; ++half) {
-                                const bf16x8 v = as_bf16x8(wv[((s * terms + term) * 2 + half) * 64]);
-#pragma unroll
-                                for (int n = 0; n < 2; ++n)
-                                    tot[f][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(half == 0 ? eight_as_bf16(x[s][n].x, x[s][n].y) : eight_as_bf16(x[s][n].z, x[s][n].w), v, tot[f][n], 0, 0, 0);
-                                __builtin_amdgcn_sched_barrier(0);
-                            }
-                }
-            }
+            raw[f].operands(kind, w);
+            __builtin_amdgcn_sched_barrier(0);
+            raw[f].load(next[f].kind, next[f].fields, lane);
+            alpha_next[f] = affine[f][then.j * 64 + sub];
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int s = 0; s < S; ++s) {
@@ -203,7 +159,8 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            if (both) {
+            asm volatile("" : "+v"(tot[other][0]), "+v"(tot[other][1]));       // here, between the matrix instructions, and not in a later block
+                            if (both) {
 #pragma unroll
                 for (int n = 0; n < 2; ++n) tot[f][n] = __builtin_amdgcn_mfma_f32_32x32x2f32(pair_sum[n], pair_beta[f], tot[f][n], 0, 0, 0);
             }
@@ -213,10 +170,8 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
         behind = alpha[1];
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
-            now[f] = unit_of(f, then);
-            raw[f].load(now[f].kind, now[f].fields, lane);
-            const float v = affine[f][(then / Q.per_chunk) * 64];
-            alpha[f] = now[f].kind == 0 || now[f].kind == 7 ? 0.0f : v;
+            now[f] = next[f];
+            alpha[f] = now[f].kind == 0 || now[f].kind == 7 ? 0.0f : alpha_next[f];
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -224,6 +179,44 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
     for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i) tot[1][n][i] = fmaf(behind, (float)acc[1][n][i], tot[1][n][i]);
+
+    // Weights that stay as they are, unit by unit, with the tokens from where they lie: few units, and none of the others waits for them.
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+        for (int32_t j0 = 0; j0 < Q.n_chunks; j0 += 64) {
+            const bool valid = j0 + lane < Q.n_chunks;
+            const uint2 v = words[f][valid ? j0 + lane : j0];
+            for (uint64_t left = __ballot(valid && (v.y & 7u) == 0); left != 0; left &= left - 1) {
+                const int at = __builtin_ctzll(left);
+                const int terms = w_f32 ? 3 : 1;
+                for (int32_t c = 0; c < Q.per_chunk; ++c) {
+                    const EightBlock u = block_of(f, make_uint2((uint32_t)__builtin_amdgcn_readlane((int)v.x, at), (uint32_t)__builtin_amdgcn_readlane((int)v.y, at)), c);
+                    if (u.kind != 0) continue;
+                    const uint4* const w = reinterpret_cast<const uint4*>(u.fields) + lane;
+                    uint4 x[S][2];
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        const int64_t t = t0 + wt * 64 + n * 32 + sub;
+                        const int8_t* const from = Q.codes + (t < Q.T ? t : Q.T - 1) * Q.width + ((int64_t)(j0 + at) * Q.per_chunk + c) * (32 * S) + hh * 16;
+#pragma unroll
+                        for (int s = 0; s < S; ++s) x[s][n] = *reinterpret_cast<const uint4*>(from + s * 32);
+                    }
+#pragma unroll
+                    for (int s = 0; s < S; ++s)
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            bf16x8 xb[2];
+#pragma unroll
+                            for (int n = 0; n < 2; ++n) xb[n] = half == 0 ? eight_as_bf16(x[s][n].x, x[s][n].y) : eight_as_bf16(x[s][n].z, x[s][n].w);
+                            for (int term = 0; term < terms; ++term) {
+                                const bf16x8 wv = as_bf16x8(w[((s * terms + term) * 2 + half) * 64]);
+#pragma unroll
+                                for (int n = 0; n < 2; ++n) tot[f][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[n], wv, tot[f][n], 0, 0, 0);
+                            }
+                        }
+                }
+            }
+        }
 
     YT* __restrict__ const Y = static_cast<YT*>(Q.Y);
 #pragma unroll
