@@ -136,12 +136,13 @@ __global__ __launch_bounds__(256) void serving_lay_kernel(const PackArgs P, cons
     int kind = eight_kind(a);
     const int64_t block = eight_bytes(kind, E.S, P.w_f32 != 0), need = block * per_unit, at = image_off[u], end = image_off[u + 1];
     if (at < E.header || (at & 255) != 0 || end > bytes || end - at < need || at > bytes - EIGHT_PAST - need) kind = 7;
-    if (i == 0 && c == 0 && lane == 0)
-        reinterpret_cast<uint2*>(image)[u] = kind == 7 ? make_uint2(0u, 7u) : make_uint2((uint32_t)(at >> 8), (uint32_t)kind | (uint32_t)(block >> 8) << 8);
+    const int64_t mine = (rb * E.RB + i) * E.n_kb + j * E.per_chunk + c;
+    const int64_t here = at + (i * E.per_chunk + c) * block;
+    if (lane == 0) reinterpret_cast<uint32_t*>(image)[mine] = kind == 7 ? 7u : (uint32_t)(here >> 8) << 3 | (uint32_t)kind;
     const int64_t lrow = i * EIGHT_ROWS + sub;
     const bool in = lrow < P.R_u;
     const int64_t row = rb * P.R_u + (in ? lrow : 0);
-    if (c == 0) {
+    {
         const float scale = in ? P.scale[u * P.R_u + lrow] : 0.0f, offset = in ? P.offset[u * P.R_u + lrow] : 0.0f;
         float alpha = scale, beta = offset;
         if (a == 1) beta = fmaf(128.0f, scale, offset);
@@ -154,11 +155,11 @@ __global__ __launch_bounds__(256) void serving_lay_kernel(const PackArgs P, cons
             alpha = in && kind == 0 ? 1.0f : 0.0f;
             beta = 0.0f;
         }
-        float* const to = reinterpret_cast<float*>(image + (E.U * 8 + 255) / 256 * 256) + ((rb * E.RB + i) * E.n_chunks + j) * 64;
+        float* const to = reinterpret_cast<float*>(image + E.affine) + mine * 64;
         to[hh * 32 + sub] = hh == 0 ? alpha : beta;
     }
     if (kind == 7) return;
-    char* const to = image + at + (i * E.per_chunk + c) * block;
+    char* const to = image + here;
     const uint8_t* const codes = P.codes + base + (in ? lrow : 0) * pk_bytes_per_group(a, P.G);
     uint32_t bits = 0;
     for (int s = 0; s < E.S; ++s) {
@@ -229,12 +230,10 @@ __global__ __launch_bounds__(WAVES * 64) void eight_kernel(const EightArgs Q, co
         x[n] = Q.codes + t * Q.width + hh * 16;
         xs[n] = Q.sums + t * Q.sums_ld;
     }
-    const float* const affine = reinterpret_cast<const float*>(P.image + Q.affine) + b * Q.n_chunks * 64 + hh * 4;
+    const float* const affine = reinterpret_cast<const float*>(P.image + Q.affine) + b * Q.n_kb * 64 + hh * 4;
     f32x16 tot[N] = {};
     for (int32_t kb = wave % EACH; kb < Q.n_kb; kb += EACH) {
-        const int32_t j = kb / Q.per_chunk, c = kb - j * Q.per_chunk;
-        const uint2 word = reinterpret_cast<const uint2*>(P.image)[rb * Q.n_chunks + j];
-        const EightBlock u = eight_block(P, __builtin_amdgcn_readfirstlane((int)word.x), __builtin_amdgcn_readfirstlane((int)word.y), (uint32_t)(i * Q.per_chunk + c));
+        const EightBlock u = eight_block(P, eight_word(P, __builtin_amdgcn_readfirstlane((int)reinterpret_cast<const uint32_t*>(P.image)[b * Q.n_kb + kb]), S, w_f32));
         const int kind = u.kind;
         if (kind == 7) continue;
         const char* const fields = u.fields;
@@ -264,8 +263,8 @@ __global__ __launch_bounds__(WAVES * 64) void eight_kernel(const EightArgs Q, co
         float4 al[4], be[4];
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-            al[g] = *reinterpret_cast<const float4*>(affine + j * 64 + g * 8);
-            be[g] = *reinterpret_cast<const float4*>(affine + j * 64 + 32 + g * 8);
+            al[g] = *reinterpret_cast<const float4*>(affine + kb * 64 + g * 8);
+            be[g] = *reinterpret_cast<const float4*>(affine + kb * 64 + 32 + g * 8);
         }
         float sum[N];
 #pragma unroll
@@ -349,7 +348,7 @@ static int check_serving(const windq_serving* S, EightShape* E, EightPlan* P) {
     if (!chunk_ok(S->cols, S->chunk_w) || S->rows <= 0 || S->rows > MOST_SIDE || S->unit_rows < 0 || (S->unit_rows != 0 && S->rows % S->unit_rows != 0)) return WINDQ_ESHAPE;
     if (!sizes_fit(0, S->rows, S->cols, 0, 0)) return WINDQ_ESHAPE;
     *E = eight_shape(S->rows, S->cols, S->unit_rows == 0 ? S->rows : S->unit_rows, S->chunk_w);
-    if (S->image_bytes > (size_t)1 << 39) return WINDQ_ESHAPE;
+    if (S->image_bytes > (size_t)1 << 37) return WINDQ_ESHAPE;
     if ((int64_t)S->image_bytes < E->header) return WINDQ_EINVAL;
     *P = {static_cast<const char*>(S->image), (int64_t)S->image_bytes, E->header};
     return WINDQ_OK;
@@ -386,9 +385,7 @@ static int product(const windq_serving* first, const windq_serving* second, cons
     Q.NB = E.NB;
     Q.width = E.width;
     Q.sums_ld = E.sums_ld;
-    Q.affine = (int64_t)round_up((size_t)E.U * 8, 256);
-    Q.n_chunks = E.n_chunks;
-    Q.per_chunk = E.per_chunk;
+    Q.affine = E.affine;
     Q.n_kb = E.n_kb;
     Q.act = act;
     Q.w_f32 = first->dtype == WINDQ_F32;
@@ -446,7 +443,7 @@ extern "C" int windq_serving_lay(const windq_packed* P, const int64_t* image_off
     if (A.mask != nullptr || image_off == nullptr || image == nullptr || !aligned(image_off, 8) || !aligned(image, 256)) return WINDQ_EINVAL;
     if (!sizes_fit(0, A.rows, A.cols, 0, 0)) return WINDQ_ESHAPE;
     const EightShape E = eight_shape(A.rows, A.cols, A.R_u, A.G);
-    if (image_bytes > (size_t)1 << 39 || E.RB * E.per_chunk > (int64_t)1 << 31) return WINDQ_ESHAPE;
+    if (image_bytes > (size_t)1 << 37) return WINDQ_ESHAPE;
     if ((int64_t)image_bytes < E.header) return WINDQ_EWORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     return launch_pieces(tokens_in(E.U * E.RB * E.per_chunk, 4), 256,

@@ -27,7 +27,7 @@ struct EightShape {
     int64_t width, sums_ld;    // bytes of a token, sums of a token (in fours)
     int64_t RB;                // row blocks of a unit
     int64_t n_rb, NB;          // unit row blocks; row blocks of the matrix
-    int64_t U, header;         // units; bytes ahead of the fields
+    int64_t U, affine, header; // units; bytes ahead of alpha and beta, and of the fields
 };
 
 // How a chunk is cut: as few k-blocks as have four steps at most, alike.
@@ -37,8 +37,8 @@ inline void eight_cut(int32_t G, int32_t* S, int32_t* per_chunk) {
     *S = (steps + *per_chunk - 1) / *per_chunk;
 }
 
-// The serving form's first part: two words a unit (where its fields begin, in 256s of bytes; its kind, and the 256s of bytes of a block of them), then for every
-// unit and row block of it the 32 rows' alpha and beta.
+// The serving form's first part, of the matrix's row blocks (unit by unit down the rows) and k-blocks: a word each, of where its fields begin in
+// 256s of bytes and of their kind (the lowest three bits); then the 32 rows' alpha and beta, again for each k-block of a chunk.
 inline EightShape eight_shape(int64_t rows, int64_t cols, int64_t R_u, int32_t G) {
     EightShape E;
     E.rows = rows;
@@ -54,7 +54,8 @@ inline EightShape eight_shape(int64_t rows, int64_t cols, int64_t R_u, int32_t G
     E.n_rb = rows / R_u;
     E.NB = E.n_rb * E.RB;
     E.U = E.n_rb * E.n_chunks;
-    E.header = (int64_t)round_up((size_t)E.U * 8, 256) + E.U * E.RB * 256;
+    E.affine = (int64_t)round_up((size_t)(E.NB * E.n_kb) * 4, 256);
+    E.header = E.affine + E.NB * E.n_kb * 256;
     return E;
 }
 
@@ -95,7 +96,7 @@ struct EightArgs {
     void* Y;
     int64_t ldy;
     int64_t rows, R_u, RB, NB, width, sums_ld, affine;      // affine: where alpha and beta begin
-    int32_t n_chunks, per_chunk, n_kb, act, w_f32;
+    int32_t n_kb, act, w_f32;
 };
 
 #ifdef __HIPCC__
@@ -105,17 +106,18 @@ typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ i32x4 as_i32x4(uint4 v) { return __builtin_bit_cast(i32x4, v); }
 
-// Where a row block's fields of a k-block lie and what they are: block `index` of its unit's, whose words are `unit`.  What does not lie
-// between the header and the image's end counts as nothing.
+// Where a row block's fields of a k-block lie and what they are.  What does not lie between the header and the image's end counts as
+// nothing, whatever the image's words say.
 struct EightBlock {
     const char* fields;
     int kind;
 };
-__device__ __forceinline__ EightBlock eight_block(const EightPlan& P, uint32_t unit, uint32_t what, uint32_t index) {
-    const uint32_t size = what >> 8, at = unit + index * size;
-    const bool fits = at >= (uint32_t)(P.header >> 8) && at < (uint32_t)(P.bytes >> 8) && size < (uint32_t)(P.bytes >> 8) - at;
-    return {fits ? P.image + ((uint64_t)at << 8) : P.image, fits ? (int)(what & 7u) : 7};
+__device__ __forceinline__ uint32_t eight_word(const EightPlan& P, uint32_t word, int S, bool w_f32) {
+    const int64_t at = (int64_t)(word >> 3) << 8;
+    const int kind = (int)(word & 7u);
+    return kind != 7 && at >= P.header && at <= P.bytes - EIGHT_PAST - eight_bytes(kind, S, w_f32) ? word : 7u;
 }
+__device__ __forceinline__ EightBlock eight_block(const EightPlan& P, uint32_t word) { return {P.image + ((uint64_t)(word >> 3) << 8), (int)(word & 7u)}; }
 
 // Operands of a step out of a lane's words.
 __device__ __forceinline__ i32x4 eight_fields4(uint2 v) {

@@ -15,7 +15,9 @@ struct Const {
 template <typename YT, int S, int WR, int WT, bool PAIR>
 __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void eight_tiles_kernel(const EightArgs Q, const uint32_t row_tiles) {
     constexpr int TOKENS = WT * 64, LOADS = 8 / WR;
-    __shared__ uint4 xt[2][TOKENS * 8];
+    constexpr int SUMS = 64;                                // k-blocks whose words are in registers, a lane each, and whose tokens' sums are in LDS
+    __shared__ uint4 xt[3][2][TOKENS * 8];
+    __shared__ int32_t st[TOKENS * (SUMS + 1)];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, sub = lane & 31, hh = lane >> 5;
     const int wr = wave % WR, wt = wave / WR;
     const bool w_f32 = Q.w_f32 != 0;
@@ -28,9 +30,8 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
 
     // a wavefront's two row blocks: neighbours, or the same of the gate and of the up; past the last one: computed for nothing, stored by nobody
     int64_t b[2], rb[2], in[2];
-    const uint2* words[2];
+    const uint32_t* words[2];
     const float* affine[2];
-    uint32_t first[2];
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
         b[f] = PAIR ? b0 : 2 * b0 + f;
@@ -38,9 +39,8 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
         rb[f] = at / Q.RB;
         in[f] = at - rb[f] * Q.RB;
         const char* const image = Q.P[PAIR ? f : 0].image;
-        words[f] = reinterpret_cast<const uint2*>(image) + rb[f] * Q.n_chunks;
-        affine[f] = reinterpret_cast<const float*>(image + Q.affine) + at * Q.n_chunks * 64;
-        first[f] = (uint32_t)(in[f] * Q.per_chunk);
+        words[f] = reinterpret_cast<const uint32_t*>(image) + at * n_kb;
+        affine[f] = reinterpret_cast<const float*>(image + Q.affine) + at * n_kb * 64 + sub;
     }
 
     // X: a row of 128 bytes a token, eight slots; slot p of token n holds slot p ^ (n / 2 & 7)
@@ -52,86 +52,99 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
         xsrc[k] = Q.codes + t * Q.width + (slot < 2 * S ? slot : 0) * 16;
     }
     const uint32_t lds_xt = lds_address(xt);
-    auto load_x = [&](int32_t kb, int buf) {
+    auto load_x = [&](int32_t pair, int stage) {            // past the last one: the last one again
 #pragma unroll
-        for (int k = 0; k < LOADS; ++k) lds_load16(lds_xt + (buf * (TOKENS * 8) + (k * WR * WT + wave) * 64) * 16, xsrc[k] + (int64_t)kb * (32 * S));
+        for (int q = 0; q < 2; ++q) {
+            const int32_t kb = 2 * pair + q < n_kb ? 2 * pair + q : n_kb - 1;
+#pragma unroll
+            for (int k = 0; k < LOADS; ++k)
+                lds_load16(lds_xt + ((stage * 2 + q) * (TOKENS * 8) + (k * WR * WT + wave) * 64) * 16, xsrc[k] + (int64_t)kb * (32 * S));
+        }
     };
-    const int32_t* sums[2];
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-        const int64_t t = t0 + wt * 64 + n * 32 + sub;
-        sums[n] = Q.sums + (t < Q.T ? t : Q.T - 1) * Q.sums_ld;
-    }
+    const uint32_t lds_st = lds_address(st);
+    auto load_sums = [&](int32_t kb) {
+#pragma unroll 1
+        for (int n = wave; n < TOKENS; n += WR * WT)
+            lds_load4(lds_st + n * (SUMS + 1) * 4, Q.sums + (t0 + n < Q.T ? t0 + n : Q.T - 1) * Q.sums_ld + (kb + lane < n_kb ? kb + lane : n_kb - 1));
+    };
 
-    // Where a k-block's fields lie: its unit's words are asked for two k-blocks ahead, its fields one.
-    struct Place {
-        int32_t j, c;
+    // The words of SUMS k-blocks, checked; those of the next ones are on their way meanwhile.
+    auto load_words = [&](int f, int32_t kb) {
+        const int32_t at = kb + lane;
+        return at < n_kb ? eight_word(Q.P[PAIR ? f : 0], words[f][at], S, w_f32) : 7u;
     };
-    auto after = [&](Place p) {                             // of the last k-block: itself
-        const bool wrap = p.c + 1 == Q.per_chunk;
-        if (wrap && p.j + 1 == Q.n_chunks) return p;
-        return Place{p.j + (wrap ? 1 : 0), wrap ? 0 : p.c + 1};
-    };
-    auto block_of = [&](int f, uint2 v, int32_t c) {
-        return eight_block(Q.P[PAIR ? f : 0], (uint32_t)__builtin_amdgcn_readfirstlane((int)v.x), (uint32_t)__builtin_amdgcn_readfirstlane((int)v.y), first[f] + (uint32_t)c);
+    auto block_of = [&](int f, uint32_t of, int32_t kb) {
+        return eight_block(Q.P[PAIR ? f : 0], (uint32_t)__builtin_amdgcn_readlane((int)of, kb & (SUMS - 1)));
     };
 
     f32x16 tot[2][2] = {};
     i32x16 acc[2][2] = {};
     EightFields<S> raw[2];
     EightBlock now[2], next[2];
-    uint2 word[2];
-    Place ahead = {0, 0};
+    uint32_t word[2], word_next[2];
     float alpha[2], alpha_next[2], behind = 0.0f;           // of the k-block; of the second row block's sums that are still to be added up
-    // beta times the tokens' sums, two k-blocks an instruction, a lane's half one of them: asked for a k-block ahead
-    float beta[2] = {};
-    int32_t sum[2] = {};
-    auto last_of_pair = [&](int32_t kb) { return (kb & 1) != 0 || kb + 1 == n_kb; };
-    auto load_pair = [&](int32_t kb) {
-        const int32_t at = (kb & ~1) + hh < n_kb ? (kb & ~1) + hh : kb, j = (int32_t)((uint32_t)at / (uint32_t)Q.per_chunk);
+    float beta[2];                                          // of a pair of k-blocks, a lane's half one of them
+    auto load_beta = [&](int32_t pair) {
+        const int32_t kb = 2 * pair + hh < n_kb ? 2 * pair + hh : n_kb - 1;
 #pragma unroll
-        for (int f = 0; f < 2; ++f) beta[f] = affine[f][j * 64 + 32 + sub];
-#pragma unroll
-        for (int n = 0; n < 2; ++n) sum[n] = sums[n][at];
+        for (int f = 0; f < 2; ++f) beta[f] = affine[f][(int64_t)kb * 64 + 32];
     };
+    const char* const xb = reinterpret_cast<const char*>(xt) + (wt * 64 + sub) * 128;
+    uint4 x[S][2];
+    auto read_x = [&](int s, int half) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n) x[s][n] = *reinterpret_cast<const uint4*>(xb + half * (TOKENS * 128) + n * 32 * 128 + (((2 * s + hh) ^ ((sub >> 1) & 7)) << 4));
+    };
+    const int32_t n_pairs = (n_kb + 1) >> 1;
+    load_x(0, 0);
+    load_sums(0);
+#pragma unroll
+    for (int f = 0; f < 2; ++f) word[f] = load_words(f, 0);
+    load_x(1, 1);
+    load_beta(0);
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
-        now[f] = block_of(f, words[f][0], 0);
+        word_next[f] = load_words(f, SUMS);
+        now[f] = block_of(f, word[f], 0);
         raw[f].load(now[f].kind, now[f].fields, lane);
-        alpha[f] = now[f].kind == 0 || now[f].kind == 7 ? 0.0f : affine[f][sub];
+        alpha[f] = affine[f][0];
     }
-    ahead = after(ahead);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
 #pragma unroll
-    for (int f = 0; f < 2; ++f) word[f] = words[f][ahead.j];
-    load_x(0, 0);
-    if (n_kb == 1) load_pair(0);
+    for (int s = 0; s < S; ++s) read_x(s, 0);
 
-    for (int32_t kb = 0; kb < n_kb; ++kb) {
-        const int buf = kb & 1;
+    // Pairs of k-blocks.  Tokens are asked for two pairs ahead, and read into registers while the k-block before is multiplied: a stage that is
+    // written to has been read by everybody a barrier ago.
+    int stage = 0;
+    for (int32_t pair = 0; pair < n_pairs; ++pair) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        const Place then = ahead;
-        ahead = after(ahead);
+        if (pair != 0 && (pair & (SUMS / 2 - 1)) == 0) {    // the next sums, this pair's among them
+            load_sums(2 * pair);
 #pragma unroll
-        for (int f = 0; f < 2; ++f) {
-            next[f] = block_of(f, word[f], then.c);
-            word[f] = words[f][ahead.j];
+            for (int f = 0; f < 2; ++f) word_next[f] = load_words(f, 2 * pair + SUMS);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
         }
-        load_x(kb + 1 < n_kb ? kb + 1 : kb, buf ^ 1);
-        const bool both = last_of_pair(kb);
+        const int stage1 = stage == 2 ? 0 : stage + 1, stage2 = stage1 == 2 ? 0 : stage1 + 1;
+        load_x(pair + 2, stage2);
         float pair_beta[2], pair_sum[2];
 #pragma unroll
-        for (int f = 0; f < 2; ++f) pair_beta[f] = (kb & ~1) + hh < n_kb ? beta[f] : 0.0f;
+        for (int f = 0; f < 2; ++f) pair_beta[f] = 2 * pair + hh < n_kb ? beta[f] : 0.0f;
 #pragma unroll
-        for (int n = 0; n < 2; ++n) pair_sum[n] = (kb & ~1) + hh < n_kb ? (float)sum[n] : 0.0f;
-        if (kb + 1 < n_kb && last_of_pair(kb + 1)) load_pair(kb + 1);
-        uint4 x[S][2];
-        const char* const xb = reinterpret_cast<const char*>(xt[buf]) + (wt * 64 + sub) * 128;
-#pragma unroll
-        for (int s = 0; s < S; ++s)
-#pragma unroll
-            for (int n = 0; n < 2; ++n) x[s][n] = *reinterpret_cast<const uint4*>(xb + n * 32 * 128 + (((2 * s + hh) ^ ((sub >> 1) & 7)) << 4));
+        for (int n = 0; n < 2; ++n) pair_sum[n] = (float)st[(wt * 64 + n * 32 + sub) * (SUMS + 1) + ((2 * pair + hh) & (SUMS - 1))];
+        load_beta(pair + 1);
 
+        auto k_block = [&](auto HALF) {
+        constexpr int half = decltype(HALF)::value;
+        const int32_t then = 2 * pair + half + 1;
+        if (half == 1 && (then & (SUMS - 1)) == 0) {
+#pragma unroll
+            for (int f = 0; f < 2; ++f) word[f] = word_next[f];
+        }
+#pragma unroll
+        for (int f = 0; f < 2; ++f) next[f] = block_of(f, word[f], then);
         auto phase = [&](auto F) {
             constexpr int f = decltype(F)::value, other = f ^ 1;
             const float fold = f == 0 ? behind : alpha[0];
@@ -148,7 +161,7 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
             raw[f].operands(kind, w);
             __builtin_amdgcn_sched_barrier(0);
             raw[f].load(next[f].kind, next[f].fields, lane);
-            alpha_next[f] = affine[f][then.j * 64 + sub];
+            alpha_next[f] = affine[f][(int64_t)(then < n_kb ? then : n_kb - 1) * 64];
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int s = 0; s < S; ++s) {
@@ -156,11 +169,12 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
                 for (int n = 0; n < 2; ++n) {
                     acc[f][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(as_i32x4(x[s][n]), w[s], s == 0 ? i32x16{} : acc[f][n], 0, 0, 0);
                     add_up((2 * s + n) * 16 / S, (2 * s + n + 1) * 16 / S - (2 * s + n) * 16 / S);
+                    if (f == 1 && n == 1) read_x(s, half == 0 ? 2 * stage + 1 : 2 * stage1);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
             asm volatile("" : "+v"(tot[other][0]), "+v"(tot[other][1]));       // here, between the matrix instructions, and not in a later block
-                            if (both) {
+                            if (half == 1) {                                // beta times the tokens' sums, two k-blocks an instruction
 #pragma unroll
                 for (int n = 0; n < 2; ++n) tot[f][n] = __builtin_amdgcn_mfma_f32_32x32x2f32(pair_sum[n], pair_beta[f], tot[f][n], 0, 0, 0);
             }
@@ -171,8 +185,12 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
         for (int f = 0; f < 2; ++f) {
             now[f] = next[f];
-            alpha[f] = now[f].kind == 0 || now[f].kind == 7 ? 0.0f : alpha_next[f];
+            alpha[f] = alpha_next[f];
         }
+        };
+        k_block(Const<0>());
+        k_block(Const<1>());
+        stage = stage1;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
@@ -183,21 +201,19 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
     // Weights that stay as they are, unit by unit, with the tokens from where they lie: few units, and none of the others waits for them.
 #pragma unroll
     for (int f = 0; f < 2; ++f)
-        for (int32_t j0 = 0; j0 < Q.n_chunks; j0 += 64) {
-            const bool valid = j0 + lane < Q.n_chunks;
-            const uint2 v = words[f][valid ? j0 + lane : j0];
-            for (uint64_t left = __ballot(valid && (v.y & 7u) == 0); left != 0; left &= left - 1) {
-                const int at = __builtin_ctzll(left);
+        for (int32_t kb0 = 0; kb0 < n_kb; kb0 += 64) {
+            const uint32_t of = load_words(f, kb0);
+            for (uint64_t left = __ballot((of & 7u) == 0u); left != 0; left &= left - 1) {
+                const int32_t kb = kb0 + __builtin_ctzll(left);
+                const EightBlock u = block_of(f, of, kb);
                 const int terms = w_f32 ? 3 : 1;
-                for (int32_t c = 0; c < Q.per_chunk; ++c) {
-                    const EightBlock u = block_of(f, make_uint2((uint32_t)__builtin_amdgcn_readlane((int)v.x, at), (uint32_t)__builtin_amdgcn_readlane((int)v.y, at)), c);
-                    if (u.kind != 0) continue;
+                {
                     const uint4* const w = reinterpret_cast<const uint4*>(u.fields) + lane;
                     uint4 x[S][2];
 #pragma unroll
                     for (int n = 0; n < 2; ++n) {
                         const int64_t t = t0 + wt * 64 + n * 32 + sub;
-                        const int8_t* const from = Q.codes + (t < Q.T ? t : Q.T - 1) * Q.width + ((int64_t)(j0 + at) * Q.per_chunk + c) * (32 * S) + hh * 16;
+                        const int8_t* const from = Q.codes + (t < Q.T ? t : Q.T - 1) * Q.width + (int64_t)kb * (32 * S) + hh * 16;
 #pragma unroll
                         for (int s = 0; s < S; ++s) x[s][n] = *reinterpret_cast<const uint4*>(from + s * 32);
                     }
