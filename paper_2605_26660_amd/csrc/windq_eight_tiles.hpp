@@ -198,41 +198,52 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
         for (int i = 0; i < 16; ++i) tot[1][n][i] = fmaf(behind, (float)acc[1][n][i], tot[1][n][i]);
 
-    // Weights that stay as they are, unit by unit, with the tokens from where they lie: few units, and none of the others waits for them.
+    // Weights that stay as they are, with the tokens from where they lie: few k-blocks, and no others wait for them.  All of a k-block's loads are
+    // asked for at once.
+    for (int32_t kb0 = 0; kb0 < n_kb; kb0 += 64) {
+        uint32_t of[2];
+        uint64_t kept[2];
 #pragma unroll
-    for (int f = 0; f < 2; ++f)
-        for (int32_t kb0 = 0; kb0 < n_kb; kb0 += 64) {
-            const uint32_t of = load_words(f, kb0);
-            for (uint64_t left = __ballot((of & 7u) == 0u); left != 0; left &= left - 1) {
-                const int32_t kb = kb0 + __builtin_ctzll(left);
-                const EightBlock u = block_of(f, of, kb);
-                const int terms = w_f32 ? 3 : 1;
-                {
-                    const uint4* const w = reinterpret_cast<const uint4*>(u.fields) + lane;
-                    uint4 x[S][2];
+        for (int f = 0; f < 2; ++f) {
+            of[f] = load_words(f, kb0);
+            kept[f] = __ballot((of[f] & 7u) == 0u);
+        }
+        for (uint64_t left = kept[0] | kept[1]; left != 0; left &= left - 1) {
+            const int at = __builtin_ctzll(left);
+            uint4 v[2][S];
 #pragma unroll
-                    for (int n = 0; n < 2; ++n) {
-                        const int64_t t = t0 + wt * 64 + n * 32 + sub;
-                        const int8_t* const from = Q.codes + (t < Q.T ? t : Q.T - 1) * Q.width + (int64_t)kb * (32 * S) + hh * 16;
+            for (int n = 0; n < 2; ++n) {
+                const int64_t t = t0 + wt * 64 + n * 32 + sub;
+                const int8_t* const from = Q.codes + (t < Q.T ? t : Q.T - 1) * Q.width + (int64_t)(kb0 + at) * (32 * S) + hh * 16;
 #pragma unroll
-                        for (int s = 0; s < S; ++s) x[s][n] = *reinterpret_cast<const uint4*>(from + s * 32);
-                    }
+                for (int s = 0; s < S; ++s) v[n][s] = *reinterpret_cast<const uint4*>(from + s * 32);
+            }
+            const int terms = w_f32 ? 3 : 1;
+#pragma unroll 1
+            for (int term = 0; term < terms; ++term) {
+                uint4 w[2][S][2] = {};
+#pragma unroll
+                for (int f = 0; f < 2; ++f) {
+                    if (((kept[f] >> at) & 1ull) == 0) continue;
+                    const uint4* const from = reinterpret_cast<const uint4*>(block_of(f, of[f], at).fields) + lane;
 #pragma unroll
                     for (int s = 0; s < S; ++s)
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            bf16x8 xb[2];
-#pragma unroll
-                            for (int n = 0; n < 2; ++n) xb[n] = half == 0 ? eight_as_bf16(x[s][n].x, x[s][n].y) : eight_as_bf16(x[s][n].z, x[s][n].w);
-                            for (int term = 0; term < terms; ++term) {
-                                const bf16x8 wv = as_bf16x8(w[((s * terms + term) * 2 + half) * 64]);
-#pragma unroll
-                                for (int n = 0; n < 2; ++n) tot[f][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xb[n], wv, tot[f][n], 0, 0, 0);
-                            }
-                        }
+                        for (int half = 0; half < 2; ++half) w[f][s][half] = from[((s * terms + term) * 2 + half) * 64];
                 }
+#pragma unroll
+                for (int s = 0; s < S; ++s)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+#pragma unroll
+                        for (int n = 0; n < 2; ++n) {
+                            const bf16x8 xv = half == 0 ? eight_as_bf16(v[n][s].x, v[n][s].y) : eight_as_bf16(v[n][s].z, v[n][s].w);
+#pragma unroll
+                            for (int f = 0; f < 2; ++f) tot[f][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xv, as_bf16x8(w[f][s][half]), tot[f][n], 0, 0, 0);
+                        }
             }
         }
+    }
 
     YT* __restrict__ const Y = static_cast<YT*>(Q.Y);
 #pragma unroll
