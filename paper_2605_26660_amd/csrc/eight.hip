@@ -135,10 +135,10 @@ __global__ __launch_bounds__(256) void serving_lay_kernel(const PackArgs P, cons
     const int a = pk_action(P, u, base);
     int kind = eight_kind(a);
     const int64_t block = eight_bytes(kind, E.S, P.w_f32 != 0), need = block * per_unit, at = image_off[u], end = image_off[u + 1];
-    if (at < E.header || (at & 255) != 0 || end > bytes || end - at < need || at > bytes - EIGHT_PAST - need) kind = 7;
+    if (at < E.header || (at & 255) != 0 || end > bytes || end - at < need || at > bytes - EIGHT_PAST - need) kind = EIGHT_NOTHING;
     const int64_t mine = (rb * E.RB + i) * E.n_kb + j * E.per_chunk + c;
     const int64_t here = at + (i * E.per_chunk + c) * block;
-    if (lane == 0) reinterpret_cast<uint32_t*>(image)[mine] = kind == 7 ? 7u : (uint32_t)(here >> 8) << 3 | (uint32_t)kind;
+    if (lane == 0) reinterpret_cast<uint32_t*>(image)[mine] = kind == EIGHT_NOTHING ? (uint32_t)kind : (uint32_t)(here >> 8) << 3 | (uint32_t)kind;
     const int64_t lrow = i * EIGHT_ROWS + sub;
     const bool in = lrow < P.R_u;
     const int64_t row = rb * P.R_u + (in ? lrow : 0);
@@ -151,14 +151,14 @@ __global__ __launch_bounds__(256) void serving_lay_kernel(const PackArgs P, cons
             alpha = 2.0f * scale;
             beta = -scale;
         }
-        if (kind == 0 || kind == 7) {
+        if (kind == 0 || kind == EIGHT_NOTHING) {
             alpha = in && kind == 0 ? 1.0f : 0.0f;
             beta = 0.0f;
         }
         float* const to = reinterpret_cast<float*>(image + E.affine) + mine * 64;
         to[hh * 32 + sub] = hh == 0 ? alpha : beta;
     }
-    if (kind == 7) return;
+    if (kind == EIGHT_NOTHING) return;
     char* const to = image + here;
     const uint8_t* const codes = P.codes + base + (in ? lrow : 0) * pk_bytes_per_group(a, P.G);
     uint32_t bits = 0;
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(WAVES * 64) void eight_kernel(const EightArgs Q, co
     for (int32_t kb = wave % EACH; kb < Q.n_kb; kb += EACH) {
         const EightBlock u = eight_block(P, eight_word(P, __builtin_amdgcn_readfirstlane((int)reinterpret_cast<const uint32_t*>(P.image)[b * Q.n_kb + kb]), S, w_f32));
         const int kind = u.kind;
-        if (kind == 7) continue;
+        if (kind == EIGHT_NOTHING) continue;
         const char* const fields = u.fields;
         uint4 xv[S][N];
 #pragma unroll

@@ -59,7 +59,8 @@ inline EightShape eight_shape(int64_t rows, int64_t cols, int64_t R_u, int32_t G
     return E;
 }
 
-// Kinds of fields: 0 weights that stay as they are, 1: 8 bits, 2: 4 bits (3 as well), 4: 2 bits (trits as well), 6: 1 bit, 7: nothing (zeros).
+// Kinds of fields: 0 weights that stay as they are, 1: 8 bits, 2: 4 bits (3 as well), 3: nothing (zeros), 4: 2 bits (trits as well), 6: 1 bit.
+constexpr int EIGHT_NOTHING = 3;
 __host__ __device__ inline int eight_kind(int action) { return action == 3 ? 2 : (action == 5 ? 4 : action); }
 
 // Bytes of a row block's fields of one k-block: a string of words a lane, step by step, in pieces of 16 bytes, [piece][lane][16], and what is left over,
@@ -115,7 +116,7 @@ struct EightBlock {
 __device__ __forceinline__ uint32_t eight_word(const EightPlan& P, uint32_t word, int S, bool w_f32) {
     const int64_t at = (int64_t)(word >> 3) << 8;
     const int kind = (int)(word & 7u);
-    return kind != 7 && at >= P.header && at <= P.bytes - EIGHT_PAST - eight_bytes(kind, S, w_f32) ? word : 7u;
+    return kind != EIGHT_NOTHING && at >= P.header && at <= P.bytes - EIGHT_PAST - eight_bytes(kind, S, w_f32) ? word : (uint32_t)EIGHT_NOTHING;
 }
 __device__ __forceinline__ EightBlock eight_block(const EightPlan& P, uint32_t word) { return {P.image + ((uint64_t)(word >> 3) << 8), (int)(word & 7u)}; }
 
@@ -128,52 +129,42 @@ __device__ __forceinline__ i32x4 eight_fields4(uint2 v) {
     f[3] = (int)((v.y >> 4) & 0x0f0f0f0fu);
     return f;
 }
-__device__ __forceinline__ i32x4 eight_fields2(uint32_t v) {
-    i32x4 f;
-    f[0] = (int)(v & 0x03030303u);
-    f[1] = (int)((v >> 2) & 0x03030303u);
-    f[2] = (int)((v >> 4) & 0x03030303u);
-    f[3] = (int)((v >> 6) & 0x03030303u);
-    return f;
-}
-__device__ __forceinline__ i32x4 eight_fields1(uint32_t v, int odd) {
-    i32x4 f;
-    f[0] = (int)((v >> (4 * odd)) & 0x01010101u);
-    f[1] = (int)((v >> (4 * odd + 1)) & 0x01010101u);
-    f[2] = (int)((v >> (4 * odd + 2)) & 0x01010101u);
-    f[3] = (int)((v >> (4 * odd + 3)) & 0x01010101u);
-    return f;
-}
-
 // A lane's string of one row block and k-block.
 template <int S>
 struct EightFields {
     uint32_t v[S][4];
     __device__ __forceinline__ void load(int kind, const char* __restrict__ fields, int lane) {
         auto piece = [&](int k, int stride) { __builtin_memcpy(v[k], fields + k * 1024 + lane * stride, 16); };
-        // the first piece whatever the kind (what holds no string reads its first bytes), so that no register waits for what comes in by another way
-        piece(0, kind == 0 || kind == 7 ? 0 : (kind == 6 ? 4 * ((S + 1) / 2) : (kind == 4 ? 4 * S : (kind == 2 && S == 1 ? 8 : 16))));
-        if constexpr (S >= 3) {
-            if (kind == 2 || kind == 1) piece(1, kind == 2 && S == 3 ? 8 : 16);
-        } else if constexpr (S == 2) {
-            if (kind == 1) piece(1, 16);
-        }
-        if constexpr (S >= 3) {
-            if (kind == 1) {
-                piece(2, 16);
-                if constexpr (S == 4) piece(3, 16);
+        // The first piece whatever the kind (what holds no string reads its first bytes), so that no register waits for what comes in by another
+        // way; a lane's stride in it by kind, a byte each.
+        constexpr uint64_t strides = 16ull << 8 | (S == 1 ? 8ull : 16ull) << 16 | (uint64_t)(4 * S) << 32 | (uint64_t)(4 * ((S + 1) / 2)) << 48;
+        piece(0, (int)(strides >> (8 * kind)) & 0xff);
+        if constexpr (S > 1) {
+            if (kind == 1 || (S > 2 && kind == 2)) {
+                piece(1, kind == 2 && S == 3 ? 8 : 16);
+                if constexpr (S > 2) {
+                    if (kind == 1) {
+                        piece(2, 16);
+                        if constexpr (S == 4) piece(3, 16);
+                    }
+                }
             }
         }
     }
     __device__ __forceinline__ uint32_t word(int k) const { return v[k >> 2][k & 3]; }
-    // The operands of all steps; zeros for what holds no string.
+    // The operands of all steps; zeros for what holds no string.  1 and 2 bits (nine weights of ten in a plan of two bits on average) by the same instructions: a branch
+    // costs more than they do.
     __device__ __forceinline__ void operands(int kind, i32x4 (&w)[S]) const {
-        if (kind == 6) {
+        if ((kind & 4) != 0) {
+            const bool one = kind == 6;
+            const uint32_t mask = one ? 0x01010101u : 0x03030303u;
+            const int by = one ? 1 : 2;
 #pragma unroll
-            for (int s = 0; s < S; ++s) w[s] = eight_fields1(word(s >> 1), s & 1);
-        } else if (kind == 4) {
+            for (int s = 0; s < S; ++s) {
+                const uint32_t f = one ? word(s >> 1) >> (4 * (s & 1)) : word(s);
 #pragma unroll
-            for (int s = 0; s < S; ++s) w[s] = eight_fields2(word(s));
+                for (int i = 0; i < 4; ++i) w[s][i] = (int)((f >> (i * by)) & mask);
+            }
         } else if (kind == 2) {
 #pragma unroll
             for (int s = 0; s < S; ++s) w[s] = eight_fields4(make_uint2(word(2 * s), word(2 * s + 1)));

@@ -12,6 +12,14 @@ struct Const {
     static constexpr int value = V;
 };
 
+// All loads done, direct ones among them.  As a builtin: the compiler then knows it of its own loads and waits for none of them again, which would wait for
+// direct loads that it does not count.
+__device__ __forceinline__ void wait_for_loads() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    asm volatile("" ::: "memory");
+}
+
 template <typename YT, int S, int WR, int WT, bool PAIR>
 __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void eight_tiles_kernel(const EightArgs Q, const uint32_t row_tiles) {
     constexpr int TOKENS = WT * 64, LOADS = 8 / WR;
@@ -71,7 +79,7 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
     // The words of SUMS k-blocks, checked; those of the next ones are on their way meanwhile.
     auto load_words = [&](int f, int32_t kb) {
         const int32_t at = kb + lane;
-        return at < n_kb ? eight_word(Q.P[PAIR ? f : 0], words[f][at], S, w_f32) : 7u;
+        return at < n_kb ? eight_word(Q.P[PAIR ? f : 0], words[f][at], S, w_f32) : (uint32_t)EIGHT_NOTHING;
     };
     auto block_of = [&](int f, uint32_t of, int32_t kb) {
         return eight_block(Q.P[PAIR ? f : 0], (uint32_t)__builtin_amdgcn_readlane((int)of, kb & (SUMS - 1)));
@@ -109,7 +117,7 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
         raw[f].load(now[f].kind, now[f].fields, lane);
         alpha[f] = affine[f][0];
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    wait_for_loads();
     __syncthreads();
 #pragma unroll
     for (int s = 0; s < S; ++s) read_x(s, 0);
@@ -118,13 +126,13 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
     // written to has been read by everybody a barrier ago.
     int stage = 0;
     for (int32_t pair = 0; pair < n_pairs; ++pair) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        wait_for_loads();
         __syncthreads();
         if (pair != 0 && (pair & (SUMS / 2 - 1)) == 0) {    // the next sums, this pair's among them
             load_sums(2 * pair);
 #pragma unroll
             for (int f = 0; f < 2; ++f) word_next[f] = load_words(f, 2 * pair + SUMS);
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            wait_for_loads();
             __syncthreads();
         }
         const int stage1 = stage == 2 ? 0 : stage + 1, stage2 = stage1 == 2 ? 0 : stage1 + 1;
@@ -192,7 +200,7 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
         k_block(Const<1>());
         stage = stage1;
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    wait_for_loads();
 #pragma unroll
     for (int n = 0; n < 2; ++n)
 #pragma unroll
@@ -245,28 +253,46 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
         }
     }
 
-    YT* __restrict__ const Y = static_cast<YT*>(Q.Y);
+    float scale[2][16];
 #pragma unroll
     for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
+        for (int i = 0; i < 16; ++i) {
+            const int64_t t = t0 + wt * 64 + n * 32 + (i >> 2) * 8 + hh * 4 + (i & 3);
+            scale[n][i] = Q.scale[t < Q.T ? t : Q.T - 1];
+        }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t t = t0 + wt * 64 + n * 32 + g * 8 + hh * 4 + i;
-                if (t >= Q.T) continue;
-                const float scale = Q.scale[t];
+    for (int n = 0; n < 2; ++n)
 #pragma unroll
-                for (int f = 0; f < (PAIR ? 1 : 2); ++f) {
-                    const int64_t lrow = in[f] * EIGHT_ROWS + sub;
-                    if (b[f] >= Q.NB || lrow >= Q.R_u) continue;
-                    float v = tot[f][n][g * 4 + i] * scale;
-                    if constexpr (PAIR) {
-                        float none;
-                        v = activation<false>(Q.act, v, none) * (tot[1][n][g * 4 + i] * scale);
-                    }
-                    eight_store(Y + t * Q.ldy + rb[f] * Q.R_u + lrow, v);
-                }
+        for (int i = 0; i < 16; ++i) {
+            tot[0][n][i] *= scale[n][i];
+            tot[1][n][i] *= scale[n][i];
+            if constexpr (PAIR) {
+                float none;
+                tot[0][n][i] = activation<false>(Q.act, tot[0][n][i], none) * tot[1][n][i];
             }
+        }
+#pragma unroll
+    for (int f = 0; f < (PAIR ? 1 : 2); ++f) {
+        const int64_t lrow = in[f] * EIGHT_ROWS + sub;
+        if (b[f] >= Q.NB || lrow >= Q.R_u) continue;
+        const int64_t t1 = t0 + wt * 64 + hh * 4;
+        YT* __restrict__ const y = static_cast<YT*>(Q.Y) + t1 * Q.ldy + rb[f] * Q.R_u + lrow;
+        if (t0 + TOKENS <= Q.T) {
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) eight_store(y + (n * 32 + (i >> 2) * 8 + (i & 3)) * Q.ldy, tot[f][n][i]);
+        } else {
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int at = n * 32 + (i >> 2) * 8 + (i & 3);
+                    if (t1 + at < Q.T) eight_store(y + at * Q.ldy, tot[f][n][i]);
+                }
+        }
+    }
 }
 
 #endif  // __HIPCC__
