@@ -210,13 +210,18 @@ __global__ __launch_bounds__(256) void serving_lay_kernel(const PackArgs P, cons
 }
 
 // ------------------------------------------------------------------------------------------------ the product
+constexpr int64_t EIGHT_FEW = 128;
+
 // A row block and 32 N tokens a workgroup; its wavefronts share the k-blocks (of a pair: half of them the gate's, the others the up's) and
-// add up through LDS.  Fields and tokens go straight to the registers that the matrix instructions read.
+// add up through LDS.  Bound by latency: everything that a k-block needs is asked for at once, and the next one's fields before this one is multiplied.
+// Tokens are the M side of the matrix instructions and rows the N side, so that a lane has one row, with one alpha and one beta; beta times the tokens' sums
+// is an instruction of its own, with nothing in its other half.
 template <typename YT, int S, int N, int WAVES, bool PAIR>
 __global__ __launch_bounds__(WAVES * 64) void eight_kernel(const EightArgs Q, const int64_t first) {
     constexpr int EACH = PAIR ? WAVES / 2 : WAVES;
     __shared__ float red[WAVES][N * 16][64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, sub = lane & 31, hh = lane >> 5;
+    const int turn = wave % EACH;
     const EightPlan& P = Q.P[PAIR ? wave / EACH : 0];
     const int64_t id = first + blockIdx.x, tb = id / Q.NB, b = id - tb * Q.NB, t0 = tb * (N * 32);
     const int64_t rb = b / Q.RB, i = b - rb * Q.RB;
@@ -230,62 +235,64 @@ __global__ __launch_bounds__(WAVES * 64) void eight_kernel(const EightArgs Q, co
         x[n] = Q.codes + t * Q.width + hh * 16;
         xs[n] = Q.sums + t * Q.sums_ld;
     }
-    const float* const affine = reinterpret_cast<const float*>(P.image + Q.affine) + b * Q.n_kb * 64 + hh * 4;
+    const uint32_t* const words = reinterpret_cast<const uint32_t*>(P.image) + b * Q.n_kb;
+    const float* const affine = reinterpret_cast<const float*>(P.image + Q.affine) + b * Q.n_kb * 64 + sub;
     f32x16 tot[N] = {};
-    for (int32_t kb = wave % EACH; kb < Q.n_kb; kb += EACH) {
-        const EightBlock u = eight_block(P, eight_word(P, __builtin_amdgcn_readfirstlane((int)reinterpret_cast<const uint32_t*>(P.image)[b * Q.n_kb + kb]), S, w_f32));
-        const int kind = u.kind;
-        if (kind == EIGHT_NOTHING) continue;
-        const char* const fields = u.fields;
-        uint4 xv[S][N];
-#pragma unroll
-        for (int s = 0; s < S; ++s)
-#pragma unroll
-            for (int n = 0; n < N; ++n) xv[s][n] = *reinterpret_cast<const uint4*>(x[n] + (int64_t)kb * (32 * S) + s * 32);
-        if (kind == 0) {
-            const int terms = w_f32 ? 3 : 1;
-            const uint4* const w = reinterpret_cast<const uint4*>(fields) + lane;
+    for (int32_t from = turn; from < Q.n_kb; from += 64 * EACH) {
+        // the words of the wavefront's next 64 k-blocks, a lane each
+        const int32_t mine = from + lane * EACH;
+        const uint32_t of = mine < Q.n_kb ? eight_word(P, words[mine], S, w_f32) : (uint32_t)EIGHT_NOTHING;
+        const int32_t count = (Q.n_kb - from + EACH - 1) / EACH < 64 ? (Q.n_kb - from + EACH - 1) / EACH : 64;
+        EightBlock u = eight_block(P, (uint32_t)__builtin_amdgcn_readlane((int)of, 0));
+        EightFields<S> raw;
+        raw.load(u.kind, u.fields, lane);
+        for (int32_t it = 0; it < count; ++it) {
+            const int32_t kb = from + it * EACH;
+            const int kind = u.kind;
+            uint4 xv[S][N];
 #pragma unroll
             for (int s = 0; s < S; ++s)
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    bf16x8 xb[N];
+                for (int n = 0; n < N; ++n) xv[s][n] = *reinterpret_cast<const uint4*>(x[n] + (int64_t)kb * (32 * S) + s * 32);
+            const float alpha = affine[(int64_t)kb * 64], beta = affine[(int64_t)kb * 64 + 32];
+            int32_t sum[N];
 #pragma unroll
-                    for (int n = 0; n < N; ++n) xb[n] = half == 0 ? eight_as_bf16(xv[s][n].x, xv[s][n].y) : eight_as_bf16(xv[s][n].z, xv[s][n].w);
-                    for (int term = 0; term < terms; ++term) {
-                        const bf16x8 wv = as_bf16x8(w[((s * terms + term) * 2 + half) * 64]);
+            for (int n = 0; n < N; ++n) sum[n] = xs[n][kb];
+            i32x4 w[S];
+            raw.operands(kind, w);
+            const EightBlock here = u;
+            u = eight_block(P, (uint32_t)__builtin_amdgcn_readlane((int)of, it + 1 < count ? it + 1 : it));
+            raw.load(u.kind, u.fields, lane);
+            if (kind == 0) {
+                const int terms = w_f32 ? 3 : 1;
+                const uint4* const weights = reinterpret_cast<const uint4*>(here.fields) + lane;
+                for (int term = 0; term < terms; ++term) {
+                    uint4 v[S][2];
 #pragma unroll
-                        for (int n = 0; n < N; ++n) tot[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wv, xb[n], tot[n], 0, 0, 0);
-                    }
+                    for (int s = 0; s < S; ++s)
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) v[s][half] = weights[((s * terms + term) * 2 + half) * 64];
+#pragma unroll
+                    for (int s = 0; s < S; ++s)
+#pragma unroll
+                        for (int n = 0; n < N; ++n) {
+                            tot[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_as_bf16(xv[s][n].x, xv[s][n].y), as_bf16x8(v[s][0]), tot[n], 0, 0, 0);
+                            tot[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight_as_bf16(xv[s][n].z, xv[s][n].w), as_bf16x8(v[s][1]), tot[n], 0, 0, 0);
+                        }
                 }
-            continue;
-        }
-        float4 al[4], be[4];
+                continue;
+            }
+            i32x16 acc[N];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            al[g] = *reinterpret_cast<const float4*>(affine + kb * 64 + g * 8);
-            be[g] = *reinterpret_cast<const float4*>(affine + kb * 64 + 32 + g * 8);
-        }
-        float sum[N];
+            for (int s = 0; s < S; ++s)
 #pragma unroll
-        for (int n = 0; n < N; ++n) sum[n] = (float)xs[n][kb];
-        i32x16 acc[N] = {};
-        EightFields<S> raw;
-        raw.load(kind, fields, lane);
-        i32x4 w[S];
-        raw.operands(kind, w);
+                for (int n = 0; n < N; ++n) acc[n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(as_i32x4(xv[s][n]), w[s], s == 0 ? i32x16{} : acc[n], 0, 0, 0);
 #pragma unroll
-        for (int s = 0; s < S; ++s)
+            for (int n = 0; n < N; ++n) tot[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(hh == 0 ? (float)sum[n] : 0.0f, beta, tot[n], 0, 0, 0);
 #pragma unroll
-            for (int n = 0; n < N; ++n) acc[n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[s], as_i32x4(xv[s][n]), acc[n], 0, 0, 0);
+            for (int n = 0; n < N; ++n)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const float av[4] = {al[g].x, al[g].y, al[g].z, al[g].w}, bv[4] = {be[g].x, be[g].y, be[g].z, be[g].w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int n = 0; n < N; ++n)
-                    tot[n][g * 4 + k] = fmaf(av[k], (float)acc[n][g * 4 + k], fmaf(bv[k], sum[n], tot[n][g * 4 + k]));
+                for (int k = 0; k < 16; ++k) tot[n][k] = fmaf(alpha, (float)acc[n][k], tot[n][k]);
         }
     }
 #pragma unroll
@@ -298,7 +305,7 @@ __global__ __launch_bounds__(WAVES * 64) void eight_kernel(const EightArgs Q, co
         const int r = e & 31, n = e >> 5;                  // neighbouring lanes: neighbouring rows of a token
         const int64_t t = t0 + n;
         if (r >= rows_left || t >= Q.T) continue;
-        const int slot = (n >> 5) * 16 + (r >> 3) * 4 + (r & 3), at = ((r >> 2) & 1) * 32 + (n & 31);
+        const int slot = (n >> 5) * 16 + ((n >> 3) & 3) * 4 + (n & 3), at = ((n >> 2) & 1) * 32 + r;
         float v = 0.0f, up = 0.0f;
 #pragma unroll
         for (int w = 0; w < EACH; ++w) v += red[w][slot][at];
@@ -316,16 +323,19 @@ __global__ __launch_bounds__(WAVES * 64) void eight_kernel(const EightArgs Q, co
 
 template <typename YT, int S, bool PAIR>
 int launch_eight(const EightArgs& Q, hipStream_t st) {
-    constexpr int WAVES = 8;
-    if (Q.T <= 32) return launch_pieces(Q.NB, WAVES * 64, [&](int64_t first, dim3 g) { eight_kernel<YT, S, 1, WAVES, PAIR><<<g, dim3(WAVES * 64), 0, st>>>(Q, first); });
-    if (Q.T > 128) {
-        constexpr int WR = 4, WT = 2;
+    if (Q.T <= 32) {
+        constexpr int WAVES = 16;
+        return launch_pieces(Q.NB, WAVES * 64, [&](int64_t first, dim3 g) { eight_kernel<YT, S, 1, WAVES, PAIR><<<g, dim3(WAVES * 64), 0, st>>>(Q, first); });
+    }
+    if (Q.T > EIGHT_FEW) {
+        constexpr int WR = 4, WT = 1;
         const int64_t row_tiles = tokens_in(Q.NB, PAIR ? WR : 2 * WR), tiles = row_tiles * tokens_in(Q.T, WT * 64);
         if (fits_launch(tiles, WR * WT * 64)) {
             eight_tiles_kernel<YT, S, WR, WT, PAIR><<<dim3((uint32_t)tiles), dim3(WR * WT * 64), 0, st>>>(Q, (uint32_t)row_tiles);
             return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
         }
     }
+    constexpr int WAVES = 8;
     return launch_pieces(Q.NB * tokens_in(Q.T, 64), WAVES * 64, [&](int64_t first, dim3 g) { eight_kernel<YT, S, 2, WAVES, PAIR><<<g, dim3(WAVES * 64), 0, st>>>(Q, first); });
 }
 
