@@ -8,8 +8,9 @@ namespace windq {
 int check_tokens(const windq_mat* M, int64_t width, bool vector);
 
 // ------------------------------------------------------------------------------------------------ tokens
-// A workgroup a token.  Its largest magnitude first, as bits: a NaN's are above an infinity's, and those above every number's.  Octets of the padded
-// width go to neighbouring threads; a k-block's sum is collected in LDS by integer additions, whose order does not matter.
+// A workgroup a token, its octets (of the padded width) to neighbouring threads, read once where a thread has PER of them at most: they stay in registers
+// between the pass for the largest magnitude and the one that rounds.  Magnitudes are compared as bits: a NaN's are above an infinity's, and those above
+// every number's.  A k-block's sum is formed by the lanes that have it where they are 4, 8 or 16 together, else by integer additions in LDS, whose order does not matter.
 constexpr int TOKENS_SUMS = 4096;                          // k-blocks whose sums fit
 
 struct TokensArgs {
@@ -24,35 +25,67 @@ struct TokensArgs {
     int32_t n_kb;
 };
 
-template <typename XT>
-__device__ __forceinline__ bool tokens_octet(const TokensArgs& Q, const XT* __restrict__ x, int64_t o, float (&v)[8]) {
-    const int64_t j = (int64_t)((uint64_t)o / (uint32_t)Q.octets_chunk);
-    const int32_t in = (int32_t)(o - j * Q.octets_chunk);
-    if (in * 8 >= Q.G) return false;
-    load8(x + j * Q.G + in * 8, v);
-    return true;
-}
-
-template <typename XT>
+template <typename XT, int PER>                            // 0: any number of octets a thread, read twice
 __global__ __launch_bounds__(256) void tokens8_kernel(const TokensArgs Q, const int64_t first) {
+    constexpr bool F32 = sizeof(XT) == 4;
     __shared__ uint32_t most[4];
     __shared__ int32_t sums[TOKENS_SUMS];
     const int64_t t = first + blockIdx.x;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const XT* __restrict__ const x = static_cast<const XT*>(Q.X) + t * Q.ld;
-    const bool own_sums = Q.n_kb <= TOKENS_SUMS;
-    if (own_sums)
+    const bool natural = Q.octets_chunk * 8 == Q.G, whole = Q.octets_kb != 12, own_sums = Q.n_kb <= TOKENS_SUMS;
+    if (own_sums && !whole) {
         for (int32_t k = threadIdx.x; k < Q.n_kb; k += 256) sums[k] = 0;
-    uint32_t m = 0;
-    for (int64_t o = threadIdx.x; o < Q.octets; o += 256) {
-        float v[8];
-        if (!tokens_octet(Q, x, o, v)) continue;
+        __syncthreads();
+    }
+    auto load = [&](int64_t o, uint4 (&v)[F32 ? 2 : 1]) {   // zeros past the end and in the padding
+        int64_t at = o * 8;
+        bool in = o < Q.octets;
+        if (!natural) {
+            const int64_t j = (int64_t)((uint64_t)o / (uint32_t)Q.octets_chunk);
+            const int32_t c = (int32_t)(o - j * Q.octets_chunk) * 8;
+            in = in && c < Q.G;
+            at = j * Q.G + c;
+        }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
-            m = b > m ? b : m;
+        for (int k = 0; k < (F32 ? 2 : 1); ++k) v[k] = in ? reinterpret_cast<const uint4*>(x + at)[k] : make_uint4(0u, 0u, 0u, 0u);
+    };
+    auto value = [&](const uint4 (&v)[F32 ? 2 : 1], int i) {
+        const uint4 w = v[F32 ? i >> 2 : 0];
+        const int k = F32 ? i & 3 : i >> 1;
+        const uint32_t b = k == 0 ? w.x : (k == 1 ? w.y : (k == 2 ? w.z : w.w));
+        return F32 ? b : ((i & 1) != 0 ? b & 0xffff0000u : b << 16);
+    };
+    uint32_t m = 0;                                         // of bfloat16 a pair of them
+    auto largest = [&](const uint4 (&v)[F32 ? 2 : 1]) {
+#pragma unroll
+        for (int k = 0; k < (F32 ? 2 : 1); ++k) {
+            const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (F32) {
+                    const uint32_t b = w[i] & 0x7fffffffu;
+                    m = b > m ? b : m;
+                } else {
+                    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+                    m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m), __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu)));
+                }
+            }
+        }
+    };
+    uint4 held[PER > 0 ? PER : 1][F32 ? 2 : 1];
+    if constexpr (PER > 0) {
+#pragma unroll
+        for (int k = 0; k < PER; ++k) load(k * 256 + threadIdx.x, held[k]);
+#pragma unroll
+        for (int k = 0; k < PER; ++k) largest(held[k]);
+    } else {
+        for (int64_t o = threadIdx.x; o < Q.octets; o += 256) {
+            load(o, held[0]);
+            largest(held[0]);
         }
     }
+    if constexpr (!F32) m = m << 16 > (m & 0xffff0000u) ? m << 16 : m & 0xffff0000u;
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) {
         const uint32_t b = (uint32_t)__shfl_xor((int)m, d, 64);
@@ -68,25 +101,61 @@ __global__ __launch_bounds__(256) void tokens8_kernel(const TokensArgs Q, const 
     const float inverse = finite && sigma > 0.0f ? 1.0f / sigma : 0.0f;
     if (threadIdx.x == 0) Q.scale[t] = finite ? sigma : __uint_as_float(0x7fc00000u);
     uint2* __restrict__ const to = reinterpret_cast<uint2*>(Q.codes + t * Q.octets * 8);
-    for (int64_t o = threadIdx.x; o < Q.octets; o += 256) {
-        float v[8];
-        uint32_t w[2] = {0u, 0u};
-        if (tokens_octet(Q, x, o, v)) {
-            int32_t sum = 0;
+    // x / sigma is at most 127 (1 + 2^-22): no clamp.  1.5 2^23 added, the sum's last bits are the integer, ties to even.
+    auto round = [&](int64_t o, const uint4 (&v)[F32 ? 2 : 1]) {
+        uint32_t w[2];
+        int32_t sum = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float r = fminf(fmaxf(rintf(v[i] * inverse), -127.0f), 127.0f);
-                const int32_t q = finite ? (int32_t)r : 0;
-                sum += q;
-                w[i >> 2] |= ((uint32_t)q & 0xffu) << (8 * (i & 3));
+        for (int h = 0; h < 2; ++h) {
+            uint32_t q[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float y = __uint_as_float(value(v, h * 4 + i)) * inverse;
+                q[i] = __float_as_uint(y + 12582912.0f);
             }
-            if (own_sums && sum != 0) atomicAdd(&sums[(uint32_t)o / (uint32_t)Q.octets_kb], sum);
+            const uint32_t lo = __builtin_amdgcn_perm(q[1], q[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(q[3], q[2], 0x04000c0cu);
+            w[h] = finite ? lo | hi : 0u;
+            sum = __builtin_amdgcn_sdot4((int)w[h], 0x01010101, sum, false);
         }
-        to[o] = make_uint2(w[0], w[1]);
+        if (o < Q.octets) to[o] = make_uint2(w[0], w[1]);
+        if (!own_sums) return;
+        if (whole) {
+            for (int d = 1; d < Q.octets_kb; d <<= 1) sum += __shfl_xor(sum, d, 64);
+            if (o < Q.octets && (o & (Q.octets_kb - 1)) == 0) Q.sums[t * Q.sums_ld + o / Q.octets_kb] = sum;
+        } else if (o < Q.octets && sum != 0) {
+            atomicAdd(&sums[(uint32_t)o / (uint32_t)Q.octets_kb], sum);
+        }
+    };
+    if constexpr (PER > 0) {
+#pragma unroll
+        for (int k = 0; k < PER; ++k) round(k * 256 + threadIdx.x, held[k]);
+    } else {
+        for (int64_t o0 = 0; o0 < Q.octets; o0 += 256) {    // all lanes: they sum up together
+            load(o0 + threadIdx.x, held[0]);
+            round(o0 + threadIdx.x, held[0]);
+        }
     }
     if (!own_sums) return;
+    if (whole) {
+        if (threadIdx.x < Q.sums_ld - Q.n_kb) Q.sums[t * Q.sums_ld + Q.n_kb + threadIdx.x] = 0;
+        return;
+    }
     __syncthreads();
     for (int64_t k = threadIdx.x; k < Q.sums_ld; k += 256) Q.sums[t * Q.sums_ld + k] = k < Q.n_kb ? sums[k] : 0;
+}
+
+template <typename XT>
+int launch_tokens8(const TokensArgs& Q, hipStream_t st) {
+    const int64_t each = tokens_in(Q.octets, 256);
+    return launch_pieces(Q.T, 256, [&](int64_t first, dim3 g) {
+        if (each <= 1) tokens8_kernel<XT, 1><<<g, dim3(256), 0, st>>>(Q, first);
+        else if (each <= 2) tokens8_kernel<XT, 2><<<g, dim3(256), 0, st>>>(Q, first);
+        else if (each <= 3) tokens8_kernel<XT, 3><<<g, dim3(256), 0, st>>>(Q, first);
+        else if (each <= 4) tokens8_kernel<XT, 4><<<g, dim3(256), 0, st>>>(Q, first);
+        else if (each <= 6) tokens8_kernel<XT, 6><<<g, dim3(256), 0, st>>>(Q, first);
+        else if (each <= 8) tokens8_kernel<XT, 8><<<g, dim3(256), 0, st>>>(Q, first);
+        else tokens8_kernel<XT, 0><<<g, dim3(256), 0, st>>>(Q, first);
+    });
 }
 
 // Sums of tokens of more k-blocks than fit LDS, a thread a sum, from the codes.
@@ -423,10 +492,7 @@ extern "C" int windq_tokens8(const windq_mat* X, int32_t chunk_w, int8_t* codes,
     if (!aligned(codes, 16) || !aligned(scale, 4) || !aligned(sums, 16)) return WINDQ_EINVAL;
     const TokensArgs Q = {X->data, X->ld, X->rows, codes, scale, sums, chunk_w, E.per_chunk * E.S * 4, E.S * 4, E.width / 8, E.sums_ld, E.n_kb};
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const int launched = launch_pieces(X->rows, 256, [&](int64_t first, dim3 g) {
-        if (X->dtype == WINDQ_F32) tokens8_kernel<float><<<g, dim3(256), 0, st>>>(Q, first);
-        else tokens8_kernel<uint16_t><<<g, dim3(256), 0, st>>>(Q, first);
-    });
+    const int launched = X->dtype == WINDQ_F32 ? launch_tokens8<float>(Q, st) : launch_tokens8<uint16_t>(Q, st);
     if (launched != WINDQ_OK || E.n_kb <= TOKENS_SUMS) return launched;
     return launch_pieces(tokens_in(X->rows * E.sums_ld, 256), 256, [&](int64_t first, dim3 g) { tokens8_sums_kernel<<<g, dim3(256), 0, st>>>(Q, first); });
 }

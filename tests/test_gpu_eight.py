@@ -78,7 +78,7 @@ SHAPES = [(64, 128, 64, 0, 1), (200, 480, 96, 40, 5), (72, 80, 8, 0, 33), (1000,
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("T,cols,G", [(1, 8, 8), (3, 80, 8), (5, 1056, 96), (2, 4096, 128), (9, 11008, 128), (4, 72, 72), (2, 800, 160), (1, 512, 512), (300, 64, 64),
-                                      (2, 33024, 8), (1, 131072, 64)])
+                                      (2, 33024, 8), (1, 131072, 64), (3, 2080, 160), (4, 5120, 256), (2, 14400, 96)])
 def test_tokens8_is_the_definition_bit_for_bit(windq, dtype, T, cols, G):
     x = tokens(T, cols, dtype, 3)
     x[:, ::7] *= 6
