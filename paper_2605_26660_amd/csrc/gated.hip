@@ -8,9 +8,17 @@
 
 namespace windq {
 
+// Many bfloat16 tokens: the matrices are reconstructed in half precision, once a call, and multiplied by a plain product (windq_gemm.hpp).  Both factors have 11 bits of
+// significand, and powers of two for a token and for eight rows that bring them below 2^15, so that what lies 2^28 below the largest of them still has all of its
+// digits: the weights' rounding (tokens have none: bfloat16's eight bits fit) is eight times as fine as G's and U's own.
+constexpr int64_t GATED_MANY = 320;
+
 struct GatedWs {
-    size_t planes, frag, few_xs, fields[2], unit[2], xs, beta[2], alpha[2], total;
+    size_t planes, frag, few_xs, fields[2], unit[2], xs, beta[2], alpha[2], w, x, by_token, by_octet, total;
 };
+
+// Rows of both matrices, 32 and 32 in turn, filled up to whole tiles.
+inline int64_t gated_rows(int64_t rows) { return ((rows + 31) / 32 * 64 + GM_MOST - 1) / GM_MOST * GM_MOST; }
 
 GatedWs gated_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t G) {
     GatedWs w;
@@ -33,8 +41,109 @@ GatedWs gated_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t G
         w.beta[m] = take(many ? (size_t)(cols / 64) * (size_t)rows * 16 : 0);
         w.alpha[m] = take(many ? (size_t)(cols / G) * (size_t)rows * 4 : 0);
     }
+    const bool halves = few && T > GATED_MANY;
+    w.w = take(halves ? (size_t)gated_rows(rows) * (size_t)gemm_k(cols) * 2 : 0);
+    w.x = take(halves ? (size_t)T * (size_t)gemm_k(cols) * 2 : 0);
+    w.by_token = take(halves ? (size_t)T * 4 : 0);
+    w.by_octet = take(halves ? (size_t)gated_rows(rows) / 8 * 4 : 0);
     w.total = at == 0 ? 256 : at;
     return w;
+}
+
+struct HalvesArgs {
+    PackArgs P[2];
+    const uint16_t* X;
+    int64_t ldx, T, K;
+    uint16_t* x;               // [T][K]
+    float* by_token;
+    uint16_t* w;               // [rows of both in turn, 32 and 32][K]
+    float* by_octet;
+};
+
+// Workgroups [0, T): a token; the others: eight rows of a matrix.
+__global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, const int64_t first) {
+    __shared__ float most[4];
+    __shared__ uint16_t trits_of[256];
+    const int64_t id = first + blockIdx.x;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    auto of_all = [&](float m) {
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+        if (lane == 0) most[wave] = m;
+        __syncthreads();
+        return power_below(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
+    };
+    if (id < Q.T) {
+        const uint16_t* __restrict__ const x = Q.X + id * Q.ldx;
+        float m = 0.0f;
+        for (int64_t c = threadIdx.x * 8; c < Q.P[0].cols; c += 2048) {
+            float v[8];
+            load8(x + c, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = finite_max(m, v[i]);
+        }
+        const float by = of_all(m);
+        if (threadIdx.x == 0) Q.by_token[id] = 1.0f / by;
+        for (int64_t c = threadIdx.x * 8; c < Q.K; c += 2048) {
+            float v[8] = {};
+            if (c < Q.P[0].cols) load8(x + c, v);
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = half_bits<_Float16>(v[i] * by);
+            *reinterpret_cast<uint4*>(Q.x + id * Q.K + c) = pack8(w);
+        }
+        return;
+    }
+    trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);      // there by the barrier in of_all
+    const int64_t octets = Q.P[0].rows / 8, block = id - Q.T;
+    const int mat = block >= octets ? 1 : 0;
+    const PackArgs& P = Q.P[mat];
+    const int64_t r0 = (block - mat * octets) * 8, at = (r0 >> 5) * 64 + mat * 32 + (r0 & 31);
+    float m = 0.0f;
+    for (int64_t k = threadIdx.x; k < (int64_t)P.n_chunks * 8; k += 256) m = group_max(P, r0 + (k & 7), k >> 3, m);
+    const float by = of_all(m);
+    if (threadIdx.x == 0) Q.by_octet[at >> 3] = 1.0f / by;
+    for (int64_t c = threadIdx.x * 8; c < Q.K; c += 2048) {
+        uint32_t w[8][4] = {};
+        if (c < P.cols)
+            eight_rows(P, r0, c, trits_of, [&](int i, int k, float v) {
+                const uint32_t b = half_bits<_Float16>(v * by);
+                w[i][k >> 1] = (k & 1) != 0 ? w[i][k >> 1] | b << 16 : b;
+            });
+#pragma unroll
+        for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(Q.w + (at + i) * Q.K + c) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+    }
+}
+
+int launch_gated_halves(const ProjectArgs& Q, char* ws, const GatedWs& at, hipStream_t st) {
+    const int64_t K = gemm_k(Q.P.cols), rows = gated_rows(Q.P.rows), tall = tokens_in(Q.T, GM_N);
+    const HalvesArgs H = {{Q.P, Q.pair.up}, Q.X, Q.ldx, Q.T, K, reinterpret_cast<uint16_t*>(ws + at.x), reinterpret_cast<float*>(ws + at.by_token),
+                          reinterpret_cast<uint16_t*>(ws + at.w), reinterpret_cast<float*>(ws + at.by_octet)};
+    const int status = launch_pieces(Q.T + Q.P.rows / 4, 256, [&](int64_t first, dim3 g) { gated_halves_kernel<<<g, dim3(256), 0, st>>>(H, first); });
+    if (status != WINDQ_OK) return status;
+    const int64_t by = rows / 256 * tall >= GM_TILES ? 256 : 128, tiles = rows / by * tall;
+    GemmArgs M = {};
+    M.wt = H.w;
+    M.dY = H.x;
+    M.ldy = K;
+    M.K = (int32_t)K;
+    M.T = Q.T;
+    M.cols = rows;
+    M.dX = static_cast<uint16_t*>(Q.Y);
+    M.ldx = Q.ldy;
+    M.col_blocks = (uint32_t)(rows / by);
+    M.tiles = (int32_t)tiles;
+    M.each = (int32_t)(K / GM_K);
+    M.by_token = H.by_token;
+    M.by_octet = H.by_octet;
+    M.gate = Q.P;
+    M.pair = Q.pair;
+    M.raw = Q.X;
+    M.ld_raw = Q.ldx;
+    // tiles are no more than 2^31 / (64 x 128) and two sides' edges: one launch holds them
+    if (by == 256) dx_gemm_kernel<4, true, true><<<dim3((uint32_t)tiles), dim3(GM_THREADS), 0, st>>>(M);
+    else dx_gemm_kernel<2, true, true><<<dim3((uint32_t)tiles), dim3(GM_THREADS), 0, st>>>(M);
+    return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
 }
 
 template <typename XT, int S>
@@ -93,6 +202,9 @@ int gated_all(ProjectArgs& Q, const windq_mat* X, char* ws, const GatedWs& at, h
             F.n_kb = (int32_t)(Q.P.cols / (16 * steps));
             return steps == 8 ? launch_few<8, true>(F, nullptr, st) : (steps == 6 ? launch_few<6, true>(F, nullptr, st) : launch_few<4, true>(F, nullptr, st));
         }
+    }
+    if constexpr (sizeof(XT) == 2) {
+        if (T > GATED_MANY && Q.P.rows % 8 == 0) return launch_gated_halves(Q, ws, at, st);
     }
     const bool mask = Q.P.mask != nullptr || Q.pair.up.mask != nullptr;
     const int64_t general = (Q.P.rows + 15) / 16 * tokens_in(T, 64);
@@ -171,14 +283,6 @@ __device__ __forceinline__ void store_octet(XT* __restrict__ p, int64_t left, bo
         if (i < left) store_y(p + i, v[i]);
 }
 
-// The power of two that brings magnitudes up to `most` below 2^15 (1 where there are none), itself within fp32's normal numbers.
-__device__ __forceinline__ float power_below(float most) {
-    const int e = (int)(__float_as_uint(most) >> 23);       // biased; most < 2^(e - 126)
-    const int by = most > 0.0f ? 127 + 14 - (e - 127) : 127;
-    return __uint_as_float((uint32_t)(by > 253 ? 253 : by) << 23);
-}
-__device__ __forceinline__ float finite_max(float m, float x) { return isfinite(x) && fabsf(x) > m ? fabsf(x) : m; }
-
 template <typename XT>
 __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
     __shared__ float most[4];
@@ -250,21 +354,7 @@ __device__ __forceinline__ void range_of(const SlopeArgs& Q, int64_t block) {
     for (int k = threadIdx.x; k < RANGE_ROWS; k += 256) {
         const int64_t row = strip * RANGE_ROWS + k;
         if (row >= P.rows) break;
-        const int64_t rb = row / P.R_u, u = rb * P.n_chunks + j, g = u * P.R_u + row - rb * P.R_u;
-        int64_t base;
-        const int a = pk_action(P, u, base);
-        if (a == 0) {
-            for (int32_t c = 0; c < P.G; c += 8) {
-                float w[8];
-                skip_row(P, row, j * P.G + c, w);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) most_here = finite_max(most_here, w[i]);
-            }
-        } else {
-            const float s = P.scale[g], o = a >= 5 ? 0.0f : P.offset[g];
-            const float L = a == 1 ? 255.0f : (a == 2 ? 15.0f : (a == 3 ? 7.0f : (a == 4 ? 3.0f : 1.0f)));
-            most_here = finite_max(finite_max(most_here, o), fmaf(s, L, o));
-        }
+        most_here = group_max(P, row, j, most_here);
     }
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) most_here = fmaxf(most_here, __shfl_xor(most_here, d, 64));

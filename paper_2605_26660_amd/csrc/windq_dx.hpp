@@ -55,25 +55,9 @@ __device__ __forceinline__ void weight_octet(const PackArgs& P, int64_t row, int
     }
 }
 
-// w_hat rounded to bfloat16 and turned: wt [cols][ld], zeros from the last row to K.  A thread has eight rows by eight columns.  In half precision (_Float16)
-// weights are multiplied by a power of two first, the same for an octet of columns.
-template <typename HT>
-__device__ __forceinline__ uint32_t half_bits(float x) {
-    if constexpr (__is_same(HT, _Float16)) return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x);
-    else return f32_to_bf16_bits(x);
-}
-
-template <typename HT>
-__device__ __forceinline__ void turn(const PackArgs& P, int32_t K, int64_t ld, float by, uint16_t* __restrict__ wt, int64_t block) {
-    __shared__ uint16_t trits_of[256];
-    trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
-    __syncthreads();
-    const int32_t row_blocks = (K + 255) / 256;
-    const int64_t cb = block / row_blocks;
-    const int64_t r0 = (block - cb * row_blocks) * 256 + (threadIdx.x & 31) * 8, col = cb * 64 + (threadIdx.x >> 5) * 8;
-    if (col >= P.cols || r0 >= K) return;
-    auto bits_of = [&](float x) { return half_bits<HT>(__is_same(HT, _Float16) ? x * by : x); };
-    uint32_t v[8][4];
+// Eight rows by eight columns of w_hat, put(row, column, weight) for each; rows past the last one are zeros.
+template <typename Put>
+__device__ __forceinline__ void eight_rows(const PackArgs& P, int64_t r0, int64_t col, const uint16_t* __restrict__ trits_of, Put put) {
     const uint32_t R_u = (uint32_t)P.R_u, rb = (uint32_t)r0 / R_u, lrow = (uint32_t)r0 - rb * R_u;
     if (r0 + 8 <= P.rows && lrow + 8 <= R_u) {              // one unit's rows
         const uint32_t j = (uint32_t)col / (uint32_t)P.G;
@@ -83,12 +67,11 @@ __device__ __forceinline__ void turn(const PackArgs& P, int32_t K, int64_t ld, f
         const int a = pk_action(P, u, base);
         if (a == 0) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float w0[8], w1[8];
-                skip_row(P, r0 + 2 * i, col, w0);
-                skip_row(P, r0 + 2 * i + 1, col, w1);
+            for (int i = 0; i < 8; ++i) {
+                float w[8];
+                skip_row(P, r0 + i, col, w);
 #pragma unroll
-                for (int m = 0; m < 8; ++m) v[m][i] = bits_of(w0[m]) | bits_of(w1[m]) << 16;
+                for (int m = 0; m < 8; ++m) put(i, m, w[m]);
             }
         } else {
             const int32_t nb = (int32_t)pk_bytes_per_group(a, P.G);
@@ -116,33 +99,77 @@ __device__ __forceinline__ void turn(const PackArgs& P, int32_t K, int64_t ld, f
                 for (int i = 0; i < 8; ++i) m8[i] = P.mask[(r0 + i) * P.mask_ld + (col >> 3)];
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int m = 0; m < 8; ++m) {
-                    uint32_t w[2];
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const uint4& g = f[2 * i + k];
-                        const uint32_t pair = (m >> 1) == 0 ? g.x : ((m >> 1) == 1 ? g.y : ((m >> 1) == 2 ? g.z : g.w));
-                        const float q = ((m & 1) != 0 ? __uint_as_float(pair & 0xffff0000u) : __uint_as_float(pair << 16)) - f0;
-                        const float x = fmaf(q, sc[2 * i + k], a >= 5 ? 0.0f : of[2 * i + k]);
-                        w[k] = bits_of(((m8[2 * i + k] >> m) & 1u) != 0u ? 0.0f : x);
-                    }
-                    v[m][i] = w[0] | w[1] << 16;
+                    const uint32_t pair = (m >> 1) == 0 ? f[i].x : ((m >> 1) == 1 ? f[i].y : ((m >> 1) == 2 ? f[i].z : f[i].w));
+                    const float q = ((m & 1) != 0 ? __uint_as_float(pair & 0xffff0000u) : __uint_as_float(pair << 16)) - f0;
+                    const float x = fmaf(q, sc[i], a >= 5 ? 0.0f : of[i]);
+                    put(i, m, ((m8[i] >> m) & 1u) != 0u ? 0.0f : x);
                 }
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float w0[8] = {}, w1[8] = {};
-            if (r0 + 2 * i < P.rows) weight_octet(P, r0 + 2 * i, col, trits_of, w0);
-            if (r0 + 2 * i + 1 < P.rows) weight_octet(P, r0 + 2 * i + 1, col, trits_of, w1);
+        for (int i = 0; i < 8; ++i) {
+            float w[8] = {};
+            if (r0 + i < P.rows) weight_octet(P, r0 + i, col, trits_of, w);
 #pragma unroll
-            for (int m = 0; m < 8; ++m) v[m][i] = bits_of(w0[m]) | bits_of(w1[m]) << 16;
+            for (int m = 0; m < 8; ++m) put(i, m, w[m]);
         }
     }
+}
+
+template <typename HT>
+__device__ __forceinline__ uint32_t half_bits(float x) {
+    if constexpr (__is_same(HT, _Float16)) return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x);
+    else return f32_to_bf16_bits(x);
+}
+
+// w_hat rounded to bfloat16 and turned: wt [cols][ld], zeros from the last row to K.  A thread has eight rows by eight columns.  In half precision (_Float16)
+// weights are multiplied by a power of two first, the same for an octet of columns.
+template <typename HT>
+__device__ __forceinline__ void turn(const PackArgs& P, int32_t K, int64_t ld, float by, uint16_t* __restrict__ wt, int64_t block) {
+    __shared__ uint16_t trits_of[256];
+    trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
+    __syncthreads();
+    const int32_t row_blocks = (K + 255) / 256;
+    const int64_t cb = block / row_blocks;
+    const int64_t r0 = (block - cb * row_blocks) * 256 + (threadIdx.x & 31) * 8, col = cb * 64 + (threadIdx.x >> 5) * 8;
+    if (col >= P.cols || r0 >= K) return;
+    uint32_t v[8][4];
+    eight_rows(P, r0, col, trits_of, [&](int i, int m, float x) {
+        const uint32_t b = half_bits<HT>(__is_same(HT, _Float16) ? x * by : x);
+        v[m][i >> 1] = (i & 1) != 0 ? v[m][i >> 1] | b << 16 : b;
+    });
 #pragma unroll
     for (int m = 0; m < 8; ++m) *reinterpret_cast<uint4*>(wt + (col + m) * ld + r0) = make_uint4(v[m][0], v[m][1], v[m][2], v[m][3]);
+}
+
+// The largest finite magnitude that the weights of a row's group can have, and the power of two that brings magnitudes up to `most` below 2^15 (1 where
+// there are none), itself within fp32's normal numbers.
+__device__ __forceinline__ float finite_max(float m, float x) { return isfinite(x) && fabsf(x) > m ? fabsf(x) : m; }
+__device__ __forceinline__ float group_max(const PackArgs& P, int64_t row, int64_t j, float m) {
+    const int64_t rb = row / P.R_u, u = rb * P.n_chunks + j, g = u * P.R_u + row - rb * P.R_u;
+    int64_t base;
+    const int a = pk_action(P, u, base);
+    if (a == 0) {
+#pragma unroll 8
+        for (int32_t c = 0; c < P.G; c += 8) {
+            float w[8];
+            skip_row(P, row, j * P.G + c, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = finite_max(m, w[i]);
+        }
+        return m;
+    }
+    const float s = P.scale[g], o = a >= 5 ? 0.0f : P.offset[g];
+    const float L = a == 1 ? 255.0f : (a == 2 ? 15.0f : (a == 3 ? 7.0f : (a == 4 ? 3.0f : 1.0f)));
+    return finite_max(finite_max(m, o), fmaf(s, L, o));
+}
+__device__ __forceinline__ float power_below(float most) {
+    const int e = (int)(__float_as_uint(most) >> 23);       // biased; most < 2^(e - 126)
+    const int by = most > 0.0f ? 127 + 14 - (e - 127) : 127;
+    return __uint_as_float((uint32_t)(by > 253 ? 253 : by) << 23);
 }
 
 #endif  // __HIPCC__

@@ -13,7 +13,7 @@
 // lanes reading sixteen rows' same slot meet all 64 banks (two rows have a turn of them).
 #pragma once
 
-#include "windq_adapters.hpp"
+#include "windq_pair.hpp"
 
 namespace windq {
 
@@ -35,6 +35,11 @@ struct GemmArgs {
     int32_t tiles, each;       // workgroups of a split, its steps of GM_K
     const float* by_token;     // halves: what a token's results are multiplied by, and an octet of columns'
     const float* by_octet;
+    // Of a pair (windq_gated) `columns` are rows of the gate and of the up, 32 and 32 in turn, and dX is H.
+    PackArgs gate;
+    PairArgs pair;
+    const uint16_t* raw;       // the caller's X
+    int64_t ld_raw;
 };
 
 inline int64_t gemm_k(int64_t rows) { return (rows + GM_K - 1) / GM_K * GM_K; }
@@ -56,7 +61,7 @@ inline int64_t gemm_cols(int64_t cols) { return (cols + GM_MOST - 1) / GM_MOST *
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-template <int MF, bool HALF = false>                       // fragments of a wavefront along the columns; factors in half precision
+template <int MF, bool HALF = false, bool PAIR = false>    // fragments of a wavefront along the columns; factors in half precision
 __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
     constexpr int GM_M = MF * 64, WM = MF * 32, LOADS = (GM_M + GM_N) / 32;
     __shared__ uint4 tile[GM_BUFFERS][(GM_M + GM_N) * 8];
@@ -147,6 +152,88 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
 
+    if constexpr (PAIR) {
+        // Fragments 2 p and 2 p + 1 are the gate's and the up's of the same 32 rows.  What is written goes through LDS: a lane has four rows of a token, and 8
+        // bytes of each of 32 tokens are written at a third of the rate of whole lines.
+        constexpr int ROWS = GM_M / 2, LD = ROWS + 8;       // of a tile's tokens in LDS
+        const int64_t rows = Q.gate.rows;
+        uint16_t* const out = reinterpret_cast<uint16_t*>(tile);
+        static_assert(3 * GM_N * LD * 2 <= sizeof(tile), "G, U and H of a tile fit");
+        __syncthreads();                                    // everybody is done with the last buffer
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            const int64_t t = t0 + wn * 64 + n * 32 + sub;
+            const float token = Q.by_token[t < Q.T ? t : Q.T - 1];
+#pragma unroll
+            for (int f = 0; f < MF; ++f) {
+                const int64_t c = c0 + wm * WM + f * 32, row0 = (c >> 6) * 32 + hh * 4;
+                bool bad = false;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float octet = Q.by_octet[(c >> 3) + g];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        acc[f][n][g * 4 + i] = acc[f][n][g * 4 + i] * token * octet;
+                        bad |= !isfinite(acc[f][n][g * 4 + i]);
+                    }
+                }
+                // what is not finite so far: weight by weight
+                if (__any(bad && row0 < rows && t < Q.T)) {
+#pragma unroll 1
+                    for (int i = 0; i < 16; ++i) {
+                        const int64_t row = row0 + (i >> 2) * 8 + (i & 3);
+                        float v = 0.0f;
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) v = i == k ? acc[f][n][k] : v;
+                        if (!isfinite(v) && row < rows && t < Q.T) v = (float)pk_slow_dot((f & 1) == 0 ? Q.gate : Q.pair.up, row, Q.raw + t * Q.ld_raw);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) acc[f][n][k] = i == k ? v : acc[f][n][k];
+                    }
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < MF / 2; ++p)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    uint32_t v[3][4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float none;
+                        const float x = acc[2 * p][n][g * 4 + i], y = acc[2 * p + 1][n][g * 4 + i];
+                        v[0][i] = f32_to_bf16_bits(activation<false>(Q.pair.act, x, none) * y);
+                        v[1][i] = f32_to_bf16_bits(x);
+                        v[2][i] = f32_to_bf16_bits(y);
+                    }
+                    uint16_t* const to = out + (wn * 64 + n * 32 + sub) * LD + wm * (WM / 2) + p * 32 + g * 8 + hh * 4;
+#pragma unroll
+                    for (int k = 0; k < 3; ++k)
+                        if (k == 0 || Q.pair.G != nullptr) *reinterpret_cast<uint2*>(to + k * GM_N * LD) = make_uint2(v[k][0] | v[k][1] << 16, v[k][2] | v[k][3] << 16);
+                }
+        }
+        __syncthreads();
+#pragma unroll 1
+        for (int k = 0; k < (Q.pair.G != nullptr ? 3 : 1); ++k) {
+            uint16_t* __restrict__ const to = static_cast<uint16_t*>(k == 0 ? Q.dX : (k == 1 ? Q.pair.G : Q.pair.U));
+            const int64_t ld = k == 0 ? Q.ldx : Q.pair.ld_save;
+            const bool whole = (ld & 7) == 0 && (reinterpret_cast<uintptr_t>(to) & 15) == 0;
+#pragma unroll 4
+            for (int i = tid; i < GM_N * (ROWS / 8); i += GM_THREADS) {
+                const int n = i / (ROWS / 8), r = (i - n * (ROWS / 8)) * 8;
+                const int64_t t = t0 + n, row = (c0 >> 1) + r;
+                if (t >= Q.T || row >= rows) continue;      // rows come in eights
+                const uint4 v = *reinterpret_cast<const uint4*>(out + (k * GM_N + n) * LD + r);
+                uint16_t* __restrict__ const o = to + t * ld + row;
+                if (whole) {
+                    *reinterpret_cast<uint4*>(o) = v;
+                } else {
+                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int m = 0; m < 8; ++m) o[m] = (uint16_t)(w[m >> 1] >> (16 * (m & 1)));
+                }
+            }
+        }
+        return;
+    }
     if constexpr (HALF) {
 #pragma unroll
         for (int n = 0; n < 2; ++n) {

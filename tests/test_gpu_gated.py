@@ -1,6 +1,8 @@
 """windq_gated and windq_gated_grad against the formulas in 64 bits, and the gradients against differences of them.
 
-Bounds.  G and U are products as windq_project has them: 16 x 2^-24 of the sum of the magnitudes that are added; a bfloat16 output adds 2^-8 of its value.  In H an error e of G
+Bounds.  G and U are products as windq_project has them: 16 x 2^-24 of the sum of the magnitudes that are added; a bfloat16 output adds 2^-8 of its value.  Where many bfloat16
+tokens go through weights in half precision, every weight is off by half a step of 2^-10 (2^-11 of it) at most, or, below 2^-14 of eight rows' largest times a power
+of two (2^14 at least), half a step of 2^-24: 2^-39 of the largest; a token's values by 2^-39 of its largest.  In H an error e of G
 comes out as 1.13 |U| e at most, one of U as |act(G)| e; the activation and its slope are some ten fp32 roundings of terms no larger than (1 + |G|) and, where an
 exponent z of e^z is rounded first, |z| of them more, |z| < 2 (|G| + |G|^3 / 20): 16 x 2^-24 (1 + |G| + |G|^3 / 8).
 dX in bfloat16: dG, dU and the weights enter in half precision, half a step of 2^-11 each, every weight and every way of rounding, and below 2^-14 (of the largest of a token or
@@ -38,6 +40,10 @@ def forward(cs, x, word, dtype):
     x = x.double().cpu().numpy()
     g, u = (x @ c.w.T for c in cs)
     go, uo = (EPS * (np.abs(x) @ c.mag.T) for c in cs)
+    if dtype == BF and x.shape[0] > 64:
+        size = np.abs(x)
+        halves = lambda c: size @ (2.0 ** -11 * np.abs(c.w) + 2.0 ** -38 * np.abs(c.w).max()).T + 2.0 ** -38 * size.max(1, keepdims=True) * np.abs(c.w).sum(1)  # noqa: E731
+        go, uo = go + halves(cs[0]), uo + halves(cs[1])
     a = act(word, g)
     return (g, u, a * u), (go, uo, 1.13 * np.abs(u) * go + np.abs(a) * uo + 1.13 * go * uo + EPS * np.abs(u) * curve(g))
 
