@@ -60,19 +60,18 @@ struct HalvesArgs {
     float* by_octet;
 };
 
-// Workgroups [0, T): a token; the others: eight rows of a matrix.
+// Workgroups [0, T): a token; the others: 16 rows of a matrix.  A wavefront has 128 columns of them at a time, one treatment as a rule, a lane an octet of
+// columns of two rows: lanes of different treatments would take turns, each waiting for its codes.  The units' treatments and places are looked up once.
+// Bound by latency: loads wait for the stores ahead of them, so that few registers and many wavefronts count.
+constexpr int HALVES_UNITS = 512, HALVES_ROWS = 16;
+
+template <bool KNOWN>                                      // units of whole blocks of rows, and few enough of them in a row
 __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, const int64_t first) {
-    __shared__ float most[4];
+    __shared__ float most[4][2];
     __shared__ uint16_t trits_of[256];
+    __shared__ uint64_t units[HALVES_UNITS];
     const int64_t id = first + blockIdx.x;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    auto of_all = [&](float m) {
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-        if (lane == 0) most[wave] = m;
-        __syncthreads();
-        return power_below(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
-    };
     if (id < Q.T) {
         const uint16_t* __restrict__ const x = Q.X + id * Q.ldx;
         float m = 0.0f;
@@ -82,7 +81,11 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
 #pragma unroll
             for (int i = 0; i < 8; ++i) m = finite_max(m, v[i]);
         }
-        const float by = of_all(m);
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+        if (lane == 0) most[wave][0] = m;
+        __syncthreads();
+        const float by = power_below(fmaxf(fmaxf(most[0][0], most[1][0]), fmaxf(most[2][0], most[3][0])));
         if (threadIdx.x == 0) Q.by_token[id] = 1.0f / by;
         for (int64_t c = threadIdx.x * 8; c < Q.K; c += 2048) {
             float v[8] = {};
@@ -94,24 +97,56 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
         }
         return;
     }
-    trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);      // there by the barrier in of_all
-    const int64_t octets = Q.P[0].rows / 8, block = id - Q.T;
-    const int mat = block >= octets ? 1 : 0;
+    trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
+    const int64_t blocks = (Q.P[0].rows + HALVES_ROWS - 1) / HALVES_ROWS, block = id - Q.T;
+    const int mat = block >= blocks ? 1 : 0;
     const PackArgs& P = Q.P[mat];
-    const int64_t r0 = (block - mat * octets) * 8, at = (r0 >> 5) * 64 + mat * 32 + (r0 & 31);
+    const int64_t r0 = (block - mat * blocks) * HALVES_ROWS, at = (r0 >> 5) * 64 + mat * 32 + (r0 & 31), rb = r0 / P.R_u;
+    if constexpr (KNOWN)
+        for (int32_t j = threadIdx.x; j < P.n_chunks; j += 256) {
+            int64_t base;
+            const int a = pk_action(P, rb * P.n_chunks + j, base);
+            units[j] = (uint64_t)a << 56 | (uint64_t)(a == 0 ? 0 : base);
+        }
+    // the largest magnitudes of eight rows
     float m = 0.0f;
-    for (int64_t k = threadIdx.x; k < (int64_t)P.n_chunks * 8; k += 256) m = group_max(P, r0 + (k & 7), k >> 3, m);
-    const float by = of_all(m);
-    if (threadIdx.x == 0) Q.by_octet[at >> 3] = 1.0f / by;
-    for (int64_t c = threadIdx.x * 8; c < Q.K; c += 2048) {
-        uint32_t w[8][4] = {};
-        if (c < P.cols)
-            eight_rows(P, r0, c, trits_of, [&](int i, int k, float v) {
-                const uint32_t b = half_bits<_Float16>(v * by);
-                w[i][k >> 1] = (k & 1) != 0 ? w[i][k >> 1] | b << 16 : b;
-            });
+    const int64_t row = r0 + (threadIdx.x & 15);
+    if (row < P.rows)
+        for (int64_t j = threadIdx.x >> 4; j < P.n_chunks; j += 16) m = group_max(P, row, j, m);
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    m = fmaxf(m, __shfl_xor(m, 16, 64));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(Q.w + (at + i) * Q.K + c) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+    for (int d = 4; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+    if (lane == 0 || lane == 8) most[wave][lane >> 3] = m;
+    __syncthreads();
+    const int octet = wave & 1, part = octet * 4 + (lane >> 4);
+    const float by = power_below(fmaxf(fmaxf(most[0][octet], most[1][octet]), fmaxf(most[2][octet], most[3][octet])));
+    const int64_t here = r0 + part * 2;
+    if (here >= P.rows) return;                             // rows come in eights
+    if (wave < 2 && lane == 0) Q.by_octet[(at >> 3) + octet] = 1.0f / by;
+    for (int64_t c = (wave >> 1) * 128 + (lane & 15) * 8; c < Q.K; c += 256) {
+        uint32_t w[2][4] = {};
+        auto put = [&](int i, int k, float v) {
+            const uint32_t b = half_bits<_Float16>(v * by);
+            w[i][k >> 1] = (k & 1) != 0 ? w[i][k >> 1] | b << 16 : b;
+        };
+        if (c < P.cols) {
+            const uint32_t j = (uint32_t)c / (uint32_t)P.G;
+            if constexpr (KNOWN) {
+                const uint64_t unit = units[j];
+                rows_of<2>(P, here, c, rb * P.n_chunks + j, here - rb * P.R_u, ((int)c - (int)j * P.G) >> 3, (int)(unit >> 56), (int64_t)(unit & 0xffffffffffffffull), trits_of, put);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float v[8];
+                    weight_octet(P, here + i, c, trits_of, v);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) put(i, k, v[k]);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) *reinterpret_cast<uint4*>(Q.w + (at + part * 2 + i) * Q.K + c) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
     }
 }
 
@@ -119,7 +154,11 @@ int launch_gated_halves(const ProjectArgs& Q, char* ws, const GatedWs& at, hipSt
     const int64_t K = gemm_k(Q.P.cols), rows = gated_rows(Q.P.rows), tall = tokens_in(Q.T, GM_N);
     const HalvesArgs H = {{Q.P, Q.pair.up}, Q.X, Q.ldx, Q.T, K, reinterpret_cast<uint16_t*>(ws + at.x), reinterpret_cast<float*>(ws + at.by_token),
                           reinterpret_cast<uint16_t*>(ws + at.w), reinterpret_cast<float*>(ws + at.by_octet)};
-    const int status = launch_pieces(Q.T + Q.P.rows / 4, 256, [&](int64_t first, dim3 g) { gated_halves_kernel<<<g, dim3(256), 0, st>>>(H, first); });
+    const bool known = (Q.P.R_u == Q.P.rows || Q.P.R_u % HALVES_ROWS == 0) && Q.P.n_chunks <= HALVES_UNITS;
+    const int status = launch_pieces(Q.T + 2 * tokens_in(Q.P.rows, HALVES_ROWS), 256, [&](int64_t first, dim3 g) {
+        if (known) gated_halves_kernel<true><<<g, dim3(256), 0, st>>>(H, first);
+        else gated_halves_kernel<false><<<g, dim3(256), 0, st>>>(H, first);
+    });
     if (status != WINDQ_OK) return status;
     const int64_t by = rows / 256 * tall >= GM_TILES ? 256 : 128, tiles = rows / by * tall;
     GemmArgs M = {};

@@ -11,7 +11,14 @@ namespace windq {
 
 #ifdef __HIPCC__
 
-__device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
+// e^x as 2^h (1 + l ln 2) with x log2 e = h + l, h in fp32 and l what that leaves: two units in the last place, a third of the instructions of a
+// library's exponential and quotient (64 results a lane wait for them at the end of a tile).  Below 2^-126 it is 0.
+__device__ __forceinline__ float exponential(float x) {
+    const float h = x * 1.44269504f, l = fmaf(x, 1.44269504f, -h) + x * 1.92596303e-8f;
+    const float p = __builtin_amdgcn_exp2f(h);
+    return fabsf(h) < 200.0f ? fmaf(p, l * 0.693147181f, p) : p;      // infinities have no l
+}
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + exponential(-x)); }
 
 // act(x), and its slope where SLOPE.
 template <bool SLOPE>
@@ -25,7 +32,7 @@ __device__ __forceinline__ float activation(int act, float x, float& slope) {
         // erfc in the place of 1 + erf: Phi keeps its digits far to the left
         const float phi = 0.5f * erfcf(x * -0.70710678118654752f);
         y = x * phi;
-        if (SLOPE) slope = phi + x * (expf(-0.5f * x * x) * 0.39894228040143268f);
+        if (SLOPE) slope = phi + x * (exponential(-0.5f * x * x) * 0.39894228040143268f);
     } else {
         constexpr float K2 = 1.5957691216057308f;          // 2 sqrt(2 / pi)
         const float x2 = x * x, t = sigmoid(K2 * (x + 0.044715f * x2 * x));

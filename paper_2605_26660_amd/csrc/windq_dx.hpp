@@ -55,59 +55,65 @@ __device__ __forceinline__ void weight_octet(const PackArgs& P, int64_t row, int
     }
 }
 
-// Eight rows by eight columns of w_hat, put(row, column, weight) for each; rows past the last one are zeros.
+// ROWS rows by eight columns of w_hat within a unit, whose treatment and first byte are known, put(row, column, weight) for each.
+template <int ROWS, typename Put>
+__device__ __forceinline__ void rows_of(const PackArgs& P, int64_t r0, int64_t col, int64_t u, int64_t lrow, int o, int a, int64_t base,
+                                        const uint16_t* __restrict__ trits_of, Put put) {
+    if (a == 0) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            float w[8];
+            skip_row(P, r0 + i, col, w);
+#pragma unroll
+            for (int m = 0; m < 8; ++m) put(i, m, w[m]);
+        }
+        return;
+    }
+    const int32_t nb = (int32_t)pk_bytes_per_group(a, P.G);
+    const uint8_t* const first = P.codes + base + lrow * nb;
+    float sc[ROWS], of[ROWS];
+    __builtin_memcpy(sc, P.scale + u * P.R_u + lrow, 4 * ROWS);
+    __builtin_memcpy(of, P.offset + u * P.R_u + lrow, 4 * ROWS);
+    uint4 f[ROWS];
+    auto rows = [&](auto octet) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) f[i] = octet(first + i * nb);
+    };
+    switch (a) {
+        case 1: rows([&](const uint8_t* p) { uint2 q; __builtin_memcpy(&q, p + o * 8, 8); return fields8(q.x, q.y); }); break;
+        case 2: rows([&](const uint8_t* p) { uint32_t q; __builtin_memcpy(&q, p + o * 4, 4); return fields4(q); }); break;
+        case 3: rows([&](const uint8_t* p) { return octet_fields(3, p, o, trits_of); }); break;
+        case 4: rows([&](const uint8_t* p) { uint16_t q; __builtin_memcpy(&q, p + o * 2, 2); return fields2(q); }); break;
+        case 5: rows([&](const uint8_t* p) { return fields2(octet_trits(p, o, trits_of) & 0xffffu); }); break;
+        default: rows([&](const uint8_t* p) { return fields1(p[o]); }); break;
+    }
+    const float f0 = pk_f0(a);
+    uint32_t m8[ROWS] = {};
+    if (P.mask != nullptr) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) m8[i] = P.mask[(r0 + i) * P.mask_ld + (col >> 3)];
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+        for (int m = 0; m < 8; ++m) {
+            const uint32_t pair = (m >> 1) == 0 ? f[i].x : ((m >> 1) == 1 ? f[i].y : ((m >> 1) == 2 ? f[i].z : f[i].w));
+            const float q = ((m & 1) != 0 ? __uint_as_float(pair & 0xffff0000u) : __uint_as_float(pair << 16)) - f0;
+            const float x = fmaf(q, sc[i], a >= 5 ? 0.0f : of[i]);
+            put(i, m, ((m8[i] >> m) & 1u) != 0u ? 0.0f : x);
+        }
+}
+
+// Eight rows by eight columns of w_hat; rows past the last one are zeros.
 template <typename Put>
 __device__ __forceinline__ void eight_rows(const PackArgs& P, int64_t r0, int64_t col, const uint16_t* __restrict__ trits_of, Put put) {
     const uint32_t R_u = (uint32_t)P.R_u, rb = (uint32_t)r0 / R_u, lrow = (uint32_t)r0 - rb * R_u;
     if (r0 + 8 <= P.rows && lrow + 8 <= R_u) {              // one unit's rows
         const uint32_t j = (uint32_t)col / (uint32_t)P.G;
-        const int o = ((int)col - (int)j * P.G) >> 3;
         const int64_t u = (int64_t)rb * P.n_chunks + j;
         int64_t base;
         const int a = pk_action(P, u, base);
-        if (a == 0) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float w[8];
-                skip_row(P, r0 + i, col, w);
-#pragma unroll
-                for (int m = 0; m < 8; ++m) put(i, m, w[m]);
-            }
-        } else {
-            const int32_t nb = (int32_t)pk_bytes_per_group(a, P.G);
-            const uint8_t* const first = P.codes + base + (int64_t)lrow * nb;
-            float sc[8], of[8];
-            __builtin_memcpy(sc, P.scale + u * P.R_u + lrow, 32);
-            __builtin_memcpy(of, P.offset + u * P.R_u + lrow, 32);
-            uint4 f[8];
-            auto rows = [&](auto octet) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] = octet(first + i * nb);
-            };
-            switch (a) {
-                case 1: rows([&](const uint8_t* p) { uint2 q; __builtin_memcpy(&q, p + o * 8, 8); return fields8(q.x, q.y); }); break;
-                case 2: rows([&](const uint8_t* p) { uint32_t q; __builtin_memcpy(&q, p + o * 4, 4); return fields4(q); }); break;
-                case 3: rows([&](const uint8_t* p) { return octet_fields(3, p, o, trits_of); }); break;
-                case 4: rows([&](const uint8_t* p) { uint16_t q; __builtin_memcpy(&q, p + o * 2, 2); return fields2(q); }); break;
-                case 5: rows([&](const uint8_t* p) { return fields2(octet_trits(p, o, trits_of) & 0xffffu); }); break;
-                default: rows([&](const uint8_t* p) { return fields1(p[o]); }); break;
-            }
-            const float f0 = pk_f0(a);
-            uint32_t m8[8] = {};
-            if (P.mask != nullptr) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) m8[i] = P.mask[(r0 + i) * P.mask_ld + (col >> 3)];
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-#pragma unroll
-                for (int m = 0; m < 8; ++m) {
-                    const uint32_t pair = (m >> 1) == 0 ? f[i].x : ((m >> 1) == 1 ? f[i].y : ((m >> 1) == 2 ? f[i].z : f[i].w));
-                    const float q = ((m & 1) != 0 ? __uint_as_float(pair & 0xffff0000u) : __uint_as_float(pair << 16)) - f0;
-                    const float x = fmaf(q, sc[i], a >= 5 ? 0.0f : of[i]);
-                    put(i, m, ((m8[i] >> m) & 1u) != 0u ? 0.0f : x);
-                }
-        }
+        rows_of<8>(P, r0, col, u, lrow, ((int)col - (int)j * P.G) >> 3, a, base, trits_of, put);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -153,7 +159,7 @@ __device__ __forceinline__ float group_max(const PackArgs& P, int64_t row, int64
     int64_t base;
     const int a = pk_action(P, u, base);
     if (a == 0) {
-#pragma unroll 8
+#pragma unroll 2
         for (int32_t c = 0; c < P.G; c += 8) {
             float w[8];
             skip_row(P, row, j * P.G + c, w);
