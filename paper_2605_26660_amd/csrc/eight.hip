@@ -284,11 +284,14 @@ constexpr int64_t EIGHT_FEW = 128;
 // A row block and 32 N tokens a workgroup; its wavefronts share the k-blocks (of a pair: half of them the gate's, the others the up's) and
 // add up through LDS.  Bound by latency: everything that a k-block needs is asked for at once, and the next one's fields before this one is multiplied.
 // Tokens are the M side of the matrix instructions and rows the N side, so that a lane has one row, with one alpha and one beta; beta times the tokens' sums
-// is an instruction of its own, with nothing in its other half.
+// is an instruction of its own, whose halves have the sums of a step's halves.  Tokens come through a place of the wavefront's own in LDS, whole lines
+// of eight of them at a time: 16 bytes of each of 32 tokens in one load are 32 lines (48 tokens through 11008 x 4096 22 us, 14 so).
 template <typename YT, int S, int N, int WAVES, bool PAIR>
 __global__ __launch_bounds__(WAVES * 64) void eight_kernel(const EightArgs Q, const int64_t first) {
     constexpr int EACH = PAIR ? WAVES / 2 : WAVES;
-    __shared__ float red[WAVES][N * 16][64];
+    __shared__ uint4 mem[WAVES][N * 256];                   // a wavefront's tokens, 128 bytes each, and its results later
+    float(*const red)[N * 16][64] = reinterpret_cast<float(*)[N * 16][64]>(mem);
+    static_assert(sizeof(mem) == WAVES * N * 16 * 64 * sizeof(float), "results fit");
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, sub = lane & 31, hh = lane >> 5;
     const int turn = wave % EACH;
     const EightPlan& P = Q.P[PAIR ? wave / EACH : 0];
@@ -296,14 +299,15 @@ __global__ __launch_bounds__(WAVES * 64) void eight_kernel(const EightArgs Q, co
     const int64_t rb = b / Q.RB, i = b - rb * Q.RB;
     const bool w_f32 = Q.w_f32 != 0;
 
-    const int8_t* x[N];
-    const int32_t* xs[N];
+    // slot p of a token's eight holds the sixteen bytes of slot p ^ (token / 2 & 7)
+    const int8_t* x[N * 4];
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-        const int64_t t = t0 + n * 32 + sub < Q.T ? t0 + n * 32 + sub : Q.T - 1;
-        x[n] = Q.codes + t * Q.width + hh * 16;
-        xs[n] = Q.sums + t * Q.sums_ld;
+    for (int k = 0; k < N * 4; ++k) {
+        const int n = k * 8 + (lane >> 3), slot = (lane & 7) ^ ((n >> 1) & 7);
+        x[k] = Q.codes + (t0 + n < Q.T ? t0 + n : Q.T - 1) * Q.width + (slot < 2 * S ? slot : 0) * 16;
     }
+    const uint32_t lds = lds_address(mem[wave]);
+    const char* const place = reinterpret_cast<const char*>(mem[wave]) + sub * 128;
     const uint32_t* const words = reinterpret_cast<const uint32_t*>(P.image) + b * Q.n_kb;
     const float* const affine = reinterpret_cast<const float*>(P.image + Q.affine) + b * Q.n_kb * 64 + sub;
     f32x16 tot[N] = {};
@@ -318,23 +322,25 @@ __global__ __launch_bounds__(WAVES * 64) void eight_kernel(const EightArgs Q, co
         for (int32_t it = 0; it < count; ++it) {
             const int32_t kb = from + it * EACH;
             const int kind = u.kind;
+#pragma unroll
+            for (int k = 0; k < N * 4; ++k)
+                if (t0 + k * 8 < Q.T) lds_load16(lds + k * 1024, x[k] + (int64_t)kb * (32 * S));       // past the last token: whatever lies there, for results that nobody stores
+            const float alpha = affine[(int64_t)kb * 64], beta = affine[(int64_t)kb * 64 + 32];
+            i32x4 w[S];
+            raw.operands(kind, w);
+            const EightBlock here = u;
+            wait_for_loads();
+            u = eight_block(P, (uint32_t)__builtin_amdgcn_readlane((int)of, it + 1 < count ? it + 1 : it));
+            raw.load(u.kind, u.fields, lane);
             uint4 xv[S][N];
 #pragma unroll
             for (int s = 0; s < S; ++s)
 #pragma unroll
-                for (int n = 0; n < N; ++n) xv[s][n] = *reinterpret_cast<const uint4*>(x[n] + (int64_t)kb * (32 * S) + s * 32);
-            const float alpha = affine[(int64_t)kb * 64], beta = affine[(int64_t)kb * 64 + 32];
-            int32_t sum[N];
-#pragma unroll
-            for (int n = 0; n < N; ++n) sum[n] = xs[n][kb];
-            i32x4 w[S];
-            raw.operands(kind, w);
-            const EightBlock here = u;
-            u = eight_block(P, (uint32_t)__builtin_amdgcn_readlane((int)of, it + 1 < count ? it + 1 : it));
-            raw.load(u.kind, u.fields, lane);
+                for (int n = 0; n < N; ++n) xv[s][n] = *reinterpret_cast<const uint4*>(place + n * 4096 + (((2 * s + hh) ^ ((sub >> 1) & 7)) << 4));
             if (kind == 0) {
                 const int terms = w_f32 ? 3 : 1;
                 const uint4* const weights = reinterpret_cast<const uint4*>(here.fields) + lane;
+#pragma unroll 1
                 for (int term = 0; term < terms; ++term) {
                     uint4 v[S][2];
 #pragma unroll
@@ -357,7 +363,17 @@ __global__ __launch_bounds__(WAVES * 64) void eight_kernel(const EightArgs Q, co
 #pragma unroll
                 for (int n = 0; n < N; ++n) acc[n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(as_i32x4(xv[s][n]), w[s], s == 0 ? i32x16{} : acc[n], 0, 0, 0);
 #pragma unroll
-            for (int n = 0; n < N; ++n) tot[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(hh == 0 ? (float)sum[n] : 0.0f, beta, tot[n], 0, 0, 0);
+            for (int n = 0; n < N; ++n) {
+                int sum = 0;
+#pragma unroll
+                for (int s = 0; s < S; ++s) {
+                    sum = __builtin_amdgcn_sdot4((int)xv[s][n].x, 0x01010101, sum, false);
+                    sum = __builtin_amdgcn_sdot4((int)xv[s][n].y, 0x01010101, sum, false);
+                    sum = __builtin_amdgcn_sdot4((int)xv[s][n].z, 0x01010101, sum, false);
+                    sum = __builtin_amdgcn_sdot4((int)xv[s][n].w, 0x01010101, sum, false);
+                }
+                tot[n] = __builtin_amdgcn_mfma_f32_32x32x2f32((float)sum, beta, tot[n], 0, 0, 0);
+            }
 #pragma unroll
             for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -392,10 +408,11 @@ __global__ __launch_bounds__(WAVES * 64) void eight_kernel(const EightArgs Q, co
 
 template <typename YT, int S, bool PAIR>
 int launch_eight(const EightArgs& Q, hipStream_t st) {
-    if (Q.T <= 32) {
-        constexpr int WAVES = 16;
-        return launch_pieces(Q.NB, WAVES * 64, [&](int64_t first, dim3 g) { eight_kernel<YT, S, 1, WAVES, PAIR><<<g, dim3(WAVES * 64), 0, st>>>(Q, first); });
-    }
+    if (Q.T <= 32)
+        return launch_pieces(Q.NB, 1024, [&](int64_t first, dim3 g) {
+            if (Q.NB > 256) eight_kernel<YT, S, 1, 8, PAIR><<<g, dim3(512), 0, st>>>(Q, first);
+            else eight_kernel<YT, S, 1, 16, PAIR><<<g, dim3(1024), 0, st>>>(Q, first);
+        });
     if (Q.T > EIGHT_FEW) {
         constexpr int WR = 4, WT = 1;
         const int64_t row_tiles = tokens_in(Q.NB, PAIR ? WR : 2 * WR), tiles = row_tiles * tokens_in(Q.T, WT * 64);

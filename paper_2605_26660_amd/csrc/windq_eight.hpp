@@ -178,6 +178,14 @@ struct EightFields {
     }
 };
 
+// All loads done, direct ones among them.  As a builtin: the compiler then knows it of its own loads and waits for none of them again, which would wait for
+// direct loads that it does not count.
+__device__ __forceinline__ void wait_for_loads() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    asm volatile("" ::: "memory");
+}
+
 // Eight of a token's integers as bfloat16: exact.
 __device__ __forceinline__ bf16x8 eight_as_bf16(uint32_t a, uint32_t b) {
     auto pair = [](uint32_t v, int lo) {

@@ -12,14 +12,6 @@ struct Const {
     static constexpr int value = V;
 };
 
-// All loads done, direct ones among them.  As a builtin: the compiler then knows it of its own loads and waits for none of them again, which would wait for
-// direct loads that it does not count.
-__device__ __forceinline__ void wait_for_loads() {
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0f70);
-    asm volatile("" ::: "memory");
-}
-
 template <typename YT, int S, int WR, int WT, bool PAIR>
 __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void eight_tiles_kernel(const EightArgs Q, const uint32_t row_tiles) {
     constexpr int TOKENS = WT * 64, LOADS = 8 / WR;
