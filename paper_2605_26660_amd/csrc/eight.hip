@@ -279,7 +279,13 @@ __global__ __launch_bounds__(256) void serving_lay_kernel(const PackArgs P, cons
 }
 
 // ------------------------------------------------------------------------------------------------ the product
-constexpr int64_t EIGHT_FEW = 128;
+// Whether the kernel for few tokens is the faster one beyond 32 of them, by rounds of workgroups on 256 CUs: one of its own takes 0.23 us a k-block (of a pair 0.45),
+// one of tiles 1.1 (1.25) while there is one, 0.8 (1.0) each where two share a CU.  32 k-blocks, 11008 rows: 128 tokens (three rounds) 26 us, tiles 37; 256 tokens
+// (six) 50 and 38; 4096 rows: 512 tokens (four) 34 and 37, 768 (six) 50 and 38; a pair of 11008 rows: 64 tokens (two) 33 and 42, 96 (three) 47 and 44.
+inline bool eight_few(int64_t workgroups, int64_t tiles, bool pair) {
+    const int64_t rounds = tokens_in(workgroups, 256), by_tiles = tokens_in(tiles, 256);
+    return 10 * rounds <= (pair ? (by_tiles == 1 ? 27 : 22 * by_tiles) : (by_tiles == 1 ? 48 : 35 * by_tiles));
+}
 
 // A row block and 32 N tokens a workgroup; its wavefronts share the k-blocks (of a pair: half of them the gate's, the others the up's) and
 // add up through LDS.  Bound by latency: everything that a k-block needs is asked for at once, and the next one's fields before this one is multiplied.
@@ -408,21 +414,20 @@ __global__ __launch_bounds__(WAVES * 64) void eight_kernel(const EightArgs Q, co
 
 template <typename YT, int S, bool PAIR>
 int launch_eight(const EightArgs& Q, hipStream_t st) {
+    // Eight wavefronts where the row blocks are more than the CUs, so that they run at once: 344 of a pair, 16 tokens 14.6 us and 16.2 with sixteen.
     if (Q.T <= 32)
         return launch_pieces(Q.NB, 1024, [&](int64_t first, dim3 g) {
             if (Q.NB > 256) eight_kernel<YT, S, 1, 8, PAIR><<<g, dim3(512), 0, st>>>(Q, first);
             else eight_kernel<YT, S, 1, 16, PAIR><<<g, dim3(1024), 0, st>>>(Q, first);
         });
-    if (Q.T > EIGHT_FEW) {
-        constexpr int WR = 4, WT = 1;
-        const int64_t row_tiles = tokens_in(Q.NB, PAIR ? WR : 2 * WR), tiles = row_tiles * tokens_in(Q.T, WT * 64);
-        if (fits_launch(tiles, WR * WT * 64)) {
-            eight_tiles_kernel<YT, S, WR, WT, PAIR><<<dim3((uint32_t)tiles), dim3(WR * WT * 64), 0, st>>>(Q, (uint32_t)row_tiles);
-            return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
-        }
+    constexpr int WR = 4, WT = 1;
+    const int64_t row_tiles = tokens_in(Q.NB, PAIR ? WR : 2 * WR), tiles = row_tiles * tokens_in(Q.T, WT * 64), few = Q.NB * tokens_in(Q.T, 64);
+    if (!eight_few(few, tiles, PAIR) && fits_launch(tiles, WR * WT * 64)) {
+        eight_tiles_kernel<YT, S, WR, WT, PAIR><<<dim3((uint32_t)tiles), dim3(WR * WT * 64), 0, st>>>(Q, (uint32_t)row_tiles);
+        return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
     }
     constexpr int WAVES = 8;
-    return launch_pieces(Q.NB * tokens_in(Q.T, 64), WAVES * 64, [&](int64_t first, dim3 g) { eight_kernel<YT, S, 2, WAVES, PAIR><<<g, dim3(WAVES * 64), 0, st>>>(Q, first); });
+    return launch_pieces(few, WAVES * 64, [&](int64_t first, dim3 g) { eight_kernel<YT, S, 2, WAVES, PAIR><<<g, dim3(WAVES * 64), 0, st>>>(Q, first); });
 }
 
 template <typename YT, bool PAIR>

@@ -73,7 +73,9 @@ def close(got, want, off, dtype):
 
 SHAPES = [(64, 128, 64, 0, 1), (200, 480, 96, 40, 5), (72, 80, 8, 0, 33), (1000, 1056, 96, 0, 77), (128, 512, 256, 64, 64), (40, 1024, 512, 8, 65),
           (35, 800, 160, 0, 31), (96, 288, 72, 32, 130), (7, 256, 128, 1, 3), (320, 1280, 128, 64, 200), (513, 256, 64, 0, 257), (264, 384, 128, 88, 129),
-          (72, 80, 8, 0, 333), (160, 320, 32, 32, 150), (300, 480, 160, 0, 390), (1000, 1056, 96, 0, 513), (2080, 768, 128, 0, 700), (576, 512, 512, 192, 1025)]
+          (72, 80, 8, 0, 333), (160, 320, 32, 32, 150), (300, 480, 160, 0, 390), (1000, 1056, 96, 0, 513), (2080, 768, 128, 0, 700), (576, 512, 512, 192, 1025),
+          # tiles, by the rule for it: steps of 4, 3, 2 and 1, tile units, ragged rows, a last pair of one k-block
+          (8192, 640, 128, 0, 700), (6000, 288, 96, 0, 900), (8192, 320, 64, 64, 650), (8200, 160, 32, 0, 640), (4160, 1024, 512, 32, 1200), (5000, 144, 72, 1000, 1090)]
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
