@@ -781,11 +781,11 @@ int windq_tokens8(const windq_mat* X, int32_t chunk_w, int8_t* codes, float* sca
  * A packed plan in the order in which 8-bit products read it: laid out once, read by every call after that.
  * windq_serving_layout (HOST only): where every unit's fields go, from the plan's treatments on the host.  image_off[U] is the image's size.  Codes
  * of 3 and of 1.58 bits take 4 and 2; weights of skip units are copied (fp32 ones: 6 bytes); rows of a unit are filled up to a multiple of 32, chunks
- * as windq_tokens says; 8 bytes a group and a unit beside them.
+ * as windq_tokens says; beside them 8 bytes for each k-block of every such row, 4 for each k-block of 32 rows and 256 at the end.
  * windq_serving_lay: writes the image (256-byte aligned) of a packed matrix on the stream.  image_off is the layout's, on the DEVICE.  A unit whose
  * entry of the plan is malformed counts as skip, as elsewhere; one whose fields do not fit in [image_off[u], image_off[u+1]) or in image_bytes, so that an
  * image of another plan's layout is no harm to memory, counts as zeros.  P->mask is not supported (WINDQ_EINVAL): protected weights are windq_project's.
- * WINDQ_EWORKSPACE: the image does not hold what stands ahead of the fields.
+ * WINDQ_EWORKSPACE: the image does not hold what stands ahead of the fields.  WINDQ_ESHAPE: an image of more than 2^37 bytes.
  */
 typedef struct windq_serving {
     const void* image;        /* as windq_serving_lay left it */
@@ -825,6 +825,8 @@ int windq_gated8(const windq_serving* gate, const windq_serving* up, const windq
  *   G, U  [tokens][rows] of X's type, ld_save >= rows: the products, rounded once, that windq_gated_grad starts from; both or neither
  * gate and up: of one shape, chunk_w, unit_rows and weight type; treatments and masks are their own.  At most 2^31 - 1 tokens x rows.
  * Workspace: windq_gated_workspace_bytes (256-byte aligned), written anew by every call.
+ * In WINDQ_BF16 the weights of many tokens enter the product in half precision (11 bits), each eight rows times a power of two of their own, where rows is a
+ * multiple of 8; elsewhere as in windq_project.  No output may overlap another or an input.
  * Low-rank adapters of gate or up are windq_project's; dG and dU below are what their gradients (windq_project_grad with P NULL) start from.
  */
 int windq_gated(const windq_packed* gate /*HOST*/, const windq_packed* up /*HOST*/, const windq_mat* X, int32_t act, void* H, int64_t ld_h,

@@ -449,7 +449,7 @@ static int check_serving(const windq_serving* S, EightShape* E, EightPlan* P) {
     if (!chunk_ok(S->cols, S->chunk_w) || S->rows <= 0 || S->rows > MOST_SIDE || S->unit_rows < 0 || (S->unit_rows != 0 && S->rows % S->unit_rows != 0)) return WINDQ_ESHAPE;
     if (!sizes_fit(0, S->rows, S->cols, 0, 0)) return WINDQ_ESHAPE;
     *E = eight_shape(S->rows, S->cols, S->unit_rows == 0 ? S->rows : S->unit_rows, S->chunk_w);
-    if (S->image_bytes > (size_t)1 << 37) return WINDQ_ESHAPE;
+    if (S->image_bytes > (size_t)EIGHT_MOST) return WINDQ_ESHAPE;
     if ((int64_t)S->image_bytes < E->header) return WINDQ_EINVAL;
     *P = {static_cast<const char*>(S->image), (int64_t)S->image_bytes, E->header};
     return WINDQ_OK;
@@ -531,6 +531,7 @@ extern "C" int windq_serving_layout(const uint8_t* action, int64_t rows, int64_t
         at += eight_bytes(eight_kind(action[u]), E.S, dtype == WINDQ_F32) * E.RB * E.per_chunk;
     }
     image_off[E.U] = at + EIGHT_PAST;
+    if (image_off[E.U] > EIGHT_MOST) return WINDQ_ESHAPE;
     return WINDQ_OK;
 }
 
@@ -541,7 +542,7 @@ extern "C" int windq_serving_lay(const windq_packed* P, const int64_t* image_off
     if (A.mask != nullptr || image_off == nullptr || image == nullptr || !aligned(image_off, 8) || !aligned(image, 256)) return WINDQ_EINVAL;
     if (!sizes_fit(0, A.rows, A.cols, 0, 0)) return WINDQ_ESHAPE;
     const EightShape E = eight_shape(A.rows, A.cols, A.R_u, A.G);
-    if (image_bytes > (size_t)1 << 37) return WINDQ_ESHAPE;
+    if (image_bytes > (size_t)EIGHT_MOST) return WINDQ_ESHAPE;
     if ((int64_t)image_bytes < E.header) return WINDQ_EWORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     return launch_pieces(tokens_in(E.U * E.RB * E.per_chunk, 4), 256,

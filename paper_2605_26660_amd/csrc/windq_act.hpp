@@ -16,7 +16,7 @@ namespace windq {
 __device__ __forceinline__ float exponential(float x) {
     const float h = x * 1.44269504f, l = fmaf(x, 1.44269504f, -h) + x * 1.92596303e-8f;
     const float p = __builtin_amdgcn_exp2f(h);
-    return fabsf(h) < 200.0f ? fmaf(p, l * 0.693147181f, p) : p;      // infinities have no l
+    return h < 127.0f && h > -200.0f ? fmaf(p, l * 0.693147181f, p) : p;      // an infinite p or h has no use for l
 }
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + exponential(-x)); }
 
@@ -37,7 +37,8 @@ __device__ __forceinline__ float activation(int act, float x, float& slope) {
         constexpr float K2 = 1.5957691216057308f;          // 2 sqrt(2 / pi)
         const float x2 = x * x, t = sigmoid(K2 * (x + 0.044715f * x2 * x));
         y = x * t;
-        if (SLOPE) slope = t + x * (t * (1.0f - t)) * (K2 * (1.0f + 0.134145f * x2));
+        const float q = t * (1.0f - t);                    // 0 far from 0, where x^2 may be infinite
+        if (SLOPE) slope = q > 0.0f ? t + x * q * (K2 * (1.0f + 0.134145f * x2)) : t;
     }
     return y;
 }

@@ -82,6 +82,8 @@ __host__ __device__ inline int64_t eight_bytes(int kind, int S, bool w_f32) {
 __host__ __device__ inline int eight_string(int kind, int S) { return kind == 1 ? 16 * S : (kind == 2 ? 8 * S : (kind == 4 ? 4 * S : 4 * ((S + 1) / 2))); }
 constexpr int EIGHT_PAST = 256;                            // bytes past its last fields that an image has: a lane reads whole pieces
 
+constexpr int64_t EIGHT_MOST = (int64_t)1 << 37;           // bytes of an image: 256s of them in 29 bits of a word
+
 struct EightPlan {
     const char* image;
     int64_t bytes;
