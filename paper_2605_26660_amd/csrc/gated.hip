@@ -337,13 +337,14 @@ __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
             load_octet(g + r, Q.rows - r, Q.wide, b);
             load_octet(u + r, Q.rows - r, Q.wide, c);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m = finite_max(finite_max(m, 1.13f * a[i] * c[i]), a[i] * b[i]);
+            for (int i = 0; i < 8; ++i) m = fmaxf(m, fminf(fmaxf(fabsf(a[i] * c[i]), fabsf(a[i] * b[i])), 3.40282347e38f));
         }
 #pragma unroll
         for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
         if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = m;
         __syncthreads();
-        by = power_below(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
+        // a product past fp32 counts as its largest number: what an activation makes of it may be a number again
+        by = power_below(1.13f * fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
         if (threadIdx.x == 0) Q.by_token[t] = 1.0f / by;
     }
     for (int64_t r = threadIdx.x * 8; r < (Q.to != nullptr ? Q.K : Q.rows); r += 2048) {

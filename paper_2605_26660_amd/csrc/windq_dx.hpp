@@ -170,7 +170,8 @@ __device__ __forceinline__ float group_max(const PackArgs& P, int64_t row, int64
     }
     const float s = P.scale[g], o = a >= 5 ? 0.0f : P.offset[g];
     const float L = a == 1 ? 255.0f : (a == 2 ? 15.0f : (a == 3 ? 7.0f : (a == 4 ? 3.0f : 1.0f)));
-    return finite_max(finite_max(m, o), fmaf(s, L, o));
+    const float top = isfinite(s) ? fminf(fabsf(fmaf(s, L, o)), 3.40282347e38f) : 0.0f;       // codes that are there may be smaller ones than L
+    return finite_max(finite_max(m, o), isfinite(o) ? top : 0.0f);
 }
 __device__ __forceinline__ float power_below(float most) {
     const int e = (int)(__float_as_uint(most) >> 23);       // biased; most < 2^(e - 126)

@@ -33,7 +33,7 @@ struct GemmArgs {
     uint32_t col_blocks;
     float* part;               // [splits][T][cols] sums over a part of the rows, or null: one workgroup has them all
     int32_t tiles, each;       // workgroups of a split, its steps of GM_K
-    const float* by_token;     // halves: what a token's results are multiplied by, and an octet of columns'
+    const float* by_token;     // halves: the powers of two that a token's results are multiplied by, and an octet of columns'
     const float* by_octet;
     // Of a pair (windq_gated) `columns` are rows of the gate and of the up, 32 and 32 in turn, and dX is H.
     PackArgs gate;
@@ -60,6 +60,9 @@ inline int64_t gemm_cols(int64_t cols) { return (cols + GM_MOST - 1) / GM_MOST *
 #ifdef __HIPCC__
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// Of a power of two.  Two of them are put on by their exponents: their product, or a result times the first, may lie outside fp32 where the result does not.
+__device__ __forceinline__ int exponent_of(float power) { return (int)((__float_as_uint(power) >> 23) & 0xffu) - 127; }
 
 template <int MF, bool HALF = false, bool PAIR = false>    // fragments of a wavefront along the columns; factors in half precision
 __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
@@ -163,17 +166,17 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             const int64_t t = t0 + wn * 64 + n * 32 + sub;
-            const float token = Q.by_token[t < Q.T ? t : Q.T - 1];
+            const int token = exponent_of(Q.by_token[t < Q.T ? t : Q.T - 1]);
 #pragma unroll
             for (int f = 0; f < MF; ++f) {
                 const int64_t c = c0 + wm * WM + f * 32, row0 = (c >> 6) * 32 + hh * 4;
                 bool bad = false;
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const float octet = Q.by_octet[(c >> 3) + g];
+                    const int by = token + exponent_of(Q.by_octet[(c >> 3) + g]);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        acc[f][n][g * 4 + i] = acc[f][n][g * 4 + i] * token * octet;
+                        acc[f][n][g * 4 + i] = ldexpf(acc[f][n][g * 4 + i], by);
                         bad |= !isfinite(acc[f][n][g * 4 + i]);
                     }
                 }
@@ -238,15 +241,15 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             const int64_t t = t0 + wn * 64 + n * 32 + sub;
-            const float token = Q.by_token[t < Q.T ? t : Q.T - 1];
+            const int token = exponent_of(Q.by_token[t < Q.T ? t : Q.T - 1]);
 #pragma unroll
             for (int f = 0; f < MF; ++f)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const int64_t c = c0 + wm * WM + f * 32 + g * 8;
-                    const float octet = Q.by_octet[(c < Q.cols ? c : 0) >> 3];
+                    const int by = token + exponent_of(Q.by_octet[(c < Q.cols ? c : 0) >> 3]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[f][n][g * 4 + i] = acc[f][n][g * 4 + i] * token * octet;
+                    for (int i = 0; i < 4; ++i) acc[f][n][g * 4 + i] = ldexpf(acc[f][n][g * 4 + i], by);
                 }
         }
     }
