@@ -4,6 +4,7 @@
 #include <math.h>
 
 #include "windq_dx.hpp"
+#include "windq_pair_few.hpp"
 #include "windq_project_any.hpp"
 
 namespace windq {
@@ -239,6 +240,7 @@ int gated_all(ProjectArgs& Q, const windq_mat* X, char* ws, const GatedWs& at, h
             FewArgs F = {Q.P, Q.X, Q.ldx, T, static_cast<uint16_t*>(Q.Y), Q.ldy, nullptr, Q.A, 0, reinterpret_cast<uint4*>(ws + at.frag), reinterpret_cast<float*>(ws + at.few_xs), 0, 0, 0, Q.pair};
             const int steps = Q.P.G % 128 == 0 ? 8 : Q.P.G / 16;
             F.n_kb = (int32_t)(Q.P.cols / (16 * steps));
+            if (T <= PAIR_FEW) return steps == 8 ? launch_pair_few<4>(F, st) : (steps == 6 ? launch_pair_few<3>(F, st) : launch_pair_few<2>(F, st));
             return steps == 8 ? launch_few<8, true>(F, nullptr, st) : (steps == 6 ? launch_few<6, true>(F, nullptr, st) : launch_few<4, true>(F, nullptr, st));
         }
     }

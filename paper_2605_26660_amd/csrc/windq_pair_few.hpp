@@ -1,0 +1,171 @@
+// windq_gated for a few tokens of bfloat16: 16 rows of both matrices a workgroup, the k-blocks shared by its wavefronts, half of them the gate's.
+//
+// Bound by unpacking and waits, not by the codes (28 MB at 2 bits for a pair of 11008 x 4096).  Tokens are the M side of 16x16x32 instructions and rows the N
+// side, so that a lane has one row, with one scale and one offset, and a quarter of a k-block's columns side by side: its codes are one load of 4 to 32 bytes,
+// straight to registers, and nothing but trits' table and the totals goes through LDS.  Few registers leave room for five or six wavefronts a SIMD, which
+// wait for each other's loads; treatments and places of codes are looked up for all of a wavefront's k-blocks at once, ahead.
+#pragma once
+
+#include "windq_project_few.hpp"
+
+namespace windq {
+
+constexpr int PR_ROWS = 16;
+constexpr int64_t PAIR_FEW = 16;
+
+#ifdef __HIPCC__
+
+// O octets of a row (columns side by side) as f, from their first byte; r: trits ahead of them.
+template <int O, int BITS>
+__device__ __forceinline__ void pair_fields(const uint8_t* __restrict__ p, uint4 (&w)[O]) {
+    uint32_t v[2 * O + 1] = {};
+#pragma unroll
+    for (int k = 0; k + 4 <= O * BITS; k += 4) __builtin_memcpy(&v[k >> 2], p + k, 4);
+    if constexpr (O * BITS % 4 != 0) {
+        uint8_t rest[4] = {};
+#pragma unroll
+        for (int k = 0; k < O * BITS % 4; ++k) rest[k] = p[O * BITS / 4 * 4 + k];
+        v[O * BITS / 4] = (uint32_t)rest[0] | (uint32_t)rest[1] << 8 | (uint32_t)rest[2] << 16;
+    }
+#pragma unroll
+    for (int s = 0; s < O; ++s) {
+        constexpr int STEP = BITS * 8;
+        const int at = s * STEP;
+        if constexpr (BITS == 1) w[s] = fields1((v[0] >> at) & 0xffu);
+        else if constexpr (BITS == 2) w[s] = fields2((v[at >> 5] >> (at & 31)) & 0xffffu);
+        else if constexpr (BITS == 3) w[s] = fields3((at & 31) <= 8 ? (v[at >> 5] >> (at & 31)) & 0xffffffu : __builtin_amdgcn_alignbit(v[(at >> 5) + 1], v[at >> 5], at & 31) & 0xffffffu);
+        else if constexpr (BITS == 4) w[s] = fields4(v[s]);
+        else w[s] = fields8(v[2 * s], v[2 * s + 1]);
+    }
+}
+
+template <int O>
+__device__ __forceinline__ void pair_trits(const uint8_t* __restrict__ p, uint32_t r, const uint16_t* __restrict__ trits_of, uint4 (&w)[O]) {
+    uint32_t b[2], t[8], v[3];
+    __builtin_memcpy(b, p, 8);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) t[k] = trits_of[(b[k >> 2] >> (8 * (k & 3))) & 0xffu];
+    // 80 bits, two a trit
+    v[0] = t[0] | t[1] << 10 | t[2] << 20 | t[3] << 30;
+    v[1] = t[3] >> 2 | t[4] << 8 | t[5] << 18 | t[6] << 28;
+    v[2] = t[6] >> 4 | t[7] << 6;
+    if (O == 2 && r >= 16) {                                // r is below 16 for wider k-blocks
+        v[0] = v[1];
+        v[1] = v[2];
+        r -= 16;
+    }
+    v[0] = __builtin_amdgcn_alignbit(v[1], v[0], 2 * r);
+    if (O > 2) v[1] = __builtin_amdgcn_alignbit(v[2], v[1], 2 * r);
+#pragma unroll
+    for (int s = 0; s < O; ++s) w[s] = fields2((s & 1) != 0 ? v[s >> 1] >> 16 : v[s >> 1] & 0xffffu);
+}
+
+template <int O, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 6) void pair_few_kernel(const FewArgs Q) {
+    constexpr int EACH = WAVES / 2, COLS = 32 * O;          // wavefronts of a matrix; columns of a k-block
+    __shared__ float red[WAVES][4][64];
+    __shared__ uint16_t trits_of[256];
+    for (int i = threadIdx.x; i < 256; i += WAVES * 64) trits_of[i] = (uint16_t)trit_fields(i);
+    __syncthreads();
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
+    const int matrix = wave / EACH, turn = wave - matrix * EACH;
+    const PackArgs& P = matrix == 1 ? Q.pair.up : Q.P;
+    const int64_t row0 = (int64_t)blockIdx.x * PR_ROWS, rb = row0 / P.R_u, lrow0 = row0 - rb * P.R_u;
+    const int32_t rows_left = P.R_u - lrow0 < PR_ROWS ? (int32_t)(P.R_u - lrow0) : PR_ROWS;
+    const int32_t lr = sub < rows_left ? sub : rows_left - 1;
+    const int32_t per_chunk = P.G / COLS;
+    const uint32_t one = 0x3f803f80u;
+    const bf16x8 ones = as_bf16x8(make_uint4(one, one, one, one));
+    const uint16_t* const x0 = Q.X + (sub < Q.T ? sub : Q.T - 1) * Q.ldx + q * (8 * O);
+
+    f32x4 tot = {};
+    for (int32_t from = turn; from < Q.n_kb; from += 64 * EACH) {
+        // where the unit's rows start, with its treatment above, of the wavefront's next 64 k-blocks, a lane each
+        const int32_t mine = from + lane * EACH;
+        uint64_t word = 0;
+        if (mine < Q.n_kb) {
+            int64_t base;
+            const int a = pk_action(P, rb * P.n_chunks + mine / per_chunk, base);
+            if (a != 0) word = (uint64_t)reinterpret_cast<uintptr_t>(P.codes + base + lrow0 * pk_bytes_per_group(a, P.G)) | (uint64_t)a << 56;
+        }
+        const int32_t count = (Q.n_kb - from + EACH - 1) / EACH < 64 ? (Q.n_kb - from + EACH - 1) / EACH : 64;
+        for (int32_t it = 0; it < count; ++it) {
+            const int32_t kb = from + it * EACH, j = kb / per_chunk, c = kb - j * per_chunk;
+            const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(word >> 32), it);
+            const int kind = (int)(hi >> 24);
+            const uint8_t* const codes = reinterpret_cast<const uint8_t*>((uint64_t)(hi & 0xffffffu) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)word, it));
+            const int64_t g = (rb * P.n_chunks + j) * P.R_u + lrow0 + lr;
+            const float scale = P.scale[g], offset = P.offset[g];
+            uint4 x[O], w[O];
+#pragma unroll
+            for (int s = 0; s < O; ++s) x[s] = reinterpret_cast<const uint4*>(x0 + (int64_t)kb * COLS)[s];
+            const int32_t bpg = (int32_t)pk_bytes_per_group(kind, P.G), first = c * COLS + q * (8 * O);
+            const uint8_t* const row = codes + lr * bpg;
+            switch (kind) {
+                case 1: pair_fields<O, 8>(row + first, w); break;
+                case 2: pair_fields<O, 4>(row + (first >> 1), w); break;
+                case 3: pair_fields<O, 3>(row + (first >> 3) * 3, w); break;
+                case 4: pair_fields<O, 2>(row + (first >> 2), w); break;
+                case 5: {
+                    const uint32_t k = (uint32_t)first / 5u, at = k < (uint32_t)bpg - 8u ? k : (uint32_t)bpg - 8u;      // eight bytes within the row
+                    pair_trits<O>(row + at, (uint32_t)first - at * 5u, trits_of, w);
+                    break;
+                }
+                case 6: pair_fields<O, 1>(row + (first >> 3), w); break;
+                default: {
+                    const uint16_t* const from = static_cast<const uint16_t*>(P.W) + (rb * P.R_u + lrow0 + lr) * P.ld + (int64_t)kb * COLS + q * (8 * O);
+#pragma unroll
+                    for (int s = 0; s < O; ++s) w[s] = P.w_f32 != 0 ? make_uint4(0u, 0u, 0u, 0u) : reinterpret_cast<const uint4*>(from)[s];
+                }
+            }
+            f32x4 acc = {}, sums = {};
+#pragma unroll
+            for (int s = 0; s < O; ++s) {
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(x[s]), as_bf16x8(w[s]), acc, 0, 0, 0);
+                sums = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(x[s]), ones, sums, 0, 0, 0);
+            }
+            if (kind == 0 && P.w_f32 != 0) {
+#pragma unroll 1
+                for (int i = 0; i < 3 * O; ++i) {           // rare: three terms of an octet, x once more from where it lies
+                    const int term = i / O, s = i - term * O;
+                    const uint4 v = skip_octet(P, rb * P.R_u + lrow0 + lr, (int64_t)kb * COLS + q * (8 * O) + s * 8, term);
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(reinterpret_cast<const uint4*>(x0 + (int64_t)kb * COLS)[s]), as_bf16x8(v), acc, 0, 0, 0);
+                }
+            }
+            float alpha, beta;
+            pk_affine(kind, scale, offset, false, alpha, beta);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tot[i] = fmaf(alpha, acc[i], fmaf(beta, sums[i], tot[i]));
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) red[wave][i][lane] = tot[i];
+    __syncthreads();
+    for (int e = threadIdx.x; e < PR_ROWS * Q.T; e += WAVES * 64) {
+        const int r = e & 15, n = e >> 4, at = (n >> 2) * 16 + r;      // neighbouring lanes: neighbouring rows of a token
+        if (r >= rows_left) continue;
+        float v = 0.0f, up = 0.0f;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            v += red[k][n & 3][at];
+            up += red[EACH + k][n & 3][at];
+        }
+        const int64_t row = row0 + r;
+        if (!isfinite(v)) v = (float)pk_slow_dot(Q.P, row, Q.X + n * Q.ldx);
+        if (!isfinite(up)) up = (float)pk_slow_dot(Q.pair.up, row, Q.X + n * Q.ldx);
+        store_y(Q.Y + n * Q.ldy + row, pair_result<uint16_t>(Q.pair, n, row, v, up));
+    }
+}
+
+template <int O>
+int launch_pair_few(const FewArgs& Q, hipStream_t st) {
+    const int64_t wgs = tokens_in(Q.P.rows, PR_ROWS);
+    if (!fits_launch(wgs, 1024)) return WINDQ_ESHAPE;
+    if (wgs > 512) pair_few_kernel<O, 8><<<dim3((uint32_t)wgs), dim3(512), 0, st>>>(Q);
+    else pair_few_kernel<O, 16><<<dim3((uint32_t)wgs), dim3(1024), 0, st>>>(Q);
+    return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
+}
+
+#endif  // __HIPCC__
+
+}  // namespace windq
