@@ -70,50 +70,53 @@ __global__ __launch_bounds__(WAVES * 64, 6) void pair_few_kernel(const FewArgs Q
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
     const int matrix = wave / EACH, turn = wave - matrix * EACH;
     const PackArgs& P = matrix == 1 ? Q.pair.up : Q.P;
-    const int64_t row0 = (int64_t)blockIdx.x * PR_ROWS, rb = row0 / P.R_u, lrow0 = row0 - rb * P.R_u;
-    const int32_t rows_left = P.R_u - lrow0 < PR_ROWS ? (int32_t)(P.R_u - lrow0) : PR_ROWS;
-    const int32_t lr = sub < rows_left ? sub : rows_left - 1;
+    const uint32_t R_u = (uint32_t)P.R_u, row0 = blockIdx.x * PR_ROWS, rb = row0 / R_u, lrow0 = row0 - rb * R_u;
+    const int32_t rows_left = R_u - lrow0 < PR_ROWS ? (int32_t)(R_u - lrow0) : PR_ROWS;
+    const uint32_t lr = (uint32_t)(sub < rows_left ? sub : rows_left - 1);
     const int32_t per_chunk = P.G / COLS;
+    const int64_t unit0 = (int64_t)rb * P.n_chunks;
     const uint32_t one = 0x3f803f80u;
     const bf16x8 ones = as_bf16x8(make_uint4(one, one, one, one));
     const uint16_t* const x0 = Q.X + (sub < Q.T ? sub : Q.T - 1) * Q.ldx + q * (8 * O);
 
     f32x4 tot = {};
     for (int32_t from = turn; from < Q.n_kb; from += 64 * EACH) {
-        // where the unit's rows start, with its treatment above, of the wavefront's next 64 k-blocks, a lane each
+        // of the wavefront's next 64 k-blocks, a lane each: the chunk, and where the unit's rows start, with bytes of a row and treatment above
         const int32_t mine = from + lane * EACH;
         uint64_t word = 0;
+        uint32_t chunk = 0;
         if (mine < Q.n_kb) {
+            chunk = (uint32_t)mine / (uint32_t)per_chunk;
             int64_t base;
-            const int a = pk_action(P, rb * P.n_chunks + mine / per_chunk, base);
-            if (a != 0) word = (uint64_t)reinterpret_cast<uintptr_t>(P.codes + base + lrow0 * pk_bytes_per_group(a, P.G)) | (uint64_t)a << 56;
+            const int a = pk_action(P, unit0 + chunk, base);
+            const int64_t bytes = pk_bytes_per_group(a, P.G);
+            if (a != 0) word = (uint64_t)(base + lrow0 * bytes) | (uint64_t)bytes << 48 | (uint64_t)a << 61;      // tensors are no longer than 2^42 bytes
         }
         const int32_t count = (Q.n_kb - from + EACH - 1) / EACH < 64 ? (Q.n_kb - from + EACH - 1) / EACH : 64;
         for (int32_t it = 0; it < count; ++it) {
-            const int32_t kb = from + it * EACH, j = kb / per_chunk, c = kb - j * per_chunk;
-            const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(word >> 32), it);
-            const int kind = (int)(hi >> 24);
-            const uint8_t* const codes = reinterpret_cast<const uint8_t*>((uint64_t)(hi & 0xffffffu) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)word, it));
-            const int64_t g = (rb * P.n_chunks + j) * P.R_u + lrow0 + lr;
-            const float scale = P.scale[g], offset = P.offset[g];
+            const int32_t kb = from + it * EACH, j = __builtin_amdgcn_readlane((int)chunk, it), c = kb - j * per_chunk;
+            const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(word >> 32), it), bpg = hi >> 16 & 0x1fffu;
+            const int kind = (int)(hi >> 29);
+            const uint8_t* const codes = P.codes + ((uint64_t)(hi & 0xffffu) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)word, it));
+            const int64_t g = (unit0 + j) * R_u + lrow0;
+            const float scale = (P.scale + g)[lr], offset = (P.offset + g)[lr];
             uint4 x[O], w[O];
 #pragma unroll
             for (int s = 0; s < O; ++s) x[s] = reinterpret_cast<const uint4*>(x0 + (int64_t)kb * COLS)[s];
-            const int32_t bpg = (int32_t)pk_bytes_per_group(kind, P.G), first = c * COLS + q * (8 * O);
-            const uint8_t* const row = codes + lr * bpg;
+            const uint32_t first = (uint32_t)c * COLS + q * (8 * O), row = lr * bpg;
             switch (kind) {
-                case 1: pair_fields<O, 8>(row + first, w); break;
-                case 2: pair_fields<O, 4>(row + (first >> 1), w); break;
-                case 3: pair_fields<O, 3>(row + (first >> 3) * 3, w); break;
-                case 4: pair_fields<O, 2>(row + (first >> 2), w); break;
+                case 1: pair_fields<O, 8>(codes + (row + first), w); break;
+                case 2: pair_fields<O, 4>(codes + (row + (first >> 1)), w); break;
+                case 3: pair_fields<O, 3>(codes + (row + (first >> 3) * 3), w); break;
+                case 4: pair_fields<O, 2>(codes + (row + (first >> 2)), w); break;
                 case 5: {
-                    const uint32_t k = (uint32_t)first / 5u, at = k < (uint32_t)bpg - 8u ? k : (uint32_t)bpg - 8u;      // eight bytes within the row
-                    pair_trits<O>(row + at, (uint32_t)first - at * 5u, trits_of, w);
+                    const uint32_t k = first / 5u, at = k < bpg - 8u ? k : bpg - 8u;      // eight bytes within the row
+                    pair_trits<O>(codes + (row + at), first - at * 5u, trits_of, w);
                     break;
                 }
-                case 6: pair_fields<O, 1>(row + (first >> 3), w); break;
+                case 6: pair_fields<O, 1>(codes + (row + (first >> 3)), w); break;
                 default: {
-                    const uint16_t* const from = static_cast<const uint16_t*>(P.W) + (rb * P.R_u + lrow0 + lr) * P.ld + (int64_t)kb * COLS + q * (8 * O);
+                    const uint16_t* const from = static_cast<const uint16_t*>(P.W) + (int64_t)(row0 + lr) * P.ld + (int64_t)kb * COLS + q * (8 * O);
 #pragma unroll
                     for (int s = 0; s < O; ++s) w[s] = P.w_f32 != 0 ? make_uint4(0u, 0u, 0u, 0u) : reinterpret_cast<const uint4*>(from)[s];
                 }
@@ -128,7 +131,7 @@ __global__ __launch_bounds__(WAVES * 64, 6) void pair_few_kernel(const FewArgs Q
 #pragma unroll 1
                 for (int i = 0; i < 3 * O; ++i) {           // rare: three terms of an octet, x once more from where it lies
                     const int term = i / O, s = i - term * O;
-                    const uint4 v = skip_octet(P, rb * P.R_u + lrow0 + lr, (int64_t)kb * COLS + q * (8 * O) + s * 8, term);
+                    const uint4 v = skip_octet(P, row0 + lr, (int64_t)kb * COLS + q * (8 * O) + s * 8, term);
                     acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(reinterpret_cast<const uint4*>(x0 + (int64_t)kb * COLS)[s]), as_bf16x8(v), acc, 0, 0, 0);
                 }
             }
@@ -150,7 +153,7 @@ __global__ __launch_bounds__(WAVES * 64, 6) void pair_few_kernel(const FewArgs Q
             v += red[k][n & 3][at];
             up += red[EACH + k][n & 3][at];
         }
-        const int64_t row = row0 + r;
+        const int64_t row = (int64_t)row0 + r;
         if (!isfinite(v)) v = (float)pk_slow_dot(Q.P, row, Q.X + n * Q.ldx);
         if (!isfinite(up)) up = (float)pk_slow_dot(Q.pair.up, row, Q.X + n * Q.ldx);
         store_y(Q.Y + n * Q.ldy + row, pair_result<uint16_t>(Q.pair, n, row, v, up));

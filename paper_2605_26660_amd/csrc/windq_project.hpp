@@ -73,16 +73,10 @@ __device__ __forceinline__ int adapter_rank(const AdapterArgs& A, int k) {
     return r < 0 ? 0 : (r > A.max_rank ? A.max_rank : r);
 }
 
+// Without branches: lanes of different treatments would take turns.
 __device__ __forceinline__ int64_t pk_bytes_per_group(int a, int G) {
-    switch (a) {
-        case 1: return G;
-        case 2: return G >> 1;
-        case 3: return (G * 3) >> 3;
-        case 4: return G >> 2;
-        case 5: return (G + 4) / 5;
-        case 6: return G >> 3;
-        default: return 0;
-    }
+    const uint32_t bits = 0x01023480u >> (4 * (a & 7)) & 15u;
+    return a == 5 ? (G + 4) / 5 : (int)((uint32_t)G * bits >> 3);
 }
 
 // The treatment of unit u and where its codes start; an entry that does not fit counts as skip.
