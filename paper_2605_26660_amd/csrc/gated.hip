@@ -5,6 +5,7 @@
 
 #include "windq_dx.hpp"
 #include "windq_pair_few.hpp"
+#include "windq_pair_gemm.hpp"
 #include "windq_project_any.hpp"
 
 namespace windq {
@@ -66,7 +67,7 @@ struct HalvesArgs {
 // Bound by latency: loads wait for the stores ahead of them, so that few registers and many wavefronts count.
 constexpr int HALVES_UNITS = 512, HALVES_ROWS = 16;
 
-template <bool KNOWN>                                      // units of whole blocks of rows, and few enough of them in a row
+template <bool KNOWN, bool PLAIN>                          // units of whole blocks of rows, and few enough of them in a row; no mask besides
 __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, const int64_t first) {
     __shared__ float most[4][2];
     __shared__ uint16_t trits_of[256];
@@ -133,7 +134,18 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
         };
         if (c < P.cols) {
             const uint32_t j = (uint32_t)c / (uint32_t)P.G;
-            if constexpr (KNOWN) {
+            if constexpr (PLAIN) {
+                const uint64_t unit = units[j];
+                uint4 h[2];
+                half_rows<2>(P, here, c, rb * P.n_chunks + j, here - rb * P.R_u, ((int)c - (int)j * P.G) >> 3, (int)(unit >> 56), (int64_t)(unit & 0xffffffffffffffull), trits_of, by, h);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    w[i][0] = h[i].x;
+                    w[i][1] = h[i].y;
+                    w[i][2] = h[i].z;
+                    w[i][3] = h[i].w;
+                }
+            } else if constexpr (KNOWN) {
                 const uint64_t unit = units[j];
                 rows_of<2>(P, here, c, rb * P.n_chunks + j, here - rb * P.R_u, ((int)c - (int)j * P.G) >> 3, (int)(unit >> 56), (int64_t)(unit & 0xffffffffffffffull), trits_of, put);
             } else {
@@ -155,13 +167,17 @@ int launch_gated_halves(const ProjectArgs& Q, char* ws, const GatedWs& at, hipSt
     const int64_t K = gemm_k(Q.P.cols), rows = gated_rows(Q.P.rows), tall = tokens_in(Q.T, GM_N);
     const HalvesArgs H = {{Q.P, Q.pair.up}, Q.X, Q.ldx, Q.T, K, reinterpret_cast<uint16_t*>(ws + at.x), reinterpret_cast<float*>(ws + at.by_token),
                           reinterpret_cast<uint16_t*>(ws + at.w), reinterpret_cast<float*>(ws + at.by_octet)};
+    const bool mask = Q.P.mask != nullptr || Q.pair.up.mask != nullptr;
     const bool known = (Q.P.R_u == Q.P.rows || Q.P.R_u % HALVES_ROWS == 0) && Q.P.n_chunks <= HALVES_UNITS;
     const int status = launch_pieces(Q.T + 2 * tokens_in(Q.P.rows, HALVES_ROWS), 256, [&](int64_t first, dim3 g) {
-        if (known) gated_halves_kernel<true><<<g, dim3(256), 0, st>>>(H, first);
-        else gated_halves_kernel<false><<<g, dim3(256), 0, st>>>(H, first);
+        if (known && !mask) gated_halves_kernel<true, true><<<g, dim3(256), 0, st>>>(H, first);
+        else if (known) gated_halves_kernel<true, false><<<g, dim3(256), 0, st>>>(H, first);
+        else gated_halves_kernel<false, false><<<g, dim3(256), 0, st>>>(H, first);
     });
     if (status != WINDQ_OK) return status;
-    const int64_t by = rows / 256 * tall >= GM_TILES ? 256 : 128, tiles = rows / by * tall;
+    const int64_t by = rows / 256 * tall >= GM_TILES ? 256 : 128, large = rows / GM_MOST * tokens_in(Q.T, GW_N);
+    const bool wide = gemm_wide(large, rows / by * tall);
+    const int64_t tiles = wide ? large : rows / by * tall;
     GemmArgs M = {};
     M.wt = H.w;
     M.dY = H.x;
@@ -171,7 +187,7 @@ int launch_gated_halves(const ProjectArgs& Q, char* ws, const GatedWs& at, hipSt
     M.cols = rows;
     M.dX = static_cast<uint16_t*>(Q.Y);
     M.ldx = Q.ldy;
-    M.col_blocks = (uint32_t)(rows / by);
+    M.col_blocks = (uint32_t)(rows / (wide ? GM_MOST : by));
     M.tiles = (int32_t)tiles;
     M.each = (int32_t)(K / GM_K);
     M.by_token = H.by_token;
@@ -181,7 +197,8 @@ int launch_gated_halves(const ProjectArgs& Q, char* ws, const GatedWs& at, hipSt
     M.raw = Q.X;
     M.ld_raw = Q.ldx;
     // tiles are no more than 2^31 / (64 x 128) and two sides' edges: one launch holds them
-    if (by == 256) dx_gemm_kernel<4, true, true><<<dim3((uint32_t)tiles), dim3(GM_THREADS), 0, st>>>(M);
+    if (wide) pair_gemm_kernel<<<dim3((uint32_t)tiles), dim3(GW_THREADS), 0, st>>>(M);
+    else if (by == 256) dx_gemm_kernel<4, true, true><<<dim3((uint32_t)tiles), dim3(GM_THREADS), 0, st>>>(M);
     else dx_gemm_kernel<2, true, true><<<dim3((uint32_t)tiles), dim3(GM_THREADS), 0, st>>>(M);
     return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
 }
@@ -422,6 +439,7 @@ struct GatedTurnArgs {
     float* by_octet;
 };
 
+template <bool PLAIN>
 __global__ __launch_bounds__(256) void gated_turn_kernel(const GatedTurnArgs Q, const int64_t first) {
     const int64_t id = first + blockIdx.x;
     const int m = id >= Q.turns ? 1 : 0;
@@ -438,7 +456,7 @@ __global__ __launch_bounds__(256) void gated_turn_kernel(const GatedTurnArgs Q, 
     for (int d = 16; d >= 1; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 32));
     const float by = power_below(most);
     if (id - cb * row_blocks == 0 && (threadIdx.x & 31) == 0 && col < P.cols) Q.by_octet[col >> 3] = 1.0f / by;
-    turn<_Float16>(P, Q.K, 2 * (int64_t)Q.K, by, Q.wt + (int64_t)m * Q.K, block);
+    turn<_Float16, PLAIN>(P, Q.K, 2 * (int64_t)Q.K, by, Q.wt + (int64_t)m * Q.K, block);
 }
 
 struct GatedGradWs {
@@ -497,7 +515,11 @@ int gated_grad_all(SlopeArgs& S, void* dX, int64_t ld_dx, char* ws, const GatedG
         const int32_t K2 = (int32_t)(2 * at.K);
         const GatedTurnArgs R = {{S.P[0], S.P[1]}, (int32_t)at.K, reinterpret_cast<uint16_t*>(ws + at.wt), ((cols + 63) / 64) * ((at.K + 255) / 256), S.range, S.strips,
                                  reinterpret_cast<float*>(ws + at.by_octet)};
-        status = launch_pieces(2 * R.turns, 256, [&](int64_t first, dim3 g) { gated_turn_kernel<<<g, dim3(256), 0, st>>>(R, first); });
+        const bool plain = P.mask == nullptr && S.P[1].mask == nullptr && P.rows % 8 == 0 && (P.R_u == P.rows || P.R_u % 8 == 0);
+        status = launch_pieces(2 * R.turns, 256, [&](int64_t first, dim3 g) {
+            if (plain) gated_turn_kernel<true><<<g, dim3(256), 0, st>>>(R, first);
+            else gated_turn_kernel<false><<<g, dim3(256), 0, st>>>(R, first);
+        });
         if (status != WINDQ_OK) return status;
         // tiles are no more than 2^31 / 128^2 and two sides' edges: one launch holds them
         const int64_t tall = tokens_in(T, GM_N), by = tokens_in(cols, 256) * tall >= GM_TILES ? 256 : 128, tiles = tokens_in(cols, by) * tall;

@@ -125,6 +125,77 @@ __device__ __forceinline__ void eight_rows(const PackArgs& P, int64_t r0, int64_
     }
 }
 
+// Fields as half precision numbers, two a word in their order: 4 + field, +-1, 16 + field, 8 + field as for bfloat16, three more bits of mantissa behind them.
+__device__ __forceinline__ uint4 half_fields2(uint32_t v) {
+    const uint32_t t = twice(v, 14, v);
+    return make_uint4(((t << 8) & 0x03000300u) | 0x44004400u, ((t << 4) & 0x03000300u) | 0x44004400u, (t & 0x03000300u) | 0x44004400u, ((t >> 4) & 0x03000300u) | 0x44004400u);
+}
+__device__ __forceinline__ uint4 half_fields1(uint32_t v) {
+    const uint32_t n = ~v, t = twice(n, 15, n & 0xffu);
+    return make_uint4(((t << 15) & 0x80008000u) | 0x3c003c00u, ((t << 13) & 0x80008000u) | 0x3c003c00u, ((t << 11) & 0x80008000u) | 0x3c003c00u, ((t << 9) & 0x80008000u) | 0x3c003c00u);
+}
+__device__ __forceinline__ uint4 half_fields4(uint32_t v) {
+    const uint32_t e = twice(v, 12, v & 0xffffu), o = twice(v >> 16, 12, v >> 16);
+    return make_uint4(((e << 6) & 0x03c003c0u) | 0x4c004c00u, ((e >> 2) & 0x03c003c0u) | 0x4c004c00u, ((o << 6) & 0x03c003c0u) | 0x4c004c00u, ((o >> 2) & 0x03c003c0u) | 0x4c004c00u);
+}
+__device__ __forceinline__ uint4 half_fields3(uint32_t v) {
+    return make_uint4(((v << 7) & 0x380u) | ((v << 20) & 0x3800000u) | 0x48004800u, ((v << 1) & 0x380u) | ((v << 14) & 0x3800000u) | 0x48004800u,
+                      ((v >> 5) & 0x380u) | ((v << 8) & 0x3800000u) | 0x48004800u, ((v >> 11) & 0x380u) | ((v << 2) & 0x3800000u) | 0x48004800u);
+}
+
+// Two weights as half precision numbers: f scale + beta in fp32, rounded once.
+__device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
+    return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)lo) | (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)hi) << 16;
+}
+
+// ROWS rows by eight columns of w_hat times `by`, a power of two, in half precision, within a unit whose treatment and first byte are known; no mask.  Five
+// instructions a weight, where putting on the mask, the power and the centre one by one takes eleven.
+template <int ROWS>
+__device__ __forceinline__ void half_rows(const PackArgs& P, int64_t r0, int64_t col, int64_t u, int64_t lrow, int o, int a, int64_t base, const uint16_t* __restrict__ trits_of,
+                                          float by, uint4 (&w)[ROWS]) {
+    if (a == 0) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            float v[8];
+            skip_row(P, r0 + i, col, v);
+            w[i] = make_uint4(half_pair(v[0] * by, v[1] * by), half_pair(v[2] * by, v[3] * by), half_pair(v[4] * by, v[5] * by), half_pair(v[6] * by, v[7] * by));
+        }
+        return;
+    }
+    const int32_t nb = (int32_t)pk_bytes_per_group(a, P.G);
+    const uint8_t* const first = P.codes + base + lrow * nb;
+    float sc[ROWS], be[ROWS];
+    __builtin_memcpy(sc, P.scale + u * P.R_u + lrow, 4 * ROWS);
+    __builtin_memcpy(be, P.offset + u * P.R_u + lrow, 4 * ROWS);
+    uint4 f[ROWS];
+    auto rows = [&](auto octet) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) f[i] = octet(first + i * nb);
+    };
+    switch (a) {
+        case 1: rows([&](const uint8_t* p) {
+            uint2 q;
+            __builtin_memcpy(&q, p + o * 8, 8);
+            auto byte = [&](int k) { return (float)(((k < 4 ? q.x : q.y) >> (8 * (k & 3))) & 0xffu); };
+            return make_uint4(half_pair(byte(0), byte(1)), half_pair(byte(2), byte(3)), half_pair(byte(4), byte(5)), half_pair(byte(6), byte(7)));
+        }); break;
+        case 2: rows([&](const uint8_t* p) { uint32_t q; __builtin_memcpy(&q, p + o * 4, 4); return half_fields4(q); }); break;
+        case 3: rows([&](const uint8_t* p) { return half_fields3((uint32_t)p[o * 3] | (uint32_t)p[o * 3 + 1] << 8 | (uint32_t)p[o * 3 + 2] << 16); }); break;
+        case 4: rows([&](const uint8_t* p) { uint16_t q; __builtin_memcpy(&q, p + o * 2, 2); return half_fields2(q); }); break;
+        case 5: rows([&](const uint8_t* p) { return half_fields2(octet_trits(p, o, trits_of) & 0xffffu); }); break;
+        default: rows([&](const uint8_t* p) { return half_fields1(p[o]); }); break;
+    }
+    const float f0 = pk_f0(a);
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const float s = sc[i] * by, b = fmaf(-f0, s, a >= 5 ? 0.0f : be[i] * by);
+        auto two = [&](uint32_t q) {
+            return half_pair(fmaf((float)__builtin_bit_cast(_Float16, (uint16_t)q), s, b), fmaf((float)__builtin_bit_cast(_Float16, (uint16_t)(q >> 16)), s, b));
+        };
+        w[i] = make_uint4(two(f[i].x), two(f[i].y), two(f[i].z), two(f[i].w));
+    }
+}
+
 template <typename HT>
 __device__ __forceinline__ uint32_t half_bits(float x) {
     if constexpr (__is_same(HT, _Float16)) return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)x);
@@ -132,8 +203,8 @@ __device__ __forceinline__ uint32_t half_bits(float x) {
 }
 
 // w_hat rounded to bfloat16 and turned: wt [cols][ld], zeros from the last row to K.  A thread has eight rows by eight columns.  In half precision (_Float16)
-// weights are multiplied by a power of two first, the same for an octet of columns.
-template <typename HT>
+// weights are multiplied by a power of two first, the same for an octet of columns.  PLAIN: so, with no mask and whole eights of rows.
+template <typename HT, bool PLAIN = false>
 __device__ __forceinline__ void turn(const PackArgs& P, int32_t K, int64_t ld, float by, uint16_t* __restrict__ wt, int64_t block) {
     __shared__ uint16_t trits_of[256];
     trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
@@ -143,6 +214,28 @@ __device__ __forceinline__ void turn(const PackArgs& P, int32_t K, int64_t ld, f
     const int64_t r0 = (block - cb * row_blocks) * 256 + (threadIdx.x & 31) * 8, col = cb * 64 + (threadIdx.x >> 5) * 8;
     if (col >= P.cols || r0 >= K) return;
     uint32_t v[8][4];
+    if constexpr (PLAIN) {
+        uint4 w[8] = {};
+        if (r0 < P.rows) {
+            const uint32_t R_u = (uint32_t)P.R_u, rb = (uint32_t)r0 / R_u, lrow = (uint32_t)r0 - rb * R_u;
+            const uint32_t j = (uint32_t)col / (uint32_t)P.G;
+            const int64_t u = (int64_t)rb * P.n_chunks + j;
+            int64_t base;
+            const int a = pk_action(P, u, base);
+            half_rows<8>(P, r0, col, u, lrow, ((int)col - (int)j * P.G) >> 3, a, base, trits_of, by, w);
+        }
+#pragma unroll
+        for (int m = 0; m < 8; ++m) {
+            uint32_t t[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                auto word = [&](uint4 x) { return (m >> 1) == 0 ? x.x : ((m >> 1) == 1 ? x.y : ((m >> 1) == 2 ? x.z : x.w)); };
+                t[i] = __builtin_amdgcn_perm(word(w[2 * i + 1]), word(w[2 * i]), (m & 1) != 0 ? 0x07060302u : 0x05040100u);
+            }
+            *reinterpret_cast<uint4*>(wt + (col + m) * ld + r0) = make_uint4(t[0], t[1], t[2], t[3]);
+        }
+        return;
+    }
     eight_rows(P, r0, col, trits_of, [&](int i, int m, float x) {
         const uint32_t b = half_bits<HT>(__is_same(HT, _Float16) ? x * by : x);
         v[m][i >> 1] = (i & 1) != 0 ? v[m][i >> 1] | b << 16 : b;

@@ -64,6 +64,92 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 // Of a power of two.  Two of them are put on by their exponents: their product, or a result times the first, may lie outside fp32 where the result does not.
 __device__ __forceinline__ int exponent_of(float power) { return (int)((__float_as_uint(power) >> 23) & 0xffu) - 127; }
 
+// H, G and U of a pair's tile: a wavefront has MF x 2 fragments, 2 p and 2 p + 1 along the rows are the gate's and the up's of the same 32 rows.  What is written
+// goes through LDS (`out`), one after the other: a lane has four rows of a token, and 8 bytes of each of 32 tokens are written at a third of the rate of whole lines.
+template <int MF, int THREADS>
+__device__ __forceinline__ void pair_tile(const GemmArgs& Q, f32x16 (&acc)[MF][2], uint16_t* const out, int64_t c0, int64_t t0, int wm, int wn, int tid) {
+    constexpr int ROWS = MF * 32, LD = ROWS + 8, WM = MF * 32, TOKENS = THREADS / 2;       // of a token in LDS; of a tile
+    const int64_t rows = Q.gate.rows;
+    const int lane = tid & 63, sub = lane & 31, hh = lane >> 5;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        const int64_t t = t0 + wn * 64 + n * 32 + sub;
+        const int token = exponent_of(Q.by_token[t < Q.T ? t : Q.T - 1]);
+#pragma unroll
+        for (int f = 0; f < MF; ++f) {
+            const int64_t c = c0 + wm * WM + f * 32, first = (c >> 6) * 32 + hh * 4;
+            bool bad = false;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int by = token + exponent_of(Q.by_octet[(c >> 3) + g]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    acc[f][n][g * 4 + i] = ldexpf(acc[f][n][g * 4 + i], by);
+                    bad |= !isfinite(acc[f][n][g * 4 + i]);
+                }
+            }
+            // what is not finite so far: weight by weight
+            if (__any(bad && first < rows && t < Q.T)) {
+#pragma unroll 1
+                for (int i = 0; i < 16; ++i) {
+                    const int64_t row = first + (i >> 2) * 8 + (i & 3);
+                    float v = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) v = i == k ? acc[f][n][k] : v;
+                    if (!isfinite(v) && row < rows && t < Q.T) v = (float)pk_slow_dot((f & 1) == 0 ? Q.gate : Q.pair.up, row, Q.raw + t * Q.ld_raw);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) acc[f][n][k] = i == k ? v : acc[f][n][k];
+                }
+            }
+        }
+    }
+    auto lay = [&](auto value) {
+        __syncthreads();                                    // everybody is done with what lies there
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int p = 0; p < MF / 2; ++p)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    uint32_t v[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = f32_to_bf16_bits(value(acc[2 * p][n][g * 4 + i], acc[2 * p + 1][n][g * 4 + i]));
+                    *reinterpret_cast<uint2*>(out + (wn * 64 + n * 32 + sub) * LD + wm * (WM / 2) + p * 32 + g * 8 + hh * 4) = make_uint2(v[0] | v[1] << 16, v[2] | v[3] << 16);
+                }
+        __syncthreads();
+    };
+    auto write = [&](void* to_, int64_t ld) {
+        uint16_t* __restrict__ const to = static_cast<uint16_t*>(to_);
+        const bool whole = (ld & 7) == 0 && (reinterpret_cast<uintptr_t>(to) & 15) == 0;
+#pragma unroll 4
+        for (int i = tid; i < TOKENS * (ROWS / 8); i += THREADS) {
+            const int n = i / (ROWS / 8), r = (i - n * (ROWS / 8)) * 8;
+            const int64_t t = t0 + n, row = (c0 >> 1) + r;
+            if (t >= Q.T || row >= rows) continue;          // rows come in eights
+            const uint4 v = *reinterpret_cast<const uint4*>(out + n * LD + r);
+            uint16_t* __restrict__ const o = to + t * ld + row;
+            if (whole) {
+                *reinterpret_cast<uint4*>(o) = v;
+            } else {
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int m = 0; m < 8; ++m) o[m] = (uint16_t)(w[m >> 1] >> (16 * (m & 1)));
+            }
+        }
+    };
+    if (Q.pair.G != nullptr) {
+        lay([](float x, float) { return x; });
+        write(Q.pair.G, Q.pair.ld_save);
+        lay([](float, float y) { return y; });
+        write(Q.pair.U, Q.pair.ld_save);
+    }
+    lay([&](float x, float y) {
+        float none;
+        return activation<false>(Q.pair.act, x, none) * y;
+    });
+    write(Q.dX, Q.ldx);
+}
+
 template <int MF, bool HALF = false, bool PAIR = false>    // fragments of a wavefront along the columns; factors in half precision
 __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
     constexpr int GM_M = MF * 64, WM = MF * 32, LOADS = (GM_M + GM_N) / 32;
@@ -155,88 +241,7 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
 
-    if constexpr (PAIR) {
-        // Fragments 2 p and 2 p + 1 are the gate's and the up's of the same 32 rows.  What is written goes through LDS: a lane has four rows of a token, and 8
-        // bytes of each of 32 tokens are written at a third of the rate of whole lines.
-        constexpr int ROWS = GM_M / 2, LD = ROWS + 8;       // of a tile's tokens in LDS
-        const int64_t rows = Q.gate.rows;
-        uint16_t* const out = reinterpret_cast<uint16_t*>(tile);
-        static_assert(3 * GM_N * LD * 2 <= sizeof(tile), "G, U and H of a tile fit");
-        __syncthreads();                                    // everybody is done with the last buffer
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const int64_t t = t0 + wn * 64 + n * 32 + sub;
-            const int token = exponent_of(Q.by_token[t < Q.T ? t : Q.T - 1]);
-#pragma unroll
-            for (int f = 0; f < MF; ++f) {
-                const int64_t c = c0 + wm * WM + f * 32, row0 = (c >> 6) * 32 + hh * 4;
-                bool bad = false;
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int by = token + exponent_of(Q.by_octet[(c >> 3) + g]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        acc[f][n][g * 4 + i] = ldexpf(acc[f][n][g * 4 + i], by);
-                        bad |= !isfinite(acc[f][n][g * 4 + i]);
-                    }
-                }
-                // what is not finite so far: weight by weight
-                if (__any(bad && row0 < rows && t < Q.T)) {
-#pragma unroll 1
-                    for (int i = 0; i < 16; ++i) {
-                        const int64_t row = row0 + (i >> 2) * 8 + (i & 3);
-                        float v = 0.0f;
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) v = i == k ? acc[f][n][k] : v;
-                        if (!isfinite(v) && row < rows && t < Q.T) v = (float)pk_slow_dot((f & 1) == 0 ? Q.gate : Q.pair.up, row, Q.raw + t * Q.ld_raw);
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) acc[f][n][k] = i == k ? v : acc[f][n][k];
-                    }
-                }
-            }
-#pragma unroll
-            for (int p = 0; p < MF / 2; ++p)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    uint32_t v[3][4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float none;
-                        const float x = acc[2 * p][n][g * 4 + i], y = acc[2 * p + 1][n][g * 4 + i];
-                        v[0][i] = f32_to_bf16_bits(activation<false>(Q.pair.act, x, none) * y);
-                        v[1][i] = f32_to_bf16_bits(x);
-                        v[2][i] = f32_to_bf16_bits(y);
-                    }
-                    uint16_t* const to = out + (wn * 64 + n * 32 + sub) * LD + wm * (WM / 2) + p * 32 + g * 8 + hh * 4;
-#pragma unroll
-                    for (int k = 0; k < 3; ++k)
-                        if (k == 0 || Q.pair.G != nullptr) *reinterpret_cast<uint2*>(to + k * GM_N * LD) = make_uint2(v[k][0] | v[k][1] << 16, v[k][2] | v[k][3] << 16);
-                }
-        }
-        __syncthreads();
-#pragma unroll 1
-        for (int k = 0; k < (Q.pair.G != nullptr ? 3 : 1); ++k) {
-            uint16_t* __restrict__ const to = static_cast<uint16_t*>(k == 0 ? Q.dX : (k == 1 ? Q.pair.G : Q.pair.U));
-            const int64_t ld = k == 0 ? Q.ldx : Q.pair.ld_save;
-            const bool whole = (ld & 7) == 0 && (reinterpret_cast<uintptr_t>(to) & 15) == 0;
-#pragma unroll 4
-            for (int i = tid; i < GM_N * (ROWS / 8); i += GM_THREADS) {
-                const int n = i / (ROWS / 8), r = (i - n * (ROWS / 8)) * 8;
-                const int64_t t = t0 + n, row = (c0 >> 1) + r;
-                if (t >= Q.T || row >= rows) continue;      // rows come in eights
-                const uint4 v = *reinterpret_cast<const uint4*>(out + (k * GM_N + n) * LD + r);
-                uint16_t* __restrict__ const o = to + t * ld + row;
-                if (whole) {
-                    *reinterpret_cast<uint4*>(o) = v;
-                } else {
-                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                    for (int m = 0; m < 8; ++m) o[m] = (uint16_t)(w[m >> 1] >> (16 * (m & 1)));
-                }
-            }
-        }
-        return;
-    }
+    if constexpr (PAIR) return pair_tile<MF, GM_THREADS>(Q, acc, reinterpret_cast<uint16_t*>(tile), c0, t0, wm, wn, tid);
     if constexpr (HALF) {
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
