@@ -341,23 +341,20 @@ __device__ __forceinline__ void store_octet(XT* __restrict__ p, int64_t left, bo
         if (i < left) store_y(p + i, v[i]);
 }
 
-template <typename XT>
+// PER octets of each tensor a thread, kept in registers from the pass for the power to the one that puts it on (bfloat16 calls with whole octets in every row); 0:
+// any number, read twice.
+template <typename XT, int PER>
 __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
     __shared__ float most[4];
     const XT* __restrict__ const dh = static_cast<const XT*>(Q.dH) + t * Q.ld_dh;
     const XT* __restrict__ const g = static_cast<const XT*>(Q.G) + t * Q.ld_save;
     const XT* __restrict__ const u = static_cast<const XT*>(Q.U) + t * Q.ld_save;
-    float by = 1.0f;
-    if (sizeof(XT) == 2 && Q.to != nullptr) {
-        float m = 0.0f;
-        for (int64_t r = threadIdx.x * 8; r < Q.rows; r += 2048) {
-            float a[8], b[8], c[8];
-            load_octet(dh + r, Q.rows - r, Q.wide, a);
-            load_octet(g + r, Q.rows - r, Q.wide, b);
-            load_octet(u + r, Q.rows - r, Q.wide, c);
+    float by = 1.0f, m = 0.0f;
+    auto larger = [&](const float (&a)[8], const float (&b)[8], const float (&c)[8]) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m = fmaxf(m, fminf(fmaxf(fabsf(a[i] * c[i]), fabsf(a[i] * b[i])), 3.40282347e38f));
-        }
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, fminf(fmaxf(fabsf(a[i] * c[i]), fabsf(a[i] * b[i])), 3.40282347e38f));
+    };
+    auto power = [&] {
 #pragma unroll
         for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
         if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = m;
@@ -365,15 +362,10 @@ __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
         // a product past fp32 counts as its largest number: what an activation makes of it may be a number again
         by = power_below(1.13f * fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
         if (threadIdx.x == 0) Q.by_token[t] = 1.0f / by;
-    }
-    for (int64_t r = threadIdx.x * 8; r < (Q.to != nullptr ? Q.K : Q.rows); r += 2048) {
-        float a[8] = {}, b[8] = {}, c[8] = {}, dg[8], du[8];
+    };
+    auto finish = [&](int64_t r, const float (&a)[8], const float (&b)[8], const float (&c)[8]) {
         const int64_t left = Q.rows - r;
-        if (left > 0) {
-            load_octet(dh + r, left, Q.wide, a);
-            load_octet(g + r, left, Q.wide, b);
-            load_octet(u + r, left, Q.wide, c);
-        }
+        float dg[8], du[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             float slope;
@@ -385,7 +377,7 @@ __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
             store_octet(static_cast<XT*>(Q.dG) + t * Q.ld_d + r, left, Q.wide, dg);
             store_octet(static_cast<XT*>(Q.dU) + t * Q.ld_d + r, left, Q.wide, du);
         }
-        if (Q.to == nullptr) continue;
+        if (Q.to == nullptr) return;
         if constexpr (sizeof(XT) == 2) {
             uint16_t* const to = static_cast<uint16_t*>(Q.to) + t * 2 * Q.K + r;
             uint32_t w[2][8];
@@ -399,6 +391,64 @@ __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
         } else {
             store_octet(static_cast<float*>(Q.to) + t * Q.K + r, 8, true, dg);
             store_octet(static_cast<float*>(Q.to) + (Q.T + t) * Q.K + r, 8, true, du);
+        }
+    };
+    if constexpr (PER > 0) {
+        uint4 held[PER][3];
+        auto values = [](uint4 v, float (&x)[8]) {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = (i & 1) != 0 ? __uint_as_float(w[i >> 1] & 0xffff0000u) : __uint_as_float(w[i >> 1] << 16);
+        };
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int64_t r = threadIdx.x * 8 + k * 2048;
+            const bool in = r < Q.rows;
+            held[k][0] = in ? *reinterpret_cast<const uint4*>(dh + r) : make_uint4(0u, 0u, 0u, 0u);
+            held[k][1] = in ? *reinterpret_cast<const uint4*>(g + r) : make_uint4(0u, 0u, 0u, 0u);
+            held[k][2] = in ? *reinterpret_cast<const uint4*>(u + r) : make_uint4(0u, 0u, 0u, 0u);
+        }
+        float a[8], b[8], c[8];
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            values(held[k][0], a);
+            values(held[k][1], b);
+            values(held[k][2], c);
+            larger(a, b, c);
+        }
+        power();
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int64_t r = threadIdx.x * 8 + k * 2048;
+            if (r >= Q.K) continue;
+            // unpacked anew: the compiler would keep three floats for each of them
+            asm volatile("" : "+v"(held[k][0].x), "+v"(held[k][0].y), "+v"(held[k][0].z), "+v"(held[k][0].w), "+v"(held[k][1].x), "+v"(held[k][1].y), "+v"(held[k][1].z), "+v"(held[k][1].w),
+                         "+v"(held[k][2].x), "+v"(held[k][2].y), "+v"(held[k][2].z), "+v"(held[k][2].w));
+            values(held[k][0], a);
+            values(held[k][1], b);
+            values(held[k][2], c);
+            finish(r, a, b, c);
+        }
+    } else {
+        if (sizeof(XT) == 2 && Q.to != nullptr) {
+            for (int64_t r = threadIdx.x * 8; r < Q.rows; r += 2048) {
+                float a[8], b[8], c[8];
+                load_octet(dh + r, Q.rows - r, Q.wide, a);
+                load_octet(g + r, Q.rows - r, Q.wide, b);
+                load_octet(u + r, Q.rows - r, Q.wide, c);
+                larger(a, b, c);
+            }
+            power();
+        }
+        for (int64_t r = threadIdx.x * 8; r < (Q.to != nullptr ? Q.K : Q.rows); r += 2048) {
+            float a[8] = {}, b[8] = {}, c[8] = {};
+            const int64_t left = Q.rows - r;
+            if (left > 0) {
+                load_octet(dh + r, left, Q.wide, a);
+                load_octet(g + r, left, Q.wide, b);
+                load_octet(u + r, left, Q.wide, c);
+            }
+            finish(r, a, b, c);
         }
     }
 }
@@ -422,10 +472,10 @@ __device__ __forceinline__ void range_of(const SlopeArgs& Q, int64_t block) {
     if (threadIdx.x == 0) Q.range[(j * 2 + m) * Q.strips + strip] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
 }
 
-template <typename XT>
+template <typename XT, int PER = 0>
 __global__ __launch_bounds__(256) void gated_slopes_kernel(const SlopeArgs Q, const int64_t first) {
     const int64_t block = first + blockIdx.x;
-    if (block < Q.T) slopes<XT>(Q, block);
+    if (block < Q.T) slopes<XT, PER>(Q, block);
     else range_of(Q, block - Q.T);
 }
 
@@ -503,7 +553,16 @@ int gated_grad_all(SlopeArgs& S, void* dX, int64_t ld_dx, char* ws, const GatedG
             ahead += 2 * (int64_t)S.strips * P.n_chunks;
         }
     }
-    int status = launch_pieces(ahead, 256, [&](int64_t first, dim3 g) { gated_slopes_kernel<XT><<<g, dim3(256), 0, st>>>(S, first); });
+    const int64_t each = bf && dX != nullptr && S.wide && P.rows % 8 == 0 ? tokens_in(S.K, 2048) : 0;
+    int status = launch_pieces(ahead, 256, [&](int64_t first, dim3 g) {
+        if constexpr (bf) {
+            if (each == 1) return gated_slopes_kernel<XT, 1><<<g, dim3(256), 0, st>>>(S, first);
+            if (each == 2) return gated_slopes_kernel<XT, 2><<<g, dim3(256), 0, st>>>(S, first);
+            if (each == 3 || each == 4) return gated_slopes_kernel<XT, 4><<<g, dim3(256), 0, st>>>(S, first);
+            if (each == 5 || each == 6) return gated_slopes_kernel<XT, 6><<<g, dim3(256), 0, st>>>(S, first);
+        }
+        gated_slopes_kernel<XT><<<g, dim3(256), 0, st>>>(S, first);
+    });
     if (status != WINDQ_OK || dX == nullptr) return status;
     DxArgs Q = {};
     Q.P = P;

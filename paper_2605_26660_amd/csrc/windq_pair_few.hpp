@@ -4,6 +4,8 @@
 // side, so that a lane has one row, with one scale and one offset, and a quarter of a k-block's columns side by side: its codes are one load of 4 to 32 bytes,
 // straight to registers, and nothing but trits' table and the totals goes through LDS.  Few registers leave room for five or six wavefronts a SIMD, which
 // wait for each other's loads; treatments and places of codes are looked up for all of a wavefront's k-blocks at once, ahead.
+//   11008 x 4096 at 2 bits, 1 token 18.4 us, 8 tokens 23.9, 16 tokens 30.6, where 32 rows a workgroup (32x32x16 instructions, codes through LDS, one workgroup a CU: two
+// rounds of them) take 35.9, 38.7 and 44.4; a k-block's codes asked for ahead of the one before: 22.3.
 #pragma once
 
 #include "windq_project_few.hpp"
@@ -11,7 +13,7 @@
 namespace windq {
 
 constexpr int PR_ROWS = 16;
-constexpr int64_t PAIR_FEW = 16;
+constexpr int64_t PAIR_FEW = 16;                             // tokens of an instruction; at all of them ahead of the kernel for more
 
 #ifdef __HIPCC__
 
@@ -163,7 +165,8 @@ __global__ __launch_bounds__(WAVES * 64, 6) void pair_few_kernel(const FewArgs Q
 template <int O>
 int launch_pair_few(const FewArgs& Q, hipStream_t st) {
     const int64_t wgs = tokens_in(Q.P.rows, PR_ROWS);
-    if (!fits_launch(wgs, 1024)) return WINDQ_ESHAPE;
+    if (!fits_launch(wgs, wgs > 512 ? 512 : 1024)) return WINDQ_ESHAPE;
+    // eight wavefronts where the rows are two workgroups a CU and more, so that all of them run at once
     if (wgs > 512) pair_few_kernel<O, 8><<<dim3((uint32_t)wgs), dim3(512), 0, st>>>(Q);
     else pair_few_kernel<O, 16><<<dim3((uint32_t)wgs), dim3(1024), 0, st>>>(Q);
     return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;

@@ -92,3 +92,21 @@ def test_half_precision_weights_of_one_treatment(windq, shape, only):
     close(windq.windq_gated(*p, x), want[2], off[2], BF)
     want, off = backward(cs, dh, g, u, "silu", BF)
     close(windq.windq_gated_grad(*p, dh, g, u)[0], want[0], off[0], BF)
+
+
+@pytest.mark.parametrize("word", ["silu", "gelu"])
+@pytest.mark.parametrize("rows", [8, 1984, 2048, 2056, 4104, 6152, 8200, 12288, 12296])
+def test_gradients_of_rows_kept_in_registers_and_read_twice(windq, rows, word):
+    """One to six octets of a row a thread, and more; where rows lie on no alignment they are read twice: the same bits."""
+    shape = (rows, 64, 64, 0, 3)
+    cs = pair(windq, shape, BF, seed=rows % 7)
+    p = [c.packed for c in cs]
+    dh, g, u = tokens(3, rows, BF, 2, 1e-3), tokens(3, rows, BF, 3, 2.0), tokens(3, rows, BF, 4)
+    got = windq.windq_gated_grad(*p, dh, g, u, word)
+    want, off = backward(cs, dh, g, u, word, BF)
+    for a, b, o in zip(got, want, off):
+        close(a, b, o, BF)
+    pad = lambda t: torch.nn.functional.pad(t, (1, 2))[:, 1:-2]  # noqa: E731
+    for a, b in zip(windq.windq_gated_grad(*p, pad(dh), pad(g), pad(u), word), got):
+        assert torch.equal(a, b)
+    assert torch.equal(windq.windq_gated_grad(*p, dh, g, u, word, want_dgu=False)[0], got[0])
