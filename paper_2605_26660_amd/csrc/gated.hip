@@ -62,19 +62,20 @@ struct HalvesArgs {
     float* by_octet;
 };
 
-// Workgroups [0, T): a token; the others: 16 rows of a matrix.  A wavefront has 128 columns of them at a time, one treatment as a rule, a lane an octet of
-// columns of two rows: lanes of different treatments would take turns, each waiting for its codes.  The units' treatments and places are looked up once.
-// Bound by latency: loads wait for the stores ahead of them, so that few registers and many wavefronts count.
+// Workgroups ahead: 16 rows of a matrix, the longer ones; the others: a token.  A wavefront has a k-block of them at a time, of one treatment, a lane a row and a quarter of its
+// columns; where chunks are not whole k-blocks or a mask lies over them 128 columns, a lane an octet of two rows: lanes of different treatments would take
+// turns, each waiting for its codes.  The units' treatments and places are looked up once.  Bound by the stores (180 MB for a pair of 11008 x 4096, 35 us at a copy's rate) and by chains
+// of loads ahead of them: 66 us; a lane an octet 79, with skip rows looked through by one lane each 82 either way.
 constexpr int HALVES_UNITS = 512, HALVES_ROWS = 16;
 
-template <bool KNOWN, bool PLAIN>                          // units of whole blocks of rows, and few enough of them in a row; no mask besides
+template <bool KNOWN, int O>                               // units of whole blocks of rows, and few enough of them in a row; O: chunks of one or more 32 O columns, no mask, or 0
 __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, const int64_t first) {
     __shared__ float most[4][2];
     __shared__ uint16_t trits_of[256];
     __shared__ uint64_t units[HALVES_UNITS];
-    const int64_t id = first + blockIdx.x;
+    const int64_t blocks = (Q.P[0].rows + HALVES_ROWS - 1) / HALVES_ROWS, block = first + blockIdx.x, id = block - 2 * blocks;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    if (id < Q.T) {
+    if (id >= 0) {
         const uint16_t* __restrict__ const x = Q.X + id * Q.ldx;
         float m = 0.0f;
         for (int64_t c = threadIdx.x * 8; c < Q.P[0].cols; c += 2048) {
@@ -100,7 +101,6 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
         return;
     }
     trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
-    const int64_t blocks = (Q.P[0].rows + HALVES_ROWS - 1) / HALVES_ROWS, block = id - Q.T;
     const int mat = block >= blocks ? 1 : 0;
     const PackArgs& P = Q.P[mat];
     const int64_t r0 = (block - mat * blocks) * HALVES_ROWS, at = (r0 >> 5) * 64 + mat * 32 + (r0 & 31), rb = r0 / P.R_u;
@@ -113,14 +113,92 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
     // the largest magnitudes of eight rows
     float m = 0.0f;
     const int64_t row = r0 + (threadIdx.x & 15);
-    if (row < P.rows)
+    if constexpr (KNOWN) {                                  // rows of skip units by all threads: one that looks through 128 weights by itself takes as long as all the rest
+        __syncthreads();
+        const int64_t g0 = rb * P.n_chunks * P.R_u + row - rb * P.R_u;
+        if (row < P.rows)
+            for (int32_t j = threadIdx.x >> 4; j < P.n_chunks; j += 16)
+                if (const int a = (int)(units[j] >> 56); a != 0) m = affine_max(P, a, g0 + j * P.R_u, m);
+        for (int32_t j = 0; j < P.n_chunks; ++j) {
+            if ((units[j] >> 56) != 0 || row >= P.rows) continue;
+            for (int32_t c = (int32_t)(threadIdx.x >> 4) * 8; c < P.G; c += 128) {
+                float w[8];
+                skip_row(P, row, (int64_t)j * P.G + c, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) m = finite_max(m, w[i]);
+            }
+        }
+    } else if (row < P.rows) {
         for (int64_t j = threadIdx.x >> 4; j < P.n_chunks; j += 16) m = group_max(P, row, j, m);
+    }
     m = fmaxf(m, __shfl_xor(m, 32, 64));
     m = fmaxf(m, __shfl_xor(m, 16, 64));
 #pragma unroll
     for (int d = 4; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
     if (lane == 0 || lane == 8) most[wave][lane >> 3] = m;
     __syncthreads();
+    if constexpr (O > 0) {
+        // 16 rows by 32 O columns a wavefront at a time, a lane a row and O octets of it, whose codes are one load; they leave through LDS by whole lines
+        constexpr int COLS = 32 * O, LD = 4 * O + 1;        // a row's sixteens of bytes in LDS
+        __shared__ uint4 turned[4][16 * LD];
+        const int sub = lane & 15, q = lane >> 4, eight = sub >> 3;
+        const float by = power_below(fmaxf(fmaxf(most[0][eight], most[1][eight]), fmaxf(most[2][eight], most[3][eight])));
+        const int32_t there = P.rows - r0 < HALVES_ROWS ? (int32_t)(P.rows - r0) : HALVES_ROWS;
+        const uint32_t lr = (uint32_t)(sub < there ? sub : there - 1);
+        if (wave == 0 && (lane == 0 || lane == 8) && sub < there) Q.by_octet[(at >> 3) + eight] = 1.0f / by;
+        uint4* const mine = turned[wave];
+        const int32_t per_chunk = P.G / COLS;
+        const uint32_t lrow0 = (uint32_t)(r0 - rb * P.R_u);
+        for (int32_t kb = wave; kb < (int32_t)(P.cols / COLS); kb += 4) {
+            const int32_t j = kb / per_chunk, c = kb - j * per_chunk;
+            const uint64_t unit = units[j];
+            const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(unit >> 32)), lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)unit);
+            const int kind = (int)(hi >> 24);
+            const uint32_t bpg = (uint32_t)pk_bytes_per_group(kind, P.G);
+            const uint8_t* const codes = P.codes + (((uint64_t)(hi & 0xffffffu) << 32 | lo) + (uint64_t)lrow0 * bpg);
+            const int64_t g = (rb * P.n_chunks + j) * P.R_u + lrow0;
+            const float scale = (P.scale + g)[lr] * by, offset = (P.offset + g)[lr] * by;
+            const uint32_t first = (uint32_t)c * COLS + q * (8 * O), row_at = lr * bpg;
+            uint4 w[O];
+            switch (kind) {
+                case 1: pair_fields<O, 8, true>(codes + (row_at + first), w); break;
+                case 2: pair_fields<O, 4, true>(codes + (row_at + (first >> 1)), w); break;
+                case 3: pair_fields<O, 3, true>(codes + (row_at + (first >> 3) * 3), w); break;
+                case 4: pair_fields<O, 2, true>(codes + (row_at + (first >> 2)), w); break;
+                case 5: {
+                    const uint32_t k = first / 5u, from = k < bpg - 8u ? k : bpg - 8u;       // eight bytes within the row
+                    pair_trits<O, true>(codes + (row_at + from), first - from * 5u, trits_of, w);
+                    break;
+                }
+                case 6: pair_fields<O, 1, true>(codes + (row_at + (first >> 3)), w); break;
+                default: {
+#pragma unroll
+                    for (int s = 0; s < O; ++s) {
+                        float v[8];
+                        skip_row(P, r0 + lr, (int64_t)kb * COLS + q * (8 * O) + s * 8, v);
+                        w[s] = make_uint4(half_pair(v[0] * by, v[1] * by), half_pair(v[2] * by, v[3] * by), half_pair(v[4] * by, v[5] * by), half_pair(v[6] * by, v[7] * by));
+                    }
+                }
+            }
+            if (kind != 0) {
+                const float b = fmaf(-pk_f0(kind), scale, kind >= 5 ? 0.0f : offset);
+#pragma unroll
+                for (int s = 0; s < O; ++s) w[s] = half_weights(w[s], scale, b);
+            }
+#pragma unroll
+            for (int s = 0; s < O; ++s) mine[sub * LD + q * O + s] = w[s];
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < O; ++i) {
+                const int n = (i * 64 + lane) / (4 * O), slot = i * 64 + lane - n * (4 * O);
+                if (n < there) *reinterpret_cast<uint4*>(Q.w + (at + n) * Q.K + (int64_t)kb * COLS + slot * 8) = mine[n * LD + slot];
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+        for (int32_t c = (int32_t)P.cols + (int)(threadIdx.x >> 4) * 8; c < Q.K; c += 128)         // columns up to a whole step of the product
+            if (sub < there) *reinterpret_cast<uint4*>(Q.w + (at + sub) * Q.K + c) = make_uint4(0u, 0u, 0u, 0u);
+        return;
+    }
     const int octet = wave & 1, part = octet * 4 + (lane >> 4);
     const float by = power_below(fmaxf(fmaxf(most[0][octet], most[1][octet]), fmaxf(most[2][octet], most[3][octet])));
     const int64_t here = r0 + part * 2;
@@ -134,18 +212,7 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
         };
         if (c < P.cols) {
             const uint32_t j = (uint32_t)c / (uint32_t)P.G;
-            if constexpr (PLAIN) {
-                const uint64_t unit = units[j];
-                uint4 h[2];
-                half_rows<2>(P, here, c, rb * P.n_chunks + j, here - rb * P.R_u, ((int)c - (int)j * P.G) >> 3, (int)(unit >> 56), (int64_t)(unit & 0xffffffffffffffull), trits_of, by, h);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    w[i][0] = h[i].x;
-                    w[i][1] = h[i].y;
-                    w[i][2] = h[i].z;
-                    w[i][3] = h[i].w;
-                }
-            } else if constexpr (KNOWN) {
+            if constexpr (KNOWN) {
                 const uint64_t unit = units[j];
                 rows_of<2>(P, here, c, rb * P.n_chunks + j, here - rb * P.R_u, ((int)c - (int)j * P.G) >> 3, (int)(unit >> 56), (int64_t)(unit & 0xffffffffffffffull), trits_of, put);
             } else {
@@ -170,9 +237,11 @@ int launch_gated_halves(const ProjectArgs& Q, char* ws, const GatedWs& at, hipSt
     const bool mask = Q.P.mask != nullptr || Q.pair.up.mask != nullptr;
     const bool known = (Q.P.R_u == Q.P.rows || Q.P.R_u % HALVES_ROWS == 0) && Q.P.n_chunks <= HALVES_UNITS;
     const int status = launch_pieces(Q.T + 2 * tokens_in(Q.P.rows, HALVES_ROWS), 256, [&](int64_t first, dim3 g) {
-        if (known && !mask) gated_halves_kernel<true, true><<<g, dim3(256), 0, st>>>(H, first);
-        else if (known) gated_halves_kernel<true, false><<<g, dim3(256), 0, st>>>(H, first);
-        else gated_halves_kernel<false, false><<<g, dim3(256), 0, st>>>(H, first);
+        if (known && !mask && Q.P.G % 128 == 0) gated_halves_kernel<true, 4><<<g, dim3(256), 0, st>>>(H, first);
+        else if (known && !mask && Q.P.G == 96) gated_halves_kernel<true, 3><<<g, dim3(256), 0, st>>>(H, first);
+        else if (known && !mask && Q.P.G == 64) gated_halves_kernel<true, 2><<<g, dim3(256), 0, st>>>(H, first);
+        else if (known) gated_halves_kernel<true, 0><<<g, dim3(256), 0, st>>>(H, first);
+        else gated_halves_kernel<false, 0><<<g, dim3(256), 0, st>>>(H, first);
     });
     if (status != WINDQ_OK) return status;
     const int64_t by = rows / 256 * tall >= GM_TILES ? 256 : 128, large = rows / GM_MOST * tokens_in(Q.T, GW_N);
@@ -307,6 +376,7 @@ struct SlopeArgs {
     PackArgs P[2];
     float* range;              // [chunks][2][strips]
     int32_t strips;
+    int64_t ranges;            // workgroups for them
 };
 
 template <typename XT>
@@ -474,9 +544,9 @@ __device__ __forceinline__ void range_of(const SlopeArgs& Q, int64_t block) {
 
 template <typename XT, int PER = 0>
 __global__ __launch_bounds__(256) void gated_slopes_kernel(const SlopeArgs Q, const int64_t first) {
-    const int64_t block = first + blockIdx.x;
-    if (block < Q.T) slopes<XT, PER>(Q, block);
-    else range_of(Q, block - Q.T);
+    const int64_t block = first + blockIdx.x;               // the weights' ahead: those of skip units take long
+    if (block < Q.ranges) range_of(Q, block);
+    else slopes<XT, PER>(Q, block - Q.ranges);
 }
 
 struct GatedTurnArgs {
@@ -550,7 +620,8 @@ int gated_grad_all(SlopeArgs& S, void* dX, int64_t ld_dx, char* ws, const GatedG
             S.by_token = reinterpret_cast<float*>(ws + at.by_token);
             S.range = reinterpret_cast<float*>(ws + at.range);
             S.strips = (int32_t)tokens_in(P.rows, RANGE_ROWS);
-            ahead += 2 * (int64_t)S.strips * P.n_chunks;
+            S.ranges = 2 * (int64_t)S.strips * P.n_chunks;
+            ahead += S.ranges;
         }
     }
     const int64_t each = bf && dX != nullptr && S.wide && P.rows % 8 == 0 ? tokens_in(S.K, 2048) : 0;

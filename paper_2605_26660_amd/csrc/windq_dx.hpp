@@ -148,6 +148,16 @@ __device__ __forceinline__ uint32_t half_pair(float lo, float hi) {
     return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)lo) | (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)hi) << 16;
 }
 
+__device__ __forceinline__ uint4 half_fields8(uint32_t v0, uint32_t v1) {
+    auto pair = [](uint32_t v, int lo) { return half_pair((float)((v >> (8 * lo)) & 0xffu), (float)((v >> (8 * lo + 8)) & 0xffu)); };
+    return make_uint4(pair(v0, 0), pair(v0, 2), pair(v1, 0), pair(v1, 2));
+}
+
+__device__ __forceinline__ uint4 half_weights(uint4 f, float s, float b) {
+    auto two = [&](uint32_t q) { return half_pair(fmaf((float)__builtin_bit_cast(_Float16, (uint16_t)q), s, b), fmaf((float)__builtin_bit_cast(_Float16, (uint16_t)(q >> 16)), s, b)); };
+    return make_uint4(two(f.x), two(f.y), two(f.z), two(f.w));
+}
+
 // ROWS rows by eight columns of w_hat times `by`, a power of two, in half precision, within a unit whose treatment and first byte are known; no mask.  Five
 // instructions a weight, where putting on the mask, the power and the centre one by one takes eleven.
 template <int ROWS>
@@ -176,8 +186,7 @@ __device__ __forceinline__ void half_rows(const PackArgs& P, int64_t r0, int64_t
         case 1: rows([&](const uint8_t* p) {
             uint2 q;
             __builtin_memcpy(&q, p + o * 8, 8);
-            auto byte = [&](int k) { return (float)(((k < 4 ? q.x : q.y) >> (8 * (k & 3))) & 0xffu); };
-            return make_uint4(half_pair(byte(0), byte(1)), half_pair(byte(2), byte(3)), half_pair(byte(4), byte(5)), half_pair(byte(6), byte(7)));
+            return half_fields8(q.x, q.y);
         }); break;
         case 2: rows([&](const uint8_t* p) { uint32_t q; __builtin_memcpy(&q, p + o * 4, 4); return half_fields4(q); }); break;
         case 3: rows([&](const uint8_t* p) { return half_fields3((uint32_t)p[o * 3] | (uint32_t)p[o * 3 + 1] << 8 | (uint32_t)p[o * 3 + 2] << 16); }); break;
@@ -189,10 +198,7 @@ __device__ __forceinline__ void half_rows(const PackArgs& P, int64_t r0, int64_t
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
         const float s = sc[i] * by, b = fmaf(-f0, s, a >= 5 ? 0.0f : be[i] * by);
-        auto two = [&](uint32_t q) {
-            return half_pair(fmaf((float)__builtin_bit_cast(_Float16, (uint16_t)q), s, b), fmaf((float)__builtin_bit_cast(_Float16, (uint16_t)(q >> 16)), s, b));
-        };
-        w[i] = make_uint4(two(f[i].x), two(f[i].y), two(f[i].z), two(f[i].w));
+        w[i] = half_weights(f[i], s, b);
     }
 }
 
@@ -247,8 +253,14 @@ __device__ __forceinline__ void turn(const PackArgs& P, int32_t K, int64_t ld, f
 // The largest finite magnitude that the weights of a row's group can have, and the power of two that brings magnitudes up to `most` below 2^15 (1 where
 // there are none), itself within fp32's normal numbers.
 __device__ __forceinline__ float finite_max(float m, float x) { return isfinite(x) && fabsf(x) > m ? fabsf(x) : m; }
+__device__ __forceinline__ float affine_max(const PackArgs& P, int a, int64_t g, float m) {
+    const float s = P.scale[g], o = a >= 5 ? 0.0f : P.offset[g];
+    const float L = a == 1 ? 255.0f : (a == 2 ? 15.0f : (a == 3 ? 7.0f : (a == 4 ? 3.0f : 1.0f)));
+    const float top = isfinite(s) ? fminf(fabsf(fmaf(s, L, o)), 3.40282347e38f) : 0.0f;       // codes that are there may be smaller ones than L
+    return finite_max(finite_max(m, o), isfinite(o) ? top : 0.0f);
+}
 __device__ __forceinline__ float group_max(const PackArgs& P, int64_t row, int64_t j, float m) {
-    const int64_t rb = row / P.R_u, u = rb * P.n_chunks + j, g = u * P.R_u + row - rb * P.R_u;
+    const int64_t rb = row / P.R_u, u = rb * P.n_chunks + j;
     int64_t base;
     const int a = pk_action(P, u, base);
     if (a == 0) {
@@ -261,10 +273,7 @@ __device__ __forceinline__ float group_max(const PackArgs& P, int64_t row, int64
         }
         return m;
     }
-    const float s = P.scale[g], o = a >= 5 ? 0.0f : P.offset[g];
-    const float L = a == 1 ? 255.0f : (a == 2 ? 15.0f : (a == 3 ? 7.0f : (a == 4 ? 3.0f : 1.0f)));
-    const float top = isfinite(s) ? fminf(fabsf(fmaf(s, L, o)), 3.40282347e38f) : 0.0f;       // codes that are there may be smaller ones than L
-    return finite_max(finite_max(m, o), isfinite(o) ? top : 0.0f);
+    return affine_max(P, a, u * P.R_u + row - rb * P.R_u, m);
 }
 __device__ __forceinline__ float power_below(float most) {
     const int e = (int)(__float_as_uint(most) >> 23);       // biased; most < 2^(e - 126)

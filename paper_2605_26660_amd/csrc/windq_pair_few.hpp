@@ -8,6 +8,7 @@
 // rounds of them) take 35.9, 38.7 and 44.4; a k-block's codes asked for ahead of the one before: 22.3.
 #pragma once
 
+#include "windq_dx.hpp"
 #include "windq_project_few.hpp"
 
 namespace windq {
@@ -17,8 +18,8 @@ constexpr int64_t PAIR_FEW = 16;                             // tokens of an ins
 
 #ifdef __HIPCC__
 
-// O octets of a row (columns side by side) as f, from their first byte; r: trits ahead of them.
-template <int O, int BITS>
+// O octets of a row (columns side by side) as f, from their first byte, in bfloat16 or (HALF) in half precision; r: trits ahead of them.
+template <int O, int BITS, bool HALF = false>
 __device__ __forceinline__ void pair_fields(const uint8_t* __restrict__ p, uint4 (&w)[O]) {
     uint32_t v[2 * O + 1] = {};
 #pragma unroll
@@ -33,15 +34,17 @@ __device__ __forceinline__ void pair_fields(const uint8_t* __restrict__ p, uint4
     for (int s = 0; s < O; ++s) {
         constexpr int STEP = BITS * 8;
         const int at = s * STEP;
-        if constexpr (BITS == 1) w[s] = fields1((v[0] >> at) & 0xffu);
-        else if constexpr (BITS == 2) w[s] = fields2((v[at >> 5] >> (at & 31)) & 0xffffu);
-        else if constexpr (BITS == 3) w[s] = fields3((at & 31) <= 8 ? (v[at >> 5] >> (at & 31)) & 0xffffffu : __builtin_amdgcn_alignbit(v[(at >> 5) + 1], v[at >> 5], at & 31) & 0xffffffu);
-        else if constexpr (BITS == 4) w[s] = fields4(v[s]);
-        else w[s] = fields8(v[2 * s], v[2 * s + 1]);
+        if constexpr (BITS == 1) w[s] = HALF ? half_fields1((v[0] >> at) & 0xffu) : fields1((v[0] >> at) & 0xffu);
+        else if constexpr (BITS == 2) w[s] = HALF ? half_fields2((v[at >> 5] >> (at & 31)) & 0xffffu) : fields2((v[at >> 5] >> (at & 31)) & 0xffffu);
+        else if constexpr (BITS == 3) {
+            const uint32_t q = (at & 31) <= 8 ? (v[at >> 5] >> (at & 31)) & 0xffffffu : __builtin_amdgcn_alignbit(v[(at >> 5) + 1], v[at >> 5], at & 31) & 0xffffffu;
+            w[s] = HALF ? half_fields3(q) : fields3(q);
+        } else if constexpr (BITS == 4) w[s] = HALF ? half_fields4(v[s]) : fields4(v[s]);
+        else w[s] = HALF ? half_fields8(v[2 * s], v[2 * s + 1]) : fields8(v[2 * s], v[2 * s + 1]);
     }
 }
 
-template <int O>
+template <int O, bool HALF = false>
 __device__ __forceinline__ void pair_trits(const uint8_t* __restrict__ p, uint32_t r, const uint16_t* __restrict__ trits_of, uint4 (&w)[O]) {
     uint32_t b[2], t[8], v[3];
     __builtin_memcpy(b, p, 8);
@@ -59,7 +62,10 @@ __device__ __forceinline__ void pair_trits(const uint8_t* __restrict__ p, uint32
     v[0] = __builtin_amdgcn_alignbit(v[1], v[0], 2 * r);
     if (O > 2) v[1] = __builtin_amdgcn_alignbit(v[2], v[1], 2 * r);
 #pragma unroll
-    for (int s = 0; s < O; ++s) w[s] = fields2((s & 1) != 0 ? v[s >> 1] >> 16 : v[s >> 1] & 0xffffu);
+    for (int s = 0; s < O; ++s) {
+        const uint32_t q = (s & 1) != 0 ? v[s >> 1] >> 16 : v[s >> 1] & 0xffffu;
+        w[s] = HALF ? half_fields2(q) : fields2(q);
+    }
 }
 
 template <int O, int WAVES>
