@@ -13,7 +13,12 @@ namespace windq {
 // Many bfloat16 tokens: the matrices are reconstructed in half precision, once a call, and multiplied by a plain product (windq_gemm.hpp).  Both factors have 11 bits of
 // significand, and powers of two for a token and for eight rows that bring them below 2^15, so that what lies 2^28 below the largest of them still has all of its
 // digits: the weights' rounding (tokens have none: bfloat16's eight bits fit) is eight times as fine as G's and U's own.
-constexpr int64_t GATED_MANY = 320;
+// From 65 tokens on, unless the kernel for few tokens has them all in one round of workgroups: 11008 x 4096, 128 tokens 88 us (by it some 130), 64 tokens 87 and 67 by it; 4096 x 4096, 128 tokens
+// 57 and 38 by it (one round), 192 tokens 56 and 148; unpacking for every 128 tokens anew (as fp32 calls do) 118, 97 and 105.
+constexpr int64_t GATED_MANY = PROJECT_FEW;
+inline bool gated_few(const PackArgs& P, const PackArgs& up, int64_t T) {
+    return (T <= PROJECT_FEW || tokens_in(P.rows, PF_ROWS) * tokens_in(T, 64) <= 256) && few_fits(P, T) && few_fits(up, T);
+}
 
 struct GatedWs {
     size_t planes, frag, few_xs, fields[2], unit[2], xs, beta[2], alpha[2], w, x, by_token, by_octet, total;
@@ -35,7 +40,7 @@ GatedWs gated_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t G
     const int64_t few_tokens = T < few_most(rows, cols, G) ? tokens_in(T, 64) * 64 : few_most(rows, cols, G);
     w.frag = take(few ? (size_t)cols * (size_t)few_tokens * 2 : 0);
     w.few_xs = take(few ? (size_t)(cols / 64 + 1) * (size_t)few_tokens * 4 : 0);
-    const bool many = T > PROJECT_FEW;
+    const bool many = dtype == WINDQ_F32 && T > PROJECT_FEW;
     w.xs = take(many ? (size_t)(cols / 64) * (size_t)T * 16 : 0);
     for (int m = 0; m < 2; ++m) {
         w.fields[m] = take(many ? (size_t)(rows * cols) / (G == 128 || G == 96 || G == 64 ? 2 : 1) : 0);
@@ -245,7 +250,7 @@ int launch_gated_halves(const ProjectArgs& Q, char* ws, const GatedWs& at, hipSt
     });
     if (status != WINDQ_OK) return status;
     const int64_t by = rows / 256 * tall >= GM_TILES ? 256 : 128, large = rows / GM_MOST * tokens_in(Q.T, GW_N);
-    const bool wide = gemm_wide(large, rows / by * tall);
+    const bool wide = gemm_wide(large, rows / by * tall, by);
     const int64_t tiles = wide ? large : rows / by * tall;
     GemmArgs M = {};
     M.wt = H.w;
@@ -272,7 +277,7 @@ int launch_gated_halves(const ProjectArgs& Q, char* ws, const GatedWs& at, hipSt
     return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
 }
 
-template <typename XT, int S>
+template <int S>
 int launch_gated_tiles(const ProjectArgs& Q, char* ws, const GatedWs& at, hipStream_t st) {
     TileArgs A = {};
     A.P = Q.P;
@@ -300,14 +305,14 @@ int launch_gated_tiles(const ProjectArgs& Q, char* ws, const GatedWs& at, hipStr
         matrix(m);
         A.P = m == 1 ? Q.pair.up : Q.P;
         const int64_t wgs = strips + (m == 0 ? tokens_in(A.n_kb * Q.T, PT_SUMS) : 0);
-        const int status = launch_pieces(wgs, 256, [&](int64_t first, dim3 g) { tiles_prepare_kernel<XT, S><<<g, dim3(256), 0, st>>>(A, strips, first); });
+        const int status = launch_pieces(wgs, 256, [&](int64_t first, dim3 g) { tiles_prepare_kernel<float, S><<<g, dim3(256), 0, st>>>(A, strips, first); });
         if (status != WINDQ_OK) return status;
     }
     A.unit_up = reinterpret_cast<KbWord*>(ws + at.unit[1]);
     A.beta_up = reinterpret_cast<uint4*>(ws + at.beta[1]);
     // tiles are no more than 2^31 / (64 x 128) and two sides' edges: one launch holds them
     const int64_t tiles = (int64_t)A.row_blocks * ((Q.T + PT_TOKENS - 1) / PT_TOKENS);
-    project_tiles_kernel<XT, S, true><<<dim3((uint32_t)tiles), dim3(PT_THREADS), 0, st>>>(A);
+    project_tiles_kernel<float, S, true><<<dim3((uint32_t)tiles), dim3(PT_THREADS), 0, st>>>(A);
     return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
 }
 
@@ -322,7 +327,7 @@ int gated_all(ProjectArgs& Q, const windq_mat* X, char* ws, const GatedWs& at, h
         Q.ldx = Q.P.cols;
         Q.plane = T * Q.P.cols;
     } else {
-        if (few_fits(Q.P, T) && few_fits(Q.pair.up, T)) {
+        if (gated_few(Q.P, Q.pair.up, T)) {
             FewArgs F = {Q.P, Q.X, Q.ldx, T, static_cast<uint16_t*>(Q.Y), Q.ldy, nullptr, Q.A, 0, reinterpret_cast<uint4*>(ws + at.frag), reinterpret_cast<float*>(ws + at.few_xs), 0, 0, 0, Q.pair};
             const int steps = Q.P.G % 128 == 0 ? 8 : Q.P.G / 16;
             F.n_kb = (int32_t)(Q.P.cols / (16 * steps));
@@ -330,15 +335,15 @@ int gated_all(ProjectArgs& Q, const windq_mat* X, char* ws, const GatedWs& at, h
             return steps == 8 ? launch_few<8, true>(F, nullptr, st) : (steps == 6 ? launch_few<6, true>(F, nullptr, st) : launch_few<4, true>(F, nullptr, st));
         }
     }
+    const bool mask = Q.P.mask != nullptr || Q.pair.up.mask != nullptr;
     if constexpr (sizeof(XT) == 2) {
         if (T > GATED_MANY && Q.P.rows % 8 == 0) return launch_gated_halves(Q, ws, at, st);
+    } else {
+        const int S = !mask && T > PROJECT_FEW && (Q.P.rows + 15) / 16 * tokens_in(T, 64) > 512 ? tile_steps(Q.P) : 0;
+        if (S == 8) return launch_gated_tiles<8>(Q, ws, at, st);
+        if (S == 6) return launch_gated_tiles<6>(Q, ws, at, st);
+        if (S == 4) return launch_gated_tiles<4>(Q, ws, at, st);
     }
-    const bool mask = Q.P.mask != nullptr || Q.pair.up.mask != nullptr;
-    const int64_t general = (Q.P.rows + 15) / 16 * tokens_in(T, 64);
-    const int S = !mask && T > PROJECT_FEW && general > (sizeof(XT) == 2 ? 256 : 512) ? tile_steps(Q.P) : 0;
-    if (S == 8) return launch_gated_tiles<XT, 8>(Q, ws, at, st);
-    if (S == 6) return launch_gated_tiles<XT, 6>(Q, ws, at, st);
-    if (S == 4) return launch_gated_tiles<XT, 4>(Q, ws, at, st);
     return mask ? launch_project_any<XT, true, true>(Q, st) : launch_project_any<XT, false, true>(Q, st);
 }
 

@@ -11,9 +11,9 @@ namespace windq {
 
 constexpr int GW_N = 256, GW_K = 32, GW_BUFFERS = 4, GW_THREADS = 512, GW_LOADS = (GM_MOST + GW_N) / 128;
 
-// Tiles of 256 x 256 (pair_gemm_kernel) where their rounds of workgroups on 256 CUs take less time, 1.8 of the others' each: a pair of 11008 x 4096, 2048 tokens (3 rounds and 6) 359 us
-// and 417, 768 tokens (2 and 3) 273 and 265 with what comes ahead.
-inline bool gemm_wide(int64_t large, int64_t tiles) { return 9 * ((large + 255) / 256) <= 5 * ((tiles + 255) / 256); }
+// Tiles of 256 x 256 (pair_gemm_kernel) where their rounds of workgroups on 256 CUs take less time: 1.8 of the others' each, 3 of theirs where they are 128 wide.  A pair of
+// 11008 x 4096, 2048 tokens (3 rounds and 6) 359 us and 417, 768 tokens (2 and 3) 273 and 265 with what comes ahead.
+inline bool gemm_wide(int64_t large, int64_t tiles, int64_t by) { return 9 * ((large + 255) / 256) <= (by == 256 ? 5 : 3) * ((tiles + 255) / 256); }
 
 #ifdef __HIPCC__
 

@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
 EPS = 16 * 2.0 ** -24
 
-# windq_gated, windq_gated_grad: few bfloat16 tokens; the general kernel; tiles; halves by known units, by small units, by many chunks; halves' fallbacks
+# windq_gated, windq_gated_grad: few bfloat16 tokens; the general kernel; tiles (fp32); halves by known units, by small units, by many chunks; halves' fallbacks
 GATED = [(256, 512, 128, 0, 7, BF), (256, 512, 128, 0, 7, F32), (100, 256, 128, 0, 90, BF), (1096, 512, 128, 0, 300, BF), (1096, 512, 128, 0, 700, F32), (256, 512, 128, 0, 400, BF),
          (72, 256, 64, 8, 321, BF), (64, 4160, 8, 0, 330, BF), (35, 800, 160, 0, 400, BF), (1001, 512, 128, 0, 400, BF)]
 # 8-bit tokens: few by one and by two fragments, tiles (by rounds of workgroups), fp32 weights among them
