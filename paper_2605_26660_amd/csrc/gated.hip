@@ -316,6 +316,11 @@ int launch_gated_tiles(const ProjectArgs& Q, char* ws, const GatedWs& at, hipStr
     return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
 }
 
+// fp32: 16 rows by 16 tokens a workgroup up to so many tiles of 128 rows of both by 128 tokens, whose time is a round's until the CUs are full.  1024 x 4096, 300 tokens (24
+// tiles) 179 us, tiles some 490; 2048 x 2048, 300 tokens (48) 158 and 300, 1000 tokens (128) 472 and 300; 1024 x 4096, 1000 tokens (64) 520 and 493; 1000 x 1056, 1000 tokens (64)
+// 126 and 154; 4096 x 1024, 300 tokens (96) 211 and 164.
+constexpr int64_t PAIR_TILES = 64;
+
 template <typename XT>
 int gated_all(ProjectArgs& Q, const windq_mat* X, char* ws, const GatedWs& at, hipStream_t st) {
     const int64_t T = Q.T;
@@ -331,7 +336,11 @@ int gated_all(ProjectArgs& Q, const windq_mat* X, char* ws, const GatedWs& at, h
             FewArgs F = {Q.P, Q.X, Q.ldx, T, static_cast<uint16_t*>(Q.Y), Q.ldy, nullptr, Q.A, 0, reinterpret_cast<uint4*>(ws + at.frag), reinterpret_cast<float*>(ws + at.few_xs), 0, 0, 0, Q.pair};
             const int steps = Q.P.G % 128 == 0 ? 8 : Q.P.G / 16;
             F.n_kb = (int32_t)(Q.P.cols / (16 * steps));
-            if (T <= PAIR_FEW) return steps == 8 ? launch_pair_few<4>(F, st) : (steps == 6 ? launch_pair_few<3>(F, st) : launch_pair_few<2>(F, st));
+            if (T <= PAIR_FEW) {
+                F.raw = Q.raw;
+                F.ld_raw = Q.ld_raw;
+                return launch_pair_few<uint16_t>(F, st);
+            }
             return steps == 8 ? launch_few<8, true>(F, nullptr, st) : (steps == 6 ? launch_few<6, true>(F, nullptr, st) : launch_few<4, true>(F, nullptr, st));
         }
     }
@@ -340,6 +349,20 @@ int gated_all(ProjectArgs& Q, const windq_mat* X, char* ws, const GatedWs& at, h
         if (T > GATED_MANY && Q.P.rows % 8 == 0) return launch_gated_halves(Q, ws, at, st);
     } else {
         const int S = !mask && T > PROJECT_FEW && (Q.P.rows + 15) / 16 * tokens_in(T, 64) > 512 ? tile_steps(Q.P) : 0;
+        if (pair_fits(Q.P) && pair_fits(Q.pair.up) && fits_launch(tokens_in(Q.P.rows, PR_ROWS) * tokens_in(T, 16), 512) && (S == 0 || tokens_in(Q.P.rows, PT_ROWS / 2) * tokens_in(T, PT_TOKENS) <= PAIR_TILES)) {
+            FewArgs F = {};
+            F.P = Q.P;
+            F.X = Q.X;
+            F.ldx = Q.ldx;
+            F.T = T;
+            F.Y = static_cast<uint16_t*>(Q.Y);
+            F.ldy = Q.ldy;
+            F.pair = Q.pair;
+            F.plane = Q.plane;
+            F.raw = Q.raw;
+            F.ld_raw = Q.ld_raw;
+            return launch_pair_few<float>(F, st);
+        }
         if (S == 8) return launch_gated_tiles<8>(Q, ws, at, st);
         if (S == 6) return launch_gated_tiles<6>(Q, ws, at, st);
         if (S == 4) return launch_gated_tiles<4>(Q, ws, at, st);

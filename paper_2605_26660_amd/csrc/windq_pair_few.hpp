@@ -1,4 +1,4 @@
-// windq_gated for a few tokens of bfloat16: 16 rows of both matrices a workgroup, the k-blocks shared by its wavefronts, half of them the gate's.
+// windq_gated for a few tokens of bfloat16, or for fp32 ones: 16 rows of both matrices by 16 tokens a workgroup, the k-blocks shared by its wavefronts, half of them the gate's.
 //
 // Bound by unpacking and waits, not by the codes (28 MB at 2 bits for a pair of 11008 x 4096).  Tokens are the M side of 16x16x32 instructions and rows the N
 // side, so that a lane has one row, with one scale and one offset, and a quarter of a k-block's columns side by side: its codes are one load of 4 to 32 bytes,
@@ -6,6 +6,7 @@
 // wait for each other's loads; treatments and places of codes are looked up for all of a wavefront's k-blocks at once, ahead.
 //   11008 x 4096 at 2 bits, 1 token 18.4 us, 8 tokens 23.9, 16 tokens 30.6, where 32 rows a workgroup (32x32x16 instructions, codes through LDS, one workgroup a CU: two
 // rounds of them) take 35.9, 38.7 and 44.4; a k-block's codes asked for ahead of the one before: 22.3.
+// fp32, 1000 x 1056, 77 tokens 27 us (by the general kernel 51), 1024 x 4096, 16 tokens 42 (100).
 #pragma once
 
 #include "windq_dx.hpp"
@@ -15,6 +16,10 @@ namespace windq {
 
 constexpr int PR_ROWS = 16;
 constexpr int64_t PAIR_FEW = 16;                             // tokens of an instruction; at all of them ahead of the kernel for more
+
+inline bool pair_fits(const PackArgs& P) {
+    return P.mask == nullptr && P.rows % 8 == 0 && (P.R_u == P.rows || P.R_u % PR_ROWS == 0) && (P.G % 128 == 0 || P.G == 96 || P.G == 64);
+}
 
 #ifdef __HIPCC__
 
@@ -68,8 +73,10 @@ __device__ __forceinline__ void pair_trits(const uint8_t* __restrict__ p, uint32
     }
 }
 
-template <int O, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, 6) void pair_few_kernel(const FewArgs Q) {
+// fp32 tokens are three planes, their codes centred.
+template <typename YT, int O, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, sizeof(YT) == 4 ? 4 : 6) void pair_few_kernel(const FewArgs Q) {
+    constexpr int NP = sizeof(YT) == 4 ? 3 : 1;
     constexpr int EACH = WAVES / 2, COLS = 32 * O;          // wavefronts of a matrix; columns of a k-block
     __shared__ float red[WAVES][4][64];
     __shared__ uint16_t trits_of[256];
@@ -78,14 +85,16 @@ __global__ __launch_bounds__(WAVES * 64, 6) void pair_few_kernel(const FewArgs Q
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
     const int matrix = wave / EACH, turn = wave - matrix * EACH;
     const PackArgs& P = matrix == 1 ? Q.pair.up : Q.P;
-    const uint32_t R_u = (uint32_t)P.R_u, row0 = blockIdx.x * PR_ROWS, rb = row0 / R_u, lrow0 = row0 - rb * R_u;
+    const uint32_t R_u = (uint32_t)P.R_u, tb = blockIdx.x / Q.row_blocks, row0 = (blockIdx.x - tb * Q.row_blocks) * PR_ROWS, rb = row0 / R_u, lrow0 = row0 - rb * R_u;
     const int32_t rows_left = R_u - lrow0 < PR_ROWS ? (int32_t)(R_u - lrow0) : PR_ROWS;
     const uint32_t lr = (uint32_t)(sub < rows_left ? sub : rows_left - 1);
     const int32_t per_chunk = P.G / COLS;
     const int64_t unit0 = (int64_t)rb * P.n_chunks;
     const uint32_t one = 0x3f803f80u;
     const bf16x8 ones = as_bf16x8(make_uint4(one, one, one, one));
-    const uint16_t* const x0 = Q.X + (sub < Q.T ? sub : Q.T - 1) * Q.ldx + q * (8 * O);
+    const int64_t t0 = (int64_t)tb * 16;
+    const int32_t tokens = Q.T - t0 < 16 ? (int32_t)(Q.T - t0) : 16;
+    const uint16_t* const x0 = Q.X + (t0 + (sub < tokens ? sub : tokens - 1)) * Q.ldx + q * (8 * O);
 
     f32x4 tot = {};
     for (int32_t from = turn; from < Q.n_kb; from += 64 * EACH) {
@@ -108,9 +117,11 @@ __global__ __launch_bounds__(WAVES * 64, 6) void pair_few_kernel(const FewArgs Q
             const uint8_t* const codes = P.codes + ((uint64_t)(hi & 0xffffu) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)word, it));
             const int64_t g = (unit0 + j) * R_u + lrow0;
             const float scale = (P.scale + g)[lr], offset = (P.offset + g)[lr];
-            uint4 x[O], w[O];
+            uint4 x[NP][O], w[O];
 #pragma unroll
-            for (int s = 0; s < O; ++s) x[s] = reinterpret_cast<const uint4*>(x0 + (int64_t)kb * COLS)[s];
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int s = 0; s < O; ++s) x[p][s] = reinterpret_cast<const uint4*>(x0 + p * Q.plane + (int64_t)kb * COLS)[s];
             const uint32_t first = (uint32_t)c * COLS + q * (8 * O), row = lr * bpg;
             switch (kind) {
                 case 1: pair_fields<O, 8>(codes + (row + first), w); break;
@@ -132,19 +143,26 @@ __global__ __launch_bounds__(WAVES * 64, 6) void pair_few_kernel(const FewArgs Q
             f32x4 acc = {}, sums = {};
 #pragma unroll
             for (int s = 0; s < O; ++s) {
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(x[s]), as_bf16x8(w[s]), acc, 0, 0, 0);
-                sums = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(x[s]), ones, sums, 0, 0, 0);
+                if (NP == 3 && kind != 0) w[s] = centred(w[s], pk_centre(kind));
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p) {
+                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(x[p][s]), as_bf16x8(w[s]), acc, 0, 0, 0);
+                    sums = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(x[p][s]), ones, sums, 0, 0, 0);
+                }
             }
             if (kind == 0 && P.w_f32 != 0) {
 #pragma unroll 1
                 for (int i = 0; i < 3 * O; ++i) {           // rare: three terms of an octet, x once more from where it lies
                     const int term = i / O, s = i - term * O;
                     const uint4 v = skip_octet(P, row0 + lr, (int64_t)kb * COLS + q * (8 * O) + s * 8, term);
-                    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(reinterpret_cast<const uint4*>(x0 + (int64_t)kb * COLS)[s]), as_bf16x8(v), acc, 0, 0, 0);
+#pragma unroll
+                    for (int p = 0; p < NP; ++p)
+                        if (NP == 1 || p + term < 3)
+                            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(reinterpret_cast<const uint4*>(x0 + p * Q.plane + (int64_t)kb * COLS)[s]), as_bf16x8(v), acc, 0, 0, 0);
                 }
             }
             float alpha, beta;
-            pk_affine(kind, scale, offset, false, alpha, beta);
+            pk_affine(kind, scale, offset, NP == 3, alpha, beta);
 #pragma unroll
             for (int i = 0; i < 4; ++i) tot[i] = fmaf(alpha, acc[i], fmaf(beta, sums[i], tot[i]));
         }
@@ -152,7 +170,7 @@ __global__ __launch_bounds__(WAVES * 64, 6) void pair_few_kernel(const FewArgs Q
 #pragma unroll
     for (int i = 0; i < 4; ++i) red[wave][i][lane] = tot[i];
     __syncthreads();
-    for (int e = threadIdx.x; e < PR_ROWS * Q.T; e += WAVES * 64) {
+    for (int e = threadIdx.x; e < PR_ROWS * tokens; e += WAVES * 64) {
         const int r = e & 15, n = e >> 4, at = (n >> 2) * 16 + r;      // neighbouring lanes: neighbouring rows of a token
         if (r >= rows_left) continue;
         float v = 0.0f, up = 0.0f;
@@ -161,21 +179,31 @@ __global__ __launch_bounds__(WAVES * 64, 6) void pair_few_kernel(const FewArgs Q
             v += red[k][n & 3][at];
             up += red[EACH + k][n & 3][at];
         }
-        const int64_t row = (int64_t)row0 + r;
-        if (!isfinite(v)) v = (float)pk_slow_dot(Q.P, row, Q.X + n * Q.ldx);
-        if (!isfinite(up)) up = (float)pk_slow_dot(Q.pair.up, row, Q.X + n * Q.ldx);
-        store_y(Q.Y + n * Q.ldy + row, pair_result<uint16_t>(Q.pair, n, row, v, up));
+        const int64_t row = (int64_t)row0 + r, t = t0 + n;
+        const YT* const raw = static_cast<const YT*>(Q.raw) + t * Q.ld_raw;
+        if (!isfinite(v)) v = (float)pk_slow_dot(Q.P, row, raw);
+        if (!isfinite(up)) up = (float)pk_slow_dot(Q.pair.up, row, raw);
+        store_y(reinterpret_cast<YT*>(Q.Y) + t * Q.ldy + row, pair_result<YT>(Q.pair, t, row, v, up));
     }
 }
 
-template <int O>
-int launch_pair_few(const FewArgs& Q, hipStream_t st) {
-    const int64_t wgs = tokens_in(Q.P.rows, PR_ROWS);
+template <typename YT, int O>
+int launch_pair_few(FewArgs Q, hipStream_t st) {
+    Q.row_blocks = (uint32_t)tokens_in(Q.P.rows, PR_ROWS);
+    const int64_t wgs = Q.row_blocks * tokens_in(Q.T, 16);
     if (!fits_launch(wgs, wgs > 512 ? 512 : 1024)) return WINDQ_ESHAPE;
-    // eight wavefronts where the rows are two workgroups a CU and more, so that all of them run at once
-    if (wgs > 512) pair_few_kernel<O, 8><<<dim3((uint32_t)wgs), dim3(512), 0, st>>>(Q);
-    else pair_few_kernel<O, 16><<<dim3((uint32_t)wgs), dim3(1024), 0, st>>>(Q);
+    // eight wavefronts where there are two workgroups a CU and more, so that all of them run at once
+    if (wgs > 512) pair_few_kernel<YT, O, 8><<<dim3((uint32_t)wgs), dim3(512), 0, st>>>(Q);
+    else pair_few_kernel<YT, O, 16><<<dim3((uint32_t)wgs), dim3(1024), 0, st>>>(Q);
     return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
+}
+
+// Chunks of whole k-blocks (given by their sixteens of columns).
+template <typename YT>
+int launch_pair_few(FewArgs F, hipStream_t st) {
+    const int steps = F.P.G % 128 == 0 ? 8 : F.P.G / 16;
+    F.n_kb = (int32_t)(F.P.cols / (16 * steps));
+    return steps == 8 ? launch_pair_few<YT, 4>(F, st) : (steps == 6 ? launch_pair_few<YT, 3>(F, st) : launch_pair_few<YT, 2>(F, st));
 }
 
 #endif  // __HIPCC__

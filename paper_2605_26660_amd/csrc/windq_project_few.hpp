@@ -32,6 +32,9 @@ struct FewArgs {
     int32_t fragments;         // of 32 tokens
     uint32_t row_blocks;
     PairArgs pair;
+    int64_t plane;             // fp32 pairs: elements between the planes of X; the caller's X
+    const void* raw;
+    int64_t ld_raw;
 };
 
 // Up to FEW_DIRECT tokens X is read as it lies, a launch less: at 8 tokens 4096 x 4096 takes 13.7 us and 18.5 laid out, 11008 x 4096 25.7 and 31.4 (at 16

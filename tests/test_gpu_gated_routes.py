@@ -18,14 +18,15 @@ LARGE = [(2064, 64, 64, 0, 1930), (2056, 192, 64, 0, 2048), (2080, 384, 128, 32,
 
 
 def check(windq, shape, x, w_dtype=BF, word="silu"):
-    cs = pair(windq, shape, BF, w_dtype=w_dtype, seed=shape[0] % 7)
+    dtype = x.dtype
+    cs = pair(windq, shape, dtype, w_dtype=w_dtype, seed=shape[0] % 7)
     T, rows = shape[4], shape[0]
-    save = torch.full((2, T, rows + 8), 7.0, dtype=BF, device=DEV)
-    out = torch.full((T, rows + 1), 5.0, dtype=BF, device=DEV)
+    save = torch.full((2, T, rows + 8), 7.0, dtype=dtype, device=DEV)
+    out = torch.full((T, rows + 1), 5.0, dtype=dtype, device=DEV)
     h = windq.windq_gated(cs[0].packed, cs[1].packed, x, word, save=(save[0, :, :-8], save[1, :, :-8]), out=out[:, :-1])
-    want, off = forward(cs, x, word, BF)
+    want, off = forward(cs, x, word, dtype)
     for got, w, o in zip((save[0, :, :-8], save[1, :, :-8], h), want, off):
-        close(got, w, o, BF)
+        close(got, w, o, dtype)
     assert torch.all(save[:, :, -8:] == 7.0) and torch.all(out[:, -1] == 5.0)
     # without what the way back needs, rows on 16 bytes: the same
     assert torch.equal(windq.windq_gated(cs[0].packed, cs[1].packed, x, word), h)
@@ -39,21 +40,36 @@ def test_up_to_16_tokens(windq, shape, word, w_dtype):
     check(windq, shape, tokens(shape[4], shape[1], BF, 4, 2.0), w_dtype, word)
 
 
+# up to 64 tokens, and more of them while they are one round of workgroups; past it the half precision product, narrow tiles first
+@pytest.mark.parametrize("shape", [(8224, 256, 128, 32, 33), (352, 768, 96, 32, 64), (256, 512, 128, 0, 700), (40, 640, 64, 0, 1000), (8200, 256, 128, 0, 65), (8192, 128, 64, 0, 130),
+                                   (4104, 512, 256, 0, 257), (16384, 64, 64, 0, 129)])
+def test_tokens_between(windq, shape):
+    check(windq, shape, tokens(shape[4], shape[1], BF, 4, 2.0))
+
+
+# fp32 by 16 rows and 16 tokens a workgroup: the last ones not full, and tiles beyond
+@pytest.mark.parametrize("w_dtype", [BF, F32])
+@pytest.mark.parametrize("shape", FEW + [(1000, 384, 96, 0, 301), (264, 512, 256, 0, 130), (96, 192, 64, 32, 1000), (2048, 256, 128, 0, 600)])
+def test_fp32(windq, shape, w_dtype):
+    check(windq, shape, tokens(shape[4], shape[1], F32, 4, 2.0), w_dtype, "gelu")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("only", range(7))
 @pytest.mark.parametrize("G", [64, 96, 128, 256])
-def test_up_to_16_tokens_of_one_treatment(windq, only, G):
+def test_up_to_16_tokens_of_one_treatment(windq, only, G, dtype):
     """Every column has its place: unit vectors for tokens give the reconstruction's columns."""
     from test_gpu_project import Case
     rows, cols = 48, 4 * G
-    cs = [Case(windq, rows, cols, G, 0, BF, seed=k, only=only) for k in range(2)]
+    cs = [Case(windq, rows, cols, G, 0, dtype, seed=k, only=only) for k in range(2)]
     for first in range(0, cols, 16):
-        x = torch.zeros(16, cols, dtype=BF, device=DEV)
+        x = torch.zeros(16, cols, dtype=dtype, device=DEV)
         x[torch.arange(16), first + torch.arange(16)] = 1.0
-        save = torch.empty(2, 16, rows, dtype=BF, device=DEV)
+        save = torch.empty(2, 16, rows, dtype=dtype, device=DEV)
         windq.windq_gated(cs[0].packed, cs[1].packed, x, save=(save[0], save[1]))
-        (g, u, _), (go, uo, _) = forward(cs, x, "silu", BF)
-        close(save[0], g, go, BF)
-        close(save[1], u, uo, BF)
+        (g, u, _), (go, uo, _) = forward(cs, x, "silu", dtype)
+        close(save[0], g, go, dtype)
+        close(save[1], u, uo, dtype)
 
 
 @pytest.mark.parametrize("shape", [FEW[1], FEW[5], LARGE[2]])
