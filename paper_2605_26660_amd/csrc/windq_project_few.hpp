@@ -307,8 +307,14 @@ int launch_few(FewArgs Q, float* h, hipStream_t st) {
         if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
     }
     const dim3 g((uint32_t)wgs);
-    if (!laid) project_few_kernel<S, 1, 16, false, PAIR><<<g, dim3(1024), 0, st>>>(Q);
-    else if (Q.fragments == 1) project_few_kernel<S, 1, PAIR ? 16 : 8, true, PAIR><<<g, dim3(PAIR ? 1024 : 512), 0, st>>>(Q);
+    if constexpr (!PAIR) {                                  // a pair's few tokens are pair_few_kernel's
+        if (!laid) {
+            project_few_kernel<S, 1, 16, false><<<g, dim3(1024), 0, st>>>(Q);
+            return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
+        }
+    }
+    // two fragments of a pair by sixteen wavefronts would spill: 11008 x 4096, 48 tokens 140 us, by eight 63
+    if (Q.fragments == 1) project_few_kernel<S, 1, PAIR ? 16 : 8, true, PAIR><<<g, dim3(PAIR ? 1024 : 512), 0, st>>>(Q);
     else project_few_kernel<S, 2, 8, true, PAIR><<<g, dim3(512), 0, st>>>(Q);
     return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
 }
