@@ -1,0 +1,27 @@
+"""What the feed-forward calls launch: the host code alone, without a GPU."""
+import ctypes
+
+from host_launches import AT, recorder  # noqa: F401
+from paper_2605_26660_amd import binding
+
+
+def gated(recorder, shape, dtype=binding.WINDQ_BF16, w_dtype=None, mask=False, codes_bytes=1 << 30):
+    """One call of windq_gated with made-up addresses. -> (status, the launches' names)"""
+    B, L, ref = binding, recorder.lib, ctypes.byref
+    rows, cols, G, unit_rows, T = shape
+    W = B.windq_mat(AT, dtype if w_dtype is None else w_dtype, 0, rows, cols, cols)
+    X = B.windq_mat(AT, dtype, 0, T, cols, cols)
+    P = B.windq_packed(ctypes.pointer(W), AT if mask else None, AT, AT, AT, codes_bytes, AT, AT, G, 0, unit_rows)
+    need = L.windq_gated_workspace_bytes(0, dtype, T, rows, cols, G)
+    L.recorded_clear()
+    status = L.windq_gated(ref(P), ref(P), ref(X), 0, AT, rows, AT, AT, rows, AT, need, None)
+    return status, " ".join(x.name for x in recorder.launches())
+
+
+def test_the_routes_tests_take_the_routes_they_name(recorder):
+    """The shapes that are compared with 64 bits on the GPU, kernel by kernel: a rule that moves one of them to another kernel shows here."""
+    import test_gpu_feedforward_routes as R
+
+    for kernels, shape in R.HALVES:
+        status, names = gated(recorder, shape)
+        assert status == 0 and all(k in names for k in kernels), (kernels, shape, names)
