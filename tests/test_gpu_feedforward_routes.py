@@ -19,7 +19,9 @@ HALVES = [(("gated_halves_kernelILb1ELi4E", "dx_gemm_kernelILi2ELb1ELb1E"), (109
           (("gated_halves_kernelILb1ELi2E", "dx_gemm_kernelILi2ELb1ELb1E"), (2048, 448, 64, 64, 700)),
           (("gated_halves_kernelILb1ELi0E", "dx_gemm_kernelILi2ELb1ELb1E"), (1096, 1120, 160, 0, 400)),
           (("gated_halves_kernelILb0ELi0E", "dx_gemm_kernelILi2ELb1ELb1E"), (1032, 896, 128, 24, 700)),
-          (("gated_halves_kernelILb1ELi4E", "dx_gemm_kernelILi4ELb1ELb1E"), (2048, 896, 128, 0, 2048))]
+          (("gated_halves_kernelILb1ELi4E", "dx_gemm_kernelILi4ELb1ELb1E"), (2048, 896, 128, 0, 2048)),
+          (("gated_halves_kernelILb1ELi4E", "pair_gemm_kernel"), (2080, 384, 128, 32, 2047)),
+          (("gated_halves_kernelILb1ELi3E", "pair_gemm_kernel"), (2056, 672, 96, 0, 2047))]
 SHAPES = [shape for _, shape in HALVES]
 
 
@@ -51,7 +53,7 @@ def test_tokens_at_both_ends_of_the_range(windq, shape, size):
 
 
 @pytest.mark.parametrize("only", range(7))
-@pytest.mark.parametrize("shape", [SHAPES[k] for k in (0, 1, 2, 3, 4)])
+@pytest.mark.parametrize("shape", [SHAPES[k] for k in (0, 1, 2, 3, 4, 7)])
 def test_one_treatment(windq, shape, only):
     """The reconstruction as it lies, in units of whole blocks of rows, and the product behind it."""
     rows, cols, G, unit_rows, T = shape
@@ -100,7 +102,7 @@ def test_rows_further_apart(windq, shape):
     assert torch.all(out[:, 0] == 5.0) and torch.all(out[:, -2:] == 5.0) and torch.all(save[:, :, :2] == 7.0) and torch.all(save[:, :, -3:] == 7.0)
 
 
-@pytest.mark.parametrize("shape", [SHAPES[0]])
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[7]])
 def test_on_a_stream_of_its_own(windq, shape):
     """The call waits for nothing but its stream, whose earlier work it sees."""
     rows, cols, _, _, T = shape
@@ -128,7 +130,7 @@ def test_on_a_stream_of_its_own(windq, shape):
 
 
 @pytest.mark.parametrize("word", ["silu", "gelu"])
-@pytest.mark.parametrize("shape", [SHAPES[k] for k in (0, 2, 3, 5)])
+@pytest.mark.parametrize("shape", [SHAPES[k] for k in (0, 2, 3, 5, 8)])
 def test_there_and_back(windq, shape, word):
     rows, cols, _, _, T = shape
     cs = pair(windq, shape, BF, seed=3)
