@@ -22,6 +22,6 @@ def test_the_routes_tests_take_the_routes_they_name(recorder):
     """The shapes that are compared with 64 bits on the GPU, kernel by kernel: a rule that moves one of them to another kernel shows here."""
     import test_gpu_feedforward_routes as R
 
-    for kernels, shape in R.HALVES:
+    for kernels, shape in R.HALVES + R.EXACT:
         status, names = gated(recorder, shape)
         assert status == 0 and all(k in names for k in kernels), (kernels, shape, names)

@@ -22,6 +22,10 @@ HALVES = [(("gated_halves_kernelILb1ELi4E", "dx_gemm_kernelILi2ELb1ELb1E"), (109
           (("gated_halves_kernelILb1ELi4E", "dx_gemm_kernelILi4ELb1ELb1E"), (2048, 896, 128, 0, 2048)),
           (("gated_halves_kernelILb1ELi4E", "pair_gemm_kernel"), (2080, 384, 128, 32, 2047)),
           (("gated_halves_kernelILb1ELi3E", "pair_gemm_kernel"), (2056, 672, 96, 0, 2047))]
+# kernels that do not round weights, whatever the tokens: for few of them, and the general one
+EXACT = [(("project_few_kernelILi6ELi2ELi8ELb1ELb1E",), (1000, 1056, 96, 0, 77)), (("project_few_kernelILi8ELi2ELi8ELb1ELb1E",), (256, 512, 128, 0, 700)),
+         (("project_few_kernelILi4ELi2ELi8ELb1ELb1E",), (40, 640, 64, 0, 1000)), (("project_kernelItLi2ELb0ELb1E",), (1001, 512, 128, 0, 400)),
+         (("project_kernelItLi2ELb0ELb1E",), (2002, 256, 128, 0, 2047)), (("project_kernelItLi1ELb0ELb1E",), (35, 800, 160, 0, 400))]
 SHAPES = [shape for _, shape in HALVES]
 
 
@@ -36,6 +40,19 @@ def memory():
 @pytest.mark.parametrize("shape", SHAPES)
 def test_values(windq, shape, word):
     check(windq, shape, tokens(shape[4], shape[1], BF, 4, 2.0), word=word)
+
+
+@pytest.mark.parametrize("w_dtype", [BF, F32])
+@pytest.mark.parametrize("shape", [shape for _, shape in EXACT])
+def test_values_where_no_weight_is_rounded(windq, shape, w_dtype):
+    """As many tokens as others have in half precision, without the room that it takes."""
+    cs = pair(windq, shape, BF, w_dtype=w_dtype, seed=shape[0] % 7)
+    x = tokens(shape[4], shape[1], BF, 4, 2.0)
+    save = torch.empty(2, shape[4], shape[0], dtype=BF, device=DEV)
+    h = windq.windq_gated(cs[0].packed, cs[1].packed, x, save=(save[0], save[1]))
+    want, off = forward(cs, x, "silu", F32)
+    for got, w, o in zip((save[0], save[1], h), want, off):
+        close(got, w, o, BF)
 
 
 @pytest.mark.parametrize("size", [2.0 ** 100, 2.0 ** -100])
