@@ -825,7 +825,7 @@ int windq_gated8(const windq_serving* gate, const windq_serving* up, const windq
  *   G, U  [tokens][rows] of X's type, ld_save >= rows: the products, rounded once, that windq_gated_grad starts from; both or neither
  * gate and up: of one shape, chunk_w, unit_rows and weight type; treatments and masks are their own.  At most 2^31 - 1 tokens x rows.
  * Workspace: windq_gated_workspace_bytes (256-byte aligned), written anew by every call.
- * In WINDQ_BF16 the weights of many tokens enter the product in half precision (11 bits), each eight rows times a power of two of their own, where rows is a
+ * In WINDQ_BF16 the weights of many tokens enter the product in half precision (11 bits), each row times a power of two of its own, where rows is a
  * multiple of 8; elsewhere as in windq_project.  No output may overlap another or an input.
  * Low-rank adapters of gate or up are windq_project's; dG and dU below are what their gradients (windq_project_grad with P NULL) start from.
  */

@@ -11,7 +11,7 @@
 namespace windq {
 
 // Many bfloat16 tokens: the matrices are reconstructed in half precision, once a call, and multiplied by a plain product (windq_gemm.hpp).  Both factors have 11 bits of
-// significand, and powers of two for a token and for eight rows that bring them below 2^15, so that what lies 2^28 below the largest of them still has all of its
+// significand, and powers of two for a token and for a row that bring them below 2^15, so that what lies 2^28 below the largest of them still has all of its
 // digits: the weights' rounding (tokens have none: bfloat16's eight bits fit) is eight times as fine as G's and U's own.
 // From 65 tokens on, unless the kernel for few tokens has them all in one round of workgroups: 11008 x 4096, 128 tokens 88 us (by it some 130), 64 tokens 87 and 67 by it; 4096 x 4096, 128 tokens
 // 57 and 38 by it (one round), 192 tokens 56 and 148; unpacking for every 128 tokens anew (as fp32 calls do) 118, 97 and 105.
@@ -21,7 +21,7 @@ inline bool gated_few(const PackArgs& P, const PackArgs& up, int64_t T) {
 }
 
 struct GatedWs {
-    size_t planes, frag, few_xs, fields[2], unit[2], xs, beta[2], alpha[2], w, x, by_token, by_octet, total;
+    size_t planes, frag, few_xs, fields[2], unit[2], xs, beta[2], alpha[2], w, x, by_token, by_row, total;
 };
 
 // Rows of both matrices, 32 and 32 in turn, filled up to whole tiles.
@@ -52,7 +52,7 @@ GatedWs gated_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t G
     w.w = take(halves ? (size_t)gated_rows(rows) * (size_t)gemm_k(cols) * 2 : 0);
     w.x = take(halves ? (size_t)T * (size_t)gemm_k(cols) * 2 : 0);
     w.by_token = take(halves ? (size_t)T * 4 : 0);
-    w.by_octet = take(halves ? (size_t)gated_rows(rows) / 8 * 4 : 0);
+    w.by_row = take(halves ? (size_t)gated_rows(rows) * 4 : 0);
     w.total = at == 0 ? 256 : at;
     return w;
 }
@@ -64,7 +64,7 @@ struct HalvesArgs {
     uint16_t* x;               // [T][K]
     float* by_token;
     uint16_t* w;               // [rows of both in turn, 32 and 32][K]
-    float* by_octet;
+    float* by_row;
 };
 
 // Workgroups ahead: 16 rows of a matrix, the longer ones; the others: a token.  A wavefront has a k-block of them at a time, of one treatment, a lane a row and a quarter of its
@@ -75,7 +75,7 @@ constexpr int HALVES_UNITS = 512, HALVES_ROWS = 16;
 
 template <bool KNOWN, int O>                               // units of whole blocks of rows, and few enough of them in a row; O: chunks of one or more 32 O columns, no mask, or 0
 __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, const int64_t first) {
-    __shared__ float most[4][2];
+    __shared__ float most[4][HALVES_ROWS];
     __shared__ uint16_t trits_of[256];
     __shared__ uint64_t units[HALVES_UNITS];
     const int64_t blocks = (Q.P[0].rows + HALVES_ROWS - 1) / HALVES_ROWS, block = first + blockIdx.x, id = block - 2 * blocks;
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
             const int a = pk_action(P, rb * P.n_chunks + j, base);
             units[j] = (uint64_t)a << 56 | (uint64_t)(a == 0 ? 0 : base);
         }
-    // the largest magnitudes of eight rows
+    // the rows' largest magnitudes
     float m = 0.0f;
     const int64_t row = r0 + (threadIdx.x & 15);
     if constexpr (KNOWN) {                                  // rows of skip units by all threads: one that looks through 128 weights by itself takes as long as all the rest
@@ -138,19 +138,18 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
     }
     m = fmaxf(m, __shfl_xor(m, 32, 64));
     m = fmaxf(m, __shfl_xor(m, 16, 64));
-#pragma unroll
-    for (int d = 4; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-    if (lane == 0 || lane == 8) most[wave][lane >> 3] = m;
+    if (lane < HALVES_ROWS) most[wave][lane] = m;
     __syncthreads();
+    auto power_of = [&](int r) { return power_below(fmaxf(fmaxf(most[0][r], most[1][r]), fmaxf(most[2][r], most[3][r]))); };
     if constexpr (O > 0) {
         // 16 rows by 32 O columns a wavefront at a time, a lane a row and O octets of it, whose codes are one load; they leave through LDS by whole lines
         constexpr int COLS = 32 * O, LD = 4 * O + 1;        // a row's sixteens of bytes in LDS
         __shared__ uint4 turned[4][16 * LD];
-        const int sub = lane & 15, q = lane >> 4, eight = sub >> 3;
-        const float by = power_below(fmaxf(fmaxf(most[0][eight], most[1][eight]), fmaxf(most[2][eight], most[3][eight])));
+        const int sub = lane & 15, q = lane >> 4;
+        const float by = power_of(sub);
         const int32_t there = P.rows - r0 < HALVES_ROWS ? (int32_t)(P.rows - r0) : HALVES_ROWS;
         const uint32_t lr = (uint32_t)(sub < there ? sub : there - 1);
-        if (wave == 0 && (lane == 0 || lane == 8) && sub < there) Q.by_octet[(at >> 3) + eight] = 1.0f / by;
+        if (wave == 0 && lane < there) Q.by_row[at + lane] = 1.0f / by;
         uint4* const mine = turned[wave];
         const int32_t per_chunk = P.G / COLS;
         const uint32_t lrow0 = (uint32_t)(r0 - rb * P.R_u);
@@ -205,14 +204,14 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
         return;
     }
     const int octet = wave & 1, part = octet * 4 + (lane >> 4);
-    const float by = power_below(fmaxf(fmaxf(most[0][octet], most[1][octet]), fmaxf(most[2][octet], most[3][octet])));
+    const float by[2] = {power_of(part * 2), power_of(part * 2 + 1)};
     const int64_t here = r0 + part * 2;
     if (here >= P.rows) return;                             // rows come in eights
-    if (wave < 2 && lane == 0) Q.by_octet[(at >> 3) + octet] = 1.0f / by;
+    if (wave < 2 && (lane & 15) < 2) Q.by_row[at + part * 2 + (lane & 15)] = 1.0f / ((lane & 15) == 0 ? by[0] : by[1]);
     for (int64_t c = (wave >> 1) * 128 + (lane & 15) * 8; c < Q.K; c += 256) {
         uint32_t w[2][4] = {};
         auto put = [&](int i, int k, float v) {
-            const uint32_t b = half_bits<_Float16>(v * by);
+            const uint32_t b = half_bits<_Float16>(v * by[i]);
             w[i][k >> 1] = (k & 1) != 0 ? w[i][k >> 1] | b << 16 : b;
         };
         if (c < P.cols) {
@@ -238,7 +237,7 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
 int launch_gated_halves(const ProjectArgs& Q, char* ws, const GatedWs& at, hipStream_t st) {
     const int64_t K = gemm_k(Q.P.cols), rows = gated_rows(Q.P.rows), tall = tokens_in(Q.T, GM_N);
     const HalvesArgs H = {{Q.P, Q.pair.up}, Q.X, Q.ldx, Q.T, K, reinterpret_cast<uint16_t*>(ws + at.x), reinterpret_cast<float*>(ws + at.by_token),
-                          reinterpret_cast<uint16_t*>(ws + at.w), reinterpret_cast<float*>(ws + at.by_octet)};
+                          reinterpret_cast<uint16_t*>(ws + at.w), reinterpret_cast<float*>(ws + at.by_row)};
     const bool mask = Q.P.mask != nullptr || Q.pair.up.mask != nullptr;
     const bool known = (Q.P.R_u == Q.P.rows || Q.P.R_u % HALVES_ROWS == 0) && Q.P.n_chunks <= HALVES_UNITS;
     const int status = launch_pieces(Q.T + 2 * tokens_in(Q.P.rows, HALVES_ROWS), 256, [&](int64_t first, dim3 g) {
@@ -265,7 +264,7 @@ int launch_gated_halves(const ProjectArgs& Q, char* ws, const GatedWs& at, hipSt
     M.tiles = (int32_t)tiles;
     M.each = (int32_t)(K / GM_K);
     M.by_token = H.by_token;
-    M.by_octet = H.by_octet;
+    M.by_row = H.by_row;
     M.gate = Q.P;
     M.pair = Q.pair;
     M.raw = Q.X;

@@ -38,6 +38,7 @@ struct GemmArgs {
     // Of a pair (windq_gated) `columns` are rows of the gate and of the up, 32 and 32 in turn, and dX is H.
     PackArgs gate;
     PairArgs pair;
+    const float* by_row;       // the powers of those rows
     const uint16_t* raw;       // the caller's X
     int64_t ld_raw;
 };
@@ -81,10 +82,11 @@ __device__ __forceinline__ void pair_tile(const GemmArgs& Q, f32x16 (&acc)[MF][2
             bool bad = false;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const int by = token + exponent_of(Q.by_octet[(c >> 3) + g]);
+                const float4 rows4 = *reinterpret_cast<const float4*>(Q.by_row + c + g * 8 + hh * 4);
+                const float by[4] = {rows4.x, rows4.y, rows4.z, rows4.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    acc[f][n][g * 4 + i] = ldexpf(acc[f][n][g * 4 + i], by);
+                    acc[f][n][g * 4 + i] = ldexpf(acc[f][n][g * 4 + i], token + exponent_of(by[i]));
                     bad |= !isfinite(acc[f][n][g * 4 + i]);
                 }
             }
