@@ -825,8 +825,10 @@ int windq_gated8(const windq_serving* gate, const windq_serving* up, const windq
  *   G, U  [tokens][rows] of X's type, ld_save >= rows: the products, rounded once, that windq_gated_grad starts from; both or neither
  * gate and up: of one shape, chunk_w, unit_rows and weight type; treatments and masks are their own.  At most 2^31 - 1 tokens x rows.
  * Workspace: windq_gated_workspace_bytes (256-byte aligned), written anew by every call.
- * In WINDQ_BF16 the weights of many tokens enter the product in half precision (11 bits), each row times a power of two of its own, where rows is a
- * multiple of 8; elsewhere as in windq_project.  No output may overlap another or an input.
+ * In WINDQ_BF16 with rows a multiple of 8, and more than 64 tokens in more than 256 pieces of 32 rows by 64 tokens (or a mask, chunks other than 64, 96 and multiples of
+ * 128, units not of whole 32s of rows, or codes_bytes no multiple of 16), weights enter the product in half precision: 11 bits, 2^-12 of a weight, each row and each token times a power of two of its own.  What lies
+ * 2^28 and more below the largest of its row or token loses digits, but results do not: one that this could change by 2^-10 of its value is formed again weight by weight, as
+ * one that is not finite is.  Elsewhere no weight is rounded, so that a token may come out in other last bits from a larger batch.  No output may overlap another or an input.
  * Low-rank adapters of gate or up are windq_project's; dG and dU below are what their gradients (windq_project_grad with P NULL) start from.
  */
 int windq_gated(const windq_packed* gate /*HOST*/, const windq_packed* up /*HOST*/, const windq_mat* X, int32_t act, void* H, int64_t ld_h,

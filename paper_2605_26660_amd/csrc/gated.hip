@@ -62,7 +62,7 @@ struct HalvesArgs {
     const uint16_t* X;
     int64_t ldx, T, K;
     uint16_t* x;               // [T][K]
-    float* by_token;
+    float* by_token;           // powers, and losses in them (with_loss)
     uint16_t* w;               // [rows of both in turn, 32 and 32][K]
     float* by_row;
 };
@@ -75,14 +75,14 @@ constexpr int HALVES_UNITS = 512, HALVES_ROWS = 16;
 
 template <bool KNOWN, int O>                               // units of whole blocks of rows, and few enough of them in a row; O: chunks of one or more 32 O columns, no mask, or 0
 __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, const int64_t first) {
-    __shared__ float most[4][HALVES_ROWS];
+    __shared__ float most[4][HALVES_ROWS], losses[4][HALVES_ROWS];
     __shared__ uint16_t trits_of[256];
     __shared__ uint64_t units[HALVES_UNITS];
     const int64_t blocks = (Q.P[0].rows + HALVES_ROWS - 1) / HALVES_ROWS, block = first + blockIdx.x, id = block - 2 * blocks;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     if (id >= 0) {
         const uint16_t* __restrict__ const x = Q.X + id * Q.ldx;
-        float m = 0.0f;
+        float m = 0.0f, lost = 0.0f;
         for (int64_t c = threadIdx.x * 8; c < Q.P[0].cols; c += 2048) {
             float v[8];
             load8(x + c, v);
@@ -94,15 +94,24 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
         if (lane == 0) most[wave][0] = m;
         __syncthreads();
         const float by = power_below(fmaxf(fmaxf(most[0][0], most[1][0]), fmaxf(most[2][0], most[3][0])));
-        if (threadIdx.x == 0) Q.by_token[id] = 1.0f / by;
+        const bool narrow = by >= 0x1p-16f;                 // no value becomes zero, and 8 bits are all there from 2^-14 on
         for (int64_t c = threadIdx.x * 8; c < Q.K; c += 2048) {
             float v[8] = {};
             if (c < Q.P[0].cols) load8(x + c, v);
             uint32_t w[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = half_bits<_Float16>(v[i] * by);
+            for (int i = 0; i < 8; ++i) {
+                const float y = v[i] * by;
+                w[i] = half_bits<_Float16>(y);
+                lost += narrow ? fabsf(y - (float)(_Float16)y) * 0x1p25f : half_lost(v[i], y);
+            }
             *reinterpret_cast<uint4*>(Q.x + id * Q.K + c) = pack8(w);
         }
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) lost += __shfl_xor(lost, d, 64);
+        if (lane == 0) losses[wave][0] = lost;
+        __syncthreads();
+        if (threadIdx.x == 0) Q.by_token[id] = with_loss(1.0f / by, losses[0][0] + losses[1][0] + losses[2][0] + losses[3][0]);
         return;
     }
     trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
@@ -115,32 +124,67 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
             const int a = pk_action(P, rb * P.n_chunks + j, base);
             units[j] = (uint64_t)a << 56 | (uint64_t)(a == 0 ? 0 : base);
         }
-    // the rows' largest magnitudes
-    float m = 0.0f;
+    // A row's groups by sixteen threads: group(treatment, number) for those of codes, weight(value) for what stays as it is.
     const int64_t row = r0 + (threadIdx.x & 15);
-    if constexpr (KNOWN) {                                  // rows of skip units by all threads: one that looks through 128 weights by itself takes as long as all the rest
-        __syncthreads();
-        const int64_t g0 = rb * P.n_chunks * P.R_u + row - rb * P.R_u;
-        if (row < P.rows)
-            for (int32_t j = threadIdx.x >> 4; j < P.n_chunks; j += 16)
-                if (const int a = (int)(units[j] >> 56); a != 0) m = affine_max(P, a, g0 + j * P.R_u, m);
-        for (int32_t j = 0; j < P.n_chunks; ++j) {
-            if ((units[j] >> 56) != 0 || row >= P.rows) continue;
-            for (int32_t c = (int32_t)(threadIdx.x >> 4) * 8; c < P.G; c += 128) {
+    auto look = [&](auto group, auto weight) {
+        auto weights = [&](int64_t j, int32_t first, int32_t step) {
+#pragma unroll 2
+            for (int32_t c = first; c < P.G; c += step) {
                 float w[8];
-                skip_row(P, row, (int64_t)j * P.G + c, w);
+                skip_row(P, row, j * P.G + c, w);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) m = finite_max(m, w[i]);
+                for (int i = 0; i < 8; ++i) weight(w[i]);
+            }
+        };
+        if (row >= P.rows) return;
+        if constexpr (KNOWN) {                              // rows of skip units by all threads: one that looks through 128 weights by itself takes as long as all the rest
+            const int64_t g0 = rb * P.n_chunks * P.R_u + row - rb * P.R_u;
+            for (int32_t j = threadIdx.x >> 4; j < P.n_chunks; j += 16)
+                if (const int a = (int)(units[j] >> 56); a != 0) group(a, g0 + j * P.R_u);
+            for (int32_t j = 0; j < P.n_chunks; ++j)
+                if ((units[j] >> 56) == 0) weights(j, (int32_t)(threadIdx.x >> 4) * 8, 128);
+        } else {
+            const int64_t own = row / P.R_u;
+            for (int64_t j = threadIdx.x >> 4; j < P.n_chunks; j += 16) {
+                const int64_t u = own * P.n_chunks + j;
+                int64_t base;
+                const int a = pk_action(P, u, base);
+                if (a != 0) group(a, u * P.R_u + row - own * P.R_u);
+                else weights(j, 0, 8);
             }
         }
-    } else if (row < P.rows) {
-        for (int64_t j = threadIdx.x >> 4; j < P.n_chunks; j += 16) m = group_max(P, row, j, m);
-    }
+    };
+    // the rows' largest magnitudes, and the smallest that half precision may take something from
+    float m = 0.0f, least_group = 3.40282347e38f, least_weight = least_group;
+    if constexpr (KNOWN) __syncthreads();
+    look(
+        [&](int a, int64_t g) {
+            const float top = affine_top(P, a, g);
+            m = fmaxf(m, top);
+            least_group = top > 0.0f && top < least_group ? top : least_group;
+        },
+        [&](float w) {
+            m = finite_max(m, w);
+            least_weight = w != 0.0f && fabsf(w) < least_weight ? fabsf(w) : least_weight;
+        });
     m = fmaxf(m, __shfl_xor(m, 32, 64));
     m = fmaxf(m, __shfl_xor(m, 16, 64));
     if (lane < HALVES_ROWS) most[wave][lane] = m;
     __syncthreads();
     auto power_of = [&](int r) { return power_below(fmaxf(fmaxf(most[0][r], most[1][r]), fmaxf(most[2][r], most[3][r]))); };
+    {
+        const float by = power_of(threadIdx.x & 15);
+        float lost = 0.0f;
+        if (__any(least_group * by < HALF_GROUP || least_weight * by < HALF_NORMAL)) {         // rare
+            look([&](int a, int64_t g) { lost += P.G * group_lost(P, a, g, by); }, [&](float w) { lost += half_lost(w, w * by); });
+            lost += __shfl_xor(lost, 32, 64);
+            lost += __shfl_xor(lost, 16, 64);
+        }
+        if (lane < HALVES_ROWS) losses[wave][lane] = lost;
+        __syncthreads();
+        if (threadIdx.x < HALVES_ROWS && row < P.rows)
+            Q.by_row[at + threadIdx.x] = with_loss(1.0f / by, losses[0][threadIdx.x] + losses[1][threadIdx.x] + losses[2][threadIdx.x] + losses[3][threadIdx.x]);
+    }
     if constexpr (O > 0) {
         // 16 rows by 32 O columns a wavefront at a time, a lane a row and O octets of it, whose codes are one load; they leave through LDS by whole lines
         constexpr int COLS = 32 * O, LD = 4 * O + 1;        // a row's sixteens of bytes in LDS
@@ -149,7 +193,6 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
         const float by = power_of(sub);
         const int32_t there = P.rows - r0 < HALVES_ROWS ? (int32_t)(P.rows - r0) : HALVES_ROWS;
         const uint32_t lr = (uint32_t)(sub < there ? sub : there - 1);
-        if (wave == 0 && lane < there) Q.by_row[at + lane] = 1.0f / by;
         uint4* const mine = turned[wave];
         const int32_t per_chunk = P.G / COLS;
         const uint32_t lrow0 = (uint32_t)(r0 - rb * P.R_u);
@@ -207,7 +250,6 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
     const float by[2] = {power_of(part * 2), power_of(part * 2 + 1)};
     const int64_t here = r0 + part * 2;
     if (here >= P.rows) return;                             // rows come in eights
-    if (wave < 2 && (lane & 15) < 2) Q.by_row[at + part * 2 + (lane & 15)] = 1.0f / ((lane & 15) == 0 ? by[0] : by[1]);
     for (int64_t c = (wave >> 1) * 128 + (lane & 15) * 8; c < Q.K; c += 256) {
         uint32_t w[2][4] = {};
         auto put = [&](int i, int k, float v) {

@@ -253,11 +253,18 @@ __device__ __forceinline__ void turn(const PackArgs& P, int32_t K, int64_t ld, f
 // The largest finite magnitude that the weights of a row's group can have, and the power of two that brings magnitudes up to `most` below 2^15 (1 where
 // there are none), itself within fp32's normal numbers.
 __device__ __forceinline__ float finite_max(float m, float x) { return isfinite(x) && fabsf(x) > m ? fabsf(x) : m; }
-__device__ __forceinline__ float affine_max(const PackArgs& P, int a, int64_t g, float m) {
+__device__ __forceinline__ float affine_top(const PackArgs& P, int a, int64_t g) {
     const float s = P.scale[g], o = a >= 5 ? 0.0f : P.offset[g];
     const float L = a == 1 ? 255.0f : (a == 2 ? 15.0f : (a == 3 ? 7.0f : (a == 4 ? 3.0f : 1.0f)));
     const float top = isfinite(s) ? fminf(fabsf(fmaf(s, L, o)), 3.40282347e38f) : 0.0f;       // codes that are there may be smaller ones than L
-    return finite_max(finite_max(m, o), isfinite(o) ? top : 0.0f);
+    return isfinite(o) ? fmaxf(fabsf(o), top) : 0.0f;
+}
+// half_lost of each weight of a group: no more than half a step and than the largest.  From HALF_GROUP on a group's weights are off by 2^-15 of its largest at most, and nothing
+// counts as lost.
+constexpr float HALF_GROUP = 0x1p-10f;
+__device__ __forceinline__ float group_lost(const PackArgs& P, int a, int64_t g, float by) {
+    const float top = affine_top(P, a, g);
+    return top > 0.0f && top * by < HALF_GROUP ? fmaxf(fminf(top * by, 0x1p-25f), 0x1p-100f) * 0x1p25f : 0.0f;
 }
 __device__ __forceinline__ float group_max(const PackArgs& P, int64_t row, int64_t j, float m) {
     const int64_t rb = row / P.R_u, u = rb * P.n_chunks + j;
@@ -273,7 +280,7 @@ __device__ __forceinline__ float group_max(const PackArgs& P, int64_t row, int64
         }
         return m;
     }
-    return affine_max(P, a, u * P.R_u + row - rb * P.R_u, m);
+    return fmaxf(m, affine_top(P, a, u * P.R_u + row - rb * P.R_u));
 }
 __device__ __forceinline__ float power_below(float most) {
     const int e = (int)(__float_as_uint(most) >> 23);       // biased; most < 2^(e - 126)

@@ -38,7 +38,7 @@ struct GemmArgs {
     // Of a pair (windq_gated) `columns` are rows of the gate and of the up, 32 and 32 in turn, and dX is H.
     PackArgs gate;
     PairArgs pair;
-    const float* by_row;       // the powers of those rows
+    const float* by_row;       // the powers of those rows, and as in by_token what rounding has taken from them (with_loss)
     const uint16_t* raw;       // the caller's X
     int64_t ld_raw;
 };
@@ -65,6 +65,18 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 // Of a power of two.  Two of them are put on by their exponents: their product, or a result times the first, may lie outside fp32 where the result does not.
 __device__ __forceinline__ int exponent_of(float power) { return (int)((__float_as_uint(power) >> 23) & 0xffu) - 127; }
 
+// What half precision takes from a value x that enters as y, x times a power of two: y below its normal numbers (2^-14) is rounded to a multiple of 2^-24, which may
+// be all of it.  A factor of the product is below 2^15, so that a sum is off by 2^15 of what is lost; times 2^25: the results, as they come out of the product, for which
+// that is 2^-10 and more.  One below what its token and its row have lost is formed again weight by weight.
+constexpr float HALF_NORMAL = 0x1p-14f;
+__device__ __forceinline__ float half_lost(float x, float y) {
+    const float off = fabsf(y) < HALF_NORMAL && x != 0.0f ? fmaxf(fabsf(y - (float)(_Float16)y), y == 0.0f ? 0x1p-100f : 0.0f) : 0.0f;
+    return off * 0x1p25f;
+}
+// A power of two with a loss in its last fifteen bits: the loss as bfloat16, rounded up.  Whoever reads the power reads its exponent.
+__device__ __forceinline__ float with_loss(float power, float lost) { return __uint_as_float(__float_as_uint(power) | (__float_as_uint(lost) + 0xffffu) >> 16); }
+__device__ __forceinline__ float loss_in(float word) { return __uint_as_float(__float_as_uint(word) << 16 & 0x7fff0000u); }
+
 // H, G and U of a pair's tile: a wavefront has MF x 2 fragments, 2 p and 2 p + 1 along the rows are the gate's and the up's of the same 32 rows.  What is written
 // goes through LDS (`out`), one after the other: a lane has four rows of a token, and 8 bytes of each of 32 tokens are written at a third of the rate of whole lines.
 template <int MF, int THREADS>
@@ -72,38 +84,72 @@ __device__ __forceinline__ void pair_tile(const GemmArgs& Q, f32x16 (&acc)[MF][2
     constexpr int ROWS = MF * 32, LD = ROWS + 8, WM = MF * 32, TOKENS = THREADS / 2;       // of a token in LDS; of a tile
     const int64_t rows = Q.gate.rows;
     const int lane = tid & 63, sub = lane & 31, hh = lane >> 5;
+    // Powers come off; what is then not finite, or lies too low, is noted.  A fragment's powers are loaded while the one before it is gone through.
+    float by_token[2];
+    float4 next[4];
+    auto load_powers = [&](int f) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) next[g] = *reinterpret_cast<const float4*>(Q.by_row + c0 + wm * WM + f * 32 + g * 8 + hh * 4);
+    };
+    load_powers(0);
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
         const int64_t t = t0 + wn * 64 + n * 32 + sub;
-        const int token = exponent_of(Q.by_token[t < Q.T ? t : Q.T - 1]);
+        by_token[n] = Q.by_token[t < Q.T ? t : Q.T - 1];
+    }
+    uint32_t bad = 0;
 #pragma unroll
-        for (int f = 0; f < MF; ++f) {
-            const int64_t c = c0 + wm * WM + f * 32, first = (c >> 6) * 32 + hh * 4;
-            bool bad = false;
+    for (int f = 0; f < MF; ++f) {
+        float by[16];
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const float4 rows4 = *reinterpret_cast<const float4*>(Q.by_row + c + g * 8 + hh * 4);
-                const float by[4] = {rows4.x, rows4.y, rows4.z, rows4.w};
+        for (int g = 0; g < 4; ++g) by[g * 4] = next[g].x, by[g * 4 + 1] = next[g].y, by[g * 4 + 2] = next[g].z, by[g * 4 + 3] = next[g].w;
+        if (f + 1 < MF) load_powers(f + 1);
+        asm volatile("" ::: "memory");                      // no others ahead: there are no registers for them
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    acc[f][n][g * 4 + i] = ldexpf(acc[f][n][g * 4 + i], token + exponent_of(by[i]));
-                    bad |= !isfinite(acc[f][n][g * 4 + i]);
-                }
+        for (int n = 0; n < 2; ++n) {
+            uint32_t most = 0;                              // of the magnitudes' bits
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float v = acc[f][n][i];
+                acc[f][n][i] = fabsf(v) < loss_in(by_token[n]) + loss_in(by[i]) ? __builtin_nanf("") : ldexpf(v, exponent_of(by_token[n]) + exponent_of(by[i]));
+                const uint32_t bits = __float_as_uint(acc[f][n][i]) & 0x7fffffffu;
+                most = bits > most ? bits : most;
             }
-            // what is not finite so far: weight by weight
-            if (__any(bad && first < rows && t < Q.T)) {
-#pragma unroll 1
-                for (int i = 0; i < 16; ++i) {
-                    const int64_t row = first + (i >> 2) * 8 + (i & 3);
-                    float v = 0.0f;
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) v = i == k ? acc[f][n][k] : v;
-                    if (!isfinite(v) && row < rows && t < Q.T) v = (float)pk_slow_dot((f & 1) == 0 ? Q.gate : Q.pair.up, row, Q.raw + t * Q.ld_raw);
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) acc[f][n][k] = i == k ? v : acc[f][n][k];
-                }
-            }
+            bad |= most >= 0x7f800000u ? 1u << (f * 2 + n) : 0u;
         }
+    }
+    // Weight by weight, a fragment after the other; the code for it once.
+    const bool stored[2] = {t0 + wn * 64 + sub < Q.T, t0 + wn * 64 + 32 + sub < Q.T};
+    uint32_t todo = 0;
+#pragma unroll
+    for (int k = 0; k < 2 * MF; ++k) todo |= __any((bad >> k & 1u) != 0u && stored[k & 1] && ((c0 + wm * WM + (k >> 1) * 32) >> 6) * 32 + hh * 4 < rows) ? 1u << k : 0u;
+#pragma unroll 1
+    for (; todo != 0; todo &= todo - 1) {
+        const int which = __builtin_ctz(todo), f = which >> 1, n = which & 1;
+        float v[16];
+#pragma unroll
+        for (int k = 0; k < 2 * MF; ++k)
+            if (k == which) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = acc[k >> 1][k & 1][i];
+            }
+        const int64_t first = ((c0 + wm * WM + f * 32) >> 6) * 32 + hh * 4, t = t0 + wn * 64 + n * 32 + sub;
+#pragma unroll 1
+        for (int i = 0; i < 16; ++i) {
+            const int64_t row = first + (i >> 2) * 8 + (i & 3);
+            float x = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) x = i == k ? v[k] : x;
+            if (!isfinite(x) && row < rows && t < Q.T) x = (float)pk_slow_dot((f & 1) == 0 ? Q.gate : Q.pair.up, row, Q.raw + t * Q.ld_raw);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] = i == k ? x : v[k];
+        }
+#pragma unroll
+        for (int k = 0; k < 2 * MF; ++k)
+            if (k == which) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[k >> 1][k & 1][i] = v[i];
+            }
     }
     auto lay = [&](auto value) {
         __syncthreads();                                    // everybody is done with what lies there

@@ -68,3 +68,61 @@ def test_rows_far_apart(windq, shape):
     for c, got in zip(cs, saved(windq, cs, x)):
         want, off = products(c, x)
         close(got, want, off, BF)
+
+
+@pytest.mark.parametrize("up", [2.0 ** 45, 2.0 ** 33, 2.0 ** 27, 2.0 ** 15])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_groups_far_above_the_rest_of_their_row(windq, shape, up):
+    """A row whose largest weights meet zeros of a token is the sum of the others."""
+    nc = shape[1] // shape[2]
+    cs = [scaled(windq, c, groups={(3, 1): up, (k * 5, nc - 1): up, (20, 0): up, (shape[0] - 2, 0): up}) for k, c in enumerate(pair(windq, shape, BF))]
+    x = tokens(shape[4], shape[1], BF, 4)
+    for k, j in enumerate((1, nc - 1, 0)):
+        x[k::4, j * shape[2]:(j + 1) * shape[2]] = 0.0
+    for c, got in zip(cs, saved(windq, cs, x)):
+        want, off = products(c, x)
+        close(got, want, off, BF)
+
+
+@pytest.mark.parametrize("up", [2.0 ** 110, 2.0 ** 45, 2.0 ** 33, 2.0 ** 26])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_a_value_far_above_the_rest_of_its_token(windq, shape, up):
+    """What meets a weight of 0 leaves the others to be the sum."""
+    rows, cols, G, _, T = shape
+    cs = [scaled(windq, c, groups={(r, 1): 0.0 for r in (0, 1, 9, 18, 40, rows - 1 - k)}) for k, c in enumerate(pair(windq, shape, BF))]
+    x = tokens(T, cols, BF, 4)
+    x[3::7, G + 5] *= up
+    x[5, G:2 * G] = up
+    for c, got in zip(cs, saved(windq, cs, x)):
+        want, off = products(c, x)
+        close(got, want, off, BF)
+
+
+@pytest.mark.parametrize("up", [2.0 ** 37, 2.0 ** 30])
+@pytest.mark.parametrize("shape", [SHAPES[0], SHAPES[7]])
+def test_values_below_half_precisions_normal_numbers_that_lose_nothing(windq, shape, up):
+    """Powers of two next to one far above them: multiples of 2^-24 behind the token's power, which the product takes as they are."""
+    rows, cols, G, _, T = shape
+    cs = [scaled(windq, c, groups={(r, 1): 0.0 for r in range(0, rows, 3)}) for c in pair(windq, shape, BF)]
+    x = tokens(T, cols, BF, 4).sign()
+    x[:, G + 5] = up
+    for c, got in zip(cs, saved(windq, cs, x)):
+        want, off = products(c, x)
+        close(got, want, off, BF)
+
+
+@pytest.mark.parametrize("size", [2.0 ** -80, 2.0 ** 60])
+def test_both_at_once_and_small_tokens(windq, size):
+    """Rows and tokens of their own ranges: weights and values below what fp32 holds next to them."""
+    shape = SHAPES[0]
+    rows, cols, G, _, T = shape
+    nc = cols // G
+    cs = [scaled(windq, c, rows={2: 2.0 ** -60}, groups={(2, 1): 2.0 ** 110, (11, 2): 2.0 ** 50, (12, 3): 2.0 ** -60}) for c in pair(windq, shape, BF)]
+    x = tokens(T, cols, BF, 4, size)
+    x[1::5, G:2 * G] = 0.0
+    x[2::5, 2 * G:3 * G] = 0.0
+    x[0::5, 3 * G + 1] *= 2.0 ** 60
+    for c, got in zip(cs, saved(windq, cs, x)):
+        want, off = products(c, x)
+        assert np.abs(want).max() < 3e38
+        close(got, want, off + 2.0 ** -133, BF)
