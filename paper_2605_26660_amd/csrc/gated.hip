@@ -425,7 +425,7 @@ int check_pair(const windq_packed* gate, const windq_packed* up, PackArgs* A, Pa
 // significand, where bfloat16's 8 would be as coarse as dX's own rounding three times over (dX 1.7 times as far off as its rounding alone).  Their
 // range is what powers of two make of it: a token's dG and dU, and a chunk's weights in both matrices, are brought below 2^15, and what lies 2^28 below the
 // largest of them still has all of its digits.  The powers come off dX in fp32.
-//   The launch ahead: a workgroup a token (dG, dU and the token's power from a bound on them, |dH U| 1.13 and |dH G|: no activation is steeper than 1.13), and
+//   The launch ahead: a workgroup a token (dG, dU and, from them, the token's power: what an activation shuts out has no part in it), and
 // workgroups of 512 rows by one chunk (the largest magnitude their groups can take).  Then the reconstruction, turned, then the product.
 constexpr int RANGE_ROWS = 512;
 
@@ -480,8 +480,8 @@ __device__ __forceinline__ void store_octet(XT* __restrict__ p, int64_t left, bo
         if (i < left) store_y(p + i, v[i]);
 }
 
-// PER octets of each tensor a thread, kept in registers from the pass for the power to the one that puts it on (bfloat16 calls with whole octets in every row); 0:
-// any number, read twice.
+// PER octets of dG and of dU a thread, kept in registers from where they are formed, and stored for the caller, to where the token's power is put on (bfloat16 calls with whole
+// octets in every row); 0: any number, formed twice.
 template <typename XT, int PER>
 __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
     __shared__ float most[4];
@@ -489,22 +489,7 @@ __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
     const XT* __restrict__ const g = static_cast<const XT*>(Q.G) + t * Q.ld_save;
     const XT* __restrict__ const u = static_cast<const XT*>(Q.U) + t * Q.ld_save;
     float by = 1.0f, m = 0.0f;
-    auto larger = [&](const float (&a)[8], const float (&b)[8], const float (&c)[8]) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) m = fmaxf(m, fminf(fmaxf(fabsf(a[i] * c[i]), fabsf(a[i] * b[i])), 3.40282347e38f));
-    };
-    auto power = [&] {
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-        if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = m;
-        __syncthreads();
-        // a product past fp32 counts as its largest number: what an activation makes of it may be a number again
-        by = power_below(1.13f * fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
-        if (threadIdx.x == 0) Q.by_token[t] = 1.0f / by;
-    };
-    auto finish = [&](int64_t r, const float (&a)[8], const float (&b)[8], const float (&c)[8]) {
-        const int64_t left = Q.rows - r;
-        float dg[8], du[8];
+    auto form = [&](const float (&a)[8], const float (&b)[8], const float (&c)[8], float (&dg)[8], float (&du)[8]) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             float slope;
@@ -512,11 +497,26 @@ __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
             dg[i] = a[i] * c[i] * slope;
             du[i] = a[i] * y;
         }
-        if (Q.dG != nullptr && left > 0) {
-            store_octet(static_cast<XT*>(Q.dG) + t * Q.ld_d + r, left, Q.wide, dg);
-            store_octet(static_cast<XT*>(Q.dU) + t * Q.ld_d + r, left, Q.wide, du);
-        }
-        if (Q.to == nullptr) return;
+    };
+    auto larger = [&](const float (&dg)[8], const float (&du)[8]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = finite_max(finite_max(m, dg[i]), du[i]);
+    };
+    auto power = [&] {
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+        if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = m;
+        __syncthreads();
+        by = power_below(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
+        if (threadIdx.x == 0) Q.by_token[t] = 1.0f / by;
+    };
+    auto keep = [&](int64_t r, const float (&dg)[8], const float (&du)[8]) {
+        const int64_t left = Q.rows - r;
+        if (Q.dG == nullptr || left <= 0) return;
+        store_octet(static_cast<XT*>(Q.dG) + t * Q.ld_d + r, left, Q.wide, dg);
+        store_octet(static_cast<XT*>(Q.dU) + t * Q.ld_d + r, left, Q.wide, du);
+    };
+    auto hand_on = [&](int64_t r, const float (&dg)[8], const float (&du)[8]) {
         if constexpr (sizeof(XT) == 2) {
             uint16_t* const to = static_cast<uint16_t*>(Q.to) + t * 2 * Q.K + r;
             uint32_t w[2][8];
@@ -534,6 +534,7 @@ __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
     };
     if constexpr (PER > 0) {
         uint4 held[PER][3];
+        float dg[PER][8], du[PER][8];
         auto values = [](uint4 v, float (&x)[8]) {
             const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -547,39 +548,24 @@ __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
             held[k][1] = in ? *reinterpret_cast<const uint4*>(g + r) : make_uint4(0u, 0u, 0u, 0u);
             held[k][2] = in ? *reinterpret_cast<const uint4*>(u + r) : make_uint4(0u, 0u, 0u, 0u);
         }
-        float a[8], b[8], c[8];
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
+            float a[8], b[8], c[8];
             values(held[k][0], a);
             values(held[k][1], b);
             values(held[k][2], c);
-            larger(a, b, c);
+            form(a, b, c, dg[k], du[k]);
+            larger(dg[k], du[k]);
+            keep(threadIdx.x * 8 + k * 2048, dg[k], du[k]);
         }
         power();
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
             const int64_t r = threadIdx.x * 8 + k * 2048;
-            if (r >= Q.K) continue;
-            // unpacked anew: the compiler would keep three floats for each of them
-            asm volatile("" : "+v"(held[k][0].x), "+v"(held[k][0].y), "+v"(held[k][0].z), "+v"(held[k][0].w), "+v"(held[k][1].x), "+v"(held[k][1].y), "+v"(held[k][1].z), "+v"(held[k][1].w),
-                         "+v"(held[k][2].x), "+v"(held[k][2].y), "+v"(held[k][2].z), "+v"(held[k][2].w));
-            values(held[k][0], a);
-            values(held[k][1], b);
-            values(held[k][2], c);
-            finish(r, a, b, c);
+            if (r < Q.K) hand_on(r, dg[k], du[k]);
         }
     } else {
-        if (sizeof(XT) == 2 && Q.to != nullptr) {
-            for (int64_t r = threadIdx.x * 8; r < Q.rows; r += 2048) {
-                float a[8], b[8], c[8];
-                load_octet(dh + r, Q.rows - r, Q.wide, a);
-                load_octet(g + r, Q.rows - r, Q.wide, b);
-                load_octet(u + r, Q.rows - r, Q.wide, c);
-                larger(a, b, c);
-            }
-            power();
-        }
-        for (int64_t r = threadIdx.x * 8; r < (Q.to != nullptr ? Q.K : Q.rows); r += 2048) {
+        auto formed = [&](int64_t r, float (&dg)[8], float (&du)[8]) {
             float a[8] = {}, b[8] = {}, c[8] = {};
             const int64_t left = Q.rows - r;
             if (left > 0) {
@@ -587,7 +573,21 @@ __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
                 load_octet(g + r, left, Q.wide, b);
                 load_octet(u + r, left, Q.wide, c);
             }
-            finish(r, a, b, c);
+            form(a, b, c, dg, du);
+        };
+        if (sizeof(XT) == 2 && Q.to != nullptr) {
+            for (int64_t r = threadIdx.x * 8; r < Q.rows; r += 2048) {
+                float dg[8], du[8];
+                formed(r, dg, du);
+                larger(dg, du);
+            }
+            power();
+        }
+        for (int64_t r = threadIdx.x * 8; r < (Q.to != nullptr ? Q.K : Q.rows); r += 2048) {
+            float dg[8], du[8];
+            formed(r, dg, du);
+            keep(r, dg, du);
+            if (Q.to != nullptr) hand_on(r, dg, du);
         }
     }
 }

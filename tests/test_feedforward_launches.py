@@ -25,3 +25,23 @@ def test_the_routes_tests_take_the_routes_they_name(recorder):
     for kernels, shape in R.HALVES + R.EXACT:
         status, names = gated(recorder, shape)
         assert status == 0 and all(k in names for k in kernels), (kernels, shape, names)
+
+
+def gated_grad(recorder, shape, masked=False, dtype=binding.WINDQ_BF16):
+    """One call of windq_gated_grad with made-up addresses. -> (status, the launches' names)"""
+    B, L, ref = binding, recorder.lib, ctypes.byref
+    rows, cols, G, unit_rows, T = shape
+    W, dH = B.windq_mat(AT, dtype, 0, rows, cols, cols), B.windq_mat(AT, dtype, 0, T, rows, rows)
+    P = B.windq_packed(ctypes.pointer(W), AT if masked else None, AT, AT, AT, 1 << 30, AT, AT, G, 0, unit_rows)
+    need = L.windq_gated_workspace_bytes(1, dtype, T, rows, cols, G)
+    L.recorded_clear()
+    status = L.windq_gated_grad(ref(P), ref(P), ref(dH), AT, AT, rows, 0, AT, cols, AT, AT, rows, AT, need, None)
+    return status, " ".join(x.name for x in recorder.launches())
+
+
+def test_the_ways_back_take_the_routes_they_name(recorder):
+    import test_gpu_feedforward_range as R
+
+    for kernels, other, shape, masked in R.BACK:
+        status, names = gated_grad(recorder, shape, masked)
+        assert status == 0 and all(k in names for k in kernels) and other not in names, (kernels, shape, names)

@@ -126,3 +126,44 @@ def test_both_at_once_and_small_tokens(windq, size):
         want, off = products(c, x)
         assert np.abs(want).max() < 3e38
         close(got, want, off + 2.0 ** -133, BF)
+
+
+# kernels (as mangled) that the way back takes, and one that it does not; rows, cols, G, unit_rows, tokens; whether a mask lies over the gate
+BACK = [(("gated_turn_kernelILb1E", "dx_gemm_kernelILi4ELb1ELb0E"), "dx_join_kernel", (72, 4096, 128, 0, 2048), False),
+        (("gated_turn_kernelILb1E", "dx_gemm_kernelILi2ELb1ELb0E"), "dx_join_kernel", (64, 896, 128, 32, 700), False),
+        (("gated_turn_kernelILb1E", "dx_gemm_kernelILi2ELb1ELb0E", "dx_join_kernel"), "ILi4ELb1E", (1096, 672, 96, 0, 70), False),
+        (("gated_turn_kernelILb0E", "dx_gemm_kernelILi2ELb1ELb0E", "dx_join_kernel"), "ILi4ELb1E", (301, 560, 80, 43, 200), False),
+        (("gated_turn_kernelILb0E", "dx_gemm_kernelILi2ELb1ELb0E", "dx_join_kernel"), "ILi4ELb1E", (264, 512, 128, 0, 1), True)]
+WAYS = [(shape, masked) for _, _, shape, masked in BACK]
+
+
+def gradients(cs, dh, g, u, word):
+    """dX and how far off it may be before its own rounding in 64 bits.  Slopes are 0 or 1 and no fp32 function rounds them from |G| = 100 on."""
+    dh, g, u = (t.double().cpu().numpy() for t in (dh, g, u))
+    far = np.abs(g) >= 100
+    near = np.where(far, 0.0, g)
+    up, y = np.where(far, (g > 0) * 1.0, slope(word, near)), np.where(far, np.maximum(g, 0.0), act(word, near))
+    dg, du = dh * u * up, dh * y
+    size = np.where(far, np.abs(up), curve(near)), np.where(far, np.abs(y), np.abs(near) * curve(near))
+    each = [(dg, EPS * np.abs(dh * u) * size[0], cs[0]), (du, EPS * np.abs(dh) * size[1], cs[1])]
+    want = sum(d @ c.w for d, _, c in each)
+    # dG, dU and the weights each half a step of 2^-10, all of it in fp32 sums
+    off = sum(o @ np.abs(c.w) * (1 + 2.0 ** -9) + (EPS + 2 * 2.0 ** -11 + 2.0 ** -21) * (np.abs(d) @ np.abs(c.w)) + 2.0 ** -14 * (np.abs(d) @ c.mag) for d, o, c in each)
+    return want, off + 2.0 ** -10 * np.abs(want)
+
+
+def back(windq, cs, dh, g, u, word="silu"):
+    want, off = gradients(cs, dh, g, u, word)
+    close(windq.windq_gated_grad(cs[0].packed, cs[1].packed, dh, g, u, word)[0], want, off + 2.0 ** -133, BF)
+
+
+@pytest.mark.parametrize("word", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("shape,masked", WAYS)
+def test_a_gate_that_is_shut_takes_nothing_from_its_token(windq, shape, masked, word):
+    """dH U and dH G far above everything else, where the slope and the activation are 0."""
+    rows, cols, _, _, T = shape
+    cs = pair(windq, shape, BF, masked=masked)
+    dh, g, u = tokens(T, rows, BF, 6, 1e-3), tokens(T, rows, BF, 7, 2.0), tokens(T, rows, BF, 8, 1.5)
+    g[::2, 5], u[::2, 5] = -200.0, 2.0 ** 50
+    g[::3, 9] = -2.0 ** 60
+    back(windq, cs, dh, g, u, word)
