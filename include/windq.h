@@ -840,8 +840,9 @@ int windq_gated(const windq_packed* gate /*HOST*/, const windq_packed* up /*HOST
  *   dH  [tokens][rows] (leading dimension >= rows, any); G, U of its type as windq_gated left them
  *   dX  [tokens][cols] of that type, ld_dx >= cols, or NULL: not wanted (then no workspace is either)
  *   dG, dU [tokens][rows] of that type, ld_d >= rows; both or neither, not NULL where dX is
- * dG and dU are formed in fp32 and rounded once on their way out.  In WINDQ_BF16 they and the weights enter dX's product in half precision (11 bits), each token and
- * each chunk times a power of two of its own, so that dX's own rounding outweighs theirs by far; in WINDQ_F32 neither is rounded.  Sums are fp32 in a fixed
+ * dG and dU are formed in fp32 and rounded once on their way out.  In WINDQ_BF16 they and the weights enter dX's product in half precision: 11 bits, 2^-12 of a value, each token
+ * (its dG and dU) and each chunk (of both matrices) times a power of two of its own.  What lies 2^28 and more below the largest of its token or chunk loses digits, but results
+ * do not: a value of dX that this could change by 2^-10 of it is formed again weight by weight.  In WINDQ_F32 neither is rounded.  Sums are fp32 in a fixed
  * order: results are bit-reproducible.  A token that holds something not finite, or a weight that is not, makes what the formula multiplies it with not finite (infinities may come
  * out as NaN); other tokens and columns keep their values.  No output may overlap an input.  At most 2^31 - 1 tokens x rows and tokens x cols, 2^30 - 512 rows.
  */

@@ -93,7 +93,8 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
         for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
         if (lane == 0) most[wave][0] = m;
         __syncthreads();
-        const float by = power_below(fmaxf(fmaxf(most[0][0], most[1][0]), fmaxf(most[2][0], most[3][0])));
+        m = fmaxf(fmaxf(most[0][0], most[1][0]), fmaxf(most[2][0], most[3][0]));
+        const float by = power_below(m);
         const bool narrow = by >= 0x1p-16f;                 // no value becomes zero, and 8 bits are all there from 2^-14 on
         for (int64_t c = threadIdx.x * 8; c < Q.K; c += 2048) {
             float v[8] = {};
@@ -111,7 +112,7 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
         for (int d = 32; d >= 1; d >>= 1) lost += __shfl_xor(lost, d, 64);
         if (lane == 0) losses[wave][0] = lost;
         __syncthreads();
-        if (threadIdx.x == 0) Q.by_token[id] = with_loss(1.0f / by, losses[0][0] + losses[1][0] + losses[2][0] + losses[3][0]);
+        if (threadIdx.x == 0) Q.by_token[id] = m > 0.0f ? with_loss(1.0f / by, losses[0][0] + losses[1][0] + losses[2][0] + losses[3][0]) : power_of_nothing();
         return;
     }
     trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
@@ -171,7 +172,8 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
     m = fmaxf(m, __shfl_xor(m, 16, 64));
     if (lane < HALVES_ROWS) most[wave][lane] = m;
     __syncthreads();
-    auto power_of = [&](int r) { return power_below(fmaxf(fmaxf(most[0][r], most[1][r]), fmaxf(most[2][r], most[3][r]))); };
+    auto most_of = [&](int r) { return fmaxf(fmaxf(most[0][r], most[1][r]), fmaxf(most[2][r], most[3][r])); };
+    auto power_of = [&](int r) { return power_below(most_of(r)); };
     {
         const float by = power_of(threadIdx.x & 15);
         float lost = 0.0f;
@@ -183,7 +185,8 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
         if (lane < HALVES_ROWS) losses[wave][lane] = lost;
         __syncthreads();
         if (threadIdx.x < HALVES_ROWS && row < P.rows)
-            Q.by_row[at + threadIdx.x] = with_loss(1.0f / by, losses[0][threadIdx.x] + losses[1][threadIdx.x] + losses[2][threadIdx.x] + losses[3][threadIdx.x]);
+            Q.by_row[at + threadIdx.x] =
+                most_of(threadIdx.x) > 0.0f ? with_loss(1.0f / by, losses[0][threadIdx.x] + losses[1][threadIdx.x] + losses[2][threadIdx.x] + losses[3][threadIdx.x]) : power_of_nothing();
     }
     if constexpr (O > 0) {
         // 16 rows by 32 O columns a wavefront at a time, a lane a row and O octets of it, whose codes are one load; they leave through LDS by whole lines
@@ -424,7 +427,8 @@ int check_pair(const windq_packed* gate, const windq_packed* up, PackArgs* A, Pa
 // dX is one product whose sum runs along the gate's rows and then the up's.  In bfloat16 calls both factors are half precision numbers: 11 bits of
 // significand, where bfloat16's 8 would be as coarse as dX's own rounding three times over (dX 1.7 times as far off as its rounding alone).  Their
 // range is what powers of two make of it: a token's dG and dU, and a chunk's weights in both matrices, are brought below 2^15, and what lies 2^28 below the
-// largest of them still has all of its digits.  The powers come off dX in fp32.
+// largest of them still has all of its digits.  The powers come off dX in fp32.  What lies lower is counted as lost, token by token and octet of columns by octet, and a value of dX
+// that it could change by 2^-10 is formed again from dH, G, U and the weights in fp64 (dx_again), by the product or by the join of its parts.
 //   The launch ahead: a workgroup a token (dG, dU and, from them, the token's power: what an activation shuts out has no part in it), and
 // workgroups of 512 rows by one chunk (the largest magnitude their groups can take).  Then the reconstruction, turned, then the product.
 constexpr int RANGE_ROWS = 512;
@@ -440,12 +444,14 @@ struct SlopeArgs {
     int64_t ld_d;
     void* to;                  // bfloat16 calls: [T][2 K] in half precision; fp32: [2][T][K]; or null: dX is not wanted
     int64_t K;
-    float* by_token;
+    float* by_token;           // powers, and losses in them (with_loss)
     bool wide;                 // all rows of all tensors on 16 bytes
     PackArgs P[2];
-    float* range;              // [chunks][2][strips]
+    float2* range;             // [chunks][2][strips]
     int32_t strips;
     int64_t ranges;            // workgroups for them
+    int32_t* lost_octet;       // counted by the next launch, zeros so far
+    int64_t octets;
 };
 
 template <typename XT>
@@ -482,13 +488,14 @@ __device__ __forceinline__ void store_octet(XT* __restrict__ p, int64_t left, bo
 
 // PER octets of dG and of dU a thread, kept in registers from where they are formed, and stored for the caller, to where the token's power is put on (bfloat16 calls with whole
 // octets in every row); 0: any number, formed twice.
-template <typename XT, int PER>
+template <typename XT, int PER, int THREADS>
 __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
-    __shared__ float most[4];
+    constexpr int STEP = THREADS * 8, WAVES = THREADS / 64;
+    __shared__ float most[WAVES], losses[WAVES];
     const XT* __restrict__ const dh = static_cast<const XT*>(Q.dH) + t * Q.ld_dh;
     const XT* __restrict__ const g = static_cast<const XT*>(Q.G) + t * Q.ld_save;
     const XT* __restrict__ const u = static_cast<const XT*>(Q.U) + t * Q.ld_save;
-    float by = 1.0f, m = 0.0f;
+    float by = 1.0f, m = 0.0f, lost = 0.0f;
     auto form = [&](const float (&a)[8], const float (&b)[8], const float (&c)[8], float (&dg)[8], float (&du)[8]) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -497,6 +504,16 @@ __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
             dg[i] = a[i] * c[i] * slope;
             du[i] = a[i] * y;
         }
+    };
+    auto formed = [&](int64_t r, float (&dg)[8], float (&du)[8]) {
+        float a[8] = {}, b[8] = {}, c[8] = {};
+        const int64_t left = Q.rows - r;
+        if (left > 0) {
+            load_octet(dh + r, left, Q.wide, a);
+            load_octet(g + r, left, Q.wide, b);
+            load_octet(u + r, left, Q.wide, c);
+        }
+        form(a, b, c, dg, du);
     };
     auto larger = [&](const float (&dg)[8], const float (&du)[8]) {
 #pragma unroll
@@ -507,8 +524,19 @@ __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
         for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
         if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = m;
         __syncthreads();
-        by = power_below(fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
-        if (threadIdx.x == 0) Q.by_token[t] = 1.0f / by;
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) m = fmaxf(m, most[k]);
+        by = power_below(m);
+    };
+    auto power_with_loss = [&] {
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) lost += __shfl_xor(lost, d, 64);
+        if ((threadIdx.x & 63) == 0) losses[threadIdx.x >> 6] = lost;
+        __syncthreads();
+        float all = 0.0f;
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) all += losses[k];
+        if (threadIdx.x == 0) Q.by_token[t] = m > 0.0f ? with_loss(1.0f / by, all) : power_of_nothing();
     };
     auto keep = [&](int64_t r, const float (&dg)[8], const float (&du)[8]) {
         const int64_t left = Q.rows - r;
@@ -525,8 +553,17 @@ __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
                 w[0][i] = half_bits<_Float16>(dg[i] * by);
                 w[1][i] = half_bits<_Float16>(du[i] * by);
             }
-            *reinterpret_cast<uint4*>(to) = pack8(w[0]);
-            *reinterpret_cast<uint4*>(to + Q.K) = pack8(w[1]);
+            const uint4 a = pack8(w[0]), b = pack8(w[1]);
+            *reinterpret_cast<uint4*>(to) = a;
+            *reinterpret_cast<uint4*>(to + Q.K) = b;
+            // seldom: a half below the normal numbers
+            typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+            u16x2 least = {0x7fff, 0x7fff};
+            for (uint32_t x : {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}) least = __builtin_elementwise_min(least, __builtin_bit_cast(u16x2, x & 0x7fff7fffu));
+            if (r < Q.rows && (least[0] < 0x400 || least[1] < 0x400)) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) lost += half_lost(dg[i], dg[i] * by) + half_lost(du[i], du[i] * by);
+            }
         } else {
             store_octet(static_cast<float*>(Q.to) + t * Q.K + r, 8, true, dg);
             store_octet(static_cast<float*>(Q.to) + (Q.T + t) * Q.K + r, 8, true, du);
@@ -542,7 +579,7 @@ __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
         };
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-            const int64_t r = threadIdx.x * 8 + k * 2048;
+            const int64_t r = threadIdx.x * 8 + k * STEP;
             const bool in = r < Q.rows;
             held[k][0] = in ? *reinterpret_cast<const uint4*>(dh + r) : make_uint4(0u, 0u, 0u, 0u);
             held[k][1] = in ? *reinterpret_cast<const uint4*>(g + r) : make_uint4(0u, 0u, 0u, 0u);
@@ -556,66 +593,67 @@ __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
             values(held[k][2], c);
             form(a, b, c, dg[k], du[k]);
             larger(dg[k], du[k]);
-            keep(threadIdx.x * 8 + k * 2048, dg[k], du[k]);
+            keep(threadIdx.x * 8 + k * STEP, dg[k], du[k]);
         }
         power();
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-            const int64_t r = threadIdx.x * 8 + k * 2048;
+            const int64_t r = threadIdx.x * 8 + k * STEP;
             if (r < Q.K) hand_on(r, dg[k], du[k]);
         }
+        power_with_loss();
     } else {
-        auto formed = [&](int64_t r, float (&dg)[8], float (&du)[8]) {
-            float a[8] = {}, b[8] = {}, c[8] = {};
-            const int64_t left = Q.rows - r;
-            if (left > 0) {
-                load_octet(dh + r, left, Q.wide, a);
-                load_octet(g + r, left, Q.wide, b);
-                load_octet(u + r, left, Q.wide, c);
-            }
-            form(a, b, c, dg, du);
-        };
         if (sizeof(XT) == 2 && Q.to != nullptr) {
-            for (int64_t r = threadIdx.x * 8; r < Q.rows; r += 2048) {
+            for (int64_t r = threadIdx.x * 8; r < Q.rows; r += STEP) {
                 float dg[8], du[8];
                 formed(r, dg, du);
                 larger(dg, du);
             }
             power();
         }
-        for (int64_t r = threadIdx.x * 8; r < (Q.to != nullptr ? Q.K : Q.rows); r += 2048) {
+        for (int64_t r = threadIdx.x * 8; r < (Q.to != nullptr ? Q.K : Q.rows); r += STEP) {
             float dg[8], du[8];
             formed(r, dg, du);
             keep(r, dg, du);
             if (Q.to != nullptr) hand_on(r, dg, du);
         }
+        if (sizeof(XT) == 2 && Q.to != nullptr) power_with_loss();
     }
 }
 
-// The largest finite magnitude that a weight of RANGE_ROWS rows of a chunk can have.
+// The largest finite magnitude that a weight of RANGE_ROWS rows of a chunk can have, and the smallest that half precision may take something from (group_range).
+template <int THREADS>
 __device__ __forceinline__ void range_of(const SlopeArgs& Q, int64_t block) {
-    __shared__ float most[4];
+    constexpr int WAVES = THREADS / 64;
+    __shared__ float most[WAVES], least[WAVES];
     const int m = (int)(block / ((int64_t)Q.strips * Q.P[0].n_chunks));
     const PackArgs& P = Q.P[m];
     const int64_t rest = block - (int64_t)m * Q.strips * P.n_chunks, j = rest / Q.strips, strip = rest - j * Q.strips;
-    float most_here = 0.0f;
-    for (int k = threadIdx.x; k < RANGE_ROWS; k += 256) {
+    float most_here = 0.0f, least_here = 3.40282347e38f;
+    for (int k = threadIdx.x; k < RANGE_ROWS; k += THREADS) {
         const int64_t row = strip * RANGE_ROWS + k;
         if (row >= P.rows) break;
-        most_here = group_max(P, row, j, most_here);
+        group_range(P, row, j, most_here, least_here);
     }
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) most_here = fmaxf(most_here, __shfl_xor(most_here, d, 64));
-    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = most_here;
+    for (int d = 32; d >= 1; d >>= 1) {
+        most_here = fmaxf(most_here, __shfl_xor(most_here, d, 64));
+        least_here = fminf(least_here, __shfl_xor(least_here, d, 64));
+    }
+    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = most_here, least[threadIdx.x >> 6] = least_here;
     __syncthreads();
-    if (threadIdx.x == 0) Q.range[(j * 2 + m) * Q.strips + strip] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) most_here = fmaxf(most_here, most[k]), least_here = fminf(least_here, least[k]);
+    if (threadIdx.x == 0) Q.range[(j * 2 + m) * Q.strips + strip] = make_float2(most_here, least_here);
+    if (block == 0)
+        for (int64_t k = threadIdx.x; k < Q.octets; k += THREADS) Q.lost_octet[k] = 0;
 }
 
-template <typename XT, int PER = 0>
-__global__ __launch_bounds__(256) void gated_slopes_kernel(const SlopeArgs Q, const int64_t first) {
+template <typename XT, int PER = 0, int THREADS = 256>
+__global__ __launch_bounds__(THREADS) void gated_slopes_kernel(const SlopeArgs Q, const int64_t first) {
     const int64_t block = first + blockIdx.x;               // the weights' ahead: those of skip units take long
-    if (block < Q.ranges) range_of(Q, block);
-    else slopes<XT, PER>(Q, block - Q.ranges);
+    if (block < Q.ranges) range_of<THREADS>(Q, block);
+    else slopes<XT, PER, THREADS>(Q, block - Q.ranges);
 }
 
 struct GatedTurnArgs {
@@ -623,9 +661,10 @@ struct GatedTurnArgs {
     int32_t K;
     uint16_t* wt;              // [cols][2 K]
     int64_t turns;             // workgroups of a matrix
-    const float* range;
+    const float2* range;
     int32_t strips;
     float* by_octet;
+    int32_t* lost_octet;
 };
 
 template <bool PLAIN>
@@ -636,20 +675,76 @@ __global__ __launch_bounds__(256) void gated_turn_kernel(const GatedTurnArgs Q, 
     const int32_t row_blocks = (Q.K + 255) / 256;
     const int64_t cb = block / row_blocks, col = cb * 64 + (threadIdx.x >> 5) * 8;
     const PackArgs& P = Q.P[m];
-    float most = 0.0f;
+    float most = 0.0f, least = 3.40282347e38f;
     if (col < P.cols) {
-        const float* const range = Q.range + col / P.G * 2 * Q.strips;
-        for (int32_t k = threadIdx.x & 31; k < 2 * Q.strips; k += 32) most = fmaxf(most, range[k]);
+        const float2* const range = Q.range + col / P.G * 2 * Q.strips;
+        for (int32_t k = threadIdx.x & 31; k < 2 * Q.strips; k += 32) most = fmaxf(most, range[k].x), least = fminf(least, range[k].y);
     }
 #pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 32));
+    for (int d = 16; d >= 1; d >>= 1) {
+        most = fmaxf(most, __shfl_xor(most, d, 32));
+        least = fminf(least, __shfl_xor(least, d, 32));
+    }
     const float by = power_below(most);
-    if (id - cb * row_blocks == 0 && (threadIdx.x & 31) == 0 && col < P.cols) Q.by_octet[col >> 3] = 1.0f / by;
+    if (id - cb * row_blocks == 0 && (threadIdx.x & 31) == 0 && col < P.cols) Q.by_octet[col >> 3] = most > 0.0f ? 1.0f / by : power_of_nothing();
+    if (least * by < HALF_GROUP && col < P.cols) {          // rare
+        const int32_t lost = rows_lost(P, (block - cb * row_blocks) * 256 + (threadIdx.x & 31) * 8, col, by);
+        if (lost != 0) atomicAdd(Q.lost_octet + (col >> 3), lost);
+    }
     turn<_Float16, PLAIN>(P, Q.K, 2 * (int64_t)Q.K, by, Q.wt + (int64_t)m * Q.K, block);
 }
 
+// The parts of dX added up, a thread per token and octet of columns; columns that lie too low are formed again.
+struct GatedJoinArgs {
+    GemmArgs M;
+    int32_t splits;
+};
+
+__global__ __launch_bounds__(256) void gated_join_kernel(const GatedJoinArgs J, const int64_t first) {
+    const GemmArgs& Q = J.M;
+    const int lane = threadIdx.x & 63;
+    const int64_t i = (first + blockIdx.x) * 256 + threadIdx.x, octets = Q.cols >> 3;
+    const bool in = i < Q.T * octets;
+    const int64_t t = in ? i / octets : Q.T - 1, o = in ? i - t * octets : 0, c = o * 8;
+    const float by_token = Q.by_token[t], by_octet = Q.by_octet[o];
+    const int32_t lost = Q.lost_octet[o];
+    float v[8] = {};
+#pragma unroll 4
+    for (int32_t s = 0; s < J.splits; ++s) {
+        float p[8];
+        load8(Q.part + (s * Q.T + t) * Q.cols + c, p);
+#pragma unroll
+        for (int m = 0; m < 8; ++m) v[m] += p[m];
+    }
+    const float low = ldexpf(lost_below(by_token, by_octet, lost), exponent_of(by_token) + exponent_of(by_octet));
+    bool bad = false;
+#pragma unroll
+    for (int m = 0; m < 8; ++m) bad |= fabsf(v[m]) < low;
+#pragma unroll 1
+    for (uint64_t left = __ballot(bad && in); left != 0; left &= left - 1) {
+        const int which = __builtin_ctzll(left);
+        const int64_t id = i - lane + which, token = id / octets;
+        double sum[8];
+        dx_again(Q.gate, Q.pair.up, Q.pair.act, Q.again, token, (id - token * octets) * 8, lane, sum);
+#pragma unroll
+        for (int m = 0; m < 8; ++m)
+            if (lane == which && fabsf(v[m]) < low) v[m] = (float)sum[m];
+    }
+    if (!in) return;
+    uint16_t* __restrict__ const out = Q.dX + t * Q.ldx + c;
+    uint32_t w[8];
+#pragma unroll
+    for (int m = 0; m < 8; ++m) w[m] = f32_to_bf16_bits(v[m]);
+    if ((Q.ldx & 7) == 0 && (reinterpret_cast<uintptr_t>(Q.dX) & 15) == 0) {
+        *reinterpret_cast<uint4*>(out) = pack8(w);
+    } else {
+#pragma unroll
+        for (int m = 0; m < 8; ++m) out[m] = (uint16_t)w[m];
+    }
+}
+
 struct GatedGradWs {
-    size_t to, wt, gm, by_token, by_octet, range, dxf, total;
+    size_t to, wt, gm, by_token, by_octet, lost_octet, range, dxf, total;
     int64_t K;
 };
 
@@ -668,7 +763,8 @@ GatedGradWs gated_grad_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, 
     w.gm = take(bf ? (size_t)gemm_parts(T, 2 * w.K, cols) * 4 : 0);
     w.by_token = take(bf ? (size_t)T * 4 : 0);
     w.by_octet = take(bf ? (size_t)(cols / 8 + 1) * 4 : 0);
-    w.range = take(bf ? (size_t)(cols / G + 1) * 2 * (size_t)tokens_in(rows, RANGE_ROWS) * 4 : 0);
+    w.lost_octet = take(bf ? (size_t)(cols / 8 + 1) * 4 : 0);
+    w.range = take(bf ? (size_t)(cols / G + 1) * 2 * (size_t)tokens_in(rows, RANGE_ROWS) * 8 : 0);
     w.dxf = take(bf ? 0 : DXF_BYTES);
     w.total = at == 0 ? 256 : at;
     return w;
@@ -687,19 +783,23 @@ int gated_grad_all(SlopeArgs& S, void* dX, int64_t ld_dx, char* ws, const GatedG
         S.K = at.K;
         if (bf) {
             S.by_token = reinterpret_cast<float*>(ws + at.by_token);
-            S.range = reinterpret_cast<float*>(ws + at.range);
+            S.range = reinterpret_cast<float2*>(ws + at.range);
+            S.lost_octet = reinterpret_cast<int32_t*>(ws + at.lost_octet);
+            S.octets = cols / 8;
             S.strips = (int32_t)tokens_in(P.rows, RANGE_ROWS);
             S.ranges = 2 * (int64_t)S.strips * P.n_chunks;
             ahead += S.ranges;
         }
     }
     const int64_t each = bf && dX != nullptr && S.wide && P.rows % 8 == 0 ? tokens_in(S.K, 2048) : 0;
-    int status = launch_pieces(ahead, 256, [&](int64_t first, dim3 g) {
+    int status = launch_pieces(ahead, 512, [&](int64_t first, dim3 g) {
         if constexpr (bf) {
             if (each == 1) return gated_slopes_kernel<XT, 1><<<g, dim3(256), 0, st>>>(S, first);
-            if (each == 2) return gated_slopes_kernel<XT, 2><<<g, dim3(256), 0, st>>>(S, first);
-            if (each == 3 || each == 4) return gated_slopes_kernel<XT, 4><<<g, dim3(256), 0, st>>>(S, first);
-            if (each == 5 || each == 6) return gated_slopes_kernel<XT, 6><<<g, dim3(256), 0, st>>>(S, first);
+            if (each == 2) return gated_slopes_kernel<XT, 1, 512><<<g, dim3(512), 0, st>>>(S, first);
+            if (each == 3) return gated_slopes_kernel<XT, 3><<<g, dim3(256), 0, st>>>(S, first);
+            if (each == 4) return gated_slopes_kernel<XT, 2, 512><<<g, dim3(512), 0, st>>>(S, first);
+            if (each == 5 || each == 6) return gated_slopes_kernel<XT, 3, 512><<<g, dim3(512), 0, st>>>(S, first);
+            if (each == 7 || each == 8) return gated_slopes_kernel<XT, 4, 512><<<g, dim3(512), 0, st>>>(S, first);
         }
         gated_slopes_kernel<XT><<<g, dim3(256), 0, st>>>(S, first);
     });
@@ -713,7 +813,7 @@ int gated_grad_all(SlopeArgs& S, void* dX, int64_t ld_dx, char* ws, const GatedG
     if constexpr (bf) {
         const int32_t K2 = (int32_t)(2 * at.K);
         const GatedTurnArgs R = {{S.P[0], S.P[1]}, (int32_t)at.K, reinterpret_cast<uint16_t*>(ws + at.wt), ((cols + 63) / 64) * ((at.K + 255) / 256), S.range, S.strips,
-                                 reinterpret_cast<float*>(ws + at.by_octet)};
+                                 reinterpret_cast<float*>(ws + at.by_octet), S.lost_octet};
         const bool plain = P.mask == nullptr && S.P[1].mask == nullptr && P.rows % 8 == 0 && (P.R_u == P.rows || P.R_u % 8 == 0);
         status = launch_pieces(2 * R.turns, 256, [&](int64_t first, dim3 g) {
             if (plain) gated_turn_kernel<true><<<g, dim3(256), 0, st>>>(R, first);
@@ -723,7 +823,11 @@ int gated_grad_all(SlopeArgs& S, void* dX, int64_t ld_dx, char* ws, const GatedG
         // tiles are no more than 2^31 / 128^2 and two sides' edges: one launch holds them
         const int64_t tall = tokens_in(T, GM_N), by = tokens_in(cols, 256) * tall >= GM_TILES ? 256 : 128, tiles = tokens_in(cols, by) * tall;
         GemmArgs M = {R.wt, static_cast<const uint16_t*>(S.to), K2, K2, T, cols, static_cast<uint16_t*>(dX), ld_dx, nullptr, nullptr, {}, (uint32_t)tokens_in(cols, by), nullptr,
-                      (int32_t)tiles, K2 / GM_K, S.by_token, R.by_octet};
+                      (int32_t)tiles, K2 / GM_K, S.by_token, R.by_octet, S.P[0]};
+        M.pair.up = S.P[1];
+        M.pair.act = S.act;
+        M.lost_octet = S.lost_octet;
+        M.again = {static_cast<const uint16_t*>(S.dH), static_cast<const uint16_t*>(S.G), static_cast<const uint16_t*>(S.U), S.ld_dh, S.ld_save};
         if (by == 256) {
             dx_gemm_kernel<4, true><<<dim3((uint32_t)tiles), dim3(GM_THREADS), 0, st>>>(M);
             return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
@@ -731,12 +835,13 @@ int gated_grad_all(SlopeArgs& S, void* dX, int64_t ld_dx, char* ws, const GatedG
         const int32_t each = gemm_each(K2, tiles), splits = (int32_t)tokens_in(K2 / GM_K, each);
         if (splits > 1) {
             M.each = each;
-            M.part = Q.part = reinterpret_cast<float*>(ws + at.gm);
-            Q.splits = splits;
+            M.part = reinterpret_cast<float*>(ws + at.gm);
         }
         dx_gemm_kernel<2, true><<<dim3((uint32_t)(tiles * splits)), dim3(GM_THREADS), 0, st>>>(M);
         if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
-        return splits == 1 ? WINDQ_OK : launch_dx_join(Q, st);
+        if (splits == 1) return WINDQ_OK;
+        const GatedJoinArgs J = {M, splits};
+        return launch_pieces(tokens_in(T * (cols / 8), 256), 256, [&](int64_t first, dim3 g) { gated_join_kernel<<<g, dim3(256), 0, st>>>(J, first); });
     } else {
         Q.dY = S.to;
         Q.ldy = at.K;

@@ -266,7 +266,8 @@ __device__ __forceinline__ float group_lost(const PackArgs& P, int a, int64_t g,
     const float top = affine_top(P, a, g);
     return top > 0.0f && top * by < HALF_GROUP ? fmaxf(fminf(top * by, 0x1p-25f), 0x1p-100f) * 0x1p25f : 0.0f;
 }
-__device__ __forceinline__ float group_max(const PackArgs& P, int64_t row, int64_t j, float m) {
+// A row's group's part in the largest magnitude and in the smallest, weights that stay as they are counting 16 times: HALF_GROUP is 16 HALF_NORMAL.
+__device__ __forceinline__ void group_range(const PackArgs& P, int64_t row, int64_t j, float& most, float& least) {
     const int64_t rb = row / P.R_u, u = rb * P.n_chunks + j;
     int64_t base;
     const int a = pk_action(P, u, base);
@@ -276,11 +277,38 @@ __device__ __forceinline__ float group_max(const PackArgs& P, int64_t row, int64
             float w[8];
             skip_row(P, row, j * P.G + c, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m = finite_max(m, w[i]);
+            for (int i = 0; i < 8; ++i) {
+                most = finite_max(most, w[i]);
+                least = w[i] != 0.0f ? fminf(least, 16.0f * fabsf(w[i])) : least;
+            }
         }
-        return m;
+        return;
     }
-    return fmaxf(m, affine_top(P, a, u * P.R_u + row - rb * P.R_u));
+    const float top = affine_top(P, a, u * P.R_u + row - rb * P.R_u);
+    most = fmaxf(most, top);
+    least = top > 0.0f ? fminf(least, top) : least;
+}
+// Of eight rows from r0 on, those that rounding takes something from in an octet of columns.
+__device__ __forceinline__ int32_t rows_lost(const PackArgs& P, int64_t r0, int64_t col, float by) {
+    const int64_t j = col / P.G;
+    int32_t n = 0;
+#pragma unroll 1
+    for (int64_t row = r0; row < r0 + 8 && row < P.rows; ++row) {
+        const int64_t rb = row / P.R_u, u = rb * P.n_chunks + j;
+        int64_t base;
+        const int a = pk_action(P, u, base);
+        float lost = 0.0f;
+        if (a == 0) {
+            float w[8];
+            skip_row(P, row, col, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) lost += half_lost(w[i], w[i] * by);
+        } else {
+            lost = group_lost(P, a, u * P.R_u + row - rb * P.R_u, by);
+        }
+        n += lost > 0.0f ? 1 : 0;
+    }
+    return n;
 }
 __device__ __forceinline__ float power_below(float most) {
     const int e = (int)(__float_as_uint(most) >> 23);       // biased; most < 2^(e - 126)

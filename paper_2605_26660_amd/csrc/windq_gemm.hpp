@@ -19,6 +19,14 @@ namespace windq {
 
 constexpr int GM_MOST = 256, GM_N = 128, GM_K = 64, GM_THREADS = 256, GM_BUFFERS = 3;
 
+// What dX is formed from again, column by column: the caller's.
+struct AgainArgs {
+    const uint16_t* dH;
+    const uint16_t* G;
+    const uint16_t* U;
+    int64_t ld_dh, ld_save;
+};
+
 struct GemmArgs {
     const uint16_t* wt;        // [cols rounded up to GM_MOST][K]
     const uint16_t* dY;        // [T][ldy], zeros from rows to K
@@ -41,6 +49,9 @@ struct GemmArgs {
     const float* by_row;       // the powers of those rows, and as in by_token what rounding has taken from them (with_loss)
     const uint16_t* raw;       // the caller's X
     int64_t ld_raw;
+    // Of its way back: weights of an octet of columns that rounding has taken something from, by 2^-25 at most.
+    const int32_t* lost_octet;
+    AgainArgs again;
 };
 
 inline int64_t gemm_k(int64_t rows) { return (rows + GM_K - 1) / GM_K * GM_K; }
@@ -73,9 +84,56 @@ __device__ __forceinline__ float half_lost(float x, float y) {
     const float off = fabsf(y) < HALF_NORMAL && x != 0.0f ? fmaxf(fabsf(y - (float)(_Float16)y), y == 0.0f ? 0x1p-100f : 0.0f) : 0.0f;
     return off * 0x1p25f;
 }
-// A power of two with a loss in its last fifteen bits: the loss as bfloat16, rounded up.  Whoever reads the power reads its exponent.
+// A power of two with a loss in its last sixteen bits: the loss as bfloat16, rounded up.  Whoever reads the power reads its exponent.  Where there is nothing but zeros, and
+// nothing to lose, the loss is far below 0, whatever the other side adds.
 __device__ __forceinline__ float with_loss(float power, float lost) { return __uint_as_float(__float_as_uint(power) | (__float_as_uint(lost) + 0xffffu) >> 16); }
-__device__ __forceinline__ float loss_in(float word) { return __uint_as_float(__float_as_uint(word) << 16 & 0x7fff0000u); }
+__device__ __forceinline__ float loss_in(float word) { return __uint_as_float(__float_as_uint(word) << 16); }
+__device__ __forceinline__ float power_of_nothing() { return __uint_as_float(0x0000ff7fu); }
+
+// A kernel's first argument from where it lies, for what is seldom needed: the compiler would load all of it at the kernel's start, into more scalar registers than there are.
+template <typename Args>
+__device__ __forceinline__ const Args& argument_in_place() {
+    typedef const __attribute__((address_space(4))) Args* Place;
+    Place at = (Place)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    return *(const Args*)at;
+}
+
+// Results of a token and an octet of columns below which what both have lost counts.
+__device__ __forceinline__ float lost_below(float by_token, float by_octet, int32_t lost) { return loss_in(by_token) + loss_in(by_octet) + (float)lost; }
+
+// Eight columns of dX of a token in fp64, by all lanes of a wavefront, 64 rows at a time: all of them get the sums.
+__device__ __forceinline__ void dx_again(const PackArgs& gate, const PackArgs& up, int act, const AgainArgs& A, int64_t t, int64_t col, int lane, double (&sum)[8]) {
+    const int32_t j = (int32_t)(col / gate.G), c0 = (int32_t)(col - (int64_t)j * gate.G);
+#pragma unroll
+    for (int m = 0; m < 8; ++m) sum[m] = 0.0;
+#pragma unroll 1
+    for (int64_t row = lane; row < gate.rows; row += 64) {
+        const float a = bf16_bits_to_f32(A.dH[t * A.ld_dh + row]), g = bf16_bits_to_f32(A.G[t * A.ld_save + row]), u = bf16_bits_to_f32(A.U[t * A.ld_save + row]);
+        float slope;
+        const float y = activation<true>(act, g, slope);
+        const float d[2] = {a * u * slope, a * y};
+        const int64_t rb = row / gate.R_u, lrow = row - rb * gate.R_u, unit = rb * gate.n_chunks + j;
+#pragma unroll 1
+        for (int k = 0; k < 2; ++k) {
+            const PackArgs& P = k == 0 ? gate : up;
+            int64_t base;
+            const int kind = pk_action(P, unit, base);
+            const uint8_t* const codes = P.codes + base + lrow * pk_bytes_per_group(kind, P.G);
+            const float s = P.scale[unit * P.R_u + lrow], o = P.offset[unit * P.R_u + lrow];
+            const uint32_t mask = kind != 0 && P.mask != nullptr ? P.mask[row * P.mask_ld + (col >> 3)] : 0u;
+#pragma unroll
+            for (int m = 0; m < 8; ++m) {
+                const double w = kind == 0 ? (double)elem(P.W, row * P.ld + col + m, P.w_f32 != 0) : pk_weight(kind, codes, c0 + m, s, o);
+                sum[m] = fma((double)d[k], (mask >> m & 1u) != 0u ? 0.0 : w, sum[m]);
+            }
+        }
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1)
+#pragma unroll
+        for (int m = 0; m < 8; ++m) sum[m] += __shfl_xor(sum[m], d, 64);
+}
 
 // H, G and U of a pair's tile: a wavefront has MF x 2 fragments, 2 p and 2 p + 1 along the rows are the gate's and the up's of the same 32 rows.  What is written
 // goes through LDS (`out`), one after the other: a lane has four rows of a token, and 8 bytes of each of 32 tokens are written at a third of the rate of whole lines.
@@ -134,13 +192,14 @@ __device__ __forceinline__ void pair_tile(const GemmArgs& Q, f32x16 (&acc)[MF][2
                 for (int i = 0; i < 16; ++i) v[i] = acc[k >> 1][k & 1][i];
             }
         const int64_t first = ((c0 + wm * WM + f * 32) >> 6) * 32 + hh * 4, t = t0 + wn * 64 + n * 32 + sub;
+        const GemmArgs& A = argument_in_place<GemmArgs>();
 #pragma unroll 1
         for (int i = 0; i < 16; ++i) {
             const int64_t row = first + (i >> 2) * 8 + (i & 3);
             float x = 0.0f;
 #pragma unroll
             for (int k = 0; k < 16; ++k) x = i == k ? v[k] : x;
-            if (!isfinite(x) && row < rows && t < Q.T) x = (float)pk_slow_dot((f & 1) == 0 ? Q.gate : Q.pair.up, row, Q.raw + t * Q.ld_raw);
+            if (!isfinite(x) && row < rows && t < Q.T) x = (float)pk_slow_dot((f & 1) == 0 ? A.gate : A.pair.up, row, A.raw + t * A.ld_raw);
 #pragma unroll
             for (int k = 0; k < 16; ++k) v[k] = i == k ? x : v[k];
         }
@@ -291,18 +350,82 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
 
     if constexpr (PAIR) return pair_tile<MF, GM_THREADS>(Q, acc, reinterpret_cast<uint16_t*>(tile), c0, t0, wm, wn, tid);
     if constexpr (HALF) {
+        // a tile's octets by lanes
+        const int64_t mine = (c0 >> 3) + (lane < GM_M / 8 ? lane : 0), last = (Q.cols >> 3) - 1;
+        const float octet_power = Q.by_octet[mine < last ? mine : last];
+        const int octet_lost = Q.lost_octet[mine < last ? mine : last];
+        auto power_of = [&](int k) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(octet_power), k)); };
+        auto below = [&](float by_token, int k) { return lost_below(by_token, power_of(k), __builtin_amdgcn_readlane(octet_lost, k)); };
+        const int octet0 = wm * (WM / 8);
+        uint32_t todo = 0;                                  // fragments with something that lies too low; of a part of the sum the join says so
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
             const int64_t t = t0 + wn * 64 + n * 32 + sub;
-            const int token = exponent_of(Q.by_token[t < Q.T ? t : Q.T - 1]);
+            const float by_token = Q.by_token[t < Q.T ? t : Q.T - 1];
 #pragma unroll
-            for (int f = 0; f < MF; ++f)
+            for (int f = 0; f < MF; ++f) {
+                bool bad = false;
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const int64_t c = c0 + wm * WM + f * 32 + g * 8;
-                    const int by = token + exponent_of(Q.by_octet[(c < Q.cols ? c : 0) >> 3]);
+                    const float low = below(by_token, octet0 + f * 4 + g);
+                    const int by = exponent_of(by_token) + exponent_of(power_of(octet0 + f * 4 + g));
+                    float least = fabsf(acc[f][n][g * 4]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[f][n][g * 4 + i] = ldexpf(acc[f][n][g * 4 + i], by);
+                    for (int i = 0; i < 4; ++i) {
+                        least = fminf(least, fabsf(acc[f][n][g * 4 + i]));
+                        acc[f][n][g * 4 + i] = ldexpf(acc[f][n][g * 4 + i], by);
+                    }
+                    bad |= least < low && c < Q.cols;
+                }
+                todo |= __any(bad && t < Q.T) ? 1u << (f * 2 + n) : 0u;
+            }
+        }
+        if (Q.part != nullptr) todo = 0;
+#pragma unroll 1
+        for (; todo != 0; todo &= todo - 1) {
+            const int which = __builtin_ctz(todo), f = which >> 1, n = which & 1;
+            float v[16];
+#pragma unroll
+            for (int k = 0; k < 2 * MF; ++k)
+                if (k == which) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = acc[k >> 1][k & 1][i];
+                }
+            const int64_t t = t0 + wn * 64 + n * 32 + sub;
+            const float by_token = Q.by_token[t < Q.T ? t : Q.T - 1];
+            const GemmArgs& A = argument_in_place<GemmArgs>();
+#pragma unroll 1
+            for (int g = 0; g < 4; ++g) {
+                const int64_t c = c0 + wm * WM + f * 32 + g * 8;
+                if (c >= Q.cols) break;
+                const float low = below(by_token, octet0 + f * 4 + g);
+                const int by = exponent_of(by_token) + exponent_of(power_of(octet0 + f * 4 + g));
+                float x[4];
+                bool again[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[i] = g == 0 ? v[i] : (g == 1 ? v[4 + i] : (g == 2 ? v[8 + i] : v[12 + i]));
+                    again[i] = fabsf(x[i]) < ldexpf(low, by) && t < Q.T;
+                }
+                const uint64_t lanes = __ballot(again[0] || again[1] || again[2] || again[3]);
+#pragma unroll 1
+                for (uint32_t left = (uint32_t)lanes | (uint32_t)(lanes >> 32); left != 0; left &= left - 1) {
+                    const int token = __builtin_ctz(left);
+                    double sum[8];
+                    dx_again(A.gate, A.pair.up, A.pair.act, A.again, t0 + wn * 64 + n * 32 + token, c, lane, sum);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (sub == token && again[i]) x[i] = (float)(hh != 0 ? sum[4 + i] : sum[i]);
+                }
+#pragma unroll
+                for (int k = 0; k < 16; ++k) v[k] = g == k >> 2 ? x[k & 3] : v[k];
+            }
+#pragma unroll
+            for (int k = 0; k < 2 * MF; ++k)
+                if (k == which) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[k >> 1][k & 1][i] = v[i];
                 }
         }
     }

@@ -129,11 +129,11 @@ def test_both_at_once_and_small_tokens(windq, size):
 
 
 # kernels (as mangled) that the way back takes, and one that it does not; rows, cols, G, unit_rows, tokens; whether a mask lies over the gate
-BACK = [(("gated_turn_kernelILb1E", "dx_gemm_kernelILi4ELb1ELb0E"), "dx_join_kernel", (72, 4096, 128, 0, 2048), False),
-        (("gated_turn_kernelILb1E", "dx_gemm_kernelILi2ELb1ELb0E"), "dx_join_kernel", (64, 896, 128, 32, 700), False),
-        (("gated_turn_kernelILb1E", "dx_gemm_kernelILi2ELb1ELb0E", "dx_join_kernel"), "ILi4ELb1E", (1096, 672, 96, 0, 70), False),
-        (("gated_turn_kernelILb0E", "dx_gemm_kernelILi2ELb1ELb0E", "dx_join_kernel"), "ILi4ELb1E", (301, 560, 80, 43, 200), False),
-        (("gated_turn_kernelILb0E", "dx_gemm_kernelILi2ELb1ELb0E", "dx_join_kernel"), "ILi4ELb1E", (264, 512, 128, 0, 1), True)]
+BACK = [(("gated_turn_kernelILb1E", "dx_gemm_kernelILi4ELb1ELb0E"), "gated_join_kernel", (72, 4096, 128, 0, 2048), False),
+        (("gated_turn_kernelILb1E", "dx_gemm_kernelILi2ELb1ELb0E"), "gated_join_kernel", (64, 896, 128, 32, 700), False),
+        (("gated_turn_kernelILb1E", "dx_gemm_kernelILi2ELb1ELb0E", "gated_join_kernel"), "ILi4ELb1E", (1096, 672, 96, 0, 70), False),
+        (("gated_turn_kernelILb0E", "dx_gemm_kernelILi2ELb1ELb0E", "gated_join_kernel"), "ILi4ELb1E", (301, 560, 80, 43, 200), False),
+        (("gated_turn_kernelILb0E", "dx_gemm_kernelILi2ELb1ELb0E", "gated_join_kernel"), "ILi4ELb1E", (264, 512, 128, 0, 1), True)]
 WAYS = [(shape, masked) for _, _, shape, masked in BACK]
 
 
@@ -167,3 +167,61 @@ def test_a_gate_that_is_shut_takes_nothing_from_its_token(windq, shape, masked, 
     g[::2, 5], u[::2, 5] = -200.0, 2.0 ** 50
     g[::3, 9] = -2.0 ** 60
     back(windq, cs, dh, g, u, word)
+
+
+@pytest.mark.parametrize("up", [2.0 ** 100, 2.0 ** 45, 2.0 ** 30])
+@pytest.mark.parametrize("shape,masked", WAYS)
+def test_a_gradient_far_above_the_rest_of_its_token(windq, shape, masked, up):
+    """Columns whose weights meet it with 0 are the sum of the others."""
+    rows, cols, G, _, T = shape
+    nc = cols // G
+    cs = [scaled(windq, c, groups={(5, 1): 0.0, (5, nc - 1): 0.0, (rows - 1, 0): 0.0}) for c in pair(windq, shape, BF, masked=masked)]
+    dh, g, u = tokens(T, rows, BF, 6, 1e-3), tokens(T, rows, BF, 7, 2.0), tokens(T, rows, BF, 8, 1.5)
+    u[::5, 5] *= up
+    dh[1::5, 5] *= up
+    dh[2::5, rows - 1] *= up
+    back(windq, cs, dh, g, u)
+
+
+@pytest.mark.parametrize("up", [2.0 ** 100, 2.0 ** 45, 2.0 ** 27])
+@pytest.mark.parametrize("shape,masked", WAYS)
+def test_groups_far_above_the_rest_of_their_chunk(windq, shape, masked, up):
+    """Where a token's gradient is 0 in that row the others are its sum; a token of zeros has none at all."""
+    rows, cols, G, _, T = shape
+    nc = cols // G
+    cs = [scaled(windq, c, groups={(7, 1): up, (rows - 2, nc - 1): up if k == 0 else 1.0}) for k, c in enumerate(pair(windq, shape, BF, masked=masked))]
+    dh, g, u = tokens(T, rows, BF, 6, 1e-3), tokens(T, rows, BF, 7, 2.0), tokens(T, rows, BF, 8, 1.5)
+    dh[::4, 7] = 0.0
+    dh[1::4, rows - 2] = 0.0
+    dh[2::4, 7], dh[2::4, rows - 2] = 0.0, 0.0
+    dh[3::8] = 0.0
+    back(windq, cs, dh, g, u)
+
+
+@pytest.mark.parametrize("up", [2.0 ** 60, 2.0 ** 27])
+@pytest.mark.parametrize("shape,masked", WAYS)
+def test_one_weight_far_above_its_chunk(windq, shape, masked, up):
+    """A weight that stays as it is; the other columns of its chunk keep theirs."""
+    rows, cols, G, _, T = shape
+    cs = pair(windq, shape, BF, masked=masked)
+    for unit, c in [(c.action.tolist().index(0), c) for c in cs if 0 in c.action.tolist()]:
+        row, col = unit // (cols // G) * c.R_u + c.R_u // 2, unit % (cols // G) * G + 3
+        c.W, c.w = c.W.clone(), c.w.copy()
+        c.W[row, col] = up
+        c.w[row, col], c.mag[row, col] = up, up
+        c.packed = c.describe(windq)
+    dh, g, u = tokens(T, rows, BF, 6, 1e-3), tokens(T, rows, BF, 7, 2.0), tokens(T, rows, BF, 8, 1.5)
+    back(windq, cs, dh, g, u, "gelu")
+
+
+@pytest.mark.parametrize("size", [2.0 ** -90, 2.0 ** 60])
+@pytest.mark.parametrize("shape,masked", [WAYS[0], WAYS[2], WAYS[3]])
+def test_gradients_and_weights_of_their_own_ranges(windq, shape, masked, size):
+    rows, cols, G, _, T = shape
+    nc = cols // G
+    cs = [scaled(windq, c, groups={(4, 1): 2.0 ** 50, (11, 2): 2.0 ** -60, (12, nc - 1): 2.0 ** 40, (13, nc - 1): 0.0}) for c in pair(windq, shape, BF, masked=masked)]
+    dh, g, u = tokens(T, rows, BF, 6, size), tokens(T, rows, BF, 7, 2.0), tokens(T, rows, BF, 8, 1.5)
+    dh[::3, 4] = 0.0
+    dh[1::3, 13] *= 2.0 ** 50
+    dh[2::3, 12] *= 2.0 ** -60
+    back(windq, cs, dh, g, u, "gelu_tanh")
