@@ -102,30 +102,99 @@ __device__ __forceinline__ const Args& argument_in_place() {
 // Results of a token and an octet of columns below which what both have lost counts.
 __device__ __forceinline__ float lost_below(float by_token, float by_octet, int32_t lost) { return loss_in(by_token) + loss_in(by_octet) + (float)lost; }
 
-// Eight columns of dX of a token in fp64, by all lanes of a wavefront, 64 rows at a time: all of them get the sums.
-__device__ __forceinline__ void dx_again(const PackArgs& gate, const PackArgs& up, int act, const AgainArgs& A, int64_t t, int64_t col, int lane, double (&sum)[8]) {
-    const int32_t j = (int32_t)(col / gate.G), c0 = (int32_t)(col - (int64_t)j * gate.G);
+// Eight columns of dX of a token in fp64, by all lanes of a wavefront, ROWS times 64 rows at a time: all of them get the sums.  Two rounds of loads a turn, without branches between
+// those of a round; 240 us for 11008 rows, where one load after the other takes 480.  Seldom: none of 8.4 M values at G of 1.7 on average, two to four at 8, where
+// most slopes are 0.  WINDOW: code streams of eight bytes and more, read eight at a time.
+template <int ROWS, bool WINDOW>
+__device__ __forceinline__ void dx_again_by(const PackArgs& gate, const PackArgs& up, int act, const AgainArgs& A, int64_t t, int64_t col, int lane, double (&sum)[8]) {
+    const uint32_t j = (uint32_t)(col / gate.G), o = (uint32_t)(col - (int64_t)j * gate.G) >> 3, R_u = (uint32_t)gate.R_u, n_rows = (uint32_t)gate.rows;
 #pragma unroll
     for (int m = 0; m < 8; ++m) sum[m] = 0.0;
 #pragma unroll 1
-    for (int64_t row = lane; row < gate.rows; row += 64) {
-        const float a = bf16_bits_to_f32(A.dH[t * A.ld_dh + row]), g = bf16_bits_to_f32(A.G[t * A.ld_save + row]), u = bf16_bits_to_f32(A.U[t * A.ld_save + row]);
-        float slope;
-        const float y = activation<true>(act, g, slope);
-        const float d[2] = {a * u * slope, a * y};
-        const int64_t rb = row / gate.R_u, lrow = row - rb * gate.R_u, unit = rb * gate.n_chunks + j;
-#pragma unroll 1
-        for (int k = 0; k < 2; ++k) {
-            const PackArgs& P = k == 0 ? gate : up;
-            int64_t base;
-            const int kind = pk_action(P, unit, base);
-            const uint8_t* const codes = P.codes + base + lrow * pk_bytes_per_group(kind, P.G);
-            const float s = P.scale[unit * P.R_u + lrow], o = P.offset[unit * P.R_u + lrow];
-            const uint32_t mask = kind != 0 && P.mask != nullptr ? P.mask[row * P.mask_ld + (col >> 3)] : 0u;
+    for (uint32_t row0 = 0; row0 < n_rows; row0 += 64 * ROWS) {
+        uint32_t row[ROWS], rb[ROWS], action[2][ROWS];
+        uint16_t h[ROWS], g[ROWS], u[ROWS];
+        int64_t base[2][ROWS];
 #pragma unroll
-            for (int m = 0; m < 8; ++m) {
-                const double w = kind == 0 ? (double)elem(P.W, row * P.ld + col + m, P.w_f32 != 0) : pk_weight(kind, codes, c0 + m, s, o);
-                sum[m] = fma((double)d[k], (mask >> m & 1u) != 0u ? 0.0 : w, sum[m]);
+        for (int i = 0; i < ROWS; ++i) {
+            const uint32_t r = row0 + 64 * i + lane;
+            row[i] = r < n_rows ? r : n_rows - 1;
+            rb[i] = row[i] / R_u;
+            h[i] = A.dH[t * A.ld_dh + row[i]];
+            g[i] = A.G[t * A.ld_save + row[i]];
+            u[i] = A.U[t * A.ld_save + row[i]];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const PackArgs& P = k == 0 ? gate : up;
+                action[k][i] = P.action[(int64_t)rb[i] * P.n_chunks + j];
+                base[k][i] = P.code_off[(int64_t)rb[i] * P.n_chunks + j];
+            }
+        }
+        int kind[2][ROWS];
+        float s[2][ROWS], offset[2][ROWS];
+        uint64_t v[2][ROWS];
+        uint4 kept[2][ROWS][2];
+        uint8_t mask[2][ROWS];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i) {
+                const PackArgs& P = k == 0 ? gate : up;
+                const uint32_t lrow = row[i] - rb[i] * R_u;
+                // as pk_action has it
+                const int a = action[k][i] < WINDQ_N_ACTIONS ? (int)action[k][i] : 0;
+                const int64_t bytes = pk_bytes_per_group(a, P.G);
+                const bool fits = (base[k][i] >= 0) & ((base[k][i] & 15) == 0) & (base[k][i] <= P.codes_bytes - bytes * P.R_u);
+                kind[k][i] = fits ? a : 0;
+                const int64_t group = ((int64_t)rb[i] * P.n_chunks + j) * R_u + lrow;
+                s[k][i] = P.scale[group];
+                offset[k][i] = P.offset[group];
+                const uint32_t per = 0x01023480u >> (4 * a) & 15u;     // bytes of an octet
+                const int64_t first = kind[k][i] == 0 ? 0 : base[k][i] + lrow * bytes + (a == 5 ? o * 8u / 5u : o * per);
+                v[k][i] = 0;
+                if constexpr (WINDOW) {                     // eight bytes within the stream
+                    const int64_t from = first < P.codes_bytes - 8 ? first : P.codes_bytes - 8;
+                    uint64_t eight;
+                    __builtin_memcpy(&eight, P.codes + from, 8);
+                    v[k][i] = eight >> (uint32_t)(8 * (first - from));
+                } else {
+                    for (int b = 0; b < 8; ++b)
+                        if (first + b < P.codes_bytes) v[k][i] |= (uint64_t)P.codes[first + b] << (8 * b);
+                }
+                mask[k][i] = 0;
+                if (P.mask != nullptr) mask[k][i] = P.mask[(int64_t)row[i] * P.mask_ld + (col >> 3)];
+                kept[k][i][0] = kept[k][i][1] = make_uint4(0u, 0u, 0u, 0u);
+                if (kind[k][i] == 0) {
+                    const int64_t at = (int64_t)row[i] * P.ld + col;
+                    if (P.w_f32 != 0) {
+                        kept[k][i][0] = reinterpret_cast<const uint4*>(static_cast<const float*>(P.W) + at)[0];
+                        kept[k][i][1] = reinterpret_cast<const uint4*>(static_cast<const float*>(P.W) + at)[1];
+                    } else {
+                        kept[k][i][0] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(P.W) + at);
+                    }
+                }
+            }
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            float slope;
+            const float y = activation<true>(act, bf16_bits_to_f32(g[i]), slope), x = row0 + 64 * i + lane < n_rows ? bf16_bits_to_f32(h[i]) : 0.0f;
+            const float d[2] = {x * bf16_bits_to_f32(u[i]) * slope, x * y};
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const PackArgs& P = k == 0 ? gate : up;
+                const int a = kind[k][i], b = a == 1 ? 8 : (a == 2 ? 4 : (a == 3 ? 3 : (a == 6 ? 1 : 2)));
+                uint32_t lo = (uint32_t)v[k][i];
+                const uint32_t hi = a == 1 ? (uint32_t)(v[k][i] >> 32) : 0u;
+                if (a == 5) lo = (trit_fields(lo & 0xffu) | trit_fields(lo >> 8 & 0xffu) << 10 | trit_fields(lo >> 16 & 0xffu) << 20) >> (2 * (o * 8u % 5u));
+                const float step = a == 6 ? 2.0f : 1.0f, from = a >= 5 ? -1.0f : 0.0f, off = a >= 5 ? 0.0f : offset[k][i];      // code q stands for (step q + from) s + off
+                const uint32_t as_is[8] = {kept[k][i][0].x, kept[k][i][0].y, kept[k][i][0].z, kept[k][i][0].w, kept[k][i][1].x, kept[k][i][1].y, kept[k][i][1].z, kept[k][i][1].w};
+#pragma unroll
+                for (int m = 0; m < 8; ++m) {
+                    const float q = (float)__builtin_amdgcn_ubfe(a == 1 && m >= 4 ? hi : lo, (uint32_t)(b * m) & 31u, (uint32_t)b);
+                    const uint32_t w16 = (m & 1) != 0 ? as_is[m >> 1] & 0xffff0000u : as_is[m >> 1] << 16;
+                    const float coded = (mask[k][i] >> m & 1u) != 0u ? 0.0f : fmaf(fmaf(step, q, from), s[k][i], off), w = __uint_as_float(P.w_f32 != 0 ? as_is[m] : w16);
+                    sum[m] = fma((double)d[k], (double)(a == 0 ? w : coded), sum[m]);
+                }
             }
         }
     }
@@ -133,6 +202,10 @@ __device__ __forceinline__ void dx_again(const PackArgs& gate, const PackArgs& u
     for (int d = 32; d >= 1; d >>= 1)
 #pragma unroll
         for (int m = 0; m < 8; ++m) sum[m] += __shfl_xor(sum[m], d, 64);
+}
+__device__ __forceinline__ void dx_again(const PackArgs& gate, const PackArgs& up, int act, const AgainArgs& A, int64_t t, int64_t col, int lane, double (&sum)[8]) {
+    if (gate.codes_bytes >= 8 && up.codes_bytes >= 8) dx_again_by<2, true>(gate, up, act, A, t, col, lane, sum);
+    else dx_again_by<1, false>(gate, up, act, A, t, col, lane, sum);
 }
 
 // H, G and U of a pair's tile: a wavefront has MF x 2 fragments, 2 p and 2 p + 1 along the rows are the gate's and the up's of the same 32 rows.  What is written

@@ -11,7 +11,7 @@ import torch
 from test_gpu_eight import act, close
 from test_gpu_feedforward_routes import SHAPES
 from test_gpu_gated import EPS, curve, pair, slope
-from test_gpu_project import DEV, tokens
+from test_gpu_project import DEV, Case, tokens
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
@@ -34,6 +34,7 @@ class Scaled:
         W = c.W * torch.from_numpy(wide).to(c.W.dtype).to(DEV)
         group = torch.from_numpy(by.reshape(c.rows // R_u, R_u, nc).transpose(0, 2, 1).reshape(-1, R_u)).to(torch.float32).to(DEV)
         scale, offset = ((t.view(-1, R_u) * group).view(-1).contiguous() for t in (c.scale, c.offset))
+        self.case, self.W, self.scale, self.offset = c, W, scale, offset
         self.packed = c.describe(windq, W=W, scale=scale, offset=offset)
 
 
@@ -225,3 +226,20 @@ def test_gradients_and_weights_of_their_own_ranges(windq, shape, masked, size):
     dh[1::3, 13] *= 2.0 ** 50
     dh[2::3, 12] *= 2.0 ** -60
     back(windq, cs, dh, g, u, "gelu_tanh")
+
+
+@pytest.mark.parametrize("only", range(1, 7))
+@pytest.mark.parametrize("shape", [(1, 8, 8, 0, 3), (4, 8, 8, 0, 3), (9, 8, 8, 0, 70), (301, 40, 8, 0, 5), (64, 256, 128, 0, 9)])
+def test_code_streams_that_end_with_their_last_code(windq, shape, only):
+    """Values formed again read codes eight bytes at a time: within the stream, down to one of a byte."""
+    from oracle import windq_oracle as O
+    rows, cols, G, _, T = shape
+    cs = [Case(windq, rows, cols, G, 0, BF, seed=k, only=only) for k in range(2)]
+    cs = [scaled(windq, c, rows={rows // 2: 0.0} if rows > 1 else {}) for c in cs]
+    end = int(windq.windq_plan_layout(torch.full((cols // G,), only, dtype=torch.uint8), rows, G)[-2]) + O.bytes_per_group(only, G) * rows
+    dh, g, u = tokens(T, rows, BF, 6, 1e-3), tokens(T, rows, BF, 7, 2.0), tokens(T, rows, BF, 8, 1.5)
+    if rows > 1:
+        u[:, rows // 2] = 2.0 ** 50
+    packed = [c.case.describe(windq, W=c.W, scale=c.scale, offset=c.offset, codes=c.case.codes[:end].clone()) for c in cs]
+    want, off = gradients(cs, dh, g, u, "silu")
+    close(windq.windq_gated_grad(packed[0], packed[1], dh, g, u)[0], want, off + 2.0 ** -133, BF)
