@@ -377,7 +377,7 @@ int gated_all(ProjectArgs& Q, const windq_mat* X, char* ws, const GatedWs& at, h
         Q.plane = T * Q.P.cols;
     } else {
         if (gated_few(Q.P, Q.pair.up, T)) {
-            FewArgs F = {Q.P, Q.X, Q.ldx, T, static_cast<uint16_t*>(Q.Y), Q.ldy, nullptr, Q.A, 0, reinterpret_cast<uint4*>(ws + at.frag), reinterpret_cast<float*>(ws + at.few_xs), 0, 0, 0, Q.pair};
+            FewArgs F = {Q.P, Q.X, Q.ldx, T, static_cast<uint16_t*>(Q.Y), Q.ldy, nullptr, Q.A, 0, reinterpret_cast<uint4*>(ws + at.frag), reinterpret_cast<float*>(ws + at.few_xs), 0, 0, 0, 0, Q.pair};
             const int steps = Q.P.G % 128 == 0 ? 8 : Q.P.G / 16;
             F.n_kb = (int32_t)(Q.P.cols / (16 * steps));
             if (T <= PAIR_FEW) {

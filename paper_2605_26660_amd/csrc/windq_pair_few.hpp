@@ -85,7 +85,7 @@ __global__ __launch_bounds__(WAVES * 64, sizeof(YT) == 4 ? 4 : 6) void pair_few_
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, sub = lane & 15, q = lane >> 4;
     const int matrix = wave / EACH, turn = wave - matrix * EACH;
     const PackArgs& P = matrix == 1 ? Q.pair.up : Q.P;
-    const uint32_t R_u = (uint32_t)P.R_u, tb = blockIdx.x / Q.row_blocks, row0 = (blockIdx.x - tb * Q.row_blocks) * PR_ROWS, rb = row0 / R_u, lrow0 = row0 - rb * R_u;
+    const uint32_t R_u = (uint32_t)P.R_u, block = Q.first + blockIdx.x, tb = block / Q.row_blocks, row0 = (block - tb * Q.row_blocks) * PR_ROWS, rb = row0 / R_u, lrow0 = row0 - rb * R_u;
     const int32_t rows_left = R_u - lrow0 < PR_ROWS ? (int32_t)(R_u - lrow0) : PR_ROWS;
     const uint32_t lr = (uint32_t)(sub < rows_left ? sub : rows_left - 1);
     const int32_t per_chunk = P.G / COLS;
@@ -191,11 +191,12 @@ template <typename YT, int O>
 int launch_pair_few(FewArgs Q, hipStream_t st) {
     Q.row_blocks = (uint32_t)tokens_in(Q.P.rows, PR_ROWS);
     const int64_t wgs = Q.row_blocks * tokens_in(Q.T, 16);
-    if (!fits_launch(wgs, wgs > 512 ? 512 : 1024)) return WINDQ_ESHAPE;
-    // eight wavefronts where there are two workgroups a CU and more, so that all of them run at once
-    if (wgs > 512) pair_few_kernel<YT, O, 8><<<dim3((uint32_t)wgs), dim3(512), 0, st>>>(Q);
-    else pair_few_kernel<YT, O, 16><<<dim3((uint32_t)wgs), dim3(1024), 0, st>>>(Q);
-    return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
+    return launch_pieces(wgs, wgs > 512 ? 512 : 1024, [&](int64_t first, dim3 g) {
+        Q.first = (uint32_t)first;
+        // eight wavefronts where there are two workgroups a CU and more, so that all of them run at once
+        if (wgs > 512) pair_few_kernel<YT, O, 8><<<g, dim3(512), 0, st>>>(Q);
+        else pair_few_kernel<YT, O, 16><<<g, dim3(1024), 0, st>>>(Q);
+    });
 }
 
 // Chunks of whole k-blocks (given by their sixteens of columns).

@@ -31,6 +31,7 @@ struct FewArgs {
     int64_t xs_ld;             // tokens in 64s
     int32_t fragments;         // of 32 tokens
     uint32_t row_blocks;
+    uint32_t first;            // of the workgroups of this launch
     PairArgs pair;
     int64_t plane;             // fp32 pairs: elements between the planes of X; the caller's X
     const void* raw;
@@ -125,8 +126,8 @@ __global__ __launch_bounds__(WAVES * 64) void project_few_kernel(const FewArgs Q
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, sub = lane & 31, hh = lane >> 5;
     const int matrix = PAIR ? wave / EACH : 0, turn = wave - matrix * EACH;
     const PackArgs& P = PAIR && matrix == 1 ? Q.pair.up : Q.P;
-    const uint32_t tb = blockIdx.x / Q.row_blocks;
-    const int64_t row0 = (int64_t)(blockIdx.x - tb * Q.row_blocks) * PF_ROWS, t0 = (int64_t)tb * (NTF * 32);
+    const uint32_t block = Q.first + blockIdx.x, tb = block / Q.row_blocks;
+    const int64_t row0 = (int64_t)(block - tb * Q.row_blocks) * PF_ROWS, t0 = (int64_t)tb * (NTF * 32);
     const int64_t rb = row0 / P.R_u, lrow0 = row0 - rb * P.R_u;
     const int32_t rows_left = P.R_u - lrow0 < PF_ROWS ? (int32_t)(P.R_u - lrow0) : PF_ROWS;
     const int32_t lr = sub < rows_left ? sub : rows_left - 1;
@@ -301,22 +302,20 @@ int launch_few(FewArgs Q, float* h, hipStream_t st) {
     const int64_t wgs = (int64_t)Q.row_blocks * tokens_in(Q.T, Q.fragments == 1 ? 32 : 64);
     const int64_t shrinks = h != nullptr ? shrink_token_workgroups(Q.T, Q.A.max_rank) : 0;
     const int64_t ahead = shrinks + (laid ? tokens_in((int64_t)Q.n_kb * Q.fragments, 4) : 0);
-    if (!fits_launch(wgs, 1024) || !fits_launch(ahead, 256)) return WINDQ_ESHAPE;
+    if (!fits_launch(ahead, 256)) return WINDQ_ESHAPE;
     if (ahead > 0) {
         few_prepare_kernel<S><<<dim3((uint32_t)ahead), dim3(256), 0, st>>>(Q, shrinks, h);
         if (hipGetLastError() != hipSuccess) return WINDQ_EHIP;
     }
-    const dim3 g((uint32_t)wgs);
-    if constexpr (!PAIR) {                                  // a pair's few tokens are pair_few_kernel's
-        if (!laid) {
-            project_few_kernel<S, 1, 16, false><<<g, dim3(1024), 0, st>>>(Q);
-            return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
+    return launch_pieces(wgs, 1024, [&](int64_t first, dim3 g) {
+        Q.first = (uint32_t)first;
+        if constexpr (!PAIR) {                              // a pair's few tokens are pair_few_kernel's
+            if (!laid) return project_few_kernel<S, 1, 16, false><<<g, dim3(1024), 0, st>>>(Q);
         }
-    }
-    // two fragments of a pair by sixteen wavefronts would spill: 11008 x 4096, 48 tokens 140 us, by eight 63
-    if (Q.fragments == 1) project_few_kernel<S, 1, PAIR ? 16 : 8, true, PAIR><<<g, dim3(PAIR ? 1024 : 512), 0, st>>>(Q);
-    else project_few_kernel<S, 2, 8, true, PAIR><<<g, dim3(512), 0, st>>>(Q);
-    return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
+        // two fragments of a pair by sixteen wavefronts would spill: 11008 x 4096, 48 tokens 140 us, by eight 63
+        if (Q.fragments == 1) project_few_kernel<S, 1, PAIR ? 16 : 8, true, PAIR><<<g, dim3(PAIR ? 1024 : 512), 0, st>>>(Q);
+        else project_few_kernel<S, 2, 8, true, PAIR><<<g, dim3(512), 0, st>>>(Q);
+    });
 }
 
 #endif  // __HIPCC__

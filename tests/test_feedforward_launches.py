@@ -45,3 +45,29 @@ def test_the_ways_back_take_the_routes_they_name(recorder):
     for kernels, other, shape, masked in R.BACK:
         status, names = gated_grad(recorder, shape, masked)
         assert status == 0 and all(k in names for k in kernels) and other not in names, (kernels, shape, names)
+
+
+def test_few_tokens_of_as_many_rows_as_the_header_allows(recorder):
+    """A launch holds fewer than 2^32 threads: more rows go in several, none are refused."""
+    for dtype in (binding.WINDQ_BF16, binding.WINDQ_F32):
+        for shape in ((1 << 27, 64, 64, 0, 1), ((1 << 27) + 16, 64, 64, 0, 15), ((1 << 31) - 512, 64, 64, 0, 1), ((1 << 26) + 64, 64, 64, 0, 31), ((1 << 25) - 512, 64, 64, 32, 63)):
+            status, _ = gated(recorder, shape, dtype, codes_bytes=1 << 40)
+            launches = recorder.launches()
+            assert status == 0 and all(0 < x.grid * x.block < 1 << 32 for x in launches), (dtype, shape, status, launches)
+            rows, T = shape[0], shape[4]
+            few = [x.grid for x in launches if "pair_few_kernel" in x.name]
+            if few:
+                assert sum(few) == -(-rows // 16) * -(-T // 16), (dtype, shape)
+            mine = [x.grid for x in launches if "project_few_kernel" in x.name]
+            if mine:
+                assert sum(mine) == -(-rows // 32) * -(-T // (32 if T <= 32 else 64)), (dtype, shape)
+            assert few or mine or "project_kernel" in launches[-1].name
+
+
+def test_windq_project_of_as_many_rows_as_the_header_allows(recorder):
+    for T, rows in ((1, 1 << 27), (8, (1 << 27) + 32), (1, (1 << 31) - 512), (31, (1 << 26) + 64), (63, (1 << 25) - 512)):
+        status, _, _ = recorder.product(False, T, rows, 64, 64)
+        launches = recorder.launches()
+        assert status == 0 and all(0 < x.grid * x.block < 1 << 32 for x in launches), (T, rows, status)
+        mine = [x.grid for x in launches if "project_few_kernel" in x.name]
+        assert sum(mine) == -(-rows // 32) * -(-T // (32 if T <= 32 else 64)), (T, rows)

@@ -158,3 +158,36 @@ def test_there_and_back(windq, shape, word):
     want, off = backward(cs, dh, save[0], save[1], word, BF)
     for a, b, o in zip(windq.windq_gated_grad(*p, dh, save[0], save[1], word), want, off):
         close(a, b, o, BF)
+
+
+@pytest.mark.parametrize("T", [1, 15])                      # 2^31 - 1 tokens x rows at most
+def test_more_rows_than_one_launch_holds(windq, T):
+    """Rows on both sides of where one launch ends and the next begins, the last ones, and all of them written: windq_gated and windq_project of few tokens."""
+    rows, cols = (1 << 27) + 48, 64
+    g = torch.Generator(device=DEV).manual_seed(T)
+    W = torch.empty(rows, cols, dtype=BF, device=DEV)       # no unit stays as it is: never read
+    action = torch.full((1,), 6, dtype=torch.uint8, device=DEV)
+    off = torch.tensor([0, rows * 8], dtype=torch.int64, device=DEV)
+    plans, parts = [], []
+    for _ in range(2):
+        codes = torch.randint(0, 256, (rows * 8,), generator=g, device=DEV, dtype=torch.uint8)
+        scale = torch.rand(rows, generator=g, device=DEV) + 0.5
+        plans.append(windq.Packed(W, cols, 0, action, off, codes, scale, torch.zeros(rows, device=DEV)))
+        parts.append((codes.view(rows, 8), scale))
+    x = tokens(T, cols, BF, 3)
+    h = torch.full((T, rows), float("nan"), dtype=BF, device=DEV)
+    windq.windq_gated(*plans, x, out=h)
+    y = windq.windq_project(plans[0], x, out=torch.full((T, rows), float("nan"), dtype=BF, device=DEV))
+    assert all(torch.isfinite(t[:, r:r + (1 << 24)]).all() for t in (h, y) for r in range(0, rows, 1 << 24))
+    edges = [0xffffffff // threads * piece for threads in (512, 1024) for piece in (16, 32)]
+    for at in [0, rows - 4096] + [e - 2048 for e in edges if e < rows]:
+        here = slice(at, at + 4096)
+        ref, off64 = [], []
+        for codes, scale in parts:
+            bits = (codes[here, :, None] >> torch.arange(8, device=DEV)) & 1
+            w = ((2.0 * bits.reshape(-1, cols) - 1) * scale[here, None]).double().cpu().numpy()
+            ref.append(x.double().cpu().numpy() @ w.T)
+            off64.append(16 * 2.0 ** -24 * (abs(x.double().cpu().numpy()) @ abs(w).T))
+        close(y[:, here], ref[0], off64[0], BF)
+        a = E.act("silu", ref[0])
+        close(h[:, here], a * ref[1], 1.13 * abs(ref[1]) * off64[0] + abs(a) * off64[1] + 1.13 * off64[0] * off64[1] + 16 * 2.0 ** -24 * abs(ref[1]) * (1 + abs(ref[0])), BF)
