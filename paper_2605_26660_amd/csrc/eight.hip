@@ -5,8 +5,6 @@
 
 namespace windq {
 
-int check_tokens(const windq_mat* M, int64_t width, bool vector);
-
 // ------------------------------------------------------------------------------------------------ tokens
 // A workgroup a token, its octets (of the padded width) to neighbouring threads, read once where a thread has PER of them at most: they stay in registers
 // between the pass for the largest magnitude and the one that rounds.  Magnitudes are compared as bits: a NaN's are above an infinity's, and those above
@@ -291,7 +289,7 @@ inline bool eight_few(int64_t workgroups, int64_t tiles, bool pair) {
 // add up through LDS.  Bound by latency: everything that a k-block needs is asked for at once, and the next one's fields before this one is multiplied.
 // Tokens are the M side of the matrix instructions and rows the N side, so that a lane has one row, with one alpha and one beta; beta times the tokens' sums
 // is an instruction of its own, whose halves have the sums of a step's halves.  Tokens come through a place of the wavefront's own in LDS, whole lines
-// of eight of them at a time: 16 bytes of each of 32 tokens in one load are 32 lines (48 tokens through 11008 x 4096 22 us, 14 so).
+// of eight of them at a time: 16 bytes of each of 32 tokens in one load are 32 lines (48 tokens through 11008 x 4096 22 us, 17 so; a pair of them at 16 tokens 19 and 14).
 template <typename YT, int S, int N, int WAVES, bool PAIR>
 __global__ __launch_bounds__(WAVES * 64) void eight_kernel(const EightArgs Q, const int64_t first) {
     constexpr int EACH = PAIR ? WAVES / 2 : WAVES;
@@ -420,10 +418,10 @@ int launch_eight(const EightArgs& Q, hipStream_t st) {
             if (Q.NB > 256) eight_kernel<YT, S, 1, 8, PAIR><<<g, dim3(512), 0, st>>>(Q, first);
             else eight_kernel<YT, S, 1, 16, PAIR><<<g, dim3(1024), 0, st>>>(Q, first);
         });
-    constexpr int WR = 4, WT = 1;
-    const int64_t row_tiles = tokens_in(Q.NB, PAIR ? WR : 2 * WR), tiles = row_tiles * tokens_in(Q.T, WT * 64), few = Q.NB * tokens_in(Q.T, 64);
-    if (!eight_few(few, tiles, PAIR) && fits_launch(tiles, WR * WT * 64)) {
-        eight_tiles_kernel<YT, S, WR, WT, PAIR><<<dim3((uint32_t)tiles), dim3(WR * WT * 64), 0, st>>>(Q, (uint32_t)row_tiles);
+    constexpr int WR = 4;
+    const int64_t row_tiles = tokens_in(Q.NB, PAIR ? WR : 2 * WR), tiles = row_tiles * tokens_in(Q.T, 64), few = Q.NB * tokens_in(Q.T, 64);
+    if (!eight_few(few, tiles, PAIR) && fits_launch(tiles, WR * 64)) {
+        eight_tiles_kernel<YT, S, WR, PAIR><<<dim3((uint32_t)tiles), dim3(WR * 64), 0, st>>>(Q, (uint32_t)row_tiles);
         return hipGetLastError() == hipSuccess ? WINDQ_OK : WINDQ_EHIP;
     }
     constexpr int WAVES = 8;
@@ -480,7 +478,6 @@ static int product(const windq_serving* first, const windq_serving* second, cons
     Q.T = X->tokens;
     Q.Y = Y;
     Q.ldy = ld_y;
-    Q.rows = E.rows;
     Q.R_u = E.R_u;
     Q.RB = E.RB;
     Q.NB = E.NB;

@@ -60,7 +60,7 @@ GatedWs gated_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32_t G
 struct HalvesArgs {
     PackArgs P[2];
     const uint16_t* X;
-    int64_t ldx, T, K;
+    int64_t ldx, K;
     uint16_t* x;               // [T][K]
     float* by_token;           // powers, and losses in them (with_loss)
     uint16_t* w;               // [rows of both in turn, 32 and 32][K]
@@ -281,7 +281,7 @@ __global__ __launch_bounds__(256) void gated_halves_kernel(const HalvesArgs Q, c
 
 int launch_gated_halves(const ProjectArgs& Q, char* ws, const GatedWs& at, hipStream_t st) {
     const int64_t K = gemm_k(Q.P.cols), rows = gated_rows(Q.P.rows), tall = tokens_in(Q.T, GM_N);
-    const HalvesArgs H = {{Q.P, Q.pair.up}, Q.X, Q.ldx, Q.T, K, reinterpret_cast<uint16_t*>(ws + at.x), reinterpret_cast<float*>(ws + at.by_token),
+    const HalvesArgs H = {{Q.P, Q.pair.up}, Q.X, Q.ldx, K, reinterpret_cast<uint16_t*>(ws + at.x), reinterpret_cast<float*>(ws + at.by_token),
                           reinterpret_cast<uint16_t*>(ws + at.w), reinterpret_cast<float*>(ws + at.by_row)};
     const bool mask = Q.P.mask != nullptr || Q.pair.up.mask != nullptr;
     const bool known = (Q.P.R_u == Q.P.rows || Q.P.R_u % HALVES_ROWS == 0) && Q.P.n_chunks <= HALVES_UNITS;
@@ -804,12 +804,6 @@ int gated_grad_all(SlopeArgs& S, void* dX, int64_t ld_dx, char* ws, const GatedG
         gated_slopes_kernel<XT><<<g, dim3(256), 0, st>>>(S, first);
     });
     if (status != WINDQ_OK || dX == nullptr) return status;
-    DxArgs Q = {};
-    Q.P = P;
-    Q.packed = true;
-    Q.T = T;
-    Q.dX = dX;
-    Q.ldx = ld_dx;
     if constexpr (bf) {
         const int32_t K2 = (int32_t)(2 * at.K);
         const GatedTurnArgs R = {{S.P[0], S.P[1]}, (int32_t)at.K, reinterpret_cast<uint16_t*>(ws + at.wt), ((cols + 63) / 64) * ((at.K + 255) / 256), S.range, S.strips,
@@ -843,6 +837,12 @@ int gated_grad_all(SlopeArgs& S, void* dX, int64_t ld_dx, char* ws, const GatedG
         const GatedJoinArgs J = {M, splits};
         return launch_pieces(tokens_in(T * (cols / 8), 256), 256, [&](int64_t first, dim3 g) { gated_join_kernel<<<g, dim3(256), 0, st>>>(J, first); });
     } else {
+        DxArgs Q = {};
+        Q.P = P;
+        Q.packed = true;
+        Q.T = T;
+        Q.dX = dX;
+        Q.ldx = ld_dx;
         Q.dY = S.to;
         Q.ldy = at.K;
         Q.up = S.P[1];

@@ -6,8 +6,6 @@
 
 namespace windq {
 
-int check_tokens(const windq_mat* M, int64_t width, bool vector);
-
 // ------------------------------------------------------------------------------------------------ layouts
 // out [n][C][ldo] = in [n][R][C] transposed, rows padded with zeros up to ldo.
 template <typename T>
@@ -491,7 +489,7 @@ size_t grad_ws_bytes(int32_t dtype, int64_t T, int64_t rows, int64_t cols, int32
         if (launched_ != WINDQ_OK) return launched_;                                                                                             \
     } while (0)
 
-int launch_dx_join(const DxArgs& Q, hipStream_t st) {
+static int launch_dx_join(const DxArgs& Q, hipStream_t st) {
     WINDQ_LAUNCH(tokens_in(Q.T * (Q.P.cols / 8), 256), 256, dx_join_kernel, Q);
     return WINDQ_OK;
 }

@@ -24,7 +24,6 @@ struct DxArgs {
     const void* dY_up;         // or null
 };
 
-int launch_dx_join(const DxArgs& Q, hipStream_t st);           // bfloat16: the parts added up, and the adapters'
 int launch_dx_f32(DxArgs Q, hipStream_t st);
 
 #ifdef __HIPCC__

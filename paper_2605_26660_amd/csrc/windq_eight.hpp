@@ -98,7 +98,7 @@ struct EightArgs {
     int64_t T;
     void* Y;
     int64_t ldy;
-    int64_t rows, R_u, RB, NB, width, sums_ld, affine;      // affine: where alpha and beta begin
+    int64_t R_u, RB, NB, width, sums_ld, affine;            // affine: where alpha and beta begin
     int32_t n_kb, act, w_f32;
 };
 

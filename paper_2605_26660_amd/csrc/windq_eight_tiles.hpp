@@ -1,4 +1,4 @@
-// Products of many 8-bit tokens with a plan laid out for them: tiles of 64 WR rows x 64 WT tokens (of a pair: 32 WR rows of both).
+// Products of many 8-bit tokens with a plan laid out for them: tiles of 64 WR rows x 64 tokens (of a pair: 32 WR rows of both).
 #pragma once
 
 #include "windq_eight.hpp"
@@ -12,20 +12,19 @@ struct Const {
     static constexpr int value = V;
 };
 
-template <typename YT, int S, int WR, int WT, bool PAIR>
-__global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void eight_tiles_kernel(const EightArgs Q, const uint32_t row_tiles) {
-    constexpr int TOKENS = WT * 64, LOADS = 8 / WR;
+template <typename YT, int S, int WR, bool PAIR>
+__global__ __launch_bounds__(WR * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void eight_tiles_kernel(const EightArgs Q, const uint32_t row_tiles) {
+    constexpr int TOKENS = 64, LOADS = 8 / WR;
     constexpr int SUMS = 64;                                // k-blocks whose words are in registers, a lane each, and whose tokens' sums are in LDS
     __shared__ uint4 xt[3][2][TOKENS * 8];
     __shared__ int32_t st[TOKENS * (SUMS + 1)];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, sub = lane & 31, hh = lane >> 5;
-    const int wr = wave % WR, wt = wave / WR;
     const bool w_f32 = Q.w_f32 != 0;
     // Consecutive workgroups land on the eight XCDs in turn; each XCD gets a run of tiles that share tokens.
     const uint32_t n_tiles = gridDim.x, per = n_tiles >> 3;
     const uint32_t tile = blockIdx.x < per * 8 ? (blockIdx.x & 7) * per + (blockIdx.x >> 3) : blockIdx.x;
     const uint32_t tb = tile / row_tiles;
-    const int64_t b0 = (int64_t)(tile - tb * row_tiles) * WR + wr, t0 = (int64_t)tb * TOKENS;
+    const int64_t b0 = (int64_t)(tile - tb * row_tiles) * WR + wave, t0 = (int64_t)tb * TOKENS;
     const int32_t n_kb = Q.n_kb;
 
     // a wavefront's two row blocks: neighbours, or the same of the gate and of the up; past the last one: computed for nothing, stored by nobody
@@ -47,7 +46,7 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
     const int8_t* xsrc[LOADS];
 #pragma unroll
     for (int k = 0; k < LOADS; ++k) {
-        const int n = (k * WR * WT + wave) * 8 + (lane >> 3), slot = (lane & 7) ^ ((n >> 1) & 7);
+        const int n = (k * WR + wave) * 8 + (lane >> 3), slot = (lane & 7) ^ ((n >> 1) & 7);
         const int64_t t = t0 + n < Q.T ? t0 + n : Q.T - 1;
         xsrc[k] = Q.codes + t * Q.width + (slot < 2 * S ? slot : 0) * 16;
     }
@@ -58,13 +57,13 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
             const int32_t kb = 2 * pair + q < n_kb ? 2 * pair + q : n_kb - 1;
 #pragma unroll
             for (int k = 0; k < LOADS; ++k)
-                lds_load16(lds_xt + ((stage * 2 + q) * (TOKENS * 8) + (k * WR * WT + wave) * 64) * 16, xsrc[k] + (int64_t)kb * (32 * S));
+                lds_load16(lds_xt + ((stage * 2 + q) * (TOKENS * 8) + (k * WR + wave) * 64) * 16, xsrc[k] + (int64_t)kb * (32 * S));
         }
     };
     const uint32_t lds_st = lds_address(st);
     auto load_sums = [&](int32_t kb) {
 #pragma unroll 1
-        for (int n = wave; n < TOKENS; n += WR * WT)
+        for (int n = wave; n < TOKENS; n += WR)
             lds_load4(lds_st + n * (SUMS + 1) * 4, Q.sums + (t0 + n < Q.T ? t0 + n : Q.T - 1) * Q.sums_ld + (kb + lane < n_kb ? kb + lane : n_kb - 1));
     };
 
@@ -89,7 +88,7 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
         for (int f = 0; f < 2; ++f) beta[f] = affine[f][(int64_t)kb * 64 + 32];
     };
-    const char* const xb = reinterpret_cast<const char*>(xt) + (wt * 64 + sub) * 128;
+    const char* const xb = reinterpret_cast<const char*>(xt) + sub * 128;
     uint4 x[S][2];
     auto read_x = [&](int s, int half) {
 #pragma unroll
@@ -133,60 +132,60 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
         for (int f = 0; f < 2; ++f) pair_beta[f] = 2 * pair + hh < n_kb ? beta[f] : 0.0f;
 #pragma unroll
-        for (int n = 0; n < 2; ++n) pair_sum[n] = (float)st[(wt * 64 + n * 32 + sub) * (SUMS + 1) + ((2 * pair + hh) & (SUMS - 1))];
+        for (int n = 0; n < 2; ++n) pair_sum[n] = (float)st[(n * 32 + sub) * (SUMS + 1) + ((2 * pair + hh) & (SUMS - 1))];
         load_beta(pair + 1);
 
         auto k_block = [&](auto HALF) {
-        constexpr int half = decltype(HALF)::value;
-        const int32_t then = 2 * pair + half + 1;
-        if (half == 1 && (then & (SUMS - 1)) == 0) {
+            constexpr int half = decltype(HALF)::value;
+            const int32_t then = 2 * pair + half + 1;
+            if (half == 1 && (then & (SUMS - 1)) == 0) {
 #pragma unroll
-            for (int f = 0; f < 2; ++f) word[f] = word_next[f];
-        }
+                for (int f = 0; f < 2; ++f) word[f] = word_next[f];
+            }
 #pragma unroll
-        for (int f = 0; f < 2; ++f) next[f] = block_of(f, word[f], then);
-        auto phase = [&](auto F) {
-            constexpr int f = decltype(F)::value, other = f ^ 1;
-            const float fold = f == 0 ? behind : alpha[0];
-            auto add_up = [&](int from, int count) {        // of the other row block's results
+            for (int f = 0; f < 2; ++f) next[f] = block_of(f, word[f], then);
+            auto phase = [&](auto F) {
+                constexpr int f = decltype(F)::value, other = f ^ 1;
+                const float fold = f == 0 ? behind : alpha[0];
+                auto add_up = [&](int from, int count) {        // of the other row block's results
 #pragma unroll
-                for (int k = from; k < from + count; ++k) {
-                    const int n = k >> 4, i = k & 15;
-                    tot[other][n][i] = fmaf(fold, (float)acc[other][n][i], tot[other][n][i]);
+                    for (int k = from; k < from + count; ++k) {
+                        const int n = k >> 4, i = k & 15;
+                        tot[other][n][i] = fmaf(fold, (float)acc[other][n][i], tot[other][n][i]);
+                    }
+                };
+                // Only the operands differ by kind; where there are no codes they are zeros.
+                const int kind = now[f].kind;
+                i32x4 w[S];
+                raw[f].operands(kind, w);
+                __builtin_amdgcn_sched_barrier(0);
+                raw[f].load(next[f].kind, next[f].fields, lane);
+                alpha_next[f] = affine[f][(int64_t)(then < n_kb ? then : n_kb - 1) * 64];
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int s = 0; s < S; ++s) {
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        acc[f][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(as_i32x4(x[s][n]), w[s], s == 0 ? i32x16{} : acc[f][n], 0, 0, 0);
+                        add_up((2 * s + n) * 16 / S, (2 * s + n + 1) * 16 / S - (2 * s + n) * 16 / S);
+                        if (f == 1 && n == 1) read_x(s, half == 0 ? 2 * stage + 1 : 2 * stage1);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+                asm volatile("" : "+v"(tot[other][0]), "+v"(tot[other][1]));       // here, between the matrix instructions, and not in a later block
+                if (half == 1) {                            // beta times the tokens' sums, two k-blocks an instruction
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) tot[f][n] = __builtin_amdgcn_mfma_f32_32x32x2f32(pair_sum[n], pair_beta[f], tot[f][n], 0, 0, 0);
                 }
             };
-            // Only the operands differ by kind; where there are no codes they are zeros.
-            const int kind = now[f].kind;
-            i32x4 w[S];
-            raw[f].operands(kind, w);
-            __builtin_amdgcn_sched_barrier(0);
-            raw[f].load(next[f].kind, next[f].fields, lane);
-            alpha_next[f] = affine[f][(int64_t)(then < n_kb ? then : n_kb - 1) * 64];
-            __builtin_amdgcn_sched_barrier(0);
+            phase(Const<0>());
+            phase(Const<1>());
+            behind = alpha[1];
 #pragma unroll
-            for (int s = 0; s < S; ++s) {
-#pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    acc[f][n] = __builtin_amdgcn_mfma_i32_32x32x32_i8(as_i32x4(x[s][n]), w[s], s == 0 ? i32x16{} : acc[f][n], 0, 0, 0);
-                    add_up((2 * s + n) * 16 / S, (2 * s + n + 1) * 16 / S - (2 * s + n) * 16 / S);
-                    if (f == 1 && n == 1) read_x(s, half == 0 ? 2 * stage + 1 : 2 * stage1);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+            for (int f = 0; f < 2; ++f) {
+                now[f] = next[f];
+                alpha[f] = alpha_next[f];
             }
-            asm volatile("" : "+v"(tot[other][0]), "+v"(tot[other][1]));       // here, between the matrix instructions, and not in a later block
-                            if (half == 1) {                                // beta times the tokens' sums, two k-blocks an instruction
-#pragma unroll
-                for (int n = 0; n < 2; ++n) tot[f][n] = __builtin_amdgcn_mfma_f32_32x32x2f32(pair_sum[n], pair_beta[f], tot[f][n], 0, 0, 0);
-            }
-        };
-        phase(Const<0>());
-        phase(Const<1>());
-        behind = alpha[1];
-#pragma unroll
-        for (int f = 0; f < 2; ++f) {
-            now[f] = next[f];
-            alpha[f] = alpha_next[f];
-        }
         };
         k_block(Const<0>());
         k_block(Const<1>());
@@ -213,7 +212,7 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
             uint4 v[2][S];
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
-                const int64_t t = t0 + wt * 64 + n * 32 + sub;
+                const int64_t t = t0 + n * 32 + sub;
                 const int8_t* const from = Q.codes + (t < Q.T ? t : Q.T - 1) * Q.width + (int64_t)(kb0 + at) * (32 * S) + hh * 16;
 #pragma unroll
                 for (int s = 0; s < S; ++s) v[n][s] = *reinterpret_cast<const uint4*>(from + s * 32);
@@ -250,7 +249,7 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
     for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const int64_t t = t0 + wt * 64 + n * 32 + (i >> 2) * 8 + hh * 4 + (i & 3);
+            const int64_t t = t0 + n * 32 + (i >> 2) * 8 + hh * 4 + (i & 3);
             scale[n][i] = Q.scale[t < Q.T ? t : Q.T - 1];
         }
 #pragma unroll
@@ -268,7 +267,7 @@ __global__ __launch_bounds__(WR* WT * 64) __attribute__((amdgpu_waves_per_eu(2, 
     for (int f = 0; f < (PAIR ? 1 : 2); ++f) {
         const int64_t lrow = in[f] * EIGHT_ROWS + sub;
         if (b[f] >= Q.NB || lrow >= Q.R_u) continue;
-        const int64_t t1 = t0 + wt * 64 + hh * 4;
+        const int64_t t1 = t0 + hh * 4;
         YT* __restrict__ const y = static_cast<YT*>(Q.Y) + t1 * Q.ldy + rb[f] * Q.R_u + lrow;
         if (t0 + TOKENS <= Q.T) {
 #pragma unroll

@@ -42,6 +42,7 @@ struct AdapterArgs {
 };
 
 int check_packed(const windq_packed* P, PackArgs* A);
+int check_tokens(const windq_mat* M, int64_t width, bool vector);
 int check_adapters(const windq_adapters* ad, const int32_t* adapter_of, int32_t dtype, AdapterArgs* A);
 
 #ifdef __HIPCC__

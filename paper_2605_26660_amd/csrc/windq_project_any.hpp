@@ -29,7 +29,6 @@ struct ProjectArgs {
     PairArgs pair;
 };
 
-int check_tokens(const windq_mat* M, int64_t width, bool vector);
 int launch_planes(const float* X, int64_t ldx, int64_t T, int32_t cols, uint16_t* planes, hipStream_t st);
 
 #ifdef __HIPCC__
