@@ -451,6 +451,7 @@ struct SlopeArgs {
     int32_t strips;
     int64_t ranges;            // workgroups for them
     int32_t* lost_octet;       // counted by the next launch, zeros so far
+    uint32_t* there_octet;     // as well
     int64_t octets;
 };
 
@@ -621,7 +622,8 @@ __device__ __forceinline__ void slopes(const SlopeArgs& Q, int64_t t) {
     }
 }
 
-// The largest finite magnitude that a weight of RANGE_ROWS rows of a chunk can have, and the smallest that half precision may take something from (group_range).
+// The largest finite magnitude that a weight of RANGE_ROWS rows of a chunk can have, and the smallest that half precision may take
+// something from (group_range); the largest less than 0: there are codes.
 template <int THREADS>
 __device__ __forceinline__ void range_of(const SlopeArgs& Q, int64_t block) {
     constexpr int WAVES = THREADS / 64;
@@ -630,23 +632,25 @@ __device__ __forceinline__ void range_of(const SlopeArgs& Q, int64_t block) {
     const PackArgs& P = Q.P[m];
     const int64_t rest = block - (int64_t)m * Q.strips * P.n_chunks, j = rest / Q.strips, strip = rest - j * Q.strips;
     float most_here = 0.0f, least_here = 3.40282347e38f;
+    bool coded = false;
     for (int k = threadIdx.x; k < RANGE_ROWS; k += THREADS) {
         const int64_t row = strip * RANGE_ROWS + k;
         if (row >= P.rows) break;
-        group_range(P, row, j, most_here, least_here);
+        group_range(P, row, j, most_here, least_here, coded);
     }
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) {
         most_here = fmaxf(most_here, __shfl_xor(most_here, d, 64));
         least_here = fminf(least_here, __shfl_xor(least_here, d, 64));
     }
-    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = most_here, least[threadIdx.x >> 6] = least_here;
+    coded = __any(coded);
+    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = coded ? -most_here : most_here, least[threadIdx.x >> 6] = least_here;
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < WAVES; ++k) most_here = fmaxf(most_here, most[k]), least_here = fminf(least_here, least[k]);
-    if (threadIdx.x == 0) Q.range[(j * 2 + m) * Q.strips + strip] = make_float2(most_here, least_here);
+    for (int k = 0; k < WAVES; ++k) most_here = fmaxf(most_here, fabsf(most[k])), least_here = fminf(least_here, least[k]), coded |= most[k] < 0.0f;
+    if (threadIdx.x == 0) Q.range[(j * 2 + m) * Q.strips + strip] = make_float2(coded ? -most_here : most_here, least_here);
     if (block == 0)
-        for (int64_t k = threadIdx.x; k < Q.octets; k += THREADS) Q.lost_octet[k] = 0;
+        for (int64_t k = threadIdx.x; k < Q.octets; k += THREADS) Q.lost_octet[k] = 0, Q.there_octet[k] = 0;
 }
 
 template <typename XT, int PER = 0, int THREADS = 256>
@@ -665,6 +669,7 @@ struct GatedTurnArgs {
     int32_t strips;
     float* by_octet;
     int32_t* lost_octet;
+    uint32_t* there_octet;
 };
 
 template <bool PLAIN>
@@ -676,22 +681,31 @@ __global__ __launch_bounds__(256) void gated_turn_kernel(const GatedTurnArgs Q, 
     const int64_t cb = block / row_blocks, col = cb * 64 + (threadIdx.x >> 5) * 8;
     const PackArgs& P = Q.P[m];
     float most = 0.0f, least = 3.40282347e38f;
+    bool coded = false;
     if (col < P.cols) {
         const float2* const range = Q.range + col / P.G * 2 * Q.strips;
-        for (int32_t k = threadIdx.x & 31; k < 2 * Q.strips; k += 32) most = fmaxf(most, range[k].x), least = fminf(least, range[k].y);
+        for (int32_t k = threadIdx.x & 31; k < 2 * Q.strips; k += 32) {
+            const float2 r = range[k];
+            most = fmaxf(most, fabsf(r.x)), least = fminf(least, r.y), coded |= r.x < 0.0f;
+        }
     }
+    coded = PLAIN && (uint32_t)(__ballot(coded) >> (threadIdx.x & 32)) != 0;
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) {
         most = fmaxf(most, __shfl_xor(most, d, 32));
         least = fminf(least, __shfl_xor(least, d, 32));
     }
     const float by = power_below(most);
-    if (id - cb * row_blocks == 0 && (threadIdx.x & 31) == 0 && col < P.cols) Q.by_octet[col >> 3] = most > 0.0f ? 1.0f / by : power_of_nothing();
+    if (id - cb * row_blocks == 0 && (threadIdx.x & 31) == 0 && col < P.cols) Q.by_octet[col >> 3] = most > 0.0f ? with_codes(1.0f / by, coded) : power_of_nothing();
     if (least * by < HALF_GROUP && col < P.cols) {          // rare
         const int32_t lost = rows_lost(P, (block - cb * row_blocks) * 256 + (threadIdx.x & 31) * 8, col, by);
         if (lost != 0) atomicAdd(Q.lost_octet + (col >> 3), lost);
     }
-    turn<_Float16, PLAIN>(P, Q.K, 2 * (int64_t)Q.K, by, Q.wt + (int64_t)m * Q.K, block);
+    uint32_t there = turn<_Float16, PLAIN>(P, Q.K, 2 * (int64_t)Q.K, by, Q.wt + (int64_t)m * Q.K, block);
+    if (PLAIN && !__any(there != 0)) return;                // columns of a chunk with codes are all there
+#pragma unroll 1
+    for (int d = 16; d >= 1; d >>= 1) there |= (uint32_t)__shfl_xor((int)there, d, 32);
+    if ((threadIdx.x & 31) == 0 && there != 0) atomicOr(Q.there_octet + (col >> 3), there);
 }
 
 // The parts of dX added up, a thread per token and octet of columns; columns that lie too low are formed again.
@@ -717,9 +731,10 @@ __global__ __launch_bounds__(256) void gated_join_kernel(const GatedJoinArgs J, 
         for (int m = 0; m < 8; ++m) v[m] += p[m];
     }
     const float low = ldexpf(lost_below(by_token, by_octet, lost), exponent_of(by_token) + exponent_of(by_octet));
+    const uint32_t there = has_codes(by_octet) || lost != 0 ? 0xffu : Q.there_octet[o];
     bool bad = false;
 #pragma unroll
-    for (int m = 0; m < 8; ++m) bad |= fabsf(v[m]) < low;
+    for (int m = 0; m < 8; ++m) bad |= fabsf(v[m]) < low && (there >> m & 1u) != 0u;
 #pragma unroll 1
     for (uint64_t left = __ballot(bad && in); left != 0; left &= left - 1) {
         const int which = __builtin_ctzll(left);
@@ -728,7 +743,7 @@ __global__ __launch_bounds__(256) void gated_join_kernel(const GatedJoinArgs J, 
         dx_again(Q.gate, Q.pair.up, Q.pair.act, Q.again, token, (id - token * octets) * 8, lane, sum);
 #pragma unroll
         for (int m = 0; m < 8; ++m)
-            if (lane == which && fabsf(v[m]) < low) v[m] = (float)sum[m];
+            if (lane == which && fabsf(v[m]) < low && (there >> m & 1u) != 0u) v[m] = (float)sum[m];
     }
     if (!in) return;
     uint16_t* __restrict__ const out = Q.dX + t * Q.ldx + c;
@@ -744,7 +759,7 @@ __global__ __launch_bounds__(256) void gated_join_kernel(const GatedJoinArgs J, 
 }
 
 struct GatedGradWs {
-    size_t to, wt, gm, by_token, by_octet, lost_octet, range, dxf, total;
+    size_t to, wt, gm, by_token, by_octet, lost_octet, there_octet, range, dxf, total;
     int64_t K;
 };
 
@@ -764,6 +779,7 @@ GatedGradWs gated_grad_ws(int32_t dtype, int64_t T, int64_t rows, int64_t cols, 
     w.by_token = take(bf ? (size_t)T * 4 : 0);
     w.by_octet = take(bf ? (size_t)(cols / 8 + 1) * 4 : 0);
     w.lost_octet = take(bf ? (size_t)(cols / 8 + 1) * 4 : 0);
+    w.there_octet = take(bf ? (size_t)(cols / 8 + 1) * 4 : 0);
     w.range = take(bf ? (size_t)(cols / G + 1) * 2 * (size_t)tokens_in(rows, RANGE_ROWS) * 8 : 0);
     w.dxf = take(bf ? 0 : DXF_BYTES);
     w.total = at == 0 ? 256 : at;
@@ -785,6 +801,7 @@ int gated_grad_all(SlopeArgs& S, void* dX, int64_t ld_dx, char* ws, const GatedG
             S.by_token = reinterpret_cast<float*>(ws + at.by_token);
             S.range = reinterpret_cast<float2*>(ws + at.range);
             S.lost_octet = reinterpret_cast<int32_t*>(ws + at.lost_octet);
+            S.there_octet = reinterpret_cast<uint32_t*>(ws + at.there_octet);
             S.octets = cols / 8;
             S.strips = (int32_t)tokens_in(P.rows, RANGE_ROWS);
             S.ranges = 2 * (int64_t)S.strips * P.n_chunks;
@@ -807,7 +824,7 @@ int gated_grad_all(SlopeArgs& S, void* dX, int64_t ld_dx, char* ws, const GatedG
     if constexpr (bf) {
         const int32_t K2 = (int32_t)(2 * at.K);
         const GatedTurnArgs R = {{S.P[0], S.P[1]}, (int32_t)at.K, reinterpret_cast<uint16_t*>(ws + at.wt), ((cols + 63) / 64) * ((at.K + 255) / 256), S.range, S.strips,
-                                 reinterpret_cast<float*>(ws + at.by_octet), S.lost_octet};
+                                 reinterpret_cast<float*>(ws + at.by_octet), S.lost_octet, S.there_octet};
         const bool plain = P.mask == nullptr && S.P[1].mask == nullptr && P.rows % 8 == 0 && (P.R_u == P.rows || P.R_u % 8 == 0);
         status = launch_pieces(2 * R.turns, 256, [&](int64_t first, dim3 g) {
             if (plain) gated_turn_kernel<true><<<g, dim3(256), 0, st>>>(R, first);
@@ -821,6 +838,7 @@ int gated_grad_all(SlopeArgs& S, void* dX, int64_t ld_dx, char* ws, const GatedG
         M.pair.up = S.P[1];
         M.pair.act = S.act;
         M.lost_octet = S.lost_octet;
+        M.there_octet = S.there_octet;
         M.again = {static_cast<const uint16_t*>(S.dH), static_cast<const uint16_t*>(S.G), static_cast<const uint16_t*>(S.U), S.ld_dh, S.ld_save};
         if (by == 256) {
             dx_gemm_kernel<4, true><<<dim3((uint32_t)tiles), dim3(GM_THREADS), 0, st>>>(M);

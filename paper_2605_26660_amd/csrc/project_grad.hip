@@ -292,7 +292,10 @@ struct PrepareArgs {
 template <typename XT>
 __global__ __launch_bounds__(256) void grad_prepare_kernel(const PrepareArgs<XT> Q, const int64_t first) {
     int64_t block = first + blockIdx.x;
-    if (block < Q.turns) return turn<uint16_t>(Q.P, Q.K, Q.K, 1.0f, Q.wt, block);
+    if (block < Q.turns) {
+        turn<uint16_t>(Q.P, Q.K, Q.K, 1.0f, Q.wt, block);
+        return;
+    }
     block -= Q.turns;
     if (block < Q.bs) return transpose(Q.b, Q.P.rows, Q.A.max_rank, Q.ld, Q.bt, block);
     block -= Q.bs;

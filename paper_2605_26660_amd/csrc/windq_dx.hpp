@@ -158,18 +158,24 @@ __device__ __forceinline__ uint4 half_weights(uint4 f, float s, float b) {
 }
 
 // ROWS rows by eight columns of w_hat times `by`, a power of two, in half precision, within a unit whose treatment and first byte are known; no mask.  Five
-// instructions a weight, where putting on the mask, the power and the centre one by one takes eleven.
+// instructions a weight, where putting on the mask, the power and the centre one by one takes eleven.  Comes back with the columns that have something other than 0 (of codes: with none).
 template <int ROWS>
-__device__ __forceinline__ void half_rows(const PackArgs& P, int64_t r0, int64_t col, int64_t u, int64_t lrow, int o, int a, int64_t base, const uint16_t* __restrict__ trits_of,
-                                          float by, uint4 (&w)[ROWS]) {
+__device__ __forceinline__ uint32_t half_rows(const PackArgs& P, int64_t r0, int64_t col, int64_t u, int64_t lrow, int o, int a, int64_t base, const uint16_t* __restrict__ trits_of,
+                                              float by, uint4 (&w)[ROWS]) {
     if (a == 0) {
+        uint4 all = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
             float v[8];
             skip_row(P, r0 + i, col, v);
             w[i] = make_uint4(half_pair(v[0] * by, v[1] * by), half_pair(v[2] * by, v[3] * by), half_pair(v[4] * by, v[5] * by), half_pair(v[6] * by, v[7] * by));
+            all = make_uint4(all.x | w[i].x, all.y | w[i].y, all.z | w[i].z, all.w | w[i].w);
         }
-        return;
+        const uint32_t pairs[4] = {all.x, all.y, all.z, all.w};
+        uint32_t there = 0;
+#pragma unroll
+        for (int m = 0; m < 8; ++m) there |= (pairs[m >> 1] & ((m & 1) != 0 ? 0x7fff0000u : 0x7fffu)) != 0u ? 1u << m : 0u;
+        return there;
     }
     const int32_t nb = (int32_t)pk_bytes_per_group(a, P.G);
     const uint8_t* const first = P.codes + base + lrow * nb;
@@ -199,6 +205,7 @@ __device__ __forceinline__ void half_rows(const PackArgs& P, int64_t r0, int64_t
         const float s = sc[i] * by, b = fmaf(-f0, s, a >= 5 ? 0.0f : be[i] * by);
         w[i] = half_weights(f[i], s, b);
     }
+    return 0;
 }
 
 template <typename HT>
@@ -208,17 +215,18 @@ __device__ __forceinline__ uint32_t half_bits(float x) {
 }
 
 // w_hat rounded to bfloat16 and turned: wt [cols][ld], zeros from the last row to K.  A thread has eight rows by eight columns.  In half precision (_Float16)
-// weights are multiplied by a power of two first, the same for an octet of columns.  PLAIN: so, with no mask and whole eights of rows.
+// weights are multiplied by a power of two first, the same for an octet of columns.  PLAIN: so, with no mask and whole eights of rows.  Comes back with a thread's columns that
+// have something other than 0 (PLAIN: not of codes).
 template <typename HT, bool PLAIN = false>
-__device__ __forceinline__ void turn(const PackArgs& P, int32_t K, int64_t ld, float by, uint16_t* __restrict__ wt, int64_t block) {
+__device__ __forceinline__ uint32_t turn(const PackArgs& P, int32_t K, int64_t ld, float by, uint16_t* __restrict__ wt, int64_t block) {
     __shared__ uint16_t trits_of[256];
     trits_of[threadIdx.x] = (uint16_t)trit_fields(threadIdx.x);
     __syncthreads();
     const int32_t row_blocks = (K + 255) / 256;
     const int64_t cb = block / row_blocks;
     const int64_t r0 = (block - cb * row_blocks) * 256 + (threadIdx.x & 31) * 8, col = cb * 64 + (threadIdx.x >> 5) * 8;
-    if (col >= P.cols || r0 >= K) return;
-    uint32_t v[8][4];
+    if (col >= P.cols || r0 >= K) return 0;
+    uint32_t v[8][4], there = 0;
     if constexpr (PLAIN) {
         uint4 w[8] = {};
         if (r0 < P.rows) {
@@ -227,7 +235,7 @@ __device__ __forceinline__ void turn(const PackArgs& P, int32_t K, int64_t ld, f
             const int64_t u = (int64_t)rb * P.n_chunks + j;
             int64_t base;
             const int a = pk_action(P, u, base);
-            half_rows<8>(P, r0, col, u, lrow, ((int)col - (int)j * P.G) >> 3, a, base, trits_of, by, w);
+            there = half_rows<8>(P, r0, col, u, lrow, ((int)col - (int)j * P.G) >> 3, a, base, trits_of, by, w);
         }
 #pragma unroll
         for (int m = 0; m < 8; ++m) {
@@ -239,14 +247,18 @@ __device__ __forceinline__ void turn(const PackArgs& P, int32_t K, int64_t ld, f
             }
             *reinterpret_cast<uint4*>(wt + (col + m) * ld + r0) = make_uint4(t[0], t[1], t[2], t[3]);
         }
-        return;
+        return there;
     }
     eight_rows(P, r0, col, trits_of, [&](int i, int m, float x) {
         const uint32_t b = half_bits<HT>(__is_same(HT, _Float16) ? x * by : x);
         v[m][i >> 1] = (i & 1) != 0 ? v[m][i >> 1] | b << 16 : b;
     });
 #pragma unroll
-    for (int m = 0; m < 8; ++m) *reinterpret_cast<uint4*>(wt + (col + m) * ld + r0) = make_uint4(v[m][0], v[m][1], v[m][2], v[m][3]);
+    for (int m = 0; m < 8; ++m) {
+        *reinterpret_cast<uint4*>(wt + (col + m) * ld + r0) = make_uint4(v[m][0], v[m][1], v[m][2], v[m][3]);
+        there |= ((v[m][0] | v[m][1] | v[m][2] | v[m][3]) & 0x7fff7fffu) != 0u ? 1u << m : 0u;
+    }
+    return there;
 }
 
 // The largest finite magnitude that the weights of a row's group can have, and the power of two that brings magnitudes up to `most` below 2^15 (1 where
@@ -266,7 +278,7 @@ __device__ __forceinline__ float group_lost(const PackArgs& P, int a, int64_t g,
     return top > 0.0f && top * by < HALF_GROUP ? fmaxf(fminf(top * by, 0x1p-25f), 0x1p-100f) * 0x1p25f : 0.0f;
 }
 // A row's group's part in the largest magnitude and in the smallest, weights that stay as they are counting 16 times: HALF_GROUP is 16 HALF_NORMAL.
-__device__ __forceinline__ void group_range(const PackArgs& P, int64_t row, int64_t j, float& most, float& least) {
+__device__ __forceinline__ void group_range(const PackArgs& P, int64_t row, int64_t j, float& most, float& least, bool& coded) {
     const int64_t rb = row / P.R_u, u = rb * P.n_chunks + j;
     int64_t base;
     const int a = pk_action(P, u, base);
@@ -286,6 +298,7 @@ __device__ __forceinline__ void group_range(const PackArgs& P, int64_t row, int6
     const float top = affine_top(P, a, u * P.R_u + row - rb * P.R_u);
     most = fmaxf(most, top);
     least = top > 0.0f ? fminf(least, top) : least;
+    coded |= top > 0.0f;
 }
 // Of eight rows from r0 on, those that rounding takes something from in an octet of columns.
 __device__ __forceinline__ int32_t rows_lost(const PackArgs& P, int64_t r0, int64_t col, float by) {

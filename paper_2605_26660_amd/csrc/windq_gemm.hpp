@@ -51,6 +51,7 @@ struct GemmArgs {
     int64_t ld_raw;
     // Of its way back: weights of an octet of columns that rounding has taken something from, by 2^-25 at most.
     const int32_t* lost_octet;
+    const uint32_t* there_octet;   // its columns that have something other than 0 where there are no codes or a mask lies over them: with no weight lost the others' results are 0
     AgainArgs again;
 };
 
@@ -88,6 +89,9 @@ __device__ __forceinline__ float half_lost(float x, float y) {
 // nothing to lose, the loss is far below 0, whatever the other side adds.
 __device__ __forceinline__ float with_loss(float power, float lost) { return __uint_as_float(__float_as_uint(power) | (__float_as_uint(lost) + 0xffffu) >> 16); }
 __device__ __forceinline__ float loss_in(float word) { return __uint_as_float(__float_as_uint(word) << 16); }
+// The bit above them: a chunk of columns with codes that stand for something other than 0.
+__device__ __forceinline__ float with_codes(float power, bool codes) { return __uint_as_float(__float_as_uint(power) | (codes ? 0x10000u : 0u)); }
+__device__ __forceinline__ bool has_codes(float word) { return (__float_as_uint(word) & 0x10000u) != 0u; }
 __device__ __forceinline__ float power_of_nothing() { return __uint_as_float(0x0000ff7fu); }
 
 // A kernel's first argument from where it lies, for what is seldom needed: the compiler would load all of it at the kernel's start, into more scalar registers than there are.
@@ -474,12 +478,13 @@ __global__ __launch_bounds__(GM_THREADS) void dx_gemm_kernel(const GemmArgs Q) {
                 if (c >= Q.cols) break;
                 const float low = below(by_token, octet0 + f * 4 + g);
                 const int by = exponent_of(by_token) + exponent_of(power_of(octet0 + f * 4 + g));
+                const uint32_t there = (has_codes(power_of(octet0 + f * 4 + g)) || A.lost_octet[c >> 3] != 0 ? 0xffu : A.there_octet[c >> 3]) >> (hh * 4);
                 float x[4];
                 bool again[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     x[i] = g == 0 ? v[i] : (g == 1 ? v[4 + i] : (g == 2 ? v[8 + i] : v[12 + i]));
-                    again[i] = fabsf(x[i]) < ldexpf(low, by) && t < Q.T;
+                    again[i] = fabsf(x[i]) < ldexpf(low, by) && t < Q.T && (there >> i & 1u) != 0u;
                 }
                 const uint64_t lanes = __ballot(again[0] || again[1] || again[2] || again[3]);
 #pragma unroll 1

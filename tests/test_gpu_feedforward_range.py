@@ -243,3 +243,43 @@ def test_code_streams_that_end_with_their_last_code(windq, shape, only):
     packed = [c.case.describe(windq, W=c.W, scale=c.scale, offset=c.offset, codes=c.case.codes[:end].clone()) for c in cs]
     want, off = gradients(cs, dh, g, u, "silu")
     close(windq.windq_gated_grad(packed[0], packed[1], dh, g, u)[0], want, off + 2.0 ** -133, BF)
+
+
+@pytest.mark.parametrize("shape,masked", WAYS)
+def test_columns_of_nothing(windq, shape, masked):
+    """Columns that are 0 in every row, beside others of their octet, where tokens have lost something: 0 as they are, and the others from what is there."""
+    rows, cols, G, _, T = shape
+    cs = pair(windq, shape, BF, masked=masked)
+    for c in cs:
+        bits = np.zeros((rows, cols), bool) if c.mask is None else (np.unpackbits(c.mask.cpu().numpy(), axis=1, bitorder="little")[:, :cols] == 1)
+        bits[:, 3::16] = True
+        c.mask = torch.from_numpy(np.packbits(bits, axis=1, bitorder="little")).to(DEV)
+        c.W = c.W.clone()
+        c.W[:, 3::16] = 0.0                                # in units that stay as they are
+        c.w, c.mag = c.w.copy(), c.mag.copy()
+        c.w[:, 3::16] = 0.0
+        c.mag[:, 3::16] = 0.0
+        c.packed = c.describe(windq)
+    dh, g, u = tokens(T, rows, BF, 6, 1e-3), tokens(T, rows, BF, 7, 2.0), tokens(T, rows, BF, 8, 1.5)
+    dh[:, 5] = 2.0 ** 40
+    want, off = gradients(cs, dh, g, u, "silu")
+    dx = windq.windq_gated_grad(cs[0].packed, cs[1].packed, dh, g, u)[0]
+    close(dx, want, off + 2.0 ** -133, BF)
+    assert torch.all(dx[:, 3::16] == 0.0)
+
+
+@pytest.mark.parametrize("shape", [WAYS[0][0], WAYS[2][0]])
+def test_columns_of_nothing_among_weights_that_stay_as_they_are(windq, shape):
+    rows, cols, G, _, T = shape
+    cs = [Case(windq, rows, cols, G, 0, BF, seed=k, only=0) for k in range(2)]
+    for c in cs:
+        c.W = c.W.clone()
+        c.W[:, 5::8] = 0.0
+        c.w, c.mag = c.W.double().cpu().numpy(), c.W.double().abs().cpu().numpy()
+        c.packed = c.describe(windq)
+    dh, g, u = tokens(T, rows, BF, 6, 1e-3), tokens(T, rows, BF, 7, 2.0), tokens(T, rows, BF, 8, 1.5)
+    dh[:, 5] = 2.0 ** 40
+    want, off = gradients(cs, dh, g, u, "silu")
+    dx = windq.windq_gated_grad(cs[0].packed, cs[1].packed, dh, g, u)[0]
+    close(dx, want, off + 2.0 ** -133, BF)
+    assert torch.all(dx[:, 5::8] == 0.0)
