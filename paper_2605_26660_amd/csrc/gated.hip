@@ -13,7 +13,7 @@ namespace windq {
 // Many bfloat16 tokens: the matrices are reconstructed in half precision, once a call, and multiplied by a plain product (windq_gemm.hpp).  Both factors have 11 bits of
 // significand, and powers of two for a token and for a row that bring them below 2^15, so that what lies 2^28 below the largest of them still has all of its
 // digits: the weights' rounding (tokens have none: bfloat16's eight bits fit) is eight times as fine as G's and U's own.
-// From 65 tokens on, unless the kernel for few tokens has them all in one round of workgroups: 11008 x 4096, 128 tokens 88 us (by it some 130), 64 tokens 87 and 67 by it; 4096 x 4096, 128 tokens
+// From 65 tokens on, unless the kernel for few tokens has them all in one round of workgroups: 11008 x 4096, 128 tokens 84 us (by it some 130), 64 tokens 83 and 69 by it; 4096 x 4096, 128 tokens
 // 57 and 38 by it (one round), 192 tokens 56 and 148; unpacking for every 128 tokens anew (as fp32 calls do) 118, 97 and 105.
 constexpr int64_t GATED_MANY = PROJECT_FEW;
 inline bool gated_few(const PackArgs& P, const PackArgs& up, int64_t T) {
@@ -361,7 +361,7 @@ int launch_gated_tiles(const ProjectArgs& Q, char* ws, const GatedWs& at, hipStr
 }
 
 // fp32: 16 rows by 16 tokens a workgroup up to so many tiles of 128 rows of both by 128 tokens, whose time is a round's until the CUs are full.  1024 x 4096, 300 tokens (24
-// tiles) 179 us, tiles some 490; 2048 x 2048, 300 tokens (48) 158 and 300, 1000 tokens (128) 472 and 300; 1024 x 4096, 1000 tokens (64) 520 and 493; 1000 x 1056, 1000 tokens (64)
+// tiles) 182 us (plans of all treatments alike), tiles some 490; 2048 x 2048, 300 tokens (48) 158 and 300, 1000 tokens (128) 472 and 300; 1024 x 4096, 1000 tokens (64) 520 and 493; 1000 x 1056, 1000 tokens (64)
 // 126 and 154; 4096 x 1024, 300 tokens (96) 211 and 164.
 constexpr int64_t PAIR_TILES = 64;
 
