@@ -826,7 +826,7 @@ int windq_gated8(const windq_serving* gate, const windq_serving* up, const windq
  * gate and up: of one shape, chunk_w, unit_rows and weight type; treatments and masks are their own.  At most 2^31 - 1 tokens x rows.
  * Workspace: windq_gated_workspace_bytes (256-byte aligned), written anew by every call.
  * In WINDQ_BF16 with rows a multiple of 8, and more than 64 tokens in more than 256 pieces of 32 rows by 64 tokens (or a mask, chunks other than 64, 96 and multiples of
- * 128, units not of whole 32s of rows, or codes_bytes no multiple of 16), weights enter the product in half precision: 11 bits, 2^-12 of a weight, each row and each token times a power of two of its own.  What lies
+ * 128, units not of whole 32s of rows, or codes_bytes no multiple of 16), weights enter the product in half precision: 11 bits, 2^-12 of a weight (or of codes 2^-15 of their group's largest), each row and each token times a power of two of its own.  What lies
  * 2^28 and more below the largest of its row or token loses digits, but results do not: one that this could change by 2^-10 of its value is formed again weight by weight, as
  * one that is not finite is.  Elsewhere no weight is rounded, so that a token may come out in other last bits from a larger batch.  No output may overlap another or an input.
  * Low-rank adapters of gate or up are windq_project's; dG and dU below are what their gradients (windq_project_grad with P NULL) start from.
@@ -840,7 +840,7 @@ int windq_gated(const windq_packed* gate /*HOST*/, const windq_packed* up /*HOST
  *   dH  [tokens][rows] (leading dimension >= rows, any); G, U of its type as windq_gated left them
  *   dX  [tokens][cols] of that type, ld_dx >= cols, or NULL: not wanted (then no workspace is either)
  *   dG, dU [tokens][rows] of that type, ld_d >= rows; both or neither, not NULL where dX is
- * dG and dU are formed in fp32 and rounded once on their way out.  In WINDQ_BF16 they and the weights enter dX's product in half precision: 11 bits, 2^-12 of a value, each token
+ * dG and dU are formed in fp32 and rounded once on their way out.  In WINDQ_BF16 they and the weights enter dX's product in half precision: 11 bits, 2^-12 of a value (or of codes 2^-15 of their group's largest), each token
  * (its dG and dU) and each chunk (of both matrices) times a power of two of its own.  What lies 2^28 and more below the largest of its token or chunk loses digits, but results
  * do not: a value of dX that this could change by 2^-10 of it is formed again weight by weight.  In WINDQ_F32 neither is rounded.  Sums are fp32 in a fixed
  * order: results are bit-reproducible.  A token that holds something not finite, or a weight that is not, makes what the formula multiplies it with not finite (infinities may come
