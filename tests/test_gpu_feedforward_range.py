@@ -283,3 +283,33 @@ def test_columns_of_nothing_among_weights_that_stay_as_they_are(windq, shape):
     dx = windq.windq_gated_grad(cs[0].packed, cs[1].packed, dh, g, u)[0]
     close(dx, want, off + 2.0 ** -133, BF)
     assert torch.all(dx[:, 5::8] == 0.0)
+
+
+@pytest.mark.parametrize("shape,masked", WAYS)
+def test_what_is_formed_again_repeats_itself(windq, shape, masked):
+    """Whatever lay in the workspace, eagerly and from a graph."""
+    rows, cols, G, _, T = shape
+    cs = [scaled(windq, c, groups={(7, 1): 2.0 ** 45, (5, 1): 0.0}) for c in pair(windq, shape, BF, masked=masked)]
+    p = [c.packed for c in cs]
+    x, dh, g, u = tokens(T, cols, BF, 4), tokens(T, rows, BF, 6, 1e-3), tokens(T, rows, BF, 7, 8.0), tokens(T, rows, BF, 8, 1.5)
+    x[::2, G:2 * G], dh[::2, 7], u[1::4, 5] = 0.0, 0.0, 2.0 ** 50
+    ws, ws_grad = windq.gated_workspace(*p, x), windq.gated_workspace(*p, dh, grad=True)
+    outs = [torch.empty(T, rows, dtype=BF, device=DEV), torch.empty(T, cols, dtype=BF, device=DEV), *(torch.empty(T, rows, dtype=BF, device=DEV) for _ in range(2))]
+
+    def run():
+        windq.windq_gated(*p, x, "gelu", ws=ws, out=outs[0])
+        windq.windq_gated_grad(*p, dh, g, u, "gelu", ws=ws_grad, outs=tuple(outs[1:]))
+
+    run()
+    want = [t.clone() for t in outs]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for k in range(4):
+        ws.fill_((255, 0, 127, 1)[k]), ws_grad.fill_((255, 0, 127, 1)[k])
+        run() if k % 2 else graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), k
+        for t in outs:
+            t.fill_(3.0)
